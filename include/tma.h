@@ -48,7 +48,8 @@ typedef enum {
 } tma_status;
 
 typedef enum { TMA_F32 = 0, TMA_BF16 = 1 } tma_dtype;
-typedef enum { TMA_ACT_NONE = 0, TMA_ACT_RELU = 1 } tma_act;
+/* PRELU and SILU: tma_groupnorm_act_* alone takes them. */
+typedef enum { TMA_ACT_NONE = 0, TMA_ACT_RELU = 1, TMA_ACT_PRELU = 2, TMA_ACT_SILU = 3 } tma_act;
 
 /* Library version as major*10000 + minor*100 + patch. */
 int tma_version(void);
@@ -600,6 +601,116 @@ int tma_gcn_block_bwd(int64_t n_dst, int64_t n_src, int64_t max_entries,
                       int64_t ld_next, const float *W, int32_t F_in, int32_t F_out,
                       int32_t act, int32_t dtype, float *dW, float *dbias,
                       void *dH_out, int64_t ldh, void *ws, size_t ws_bytes, tma_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Layers of nodes that are of several kinds (node types, experts): rows by
+ * group, a dense layer with weights per group, group norm with an activation,
+ * dropout.  All pointers device memory; ordered on `stream`; no allocation, no
+ * host wait, nothing cleared by a memset (the calls may be captured); fixed
+ * summation orders, no atomics.
+ *
+ * tma_group_rows: a stable counting sort of n row numbers by group[v].
+ * offsets_out [E+1]: offsets_out[g] = number of rows with an id in [0, g);
+ * order_out [n]: the rows of group 0, of group 1, ..., ascending in each.  Rows
+ * with an id outside [0, E) are in no group; order_out from offsets_out[E] on
+ * is left alone.  1 <= E <= 1024.  Workspace:
+ * tma_group_rows_workspace_bytes(n, E), 256-byte aligned.
+ * ---------------------------------------------------------------------- */
+size_t tma_group_rows_workspace_bytes(int64_t n, int32_t E);
+
+int tma_group_rows(int64_t n, const int32_t *group, int32_t E, int32_t *offsets_out, int32_t *order_out,
+                   void *ws, size_t ws_bytes, tma_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * tma_grouped_dense_fwd / _bwd: tma_dense_* with weights per group of rows.
+ *     Y[v] = act(X[v] W[g] + b[g]);   dZ = dY (.) act'(Y);   dX[v] = dZ[v] W[g]^T
+ *     dW[g] = sum of X[v]^T dZ[v],  dbias[g] = sum of dZ[v], over g's rows
+ *   offsets [E+1], order [n] or NULL as tma_group_rows writes them: group g has
+ *   the positions [offsets[g], offsets[g+1]) of the list, position i is row
+ *   order[i] (order NULL: row i) of X, Y, dY and dX.  Each row is listed at most
+ *   once; rows that are not listed (n counts all) are neither read nor written.
+ *   Groups may be empty: their dW and dbias are zero.
+ *   X [n, F_in], Y, dY [n, F_out], dX_out [n, F_in] of dtype with leading
+ *   dimensions ldx, ldy (Y and dY), ld_dx; dX_out NULL: not wanted, and it is
+ *   none of the inputs.  W [E, F_in, F_out] fp32, bias [E, F_out] fp32 or NULL;
+ *   dW [E, F_in, F_out], dbias [E, F_out] (or NULL) fp32 OVERWRITTEN.
+ *   act: TMA_ACT_NONE or TMA_ACT_RELU (Y is read by the backward only then).
+ *   Widths up to 65536, 1 <= E <= 1024.
+ * Workspaces, 256-byte aligned: tma_grouped_dense_fwd_workspace_bytes(n, E,
+ * F_in, F_out, dtype), tma_grouped_dense_bwd_workspace_bytes(..., dX_out != NULL).
+ * ---------------------------------------------------------------------- */
+size_t tma_grouped_dense_fwd_workspace_bytes(int64_t n, int32_t E, int32_t F_in, int32_t F_out, int32_t dtype);
+
+int tma_grouped_dense_fwd(int64_t n, int32_t E, const int32_t *offsets, const int32_t *order, const void *X, int64_t ldx,
+                          int32_t F_in, const float *W, const float *bias, int32_t F_out, int32_t act, int32_t dtype,
+                          void *Y_out, int64_t ldy, void *ws, size_t ws_bytes, tma_stream_t stream);
+
+size_t tma_grouped_dense_bwd_workspace_bytes(int64_t n, int32_t E, int32_t F_in, int32_t F_out, int32_t dtype,
+                                             int32_t need_dX);
+
+int tma_grouped_dense_bwd(int64_t n, int32_t E, const int32_t *offsets, const int32_t *order, const void *X, int64_t ldx,
+                          const void *Y, const void *dY, int64_t ldy, const float *W, int32_t F_in, int32_t F_out,
+                          int32_t act, int32_t dtype, float *dW, float *dbias, void *dX_out, int64_t ld_dx,
+                          void *ws, size_t ws_bytes, tma_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * tma_groupnorm_act_fwd / _bwd: group norm, channels last, then an activation.
+ * The F channels of a row form G groups of F / G neighbours (at most 1024
+ * each); mean and biased variance are taken per (segment of rows, group):
+ *     Xh = (X - mean) / sqrt(var + eps),  Y = act(gamma (.) Xh + beta)
+ *   segments != NULL: segment s is the rows [segments[s], segments[s+1]), int32
+ *     [n_segments + 1], non-decreasing, within [0, n]; segments may be empty,
+ *     and rows outside all of them are neither read nor written.
+ *   segments == NULL: runs of rows_per_segment rows, which divides n
+ *     (n_segments is not read); with rows_per_segment = 1 each row is normalised
+ *     by itself (G = 1: layer normalisation).
+ *   act: TMA_ACT_NONE, _RELU, _PRELU (slope: one fp32 value in device memory,
+ *     as for tma_layernorm_prelu_*; else slope may be NULL), _SILU.
+ *   gamma, beta [F] fp32; X, Y, dY, dX [n, F] of dtype with their own leading
+ *     dimensions.  Y_out and dX_out are not X; dX_out may be dY.
+ *   stats_out [n_segments, G, 2] fp32, 8-byte aligned, or NULL: mean and
+ *     1 / sqrt(var + eps), zeros for an empty segment; the backward's `stats`.
+ *     Neither written nor read where rows are normalised by themselves.
+ *   dgamma, dbeta [F], dslope [1] fp32 OVERWRITTEN (dslope NULL unless PReLU).
+ * Workspaces, 256-byte aligned: tma_groupnorm_act_fwd_workspace_bytes(n, F, G,
+ * n_segments, dtype) (none where rows are normalised by themselves, ws may then
+ * be NULL) and tma_groupnorm_act_bwd_workspace_bytes (for n_segments = 1 it is
+ * enough where rows are normalised by themselves).
+ * ---------------------------------------------------------------------- */
+size_t tma_groupnorm_act_fwd_workspace_bytes(int64_t n, int32_t F, int32_t G, int64_t n_segments, int32_t dtype);
+
+int tma_groupnorm_act_fwd(int64_t n, int32_t F, int32_t G, int64_t n_segments, const int32_t *segments,
+                          int64_t rows_per_segment, const void *X, int64_t ldx, const float *gamma, const float *beta,
+                          const float *slope, float eps, int32_t act, int32_t dtype, void *Y_out, int64_t ldy,
+                          float *stats_out, void *ws, size_t ws_bytes, tma_stream_t stream);
+
+size_t tma_groupnorm_act_bwd_workspace_bytes(int64_t n, int32_t F, int32_t G, int64_t n_segments, int32_t dtype);
+
+int tma_groupnorm_act_bwd(int64_t n, int32_t F, int32_t G, int64_t n_segments, const int32_t *segments,
+                          int64_t rows_per_segment, const void *X, int64_t ldx, const void *dY, int64_t ldd,
+                          const float *gamma, const float *beta, const float *slope, float eps, int32_t act, int32_t dtype,
+                          const float *stats, void *dX_out, int64_t ld_dx, float *dgamma, float *dbeta, float *dslope,
+                          void *ws, size_t ws_bytes, tma_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * tma_dropout_fwd / _bwd: dropout whose mask is never stored.  Element (v, c)
+ * of an [n, F] matrix takes 16 bits of the generator of tma_partition:
+ *     z = SplitMix64(s, (first_row + v) * ceil(F / 4) + floor(c / 4)),
+ *     field = bits [16 (c mod 4), 16 (c mod 4) + 16) of z,
+ *     Y = field >= T ? X * 65536 / (65536 - T) : 0,     T = floor(65536 p + 1/2)
+ * (p in [0, 1] is taken in steps of 2^-16, the scale is that of p as taken; a
+ * dropped element is 0 whatever it was).  s = seed, or, with d_step (one int64
+ * in device memory, 8-byte aligned), s = SplitMix64(seed, *d_step): a captured
+ * graph whose step counter advances draws other elements at every replay.
+ * first_row: number of the first row, for matrices that go through in blocks.
+ * The backward applies the same mask and scale to dY.  Input and output have
+ * leading dimensions of their own and may be one buffer (then equal ones).
+ * ---------------------------------------------------------------------- */
+int tma_dropout_fwd(int64_t n, int32_t F, const void *X, int64_t ldx, double p, uint64_t seed, const int64_t *d_step,
+                    int64_t first_row, int32_t dtype, void *Y_out, int64_t ldy, tma_stream_t stream);
+
+int tma_dropout_bwd(int64_t n, int32_t F, const void *dY, int64_t ldy, double p, uint64_t seed, const int64_t *d_step,
+                    int64_t first_row, int32_t dtype, void *dX_out, int64_t ldx, tma_stream_t stream);
 
 /* ------------------------------------------------------------------------
  * Losses on the last layer's output.

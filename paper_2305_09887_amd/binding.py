@@ -16,7 +16,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.environ.get("TMA_LIBRARY_PATH") or os.path.join(_PKG, "libtma.so")   # (a build elsewhere: set TMA_LIBRARY_PATH)
 
 TMA_F32, TMA_BF16 = 0, 1
-TMA_ACT_NONE, TMA_ACT_RELU = 0, 1
+TMA_ACT_NONE, TMA_ACT_RELU, TMA_ACT_PRELU, TMA_ACT_SILU = 0, 1, 2, 3      # the last two: tma_groupnorm_act_* alone
 
 EXPORTS = (
     "tma_version", "tma_last_error", "tma_partition", "tma_mix64",
@@ -37,6 +37,11 @@ EXPORTS = (
     "tma_sage_weights_bf16_bytes", "tma_sage_prepare_weights_bf16", "tma_sage_layer_fwd_prepared",
     "tma_block_inv_deg", "tma_sage_block_fwd", "tma_sage_block_bwd_workspace_bytes", "tma_sage_block_bwd",
     "tma_gcn_block_norm", "tma_gcn_block_fwd", "tma_gcn_block_bwd_workspace_bytes", "tma_gcn_block_bwd",
+    "tma_group_rows_workspace_bytes", "tma_group_rows",
+    "tma_grouped_dense_fwd_workspace_bytes", "tma_grouped_dense_fwd", "tma_grouped_dense_bwd_workspace_bytes",
+    "tma_grouped_dense_bwd",
+    "tma_groupnorm_act_fwd_workspace_bytes", "tma_groupnorm_act_fwd", "tma_groupnorm_act_bwd_workspace_bytes",
+    "tma_groupnorm_act_bwd", "tma_dropout_fwd", "tma_dropout_bwd",
     "tma_loss_workspace_bytes", "tma_softmax_ce", "tma_sigmoid_l2", "tma_sgd_step", "tma_adam_step", "tma_average",
     "tma_gather_rows", "tma_profile_begin", "tma_profile_end", "tma_profile_count", "tma_profile_entry",
     "tma_profile_sequence_count", "tma_profile_sequence_entry",
@@ -65,7 +70,9 @@ def lib() -> C.CDLL:
                      "tma_pair_product_bwd_workspace_bytes", "tma_prelu_bwd_workspace_bytes",
                      "tma_bce_logits_workspace_bytes", "tma_neighbor_sample_workspace_bytes",
                      "tma_mfg_relabel_workspace_bytes", "tma_sage_block_bwd_workspace_bytes",
-                     "tma_gcn_block_bwd_workspace_bytes", "tma_sage_weights_bf16_bytes"):
+                     "tma_gcn_block_bwd_workspace_bytes", "tma_sage_weights_bf16_bytes", "tma_group_rows_workspace_bytes",
+                     "tma_grouped_dense_fwd_workspace_bytes", "tma_grouped_dense_bwd_workspace_bytes",
+                     "tma_groupnorm_act_fwd_workspace_bytes", "tma_groupnorm_act_bwd_workspace_bytes"):
             getattr(L, name).restype = C.c_size_t
         L.tma_mix64.restype = C.c_uint64
         L.tma_mix64.argtypes = [C.c_uint64, C.c_uint64]
@@ -871,6 +878,248 @@ def tma_gcn_block_bwd(n_dst: int, n_src: int, max_entries: int, blk_rowptr, blk_
         C.c_void_p(dH_out.data_ptr() if dH_out is not None else 0), C.c_int64(ldh), _ptr(ws), C.c_size_t(ws.numel()),
         _stream(stream)))
     return dH_out
+
+
+# ---------------------------------------------------------------------------
+def _device(where, *tensors):
+    """The device that the tensors share; they may be None."""
+    devices = {t.device for t in tensors if t is not None}
+    if len(devices) != 1 or next(iter(devices)).type != "cuda":
+        raise TmaError(f"{where}: expected tensors on one CUDA/HIP device")
+    return next(iter(devices))
+
+
+def _launch(device, stream, call, *args):
+    """call(*args, stream) with the tensors' device as the current one (the library launches on that) and, where none is
+    given, that device's current stream."""
+    with torch.cuda.device(device):
+        _check(call(*args, _stream(stream)))
+
+
+def _rows_like(t, name, shape, dtype, device):
+    """A [rows, cols] tensor of the given shape and type with unit inner stride: its leading dimension."""
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device:
+        raise TmaError(f"{name}: expected {tuple(shape)} of {dtype} on {device}")
+    ld = _rows_ld(t, name)[2]
+    if ld < shape[1]:
+        raise TmaError(f"{name}: rows overlap")
+    return ld
+
+
+def _vector(t, name, shape, dtype, device):
+    """A dense tensor of the given shape and type."""
+    if tuple(t.shape) != tuple(shape) or t.device != device:
+        raise TmaError(f"{name}: expected shape {tuple(shape)} on {device}")
+    return _ptr(t, dtype, name)
+
+
+def tma_group_rows_workspace_bytes(n: int, E: int) -> int:
+    return int(lib().tma_group_rows_workspace_bytes(C.c_int64(n), C.c_int32(E)))
+
+
+def tma_group_rows(group, E: int, offsets_out=None, order_out=None, ws=None, stream=None):
+    """Rows by group, stable: (offsets [E+1], order [n], int32).  Rows with an id outside [0, E) are in no group; `order`
+    from offsets[E] on is left alone."""
+    dev = _device("tma_group_rows", group, offsets_out, order_out, ws)
+    if group.dim() != 1:
+        raise TmaError("tma_group_rows: group must be one-dimensional")
+    n = group.numel()
+    if offsets_out is None:
+        offsets_out = _record(torch.empty(max(E, 0) + 1, dtype=torch.int32, device=dev), stream)
+    if order_out is None:
+        order_out = _record(torch.empty(n, dtype=torch.int32, device=dev), stream)
+    if ws is None:
+        ws = _workspace(tma_group_rows_workspace_bytes(n, E), dev, stream)
+    _launch(dev, stream, lib().tma_group_rows, C.c_int64(n), _ptr(group, torch.int32, "group"), C.c_int32(E),
+            _vector(offsets_out, "offsets_out", (E + 1,), torch.int32, dev), _vector(order_out, "order_out", (n,), torch.int32, dev),
+            _ptr(ws), C.c_size_t(ws.numel() * ws.element_size()))
+    return offsets_out, order_out
+
+
+def tma_grouped_dense_fwd_workspace_bytes(n: int, E: int, F_in: int, F_out: int, dtype: int) -> int:
+    return int(lib().tma_grouped_dense_fwd_workspace_bytes(C.c_int64(n), C.c_int32(E), C.c_int32(F_in), C.c_int32(F_out),
+                                                           C.c_int32(dtype)))
+
+
+def tma_grouped_dense_fwd(X, W, bias, offsets, act: int, order=None, Y_out=None, ws=None, stream=None):
+    """Y[v] = act(X[v] W[g] + b[g]) for the rows v of each group g, as tma_group_rows lists them (order None: the rows lie
+    group by group); W [E, F_in, F_out], bias [E, F_out] or None.  Rows of no group are left alone."""
+    dev = _device("tma_grouped_dense_fwd", X, W, bias, offsets, order, Y_out, ws)
+    n, F_in, ldx = _rows_ld(X, "X")
+    if W.dim() != 3 or W.shape[1] != F_in:
+        raise TmaError("tma_grouped_dense_fwd: W must be [E, F_in, F_out]")
+    E, _, F_out = W.shape
+    if Y_out is None:
+        Y_out = _record(_padded(n, F_out, X.dtype, dev), stream)
+    if ws is None:
+        ws = _workspace(tma_grouped_dense_fwd_workspace_bytes(n, E, F_in, F_out, _feat_dtype(X)), dev, stream)
+    _launch(dev, stream, lib().tma_grouped_dense_fwd, C.c_int64(n), C.c_int32(E),
+            _vector(offsets, "offsets", (E + 1,), torch.int32, dev),
+            _vector(order, "order", (n,), torch.int32, dev) if order is not None else C.c_void_p(0),
+            C.c_void_p(X.data_ptr()), C.c_int64(_rows_like(X, "X", (n, F_in), X.dtype, dev)), C.c_int32(F_in),
+            _ptr(W, torch.float32, "W"),
+            _vector(bias, "bias", (E, F_out), torch.float32, dev) if bias is not None else C.c_void_p(0), C.c_int32(F_out),
+            C.c_int32(act), C.c_int32(_feat_dtype(X)), C.c_void_p(Y_out.data_ptr()),
+            C.c_int64(_rows_like(Y_out, "Y_out", (n, F_out), X.dtype, dev)), _ptr(ws),
+            C.c_size_t(ws.numel() * ws.element_size()))
+    return Y_out
+
+
+def tma_grouped_dense_bwd_workspace_bytes(n: int, E: int, F_in: int, F_out: int, dtype: int, need_dX: bool = True) -> int:
+    return int(lib().tma_grouped_dense_bwd_workspace_bytes(C.c_int64(n), C.c_int32(E), C.c_int32(F_in), C.c_int32(F_out),
+                                                           C.c_int32(dtype), C.c_int32(1 if need_dX else 0)))
+
+
+def tma_grouped_dense_bwd(X, Y, dY, W, offsets, act: int, order=None, dW=None, dbias=None, dX_out=None, need_dbias=True,
+                          need_dX=True, ws=None, stream=None):
+    """Returns (dW, dbias or None, dX or None); Y (the forward result) is read with ReLU only and may else be None."""
+    dev = _device("tma_grouped_dense_bwd", X, Y, dY, W, offsets, order, dW, dbias, dX_out, ws)
+    n, F_in, _ = _rows_ld(X, "X")
+    if W.dim() != 3 or W.shape[1] != F_in:
+        raise TmaError("tma_grouped_dense_bwd: W must be [E, F_in, F_out]")
+    E, _, F_out = W.shape
+    ldy = _rows_like(dY, "dY", (n, F_out), X.dtype, dev)
+    if act == TMA_ACT_RELU:
+        if Y is None:
+            raise TmaError("tma_grouped_dense_bwd: Y is required with ReLU")
+        _rows_like(Y, "Y", (n, F_out), X.dtype, dev)
+        _same_ld(Y, dY, "tma_grouped_dense_bwd: Y / dY")
+    if dW is None:
+        dW = _record(torch.empty((E, F_in, F_out), dtype=torch.float32, device=dev), stream)
+    if need_dbias and dbias is None:
+        dbias = _record(torch.empty((E, F_out), dtype=torch.float32, device=dev), stream)
+    if not need_dbias:
+        dbias = None
+    if need_dX and dX_out is None:
+        dX_out = _record(_padded(n, F_in, X.dtype, dev), stream)
+    if not need_dX:
+        dX_out = None
+    ld_dx = _rows_like(dX_out, "dX_out", (n, F_in), X.dtype, dev) if dX_out is not None else F_in
+    if ws is None:
+        ws = _workspace(tma_grouped_dense_bwd_workspace_bytes(n, E, F_in, F_out, _feat_dtype(X), need_dX), dev, stream)
+    _launch(dev, stream, lib().tma_grouped_dense_bwd, C.c_int64(n), C.c_int32(E),
+            _vector(offsets, "offsets", (E + 1,), torch.int32, dev),
+            _vector(order, "order", (n,), torch.int32, dev) if order is not None else C.c_void_p(0),
+            C.c_void_p(X.data_ptr()), C.c_int64(_rows_like(X, "X", (n, F_in), X.dtype, dev)),
+            C.c_void_p(Y.data_ptr() if Y is not None else 0), C.c_void_p(dY.data_ptr()), C.c_int64(ldy),
+            _ptr(W, torch.float32, "W"), C.c_int32(F_in), C.c_int32(F_out), C.c_int32(act), C.c_int32(_feat_dtype(X)),
+            _vector(dW, "dW", (E, F_in, F_out), torch.float32, dev),
+            _vector(dbias, "dbias", (E, F_out), torch.float32, dev) if dbias is not None else C.c_void_p(0),
+            C.c_void_p(dX_out.data_ptr() if dX_out is not None else 0), C.c_int64(ld_dx), _ptr(ws),
+            C.c_size_t(ws.numel() * ws.element_size()))
+    return dW, dbias, dX_out
+
+
+def _norm_segments(where, n, segments, rows_per_segment, dev):
+    """(number of segments, the offsets' pointer, rows of a run, whether rows are normalised by themselves)"""
+    if segments is not None:
+        if segments.dim() != 1 or segments.numel() < 2:
+            raise TmaError(f"{where}: segments must be offsets of at least one segment")
+        return segments.numel() - 1, _ptr(segments, torch.int32, "segments"), 0, False
+    R = int(rows_per_segment)
+    if R < 1 or n % R:
+        raise TmaError(f"{where}: {n} rows are no runs of {R}")
+    return n // R, C.c_void_p(0), R, R == 1
+
+
+def tma_groupnorm_act_fwd_workspace_bytes(n: int, F: int, G: int, n_segments: int, dtype: int) -> int:
+    return int(lib().tma_groupnorm_act_fwd_workspace_bytes(C.c_int64(n), C.c_int32(F), C.c_int32(G), C.c_int64(n_segments),
+                                                           C.c_int32(dtype)))
+
+
+def tma_groupnorm_act_fwd(X, G: int, gamma, beta, act: int = TMA_ACT_NONE, slope=None, segments=None, rows_per_segment: int = 1,
+                          eps: float = 1e-5, out=None, stats_out=None, need_stats=True, ws=None, stream=None):
+    """Group norm of G groups of channels, then `act` (TMA_ACT_NONE, _RELU, _PRELU with slope, _SILU): (Y, stats).  Statistics
+    per row (rows_per_segment 1; stats is None), per run of rows_per_segment rows, or per range of the int32 offsets
+    `segments`; stats [segments, G, 2] (mean, 1 / sqrt(var + eps)) is what the backward call takes."""
+    dev = _device("tma_groupnorm_act_fwd", X, gamma, beta, slope, segments, out, stats_out, ws)
+    n, F, _ = _rows_ld(X, "X")
+    S, seg, R, single = _norm_segments("tma_groupnorm_act_fwd", n, segments, rows_per_segment, dev)
+    if act == TMA_ACT_PRELU and slope is None:
+        raise TmaError("tma_groupnorm_act_fwd: PReLU needs a slope")
+    if out is None:
+        out = _record(_padded(n, F, X.dtype, dev), stream)
+    if single:
+        stats_out = None
+    elif need_stats and stats_out is None:
+        stats_out = _record(torch.empty((S, G, 2), dtype=torch.float32, device=dev), stream)
+    if ws is None and not single:
+        ws = _workspace(tma_groupnorm_act_fwd_workspace_bytes(n, F, G, S, _feat_dtype(X)), dev, stream)
+    _launch(dev, stream, lib().tma_groupnorm_act_fwd, C.c_int64(n), C.c_int32(F), C.c_int32(G), C.c_int64(S), seg, C.c_int64(R),
+            C.c_void_p(X.data_ptr()), C.c_int64(_rows_like(X, "X", (n, F), X.dtype, dev)),
+            _vector(gamma, "gamma", (F,), torch.float32, dev), _vector(beta, "beta", (F,), torch.float32, dev),
+            _vector(slope, "slope", (1,), torch.float32, dev) if slope is not None else C.c_void_p(0), C.c_float(eps),
+            C.c_int32(act), C.c_int32(_feat_dtype(X)), C.c_void_p(out.data_ptr()),
+            C.c_int64(_rows_like(out, "out", (n, F), X.dtype, dev)),
+            _vector(stats_out, "stats_out", (S, G, 2), torch.float32, dev) if stats_out is not None else C.c_void_p(0),
+            _ptr(ws), C.c_size_t(ws.numel() * ws.element_size() if ws is not None else 0))
+    return out, stats_out
+
+
+def tma_groupnorm_act_bwd_workspace_bytes(n: int, F: int, G: int, n_segments: int, dtype: int) -> int:
+    return int(lib().tma_groupnorm_act_bwd_workspace_bytes(C.c_int64(n), C.c_int32(F), C.c_int32(G), C.c_int64(n_segments),
+                                                           C.c_int32(dtype)))
+
+
+def tma_groupnorm_act_bwd(X, dY, G: int, gamma, beta, act: int = TMA_ACT_NONE, slope=None, segments=None,
+                          rows_per_segment: int = 1, eps: float = 1e-5, stats=None, dX_out=None, dgamma=None, dbeta=None,
+                          dslope=None, ws=None, stream=None):
+    """Returns (dX, dgamma, dbeta, dslope or None); stats as the forward call returned it; dX_out may be dY."""
+    dev = _device("tma_groupnorm_act_bwd", X, dY, gamma, beta, slope, segments, stats, dX_out, dgamma, dbeta, dslope, ws)
+    n, F, _ = _rows_ld(X, "X")
+    S, seg, R, single = _norm_segments("tma_groupnorm_act_bwd", n, segments, rows_per_segment, dev)
+    if act == TMA_ACT_PRELU and slope is None:
+        raise TmaError("tma_groupnorm_act_bwd: PReLU needs a slope")
+    if not single and stats is None:
+        raise TmaError("tma_groupnorm_act_bwd: stats of the forward call are required")
+    if dX_out is None:
+        dX_out = _record(_padded(n, F, X.dtype, dev), stream)
+    if dgamma is None:
+        dgamma = _record(torch.empty(F, dtype=torch.float32, device=dev), stream)
+    if dbeta is None:
+        dbeta = _record(torch.empty(F, dtype=torch.float32, device=dev), stream)
+    if act != TMA_ACT_PRELU:
+        dslope = None
+    elif dslope is None:
+        dslope = _record(torch.empty(1, dtype=torch.float32, device=dev), stream)
+    if ws is None:
+        ws = _workspace(tma_groupnorm_act_bwd_workspace_bytes(n, F, G, 1 if single else max(S, 1), _feat_dtype(X)), dev, stream)
+    _launch(dev, stream, lib().tma_groupnorm_act_bwd, C.c_int64(n), C.c_int32(F), C.c_int32(G), C.c_int64(S), seg, C.c_int64(R),
+            C.c_void_p(X.data_ptr()), C.c_int64(_rows_like(X, "X", (n, F), X.dtype, dev)),
+            C.c_void_p(dY.data_ptr()), C.c_int64(_rows_like(dY, "dY", (n, F), X.dtype, dev)),
+            _vector(gamma, "gamma", (F,), torch.float32, dev), _vector(beta, "beta", (F,), torch.float32, dev),
+            _vector(slope, "slope", (1,), torch.float32, dev) if slope is not None else C.c_void_p(0), C.c_float(eps),
+            C.c_int32(act), C.c_int32(_feat_dtype(X)),
+            _vector(stats, "stats", (S, G, 2), torch.float32, dev) if not single else C.c_void_p(0),
+            C.c_void_p(dX_out.data_ptr()), C.c_int64(_rows_like(dX_out, "dX_out", (n, F), X.dtype, dev)),
+            _vector(dgamma, "dgamma", (F,), torch.float32, dev), _vector(dbeta, "dbeta", (F,), torch.float32, dev),
+            _vector(dslope, "dslope", (1,), torch.float32, dev) if dslope is not None else C.c_void_p(0), _ptr(ws),
+            C.c_size_t(ws.numel() * ws.element_size()))
+    return dX_out, dgamma, dbeta, dslope
+
+
+def _dropout(where, call, X, p, seed, step, first_row, out, stream):
+    dev = _device(where, X, step, out)
+    n, F, _ = _rows_ld(X, "X")
+    if out is None:
+        out = _record(_padded(n, F, X.dtype, dev), stream)
+    _launch(dev, stream, call, C.c_int64(n), C.c_int32(F), C.c_void_p(X.data_ptr()),
+            C.c_int64(_rows_like(X, "X", (n, F), X.dtype, dev)), C.c_double(p), C.c_uint64(int(seed) & ((1 << 64) - 1)),
+            _vector(step, "step", (1,), torch.int64, dev) if step is not None else C.c_void_p(0), C.c_int64(int(first_row)),
+            C.c_int32(_feat_dtype(X)), C.c_void_p(out.data_ptr()),
+            C.c_int64(_rows_like(out, "out", (n, F), X.dtype, dev)))
+    return out
+
+
+def tma_dropout_fwd(X, p: float, seed: int, step=None, first_row: int = 0, out=None, stream=None):
+    """Dropout of the rows' elements with probability p; the mask is a function of (seed, the int64 `step` in device memory,
+    first_row + row, column) and stored nowhere.  out may be X."""
+    return _dropout("tma_dropout_fwd", lib().tma_dropout_fwd, X, p, seed, step, first_row, out, stream)
+
+
+def tma_dropout_bwd(dY, p: float, seed: int, step=None, first_row: int = 0, out=None, stream=None):
+    """dX of tma_dropout_fwd with the same arguments.  out may be dY."""
+    return _dropout("tma_dropout_bwd", lib().tma_dropout_bwd, dY, p, seed, step, first_row, out, stream)
 
 
 def tma_loss_workspace_bytes(n: int, Cc: int) -> int:

@@ -1,0 +1,201 @@
+// Rows by group: a stable counting sort of row numbers by a small id,
+//   offsets[g] = #{ v : 0 <= id_v < g },   order[offsets[g] + i] = the i-th row of group g in ascending row number.
+// Rows whose id is outside [0, E) are in no group.  Memory bound: reads the ids, writes the order (8 bytes a row).
+//
+// A wavefront ranks 64 consecutive rows at once: the lanes with the same id are found with one ballot per bit of the id, a
+// row's rank among them is the number of such lanes below its own, and a counter per (wavefront, group) in LDS carries the
+// rank on to the next 64 rows.  Integers throughout, every position has one writer: no atomics, one result.
+// Up to kOneBlockRows rows one block does it all (counts, their prefix, positions; measured below); above that
+// tiles of rows are counted, the counts [group][tile] are prefixed, and the tiles are ranked again from their bases.
+#include "kernels.hpp"
+
+namespace tma {
+
+constexpr int kMaxGroups = 1024;
+constexpr int kOneBlockRows = 16384;
+constexpr int kOneThreads = 1024;
+constexpr int kOneGroups = 512;                                   // 32 KB of counters, and a thread for each
+constexpr int kTileThreads = 256;
+constexpr int kTileChunks = 16;                                   // 64-row chunks of a wavefront of a tile
+constexpr int kTileRows = kTileThreads * kTileChunks;
+
+// the lanes that hold the same id as this one; `bits`: of the largest id
+__device__ __forceinline__ uint64_t same_id(int id, bool in, int bits)
+{
+    uint64_t m = __ballot(in);
+    for (int b = 0; b < bits; ++b) {
+        const uint64_t set = __ballot((id >> b) & 1);
+        m &= (id >> b) & 1 ? set : ~set;
+    }
+    return m;
+}
+
+__device__ __forceinline__ int below(uint64_t m, int lane) { return __popcll(m & ((uint64_t(1) << lane) - 1)); }
+
+// one chunk of 64 rows: rank in the wavefront's own counters, which are left advanced (a wavefront's LDS operations complete
+// in order; the fences keep the compiler from moving them)
+__device__ __forceinline__ int take(volatile int32_t *counters, int id, bool in, int bits, int lane)
+{
+    const uint64_t m = same_id(id, in, bits);
+    const int rank = below(m, lane);
+    int pos = 0;
+    if (in) pos = counters[id] + rank;
+    __builtin_amdgcn_wave_barrier();
+    if (in && rank == 0) counters[id] = pos + __popcll(m);
+    __builtin_amdgcn_wave_barrier();
+    return pos;
+}
+
+__global__ __launch_bounds__(kOneThreads) void group_rows_one_kernel(int n, const int32_t *__restrict__ ids, int E, int bits,
+                                                                     int32_t *__restrict__ offsets, int32_t *__restrict__ order)
+{
+    extern __shared__ int32_t counters[];          // [16 wavefronts][E]
+    __shared__ int32_t wave_sums[kOneThreads / kWave];
+    constexpr int kWaves = kOneThreads / kWave, kChunks = kOneBlockRows / kOneThreads;
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int chunks = (n + kOneThreads - 1) / kOneThreads, r0 = wave * chunks * kWave;   // of a wavefront, one run of rows each
+    int id[kChunks], pos[kChunks];
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) {
+        const int r = r0 + c * kWave + lane;
+        id[c] = c < chunks && r < n ? ids[r] : -1;
+    }
+    for (int i = threadIdx.x; i < kWaves * E; i += kOneThreads) counters[i] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c)
+        if (c < chunks) pos[c] = take(counters + wave * E, id[c], id[c] >= 0 && id[c] < E, bits, lane);
+    __syncthreads();
+    // counts -> bases: over the wavefronts of a group, then over the groups (a thread each)
+    int total = 0;
+    if (int(threadIdx.x) < E)
+        for (int w = 0; w < kWaves; ++w) total += counters[w * E + threadIdx.x];
+    int incl = total;
+    for (int d = 1; d < kWave; d <<= 1) {
+        const int t = __shfl_up(incl, d, kWave);
+        if (lane >= d) incl += t;
+    }
+    if (lane == kWave - 1) wave_sums[wave] = incl;
+    __syncthreads();
+    int base = incl - total;
+    for (int w = 0; w < wave; ++w) base += wave_sums[w];
+    if (int(threadIdx.x) < E) {
+        offsets[threadIdx.x] = base;
+        if (int(threadIdx.x) == E - 1) offsets[E] = base + total;
+        for (int w = 0; w < kWaves; ++w) {
+            const int c = counters[w * E + threadIdx.x];
+            counters[w * E + threadIdx.x] = base;
+            base += c;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c)
+        if (c < chunks && id[c] >= 0 && id[c] < E) order[counters[wave * E + id[c]] + pos[c]] = r0 + c * kWave + lane;
+}
+
+// kPlace: false, counts[g][tile]; true, positions from bases[g][tile] (and the offsets, by tile 0)
+template <bool kPlace>
+__global__ __launch_bounds__(kTileThreads) void group_rows_tile_kernel(int64_t n, const int32_t *__restrict__ ids, int E, int bits, int64_t tiles,
+                                                                       int32_t *__restrict__ counts, const int32_t *__restrict__ bases,
+                                                                       int32_t *__restrict__ offsets, int32_t *__restrict__ order)
+{
+    extern __shared__ int32_t counters[];          // [4 wavefronts][E]
+    constexpr int kWaves = kTileThreads / kWave;
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int64_t tile = blockIdx.x, r0 = tile * kTileRows + wave * (kTileChunks * kWave);
+    for (int i = threadIdx.x; i < kWaves * E; i += kTileThreads) counters[i] = 0;
+    int id[kTileChunks];
+#pragma unroll
+    for (int c = 0; c < kTileChunks; ++c) {
+        const int64_t r = r0 + c * kWave + lane;
+        id[c] = r < n ? ids[r] : -1;
+    }
+    __syncthreads();
+    volatile int32_t *mine = counters + wave * E;
+    int pos[kTileChunks];
+#pragma unroll
+    for (int c = 0; c < kTileChunks; ++c) pos[c] = take(mine, id[c], id[c] >= 0 && id[c] < E, bits, lane);
+    __syncthreads();
+    if constexpr (!kPlace) {
+        for (int g = threadIdx.x; g < E; g += kTileThreads) {
+            int total = 0;
+            for (int w = 0; w < kWaves; ++w) total += counters[w * E + g];
+            counts[g * tiles + tile] = total;
+        }
+    } else {
+        for (int g = threadIdx.x; g < E; g += kTileThreads) {
+            int base = bases[g * tiles + tile];
+            if (tile == 0) offsets[g] = base;
+            for (int w = 0; w < kWaves; ++w) {
+                const int c = counters[w * E + g];
+                counters[w * E + g] = base;
+                base += c;
+            }
+        }
+        if (tile == 0 && threadIdx.x == 0) offsets[E] = bases[E * tiles];
+        __syncthreads();
+        // pos: rank among the wavefront's rows of the group; now its base comes on top
+#pragma unroll
+        for (int c = 0; c < kTileChunks; ++c)
+            if (id[c] >= 0 && id[c] < E) order[counters[wave * E + id[c]] + pos[c]] = int32_t(r0 + c * kWave + lane);
+    }
+}
+
+static bool in_one_block(int64_t n, int E) { return n <= kOneBlockRows && E <= kOneGroups; }
+
+static int bits_of(int E)
+{
+    int b = 0;
+    while ((1 << b) < E) ++b;
+    return b;
+}
+
+}  // namespace tma
+
+extern "C" size_t tma_group_rows_workspace_bytes(int64_t n, int32_t E)
+{
+    using namespace tma;
+    if (n < 0 || n > INT32_MAX || E < 1 || E > kMaxGroups) return 0;
+    if (in_one_block(n, E)) return 256;
+    const int64_t cells = (n > 0 ? ceil_div(n, kTileRows) : 1) * E;
+    return round_up(size_t(cells) * 4, 256) + round_up(size_t(cells + 1) * 4, 256) + round_up(exclusive_scan_i32_workspace_bytes(cells), 256);
+}
+
+extern "C" int tma_group_rows(int64_t n, const int32_t *group, int32_t E, int32_t *offsets_out, int32_t *order_out, void *ws, size_t ws_bytes,
+                              tma_stream_t stream)
+{
+    using namespace tma;
+    const char *fn = "tma_group_rows";
+    TMA_REQUIRE(n >= 0 && n <= INT32_MAX, TMA_ERR_INVALID_ARG, "%s: n outside [0, 2^31)", fn);
+    TMA_REQUIRE(E >= 1 && E <= kMaxGroups, TMA_ERR_BAD_SHAPE, "%s: E=%d outside [1, %d]", fn, E, kMaxGroups);
+    TMA_REQUIRE(offsets_out && (n == 0 || (group && order_out)), TMA_ERR_INVALID_ARG, "%s: NULL argument", fn);
+    TMA_REQUIRE(ws && aligned(ws, 256), TMA_ERR_INVALID_ARG, "%s: workspace NULL or not 256-byte aligned", fn);
+    TMA_REQUIRE(ws_bytes >= tma_group_rows_workspace_bytes(n, E), TMA_ERR_WORKSPACE_TOO_SMALL, "%s: workspace too small", fn);
+    hipStream_t s = as_stream(stream);
+    const int bits = bits_of(E);
+    if (in_one_block(n, E)) {
+        TMA_TIMED("group_rows_one", s);
+        hipLaunchKernelGGL(group_rows_one_kernel, dim3(1), dim3(kOneThreads), size_t(kOneThreads / kWave) * E * 4, s, int(n), group, E, bits, offsets_out,
+                           order_out);
+        return check_launch(fn);
+    }
+    const int64_t tiles = n > 0 ? ceil_div(n, kTileRows) : 1, cells = tiles * E;
+    char *at = static_cast<char *>(ws);
+    int32_t *counts = reinterpret_cast<int32_t *>(at);
+    at += round_up(size_t(cells) * 4, 256);
+    int32_t *bases = reinterpret_cast<int32_t *>(at);
+    at += round_up(size_t(cells + 1) * 4, 256);
+    const size_t lds = size_t(kTileThreads / kWave) * E * 4;
+    {
+        TMA_TIMED("group_rows_count", s);
+        hipLaunchKernelGGL((group_rows_tile_kernel<false>), dim3(unsigned(tiles)), dim3(kTileThreads), lds, s, n, group, E, bits, tiles, counts, nullptr,
+                           nullptr, nullptr);
+        if (int rc = check_launch(fn)) return rc;
+    }
+    if (int rc = launch_exclusive_scan_i32(cells, counts, bases, at, s)) return rc;
+    TMA_TIMED("group_rows_place", s);
+    hipLaunchKernelGGL((group_rows_tile_kernel<true>), dim3(unsigned(tiles)), dim3(kTileThreads), lds, s, n, group, E, bits, tiles, nullptr, bases,
+                       offsets_out, order_out);
+    return check_launch(fn);
+}

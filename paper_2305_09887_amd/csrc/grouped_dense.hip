@@ -1,0 +1,330 @@
+// Dense layers of rows that are of several kinds: group g of the listed rows has weights of its own,
+//   forward   Y[v] = act(X[v] W[g] + b[g])
+//   backward  dZ = dY (.) act'(Y);  dX[v] = dZ[v] W[g]^T;  dW[g] = sum over g's rows of X[v]^T dZ[v];  db[g] = sum of dZ[v]
+// Group g has the positions [offsets[g], offsets[g+1]) of the list; position i is row order[i] of X, Y and their gradients
+// (order NULL: row i).  Sizes of groups are known to the device alone.
+//
+// Here: the entry points, and the kernels for groups of few rows, which the weights bound: they are read once as they are, in
+// fp32, every multiplication and sum is fp32.  Grids go over (group, slice of 32 columns), so that small layers still have
+// some hundred blocks; rows of a group go through LDS eight at a time.
+#include "kernels.hpp"
+
+namespace tma {
+
+constexpr int kMaxGroups = 1024;
+constexpr int kFewThreads = 256;
+constexpr int kFewCols = 32;      // columns of a block's slice: eight lanes with four each
+constexpr int kSideRows = 8;       // rows of a group side by side in registers
+constexpr int kFewK = 512;        // of the summed dimension in LDS at a time
+
+struct GroupList {
+    const int32_t *offsets, *order;
+    int E;
+    int64_t n;
+    // (what an offset says is held inside the list, and a row inside the arrays)
+    __device__ __forceinline__ int64_t begin(int g) const
+    {
+        const int64_t o = offsets[g];
+        return o < 0 ? 0 : o < n ? o : n;
+    }
+    __device__ __forceinline__ int64_t row(int64_t i) const
+    {
+        if (!order) return i;
+        const int64_t r = order[i];
+        return r >= 0 && r < n ? r : -1;
+    }
+};
+
+__device__ __forceinline__ float read1(const float *p) { return *p; }
+__device__ __forceinline__ float read1(const uint16_t *p) { return bf16_to_f32(*p); }
+__device__ __forceinline__ void write1(float *p, float v) { *p = v; }
+__device__ __forceinline__ void write1(uint16_t *p, float v) { *p = f32_to_bf16(v); }
+
+// four elements from p on, `left` of them inside (any alignment unless vec)
+__device__ __forceinline__ float4 weights4(const float *p, int left, bool vec)
+{
+    if (vec) return left > 0 ? *reinterpret_cast<const float4 *>(p) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    return make_float4(left > 0 ? p[0] : 0.0f, left > 1 ? p[1] : 0.0f, left > 2 ? p[2] : 0.0f, left > 3 ? p[3] : 0.0f);
+}
+
+// rows[r][k - k0] of the chunk's rows at columns [k0, k0 + kFewK), zeros outside; g where h > 0 with h given
+template <typename T>
+__device__ __forceinline__ void stage_rows(const GroupList &gl, int64_t i0, int m, const T *g, const T *h, int64_t ld, int k0, int K,
+                                           float (&rows)[kSideRows][kFewK + 4])
+{
+    const int width = K - k0 < kFewK ? K - k0 : kFewK;
+    for (int r = 0; r < kSideRows; ++r) {
+        const int64_t v = r < m ? gl.row(i0 + r) : -1;
+        for (int k = threadIdx.x; k < kFewK; k += kFewThreads) {
+            float x = 0.0f;
+            if (v >= 0 && k < width) {
+                x = read1(g + v * ld + k0 + k);
+                if (h && !(read1(h + v * ld + k0 + k) > 0.0f)) x = 0.0f;
+            }
+            rows[r][k] = x;
+        }
+    }
+}
+
+// Y[v][c] for the block's group and 32 columns.  Eight lanes share the columns, 32 of them the k-values.
+template <typename T>
+__global__ __launch_bounds__(kFewThreads) void grouped_few_fwd_kernel(GroupList gl, const T *__restrict__ X, int64_t ldx, int K, const float *__restrict__ W,
+                                                                      const float *__restrict__ bias, int N, bool relu, bool vec, T *__restrict__ Y,
+                                                                      int64_t ldy, int slices)
+{
+    __shared__ float rows[kSideRows][kFewK + 4];
+    __shared__ float sums[kFewThreads / kWave][kSideRows][kFewCols];
+    const int g = int(blockIdx.x) / slices, n0 = int(blockIdx.x) % slices * kFewCols;
+    const int64_t begin = gl.begin(g), end = gl.begin(g + 1);
+    const int q = int(threadIdx.x) % 8, ks = int(threadIdx.x) / 8, wave = int(threadIdx.x) / kWave, lane = int(threadIdx.x) % kWave;
+    const int left = N - n0 - 4 * q;
+    const float *Wg = W + int64_t(g) * K * N + n0 + 4 * q;
+    for (int64_t i0 = begin; i0 < end; i0 += kSideRows) {
+        const int m = end - i0 < kSideRows ? int(end - i0) : kSideRows;
+        float4 acc[kSideRows];
+        for (int r = 0; r < kSideRows; ++r) acc[r] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int k0 = 0; k0 < K; k0 += kFewK) {
+            const int width = K - k0 < kFewK ? K - k0 : kFewK;
+            __syncthreads();
+            stage_rows<T>(gl, i0, m, X, nullptr, ldx, k0, K, rows);
+            __syncthreads();
+#pragma unroll 4
+            for (int k = ks; k < width; k += 32) {
+                const float4 w = weights4(Wg + int64_t(k0 + k) * N, left, vec);
+#pragma unroll
+                for (int r = 0; r < kSideRows; ++r) {
+                    const float x = rows[r][k];
+                    acc[r].x = fmaf(x, w.x, acc[r].x);
+                    acc[r].y = fmaf(x, w.y, acc[r].y);
+                    acc[r].z = fmaf(x, w.z, acc[r].z);
+                    acc[r].w = fmaf(x, w.w, acc[r].w);
+                }
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < kSideRows; ++r) {
+            for (int d = 8; d < kWave; d *= 2) {
+                acc[r].x += __shfl_xor(acc[r].x, d, kWave);
+                acc[r].y += __shfl_xor(acc[r].y, d, kWave);
+                acc[r].z += __shfl_xor(acc[r].z, d, kWave);
+                acc[r].w += __shfl_xor(acc[r].w, d, kWave);
+            }
+            if (lane < 8) {
+                sums[wave][r][4 * q] = acc[r].x;
+                sums[wave][r][4 * q + 1] = acc[r].y;
+                sums[wave][r][4 * q + 2] = acc[r].z;
+                sums[wave][r][4 * q + 3] = acc[r].w;
+            }
+        }
+        __syncthreads();
+        const int r = int(threadIdx.x) / kFewCols, c = int(threadIdx.x) % kFewCols;
+        if (r < m && n0 + c < N) {
+            float z = (sums[0][r][c] + sums[1][r][c]) + (sums[2][r][c] + sums[3][r][c]);
+            if (bias) z += bias[int64_t(g) * N + n0 + c];
+            if (relu) z = z > 0.0f ? z : 0.0f;
+            const int64_t v = gl.row(i0 + r);
+            if (v >= 0) write1(Y + v * ldy + n0 + c, z);
+        }
+    }
+}
+
+// dX[v][i] for the block's group and 32 columns i: eight lanes share a row of W.
+template <typename T>
+__global__ __launch_bounds__(kFewThreads) void grouped_few_bwd_data_kernel(GroupList gl, const T *__restrict__ dY, const T *__restrict__ Yh, int64_t ldy, int K,
+                                                                           const float *__restrict__ W, int N, bool vec, T *__restrict__ dX, int64_t ldx,
+                                                                           int slices)
+{
+    __shared__ float rows[kSideRows][kFewK + 4];
+    const int g = int(blockIdx.x) / slices, i = int(blockIdx.x) % slices * kFewCols + int(threadIdx.x) / 8, q = int(threadIdx.x) % 8;
+    const int64_t begin = gl.begin(g), end = gl.begin(g + 1);
+    const float *Wi = W + (int64_t(g) * N + (i < N ? i : 0)) * K;
+    for (int64_t i0 = begin; i0 < end; i0 += kSideRows) {
+        const int m = end - i0 < kSideRows ? int(end - i0) : kSideRows;
+        float acc[kSideRows];
+        for (int r = 0; r < kSideRows; ++r) acc[r] = 0.0f;
+        for (int k0 = 0; k0 < K; k0 += kFewK) {
+            const int width = K - k0 < kFewK ? K - k0 : kFewK;
+            __syncthreads();
+            stage_rows<T>(gl, i0, m, dY, Yh, ldy, k0, K, rows);
+            __syncthreads();
+#pragma unroll 4
+            for (int k = 4 * q; k < width; k += 32) {
+                const float4 w = weights4(Wi + k0 + k, width - k, vec);
+#pragma unroll
+                for (int r = 0; r < kSideRows; ++r) {
+                    const float4 x = *reinterpret_cast<const float4 *>(&rows[r][k]);
+                    acc[r] = fmaf(x.x, w.x, fmaf(x.y, w.y, fmaf(x.z, w.z, fmaf(x.w, w.w, acc[r]))));
+                }
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < kSideRows; ++r) {
+            for (int d = 1; d < 8; d *= 2) acc[r] += __shfl_xor(acc[r], d, kWave);
+            const int64_t v = r < m ? gl.row(i0 + r) : -1;
+            if (q == 0 && i < N && v >= 0) write1(dX + v * ldx + i, acc[r]);
+        }
+    }
+}
+
+// dW[g][i][o] for the block's group, 32 rows i and all o (128 at a time); db with the first slice.
+constexpr int kFewO = 128;
+
+template <typename T>
+__global__ __launch_bounds__(kFewThreads) void grouped_few_bwd_weight_kernel(GroupList gl, const T *__restrict__ X, int64_t ldx, const T *__restrict__ dY,
+                                                                             const T *__restrict__ Yh, int64_t ldy, int M, int N, float *__restrict__ dW,
+                                                                             float *__restrict__ db, int slices)
+{
+    __shared__ float xs[kSideRows][kFewCols];
+    __shared__ float zs[kSideRows][kFewO];
+    const int g = int(blockIdx.x) / slices, m0 = int(blockIdx.x) % slices * kFewCols, il = int(threadIdx.x) / 8, q = int(threadIdx.x) % 8;
+    const int64_t begin = gl.begin(g), end = gl.begin(g + 1);
+    for (int o0 = 0; o0 < N; o0 += kFewO) {
+        float acc[kFewO / 32][4], sum = 0.0f;
+        for (int j = 0; j < kFewO / 32; ++j)
+            for (int c = 0; c < 4; ++c) acc[j][c] = 0.0f;
+        for (int64_t i0 = begin; i0 < end; i0 += kSideRows) {
+            const int m = end - i0 < kSideRows ? int(end - i0) : kSideRows;
+            __syncthreads();
+            {
+                const int r = int(threadIdx.x) / kFewCols, c = int(threadIdx.x) % kFewCols;
+                const int64_t v = r < m ? gl.row(i0 + r) : -1;
+                xs[r][c] = v >= 0 && m0 + c < M ? read1(X + v * ldx + m0 + c) : 0.0f;
+            }
+            for (int at = threadIdx.x; at < kSideRows * kFewO; at += kFewThreads) {
+                const int r = at / kFewO, o = o0 + at % kFewO;
+                const int64_t v = r < m ? gl.row(i0 + r) : -1;
+                float z = 0.0f;
+                if (v >= 0 && o < N) {
+                    z = read1(dY + v * ldy + o);
+                    if (Yh && !(read1(Yh + v * ldy + o) > 0.0f)) z = 0.0f;
+                }
+                zs[r][at % kFewO] = z;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int r = 0; r < kSideRows; ++r) {
+                const float x = xs[r][il];
+#pragma unroll
+                for (int j = 0; j < kFewO / 32; ++j) {
+                    const float4 z = *reinterpret_cast<const float4 *>(&zs[r][j * 32 + 4 * q]);
+                    acc[j][0] = fmaf(x, z.x, acc[j][0]);
+                    acc[j][1] = fmaf(x, z.y, acc[j][1]);
+                    acc[j][2] = fmaf(x, z.z, acc[j][2]);
+                    acc[j][3] = fmaf(x, z.w, acc[j][3]);
+                }
+                if (threadIdx.x < kFewO) sum += zs[r][threadIdx.x];
+            }
+        }
+        if (m0 + il < M) {
+            float *out = dW + (int64_t(g) * M + m0 + il) * N + o0;
+#pragma unroll
+            for (int j = 0; j < kFewO / 32; ++j)
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (o0 + j * 32 + 4 * q + c < N) out[j * 32 + 4 * q + c] = acc[j][c];
+        }
+        if (db && m0 == 0 && int(threadIdx.x) < kFewO && o0 + int(threadIdx.x) < N) db[int64_t(g) * N + o0 + threadIdx.x] = sum;
+    }
+}
+
+template <typename T>
+static int few_fwd(const char *fn, const GroupList &gl, const void *X, int64_t ldx, int K, const float *W, const float *bias, int N, bool relu, void *Y,
+                   int64_t ldy, hipStream_t s)
+{
+    const int slices = int(ceil_div(N, kFewCols));
+    TMA_TIMED(sizeof(T) == 2 ? "grouped_few_fwd_bf16" : "grouped_few_fwd", s);
+    hipLaunchKernelGGL((grouped_few_fwd_kernel<T>), dim3(unsigned(gl.E) * unsigned(slices)), dim3(kFewThreads), 0, s, gl, static_cast<const T *>(X), ldx, K, W,
+                       bias, N, relu, N % 4 == 0 && aligned(W, 16), static_cast<T *>(Y), ldy, slices);
+    return check_launch(fn);
+}
+
+template <typename T>
+static int few_bwd(const char *fn, const GroupList &gl, const void *X, int64_t ldx, const void *Y, const void *dY, int64_t ldy, const float *W, int F_in,
+                   int F_out, bool relu, float *dW, float *db, void *dX, int64_t ld_dx, hipStream_t s)
+{
+    const T *g = static_cast<const T *>(dY), *h = relu ? static_cast<const T *>(Y) : nullptr;
+    const int slices = int(ceil_div(F_in, kFewCols));
+    const dim3 grid(unsigned(gl.E) * unsigned(slices));
+    if (dX) {
+        TMA_TIMED(sizeof(T) == 2 ? "grouped_few_bwd_data_bf16" : "grouped_few_bwd_data", s);
+        hipLaunchKernelGGL((grouped_few_bwd_data_kernel<T>), grid, dim3(kFewThreads), 0, s, gl, g, h, ldy, F_out, W, F_in, F_out % 4 == 0 && aligned(W, 16),
+                           static_cast<T *>(dX), ld_dx, slices);
+        if (int rc = check_launch(fn)) return rc;
+    }
+    TMA_TIMED(sizeof(T) == 2 ? "grouped_few_bwd_weight_bf16" : "grouped_few_bwd_weight", s);
+    hipLaunchKernelGGL((grouped_few_bwd_weight_kernel<T>), grid, dim3(kFewThreads), 0, s, gl, static_cast<const T *>(X), ldx, g, h, ldy, F_in, F_out, dW, db,
+                       slices);
+    return check_launch(fn);
+}
+
+static int check_grouped(const char *fn, int64_t n, int32_t E, const int32_t *offsets, int32_t F_in, int32_t F_out, int32_t act, int32_t dtype,
+                         const void *ws, size_t ws_bytes, size_t need)
+{
+    TMA_REQUIRE(n >= 0 && n <= INT32_MAX, TMA_ERR_INVALID_ARG, "%s: n outside [0, 2^31)", fn);
+    TMA_REQUIRE(E >= 1 && E <= kMaxGroups, TMA_ERR_BAD_SHAPE, "%s: E=%d outside [1, %d]", fn, E, kMaxGroups);
+    TMA_REQUIRE(F_in >= 1 && F_out >= 1 && F_in <= (1 << 16) && F_out <= (1 << 16), TMA_ERR_BAD_SHAPE, "%s: F_in=%d F_out=%d", fn, F_in, F_out);
+    TMA_REQUIRE(act == TMA_ACT_NONE || act == TMA_ACT_RELU, TMA_ERR_INVALID_ARG, "%s: act %d", fn, act);
+    TMA_REQUIRE(dtype == TMA_F32 || dtype == TMA_BF16, TMA_ERR_UNSUPPORTED_DTYPE, "%s: dtype %d", fn, dtype);
+    TMA_REQUIRE(offsets, TMA_ERR_INVALID_ARG, "%s: offsets is NULL", fn);
+    TMA_REQUIRE(ws && aligned(ws, 256), TMA_ERR_INVALID_ARG, "%s: workspace NULL or not 256-byte aligned", fn);
+    TMA_REQUIRE(ws_bytes >= need, TMA_ERR_WORKSPACE_TOO_SMALL, "%s: workspace %zu < %zu", fn, ws_bytes, need);
+    return TMA_OK;
+}
+
+}  // namespace tma
+
+extern "C" size_t tma_grouped_dense_fwd_workspace_bytes(int64_t n, int32_t E, int32_t F_in, int32_t F_out, int32_t dtype)
+{
+    if (n < 0 || E < 1 || F_in < 1 || F_out < 1) return 0;
+    (void)dtype;
+    return 256;
+}
+
+extern "C" int tma_grouped_dense_fwd(int64_t n, int32_t E, const int32_t *offsets, const int32_t *order, const void *X, int64_t ldx, int32_t F_in,
+                                     const float *W, const float *bias, int32_t F_out, int32_t act, int32_t dtype, void *Y_out, int64_t ldy, void *ws,
+                                     size_t ws_bytes, tma_stream_t stream)
+{
+    using namespace tma;
+    const char *fn = "tma_grouped_dense_fwd";
+    if (int rc = check_grouped(fn, n, E, offsets, F_in, F_out, act, dtype, ws, ws_bytes, tma_grouped_dense_fwd_workspace_bytes(n, E, F_in, F_out, dtype)))
+        return rc;
+    if (n == 0) return TMA_OK;
+    TMA_REQUIRE(X && W && Y_out && X != Y_out, TMA_ERR_INVALID_ARG, "%s: NULL argument, or X and Y_out are one", fn);
+    TMA_REQUIRE(ldx >= F_in && ldy >= F_out, TMA_ERR_BAD_SHAPE, "%s: ldx < F_in or ldy < F_out", fn);
+    const GroupList gl{offsets, order, E, n};
+    hipStream_t s = as_stream(stream);
+    const bool relu = act == TMA_ACT_RELU;
+    return dtype == TMA_F32 ? few_fwd<float>(fn, gl, X, ldx, F_in, W, bias, F_out, relu, Y_out, ldy, s)
+                            : few_fwd<uint16_t>(fn, gl, X, ldx, F_in, W, bias, F_out, relu, Y_out, ldy, s);
+}
+
+extern "C" size_t tma_grouped_dense_bwd_workspace_bytes(int64_t n, int32_t E, int32_t F_in, int32_t F_out, int32_t dtype, int32_t need_dX)
+{
+    if (n < 0 || E < 1 || F_in < 1 || F_out < 1) return 0;
+    (void)dtype;
+    (void)need_dX;
+    return 256;
+}
+
+extern "C" int tma_grouped_dense_bwd(int64_t n, int32_t E, const int32_t *offsets, const int32_t *order, const void *X, int64_t ldx, const void *Y,
+                                     const void *dY, int64_t ldy, const float *W, int32_t F_in, int32_t F_out, int32_t act, int32_t dtype, float *dW,
+                                     float *dbias, void *dX_out, int64_t ld_dx, void *ws, size_t ws_bytes, tma_stream_t stream)
+{
+    using namespace tma;
+    const char *fn = "tma_grouped_dense_bwd";
+    if (int rc = check_grouped(fn, n, E, offsets, F_in, F_out, act, dtype, ws, ws_bytes,
+                               tma_grouped_dense_bwd_workspace_bytes(n, E, F_in, F_out, dtype, dX_out != nullptr)))
+        return rc;
+    TMA_REQUIRE(dW, TMA_ERR_INVALID_ARG, "%s: dW is NULL", fn);
+    if (n > 0) {
+        TMA_REQUIRE(X && dY && W, TMA_ERR_INVALID_ARG, "%s: NULL argument", fn);
+        TMA_REQUIRE(act == TMA_ACT_NONE || Y, TMA_ERR_INVALID_ARG, "%s: Y is required with ReLU", fn);
+        TMA_REQUIRE(ldx >= F_in && ldy >= F_out && (!dX_out || ld_dx >= F_in), TMA_ERR_BAD_SHAPE, "%s: a leading dimension is below its width", fn);
+        TMA_REQUIRE(dX_out != X && (!dX_out || (dX_out != dY && dX_out != Y)), TMA_ERR_INVALID_ARG, "%s: dX_out is one of the inputs", fn);
+    }
+    const GroupList gl{offsets, order, E, n};
+    hipStream_t s = as_stream(stream);
+    const bool relu = act == TMA_ACT_RELU;
+    return dtype == TMA_F32 ? few_bwd<float>(fn, gl, X, ldx, Y, dY, ldy, W, F_in, F_out, relu, dW, dbias, n > 0 ? dX_out : nullptr, ld_dx, s)
+                            : few_bwd<uint16_t>(fn, gl, X, ldx, Y, dY, ldy, W, F_in, F_out, relu, dW, dbias, n > 0 ? dX_out : nullptr, ld_dx, s);
+}
