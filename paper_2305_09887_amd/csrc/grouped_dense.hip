@@ -7,33 +7,14 @@
 // Here: the entry points, and the kernels for groups of few rows, which the weights bound: they are read once as they are, in
 // fp32, every multiplication and sum is fp32.  Grids go over (group, slice of 32 columns), so that small layers still have
 // some hundred blocks; rows of a group go through LDS eight at a time.
-#include "kernels.hpp"
+#include "grouped_gemm.hpp"
 
 namespace tma {
 
-constexpr int kMaxGroups = 1024;
 constexpr int kFewThreads = 256;
 constexpr int kFewCols = 32;      // columns of a block's slice: eight lanes with four each
 constexpr int kSideRows = 8;       // rows of a group side by side in registers
 constexpr int kFewK = 512;        // of the summed dimension in LDS at a time
-
-struct GroupList {
-    const int32_t *offsets, *order;
-    int E;
-    int64_t n;
-    // (what an offset says is held inside the list, and a row inside the arrays)
-    __device__ __forceinline__ int64_t begin(int g) const
-    {
-        const int64_t o = offsets[g];
-        return o < 0 ? 0 : o < n ? o : n;
-    }
-    __device__ __forceinline__ int64_t row(int64_t i) const
-    {
-        if (!order) return i;
-        const int64_t r = order[i];
-        return r >= 0 && r < n ? r : -1;
-    }
-};
 
 __device__ __forceinline__ float read1(const float *p) { return *p; }
 __device__ __forceinline__ float read1(const uint16_t *p) { return bf16_to_f32(*p); }
@@ -257,6 +238,174 @@ static int few_bwd(const char *fn, const GroupList &gl, const void *X, int64_t l
     return check_launch(fn);
 }
 
+// ---- tiles ---------------------------------------------------------------------
+// Few rows: the vector kernels, which read the weights once as they are; else tiles, which first lay them out.
+static bool few_rows_a_group(int64_t n, int E) { return n <= 16 * int64_t(E); }
+
+struct TileShape {
+    int TN, BN;            // 32-column tiles of a wavefront, columns of a block's tile
+    int steps, n_tiles;
+    size_t fragment_bytes;
+};
+
+// product of rows of K with N columns
+static TileShape tile_shape(int E, int K, int N, size_t elem)
+{
+    TileShape t;
+    const int step = int(32 / elem);
+    t.TN = N > 128 ? 2 : 1;
+    t.BN = N > 128 ? 256 : N > 64 ? 128 : 64;
+    t.steps = int(ceil_div(K, step));
+    t.n_tiles = int(ceil_div(N, t.BN));
+    t.fragment_bytes = round_up(size_t(E) * size_t(t.n_tiles) * size_t(t.BN / 32) * size_t(t.steps) * 1024, 256);
+    return t;
+}
+
+static int64_t tile_room(int64_t n, int E, int height) { return ceil_div(n, height) + E; }
+static size_t plan_bytes(int64_t n, int E, int height) { return round_up(size_t(tile_room(n, E, height)) * 16, 256) + round_up(size_t(E + 1) * 4, 256); }
+
+static TilePlan plan_at(char *&at, int64_t n, int E, int height)
+{
+    TilePlan p;
+    p.height = height;
+    p.room = tile_room(n, E, height);
+    p.tiles = reinterpret_cast<int4 *>(at);
+    p.first = reinterpret_cast<int32_t *>(at + round_up(size_t(p.room) * 16, 256));
+    at += plan_bytes(n, E, height);
+    return p;
+}
+
+// rows of a run of the weight gradient: as many runs as fill the chip twice with their tiles
+constexpr int kRunItems = 512;
+static int run_height(int64_t n, int M, int N)
+{
+    const int64_t tiles = ceil_div(M, 128) * ceil_div(N, 128), runs = kRunItems / tiles > 0 ? kRunItems / tiles : 1;
+    const int64_t rows = int64_t(round_up(size_t(ceil_div(n > 0 ? n : 1, runs)), 32));
+    return int(rows < 256 ? 256 : rows);
+}
+
+template <typename T>
+static void launch_prepare(const PrepareCall &q, bool forward, hipStream_t s)
+{
+    const int64_t pieces = q.B ? int64_t(q.gl.E) * q.col_tiles * q.steps * kWave : 0;
+    int64_t blocks = ceil_div(pieces, kGgThreads);
+    if (blocks > 4096) blocks = 4096;
+    const dim3 grid(unsigned(q.row_blocks + q.run_blocks + blocks));
+    TMA_TIMED(sizeof(T) == 2 ? "grouped_prepare_bf16" : "grouped_prepare", s);
+    if (forward) hipLaunchKernelGGL((grouped_prepare_kernel<T, true>), grid, dim3(kGgThreads), 0, s, q);
+    else hipLaunchKernelGGL((grouped_prepare_kernel<T, false>), grid, dim3(kGgThreads), 0, s, q);
+}
+
+template <typename T, int WN, int TN, int PP, bool kMask>
+static void launch_rows_as(const RowsCall &q, bool words, bool store16, int64_t most_items, hipStream_t s)
+{
+    constexpr int kPerCu = kRowBlocksPerCu<TN, PP, kMask>;
+    int64_t per_die = ceil_div(most_items, kDies);
+    if (per_die > 32 * kPerCu) per_die = 32 * kPerCu;
+    const dim3 grid(unsigned(per_die * kDies));
+    if (words && store16) hipLaunchKernelGGL((grouped_rows_kernel<T, WN, TN, PP, kMask, true, true>), grid, dim3(kGgThreads), 0, s, q);
+    else if (words) hipLaunchKernelGGL((grouped_rows_kernel<T, WN, TN, PP, kMask, true, false>), grid, dim3(kGgThreads), 0, s, q);
+    else hipLaunchKernelGGL((grouped_rows_kernel<T, WN, TN, PP, kMask, false, false>), grid, dim3(kGgThreads), 0, s, q);
+}
+
+template <typename T, bool kMask>
+static int launch_rows(const char *fn, const char *name, const RowsCall &q, const TileShape &t, hipStream_t s)
+{
+    const T *A = static_cast<const T *>(q.A), *H = static_cast<const T *>(q.H);
+    const bool words = sizeof(T) == 4 || (aligned(A, 4) && aligned(H, 4) && q.lda % 2 == 0);
+    const bool store16 = aligned(q.C, 16) && (size_t(q.ldc) * sizeof(T)) % 16 == 0;
+    const int64_t items = tile_room(q.gl.n, q.gl.E, kTileM) * q.n_tiles;
+    TMA_TIMED(name, s);
+    auto pieces = [&](auto wn, auto tn) {
+        constexpr int WN = decltype(wn)::value, TN = decltype(tn)::value;
+        if (t.steps <= 4) launch_rows_as<T, WN, TN, 8, kMask>(q, words, store16, items, s);
+        else if (t.steps <= 8) launch_rows_as<T, WN, TN, 16, kMask>(q, words, store16, items, s);
+        else launch_rows_as<T, WN, TN, 32, kMask>(q, words, store16, items, s);
+    };
+    if (t.BN == 256) pieces(std::integral_constant<int, 4>{}, std::integral_constant<int, 2>{});
+    else if (t.BN == 128) pieces(std::integral_constant<int, 4>{}, std::integral_constant<int, 1>{});
+    else pieces(std::integral_constant<int, 2>{}, std::integral_constant<int, 1>{});
+    return check_launch(fn);
+}
+
+template <typename T>
+static int tiles_fwd(const char *fn, const GroupList &gl, const void *X, int64_t ldx, int K, const float *W, const float *bias, int N, bool relu, void *Y,
+                     int64_t ldy, void *ws, hipStream_t s)
+{
+    const TileShape t = tile_shape(gl.E, K, N, sizeof(T));
+    char *at = static_cast<char *>(ws);
+    PrepareCall p{};
+    p.gl = gl;
+    p.rows = plan_at(at, gl.n, gl.E, kTileM);
+    p.row_blocks = int(ceil_div(p.rows.room, kGgThreads));
+    p.W = W;
+    p.B = reinterpret_cast<uint4 *>(at);
+    p.K = K;
+    p.N = N;
+    p.col_tiles = t.n_tiles * t.BN / 32;
+    p.steps = t.steps;
+    p.TN = t.TN;
+    launch_prepare<T>(p, true, s);
+    if (int rc = check_launch(fn)) return rc;
+    const RowsCall q{gl, p.rows.tiles, p.rows.first + gl.E, p.B, bias, X, nullptr, Y, ldx, ldy, K, N, t.steps, t.n_tiles, relu};
+    return launch_rows<T, false>(fn, sizeof(T) == 2 ? "grouped_fwd_bf16" : "grouped_fwd", q, t, s);
+}
+
+template <typename T>
+static int tiles_bwd(const char *fn, const GroupList &gl, const void *X, int64_t ldx, const void *Y, const void *dY, int64_t ldy, const float *W, int F_in,
+                     int F_out, bool relu, float *dW, float *db, void *dX, int64_t ld_dx, void *ws, hipStream_t s)
+{
+    const TileShape t = tile_shape(gl.E, F_out, F_in, sizeof(T));
+    const int height = run_height(gl.n, F_in, F_out);
+    char *at = static_cast<char *>(ws);
+    PrepareCall p{};
+    p.gl = gl;
+    p.runs = plan_at(at, gl.n, gl.E, height);
+    p.run_blocks = int(ceil_div(p.runs.room, kGgThreads));
+    float *partial = reinterpret_cast<float *>(at);
+    at += round_up(size_t(p.runs.room) * size_t(F_in) * size_t(F_out) * 4, 256);
+    float *colsum = reinterpret_cast<float *>(at);
+    at += round_up(size_t(p.runs.room) * size_t(F_out) * 4, 256);
+    if (dX) {
+        p.rows = plan_at(at, gl.n, gl.E, kTileM);
+        p.row_blocks = int(ceil_div(p.rows.room, kGgThreads));
+        p.W = W;
+        p.B = reinterpret_cast<uint4 *>(at);
+        p.K = F_out;
+        p.N = F_in;
+        p.col_tiles = t.n_tiles * t.BN / 32;
+        p.steps = t.steps;
+        p.TN = t.TN;
+    }
+    launch_prepare<T>(p, false, s);
+    if (int rc = check_launch(fn)) return rc;
+    if (dX) {
+        const RowsCall q{gl, p.rows.tiles, p.rows.first + gl.E, p.B, nullptr, dY, relu ? Y : nullptr, dX, ldy, ld_dx, F_out, F_in, t.steps, t.n_tiles, false};
+        const char *name = sizeof(T) == 2 ? "grouped_bwd_data_bf16" : "grouped_bwd_data";
+        if (int rc = relu ? launch_rows<T, true>(fn, name, q, t, s) : launch_rows<T, false>(fn, name, q, t, s)) return rc;
+    }
+    {
+        const WeightCall q{gl, p.runs.tiles, p.runs.first, X, dY, relu ? Y : nullptr, ldx, ldy, F_in, F_out, int(ceil_div(F_in, 128)), int(ceil_div(F_out, 128)),
+                           dW, db, partial, colsum};
+        const bool words = sizeof(T) == 4 || (aligned(X, 4) && aligned(dY, 4) && (!relu || aligned(Y, 4)) && ldx % 2 == 0 && ldy % 2 == 0);
+        int64_t per_die = ceil_div(p.runs.room * q.m_tiles * q.n_tiles, kDies);
+        if (per_die > 64) per_die = 64;
+        const dim3 grid(unsigned(per_die * kDies));
+        TMA_TIMED(sizeof(T) == 2 ? "grouped_bwd_weight_bf16" : "grouped_bwd_weight", s);
+        if (relu && words) hipLaunchKernelGGL((grouped_weight_kernel<T, true, true>), grid, dim3(kGgThreads), 0, s, q);
+        else if (relu) hipLaunchKernelGGL((grouped_weight_kernel<T, true, false>), grid, dim3(kGgThreads), 0, s, q);
+        else if (words) hipLaunchKernelGGL((grouped_weight_kernel<T, false, true>), grid, dim3(kGgThreads), 0, s, q);
+        else hipLaunchKernelGGL((grouped_weight_kernel<T, false, false>), grid, dim3(kGgThreads), 0, s, q);
+        if (int rc = check_launch(fn)) return rc;
+    }
+    const int64_t cells = int64_t(F_in) * F_out;
+    int64_t blocks = ceil_div(cells, kGgThreads);
+    if (blocks > 1024) blocks = 1024;
+    TMA_TIMED("grouped_join", s);
+    hipLaunchKernelGGL(grouped_join_kernel, dim3(unsigned(blocks), unsigned(gl.E)), dim3(kGgThreads), 0, s, p.runs.first, cells, F_out, partial, colsum, dW, db);
+    return check_launch(fn);
+}
+
 static int check_grouped(const char *fn, int64_t n, int32_t E, const int32_t *offsets, int32_t F_in, int32_t F_out, int32_t act, int32_t dtype,
                          const void *ws, size_t ws_bytes, size_t need)
 {
@@ -275,9 +424,10 @@ static int check_grouped(const char *fn, int64_t n, int32_t E, const int32_t *of
 
 extern "C" size_t tma_grouped_dense_fwd_workspace_bytes(int64_t n, int32_t E, int32_t F_in, int32_t F_out, int32_t dtype)
 {
+    using namespace tma;
     if (n < 0 || E < 1 || F_in < 1 || F_out < 1) return 0;
-    (void)dtype;
-    return 256;
+    if (few_rows_a_group(n, E)) return 256;
+    return plan_bytes(n, E, kTileM) + tile_shape(E, F_in, F_out, dtype == TMA_BF16 ? 2 : 4).fragment_bytes;
 }
 
 extern "C" int tma_grouped_dense_fwd(int64_t n, int32_t E, const int32_t *offsets, const int32_t *order, const void *X, int64_t ldx, int32_t F_in,
@@ -294,16 +444,23 @@ extern "C" int tma_grouped_dense_fwd(int64_t n, int32_t E, const int32_t *offset
     const GroupList gl{offsets, order, E, n};
     hipStream_t s = as_stream(stream);
     const bool relu = act == TMA_ACT_RELU;
+    if (!few_rows_a_group(n, E))
+        return dtype == TMA_F32 ? tiles_fwd<float>(fn, gl, X, ldx, F_in, W, bias, F_out, relu, Y_out, ldy, ws, s)
+                                : tiles_fwd<uint16_t>(fn, gl, X, ldx, F_in, W, bias, F_out, relu, Y_out, ldy, ws, s);
     return dtype == TMA_F32 ? few_fwd<float>(fn, gl, X, ldx, F_in, W, bias, F_out, relu, Y_out, ldy, s)
                             : few_fwd<uint16_t>(fn, gl, X, ldx, F_in, W, bias, F_out, relu, Y_out, ldy, s);
 }
 
 extern "C" size_t tma_grouped_dense_bwd_workspace_bytes(int64_t n, int32_t E, int32_t F_in, int32_t F_out, int32_t dtype, int32_t need_dX)
 {
+    using namespace tma;
     if (n < 0 || E < 1 || F_in < 1 || F_out < 1) return 0;
-    (void)dtype;
-    (void)need_dX;
-    return 256;
+    if (few_rows_a_group(n, E)) return 256;
+    const int height = run_height(n, F_in, F_out);
+    const size_t runs = size_t(tile_room(n, E, height));
+    size_t bytes = plan_bytes(n, E, height) + round_up(runs * size_t(F_in) * size_t(F_out) * 4, 256) + round_up(runs * size_t(F_out) * 4, 256);
+    if (need_dX) bytes += plan_bytes(n, E, kTileM) + tile_shape(E, F_out, F_in, dtype == TMA_BF16 ? 2 : 4).fragment_bytes;
+    return bytes;
 }
 
 extern "C" int tma_grouped_dense_bwd(int64_t n, int32_t E, const int32_t *offsets, const int32_t *order, const void *X, int64_t ldx, const void *Y,
@@ -325,6 +482,9 @@ extern "C" int tma_grouped_dense_bwd(int64_t n, int32_t E, const int32_t *offset
     const GroupList gl{offsets, order, E, n};
     hipStream_t s = as_stream(stream);
     const bool relu = act == TMA_ACT_RELU;
+    if (!few_rows_a_group(n, E))
+        return dtype == TMA_F32 ? tiles_bwd<float>(fn, gl, X, ldx, Y, dY, ldy, W, F_in, F_out, relu, dW, dbias, dX_out, ld_dx, ws, s)
+                                : tiles_bwd<uint16_t>(fn, gl, X, ldx, Y, dY, ldy, W, F_in, F_out, relu, dW, dbias, dX_out, ld_dx, ws, s);
     return dtype == TMA_F32 ? few_bwd<float>(fn, gl, X, ldx, Y, dY, ldy, W, F_in, F_out, relu, dW, dbias, n > 0 ? dX_out : nullptr, ld_dx, s)
                             : few_bwd<uint16_t>(fn, gl, X, ldx, Y, dY, ldy, W, F_in, F_out, relu, dW, dbias, n > 0 ? dX_out : nullptr, ld_dx, s);
 }
