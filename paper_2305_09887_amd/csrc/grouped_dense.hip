@@ -245,7 +245,7 @@ static bool few_rows_a_group(int64_t n, int E) { return n <= 16 * int64_t(E); }
 struct TileShape {
     int TN, BN;            // 32-column tiles of a wavefront, columns of a block's tile
     int steps, n_tiles;
-    size_t fragment_bytes;
+    size_t fragment_bytes, bias_bytes;
 };
 
 // product of rows of K with N columns
@@ -258,6 +258,7 @@ static TileShape tile_shape(int E, int K, int N, size_t elem)
     t.steps = int(ceil_div(K, step));
     t.n_tiles = int(ceil_div(N, t.BN));
     t.fragment_bytes = round_up(size_t(E) * size_t(t.n_tiles) * size_t(t.BN / 32) * size_t(t.steps) * 1024, 256);
+    t.bias_bytes = round_up(size_t(E) * size_t(t.n_tiles) * size_t(t.BN) * 4, 256);
     return t;
 }
 
@@ -275,13 +276,25 @@ static TilePlan plan_at(char *&at, int64_t n, int E, int height)
     return p;
 }
 
-// rows of a run of the weight gradient: as many runs as fill the chip twice with their tiles
-constexpr int kRunItems = 512;
-static int run_height(int64_t n, int M, int N)
+// Tiles of the weight gradient: as wide as the result up to 256 x 256, so that rows are read once.  Runs: as many as the chip holds at
+// once with all their tiles, or a few rounds of it; E fewer, since each group's last run may be short (a run more than a round's costs a round).
+struct WeightShape {
+    int BM, BN, m_tiles, n_tiles, per_cu, height;
+};
+static WeightShape weight_shape(int64_t n, int E, int M, int N)
 {
-    const int64_t tiles = ceil_div(M, 128) * ceil_div(N, 128), runs = kRunItems / tiles > 0 ? kRunItems / tiles : 1;
+    WeightShape w;
+    w.BM = M > 128 ? 256 : 128;
+    w.BN = N > 128 ? 256 : 128;
+    w.m_tiles = int(ceil_div(M, w.BM));
+    w.n_tiles = int(ceil_div(N, w.BN));
+    w.per_cu = w.BM * w.BN > 128 * 128 ? 1 : 2;
+    const int64_t slots = 256 * w.per_cu, tiles = int64_t(w.m_tiles) * w.n_tiles;
+    int64_t round = ceil_div(slots, tiles), runs = round - E;
+    while (runs < (round + 1) / 2) runs += round;
     const int64_t rows = int64_t(round_up(size_t(ceil_div(n > 0 ? n : 1, runs)), 32));
-    return int(rows < 256 ? 256 : rows);
+    w.height = int(rows < 256 ? 256 : rows < (1 << 30) ? rows : 1 << 30);
+    return w;
 }
 
 template <typename T>
@@ -290,7 +303,9 @@ static void launch_prepare(const PrepareCall &q, bool forward, hipStream_t s)
     const int64_t pieces = q.B ? int64_t(q.gl.E) * q.col_tiles * q.steps * kWave : 0;
     int64_t blocks = ceil_div(pieces, kGgThreads);
     if (blocks > 4096) blocks = 4096;
-    const dim3 grid(unsigned(q.row_blocks + q.run_blocks + blocks));
+    int64_t all = q.row_blocks + q.run_blocks + blocks;
+    if (q.bias && all < q.gl.E) all = q.gl.E;
+    const dim3 grid{unsigned(all)};
     TMA_TIMED(sizeof(T) == 2 ? "grouped_prepare_bf16" : "grouped_prepare", s);
     if (forward) hipLaunchKernelGGL((grouped_prepare_kernel<T, true>), grid, dim3(kGgThreads), 0, s, q);
     else hipLaunchKernelGGL((grouped_prepare_kernel<T, false>), grid, dim3(kGgThreads), 0, s, q);
@@ -308,11 +323,18 @@ static void launch_rows_as(const RowsCall &q, bool words, bool store16, int64_t 
     else hipLaunchKernelGGL((grouped_rows_kernel<T, WN, TN, PP, kMask, false, false>), grid, dim3(kGgThreads), 0, s, q);
 }
 
+// rows whose pieces of 16 bytes one load fetches: words throughout, and such a piece in the array
+template <typename T>
+static bool rows_in_words(const void *p, int64_t ld, int64_t n, int F)
+{
+    return (sizeof(T) == 4 || (aligned(p, 4) && ld % 2 == 0)) && (n - 1) * ld + F >= int64_t(16 / sizeof(T));
+}
+
 template <typename T, bool kMask>
 static int launch_rows(const char *fn, const char *name, const RowsCall &q, const TileShape &t, hipStream_t s)
 {
     const T *A = static_cast<const T *>(q.A), *H = static_cast<const T *>(q.H);
-    const bool words = sizeof(T) == 4 || (aligned(A, 4) && aligned(H, 4) && q.lda % 2 == 0);
+    const bool words = rows_in_words<T>(A, q.lda, q.gl.n, q.K) && (!kMask || aligned(H, 4));
     const bool store16 = aligned(q.C, 16) && (size_t(q.ldc) * sizeof(T)) % 16 == 0;
     const int64_t items = tile_room(q.gl.n, q.gl.E, kTileM) * q.n_tiles;
     TMA_TIMED(name, s);
@@ -329,6 +351,28 @@ static int launch_rows(const char *fn, const char *name, const RowsCall &q, cons
 }
 
 template <typename T>
+static void launch_weight(const WeightCall &q, const WeightShape &w, bool relu, bool words, int64_t runs, hipStream_t s)
+{
+    int64_t per_die = ceil_div(runs * w.m_tiles * w.n_tiles, kDies);
+    if (per_die > 32 * w.per_cu) per_die = 32 * w.per_cu;
+    const dim3 grid(unsigned(per_die * kDies));
+    auto go = [&](auto wm, auto wn, auto tm, auto tn) {
+        constexpr int WM = decltype(wm)::value, WN = decltype(wn)::value, TM = decltype(tm)::value, TN = decltype(tn)::value;
+        const dim3 block(WM * WN * 64);
+        if (relu && words) hipLaunchKernelGGL((grouped_weight_kernel<T, WM, WN, TM, TN, true, true>), grid, block, 0, s, q);
+        else if (relu) hipLaunchKernelGGL((grouped_weight_kernel<T, WM, WN, TM, TN, true, false>), grid, block, 0, s, q);
+        else if (words) hipLaunchKernelGGL((grouped_weight_kernel<T, WM, WN, TM, TN, false, true>), grid, block, 0, s, q);
+        else hipLaunchKernelGGL((grouped_weight_kernel<T, WM, WN, TM, TN, false, false>), grid, block, 0, s, q);
+    };
+    const std::integral_constant<int, 2> two;
+    const std::integral_constant<int, 4> four;
+    if (w.BM == 256 && w.BN == 256) go(two, four, four, two);
+    else if (w.BM == 256) go(four, two, two, two);
+    else if (w.BN == 256) go(two, four, two, two);
+    else go(two, two, two, two);
+}
+
+template <typename T>
 static int tiles_fwd(const char *fn, const GroupList &gl, const void *X, int64_t ldx, int K, const float *W, const float *bias, int N, bool relu, void *Y,
                      int64_t ldy, void *ws, hipStream_t s)
 {
@@ -339,6 +383,9 @@ static int tiles_fwd(const char *fn, const GroupList &gl, const void *X, int64_t
     p.rows = plan_at(at, gl.n, gl.E, kTileM);
     p.row_blocks = int(ceil_div(p.rows.room, kGgThreads));
     p.W = W;
+    p.bias = bias;
+    p.bias_out = reinterpret_cast<float *>(at);
+    at += t.bias_bytes;
     p.B = reinterpret_cast<uint4 *>(at);
     p.K = K;
     p.N = N;
@@ -347,7 +394,7 @@ static int tiles_fwd(const char *fn, const GroupList &gl, const void *X, int64_t
     p.TN = t.TN;
     launch_prepare<T>(p, true, s);
     if (int rc = check_launch(fn)) return rc;
-    const RowsCall q{gl, p.rows.tiles, p.rows.first + gl.E, p.B, bias, X, nullptr, Y, ldx, ldy, K, N, t.steps, t.n_tiles, relu};
+    const RowsCall q{gl, p.rows.tiles, p.rows.first + gl.E, p.B, bias ? p.bias_out : nullptr, X, nullptr, Y, ldx, ldy, K, N, t.steps, t.n_tiles, relu};
     return launch_rows<T, false>(fn, sizeof(T) == 2 ? "grouped_fwd_bf16" : "grouped_fwd", q, t, s);
 }
 
@@ -356,7 +403,7 @@ static int tiles_bwd(const char *fn, const GroupList &gl, const void *X, int64_t
                      int F_out, bool relu, float *dW, float *db, void *dX, int64_t ld_dx, void *ws, hipStream_t s)
 {
     const TileShape t = tile_shape(gl.E, F_out, F_in, sizeof(T));
-    const int height = run_height(gl.n, F_in, F_out);
+    const int height = weight_shape(gl.n, gl.E, F_in, F_out).height;
     char *at = static_cast<char *>(ws);
     PrepareCall p{};
     p.gl = gl;
@@ -385,17 +432,11 @@ static int tiles_bwd(const char *fn, const GroupList &gl, const void *X, int64_t
         if (int rc = relu ? launch_rows<T, true>(fn, name, q, t, s) : launch_rows<T, false>(fn, name, q, t, s)) return rc;
     }
     {
-        const WeightCall q{gl, p.runs.tiles, p.runs.first, X, dY, relu ? Y : nullptr, ldx, ldy, F_in, F_out, int(ceil_div(F_in, 128)), int(ceil_div(F_out, 128)),
-                           dW, db, partial, colsum};
-        const bool words = sizeof(T) == 4 || (aligned(X, 4) && aligned(dY, 4) && (!relu || aligned(Y, 4)) && ldx % 2 == 0 && ldy % 2 == 0);
-        int64_t per_die = ceil_div(p.runs.room * q.m_tiles * q.n_tiles, kDies);
-        if (per_die > 64) per_die = 64;
-        const dim3 grid(unsigned(per_die * kDies));
+        const WeightShape w = weight_shape(gl.n, gl.E, F_in, F_out);
+        const WeightCall q{gl, p.runs.tiles, p.runs.first, X, dY, relu ? Y : nullptr, ldx, ldy, F_in, F_out, w.m_tiles, w.n_tiles, dW, db, partial, colsum};
+        const bool words = rows_in_words<T>(X, ldx, gl.n, F_in) && rows_in_words<T>(dY, ldy, gl.n, F_out) && (!relu || aligned(Y, 4));
         TMA_TIMED(sizeof(T) == 2 ? "grouped_bwd_weight_bf16" : "grouped_bwd_weight", s);
-        if (relu && words) hipLaunchKernelGGL((grouped_weight_kernel<T, true, true>), grid, dim3(kGgThreads), 0, s, q);
-        else if (relu) hipLaunchKernelGGL((grouped_weight_kernel<T, true, false>), grid, dim3(kGgThreads), 0, s, q);
-        else if (words) hipLaunchKernelGGL((grouped_weight_kernel<T, false, true>), grid, dim3(kGgThreads), 0, s, q);
-        else hipLaunchKernelGGL((grouped_weight_kernel<T, false, false>), grid, dim3(kGgThreads), 0, s, q);
+        launch_weight<T>(q, w, relu, words, p.runs.room, s);
         if (int rc = check_launch(fn)) return rc;
     }
     const int64_t cells = int64_t(F_in) * F_out;
@@ -427,7 +468,8 @@ extern "C" size_t tma_grouped_dense_fwd_workspace_bytes(int64_t n, int32_t E, in
     using namespace tma;
     if (n < 0 || E < 1 || F_in < 1 || F_out < 1) return 0;
     if (few_rows_a_group(n, E)) return 256;
-    return plan_bytes(n, E, kTileM) + tile_shape(E, F_in, F_out, dtype == TMA_BF16 ? 2 : 4).fragment_bytes;
+    const TileShape t = tile_shape(E, F_in, F_out, dtype == TMA_BF16 ? 2 : 4);
+    return plan_bytes(n, E, kTileM) + t.bias_bytes + t.fragment_bytes;
 }
 
 extern "C" int tma_grouped_dense_fwd(int64_t n, int32_t E, const int32_t *offsets, const int32_t *order, const void *X, int64_t ldx, int32_t F_in,
@@ -456,7 +498,7 @@ extern "C" size_t tma_grouped_dense_bwd_workspace_bytes(int64_t n, int32_t E, in
     using namespace tma;
     if (n < 0 || E < 1 || F_in < 1 || F_out < 1) return 0;
     if (few_rows_a_group(n, E)) return 256;
-    const int height = run_height(n, F_in, F_out);
+    const int height = weight_shape(n, E, F_in, F_out).height;
     const size_t runs = size_t(tile_room(n, E, height));
     size_t bytes = plan_bytes(n, E, height) + round_up(runs * size_t(F_in) * size_t(F_out) * 4, 256) + round_up(runs * size_t(F_out) * 4, 256);
     if (need_dX) bytes += plan_bytes(n, E, kTileM) + tile_shape(E, F_out, F_in, dtype == TMA_BF16 ? 2 : 4).fragment_bytes;

@@ -164,36 +164,52 @@ struct __attribute__((packed, aligned(4))) Words4 {
 __device__ __forceinline__ uint32_t bits1(const float *p) { return __float_as_uint(*p); }
 __device__ __forceinline__ uint32_t bits1(const uint16_t *p) { return *p; }
 
-// `valid` elements from element `at` on of an array of `extent` elements, what follows them anything.  kWords: 4-byte aligned (the
-// load needs no more); past the end of the array, or without kWords, element by element
+// A piece of 16 bytes from element `at` on of an array, of which the first `valid` elements are wanted and the others read as zero.
+// kWords (4-byte aligned, the load needs no more): one load without a branch; a piece that would run past `last`, the last place where
+// 16 bytes are left, comes from there and is moved back in registers.  Else element by element.
 template <typename T, bool kWords>
-__device__ __forceinline__ uint4 fetch_piece(const T *__restrict__ x, int64_t at, int valid, int64_t extent)
-{
-    constexpr int E = 16 / sizeof(T);
-    uint4 r = make_uint4(0u, 0u, 0u, 0u);
-    if (valid <= 0) return r;
-    if (kWords && at + E <= extent) {
-        const Words4 w = *reinterpret_cast<const Words4 *>(x + at);
-        return make_uint4(w.w[0], w.w[1], w.w[2], w.w[3]);
-    }
-    uint32_t w[4] = {0u, 0u, 0u, 0u};
+struct RowPiece {
+    static constexpr int E = 16 / sizeof(T);
+    static __device__ __forceinline__ uint4 load(const T *__restrict__ x, int64_t at, int valid, int64_t last)
+    {
+        if constexpr (kWords) {
+            const Words4 w = *reinterpret_cast<const Words4 *>(x + (at < last ? at : last));
+            return make_uint4(w.w[0], w.w[1], w.w[2], w.w[3]);
+        } else {
+            uint32_t w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-    for (int j = 0; j < E; ++j)
-        if (j < valid) w[j * int(sizeof(T)) / 4] |= bits1(x + at + j) << (sizeof(T) == 2 ? 16 * (j & 1) : 0);
-    return make_uint4(w[0], w[1], w[2], w[3]);
-}
-
-template <typename T>
-__device__ __forceinline__ uint4 cut_piece(const uint4 &p, int valid)
-{
-    uint32_t w[4] = {p.x, p.y, p.z, p.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if constexpr (sizeof(T) == 4) w[i] = valid > i ? w[i] : 0u;
-        else w[i] &= valid > 2 * i + 1 ? ~0u : valid > 2 * i ? 0xFFFFu : 0u;
+            for (int j = 0; j < E; ++j)
+                if (j < valid) w[j * int(sizeof(T)) / 4] |= bits1(x + at + j) << (sizeof(T) == 2 ? 16 * (j & 1) : 0);
+            return make_uint4(w[0], w[1], w[2], w[3]);
+        }
     }
-    return make_uint4(w[0], w[1], w[2], w[3]);
-}
+    // back: elements by which the piece was fetched too early
+    static __device__ __forceinline__ uint4 moved(const uint4 &p, int back)
+    {
+        uint64_t lo = uint64_t(p.y) << 32 | p.x, hi = uint64_t(p.w) << 32 | p.z;
+        int bits = back * int(sizeof(T)) * 8;
+        if (bits >= 64) {
+            lo = hi;
+            hi = 0;
+            bits -= 64;
+        }
+        if (bits > 0) {
+            lo = lo >> bits | hi << (64 - bits);
+            hi >>= bits;
+        }
+        return make_uint4(uint32_t(lo), uint32_t(lo >> 32), uint32_t(hi), uint32_t(hi >> 32));
+    }
+    static __device__ __forceinline__ uint4 cut(const uint4 &p, int valid)
+    {
+        uint32_t w[4] = {p.x, p.y, p.z, p.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (sizeof(T) == 4) w[i] = valid > i ? w[i] : 0u;
+            else w[i] &= valid > 2 * i + 1 ? ~0u : valid > 2 * i ? 0xFFFFu : 0u;
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+};
 
 // g where h > 0 (a NaN in h: not), zeros elsewhere
 template <typename T>
@@ -211,16 +227,24 @@ __device__ __forceinline__ uint4 open_piece(const uint4 &g, const uint4 &h)
     return make_uint4(open_word<T>(g.x, h.x), open_word<T>(g.y, h.y), open_word<T>(g.z, h.z), open_word<T>(g.w, h.w));
 }
 
-template <typename T>
-__device__ __forceinline__ floatx16 multiply(const uint4 &a, const uint4 &b, floatx16 c)
+// acc[i][j] += a step's products; the fp32 instruction's four in a row go to different accumulators
+template <typename T, int TM, int TN>
+__device__ __forceinline__ void multiply(const uint4 (&w)[TN], const uint4 (&x)[TM], floatx16 (&acc)[TM][TN])
 {
     if constexpr (sizeof(T) == 2) {
-        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w[j]), __builtin_bit_cast(bf16x8, x[i]), acc[i][j], 0, 0, 0);
     } else {
-        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.x), __uint_as_float(b.x), c, 0, 0, 0);
-        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.y), __uint_as_float(b.y), c, 0, 0, 0);
-        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.z), __uint_as_float(b.z), c, 0, 0, 0);
-        return __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.w), __uint_as_float(b.w), c, 0, 0, 0);
+        auto word = [](const uint4 &v, int k) { return __uint_as_float(k == 0 ? v.x : k == 1 ? v.y : k == 2 ? v.z : v.w); };
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int i = 0; i < TM; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(word(w[j], k), word(x[i], k), acc[i][j], 0, 0, 0);
     }
 }
 
@@ -242,7 +266,7 @@ struct RowsCall {
     const int4 *tiles;
     const int32_t *tile_count;
     const uint4 *B;            // fragments: [E][column tiles][steps][64]
-    const float *bias;         // [E][N] or NULL
+    const float *bias;         // [E][n_tiles BN], zeros past N, or NULL
     const void *A, *H;         // rows; H: their mask (kMask)
     void *C;
     int64_t lda, ldc;
@@ -252,22 +276,23 @@ struct RowsCall {
 
 // blocks of a compute unit that the registers leave room for (four wavefronts each)
 template <int TN, int PP, bool kMask>
-constexpr int kRowBlocksPerCu = kMask || TN * PP >= 32 ? 2 : 3;
+constexpr int kRowBlocksPerCu = kMask && TN * PP > 32 ? 2 : 3;
 
-// PP: 16-byte pieces of a row in LDS at a time
+// PP: 16-byte pieces of a row in LDS at a time.  The numbers of a tile's rows are fetched two tiles ahead, its rows one.
 template <typename T, int WN, int TN, int PP, bool kMask, bool kWords, bool kStore16>
 __global__ __launch_bounds__(kGgThreads, (kRowBlocksPerCu<TN, PP, kMask>)) void grouped_rows_kernel(RowsCall q)
 {
     constexpr int WM = 4 / WN, TM = kTileM / WM / 32, E = Step<T>::E;
     constexpr int kRowsAtOnce = kGgThreads / PP, kPieces = kTileM / kRowsAtOnce;    // of a thread
     constexpr int kSteps = PP / 2, kAhead = 4;
+    typedef RowPiece<T, kWords> P;
     __shared__ uint4 As[kTileM * PP];
-    __shared__ int32_t row_of[kTileM];
+    __shared__ int32_t rows[2][kTileM];        // of this tile and the next, -1: none
     const T *A = static_cast<const T *>(q.A), *H = static_cast<const T *>(q.H);
-    const int lane = threadIdx.x & 63, l31 = lane & 31, hi = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, hi = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave % WN;
-    const int piece = threadIdx.x % PP, row0 = threadIdx.x / PP;
-    const int64_t extent = (q.gl.n - 1) * q.lda + q.K;
+    const int piece = tid % PP, row0 = tid / PP;
+    const int64_t last = (q.gl.n - 1) * q.lda + q.K - E;
     // pieces of a row exchanged by its number, so that the 16 rows that are read at once lie in all banks
     constexpr int kSpread = PP < 16 ? PP : 16;
     auto place = [](int row, int p) { return row * PP + (p ^ ((row / (16 / kSpread)) & (kSpread - 1))); };
@@ -275,75 +300,92 @@ __global__ __launch_bounds__(kGgThreads, (kRowBlocksPerCu<TN, PP, kMask>)) void 
     Share share(int64_t(*q.tile_count) * q.n_tiles);
     if (share.item >= share.end) return;
     const int chunks = (q.steps + kSteps - 1) / kSteps;
-    const bool ragged = q.K % E != 0;
+    const bool ragged = kWords && q.K % E != 0;
 
-    int32_t ids[kPieces];          // rows of this thread's pieces, of the tile that is fetched
+    auto row_of = [&](int64_t item) {          // of thread tid < 64
+        const int4 t = q.tiles[item / q.n_tiles];
+        return tid < t.z ? int32_t(q.gl.row(t.y + tid)) : -1;
+    };
+    auto element = [&](int at, int i, int chunk) {
+        const int v = rows[at][row0 + i * kRowsAtOnce], k = (chunk * PP + piece) * E;
+        return int64_t(v < 0 ? 0 : v) * q.lda + (k < q.K ? k : 0);
+    };
     uint4 held[kPieces], mask[kMask ? kPieces : 1];
-    auto rows_of = [&](const int4 &t) {
+    auto fetch = [&](int at, int chunk) {
+        const int valid = q.K - (chunk * PP + piece) * E;
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
-            const int r = row0 + i * kRowsAtOnce;
-            const int64_t v = q.gl.row(t.y + (r < t.z ? r : t.z - 1));
-            ids[i] = r < t.z ? int32_t(v) : -1;
-        }
-    };
-    auto fetch = [&](int chunk) {
-        const int k = (chunk * PP + piece) * E, valid = q.K - k;
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const int64_t at = int64_t(ids[i] < 0 ? 0 : ids[i]) * q.lda + k;
-            held[i] = fetch_piece<T, kWords>(A, at, valid, extent);
-            if constexpr (kMask) mask[i] = fetch_piece<T, kWords>(H, at, valid, extent);
+            const int64_t e = element(at, i, chunk);
+            held[i] = P::load(A, e, valid, last);
+            if constexpr (kMask) mask[i] = P::load(H, e, valid, last);
         }
     };
 
-    int4 tile = q.tiles[share.item / q.n_tiles];
-    rows_of(tile);
-    fetch(0);
-    for (;;) {
+    if (tid < kTileM) rows[0][tid] = row_of(share.item);
+    int32_t pending = -1;                      // of the tile after this one
+    if (tid < kTileM && share.item + share.stride < share.end) pending = row_of(share.item + share.stride);
+    __syncthreads();
+    fetch(0, 0);
+    for (int at = 0;; at ^= 1) {
         const int64_t item = share.item, next = item + share.stride;
         const bool more = next < share.end;
+        const int group = q.tiles[item / q.n_tiles].x;
         const int nt = int(item % q.n_tiles) * WN * TN + wn * TN;      // first of the wavefront's column tiles
         const int n0 = nt * 32 + hi * TN * 16;                         // first of the lane's columns
-        const uint4 *B = q.B + (int64_t(tile.x) * q.n_tiles * WN * TN + nt) * q.steps * kWave + lane;
+        const uint4 *B = q.B + (int64_t(group) * q.n_tiles * WN * TN + nt) * q.steps * kWave;
+        auto weights = [&](int j, int step) { return B[uint32_t((j * q.steps + step) * kWave + lane)]; };
         floatx16 acc[TM][TN];
+        if (q.bias) {
+            const float4 *b4 = reinterpret_cast<const float4 *>(q.bias + int64_t(group) * q.n_tiles * (WN * TN * 32) + n0);
 #pragma unroll
-        for (int j = 0; j < TN; ++j)
+            for (int j = 0; j < TN; ++j)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int col = n0 + j * 16 + r;
-                const float b = q.bias && col < q.N ? q.bias[int64_t(tile.x) * q.N + col] : 0.0f;
+                for (int r = 0; r < 4; ++r) {
+                    const float4 b = b4[j * 4 + r];
 #pragma unroll
-                for (int i = 0; i < TM; ++i) acc[i][j][r] = b;
-            }
-        int4 coming = tile;
-        if (more) coming = q.tiles[next / q.n_tiles];
+                    for (int i = 0; i < TM; ++i) {
+                        acc[i][j][4 * r] = b.x;
+                        acc[i][j][4 * r + 1] = b.y;
+                        acc[i][j][4 * r + 2] = b.z;
+                        acc[i][j][4 * r + 3] = b.w;
+                    }
+                }
+        } else {
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+        }
         for (int c = 0; c < chunks; ++c) {
-            __syncthreads();           // everyone has read what was there
-            if (piece == 0 && c == 0) {
-#pragma unroll
-                for (int i = 0; i < kPieces; ++i) row_of[row0 + i * kRowsAtOnce] = ids[i];
-            }
-            const int valid = q.K - (c * PP + piece) * E;
-#pragma unroll
-            for (int i = 0; i < kPieces; ++i) {
-                uint4 p = held[i];
-                if constexpr (kMask) p = open_piece<T>(p, mask[i]);
-                if (ragged) p = cut_piece<T>(p, valid);
-                As[place(row0 + i * kRowsAtOnce, piece)] = p;
-            }
-            __syncthreads();
-            if (c + 1 < chunks) fetch(c + 1);
-            else if (more) {
-                if (next / q.n_tiles != item / q.n_tiles) rows_of(coming);
-                fetch(0);
-            }
             const int s0 = c * kSteps, s1 = q.steps - s0 < kSteps ? q.steps - s0 : kSteps;
             uint4 b[kAhead][TN];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u)
 #pragma unroll
-                for (int j = 0; j < TN; ++j) b[u][j] = B[(int64_t(j) * q.steps + s0 + (u < s1 ? u : s1 - 1)) * kWave];
+                for (int j = 0; j < TN; ++j) b[u][j] = weights(j, s0 + (u < s1 ? u : s1 - 1));
+            __syncthreads();           // everyone has read what was there
+            const int valid = q.K - (c * PP + piece) * E;
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                uint4 p = held[i];
+                if constexpr (kMask) p = open_piece<T>(p, mask[i]);
+                if (ragged) {
+                    const int64_t over = element(at, i, c) - last;
+                    if (over > 0) p = P::moved(p, int(over));
+                    p = P::cut(p, valid);
+                } else if (valid <= 0) p = make_uint4(0u, 0u, 0u, 0u);
+                As[place(row0 + i * kRowsAtOnce, piece)] = p;
+            }
+            if (c == 0 && tid < kTileM) rows[at ^ 1][tid] = pending;
+            __syncthreads();
+            if (c + 1 < chunks) fetch(at, c + 1);
+            else if (more) {
+                fetch(at ^ 1, 0);
+                pending = -1;
+                if (tid < kTileM && next + share.stride < share.end) pending = row_of(next + share.stride);
+            }
             for (int s = 0; s < s1; s += kAhead) {
 #pragma unroll
                 for (int u = 0; u < kAhead; ++u) {
@@ -351,13 +393,10 @@ __global__ __launch_bounds__(kGgThreads, (kRowBlocksPerCu<TN, PP, kMask>)) void 
                     uint4 a[TM];
 #pragma unroll
                     for (int i = 0; i < TM; ++i) a[i] = As[place((wm * TM + i) * 32 + l31, 2 * (s + u) + hi)];
-#pragma unroll
-                    for (int j = 0; j < TN; ++j)
-#pragma unroll
-                        for (int i = 0; i < TM; ++i) acc[i][j] = multiply<T>(b[u][j], a[i], acc[i][j]);
+                    multiply<T, TM, TN>(b[u], a, acc);
                     const int ahead = s + u + kAhead < s1 ? s + u + kAhead : s1 - 1;
 #pragma unroll
-                    for (int j = 0; j < TN; ++j) b[u][j] = B[(int64_t(j) * q.steps + s0 + ahead) * kWave];
+                    for (int j = 0; j < TN; ++j) b[u][j] = weights(j, s0 + ahead);
                 }
             }
         }
@@ -365,7 +404,7 @@ __global__ __launch_bounds__(kGgThreads, (kRowBlocksPerCu<TN, PP, kMask>)) void 
         T *C = static_cast<T *>(q.C);
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
-            const int64_t v = row_of[(wm * TM + i) * 32 + l31];
+            const int64_t v = rows[at][(wm * TM + i) * 32 + l31];
             if (v < 0) continue;
             T *out = C + v * q.ldc + n0;
 #pragma unroll
@@ -396,7 +435,6 @@ __global__ __launch_bounds__(kGgThreads, (kRowBlocksPerCu<TN, PP, kMask>)) void 
         }
         if (!more) return;
         share.item = next;
-        tile = coming;
     }
 }
 
@@ -407,7 +445,7 @@ struct WeightCall {
     const int32_t *first;          // runs of each group before it, [E + 1]
     const void *X, *G, *H;         // H: the mask of G (kMask)
     int64_t ldx, ldg;
-    int M, N, m_tiles, n_tiles;    // of 128
+    int M, N, m_tiles, n_tiles;
     float *dW, *db;                // [E][M][N], [E][N] or NULL
     float *partial, *colsum;       // of each run: [M][N], [N]
 };
@@ -422,111 +460,151 @@ __device__ __forceinline__ uint4 along_rows(const uint16_t *at, int row)
     return make_uint4(lo.x, lo.y, hi.x, hi.y);
 }
 
-template <typename T, bool kMask, bool kWords>
-__global__ __launch_bounds__(kGgThreads, 2) void grouped_weight_kernel(WeightCall q)
-{
-    constexpr int E = Step<T>::E, kCols = 128, kSlab = sizeof(T) == 2 ? 32 : 16;       // rows of a slab: 8 KB an operand
-    constexpr int PP = kCols / E, kRowsAtOnce = kGgThreads / PP;                       // 16 pieces, 16 rows; 32 pieces, 8 rows
-    static_assert(kSlab == 2 * kRowsAtOnce, "two pieces a thread and operand");
-    __shared__ __attribute__((aligned(16))) T Xs[kSlab * kCols];
-    __shared__ __attribute__((aligned(16))) T Zs[kSlab * kCols];
-    __shared__ float sums[kRowsAtOnce][kCols];
-    const T *X = static_cast<const T *>(q.X), *G = static_cast<const T *>(q.G), *H = static_cast<const T *>(q.H);
-    const int lane = threadIdx.x & 63, l31 = lane & 31, hi = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = wave / 2, wn = wave % 2;
-    const int piece = threadIdx.x % PP, row0 = threadIdx.x / PP;
-    const int64_t x_extent = (q.gl.n - 1) * q.ldx + q.M, g_extent = (q.gl.n - 1) * q.ldg + q.N;
-    const int tiles = q.m_tiles * q.n_tiles;
+// One operand's slabs of ROWS rows x COLS columns on their way through registers into LDS: kDepth slabs in flight.
+template <typename T, int ROWS, int COLS, int THREADS, bool kWords>
+struct SlabPieces {
+    static constexpr int E = 16 / sizeof(T), PP = COLS / E, kAtOnce = THREADS / PP, kPieces = ROWS / kAtOnce;
+    static_assert(kPieces >= 1 && kPieces * kAtOnce == ROWS, "pieces of a slab");
+    typedef RowPiece<T, kWords> P;
     // bf16: blocks of 32 columns exchanged by the row's number, for the transposing read takes 4 rows x 16 columns at once
-    auto place = [](int row, int c) { return row * kCols + (sizeof(T) == 2 ? ((c >> 5) ^ (row & 3)) * 32 + (c & 31) : c); };
+    static __device__ __forceinline__ int place(int row, int c) { return row * COLS + (sizeof(T) == 2 ? ((c >> 5) ^ (row & 3)) * 32 + (c & 31) : c); }
+    static __device__ __forceinline__ int row(int i) { return int(threadIdx.x) / PP + i * kAtOnce; }
+    static __device__ __forceinline__ int column() { return int(threadIdx.x) % PP * E; }
+};
+
+// A block's tile is (WM TM 32) x (WN TN 32); kDepth slabs of rows are in flight in registers, two in LDS (one barrier a slab).
+template <typename T, int WM, int WN, int TM, int TN, bool kMask, bool kWords>
+__global__ __launch_bounds__(WM *WN * 64, 2) void grouped_weight_kernel(WeightCall q)
+{
+    constexpr int kThreads = WM * WN * 64, BM = WM * TM * 32, BN = WN * TN * 32, kDepth = 2;
+    constexpr int E = Step<T>::E, kSlab = sizeof(T) == 2 ? 32 : 16;
+    constexpr int kListed = 64 * kSlab;                    // rows whose numbers lie in LDS, twice: these and the ones to come
+    typedef SlabPieces<T, kSlab, BM, kThreads, kWords> XS;
+    typedef SlabPieces<T, kSlab, BN, kThreads, kWords> ZS;
+    typedef RowPiece<T, kWords> P;
+    __shared__ __attribute__((aligned(16))) T Xs[2][kSlab * BM];
+    __shared__ __attribute__((aligned(16))) T Zs[2][kSlab * BN];
+    __shared__ int32_t listed[2][kListed];
+    const T *X = static_cast<const T *>(q.X), *G = static_cast<const T *>(q.G), *H = static_cast<const T *>(q.H);
+    const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, hi = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / WN, wn = wave % WN;
+    const int64_t x_last = (q.gl.n - 1) * q.ldx + q.M - E, g_last = (q.gl.n - 1) * q.ldg + q.N - E;
+    const int tiles = q.m_tiles * q.n_tiles;
     const int quarter = lane >> 4, i16 = lane & 15;
     const int tr_row = 8 * (quarter >> 1) + (i16 >> 2), tr_col = 16 * (quarter & 1) + 4 * (i16 & 3);
 
     Share share(int64_t(q.first[q.gl.E]) * tiles);
     for (; share.item < share.end; share.item += share.stride) {
         const int64_t run = share.item / tiles;
-        const int tile = int(share.item % tiles), m0 = tile / q.n_tiles * kCols, n0 = tile % q.n_tiles * kCols;
+        const int tile = int(share.item % tiles), m0 = tile / q.n_tiles * BM, n0 = tile % q.n_tiles * BN;
         const int4 t = q.runs[run];
         const int slabs = (t.z + kSlab - 1) / kSlab;
         const bool sum = m0 == 0 && q.db;
-        uint4 xh[2], gh[2], hh[2];
-        int32_t ids[2];
-        const int mv = q.M - (m0 + piece * E), nv = q.N - (n0 + piece * E);
-        auto rows_of = [&](int slab) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int r = slab * kSlab + row0 + i * kRowsAtOnce;
-                ids[i] = r < t.z ? int32_t(q.gl.row(t.y + r)) : -1;
+        const int xc = m0 + XS::column(), zc = n0 + ZS::column(), xv = q.M - xc, zv = q.N - zc;
+        const bool x_ragged = kWords && q.M % E != 0, z_ragged = kWords && q.N % E != 0;
+        auto list = [&](int block) {           // numbers of the rows [block kListed, + kListed) of the run
+            for (int r = tid; r < kListed; r += kThreads) {
+                const int at = block * kListed + r;
+                listed[block & 1][r] = at < t.z ? int32_t(q.gl.row(t.y + at)) : -1;
             }
         };
-        auto fetch = [&]() {
+        auto row = [&](int slab, int r) { return listed[slab / 64 & 1][slab % 64 * kSlab + r]; };
+        uint4 xh[kDepth][XS::kPieces], zh[kDepth][ZS::kPieces], hh[kDepth][kMask ? ZS::kPieces : 1];
+        auto fetch = [&](int slab, int d) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int64_t v = ids[i];
-                xh[i] = fetch_piece<T, kWords>(X, v * q.ldx + m0 + piece * E, v < 0 ? 0 : mv, x_extent);
-                gh[i] = fetch_piece<T, kWords>(G, v * q.ldg + n0 + piece * E, v < 0 ? 0 : nv, g_extent);
-                if constexpr (kMask) hh[i] = fetch_piece<T, kWords>(H, v * q.ldg + n0 + piece * E, v < 0 ? 0 : nv, g_extent);
+            for (int i = 0; i < XS::kPieces; ++i) {
+                const int v = row(slab, XS::row(i));
+                xh[d][i] = P::load(X, int64_t(v < 0 ? 0 : v) * q.ldx + (xv > 0 ? xc : 0), v < 0 ? 0 : xv, x_last);
+            }
+#pragma unroll
+            for (int i = 0; i < ZS::kPieces; ++i) {
+                const int v = row(slab, ZS::row(i));
+                const int64_t e = int64_t(v < 0 ? 0 : v) * q.ldg + (zv > 0 ? zc : 0);
+                zh[d][i] = P::load(G, e, v < 0 ? 0 : zv, g_last);
+                if constexpr (kMask) hh[d][i] = P::load(H, e, v < 0 ? 0 : zv, g_last);
             }
         };
-        floatx16 acc[2][2];
+        floatx16 acc[TM][TN];
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+            for (int j = 0; j < TN; ++j)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
         float col[E];
 #pragma unroll
         for (int j = 0; j < E; ++j) col[j] = 0.0f;
-        rows_of(0);
-        fetch();
-        if (slabs > 1) rows_of(1);
-        for (int s = 0; s < slabs; ++s) {
-            __syncthreads();
+        __syncthreads();                       // (the run before is done with LDS)
+        list(0);
+        __syncthreads();
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int r = row0 + i * kRowsAtOnce;
-                uint4 g = gh[i];
-                if constexpr (kMask) g = open_piece<T>(g, hh[i]);
-                *reinterpret_cast<uint4 *>(&Xs[place(r, piece * E)]) = xh[i];
-                *reinterpret_cast<uint4 *>(&Zs[place(r, piece * E)]) = g;
-                if (sum) {
-                    float v[E];
-                    Chunk<T>::widen(g, v);
+        for (int d = 0; d < kDepth; ++d)
+            if (d < slabs) fetch(d, d);
+        for (int s0 = 0; s0 < slabs; s0 += kDepth) {
 #pragma unroll
-                    for (int j = 0; j < E; ++j) col[j] += v[j];
-                }
-            }
-            __syncthreads();
-            if (s + 1 < slabs) fetch();
-            if (s + 2 < slabs) rows_of(s + 2);
-            if constexpr (sizeof(T) == 2) {
+            for (int d = 0; d < kDepth; ++d) {
+                const int s = s0 + d;
+                if (s >= slabs) break;
+                T *x = Xs[s & 1], *z = Zs[s & 1];
 #pragma unroll
-                for (int k = 0; k < kSlab; k += 16) {
-                    uint4 a[2], b[2];
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        a[i] = along_rows(&Xs[place(k + tr_row, (wm * 2 + i) * 32 + tr_col)], kCols);
-                        b[i] = along_rows(&Zs[place(k + tr_row, (wn * 2 + i) * 32 + tr_col)], kCols);
+                for (int i = 0; i < XS::kPieces; ++i) {
+                    const int v = row(s, XS::row(i));
+                    uint4 p = xh[d][i];
+                    if (x_ragged && v >= 0) {
+                        const int64_t over = int64_t(v) * q.ldx + (xv > 0 ? xc : 0) - x_last;
+                        if (over > 0) p = P::moved(p, int(over));
                     }
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-#pragma unroll
-                        for (int j = 0; j < 2; ++j) acc[i][j] = multiply<T>(a[i], b[j], acc[i][j]);
+                    if (v < 0) p = make_uint4(0u, 0u, 0u, 0u);
+                    *reinterpret_cast<uint4 *>(&x[XS::place(XS::row(i), XS::column())]) = p;
                 }
-            } else {
 #pragma unroll
-                for (int k = 0; k < kSlab; k += 2) {
-                    float a[2], b[2];
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        a[i] = Xs[(k + hi) * kCols + (wm * 2 + i) * 32 + l31];
-                        b[i] = Zs[(k + hi) * kCols + (wn * 2 + i) * 32 + l31];
+                for (int i = 0; i < ZS::kPieces; ++i) {
+                    const int v = row(s, ZS::row(i));
+                    uint4 p = zh[d][i];
+                    if constexpr (kMask) p = open_piece<T>(p, hh[d][i]);
+                    if (z_ragged && v >= 0) {
+                        const int64_t over = int64_t(v) * q.ldg + (zv > 0 ? zc : 0) - g_last;
+                        if (over > 0) p = P::moved(p, int(over));
                     }
+                    if (v < 0) p = make_uint4(0u, 0u, 0u, 0u);
+                    *reinterpret_cast<uint4 *>(&z[ZS::place(ZS::row(i), ZS::column())]) = p;
+                    if (sum) {
+                        float w[E];
+                        Chunk<T>::widen(p, w);
 #pragma unroll
-                    for (int i = 0; i < 2; ++i)
+                        for (int j = 0; j < E; ++j) col[j] += w[j];
+                    }
+                }
+                if (s % 64 == 0 && (s + 64) < slabs) list(s / 64 + 1);       // (in use from slab s + 64 - kDepth on, some barriers away)
+                __syncthreads();
+                if (s + kDepth < slabs) fetch(s + kDepth, d);
+                if constexpr (sizeof(T) == 2) {
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[j], acc[i][j], 0, 0, 0);
+                    for (int k = 0; k < kSlab; k += 16) {
+                        uint4 a[TM], b[TN];
+#pragma unroll
+                        for (int i = 0; i < TM; ++i) a[i] = along_rows(&x[XS::place(k + tr_row, (wm * TM + i) * 32 + tr_col)], BM);
+#pragma unroll
+                        for (int j = 0; j < TN; ++j) b[j] = along_rows(&z[ZS::place(k + tr_row, (wn * TN + j) * 32 + tr_col)], BN);
+#pragma unroll
+                        for (int i = 0; i < TM; ++i)
+#pragma unroll
+                            for (int j = 0; j < TN; ++j)
+                                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a[i]), __builtin_bit_cast(bf16x8, b[j]), acc[i][j], 0, 0, 0);
+                    }
+                } else {
+#pragma unroll
+                    for (int k = 0; k < kSlab; k += 2) {
+                        float a[TM], b[TN];
+#pragma unroll
+                        for (int i = 0; i < TM; ++i) a[i] = x[(k + hi) * BM + (wm * TM + i) * 32 + l31];
+#pragma unroll
+                        for (int j = 0; j < TN; ++j) b[j] = z[(k + hi) * BN + (wn * TN + j) * 32 + l31];
+#pragma unroll
+                        for (int i = 0; i < TM; ++i)
+#pragma unroll
+                            for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[j], acc[i][j], 0, 0, 0);
+                    }
                 }
             }
         }
@@ -534,29 +612,32 @@ __global__ __launch_bounds__(kGgThreads, 2) void grouped_weight_kernel(WeightCal
         float *out = only ? q.dW + int64_t(t.x) * q.M * q.N : q.partial + run * int64_t(q.M) * q.N;
         // register r of a lane: row 8 (r / 4) + 4 (lane / 32) + r % 4, column lane % 32
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const int m = m0 + (wm * 2 + i) * 32 + 8 * (r / 4) + 4 * hi + r % 4;
+                const int m = m0 + (wm * TM + i) * 32 + 8 * (r / 4) + 4 * hi + r % 4;
                 if (m < q.M) {
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const int n = n0 + (wn * 2 + j) * 32 + l31;
+                    for (int j = 0; j < TN; ++j) {
+                        const int n = n0 + (wn * TN + j) * 32 + l31;
                         if (n < q.N) out[int64_t(m) * q.N + n] = acc[i][j][r];
                     }
                 }
             }
-        if (sum) {      // (uniform over the block)
+        if (sum) {      // (uniform over the block); the threads that share a column, in order
             __syncthreads();
+            float *sums = reinterpret_cast<float *>(&Zs[0][0]);       // [kAtOnce][BN]
+            static_assert(sizeof(float) * ZS::kAtOnce * BN <= sizeof(Zs), "room for the column sums");
 #pragma unroll
-            for (int j = 0; j < E; ++j) sums[row0][piece * E + j] = col[j];
+            for (int j = 0; j < E; ++j) sums[int(threadIdx.x) / ZS::PP * BN + ZS::column() + j] = col[j];
             __syncthreads();
-            if (threadIdx.x < kCols && n0 + int(threadIdx.x) < q.N) {
-                float total = 0.0f;
-                for (int r = 0; r < kRowsAtOnce; ++r) total += sums[r][threadIdx.x];
-                float *o = only ? q.db + int64_t(t.x) * q.N : q.colsum + run * q.N;
-                o[n0 + threadIdx.x] = total;
-            }
+            float *o = only ? q.db + int64_t(t.x) * q.N : q.colsum + run * q.N;
+            for (int c = tid; c < BN; c += kThreads)
+                if (n0 + c < q.N) {
+                    float total = 0.0f;
+                    for (int r = 0; r < ZS::kAtOnce; ++r) total += sums[r * BN + c];
+                    o[n0 + c] = total;
+                }
         }
     }
 }
@@ -591,8 +672,9 @@ struct PrepareCall {
     GroupList gl;
     TilePlan rows, runs;                  // room 0: not wanted
     int row_blocks, run_blocks;           // blocks that write them; the others lay out weights
-    const float *W;
+    const float *W, *bias;                // bias (may be NULL): copied to bias_out [E][col_tiles * 32] with zeros past N
     uint4 *B;
+    float *bias_out;
     int K, N, col_tiles, steps, TN;
 };
 
@@ -600,6 +682,9 @@ template <typename T, bool kForward>
 __global__ __launch_bounds__(kGgThreads) void grouped_prepare_kernel(PrepareCall q)
 {
     const int b = blockIdx.x;
+    if (q.bias && b < q.gl.E)
+        for (int c = threadIdx.x; c < q.col_tiles * 32; c += kGgThreads)
+            q.bias_out[int64_t(b) * q.col_tiles * 32 + c] = c < q.N ? q.bias[int64_t(b) * q.N + c] : 0.0f;
     if (b < q.row_blocks) write_plan(q.gl, q.rows, b);
     else if (b < q.row_blocks + q.run_blocks) write_plan(q.gl, q.runs, b - q.row_blocks);
     else write_fragments<T, kForward>(q.gl, q.W, q.K, q.N, q.col_tiles, q.steps, q.TN, q.B, b - q.row_blocks - q.run_blocks,
