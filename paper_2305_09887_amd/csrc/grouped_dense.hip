@@ -243,8 +243,9 @@ static int few_bwd(const char *fn, const GroupList &gl, const void *X, int64_t l
 static bool few_rows_a_group(int64_t n, int E) { return n <= 16 * int64_t(E); }
 
 struct TileShape {
-    int TN, BN;            // 32-column tiles of a wavefront, columns of a block's tile
-    int steps, n_tiles;
+    bool resident;         // weights in LDS, tiles of 32 rows; else tiles of 64 rows that fetch them
+    int TN, BN;            // column tiles of 32 whose columns are shuffled together, columns of a part of the result
+    int steps, n_tiles, height;
     size_t fragment_bytes, bias_bytes;
 };
 
@@ -253,10 +254,26 @@ static TileShape tile_shape(int E, int K, int N, size_t elem)
 {
     TileShape t;
     const int step = int(32 / elem);
-    t.TN = N > 128 ? 2 : 1;
-    t.BN = N > 128 ? 256 : N > 64 ? 128 : 64;
-    t.steps = int(ceil_div(K, step));
-    t.n_tiles = int(ceil_div(N, t.BN));
+    t.steps = int(round_up(size_t(ceil_div(K, step)), kAhead));
+    // column tiles that fit LDS beside each other; pairs
+    int cols = kResPieces / (t.steps * kWave) / 2 * 2;
+    const bool multi = t.steps > kResSteps;
+    if (multi && cols > kResChunkCols) cols = kResChunkCols;
+    t.resident = cols >= 2;
+    if (t.resident) {
+        if (cols > 8) cols = 8;
+        const int want = int(ceil_div(N, 64)) * 2;
+        t.n_tiles = int(ceil_div(want, cols));
+        const int each = int(ceil_div(want, 2 * t.n_tiles)) * 2;       // parts alike
+        t.BN = each * 32;
+        t.TN = elem == 2 ? 2 : 1;
+        t.height = kResRows;
+    } else {
+        t.TN = N > 128 ? 2 : 1;
+        t.BN = N > 128 ? 256 : N > 64 ? 128 : 64;
+        t.n_tiles = int(ceil_div(N, t.BN));
+        t.height = kTileM;
+    }
     t.fragment_bytes = round_up(size_t(E) * size_t(t.n_tiles) * size_t(t.BN / 32) * size_t(t.steps) * 1024, 256);
     t.bias_bytes = round_up(size_t(E) * size_t(t.n_tiles) * size_t(t.BN) * 4, 256);
     return t;
@@ -319,7 +336,6 @@ static void launch_rows_as(const RowsCall &q, bool words, bool store16, int64_t 
     if (per_die > 32 * kPerCu) per_die = 32 * kPerCu;
     const dim3 grid(unsigned(per_die * kDies));
     if (words && store16) hipLaunchKernelGGL((grouped_rows_kernel<T, WN, TN, PP, kMask, true, true>), grid, dim3(kGgThreads), 0, s, q);
-    else if (words) hipLaunchKernelGGL((grouped_rows_kernel<T, WN, TN, PP, kMask, true, false>), grid, dim3(kGgThreads), 0, s, q);
     else hipLaunchKernelGGL((grouped_rows_kernel<T, WN, TN, PP, kMask, false, false>), grid, dim3(kGgThreads), 0, s, q);
 }
 
@@ -335,18 +351,28 @@ static int launch_rows(const char *fn, const char *name, const RowsCall &q, cons
 {
     const T *A = static_cast<const T *>(q.A), *H = static_cast<const T *>(q.H);
     const bool words = rows_in_words<T>(A, q.lda, q.gl.n, q.K) && (!kMask || aligned(H, 4));
-    const bool store16 = aligned(q.C, 16) && (size_t(q.ldc) * sizeof(T)) % 16 == 0;
-    const int64_t items = tile_room(q.gl.n, q.gl.E, kTileM) * q.n_tiles;
+    const bool store16 = sizeof(T) == 4 || (aligned(q.C, 4) && q.ldc % 2 == 0);      // (the store needs words, no more)
     TMA_TIMED(name, s);
-    auto pieces = [&](auto wn, auto tn) {
-        constexpr int WN = decltype(wn)::value, TN = decltype(tn)::value;
-        if (t.steps <= 4) launch_rows_as<T, WN, TN, 8, kMask>(q, words, store16, items, s);
-        else if (t.steps <= 8) launch_rows_as<T, WN, TN, 16, kMask>(q, words, store16, items, s);
-        else launch_rows_as<T, WN, TN, 32, kMask>(q, words, store16, items, s);
-    };
-    if (t.BN == 256) pieces(std::integral_constant<int, 4>{}, std::integral_constant<int, 2>{});
-    else if (t.BN == 128) pieces(std::integral_constant<int, 4>{}, std::integral_constant<int, 1>{});
-    else pieces(std::integral_constant<int, 2>{}, std::integral_constant<int, 1>{});
+    if (t.resident) {
+        const ResidentCall r{q.gl, q.tiles, q.tile_count - q.gl.E, q.B, q.bias, q.A, q.H, q.C, q.lda, q.ldc, q.K, q.N, q.steps, q.n_tiles, t.BN / 32, q.relu};
+        const dim3 grid(256), block(kResWaves * 64);      // one block a compute unit: its weights take the LDS
+        auto go = [&](auto nt, auto multi) {
+            constexpr int NT = decltype(nt)::value;
+            constexpr bool kMulti = decltype(multi)::value;
+            if (words && store16) hipLaunchKernelGGL((grouped_resident_kernel<T, NT, kMulti, kMask, true, true>), grid, block, 0, s, r);
+            else hipLaunchKernelGGL((grouped_resident_kernel<T, NT, kMulti, kMask, false, false>), grid, block, 0, s, r);
+        };
+        const std::integral_constant<int, 2> two;
+        const std::integral_constant<int, 4> four;
+        if (t.steps <= kResSteps) go(two, std::false_type{});
+        else if (t.BN == 128) go(four, std::true_type{});
+        else go(two, std::true_type{});
+        return check_launch(fn);
+    }
+    const int64_t items = tile_room(q.gl.n, q.gl.E, kTileM) * q.n_tiles;
+    if (t.BN == 256) launch_rows_as<T, 4, 2, 32, kMask>(q, words, store16, items, s);
+    else if (t.BN == 128) launch_rows_as<T, 4, 1, 32, kMask>(q, words, store16, items, s);
+    else launch_rows_as<T, 2, 1, 32, kMask>(q, words, store16, items, s);
     return check_launch(fn);
 }
 
@@ -380,7 +406,7 @@ static int tiles_fwd(const char *fn, const GroupList &gl, const void *X, int64_t
     char *at = static_cast<char *>(ws);
     PrepareCall p{};
     p.gl = gl;
-    p.rows = plan_at(at, gl.n, gl.E, kTileM);
+    p.rows = plan_at(at, gl.n, gl.E, t.height);
     p.row_blocks = int(ceil_div(p.rows.room, kGgThreads));
     p.W = W;
     p.bias = bias;
@@ -414,7 +440,7 @@ static int tiles_bwd(const char *fn, const GroupList &gl, const void *X, int64_t
     float *colsum = reinterpret_cast<float *>(at);
     at += round_up(size_t(p.runs.room) * size_t(F_out) * 4, 256);
     if (dX) {
-        p.rows = plan_at(at, gl.n, gl.E, kTileM);
+        p.rows = plan_at(at, gl.n, gl.E, t.height);
         p.row_blocks = int(ceil_div(p.rows.room, kGgThreads));
         p.W = W;
         p.B = reinterpret_cast<uint4 *>(at);
@@ -469,7 +495,7 @@ extern "C" size_t tma_grouped_dense_fwd_workspace_bytes(int64_t n, int32_t E, in
     if (n < 0 || E < 1 || F_in < 1 || F_out < 1) return 0;
     if (few_rows_a_group(n, E)) return 256;
     const TileShape t = tile_shape(E, F_in, F_out, dtype == TMA_BF16 ? 2 : 4);
-    return plan_bytes(n, E, kTileM) + t.bias_bytes + t.fragment_bytes;
+    return plan_bytes(n, E, t.height) + t.bias_bytes + t.fragment_bytes;
 }
 
 extern "C" int tma_grouped_dense_fwd(int64_t n, int32_t E, const int32_t *offsets, const int32_t *order, const void *X, int64_t ldx, int32_t F_in,
@@ -501,7 +527,10 @@ extern "C" size_t tma_grouped_dense_bwd_workspace_bytes(int64_t n, int32_t E, in
     const int height = weight_shape(n, E, F_in, F_out).height;
     const size_t runs = size_t(tile_room(n, E, height));
     size_t bytes = plan_bytes(n, E, height) + round_up(runs * size_t(F_in) * size_t(F_out) * 4, 256) + round_up(runs * size_t(F_out) * 4, 256);
-    if (need_dX) bytes += plan_bytes(n, E, kTileM) + tile_shape(E, F_out, F_in, dtype == TMA_BF16 ? 2 : 4).fragment_bytes;
+    if (need_dX) {
+        const TileShape t = tile_shape(E, F_out, F_in, dtype == TMA_BF16 ? 2 : 4);
+        bytes += plan_bytes(n, E, t.height) + t.fragment_bytes;
+    }
     return bytes;
 }
 

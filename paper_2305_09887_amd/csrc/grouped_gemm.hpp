@@ -31,6 +31,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 constexpr int kDies = 8;             // workgroups are dealt round-robin to them
 constexpr int kTileM = 64;           // rows of a tile
 constexpr int kGgThreads = 256;
+constexpr int kAhead = 4;            // steps that weights are fetched ahead; a product's steps are filled up with zeros to a multiple of it
 constexpr int kMaxGroups = 1024;
 
 struct GroupList {
@@ -157,9 +158,7 @@ __device__ __forceinline__ void write_fragments(const GroupList &gl, const float
 }
 
 // ---- pieces of rows ----------------------------------------------------------------
-struct __attribute__((packed, aligned(4))) Words4 {
-    uint32_t w[4];
-};
+typedef uint32_t Words4 __attribute__((ext_vector_type(4), aligned(4)));
 
 __device__ __forceinline__ uint32_t bits1(const float *p) { return __float_as_uint(*p); }
 __device__ __forceinline__ uint32_t bits1(const uint16_t *p) { return *p; }
@@ -174,7 +173,7 @@ struct RowPiece {
     {
         if constexpr (kWords) {
             const Words4 w = *reinterpret_cast<const Words4 *>(x + (at < last ? at : last));
-            return make_uint4(w.w[0], w.w[1], w.w[2], w.w[3]);
+            return make_uint4(w.x, w.y, w.z, w.w);
         } else {
             uint32_t w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
@@ -211,7 +210,14 @@ struct RowPiece {
     }
 };
 
-// g where h > 0 (a NaN in h: not), zeros elsewhere
+// open_word, open_piece: g where h > 0 (a NaN in h: not), zeros elsewhere
+template <typename T>
+__device__ __forceinline__ uint4 from_words(const T *p)
+{
+    const Words4 w = *reinterpret_cast<const Words4 *>(p);
+    return make_uint4(w.x, w.y, w.z, w.w);
+}
+
 template <typename T>
 __device__ __forceinline__ uint32_t open_word(uint32_t g, uint32_t h)
 {
@@ -274,9 +280,18 @@ struct RowsCall {
     bool relu;
 };
 
+// Place of a row's piece in LDS, rows of PP pieces: exchanged by the row's number, so that what 16 lanes take at once, a piece each of 16
+// neighbouring rows, lies in all banks.
+template <int PP>
+__device__ __forceinline__ int spread(int row, int piece)
+{
+    constexpr int kSpan = PP < 16 ? PP : 16;
+    return row * PP + (piece ^ ((row / (16 / kSpan)) & (kSpan - 1)));
+}
+
 // blocks of a compute unit that the registers leave room for (four wavefronts each)
 template <int TN, int PP, bool kMask>
-constexpr int kRowBlocksPerCu = kMask && TN * PP > 32 ? 2 : 3;
+constexpr int kRowBlocksPerCu = TN * PP > 32 ? 2 : 3;
 
 // PP: 16-byte pieces of a row in LDS at a time.  The numbers of a tile's rows are fetched two tiles ahead, its rows one.
 template <typename T, int WN, int TN, int PP, bool kMask, bool kWords, bool kStore16>
@@ -284,26 +299,25 @@ __global__ __launch_bounds__(kGgThreads, (kRowBlocksPerCu<TN, PP, kMask>)) void 
 {
     constexpr int WM = 4 / WN, TM = kTileM / WM / 32, E = Step<T>::E;
     constexpr int kRowsAtOnce = kGgThreads / PP, kPieces = kTileM / kRowsAtOnce;    // of a thread
-    constexpr int kSteps = PP / 2, kAhead = 4;
+    constexpr int kSteps = PP / 2;
     typedef RowPiece<T, kWords> P;
-    __shared__ uint4 As[kTileM * PP];
+    constexpr int kRowPieces = TN * 32 / E;    // of a wavefront's columns of a row
+    constexpr int kOut = 4 * 32 * kRowPieces;
+    __shared__ uint4 As[kTileM * PP > kOut ? kTileM * PP : kOut];
     __shared__ int32_t rows[2][kTileM];        // of this tile and the next, -1: none
     const T *A = static_cast<const T *>(q.A), *H = static_cast<const T *>(q.H);
     const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, hi = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave % WN;
     const int piece = tid % PP, row0 = tid / PP;
     const int64_t last = (q.gl.n - 1) * q.lda + q.K - E;
-    // pieces of a row exchanged by its number, so that the 16 rows that are read at once lie in all banks
-    constexpr int kSpread = PP < 16 ? PP : 16;
-    auto place = [](int row, int p) { return row * PP + (p ^ ((row / (16 / kSpread)) & (kSpread - 1))); };
-
     Share share(int64_t(*q.tile_count) * q.n_tiles);
     if (share.item >= share.end) return;
     const int chunks = (q.steps + kSteps - 1) / kSteps;
     const bool ragged = kWords && q.K % E != 0;
 
+    auto tile_of = [&](int64_t item) { return q.n_tiles == 1 ? item : item / q.n_tiles; };
     auto row_of = [&](int64_t item) {          // of thread tid < 64
-        const int4 t = q.tiles[item / q.n_tiles];
+        const int4 t = q.tiles[tile_of(item)];
         return tid < t.z ? int32_t(q.gl.row(t.y + tid)) : -1;
     };
     auto element = [&](int at, int i, int chunk) {
@@ -329,11 +343,12 @@ __global__ __launch_bounds__(kGgThreads, (kRowBlocksPerCu<TN, PP, kMask>)) void 
     for (int at = 0;; at ^= 1) {
         const int64_t item = share.item, next = item + share.stride;
         const bool more = next < share.end;
-        const int group = q.tiles[item / q.n_tiles].x;
-        const int nt = int(item % q.n_tiles) * WN * TN + wn * TN;      // first of the wavefront's column tiles
+        const int64_t tile = tile_of(item);
+        const int group = __builtin_amdgcn_readfirstlane(q.tiles[tile].x);
+        const int nt = int(item - tile * q.n_tiles) * WN * TN + wn * TN;      // first of the wavefront's column tiles
         const int n0 = nt * 32 + hi * TN * 16;                         // first of the lane's columns
         const uint4 *B = q.B + (int64_t(group) * q.n_tiles * WN * TN + nt) * q.steps * kWave;
-        auto weights = [&](int j, int step) { return B[uint32_t((j * q.steps + step) * kWave + lane)]; };
+        auto weights = [&](int j, int step) { return (B + (j * q.steps + step) * kWave)[lane]; };
         floatx16 acc[TM][TN];
         if (q.bias) {
             const float4 *b4 = reinterpret_cast<const float4 *>(q.bias + int64_t(group) * q.n_tiles * (WN * TN * 32) + n0);
@@ -359,12 +374,12 @@ __global__ __launch_bounds__(kGgThreads, (kRowBlocksPerCu<TN, PP, kMask>)) void 
                     for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
         }
         for (int c = 0; c < chunks; ++c) {
-            const int s0 = c * kSteps, s1 = q.steps - s0 < kSteps ? q.steps - s0 : kSteps;
-            uint4 b[kAhead][TN];
+            const int s0 = c * kSteps, s1 = q.steps - s0 < kSteps ? q.steps - s0 : kSteps;      // a multiple of kAhead
+            uint4 b[kSteps][TN];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u)
 #pragma unroll
-                for (int j = 0; j < TN; ++j) b[u][j] = weights(j, s0 + (u < s1 ? u : s1 - 1));
+                for (int j = 0; j < TN; ++j) b[u][j] = weights(j, s0 + u);
             __syncthreads();           // everyone has read what was there
             const int valid = q.K - (c * PP + piece) * E;
 #pragma unroll
@@ -376,7 +391,7 @@ __global__ __launch_bounds__(kGgThreads, (kRowBlocksPerCu<TN, PP, kMask>)) void 
                     if (over > 0) p = P::moved(p, int(over));
                     p = P::cut(p, valid);
                 } else if (valid <= 0) p = make_uint4(0u, 0u, 0u, 0u);
-                As[place(row0 + i * kRowsAtOnce, piece)] = p;
+                As[spread<PP>(row0 + i * kRowsAtOnce, piece)] = p;
             }
             if (c == 0 && tid < kTileM) rows[at ^ 1][tid] = pending;
             __syncthreads();
@@ -386,55 +401,276 @@ __global__ __launch_bounds__(kGgThreads, (kRowBlocksPerCu<TN, PP, kMask>)) void 
                 pending = -1;
                 if (tid < kTileM && next + share.stride < share.end) pending = row_of(next + share.stride);
             }
-            for (int s = 0; s < s1; s += kAhead) {
+            // unrolled, and each step's loads kept in their place: of a loop the compiler makes copies of what is in flight, and waits for it
 #pragma unroll
-                for (int u = 0; u < kAhead; ++u) {
-                    if (s + u >= s1) break;
-                    uint4 a[TM];
+            for (int s = 0; s < kSteps; ++s) {
+                if (s % kAhead == 0 && s >= s1) break;
+                uint4 a[TM];
 #pragma unroll
-                    for (int i = 0; i < TM; ++i) a[i] = As[place((wm * TM + i) * 32 + l31, 2 * (s + u) + hi)];
-                    multiply<T, TM, TN>(b[u], a, acc);
-                    const int ahead = s + u + kAhead < s1 ? s + u + kAhead : s1 - 1;
+                for (int i = 0; i < TM; ++i) a[i] = As[spread<PP>((wm * TM + i) * 32 + l31, 2 * s + hi)];
+                multiply<T, TM, TN>(b[s], a, acc);
+                if (s + kAhead < kSteps) {
+                    const int ahead = s0 + s + kAhead < q.steps ? s0 + s + kAhead : q.steps - 1;     // (past the last one: again)
 #pragma unroll
-                    for (int j = 0; j < TN; ++j) b[u][j] = weights(j, s0 + ahead);
+                    for (int j = 0; j < TN; ++j) b[s + kAhead < kSteps ? s + kAhead : 0][j] = weights(j, ahead);
                 }
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
-        // lane: row l31 of the tile's 32, columns n0 + [0, 16 TN)
+        // A lane has, of row l31 of the tile's 32, the columns [0, 16 TN) or the next as many of its wavefront's.  Through LDS, 32 rows at a
+        // time: a store then goes to whole rows of the wavefront's columns, 64 to 256 bytes each.  (From registers it went to a piece of 64 rows,
+        // and the L2's requests bounded the kernel: see below.)
         T *C = static_cast<T *>(q.C);
+        __syncthreads();               // everyone has read the last steps
+        uint4 *mine = As + wave * (32 * kRowPieces);
+        const int col0 = nt * 32;      // the wavefront's first column
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
-            const int64_t v = rows[at][(wm * TM + i) * 32 + l31];
-            if (v < 0) continue;
-            T *out = C + v * q.ldc + n0;
 #pragma unroll
-            for (int j = 0; j < TN; ++j) {
-                float z[16];
+            for (int x = 0; x < TN * 16 / E; ++x) {
+                float z[E];
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    z[r] = acc[i][j][r];
-                    if (q.relu) z[r] = z[r] > 0.0f ? z[r] : 0.0f;
+                for (int y = 0; y < E; ++y) {
+                    z[y] = acc[i][x * E / 16][x * E % 16 + y];
+                    if (q.relu) z[y] = z[y] > 0.0f ? z[y] : 0.0f;
                 }
-                if (kStore16 && n0 + j * 16 + 16 <= q.N) {
+                Chunk<T>::store(reinterpret_cast<T *>(&mine[spread<kRowPieces>(l31, hi * (kRowPieces / 2) + x)]), z);
+            }
+            __builtin_amdgcn_wave_barrier();
 #pragma unroll
-                    for (int r = 0; r < 16; r += E) {
-                        float w[E];
-#pragma unroll
-                        for (int x = 0; x < E; ++x) w[x] = z[r + x];
-                        Chunk<T>::store(out + j * 16 + r, w);
-                    }
+            for (int x = 0; x < kRowPieces / 2; ++x) {
+                const int r = x * (64 / kRowPieces) + lane / kRowPieces, p = lane % kRowPieces, col = col0 + p * E;
+                const uint4 z = mine[spread<kRowPieces>(r, p)];
+                const int64_t v = rows[at][(wm * TM + i) * 32 + r];
+                if (v < 0 || col >= q.N) continue;
+                T *out = C + v * q.ldc + col;
+                if (kStore16 && col + E <= q.N) {
+                    *reinterpret_cast<Words4 *>(out) = Words4{z.x, z.y, z.z, z.w};
                 } else {
+                    float w[E];
+                    Chunk<T>::widen(z, w);
 #pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (n0 + j * 16 + r < q.N) {
-                            if constexpr (sizeof(T) == 4) out[j * 16 + r] = z[r];
-                            else out[j * 16 + r] = f32_to_bf16(z[r]);
+                    for (int y = 0; y < E; ++y)
+                        if (col + y < q.N) {
+                            if constexpr (sizeof(T) == 4) out[y] = w[y];
+                            else out[y] = uint16_t(__float_as_uint(w[y]) >> 16);
                         }
                 }
             }
+            __builtin_amdgcn_wave_barrier();
         }
         if (!more) return;
         share.item = next;
+    }
+}
+
+// ---- rows times weights that stay in LDS -----------------------------------------------
+// Where a group's weights, or those of 64 to 256 of its columns, fit 128 KB of LDS (256 x 256 of bf16, 128 x 256 of fp32), a block per compute unit
+// holds them for a run of the group's rows.  Its eight wavefronts then have nothing in common: each takes 32 rows at a time,
+// its lanes' k-values of a row straight into registers (512 bytes of a row: sixteen steps), all columns from them, and the
+// results through 4 KB of LDS of its own into whole lines.  No barrier but where the weights change, and of the L2 only rows and
+// results are asked (64-row tiles that fetched the weights from it: 128 KB a tile beside 64 KB of rows and results; 1,000,003 rows of
+// 256 -> 256 in bf16 268 us; without rows and stores still 175).
+constexpr int kResWaves = 8;
+constexpr int kResRows = 32;              // rows of a wavefront's tile
+constexpr int kResSteps = 16;             // steps of a chunk of k-values
+constexpr int kResPieces = 8192;          // 16-byte pieces of weights in LDS
+constexpr int kResChunkCols = 4;          // column tiles where a row has several chunks: all their sums are in registers
+
+struct ResidentCall {
+    GroupList gl;
+    const int4 *tiles;
+    const int32_t *first;      // tiles of the groups before each one, [E + 1]
+    const uint4 *B;            // fragments: [E][n_tiles][CT][steps][64]
+    const float *bias;         // [E][n_tiles CT 32], zeros past N, or NULL
+    const void *A, *H;
+    void *C;
+    int64_t lda, ldc;
+    int K, N, steps, n_tiles, CT;      // CT: column tiles of 32 in LDS
+    bool relu;
+};
+
+// NT: column tiles whose sums are in registers at once; kMulti: a row has several chunks (then NT = CT)
+template <typename T, int NT, bool kMulti, bool kMask, bool kWords, bool kStore16>
+__global__ __launch_bounds__(kResWaves * 64, 2) void grouped_resident_kernel(ResidentCall q)
+{
+    constexpr int E = Step<T>::E, TN = sizeof(T) == 2 ? 2 : 1;         // TN column tiles make 128 bytes of a row of results
+    constexpr int kUnit = 8;                                           // pieces of those
+    typedef RowPiece<T, kWords> P;
+    __shared__ uint4 Ws[kResPieces];
+    __shared__ uint4 staging[kResWaves][kResRows * kUnit];
+    const T *A = static_cast<const T *>(q.A), *H = static_cast<const T *>(q.H);
+    T *C = static_cast<T *>(q.C);
+    const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, hi = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int64_t last = (q.gl.n - 1) * q.lda + q.K - E;
+    const bool ragged = kWords && q.K % E != 0;
+    const int chunks = kMulti ? (q.steps + kResSteps - 1) / kResSteps : 1;
+    uint4 *mine = staging[wave];
+
+    // this block's range of the items (group, column part, tile), a die's blocks side by side
+    const int64_t total = int64_t(q.first[q.gl.E]) * q.n_tiles;
+    const int64_t blocks = gridDim.x, b = (blockIdx.x % kDies) * (blocks / kDies) + blockIdx.x / kDies;
+    int64_t item = total * b / blocks;
+    const int64_t end = total * (b + 1) / blocks;
+    if (item >= end) return;
+    int group = 0;
+    for (int lo = 0, hi_ = q.gl.E; hi_ - lo > 1;) {      // the last group that begins at or before the item
+        const int mid = (lo + hi_) / 2;
+        if (int64_t(q.first[mid]) * q.n_tiles <= item) lo = mid;
+        else hi_ = mid;
+        group = lo;
+    }
+    while (item < end) {
+        group = __builtin_amdgcn_readfirstlane(group);
+        const int64_t g0 = q.first[group], g1 = q.first[group + 1], size = g1 - g0;
+        if (item >= g1 * q.n_tiles) {      // (also steps over empty groups)
+            ++group;
+            continue;
+        }
+        const int64_t in_group = item - g0 * q.n_tiles;
+        const int part = int(in_group / size);
+        int64_t t = g0 + in_group % size;                           // tiles [t, t_end) of the plan
+        const int64_t left = end - item, t_end = t + left < g1 ? t + left : g1;
+        item += t_end - t;
+
+        __syncthreads();                                            // everyone is done with the weights before
+        const uint4 *B = q.B + (int64_t(group) * q.n_tiles + part) * q.CT * q.steps * kWave;
+        const int pieces = q.CT * q.steps * kWave;
+        for (int i = tid; i < pieces; i += kResWaves * 64) Ws[i] = B[i];
+        __syncthreads();
+
+        const int n0 = part * q.CT * 32;
+        const float *bias = q.bias ? q.bias + (int64_t(group) * q.n_tiles + part) * q.CT * 32 : nullptr;
+        auto row_of = [&](int64_t tile) {
+            int32_t v = -1;
+            if (tile < t_end) {
+                const int4 d = q.tiles[tile];
+                if (l31 < d.z) v = int32_t(q.gl.row(d.y + l31));
+            }
+            return v;
+        };
+        t += wave;
+        int32_t row = row_of(t), coming = row_of(t + kResWaves);
+        for (; t < t_end; t += kResWaves) {
+            const int32_t after = row_of(t + 2 * kResWaves);
+            const int64_t from = int64_t(row < 0 ? 0 : row) * q.lda;       // (a row that is none reads the first, and is not stored)
+            const T *a = A + from, *h = kMask ? H + from : nullptr;
+            const int limit = last - from < q.K ? int(last - from) : q.K;  // the last place in the row where 16 bytes are left
+            uint4 x[kResSteps];
+            auto fetch = [&](int c) {
+                const int k0 = c * kResSteps * Step<T>::K;
+                if (kWords && !ragged && k0 + kResSteps * Step<T>::K <= q.K) {
+                    const T *ac = a + k0 + hi * E, *hc = kMask ? h + k0 + hi * E : nullptr;
+#pragma unroll
+                    for (int s = 0; s < kResSteps; ++s) x[s] = from_words(ac + s * Step<T>::K);
+                    if constexpr (kMask) {
+                        constexpr int kPart = kMulti ? kResSteps / 4 : kResSteps;      // (registers)
+#pragma unroll
+                        for (int s0 = 0; s0 < kResSteps; s0 += kPart) {
+                            uint4 m[kPart];
+#pragma unroll
+                            for (int s = 0; s < kPart; ++s) m[s] = from_words(hc + (s0 + s) * Step<T>::K);
+#pragma unroll
+                            for (int s = 0; s < kPart; ++s) x[s0 + s] = open_piece<T>(x[s0 + s], m[s]);
+                            if (kMulti) __builtin_amdgcn_sched_barrier(0);
+                        }
+                    }
+                    return;
+                }
+#pragma unroll
+                for (int s = 0; s < kResSteps; ++s)
+                    if (c * kResSteps + s < q.steps) {
+                        const int k = k0 + s * Step<T>::K + hi * E, valid = q.K - k, in_row = valid > 0 ? k : 0;
+                        uint4 p = P::load(a, in_row, valid, limit);
+                        if constexpr (kMask) p = open_piece<T>(p, P::load(h, in_row, valid, limit));
+                        if (kWords && in_row > limit) p = P::moved(p, in_row - limit);
+                        x[s] = kWords ? P::cut(p, valid) : p;
+                    }
+            };
+            floatx16 acc[NT];
+            T *out[4];                     // where this lane stores: rows x * 8 + lane / 8 of the tile
+            bool held[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const int32_t v = __shfl(row, x * 8 + lane / 8, kWave);
+                held[x] = v >= 0;
+                out[x] = C + int64_t(held[x] ? v : 0) * q.ldc + n0 + lane % 8 * E;
+            }
+            auto start = [&](int ct) {
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    const int tile = ct + j;       // its lane's columns: see fragment_column
+                    const float4 *b4 = reinterpret_cast<const float4 *>(bias + tile / TN * TN * 32 + hi * TN * 16 + tile % TN * 16);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float4 v = bias ? b4[r] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                        acc[j][4 * r] = v.x;
+                        acc[j][4 * r + 1] = v.y;
+                        acc[j][4 * r + 2] = v.z;
+                        acc[j][4 * r + 3] = v.w;
+                    }
+                }
+            };
+            auto store = [&](int ct) {
+#pragma unroll
+                for (int unit = 0; unit < NT / TN; ++unit) {
+                    const int col0 = (ct + unit * TN) * 32;        // of the part
+                    if (n0 + col0 >= q.N) break;
+#pragma unroll
+                    for (int x = 0; x < TN * 16 / E; ++x) {
+                        float z[E];
+#pragma unroll
+                        for (int y = 0; y < E; ++y) {
+                            z[y] = acc[unit * TN + x * E / 16][x * E % 16 + y];
+                            if (q.relu) z[y] = z[y] > 0.0f ? z[y] : 0.0f;
+                        }
+                        Chunk<T>::store(reinterpret_cast<T *>(&mine[spread<kUnit>(l31, hi * (kUnit / 2) + x)]), z);
+                    }
+                    __builtin_amdgcn_wave_barrier();
+                    const int col = n0 + col0 + lane % 8 * E;
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const uint4 z = mine[spread<kUnit>(x * 8 + lane / 8, lane % 8)];
+                        if (!held[x] || col >= q.N) continue;
+                        T *o = out[x] + col0;
+                        if (kStore16 && col + E <= q.N) {
+                            *reinterpret_cast<Words4 *>(o) = Words4{z.x, z.y, z.z, z.w};
+                        } else {
+                            float w[E];
+                            Chunk<T>::widen(z, w);
+#pragma unroll
+                            for (int y = 0; y < E; ++y)
+                                if (col + y < q.N) {
+                                    if constexpr (sizeof(T) == 4) o[y] = w[y];
+                                    else o[y] = uint16_t(__float_as_uint(w[y]) >> 16);
+                                }
+                        }
+                    }
+                    __builtin_amdgcn_wave_barrier();
+                }
+            };
+            if (kMulti) start(0);
+            for (int c = 0; c < chunks; ++c) {
+                fetch(c);
+                for (int ct = 0; ct < q.CT; ct += NT) {
+                    if (!kMulti) start(ct);
+#pragma unroll
+                    for (int s = 0; s < kResSteps; ++s) {
+                        if (s % kAhead == 0 && c * kResSteps + s >= q.steps) break;
+                        uint4 w[NT];
+                        const uint4 one[1] = {x[s]};
+#pragma unroll
+                        for (int j = 0; j < NT; ++j) w[j] = Ws[((ct + j) * q.steps + c * kResSteps + s) * kWave + lane];
+                        floatx16(&row_acc)[1][NT] = reinterpret_cast<floatx16(&)[1][NT]>(acc);
+                        multiply<T, 1, NT>(w, one, row_acc);
+                    }
+                    if (!kMulti) store(ct);
+                }
+            }
+            if (kMulti) store(0);
+            row = coming;
+            coming = after;
+        }
     }
 }
 
