@@ -259,7 +259,8 @@ static TileShape tile_shape(int E, int K, int N, size_t elem)
     int cols = kResPieces / (t.steps * kWave) / 2 * 2;
     const bool multi = t.steps > kResSteps;
     if (multi && cols > kResChunkCols) cols = kResChunkCols;
-    t.resident = cols >= 2;
+    // (fp32: bound by its instruction, and few rounds of long tiles: 125,237 rows, 128 -> 256 forward 128 us so, 107 in tiles; back with ReLU 136 and 117)
+    t.resident = elem == 2 && cols >= 2;
     if (t.resident) {
         if (cols > 8) cols = 8;
         const int want = int(ceil_div(N, 64)) * 2;

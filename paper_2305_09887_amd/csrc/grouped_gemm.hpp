@@ -214,7 +214,7 @@ struct RowPiece {
 template <typename T>
 __device__ __forceinline__ uint4 from_words(const T *p)
 {
-    const Words4 w = *reinterpret_cast<const Words4 *>(p);
+    const Words4 w = __builtin_nontemporal_load(reinterpret_cast<const Words4 *>(p));
     return make_uint4(w.x, w.y, w.z, w.w);
 }
 
@@ -553,49 +553,79 @@ __global__ __launch_bounds__(kResWaves * 64, 2) void grouped_resident_kernel(Res
         int32_t row = row_of(t), coming = row_of(t + kResWaves);
         for (; t < t_end; t += kResWaves) {
             const int32_t after = row_of(t + 2 * kResWaves);
-            const int64_t from = int64_t(row < 0 ? 0 : row) * q.lda;       // (a row that is none reads the first, and is not stored)
-            const T *a = A + from, *h = kMask ? H + from : nullptr;
-            const int limit = last - from < q.K ? int(last - from) : q.K;  // the last place in the row where 16 bytes are left
+            // rows x * 8 + lane / 8 of the tile, whose pieces lane % 8, + 8, ... this lane loads and stores
+            const T *a[4], *h[kMask ? 4 : 1];
+            T *out[4];
+            bool held[4];
+            int limit[4];                  // the last place in the row where 16 bytes are left
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const int32_t v = __shfl(row, x * 8 + lane / 8, kWave);
+                held[x] = v >= 0;
+                const int64_t r = held[x] ? v : 0, from = r * q.lda;       // (a row that is none reads the first, and is not stored)
+                a[x] = A + from;
+                if constexpr (kMask) h[x] = H + from;
+                limit[x] = last - from < q.K ? int(last - from) : q.K;
+                out[x] = C + r * q.ldc + n0 + lane % 8 * E;
+            }
+            const bool full = __all(held[0] && held[1] && held[2] && held[3]);
+            // A chunk: 128 bytes of 32 rows at a time through the wavefront's LDS, from whole lines to a row per lane.  (Loads that could go one
+            // way or the other were waited for one by one: the common case has a path without a branch.)
             uint4 x[kResSteps];
+            auto turn = [&](int quarter, const uint4 (&p)[4]) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) mine[spread<kUnit>(r * 8 + lane / 8, lane % 8)] = p[r];
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int s = 0; s < 4; ++s) x[quarter * 4 + s] = mine[spread<kUnit>(l31, 2 * s + hi)];
+                __builtin_amdgcn_wave_barrier();
+            };
             auto fetch = [&](int c) {
-                const int k0 = c * kResSteps * Step<T>::K;
-                if (kWords && !ragged && k0 + kResSteps * Step<T>::K <= q.K) {
-                    const T *ac = a + k0 + hi * E, *hc = kMask ? h + k0 + hi * E : nullptr;
+                const int k0 = c * kResSteps * Step<T>::K + lane % 8 * E;
+                constexpr int kQuarter = 8 * E;
+                if (kWords && !ragged && (c + 1) * kResSteps * Step<T>::K <= q.K) {
+                    constexpr int kTogether = kMask && kMulti ? 1 : 4;         // quarters in flight (registers)
 #pragma unroll
-                    for (int s = 0; s < kResSteps; ++s) x[s] = from_words(ac + s * Step<T>::K);
-                    if constexpr (kMask) {
-                        constexpr int kPart = kMulti ? kResSteps / 4 : kResSteps;      // (registers)
+                    for (int q0 = 0; q0 < 4; q0 += kTogether) {
+                        uint4 p[kTogether][4], m[kMask ? kTogether : 1][4];
 #pragma unroll
-                        for (int s0 = 0; s0 < kResSteps; s0 += kPart) {
-                            uint4 m[kPart];
+                        for (int i = 0; i < kTogether; ++i)
 #pragma unroll
-                            for (int s = 0; s < kPart; ++s) m[s] = from_words(hc + (s0 + s) * Step<T>::K);
+                            for (int r = 0; r < 4; ++r) {
+                                p[i][r] = from_words(a[r] + k0 + (q0 + i) * kQuarter);
+                                if constexpr (kMask) m[i][r] = from_words(h[r] + k0 + (q0 + i) * kQuarter);
+                            }
 #pragma unroll
-                            for (int s = 0; s < kPart; ++s) x[s0 + s] = open_piece<T>(x[s0 + s], m[s]);
-                            if (kMulti) __builtin_amdgcn_sched_barrier(0);
+                        for (int i = 0; i < kTogether; ++i) {
+                            if constexpr (kMask) {
+#pragma unroll
+                                for (int r = 0; r < 4; ++r) p[i][r] = open_piece<T>(p[i][r], m[i][r]);
+                            }
+                            turn(q0 + i, p[i]);
                         }
                     }
                     return;
                 }
 #pragma unroll
-                for (int s = 0; s < kResSteps; ++s)
-                    if (c * kResSteps + s < q.steps) {
-                        const int k = k0 + s * Step<T>::K + hi * E, valid = q.K - k, in_row = valid > 0 ? k : 0;
-                        uint4 p = P::load(a, in_row, valid, limit);
-                        if constexpr (kMask) p = open_piece<T>(p, P::load(h, in_row, valid, limit));
-                        if (kWords && in_row > limit) p = P::moved(p, in_row - limit);
-                        x[s] = kWords ? P::cut(p, valid) : p;
+                for (int quarter = 0; quarter < 4; ++quarter)
+                    if (c * kResSteps + quarter * 4 < q.steps) {
+                        const int k = k0 + quarter * kQuarter, valid = q.K - k, in_row = valid > 0 ? k : 0;
+                        uint4 p[4], m[4];
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            p[r] = P::load(a[r], in_row, valid, limit[r]);
+                            if constexpr (kMask) m[r] = P::load(h[r], in_row, valid, limit[r]);
+                        }
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            if constexpr (kMask) p[r] = open_piece<T>(p[r], m[r]);
+                            if (kWords && in_row > limit[r]) p[r] = P::moved(p[r], in_row - limit[r]);
+                            if (kWords) p[r] = P::cut(p[r], valid);
+                        }
+                        turn(quarter, p);
                     }
             };
             floatx16 acc[NT];
-            T *out[4];                     // where this lane stores: rows x * 8 + lane / 8 of the tile
-            bool held[4];
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const int32_t v = __shfl(row, x * 8 + lane / 8, kWave);
-                held[x] = v >= 0;
-                out[x] = C + int64_t(held[x] ? v : 0) * q.ldc + n0 + lane % 8 * E;
-            }
             auto start = [&](int ct) {
 #pragma unroll
                 for (int j = 0; j < NT; ++j) {
@@ -628,25 +658,28 @@ __global__ __launch_bounds__(kResWaves * 64, 2) void grouped_resident_kernel(Res
                     }
                     __builtin_amdgcn_wave_barrier();
                     const int col = n0 + col0 + lane % 8 * E;
+                    uint4 z[4];
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) z[x] = mine[spread<kUnit>(x * 8 + lane / 8, lane % 8)];
+                    __builtin_amdgcn_wave_barrier();
+                    if (kStore16 && full && n0 + col0 + TN * 32 <= q.N) {
+#pragma unroll
+                        for (int x = 0; x < 4; ++x)
+                            __builtin_nontemporal_store(Words4{z[x].x, z[x].y, z[x].z, z[x].w}, reinterpret_cast<Words4 *>(out[x] + col0));
+                        continue;
+                    }
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
-                        const uint4 z = mine[spread<kUnit>(x * 8 + lane / 8, lane % 8)];
-                        if (!held[x] || col >= q.N) continue;
                         T *o = out[x] + col0;
-                        if (kStore16 && col + E <= q.N) {
-                            *reinterpret_cast<Words4 *>(o) = Words4{z.x, z.y, z.z, z.w};
-                        } else {
-                            float w[E];
-                            Chunk<T>::widen(z, w);
+                        float w[E];
+                        Chunk<T>::widen(z[x], w);
 #pragma unroll
-                            for (int y = 0; y < E; ++y)
-                                if (col + y < q.N) {
-                                    if constexpr (sizeof(T) == 4) o[y] = w[y];
-                                    else o[y] = uint16_t(__float_as_uint(w[y]) >> 16);
-                                }
-                        }
+                        for (int y = 0; y < E; ++y)
+                            if (held[x] && col + y < q.N) {
+                                if constexpr (sizeof(T) == 4) o[y] = w[y];
+                                else o[y] = uint16_t(__float_as_uint(w[y]) >> 16);
+                            }
                     }
-                    __builtin_amdgcn_wave_barrier();
                 }
             };
             if (kMulti) start(0);
