@@ -28,6 +28,7 @@
 // transposed ones evenly over the banks.  An operand that is contiguous along mn is transposed on the way in: a
 // thread holds two k-values of four neighbouring mn, and a bf16 pair along k costs the same to form as one along mn.
 #pragma once
+#include "split_pair.hpp"
 
 namespace tma {
 
@@ -35,35 +36,6 @@ constexpr int kSplitPerCu = 2;        // blocks per compute unit: two waves per 
 constexpr int kSlabK = 16;            // k-values per slab: one v_mfma_f32_32x32x16_bf16
 constexpr int kSplitLd = kSlabK + 8;  // row pitch of a tile plane in bf16 values
 constexpr int kFullLd = kSlabK + 4;   // row pitch in floats where a slab is staged unsplit
-constexpr float kSplitScale = 0x1p24f, kSplitUnscale = 0x1p-48f;   // of both operands; of their product (see Range)
-
-// two values -> their three parts as bf16 pairs (first value in the low half).  What a rounding left over is exact, and
-// comes from one instruction: v - h as the dot product of the pair (h0, h1) with (-1, 0) or (0, -1), plus v.
-struct SplitPair {
-    typedef __bf16 Pair __attribute__((ext_vector_type(2)));
-    uint32_t first, second;
-    __device__ __forceinline__ SplitPair() : first(0x0000BF80u), second(0xBF800000u)
-    {
-        // held in registers: as an inline constant of this instruction -1.0 would stand in the other half
-        asm("" : "+s"(first));
-        asm("" : "+s"(second));
-    }
-    __device__ __forceinline__ float left(float v, uint32_t parts, uint32_t which) const
-    {
-        return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(Pair, parts), __builtin_bit_cast(Pair, which), v, false);
-    }
-    __device__ __forceinline__ void operator()(float x, float y, uint32_t &h, uint32_t &m, uint32_t &l) const
-    {
-        x *= kSplitScale;
-        y *= kSplitScale;
-        h = pack_bf16(x, y);
-        x = left(x, h, first);
-        y = left(y, h, second);
-        m = pack_bf16(x, y);
-        l = pack_bf16(left(x, m, first), left(y, m, second));
-    }
-};
-
 // An optional member of an operand view: in_range(raw) is resolve(raw) for a k inside the operand; rows or columns past
 // its end may then hold anything finite, since their results are not stored.
 template <class View, class = void>

@@ -253,29 +253,30 @@ struct TileShape {
 static TileShape tile_shape(int E, int K, int N, size_t elem)
 {
     TileShape t;
-    const int step = int(32 / elem);
-    t.steps = int(round_up(size_t(ceil_div(K, step)), kAhead));
-    // column tiles that fit LDS beside each other; pairs
-    int cols = kResPieces / (t.steps * kWave) / 2 * 2;
-    const bool multi = t.steps > kResSteps;
-    if (multi && cols > kResChunkCols) cols = kResChunkCols;
-    // (fp32: bound by its instruction, and few rounds of long tiles: 125,237 rows, 128 -> 256 forward 128 us so, 107 in tiles; back with ReLU 136 and 117)
-    t.resident = elem == 2 && cols >= 2;
+    // steps of 16 k-values, filled up to a quarter of a chunk; column tiles that fit LDS beside each other, pairs of them
+    const int parts = elem == 4 ? 3 : 1, chunk = elem == 4 ? 8 : 16;
+    t.steps = int(round_up(size_t(ceil_div(K, 16)), chunk / 4));
+    int cols = kResPieces / (t.steps * parts * kWave) / 2 * 2;
+    const bool multi = t.steps > chunk;
+    const int most = !multi ? 8 : elem == 4 ? 2 : kResChunkCols;
+    if (cols > most) cols = most;
+    t.resident = cols >= 2;
     if (t.resident) {
-        if (cols > 8) cols = 8;
         const int want = int(ceil_div(N, 64)) * 2;
         t.n_tiles = int(ceil_div(want, cols));
         const int each = int(ceil_div(want, 2 * t.n_tiles)) * 2;       // parts alike
         t.BN = each * 32;
         t.TN = elem == 2 ? 2 : 1;
         t.height = kResRows;
+        t.fragment_bytes = round_up(size_t(E) * size_t(t.n_tiles) * size_t(t.BN / 32) * size_t(t.steps) * size_t(parts) * 1024, 256);
     } else {
+        t.steps = int(round_up(size_t(ceil_div(K, int(32 / elem))), kAhead));
         t.TN = N > 128 ? 2 : 1;
         t.BN = N > 128 ? 256 : N > 64 ? 128 : 64;
         t.n_tiles = int(ceil_div(N, t.BN));
         t.height = kTileM;
+        t.fragment_bytes = round_up(size_t(E) * size_t(t.n_tiles) * size_t(t.BN / 32) * size_t(t.steps) * 1024, 256);
     }
-    t.fragment_bytes = round_up(size_t(E) * size_t(t.n_tiles) * size_t(t.BN / 32) * size_t(t.steps) * 1024, 256);
     t.bias_bytes = round_up(size_t(E) * size_t(t.n_tiles) * size_t(t.BN) * 4, 256);
     return t;
 }
@@ -316,7 +317,7 @@ static WeightShape weight_shape(int64_t n, int E, int M, int N)
 }
 
 template <typename T>
-static void launch_prepare(const PrepareCall &q, bool forward, hipStream_t s)
+static void launch_prepare(const PrepareCall &q, bool forward, bool resident, hipStream_t s)
 {
     const int64_t pieces = q.B ? int64_t(q.gl.E) * q.col_tiles * q.steps * kWave : 0;
     int64_t blocks = ceil_div(pieces, kGgThreads);
@@ -325,8 +326,12 @@ static void launch_prepare(const PrepareCall &q, bool forward, hipStream_t s)
     if (q.bias && all < q.gl.E) all = q.gl.E;
     const dim3 grid{unsigned(all)};
     TMA_TIMED(sizeof(T) == 2 ? "grouped_prepare_bf16" : "grouped_prepare", s);
-    if (forward) hipLaunchKernelGGL((grouped_prepare_kernel<T, true>), grid, dim3(kGgThreads), 0, s, q);
-    else hipLaunchKernelGGL((grouped_prepare_kernel<T, false>), grid, dim3(kGgThreads), 0, s, q);
+    constexpr bool kParts = sizeof(T) == 4;        // the resident kernel takes fp32 weights in parts
+    if (kParts && resident) {
+        if (forward) hipLaunchKernelGGL((grouped_prepare_kernel<T, true, kParts>), grid, dim3(kGgThreads), 0, s, q);
+        else hipLaunchKernelGGL((grouped_prepare_kernel<T, false, kParts>), grid, dim3(kGgThreads), 0, s, q);
+    } else if (forward) hipLaunchKernelGGL((grouped_prepare_kernel<T, true, false>), grid, dim3(kGgThreads), 0, s, q);
+    else hipLaunchKernelGGL((grouped_prepare_kernel<T, false, false>), grid, dim3(kGgThreads), 0, s, q);
 }
 
 template <typename T, int WN, int TN, int PP, bool kMask>
@@ -348,14 +353,15 @@ static bool rows_in_words(const void *p, int64_t ld, int64_t n, int F)
 }
 
 template <typename T, bool kMask>
-static int launch_rows(const char *fn, const char *name, const RowsCall &q, const TileShape &t, hipStream_t s)
+static int launch_rows(const char *fn, const char *name, const RowsCall &q, const TileShape &t, const float *W, bool forward, hipStream_t s)
 {
     const T *A = static_cast<const T *>(q.A), *H = static_cast<const T *>(q.H);
     const bool words = rows_in_words<T>(A, q.lda, q.gl.n, q.K) && (!kMask || aligned(H, 4));
     const bool store16 = sizeof(T) == 4 || (aligned(q.C, 4) && q.ldc % 2 == 0);      // (the store needs words, no more)
     TMA_TIMED(name, s);
     if (t.resident) {
-        const ResidentCall r{q.gl, q.tiles, q.tile_count - q.gl.E, q.B, q.bias, q.A, q.H, q.C, q.lda, q.ldc, q.K, q.N, q.steps, q.n_tiles, t.BN / 32, q.relu};
+        const ResidentCall r{q.gl, q.tiles, q.tile_count - q.gl.E, q.B, q.bias, q.A, q.H, q.C, W, q.lda, q.ldc, forward ? q.N : 1, forward ? 1 : q.K, q.K, q.N,
+                             q.steps, q.n_tiles, t.BN / 32, q.relu};
         const dim3 grid(256), block(kResWaves * 64);      // one block a compute unit: its weights take the LDS
         auto go = [&](auto nt, auto multi) {
             constexpr int NT = decltype(nt)::value;
@@ -365,7 +371,8 @@ static int launch_rows(const char *fn, const char *name, const RowsCall &q, cons
         };
         const std::integral_constant<int, 2> two;
         const std::integral_constant<int, 4> four;
-        if (t.steps <= kResSteps) go(two, std::false_type{});
+        if (t.steps <= ResStep<T>::kChunk) go(two, std::false_type{});
+        else if constexpr (sizeof(T) == 4) go(two, std::true_type{});
         else if (t.BN == 128) go(four, std::true_type{});
         else go(two, std::true_type{});
         return check_launch(fn);
@@ -419,10 +426,10 @@ static int tiles_fwd(const char *fn, const GroupList &gl, const void *X, int64_t
     p.col_tiles = t.n_tiles * t.BN / 32;
     p.steps = t.steps;
     p.TN = t.TN;
-    launch_prepare<T>(p, true, s);
+    launch_prepare<T>(p, true, t.resident, s);
     if (int rc = check_launch(fn)) return rc;
     const RowsCall q{gl, p.rows.tiles, p.rows.first + gl.E, p.B, bias ? p.bias_out : nullptr, X, nullptr, Y, ldx, ldy, K, N, t.steps, t.n_tiles, relu};
-    return launch_rows<T, false>(fn, sizeof(T) == 2 ? "grouped_fwd_bf16" : "grouped_fwd", q, t, s);
+    return launch_rows<T, false>(fn, sizeof(T) == 2 ? "grouped_fwd_bf16" : "grouped_fwd", q, t, W, true, s);
 }
 
 template <typename T>
@@ -451,12 +458,12 @@ static int tiles_bwd(const char *fn, const GroupList &gl, const void *X, int64_t
         p.steps = t.steps;
         p.TN = t.TN;
     }
-    launch_prepare<T>(p, false, s);
+    launch_prepare<T>(p, false, t.resident, s);
     if (int rc = check_launch(fn)) return rc;
     if (dX) {
         const RowsCall q{gl, p.rows.tiles, p.rows.first + gl.E, p.B, nullptr, dY, relu ? Y : nullptr, dX, ldy, ld_dx, F_out, F_in, t.steps, t.n_tiles, false};
         const char *name = sizeof(T) == 2 ? "grouped_bwd_data_bf16" : "grouped_bwd_data";
-        if (int rc = relu ? launch_rows<T, true>(fn, name, q, t, s) : launch_rows<T, false>(fn, name, q, t, s)) return rc;
+        if (int rc = relu ? launch_rows<T, true>(fn, name, q, t, W, false, s) : launch_rows<T, false>(fn, name, q, t, W, false, s)) return rc;
     }
     {
         const WeightShape w = weight_shape(gl.n, gl.E, F_in, F_out);

@@ -20,7 +20,9 @@
 // bf16 storage here), fp32 accumulation, results rounded once.
 #pragma once
 #include "kernels.hpp"
+#include "split_pair.hpp"
 
+#include <cfloat>
 #include <type_traits>
 
 namespace tma {
@@ -130,30 +132,40 @@ __host__ __device__ __forceinline__ int fragment_column(int tile, int m, int TN)
     return tile / TN * TN * 32 + hi * TN * 16 + tile % TN * 16 + r;
 }
 
-// kForward: B = W[g] (k along its rows); else B = W[g]^T
-template <typename T, bool kForward>
+// kForward: B = W[g] (k along its rows); else B = W[g]^T.  kSplit (fp32): three bf16 parts of every value instead, a step 16 k-values of which a
+// lane's eight are those of two neighbouring pieces of a row: pieces (g, tile, step, part, lane).
+template <typename T, bool kForward, bool kSplit>
 __device__ __forceinline__ void write_fragments(const GroupList &gl, const float *__restrict__ W, int K, int N, int tiles, int steps, int TN,
                                                 uint4 *__restrict__ out, int64_t block, int64_t blocks)
 {
-    constexpr int E = Step<T>::E;
+    constexpr int E = kSplit ? 8 : Step<T>::E;
     const int64_t per_group = int64_t(tiles) * steps * kWave, total = per_group * gl.E;
     for (int64_t i = block * kGgThreads + threadIdx.x; i < total; i += blocks * kGgThreads) {
         const int g = int(i / per_group);
         if (gl.begin(g + 1) <= gl.begin(g)) continue;
         const int64_t q = i % per_group;
         const int lane = int(q % kWave), step = int(q / kWave % steps), tile = int(q / kWave / steps);
-        const int col = fragment_column(tile, lane & 31, TN), k0 = step * Step<T>::K + (lane >> 5) * E;
+        const int col = fragment_column(tile, lane & 31, TN), hi = lane >> 5;
         const float *w = W + int64_t(g) * K * N;
         float v[E];
 #pragma unroll
         for (int j = 0; j < E; ++j) {
+            const int k = step * 2 * E + (kSplit ? (j >> 2) * 8 + hi * 4 + (j & 3) : hi * E + j);
             v[j] = 0.0f;
-            if (col < N && k0 + j < K) v[j] = kForward ? w[int64_t(k0 + j) * N + col] : w[int64_t(col) * K + k0 + j];
+            if (col < N && k < K) v[j] = kForward ? w[int64_t(k) * N + col] : w[int64_t(col) * K + k];
         }
-        uint4 piece;
-        if constexpr (sizeof(T) == 4) piece = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-        else piece = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
-        out[i] = piece;
+        if constexpr (kSplit) {
+            const SplitPair split;
+            uint32_t part[3][4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) split(v[2 * j], v[2 * j + 1], part[0][j], part[1][j], part[2][j]);
+#pragma unroll
+            for (int p = 0; p < 3; ++p) out[(i / kWave * 3 + p) * kWave + lane] = make_uint4(part[p][0], part[p][1], part[p][2], part[p][3]);
+        } else if constexpr (sizeof(T) == 4) {
+            out[i] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+        } else {
+            out[i] = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+        }
     }
 }
 
@@ -473,9 +485,16 @@ __global__ __launch_bounds__(kGgThreads, (kRowBlocksPerCu<TN, PP, kMask>)) void 
 // 256 -> 256 in bf16 268 us; without rows and stores still 175).
 constexpr int kResWaves = 8;
 constexpr int kResRows = 32;              // rows of a wavefront's tile
-constexpr int kResSteps = 16;             // steps of a chunk of k-values
 constexpr int kResPieces = 8192;          // 16-byte pieces of weights in LDS
 constexpr int kResChunkCols = 4;          // column tiles where a row has several chunks: all their sums are in registers
+// A step is 16 k-values.  fp32: on the bf16 instruction too, three parts of each operand and six products of them a step (gemm_split.hpp says why
+// those suffice), which takes 192 cycles where the fp32 instruction takes 512; ah bh has sums of its own.  A result that is not finite (an operand
+// that is not, or is too large to be taken apart) is computed again in fp32, value by value.
+template <typename T>
+struct ResStep {
+    static constexpr bool kSplit = sizeof(T) == 4;
+    static constexpr int kParts = kSplit ? 3 : 1, kChunk = kSplit ? 8 : 16;      // parts of an operand; steps of 512 bytes of a row
+};
 
 struct ResidentCall {
     GroupList gl;
@@ -485,7 +504,8 @@ struct ResidentCall {
     const float *bias;         // [E][n_tiles CT 32], zeros past N, or NULL
     const void *A, *H;
     void *C;
-    int64_t lda, ldc;
+    const float *W;            // as they are, [E][K N], value (k, column) at k w_k + column w_col
+    int64_t lda, ldc, w_k, w_col;
     int K, N, steps, n_tiles, CT;      // CT: column tiles of 32 in LDS
     bool relu;
 };
@@ -494,8 +514,11 @@ struct ResidentCall {
 template <typename T, int NT, bool kMulti, bool kMask, bool kWords, bool kStore16>
 __global__ __launch_bounds__(kResWaves * 64, 2) void grouped_resident_kernel(ResidentCall q)
 {
-    constexpr int E = Step<T>::E, TN = sizeof(T) == 2 ? 2 : 1;         // TN column tiles make 128 bytes of a row of results
+    constexpr int E = 16 / sizeof(T), TN = sizeof(T) == 2 ? 2 : 1;     // TN column tiles make 128 bytes of a row of results
     constexpr int kUnit = 8;                                           // pieces of those
+    constexpr bool kSplit = ResStep<T>::kSplit;
+    constexpr int kParts = ResStep<T>::kParts, kResSteps = ResStep<T>::kChunk, kQuarterSteps = kResSteps / 4;
+    const SplitPair split;
     typedef RowPiece<T, kWords> P;
     __shared__ uint4 Ws[kResPieces];
     __shared__ uint4 staging[kResWaves][kResRows * kUnit];
@@ -534,9 +557,20 @@ __global__ __launch_bounds__(kResWaves * 64, 2) void grouped_resident_kernel(Res
         item += t_end - t;
 
         __syncthreads();                                            // everyone is done with the weights before
-        const uint4 *B = q.B + (int64_t(group) * q.n_tiles + part) * q.CT * q.steps * kWave;
-        const int pieces = q.CT * q.steps * kWave;
-        for (int i = tid; i < pieces; i += kResWaves * 64) Ws[i] = B[i];
+        const int pieces = q.CT * q.steps * kParts * kWave;
+        const uint4 *B = q.B + (int64_t(group) * q.n_tiles + part) * pieces;
+        {
+            constexpr int kT = kResWaves * 64;
+            int i = tid;
+            for (; i + 7 * kT < pieces; i += 8 * kT) {
+                uint4 v[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) v[u] = B[i + u * kT];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) Ws[i + u * kT] = v[u];
+            }
+            for (; i < pieces; i += kT) Ws[i] = B[i];
+        }
         __syncthreads();
 
         const int n0 = part * q.CT * 32;
@@ -571,7 +605,7 @@ __global__ __launch_bounds__(kResWaves * 64, 2) void grouped_resident_kernel(Res
             const bool full = __all(held[0] && held[1] && held[2] && held[3]);
             // A chunk: 128 bytes of 32 rows at a time through the wavefront's LDS, from whole lines to a row per lane.  (Loads that could go one
             // way or the other were waited for one by one: the common case has a path without a branch.)
-            uint4 x[kResSteps];
+            uint4 x[16];       // fp32: two a step, taken apart as the step is multiplied (parts of all steps would take half as many registers again)
             auto turn = [&](int quarter, const uint4 (&p)[4]) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) mine[spread<kUnit>(r * 8 + lane / 8, lane % 8)] = p[r];
@@ -581,9 +615,9 @@ __global__ __launch_bounds__(kResWaves * 64, 2) void grouped_resident_kernel(Res
                 __builtin_amdgcn_wave_barrier();
             };
             auto fetch = [&](int c) {
-                const int k0 = c * kResSteps * Step<T>::K + lane % 8 * E;
+                const int k0 = c * kResSteps * 16 + lane % 8 * E;
                 constexpr int kQuarter = 8 * E;
-                if (kWords && !ragged && (c + 1) * kResSteps * Step<T>::K <= q.K) {
+                if (kWords && !ragged && (c + 1) * kResSteps * 16 <= q.K) {
                     constexpr int kTogether = kMask && kMulti ? 1 : 4;         // quarters in flight (registers)
 #pragma unroll
                     for (int q0 = 0; q0 < 4; q0 += kTogether) {
@@ -608,7 +642,7 @@ __global__ __launch_bounds__(kResWaves * 64, 2) void grouped_resident_kernel(Res
                 }
 #pragma unroll
                 for (int quarter = 0; quarter < 4; ++quarter)
-                    if (c * kResSteps + quarter * 4 < q.steps) {
+                    if (c * kResSteps + quarter * kQuarterSteps < q.steps) {
                         const int k = k0 + quarter * kQuarter, valid = q.K - k, in_row = valid > 0 ? k : 0;
                         uint4 p[4], m[4];
 #pragma unroll
@@ -625,27 +659,67 @@ __global__ __launch_bounds__(kResWaves * 64, 2) void grouped_resident_kernel(Res
                         turn(quarter, p);
                     }
             };
-            floatx16 acc[NT];
+            floatx16 acc[NT], rest[kSplit ? NT : 1];      // rest: the five smaller products
+            // a lane's columns of a column tile, and their bias: see fragment_column
+            auto bias_of = [&](int tile, float (&v)[16]) {
+                const float4 *b4 = reinterpret_cast<const float4 *>(bias + tile / TN * TN * 32 + hi * TN * 16 + tile % TN * 16);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float4 b = bias ? b4[r] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    v[4 * r] = b.x;
+                    v[4 * r + 1] = b.y;
+                    v[4 * r + 2] = b.z;
+                    v[4 * r + 3] = b.w;
+                }
+            };
             auto start = [&](int ct) {
 #pragma unroll
                 for (int j = 0; j < NT; ++j) {
-                    const int tile = ct + j;       // its lane's columns: see fragment_column
-                    const float4 *b4 = reinterpret_cast<const float4 *>(bias + tile / TN * TN * 32 + hi * TN * 16 + tile % TN * 16);
+                    float v[16];
+                    if constexpr (!kSplit) bias_of(ct + j, v);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const float4 v = bias ? b4[r] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                        acc[j][4 * r] = v.x;
-                        acc[j][4 * r + 1] = v.y;
-                        acc[j][4 * r + 2] = v.z;
-                        acc[j][4 * r + 3] = v.w;
+                    for (int r = 0; r < 16; ++r) {
+                        acc[j][r] = kSplit ? 0.0f : v[r];
+                        if constexpr (kSplit) rest[j][r] = 0.0f;
                     }
                 }
+            };
+            // in fp32, from what the operands are
+            auto again = [&](int col) {
+                float sum = 0.0f;
+                if (row < 0 || col >= q.N) return sum;
+                const T *ar = A + int64_t(row) * q.lda, *hr = kMask ? H + int64_t(row) * q.lda : nullptr;
+                const float *w = q.W + int64_t(group) * q.K * q.N + col * q.w_col;
+                for (int k = 0; k < q.K; ++k) {
+                    float v;
+                    if constexpr (sizeof(T) == 4) v = kMask && !(hr[k] > 0.0f) ? 0.0f : ar[k];
+                    else v = bf16_to_f32(ar[k]);
+                    sum = fmaf(v, w[k * q.w_k], sum);
+                }
+                return sum;
             };
             auto store = [&](int ct) {
 #pragma unroll
                 for (int unit = 0; unit < NT / TN; ++unit) {
                     const int col0 = (ct + unit * TN) * 32;        // of the part
                     if (n0 + col0 >= q.N) break;
+                    if constexpr (kSplit) {
+                        float b[16];
+                        bias_of(ct + unit, b);
+                        bool odd = false;
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const float v = (acc[unit][r] + rest[unit][r]) * kSplitUnscale;
+                            odd = odd || !(fabsf(v) <= FLT_MAX);
+                            acc[unit][r] = v;
+                        }
+                        if (__any(odd && row >= 0))
+#pragma unroll
+                            for (int r = 0; r < 16; ++r)
+                                if (!(fabsf(acc[unit][r]) <= FLT_MAX)) acc[unit][r] = again(n0 + col0 + hi * 16 + r);
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) acc[unit][r] += b[r];
+                    }
 #pragma unroll
                     for (int x = 0; x < TN * 16 / E; ++x) {
                         float z[E];
@@ -689,13 +763,40 @@ __global__ __launch_bounds__(kResWaves * 64, 2) void grouped_resident_kernel(Res
                     if (!kMulti) start(ct);
 #pragma unroll
                     for (int s = 0; s < kResSteps; ++s) {
-                        if (s % kAhead == 0 && c * kResSteps + s >= q.steps) break;
-                        uint4 w[NT];
-                        const uint4 one[1] = {x[s]};
+                        if (s % kQuarterSteps == 0 && c * kResSteps + s >= q.steps) break;
+                        uint4 xp[kParts];
+                        if constexpr (kSplit) {
+                            // (held in the loop: taken out of it, the parts of all steps would not fit the registers)
+                            asm volatile("" : "+v"(x[2 * s].x), "+v"(x[2 * s].y), "+v"(x[2 * s].z), "+v"(x[2 * s].w), "+v"(x[2 * s + 1].x), "+v"(x[2 * s + 1].y),
+                                         "+v"(x[2 * s + 1].z), "+v"(x[2 * s + 1].w));
+                            const uint32_t v[8] = {x[2 * s].x, x[2 * s].y, x[2 * s].z, x[2 * s].w, x[2 * s + 1].x, x[2 * s + 1].y, x[2 * s + 1].z, x[2 * s + 1].w};
+                            uint32_t part[3][4];
 #pragma unroll
-                        for (int j = 0; j < NT; ++j) w[j] = Ws[((ct + j) * q.steps + c * kResSteps + s) * kWave + lane];
-                        floatx16(&row_acc)[1][NT] = reinterpret_cast<floatx16(&)[1][NT]>(acc);
-                        multiply<T, 1, NT>(w, one, row_acc);
+                            for (int j = 0; j < 4; ++j) split(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]), part[0][j], part[1][j], part[2][j]);
+#pragma unroll
+                            for (int o = 0; o < kParts; ++o) xp[o] = make_uint4(part[o][0], part[o][1], part[o][2], part[o][3]);
+                        } else {
+                            xp[0] = x[s];
+                        }
+#pragma unroll
+                        for (int j = 0; j < NT; ++j) {
+                            const uint4 *w = Ws + (((ct + j) * q.steps + c * kResSteps + s) * kParts) * kWave + lane;
+                            auto times = [&](const uint4 &wp, const uint4 &xp, const floatx16 &sum) {
+                                return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, wp), __builtin_bit_cast(bf16x8, xp), sum, 0, 0, 0);
+                            };
+                            if constexpr (kSplit) {
+                                const uint4 h = w[0], m = w[kWave], l = w[2 * kWave];
+                                acc[j] = times(h, xp[0], acc[j]);
+                                rest[j] = times(l, xp[0], rest[j]);
+                                rest[j] = times(h, xp[2], rest[j]);
+                                rest[j] = times(m, xp[1], rest[j]);
+                                rest[j] = times(m, xp[0], rest[j]);
+                                rest[j] = times(h, xp[1], rest[j]);
+                            } else {
+                                acc[j] = times(w[0], xp[0], acc[j]);
+                            }
+                        }
+                        if constexpr (kSplit) __builtin_amdgcn_sched_barrier(0);
                     }
                     if (!kMulti) store(ct);
                 }
@@ -947,7 +1048,7 @@ struct PrepareCall {
     int K, N, col_tiles, steps, TN;
 };
 
-template <typename T, bool kForward>
+template <typename T, bool kForward, bool kSplit>
 __global__ __launch_bounds__(kGgThreads) void grouped_prepare_kernel(PrepareCall q)
 {
     const int b = blockIdx.x;
@@ -956,7 +1057,7 @@ __global__ __launch_bounds__(kGgThreads) void grouped_prepare_kernel(PrepareCall
             q.bias_out[int64_t(b) * q.col_tiles * 32 + c] = c < q.N ? q.bias[int64_t(b) * q.N + c] : 0.0f;
     if (b < q.row_blocks) write_plan(q.gl, q.rows, b);
     else if (b < q.row_blocks + q.run_blocks) write_plan(q.gl, q.runs, b - q.row_blocks);
-    else write_fragments<T, kForward>(q.gl, q.W, q.K, q.N, q.col_tiles, q.steps, q.TN, q.B, b - q.row_blocks - q.run_blocks,
+    else write_fragments<T, kForward, kSplit>(q.gl, q.W, q.K, q.N, q.col_tiles, q.steps, q.TN, q.B, b - q.row_blocks - q.run_blocks,
                                       gridDim.x - q.row_blocks - q.run_blocks);
 }
 
