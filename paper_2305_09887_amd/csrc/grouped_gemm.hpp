@@ -526,7 +526,6 @@ __global__ __launch_bounds__(kResWaves * 64, 2) void grouped_resident_kernel(Res
     T *C = static_cast<T *>(q.C);
     const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, hi = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t last = (q.gl.n - 1) * q.lda + q.K - E;
-    const bool ragged = kWords && q.K % E != 0;
     const int chunks = kMulti ? (q.steps + kResSteps - 1) / kResSteps : 1;
     uint4 *mine = staging[wave];
 
@@ -588,21 +587,16 @@ __global__ __launch_bounds__(kResWaves * 64, 2) void grouped_resident_kernel(Res
         for (; t < t_end; t += kResWaves) {
             const int32_t after = row_of(t + 2 * kResWaves);
             // rows x * 8 + lane / 8 of the tile, whose pieces lane % 8, + 8, ... this lane loads and stores
-            const T *a[4], *h[kMask ? 4 : 1];
-            T *out[4];
-            bool held[4];
+            int32_t v[4];
             int limit[4];                  // the last place in the row where 16 bytes are left
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-                const int32_t v = __shfl(row, x * 8 + lane / 8, kWave);
-                held[x] = v >= 0;
-                const int64_t r = held[x] ? v : 0, from = r * q.lda;       // (a row that is none reads the first, and is not stored)
-                a[x] = A + from;
-                if constexpr (kMask) h[x] = H + from;
+                v[x] = __shfl(row, x * 8 + lane / 8, kWave);
+                const int64_t from = int64_t(v[x] < 0 ? 0 : v[x]) * q.lda;       // (a row that is none reads the first, and is not stored)
                 limit[x] = last - from < q.K ? int(last - from) : q.K;
-                out[x] = C + r * q.ldc + n0 + lane % 8 * E;
             }
-            const bool full = __all(held[0] && held[1] && held[2] && held[3]);
+            auto row_at = [&](const T *p, int r) { return p + int64_t(v[r] < 0 ? 0 : v[r]) * q.lda; };
+            const bool full = __all((v[0] | v[1] | v[2] | v[3]) >= 0);
             // A chunk: 128 bytes of 32 rows at a time through the wavefront's LDS, from whole lines to a row per lane.  (Loads that could go one
             // way or the other were waited for one by one: the common case has a path without a branch.)
             uint4 x[16];       // fp32: two a step, taken apart as the step is multiplied (parts of all steps would take half as many registers again)
@@ -617,49 +611,53 @@ __global__ __launch_bounds__(kResWaves * 64, 2) void grouped_resident_kernel(Res
             auto fetch = [&](int c) {
                 const int k0 = c * kResSteps * 16 + lane % 8 * E;
                 constexpr int kQuarter = 8 * E;
-                if (kWords && !ragged && (c + 1) * kResSteps * 16 <= q.K) {
-                    constexpr int kTogether = kMask && kMulti ? 1 : 4;         // quarters in flight (registers)
+                if (kWords && (c + 1) * kResSteps * 16 <= q.K) {
+                    uint4 p[4][4], m[kMask ? 4 : 1][4];
 #pragma unroll
-                    for (int q0 = 0; q0 < 4; q0 += kTogether) {
-                        uint4 p[kTogether][4], m[kMask ? kTogether : 1][4];
+                    for (int i = 0; i < 4; ++i)
 #pragma unroll
-                        for (int i = 0; i < kTogether; ++i)
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) {
-                                p[i][r] = from_words(a[r] + k0 + (q0 + i) * kQuarter);
-                                if constexpr (kMask) m[i][r] = from_words(h[r] + k0 + (q0 + i) * kQuarter);
-                            }
-#pragma unroll
-                        for (int i = 0; i < kTogether; ++i) {
-                            if constexpr (kMask) {
-#pragma unroll
-                                for (int r = 0; r < 4; ++r) p[i][r] = open_piece<T>(p[i][r], m[i][r]);
-                            }
-                            turn(q0 + i, p[i]);
+                        for (int r = 0; r < 4; ++r) {
+                            p[i][r] = from_words(row_at(A, r) + k0 + i * kQuarter);
+                            if constexpr (kMask) m[i][r] = from_words(row_at(H, r) + k0 + i * kQuarter);
                         }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if constexpr (kMask) {
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) p[i][r] = open_piece<T>(p[i][r], m[i][r]);
+                        }
+                        turn(i, p[i]);
                     }
                     return;
                 }
+                uint4 p[4][4], m[kMask ? 4 : 1][4];
+                auto in_row = [&](int quarter) { return k0 + quarter * kQuarter < q.K ? k0 + quarter * kQuarter : 0; };
 #pragma unroll
                 for (int quarter = 0; quarter < 4; ++quarter)
                     if (c * kResSteps + quarter * kQuarterSteps < q.steps) {
-                        const int k = k0 + quarter * kQuarter, valid = q.K - k, in_row = valid > 0 ? k : 0;
-                        uint4 p[4], m[4];
+                        const int valid = q.K - k0 - quarter * kQuarter;
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
-                            p[r] = P::load(a[r], in_row, valid, limit[r]);
-                            if constexpr (kMask) m[r] = P::load(h[r], in_row, valid, limit[r]);
+                            p[quarter][r] = P::load(row_at(A, r), in_row(quarter), valid, limit[r]);
+                            if constexpr (kMask) m[quarter][r] = P::load(row_at(H, r), in_row(quarter), valid, limit[r]);
                         }
+                    }
+#pragma unroll
+                for (int quarter = 0; quarter < 4; ++quarter)
+                    if (c * kResSteps + quarter * kQuarterSteps < q.steps) {
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
-                            if constexpr (kMask) p[r] = open_piece<T>(p[r], m[r]);
-                            if (kWords && in_row > limit[r]) p[r] = P::moved(p[r], in_row - limit[r]);
-                            if (kWords) p[r] = P::cut(p[r], valid);
+                            uint4 &o = p[quarter][r];
+                            if constexpr (kMask) o = open_piece<T>(o, m[quarter][r]);
+                            if (kWords && in_row(quarter) > limit[r]) o = P::moved(o, in_row(quarter) - limit[r]);
+                            if (kWords) o = P::cut(o, q.K - k0 - quarter * kQuarter);
                         }
-                        turn(quarter, p);
+                        turn(quarter, p[quarter]);
                     }
             };
-            floatx16 acc[NT], rest[kSplit ? NT : 1];      // rest: the five smaller products
+            constexpr bool kRest = kSplit && !kMulti;      // sums of their own for the five smaller products: where registers are left
+            floatx16 acc[NT], rest_[kRest ? NT : 1];
+            auto &rest = [&]() -> auto & { if constexpr (kRest) return rest_; else return acc; }();
             // a lane's columns of a column tile, and their bias: see fragment_column
             auto bias_of = [&](int tile, float (&v)[16]) {
                 const float4 *b4 = reinterpret_cast<const float4 *>(bias + tile / TN * TN * 32 + hi * TN * 16 + tile % TN * 16);
@@ -680,7 +678,7 @@ __global__ __launch_bounds__(kResWaves * 64, 2) void grouped_resident_kernel(Res
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         acc[j][r] = kSplit ? 0.0f : v[r];
-                        if constexpr (kSplit) rest[j][r] = 0.0f;
+                        if constexpr (kRest) rest[j][r] = 0.0f;
                     }
                 }
             };
@@ -709,7 +707,7 @@ __global__ __launch_bounds__(kResWaves * 64, 2) void grouped_resident_kernel(Res
                         bool odd = false;
 #pragma unroll
                         for (int r = 0; r < 16; ++r) {
-                            const float v = (acc[unit][r] + rest[unit][r]) * kSplitUnscale;
+                            const float v = (kRest ? acc[unit][r] + rest[unit][r] : acc[unit][r]) * kSplitUnscale;
                             odd = odd || !(fabsf(v) <= FLT_MAX);
                             acc[unit][r] = v;
                         }
@@ -739,17 +737,22 @@ __global__ __launch_bounds__(kResWaves * 64, 2) void grouped_resident_kernel(Res
                     if (kStore16 && full && n0 + col0 + TN * 32 <= q.N) {
 #pragma unroll
                         for (int x = 0; x < 4; ++x)
-                            __builtin_nontemporal_store(Words4{z[x].x, z[x].y, z[x].z, z[x].w}, reinterpret_cast<Words4 *>(out[x] + col0));
+                            __builtin_nontemporal_store(Words4{z[x].x, z[x].y, z[x].z, z[x].w}, reinterpret_cast<Words4 *>(C + int64_t(v[x]) * q.ldc + col));
                         continue;
                     }
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
-                        T *o = out[x] + col0;
+                        if (v[x] < 0 || col >= q.N) continue;
+                        T *o = C + int64_t(v[x]) * q.ldc + col;
+                        if (kStore16 && col + E <= q.N) {
+                            __builtin_nontemporal_store(Words4{z[x].x, z[x].y, z[x].z, z[x].w}, reinterpret_cast<Words4 *>(o));
+                            continue;
+                        }
                         float w[E];
                         Chunk<T>::widen(z[x], w);
 #pragma unroll
                         for (int y = 0; y < E; ++y)
-                            if (held[x] && col + y < q.N) {
+                            if (col + y < q.N) {
                                 if constexpr (sizeof(T) == 4) o[y] = w[y];
                                 else o[y] = uint16_t(__float_as_uint(w[y]) >> 16);
                             }
