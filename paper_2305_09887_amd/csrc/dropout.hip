@@ -26,21 +26,27 @@ struct DropRule {
 
 __device__ __forceinline__ float keep_field(float x, uint32_t field, const DropRule &r) { return field >= r.limit ? x * r.scale : 0.0f; }
 
-// A thread keeps its piece of columns (E elements; kVec: 16 bytes) and walks down the rows; `lanes` threads share a row.
-template <typename T, bool kVec>
+typedef uint32_t Words4 __attribute__((ext_vector_type(4), aligned(4)));      // 16 bytes at a 4-byte-aligned address
+
+// A thread keeps its piece of columns (16 bytes; without kWords four elements) and walks down the rows, `lanes` threads share a row.  The end of a row
+// that is no whole piece is read as one too (what follows is the row's padding or the next row) and stored element by element; in the last
+// row it is read so as well.
+template <typename T, bool kWords>
 __global__ __launch_bounds__(kDropThreads) void dropout_kernel(int64_t n, int F, const T *X, int64_t ldx, DropRule rule, T *Y, int64_t ldy, int lanes)
 {
-    constexpr int E = kVec ? Chunk<T>::kElems : 4;
+    constexpr int E = kWords ? Chunk<T>::kElems : 4;
     const int units = (F + 3) / 4, pieces = (F + E - 1) / E;
     const int rows_per_block = kDropThreads / lanes;
     const int piece = int(blockIdx.y) * lanes + int(threadIdx.x) % lanes, slot = int(threadIdx.x) / lanes;
     if (piece >= pieces || slot >= rows_per_block) return;
     const uint64_t seed = rule.step ? splitmix64_at(rule.seed, uint64_t(*rule.step)) : rule.seed;
-    const int c0 = piece * E;
-    const bool whole = kVec && c0 + E <= F;
-    const int64_t stride = int64_t(gridDim.x) * rows_per_block;
+    const int c0 = piece * E, valid = F - c0 < E ? F - c0 : E;
+    const int64_t stride = int64_t(gridDim.x) * rows_per_block, extent = (n - 1) * ldx + F;
+    // rows in which 16 bytes from the piece on lie in the matrix: all, or all but the last few
+    int64_t whole_rows = 0;
+    if (kWords && extent - c0 >= E) whole_rows = (extent - c0 - E) / ldx + 1 < n ? (extent - c0 - E) / ldx + 1 : n;
 
-    auto finish = [&](int64_t v, const float (&x)[E], float (&y)[E]) {
+    auto drop = [&](int64_t v, const float (&x)[E], float (&y)[E]) {
 #pragma unroll
         for (int u = 0; u < E / 4; ++u) {
             const uint64_t z = splitmix64_at(seed, uint64_t(rule.first_row + v) * uint64_t(units) + uint64_t(c0 / 4 + u));
@@ -48,43 +54,56 @@ __global__ __launch_bounds__(kDropThreads) void dropout_kernel(int64_t n, int F,
             for (int i = 0; i < 4; ++i) y[4 * u + i] = keep_field(x[4 * u + i], uint32_t(z >> (16 * i)) & 0xFFFFu, rule);
         }
     };
-    int64_t v = int64_t(blockIdx.x) * rows_per_block + slot;
-    if (whole) {
-        for (; v < n; v += kDropRows * stride) {
-            uint4 raw[kDropRows];
+    auto store = [&](int64_t v, const float (&y)[E]) {
+        T *out = Y + v * ldy + c0;
+        if constexpr (kWords) {
+            if (valid == E) {
+                Words4 w;
 #pragma unroll
-            for (int j = 0; j < kDropRows; ++j)
-                if (v + j * stride < n) raw[j] = *reinterpret_cast<const uint4 *>(X + (v + j * stride) * ldx + c0);
-#pragma unroll
-            for (int j = 0; j < kDropRows; ++j)
-                if (v + j * stride < n) {
-                    if constexpr (kVec) {
-                        float x[E], y[E];
-                        Chunk<T>::widen(raw[j], x);
-                        finish(v + j * stride, x, y);
-                        Chunk<T>::store(Y + (v + j * stride) * ldy + c0, y);
-                    }
-                }
-        }
-    } else {
-        for (; v < n; v += stride) {
-            float x[E], y[E];
-#pragma unroll
-            for (int i = 0; i < E; ++i) {
-                x[i] = 0.0f;
-                if (c0 + i < F) {
-                    if constexpr (sizeof(T) == 4) x[i] = X[v * ldx + c0 + i];
-                    else x[i] = bf16_to_f32(X[v * ldx + c0 + i]);
-                }
+                for (int i = 0; i < 4; ++i) w[i] = sizeof(T) == 4 ? __float_as_uint(y[i]) : pack_bf16(y[2 * i % E], y[(2 * i + 1) % E]);
+                *reinterpret_cast<Words4 *>(out) = w;
+                return;
             }
-            finish(v, x, y);
+        }
 #pragma unroll
-            for (int i = 0; i < E; ++i)
-                if (c0 + i < F) {
-                    if constexpr (sizeof(T) == 4) Y[v * ldy + c0 + i] = y[i];
-                    else Y[v * ldy + c0 + i] = f32_to_bf16(y[i]);
+        for (int i = 0; i < E; ++i)
+            if (i < valid) {
+                if constexpr (sizeof(T) == 4) out[i] = y[i];
+                else out[i] = f32_to_bf16(y[i]);
+            }
+    };
+    int64_t v = int64_t(blockIdx.x) * rows_per_block + slot;
+    if constexpr (kWords) {
+        for (; v < whole_rows; v += kDropRows * stride) {
+            Words4 raw[kDropRows];
+#pragma unroll
+            for (int j = 0; j < kDropRows; ++j)
+                if (v + j * stride < whole_rows) raw[j] = *reinterpret_cast<const Words4 *>(X + (v + j * stride) * ldx + c0);
+#pragma unroll
+            for (int j = 0; j < kDropRows; ++j)
+                if (v + j * stride < whole_rows) {
+                    float x[E], y[E];
+                    Chunk<T>::widen(make_uint4(raw[j].x, raw[j].y, raw[j].z, raw[j].w), x);
+                    drop(v + j * stride, x, y);
+                    store(v + j * stride, y);
                 }
         }
+        // the first of this thread's rows that are left
+        const int64_t first = int64_t(blockIdx.x) * rows_per_block + slot;
+        v = whole_rows > first ? first + (whole_rows - first + stride - 1) / stride * stride : first;
+    }
+    for (; v < n; v += stride) {
+        float x[E], y[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            x[i] = 0.0f;
+            if (i < valid) {
+                if constexpr (sizeof(T) == 4) x[i] = X[v * ldx + c0 + i];
+                else x[i] = bf16_to_f32(X[v * ldx + c0 + i]);
+            }
+        }
+        drop(v, x, y);
+        store(v, y);
     }
 }
 
@@ -92,14 +111,14 @@ template <typename T>
 static int launch_dropout(const char *fn, const char *name, int64_t n, int32_t F, const void *X, int64_t ldx, const DropRule &rule, void *Y,
                           int64_t ldy, hipStream_t s)
 {
-    const bool vec = aligned(X, 16) && aligned(Y, 16) && (size_t(ldx) * sizeof(T)) % 16 == 0 && (size_t(ldy) * sizeof(T)) % 16 == 0;
-    const int E = vec ? Chunk<T>::kElems : 4;
+    const bool words = sizeof(T) == 4 || (aligned(X, 4) && aligned(Y, 4) && ldx % 2 == 0 && ldy % 2 == 0);
+    const int E = words ? Chunk<T>::kElems : 4;
     const int pieces = int(ceil_div(F, E)), lanes = pieces < kDropThreads ? pieces : kDropThreads;
     int64_t blocks = ceil_div(n, kDropThreads / lanes);
     if (blocks > kDropBlocks) blocks = kDropBlocks;
     const dim3 grid(unsigned(blocks), unsigned(ceil_div(pieces, lanes)));
     TMA_TIMED(name, s);
-    if (vec) hipLaunchKernelGGL((dropout_kernel<T, true>), grid, dim3(kDropThreads), 0, s, n, F, static_cast<const T *>(X), ldx, rule, static_cast<T *>(Y), ldy, lanes);
+    if (words) hipLaunchKernelGGL((dropout_kernel<T, true>), grid, dim3(kDropThreads), 0, s, n, F, static_cast<const T *>(X), ldx, rule, static_cast<T *>(Y), ldy, lanes);
     else hipLaunchKernelGGL((dropout_kernel<T, false>), grid, dim3(kDropThreads), 0, s, n, F, static_cast<const T *>(X), ldx, rule, static_cast<T *>(Y), ldy, lanes);
     return check_launch(fn);
 }
