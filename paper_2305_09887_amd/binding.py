@@ -881,19 +881,24 @@ def tma_gcn_block_bwd(n_dst: int, n_src: int, max_entries: int, blk_rowptr, blk_
 
 
 # ---------------------------------------------------------------------------
-def _device(where, *tensors):
-    """The device that the tensors share; they may be None."""
-    devices = {t.device for t in tensors if t is not None}
-    if len(devices) != 1 or next(iter(devices)).type != "cuda":
+def _device(where, first, *others):
+    """The device that the tensors share (the first is one; others may be None)."""
+    dev = first.device
+    if dev.type != "cuda" or any(t is not None and t.device != dev for t in others):
         raise TmaError(f"{where}: expected tensors on one CUDA/HIP device")
-    return next(iter(devices))
+    return dev
 
 
 def _launch(device, stream, call, *args):
     """call(*args, stream) with the tensors' device as the current one (the library launches on that) and, where none is
     given, that device's current stream."""
-    with torch.cuda.device(device):
-        _check(call(*args, _stream(stream)))
+    index = device.index
+    s = C.c_void_p((torch.cuda.current_stream(index) if stream is None else stream).cuda_stream)
+    if index == torch.cuda.current_device():
+        _check(call(*args, s))
+    else:
+        with torch.cuda.device(index):
+            _check(call(*args, s))
 
 
 def _rows_like(t, name, shape, dtype, device):

@@ -97,17 +97,30 @@ struct GnSegments {
         const int64_t o = offsets[s];
         return o < 0 ? 0 : o < n ? o : n;
     }
-    // the segment of a row: the last that begins at or before it (-1: none)
-    __device__ __forceinline__ int64_t of(int64_t row) const
+    // the segment of a row, the last that begins at or before it (-1: none); all threads of a block call this with one row, and each
+    // step tries as many places as it has threads
+    __device__ __forceinline__ int64_t of_block(int64_t row) const
     {
         if (!offsets) return row / rows;
         int64_t lo = -1, hi = count;
         while (hi - lo > 1) {
-            const int64_t mid = (lo + hi) / 2;
-            if (start(mid) <= row) lo = mid;
-            else hi = mid;
+            const int64_t step = (hi - lo - 1 + kGnThreads - 1) / kGnThreads, p = lo + 1 + int64_t(threadIdx.x) * step;
+            const int c = __syncthreads_count(p < hi && start(p) <= row);
+            const int64_t first = lo + 1 + (c - 1) * step, next = lo + 1 + c * step;
+            if (c > 0) lo = first;
+            hi = next < hi ? next : hi;
         }
         return lo;
+    }
+    // the segment of a row at or behind one that begins at or before it
+    __device__ __forceinline__ int64_t of(int64_t row, int64_t s) const
+    {
+        if (!offsets) return row / rows;
+        int64_t d = 1;
+        for (; s + d < count && start(s + d) <= row; d *= 2) s += d;
+        for (d /= 2; d > 0; d /= 2)
+            if (s + d < count && start(s + d) <= row) s += d;
+        return s;
     }
 };
 
@@ -360,23 +373,45 @@ __global__ __launch_bounds__(kGnThreads) void gn_rows_bwd_kernel(GnShape sh, con
 }
 
 // ---- longer segments -----------------------------------------------------------
-// what(s, row, end) for every segment that the tile cuts, in order, with the rows [row, end) that it has of it
-template <class What>
-__device__ __forceinline__ void walk_tile(const GnSegments &sg, int64_t tile, What &&what)
+// The tiles of a block, U rows of a lane at a time: load(row, end) fetches the rows [row, end) of a chunk, on their way while the segments
+// are looked up; use(s, from, to) is what segment s has of them, counted from the chunk's first row; done(tile, s) follows the last of a segment's rows
+// in a tile.  By all threads of the block (`live`: those that have columns).
+template <int U, class Load, class Use, class Done>
+__device__ __forceinline__ void walk_tiles(const GnShape &sh, const GnSegments &sg, int slot, bool live, Load &&load, Use &&use, Done &&done)
 {
-    int64_t row = tile * sg.tile_rows;
-    const int64_t last = row + sg.tile_rows < sg.n ? row + sg.tile_rows : sg.n;
-    int64_t s = sg.of(row);
-    if (s < 0) s = 0;
-    while (s < sg.count && row < last) {
-        const int64_t begin = sg.start(s), end = sg.start(s + 1);
-        if (begin > row) row = begin;
-        if (end > row && row < last) {
-            const int64_t stop = end < last ? end : last;
-            what(s, row, stop);
-            row = stop;
+    for (int64_t t0 = int64_t(blockIdx.x) * sh.tpb; t0 < sg.tiles; t0 += int64_t(gridDim.x) * sh.tpb) {
+        const int64_t tile = t0 + slot, first = tile * sg.tile_rows;
+        const bool mine = live && tile < sg.tiles;
+        const int64_t last = !mine ? first : first + sg.tile_rows < sg.n ? first + sg.tile_rows : sg.n;
+        if (mine) load(first, first + U < last ? first + U : last);
+        int64_t s = sg.of_block(t0 * sg.tile_rows);
+        if (!mine) continue;
+        s = sg.of(first, s < 0 ? 0 : s);
+        int64_t begin = sg.start(s), end = sg.start(s + 1);
+        bool open = false;
+        for (int64_t c = first; c < last; c += U) {
+            const int64_t stop = c + U < last ? c + U : last;
+            if (c > first) load(c, stop);
+            int64_t row = c;
+            while (s < sg.count && row < stop) {
+                const int64_t a = begin > row ? begin : row, b = end < stop ? end : stop;
+                if (a < b) {
+                    use(s, int(a - c), int(b - c));
+                    open = true;
+                    row = b;
+                } else if (begin >= stop) {
+                    break;
+                }
+                if (end <= stop) {
+                    if (open) done(tile, s);
+                    open = false;
+                    ++s;
+                    begin = end;
+                    if (s < sg.count) end = sg.start(s + 1);
+                }
+            }
         }
-        if (end <= row) ++s;
+        if (open) done(tile, s);
     }
 }
 
@@ -408,39 +443,40 @@ __global__ __launch_bounds__(kGnThreads) void gn_moments_kernel(GnShape sh, GnSe
     typedef Piece<T, E> P;
     constexpr int U = CPL == 1 ? kGnChunk : 1;
     const GnLane<E, CPL> ln(sh);
-    if (!ln.live) return;
     const float columns = float(ln.columns());
-    for (int64_t tile = int64_t(blockIdx.x) * sh.tpb + ln.slot; tile < sg.tiles; tile += int64_t(gridDim.x) * sh.tpb)
-        walk_tile(sg, tile, [&](int64_t s, int64_t row, int64_t end) {
-            Moments all{0.0f, 0.0f, 0.0f};
-            for (; row < end; row += U) {
-                typename P::Raw raw[U][CPL];
+    typename P::Raw raw[U][CPL];
+    Moments all{0.0f, 0.0f, 0.0f};
+    walk_tiles<U>(sh, sg, ln.slot, ln.live,
+        [&](int64_t row, int64_t end) {
 #pragma unroll
-                for (int u = 0; u < U; ++u)
+            for (int u = 0; u < U; ++u)
 #pragma unroll
-                    for (int c = 0; c < CPL; ++c)
-                        if (ln.in[c] && row + u < end) raw[u][c] = P::load(X + (row + u) * ldx + ln.col(sh, c));
-                float x[U][CPL][E], sum = 0.0f, sq = 0.0f;
-                const float count = float(end - row < U ? int(end - row) : U) * columns;
+                for (int c = 0; c < CPL; ++c)
+                    if (ln.in[c] && row + u < end) raw[u][c] = P::load(X + (row + u) * ldx + ln.col(sh, c));
+        },
+        [&](int64_t, int from, int to) {
+            float x[U][CPL][E], sum = 0.0f, sq = 0.0f;
 #pragma unroll
-                for (int u = 0; u < U; ++u)
+            for (int u = 0; u < U; ++u)
 #pragma unroll
-                    for (int c = 0; c < CPL; ++c) {
-                        P::widen(raw[u][c], x[u][c]);
+                for (int c = 0; c < CPL; ++c) {
+                    P::widen(raw[u][c], x[u][c]);
 #pragma unroll
-                        for (int i = 0; i < E; ++i) sum += ln.in[c] && row + u < end ? x[u][c][i] : 0.0f;
-                    }
-                const float mean = count > 0.0f ? sum / count : 0.0f;
+                    for (int i = 0; i < E; ++i) sum += ln.in[c] && u >= from && u < to ? x[u][c][i] : 0.0f;
+                }
+            const float count = float(to - from) * columns, mean = count > 0.0f ? sum / count : 0.0f;
 #pragma unroll
-                for (int u = 0; u < U; ++u)
+            for (int u = 0; u < U; ++u)
 #pragma unroll
-                    for (int c = 0; c < CPL; ++c)
+                for (int c = 0; c < CPL; ++c)
 #pragma unroll
-                        for (int i = 0; i < E; ++i) sq += ln.in[c] && row + u < end ? (x[u][c][i] - mean) * (x[u][c][i] - mean) : 0.0f;
-                all.join(count, mean, sq);
-            }
+                    for (int i = 0; i < E; ++i) sq += ln.in[c] && u >= from && u < to ? (x[u][c][i] - mean) * (x[u][c][i] - mean) : 0.0f;
+            all.join(count, mean, sq);
+        },
+        [&](int64_t tile, int64_t s) {
             all.join_lanes(sh.W);
             if (ln.sub == 0) pairs[(tile + s) * sh.G + ln.g] = make_float2(all.mean, all.m2);
+            all = Moments{0.0f, 0.0f, 0.0f};
         });
 }
 
@@ -474,34 +510,38 @@ __global__ __launch_bounds__(kGnThreads) void gn_apply_kernel(GnShape sh, GnSegm
     typedef Piece<T, E> P;
     constexpr int U = CPL == 1 ? 4 : 1;
     const GnLane<E, CPL> ln(sh);
-    if (!ln.live) return;
     const GnAct<kSilu, sizeof(T) == 4> act(sh.act, slope_p);
     float ga[CPL][E], be[CPL][E];
     load_vector<E, CPL>(gamma, sh, ln, ga);
     load_vector<E, CPL>(beta, sh, ln, be);
-    for (int64_t tile = int64_t(blockIdx.x) * sh.tpb + ln.slot; tile < sg.tiles; tile += int64_t(gridDim.x) * sh.tpb)
-        walk_tile(sg, tile, [&](int64_t s, int64_t row, int64_t end) {
-            const float2 st = stats[s * sh.G + ln.g];
-            for (; row < end; row += U) {
-                typename P::Raw raw[U][CPL];
+    typename P::Raw raw[U][CPL];
+    float2 st = make_float2(0.0f, 0.0f);
+    int64_t of = -1, row0 = 0;
+    walk_tiles<U>(sh, sg, ln.slot, ln.live,
+        [&](int64_t row, int64_t end) {
+            row0 = row;
 #pragma unroll
-                for (int u = 0; u < U; ++u)
+            for (int u = 0; u < U; ++u)
 #pragma unroll
-                    for (int c = 0; c < CPL; ++c)
-                        if (ln.in[c] && row + u < end) raw[u][c] = P::load(X + (row + u) * ldx + ln.col(sh, c));
+                for (int c = 0; c < CPL; ++c)
+                    if (ln.in[c] && row + u < end) raw[u][c] = P::load(X + (row + u) * ldx + ln.col(sh, c));
+        },
+        [&](int64_t s, int from, int to) {
+            if (s != of) st = stats[s * sh.G + ln.g];
+            of = s;
 #pragma unroll
-                for (int u = 0; u < U; ++u)
+            for (int u = 0; u < U; ++u)
 #pragma unroll
-                    for (int c = 0; c < CPL; ++c)
-                        if (ln.in[c] && row + u < end) {
-                            float x[E];
-                            P::widen(raw[u][c], x);
+                for (int c = 0; c < CPL; ++c)
+                    if (ln.in[c] && u >= from && u < to) {
+                        float x[E];
+                        P::widen(raw[u][c], x);
 #pragma unroll
-                            for (int i = 0; i < E; ++i) x[i] = act.value(ga[c][i] * ((x[i] - st.x) * st.y) + be[c][i]);
-                            P::store(Y + (row + u) * ldy + ln.col(sh, c), x);
-                        }
-            }
-        });
+                        for (int i = 0; i < E; ++i) x[i] = act.value(ga[c][i] * ((x[i] - st.x) * st.y) + be[c][i]);
+                        P::store(Y + (row0 + u) * ldy + ln.col(sh, c), x);
+                    }
+        },
+        [&](int64_t, int64_t) {});
 }
 
 // sums of gamma dz and gamma dz xh of every (tile, segment) pair's groups; dgamma, dbeta, dslope of the block
@@ -522,43 +562,48 @@ __global__ __launch_bounds__(kGnThreads) void gn_sums_kernel(GnShape sh, GnSegme
     for (int c = 0; c < CPL; ++c)
 #pragma unroll
         for (int i = 0; i < E; ++i) dga[c][i] = dbe[c][i] = 0.0f;
-    const int64_t tiles = ln.live ? sg.tiles : 0;
-    for (int64_t tile = int64_t(blockIdx.x) * sh.tpb + ln.slot; tile < tiles; tile += int64_t(gridDim.x) * sh.tpb)
-        walk_tile(sg, tile, [&](int64_t s, int64_t row, int64_t end) {
-            const float2 st = stats[s * sh.G + ln.g];
-            float s1 = 0.0f, s2 = 0.0f;
-            for (; row < end; row += U) {
-                typename P::Raw rx[U][CPL], rg[U][CPL];
+    typename P::Raw rx[U][CPL], rg[U][CPL];
+    float2 st = make_float2(0.0f, 0.0f);
+    float s1 = 0.0f, s2 = 0.0f;
+    int64_t of = -1;
+    walk_tiles<U>(sh, sg, ln.slot, ln.live,
+        [&](int64_t row, int64_t end) {
 #pragma unroll
-                for (int u = 0; u < U; ++u)
+            for (int u = 0; u < U; ++u)
 #pragma unroll
-                    for (int c = 0; c < CPL; ++c)
-                        if (ln.in[c] && row + u < end) {
-                            rx[u][c] = P::load(X + (row + u) * ldx + ln.col(sh, c));
-                            rg[u][c] = P::load(dY + (row + u) * ldd + ln.col(sh, c));
+                for (int c = 0; c < CPL; ++c)
+                    if (ln.in[c] && row + u < end) {
+                        rx[u][c] = P::load(X + (row + u) * ldx + ln.col(sh, c));
+                        rg[u][c] = P::load(dY + (row + u) * ldd + ln.col(sh, c));
+                    }
+        },
+        [&](int64_t s, int from, int to) {
+            if (s != of) st = stats[s * sh.G + ln.g];
+            of = s;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int c = 0; c < CPL; ++c)
+                    if (ln.in[c] && u >= from && u < to) {
+                        float x[E], g[E];
+                        P::widen(rx[u][c], x);
+                        P::widen(rg[u][c], g);
+#pragma unroll
+                        for (int i = 0; i < E; ++i) {
+                            const float xh = (x[i] - st.x) * st.y;
+                            const float dz = act.back(ga[c][i] * xh + be[c][i], g[i], dsl);
+                            dga[c][i] += dz * xh;
+                            dbe[c][i] += dz;
+                            s1 += dz * ga[c][i];
+                            s2 += dz * ga[c][i] * xh;
                         }
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-#pragma unroll
-                    for (int c = 0; c < CPL; ++c)
-                        if (ln.in[c] && row + u < end) {
-                            float x[E], g[E];
-                            P::widen(rx[u][c], x);
-                            P::widen(rg[u][c], g);
-#pragma unroll
-                            for (int i = 0; i < E; ++i) {
-                                const float xh = (x[i] - st.x) * st.y;
-                                const float dz = act.back(ga[c][i] * xh + be[c][i], g[i], dsl);
-                                dga[c][i] += dz * xh;
-                                dbe[c][i] += dz;
-                                s1 += dz * ga[c][i];
-                                s2 += dz * ga[c][i] * xh;
-                            }
-                        }
-            }
+                    }
+        },
+        [&](int64_t tile, int64_t s) {
             s1 = lanes_sum(s1, sh.W);
             s2 = lanes_sum(s2, sh.W);
             if (ln.sub == 0) pairs[(tile + s) * sh.G + ln.g] = make_float2(s1, s2);
+            s1 = s2 = 0.0f;
         });
     store_sums<E, CPL>(sh, ln, dga, dbe, dsl, partial);
 }
@@ -595,53 +640,62 @@ __global__ __launch_bounds__(kGnThreads) void gn_apply_bwd_kernel(GnShape sh, Gn
     typedef Piece<T, E> P;
     constexpr int U = CPL == 1 ? 4 : 1;
     const GnLane<E, CPL> ln(sh);
-    if (!ln.live) return;
     const GnAct<kSilu, sizeof(T) == 4> act(sh.act, slope_p);
     float ga[CPL][E], be[CPL][E], unused = 0.0f;
     load_vector<E, CPL>(gamma, sh, ln, ga);
     load_vector<E, CPL>(beta, sh, ln, be);
-    for (int64_t tile = int64_t(blockIdx.x) * sh.tpb + ln.slot; tile < sg.tiles; tile += int64_t(gridDim.x) * sh.tpb)
-        walk_tile(sg, tile, [&](int64_t s, int64_t row, int64_t end) {
-            const float2 st = stats[s * sh.G + ln.g], m = means[s * sh.G + ln.g];
-            for (; row < end; row += U) {
-                typename P::Raw rx[U][CPL], rg[U][CPL];
+    typename P::Raw rx[U][CPL], rg[U][CPL];
+    float2 st = make_float2(0.0f, 0.0f), m = st;
+    int64_t of = -1, row0 = 0;
+    walk_tiles<U>(sh, sg, ln.slot, ln.live,
+        [&](int64_t row, int64_t end) {
+            row0 = row;
 #pragma unroll
-                for (int u = 0; u < U; ++u)
+            for (int u = 0; u < U; ++u)
 #pragma unroll
-                    for (int c = 0; c < CPL; ++c)
-                        if (ln.in[c] && row + u < end) {
-                            rx[u][c] = P::load(X + (row + u) * ldx + ln.col(sh, c));
-                            rg[u][c] = P::load(dY + (row + u) * ldd + ln.col(sh, c));
-                        }
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-#pragma unroll
-                    for (int c = 0; c < CPL; ++c)
-                        if (ln.in[c] && row + u < end) {
-                            float x[E], g[E];
-                            P::widen(rx[u][c], x);
-                            P::widen(rg[u][c], g);
-#pragma unroll
-                            for (int i = 0; i < E; ++i) {
-                                const float xh = (x[i] - st.x) * st.y;
-                                const float dz = act.back(ga[c][i] * xh + be[c][i], g[i], unused);
-                                x[i] = (dz * ga[c][i] - m.x - xh * m.y) * st.y;
-                            }
-                            P::store(dX + (row + u) * ldo + ln.col(sh, c), x);
-                        }
+                for (int c = 0; c < CPL; ++c)
+                    if (ln.in[c] && row + u < end) {
+                        rx[u][c] = P::load(X + (row + u) * ldx + ln.col(sh, c));
+                        rg[u][c] = P::load(dY + (row + u) * ldd + ln.col(sh, c));
+                    }
+        },
+        [&](int64_t s, int from, int to) {
+            if (s != of) {
+                st = stats[s * sh.G + ln.g];
+                m = means[s * sh.G + ln.g];
             }
-        });
+            of = s;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int c = 0; c < CPL; ++c)
+                    if (ln.in[c] && u >= from && u < to) {
+                        float x[E], g[E];
+                        P::widen(rx[u][c], x);
+                        P::widen(rg[u][c], g);
+#pragma unroll
+                        for (int i = 0; i < E; ++i) {
+                            const float xh = (x[i] - st.x) * st.y;
+                            const float dz = act.back(ga[c][i] * xh + be[c][i], g[i], unused);
+                            x[i] = (dz * ga[c][i] - m.x - xh * m.y) * st.y;
+                        }
+                        P::store(dX + (row0 + u) * ldo + ln.col(sh, c), x);
+                    }
+        },
+        [&](int64_t, int64_t) {});
 }
 
-// dgamma, dbeta, dslope from the blocks' rows: 16 columns a block, 16 slices of the rows each, combined in order
-__global__ __launch_bounds__(256) void gn_finish_kernel(int nb, int F, int parts, const float *__restrict__ partial, float *__restrict__ dgamma,
-                                                        float *__restrict__ dbeta, float *__restrict__ dslope)
+// dgamma, dbeta, dslope from the blocks' rows: 16 columns a block, 64 slices of the rows each, combined in order
+constexpr int kFinCols = 16, kFinSlices = 64;
+
+__global__ __launch_bounds__(kFinCols *kFinSlices) void gn_finish_kernel(int nb, int F, int parts, const float *__restrict__ partial, float *__restrict__ dgamma,
+                                                                        float *__restrict__ dbeta, float *__restrict__ dslope)
 {
-    __shared__ float part[16][16];
+    __shared__ float part[kFinSlices][kFinCols];
     const int64_t width = 2 * int64_t(F) + parts;
-    const int c = threadIdx.x % 16, slice = threadIdx.x / 16;
-    const int64_t j = int64_t(blockIdx.x) * 16 + c;
-    const int per = (nb + 15) / 16, b0 = slice * per, b1 = b0 + per < nb ? b0 + per : nb;
+    const int c = threadIdx.x % kFinCols, slice = threadIdx.x / kFinCols;
+    const int64_t j = int64_t(blockIdx.x) * kFinCols + c;
+    const int per = (nb + kFinSlices - 1) / kFinSlices, b0 = slice * per, b1 = b0 + per < nb ? b0 + per : nb;
     const int cells = j < 2 * int64_t(F) ? 1 : j == 2 * int64_t(F) ? parts : 0;
     float s0 = 0.0f, s1 = 0.0f, s2 = 0.0f, s3 = 0.0f;
     for (int q = 0; q < cells; ++q) {
@@ -659,7 +713,7 @@ __global__ __launch_bounds__(256) void gn_finish_kernel(int nb, int F, int parts
     __syncthreads();
     if (slice == 0 && cells > 0) {
         float s = 0.0f;
-        for (int k = 0; k < 16; ++k) s += part[k][c];
+        for (int k = 0; k < kFinSlices; ++k) s += part[k][c];
         if (j < F) dgamma[j] = s;
         else if (j < 2 * int64_t(F)) dbeta[j - F] = s;
         else if (dslope) *dslope = s;
@@ -960,6 +1014,6 @@ extern "C" int tma_groupnorm_act_bwd(int64_t n, int32_t F, int32_t G, int64_t n_
         if (int rc = check_launch(q.fn)) return rc;
     }
     TMA_TIMED("gn_finish", s);
-    hipLaunchKernelGGL(gn_finish_kernel, dim3(unsigned(ceil_div(2 * int64_t(F) + 1, 16))), dim3(256), 0, s, nb, F, sh.parts, partial, dgamma, dbeta, dslope);
+    hipLaunchKernelGGL(gn_finish_kernel, dim3(unsigned(ceil_div(2 * int64_t(F) + 1, kFinCols))), dim3(kFinCols * kFinSlices), 0, s, nb, F, sh.parts, partial, dgamma, dbeta, dslope);
     return check_launch(q.fn);
 }

@@ -33,19 +33,28 @@ template <typename T>
 __device__ __forceinline__ void stage_rows(const GroupList &gl, int64_t i0, int m, const T *g, const T *h, int64_t ld, int k0, int K,
                                            float (&rows)[kSideRows][kFewK + 4])
 {
-    const int width = K - k0 < kFewK ? K - k0 : kFewK;
-    for (int r = 0; r < kSideRows; ++r) {
-        const int64_t v = r < m ? gl.row(i0 + r) : -1;
-        for (int k = threadIdx.x; k < kFewK; k += kFewThreads) {
-            float x = 0.0f;
-            if (v >= 0 && k < width) {
-                x = read1(g + v * ld + k0 + k);
-                if (h && !(read1(h + v * ld + k0 + k) > 0.0f)) x = 0.0f;
-            }
-            rows[r][k] = x;
+    int64_t v[kSideRows];
+#pragma unroll
+    for (int r = 0; r < kSideRows; ++r) v[r] = r < m ? gl.row(i0 + r) : -1;
+    constexpr int kEach = kFewK / kFewThreads;
+    float x[kSideRows][kEach];
+#pragma unroll
+    for (int r = 0; r < kSideRows; ++r)
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const int k = k0 + j * kFewThreads + int(threadIdx.x);
+            const bool in = v[r] >= 0 && k < K;
+            const int64_t at = in ? v[r] * ld + k : 0;
+            x[r][j] = in ? read1(g + at) : 0.0f;
+            if (h && !(in && read1(h + at) > 0.0f)) x[r][j] = 0.0f;
         }
-    }
+#pragma unroll
+    for (int r = 0; r < kSideRows; ++r)
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) rows[r][j * kFewThreads + int(threadIdx.x)] = x[r][j];
 }
+
+constexpr int kFewW = kFewK / 32;      // pieces of weights of a thread in registers: all of its k-values of a chunk, on their way while rows are staged
 
 // Y[v][c] for the block's group and 32 columns.  Eight lanes share the columns, 32 of them the k-values.
 template <typename T>
@@ -60,42 +69,46 @@ __global__ __launch_bounds__(kFewThreads) void grouped_few_fwd_kernel(GroupList 
     const int q = int(threadIdx.x) % 8, ks = int(threadIdx.x) / 8, wave = int(threadIdx.x) / kWave, lane = int(threadIdx.x) % kWave;
     const int left = N - n0 - 4 * q;
     const float *Wg = W + int64_t(g) * K * N + n0 + 4 * q;
+    float4 w[kFewW];
     for (int64_t i0 = begin; i0 < end; i0 += kSideRows) {
         const int m = end - i0 < kSideRows ? int(end - i0) : kSideRows;
         float4 acc[kSideRows];
+#pragma unroll
         for (int r = 0; r < kSideRows; ++r) acc[r] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         for (int k0 = 0; k0 < K; k0 += kFewK) {
-            const int width = K - k0 < kFewK ? K - k0 : kFewK;
+            if (K > kFewK || i0 == begin) {        // (of a single chunk they stay)
+#pragma unroll
+                for (int j = 0; j < kFewW; ++j) {
+                    const int k = k0 + j * 32 + ks;
+                    w[j] = weights4(Wg + int64_t(k < K ? k : 0) * N, k < K ? left : 0, vec);
+                }
+            }
             __syncthreads();
             stage_rows<T>(gl, i0, m, X, nullptr, ldx, k0, K, rows);
             __syncthreads();
-#pragma unroll 4
-            for (int k = ks; k < width; k += 32) {
-                const float4 w = weights4(Wg + int64_t(k0 + k) * N, left, vec);
+#pragma unroll
+            for (int j = 0; j < kFewW; ++j) {
+                if (k0 + j * 32 >= K) break;
 #pragma unroll
                 for (int r = 0; r < kSideRows; ++r) {
-                    const float x = rows[r][k];
-                    acc[r].x = fmaf(x, w.x, acc[r].x);
-                    acc[r].y = fmaf(x, w.y, acc[r].y);
-                    acc[r].z = fmaf(x, w.z, acc[r].z);
-                    acc[r].w = fmaf(x, w.w, acc[r].w);
+                    const float x = rows[r][j * 32 + ks];
+                    acc[r].x = fmaf(x, w[j].x, acc[r].x);
+                    acc[r].y = fmaf(x, w[j].y, acc[r].y);
+                    acc[r].z = fmaf(x, w[j].z, acc[r].z);
+                    acc[r].w = fmaf(x, w[j].w, acc[r].w);
                 }
             }
         }
 #pragma unroll
         for (int r = 0; r < kSideRows; ++r) {
+#pragma unroll
             for (int d = 8; d < kWave; d *= 2) {
                 acc[r].x += __shfl_xor(acc[r].x, d, kWave);
                 acc[r].y += __shfl_xor(acc[r].y, d, kWave);
                 acc[r].z += __shfl_xor(acc[r].z, d, kWave);
                 acc[r].w += __shfl_xor(acc[r].w, d, kWave);
             }
-            if (lane < 8) {
-                sums[wave][r][4 * q] = acc[r].x;
-                sums[wave][r][4 * q + 1] = acc[r].y;
-                sums[wave][r][4 * q + 2] = acc[r].z;
-                sums[wave][r][4 * q + 3] = acc[r].w;
-            }
+            if (lane < 8) *reinterpret_cast<float4 *>(&sums[wave][r][4 * q]) = acc[r];
         }
         __syncthreads();
         const int r = int(threadIdx.x) / kFewCols, c = int(threadIdx.x) % kFewCols;
@@ -115,31 +128,40 @@ __global__ __launch_bounds__(kFewThreads) void grouped_few_bwd_data_kernel(Group
                                                                            const float *__restrict__ W, int N, bool vec, T *__restrict__ dX, int64_t ldx,
                                                                            int slices)
 {
-    __shared__ float rows[kSideRows][kFewK + 4];
+    __shared__ __attribute__((aligned(16))) float rows[kSideRows][kFewK + 4];
     const int g = int(blockIdx.x) / slices, i = int(blockIdx.x) % slices * kFewCols + int(threadIdx.x) / 8, q = int(threadIdx.x) % 8;
     const int64_t begin = gl.begin(g), end = gl.begin(g + 1);
     const float *Wi = W + (int64_t(g) * N + (i < N ? i : 0)) * K;
+    float4 w[kFewW];
     for (int64_t i0 = begin; i0 < end; i0 += kSideRows) {
         const int m = end - i0 < kSideRows ? int(end - i0) : kSideRows;
         float acc[kSideRows];
+#pragma unroll
         for (int r = 0; r < kSideRows; ++r) acc[r] = 0.0f;
         for (int k0 = 0; k0 < K; k0 += kFewK) {
-            const int width = K - k0 < kFewK ? K - k0 : kFewK;
+            if (K > kFewK || i0 == begin) {
+#pragma unroll
+                for (int j = 0; j < kFewW; ++j) {
+                    const int k = k0 + j * 32 + 4 * q;
+                    w[j] = weights4(Wi + (k < K ? k : 0), K - k, vec);
+                }
+            }
             __syncthreads();
             stage_rows<T>(gl, i0, m, dY, Yh, ldy, k0, K, rows);
             __syncthreads();
-#pragma unroll 4
-            for (int k = 4 * q; k < width; k += 32) {
-                const float4 w = weights4(Wi + k0 + k, width - k, vec);
+#pragma unroll
+            for (int j = 0; j < kFewW; ++j) {
+                if (k0 + j * 32 >= K) break;
 #pragma unroll
                 for (int r = 0; r < kSideRows; ++r) {
-                    const float4 x = *reinterpret_cast<const float4 *>(&rows[r][k]);
-                    acc[r] = fmaf(x.x, w.x, fmaf(x.y, w.y, fmaf(x.z, w.z, fmaf(x.w, w.w, acc[r]))));
+                    const float4 x = *reinterpret_cast<const float4 *>(&rows[r][j * 32 + 4 * q]);
+                    acc[r] = fmaf(x.x, w[j].x, fmaf(x.y, w[j].y, fmaf(x.z, w[j].z, fmaf(x.w, w[j].w, acc[r]))));
                 }
             }
         }
 #pragma unroll
         for (int r = 0; r < kSideRows; ++r) {
+#pragma unroll
             for (int d = 1; d < 8; d *= 2) acc[r] += __shfl_xor(acc[r], d, kWave);
             const int64_t v = r < m ? gl.row(i0 + r) : -1;
             if (q == 0 && i < N && v >= 0) write1(dX + v * ldx + i, acc[r]);
@@ -239,8 +261,10 @@ static int few_bwd(const char *fn, const GroupList &gl, const void *X, int64_t l
 }
 
 // ---- tiles ---------------------------------------------------------------------
-// Few rows: the vector kernels, which read the weights once as they are; else tiles, which first lay them out.
-static bool few_rows_a_group(int64_t n, int E) { return n <= 16 * int64_t(E); }
+// Few rows: the vector kernels, which read the weights once as they are; else tiles, which first lay them out.  Forward and backward of 16 groups of
+// 256 -> 256, in a graph, us: fp32 8 rows a group 16.0 + 34 and 18.6 + 46 in tiles, 16 rows 25 + 57 and 18.6 + 51; bf16 4 rows 12.3 + 26 and 14.7 + 29,
+// 8 rows 17 + 37 and 14.8 + 29 (256 groups of 128 -> 64: fp32 at 8 rows 19.5 and 19.7, bf16 at 4 rows 12.7 and 12.0).
+static bool few_rows_a_group(int64_t n, int E, int32_t dtype) { return n <= (dtype == TMA_BF16 ? 4 : 8) * int64_t(E); }
 
 struct TileShape {
     bool resident;         // weights in LDS, tiles of 32 rows; else tiles of 64 rows that fetch them
@@ -505,7 +529,7 @@ extern "C" size_t tma_grouped_dense_fwd_workspace_bytes(int64_t n, int32_t E, in
 {
     using namespace tma;
     if (n < 0 || E < 1 || F_in < 1 || F_out < 1) return 0;
-    if (few_rows_a_group(n, E)) return 256;
+    if (few_rows_a_group(n, E, dtype)) return 256;
     const TileShape t = tile_shape(E, F_in, F_out, dtype == TMA_BF16 ? 2 : 4, false);
     return plan_bytes(n, E, t.height) + t.bias_bytes + t.fragment_bytes;
 }
@@ -524,7 +548,7 @@ extern "C" int tma_grouped_dense_fwd(int64_t n, int32_t E, const int32_t *offset
     const GroupList gl{offsets, order, E, n};
     hipStream_t s = as_stream(stream);
     const bool relu = act == TMA_ACT_RELU;
-    if (!few_rows_a_group(n, E))
+    if (!few_rows_a_group(n, E, dtype))
         return dtype == TMA_F32 ? tiles_fwd<float>(fn, gl, X, ldx, F_in, W, bias, F_out, relu, Y_out, ldy, ws, s)
                                 : tiles_fwd<uint16_t>(fn, gl, X, ldx, F_in, W, bias, F_out, relu, Y_out, ldy, ws, s);
     return dtype == TMA_F32 ? few_fwd<float>(fn, gl, X, ldx, F_in, W, bias, F_out, relu, Y_out, ldy, s)
@@ -535,7 +559,7 @@ extern "C" size_t tma_grouped_dense_bwd_workspace_bytes(int64_t n, int32_t E, in
 {
     using namespace tma;
     if (n < 0 || E < 1 || F_in < 1 || F_out < 1) return 0;
-    if (few_rows_a_group(n, E)) return 256;
+    if (few_rows_a_group(n, E, dtype)) return 256;
     const int height = weight_shape(n, E, F_in, F_out).height;
     const size_t runs = size_t(tile_room(n, E, height));
     size_t bytes = plan_bytes(n, E, height) + round_up(runs * size_t(F_in) * size_t(F_out) * 4, 256) + round_up(runs * size_t(F_out) * 4, 256);
@@ -570,7 +594,7 @@ extern "C" int tma_grouped_dense_bwd(int64_t n, int32_t E, const int32_t *offset
     const GroupList gl{offsets, order, E, n};
     hipStream_t s = as_stream(stream);
     const bool relu = act == TMA_ACT_RELU;
-    if (!few_rows_a_group(n, E))
+    if (!few_rows_a_group(n, E, dtype))
         return dtype == TMA_F32 ? tiles_bwd<float>(fn, gl, X, ldx, Y, dY, ldy, W, F_in, F_out, relu, dW, dbias, dX_out, ld_dx, ws, s)
                                 : tiles_bwd<uint16_t>(fn, gl, X, ldx, Y, dY, ldy, W, F_in, F_out, relu, dW, dbias, dX_out, ld_dx, ws, s);
     return dtype == TMA_F32 ? few_bwd<float>(fn, gl, X, ldx, Y, dY, ldy, W, F_in, F_out, relu, dW, dbias, n > 0 ? dX_out : nullptr, ld_dx, s)
