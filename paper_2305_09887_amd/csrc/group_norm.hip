@@ -26,7 +26,7 @@ constexpr int kGnThreads = 256;
 constexpr int kGnMaxChannels = 1024;          // of a group
 constexpr int kGnBlocks = 256 * 8;            // forward: eight blocks fill a compute unit
 constexpr int kGnBwdBlocks = 1024;            // backward: as many partial rows of dgamma and dbeta
-constexpr int64_t kGnLanes = 256 * 2048;      // lanes that a pass over tiles should have
+constexpr int64_t kGnLanes = 256 * 1024;      // lanes that a pass over tiles should have
 constexpr int kGnChunk = 8;                   // rows of a lane in flight in the first pass
 
 template <int kBytes>

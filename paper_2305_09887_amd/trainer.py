@@ -30,12 +30,30 @@ class LocalTrainer:
     ends, runs the MLP decoder (PReLU between its layers, no bias) and takes the mean binary cross-entropy of its
     logits; ``labels`` is then unused.  The decoder's weights (Theta_k, and a slope per hidden layer) follow the
     encoder's in ``W``, so they are averaged with them.
+
+    ``norm_groups`` = G > 0 (with ``norm_act``): the hidden layers' channels are normalised in G groups per node instead
+    of all together; the same gamma, beta and slope.  ``dropout`` = p > 0: each hidden layer's output is dropped with
+    probability p while ``training`` is set (clear it to evaluate); layer l draws from the generator's stream
+    SplitMix64(dropout_seed, l) and the step's number, which is counted on the device, so that a captured step draws anew at every
+    replay.  ``node_kinds`` [n] int32 in [0, ``n_kinds``) (MLP encoder): every node is of one of several kinds, and a layer
+    has weights per kind, W [n_kinds, F_in, F_out] and bias [n_kinds, F_out].
     """
+
+    # (what a subclass with buffers of its own leaves as it is)
+    norm_groups, dropout, n_kinds, training = 0, 0.0, 0, True
 
     def __init__(self, rowptr, colidx, inv_deg, X, labels, dims, params=None, stream=None,
                  rowptr_T=None, colidx_T=None, norm_act=False, optimizer="sgd", encoder="sage",
-                 decoder_dims=None, batch_size=0, batch_seed=0, nnz=None):
+                 decoder_dims=None, batch_size=0, batch_seed=0, nnz=None, norm_groups=0, dropout=0.0, dropout_seed=0,
+                 node_kinds=None, n_kinds=0):
         self.norm_act = bool(norm_act)
+        self.norm_groups, self.dropout, self.n_kinds = int(norm_groups), float(dropout), int(n_kinds)
+        if self.norm_groups < 0 or (self.norm_groups and (not self.norm_act or any(f % self.norm_groups for f in dims[1:-1]))):
+            raise B.TmaError("LocalTrainer: norm_groups needs norm_act, and hidden widths that are multiples of it")
+        if not 0.0 <= self.dropout < 1.0:
+            raise B.TmaError("LocalTrainer: dropout must be in [0, 1)")
+        if (node_kinds is None) != (self.n_kinds == 0) or self.n_kinds < 0 or (self.n_kinds and encoder != "mlp"):
+            raise B.TmaError("LocalTrainer: node_kinds and n_kinds come together, with the MLP encoder")
         self.dec_dims = list(decoder_dims) if decoder_dims is not None else None
         if self.dec_dims is not None:
             if self.dec_dims[0] != dims[-1] or self.dec_dims[-1] != 1 or len(self.dec_dims) < 2 or batch_size < 1:
@@ -65,7 +83,7 @@ class LocalTrainer:
             raise B.TmaError("LocalTrainer: X width differs from dims[0]")
 
         n_w = 2 if encoder == "sage" else 1
-        self.n_params = sum(n_w * fi * fo + fo for fi, fo in zip(dims[:-1], dims[1:]))
+        self.n_params = max(self.n_kinds, 1) * sum(n_w * fi * fo + fo for fi, fo in zip(dims[:-1], dims[1:]))
         if self.norm_act:
             self.n_params += sum(2 * fo + 1 for fo in dims[1:-1])
         if self.dec_dims is not None:
@@ -103,10 +121,17 @@ class LocalTrainer:
             self.s_norm = torch.empty(self.n, dtype=torch.float32, device=dev)
             with torch.cuda.stream(self.stream):
                 B.tma_gcn_norm(rowptr, out=self.s_norm, stream=self.stream)
+        elif self.n_kinds:
+            ws_bytes = max(max(B.tma_grouped_dense_fwd_workspace_bytes(self.n, self.n_kinds, fi, fo, dt),
+                               B.tma_grouped_dense_bwd_workspace_bytes(self.n, self.n_kinds, fi, fo, dt, l > 0))
+                           for l, (fi, fo) in enumerate(pairs))
+            self.set_kinds(node_kinds)
         else:
             ws_bytes = max(B.tma_dense_bwd_workspace_bytes(self.n, fi, fo) for fi, fo in pairs)
         ws_bytes = max(ws_bytes, B.tma_loss_workspace_bytes(self.n, dims[-1]))
-        if self.norm_act and self.L > 1:
+        if self.norm_groups and self.L > 1:
+            ws_bytes = max(ws_bytes, max(B.tma_groupnorm_act_bwd_workspace_bytes(self.n, f, self.norm_groups, 1, dt) for f in dims[1:-1]))
+        elif self.norm_act and self.L > 1:
             ws_bytes = max(ws_bytes, max(B.tma_layernorm_prelu_bwd_workspace_bytes(self.n, f) for f in dims[1:-1]))
         if self.dec_dims is not None:
             Bn, dd = self.batch_size, self.dec_dims
@@ -122,6 +147,20 @@ class LocalTrainer:
         self.ws = torch.empty(max(ws_bytes, 256), dtype=torch.uint8, device=dev)
         self.loss = torch.zeros(1, dtype=torch.float32, device=dev)
         self.steps_done = 0
+        if self.dropout:
+            self.drop_seeds = [B.tma_mix64(int(dropout_seed), l) for l in range(self.L)]
+            self.drop_step = torch.zeros(1, dtype=torch.int64, device=dev)
+            self.stream.wait_stream(torch.cuda.current_stream(dev))
+
+    def set_kinds(self, node_kinds):
+        """The kind of each of the trainer's nodes (int32 in [0, n_kinds)); waits for the stream, to see that each has one."""
+        if node_kinds.numel() != self.n:
+            raise B.TmaError("LocalTrainer.set_kinds: one kind per node")
+        self.stream.wait_stream(torch.cuda.current_stream(node_kinds.device))
+        with torch.cuda.stream(self.stream):
+            self.kind_offsets, self.kind_order = B.tma_group_rows(node_kinds, self.n_kinds)
+            if int(self.kind_offsets[-1]) != self.n:
+                raise B.TmaError("LocalTrainer.set_kinds: a node's kind is outside [0, n_kinds)")
 
     def set_graph(self, rowptr, colidx, inv_deg, rowptr_T=None, colidx_T=None, nnz=None):
         """Point the trainer at a freshly extracted subgraph with the same node count."""
@@ -150,10 +189,14 @@ class LocalTrainer:
     def _views(self, flat):
         out, o = [], 0
         for l, (fi, fo) in enumerate(zip(self.dims[:-1], self.dims[1:])):
-            layer = []
-            for _ in range(self.n_lin - 1):
-                layer.append(flat[o:o + fi * fo].view(fi, fo)); o += fi * fo
-            layer.append(flat[o:o + fo]); o += fo
+            layer, E = [], self.n_kinds
+            if E:
+                layer.append(flat[o:o + E * fi * fo].view(E, fi, fo)); o += E * fi * fo
+                layer.append(flat[o:o + E * fo].view(E, fo)); o += E * fo
+            else:
+                for _ in range(self.n_lin - 1):
+                    layer.append(flat[o:o + fi * fo].view(fi, fo)); o += fi * fo
+                layer.append(flat[o:o + fo]); o += fo
             if self.norm_act and l < self.L - 1:
                 layer += [flat[o:o + fo], flat[o + fo:o + 2 * fo], flat[o + 2 * fo:o + 2 * fo + 1]]
                 o += 2 * fo + 1
@@ -202,6 +245,9 @@ class LocalTrainer:
         elif self.encoder == "gcn":
             B.tma_gcn_layer_fwd(self.rowptr, self.colidx, self.s_norm, self.H[l], lin[0], lin[1], act,
                                 M_out=self.M[l], Hnext_out=out, stream=self.stream)
+        elif self.n_kinds:
+            B.tma_grouped_dense_fwd(self.H[l], lin[0], lin[1], self.kind_offsets, act, order=self.kind_order, Y_out=out,
+                                    ws=self.ws, stream=self.stream)
         else:
             B.tma_dense_fwd(self.H[l], lin[0], lin[1], act, Y_out=out, stream=self.stream)
 
@@ -215,9 +261,17 @@ class LocalTrainer:
             B.tma_gcn_layer_bwd(self.rowptr_T, self.colidx_T, self.s_norm, self.H[l], self.M[l], out_act,
                                 self.dH[l + 1], lin[0], act, dW=g[0], dbias=g[1], dH_out=self.dH[l], need_dH=l > 0, ws=self.ws,
                                 stream=self.stream)
+        elif self.n_kinds:
+            B.tma_grouped_dense_bwd(self.H[l], out_act, self.dH[l + 1], lin[0], self.kind_offsets, act, order=self.kind_order,
+                                    dW=g[0], dbias=g[1], dX_out=self.dH[l], need_dX=l > 0, ws=self.ws, stream=self.stream)
         else:
             B.tma_dense_bwd(self.H[l], out_act, self.dH[l + 1], lin[0], act, dW=g[0], dbias=g[1], dX_out=self.dH[l],
                             need_dX=l > 0, ws=self.ws, stream=self.stream)
+
+    def _drop(self, call, t, l):
+        """Dropout of hidden layer l's output, or of its gradient, in place."""
+        if self.dropout and self.training and l < self.L - 1:
+            call(t, self.dropout, self.drop_seeds[l], step=self.drop_step, out=t, stream=self.stream)
 
     def time_layers(self, on: bool = True):
         """Bracket every encoder layer's forward and backward with a pair of events on the trainer's stream
@@ -245,9 +299,14 @@ class LocalTrainer:
             if self.norm_act and l < self.L - 1:
                 gamma, beta, slope = self.layers[l][self.n_lin:]
                 self._layer_fwd(l, B.TMA_ACT_NONE, self.Z[l + 1])
-                B.tma_layernorm_prelu_fwd(self.Z[l + 1], gamma, beta, slope, out=self.H[l + 1], stream=self.stream)
+                if self.norm_groups:
+                    B.tma_groupnorm_act_fwd(self.Z[l + 1], self.norm_groups, gamma, beta, B.TMA_ACT_PRELU, slope=slope,
+                                            eps=B.LN_EPS, out=self.H[l + 1], stream=self.stream)
+                else:
+                    B.tma_layernorm_prelu_fwd(self.Z[l + 1], gamma, beta, slope, out=self.H[l + 1], stream=self.stream)
             else:
                 self._layer_fwd(l, B.TMA_ACT_RELU if l < self.L - 1 else B.TMA_ACT_NONE, self.H[l + 1])
+            self._drop(B.tma_dropout_fwd, self.H[l + 1], l)
             self._mark("fwd", l)
         return self.H[self.L]
 
@@ -293,12 +352,19 @@ class LocalTrainer:
             self._mark("bwd", l)
             act = B.TMA_ACT_RELU if l < self.L - 1 else B.TMA_ACT_NONE
             out_act = self.H[l + 1]
+            # (a dropped ReLU output is zero, and so is its gradient: the sign of what is left still decides)
+            self._drop(B.tma_dropout_bwd, self.dH[l + 1], l)
             if self.norm_act and l < self.L - 1:
                 gamma, beta, slope = self.layers[l][self.n_lin:]
                 dgamma, dbeta, dslope = self.grads[l][self.n_lin:]
                 # dL/dZ replaces dL/dH' in place; the layer below then runs without an activation of its own
-                B.tma_layernorm_prelu_bwd(self.Z[l + 1], self.dH[l + 1], gamma, beta, slope, dZ_out=self.dH[l + 1],
-                                          dgamma=dgamma, dbeta=dbeta, dslope=dslope, ws=self.ws, stream=self.stream)
+                if self.norm_groups:
+                    B.tma_groupnorm_act_bwd(self.Z[l + 1], self.dH[l + 1], self.norm_groups, gamma, beta, B.TMA_ACT_PRELU,
+                                            slope=slope, eps=B.LN_EPS, dX_out=self.dH[l + 1], dgamma=dgamma, dbeta=dbeta,
+                                            dslope=dslope, ws=self.ws, stream=self.stream)
+                else:
+                    B.tma_layernorm_prelu_bwd(self.Z[l + 1], self.dH[l + 1], gamma, beta, slope, dZ_out=self.dH[l + 1],
+                                              dgamma=dgamma, dbeta=dbeta, dslope=dslope, ws=self.ws, stream=self.stream)
                 act, out_act = B.TMA_ACT_NONE, self.Z[l + 1]
             self._layer_bwd(l, act, out_act)
             self._mark("bwd", l)
@@ -309,6 +375,9 @@ class LocalTrainer:
         else:
             B.tma_sgd_step(self.W, self.dW, lr, stream=self.stream)
         self.steps_done += 1
+        if self.dropout:
+            with torch.cuda.stream(self.stream):
+                self.drop_step.add_(1)
 
     def step(self, lr: float):
         """One iteration of Alg. 2's loop body on the full local subgraph."""
