@@ -394,17 +394,21 @@ __global__ __launch_bounds__(kGgThreads, (kRowBlocksPerCu<TN, PP, kMask>)) void 
                 for (int j = 0; j < TN; ++j) b[u][j] = weights(j, s0 + u);
             __syncthreads();           // everyone has read what was there
             const int valid = q.K - (c * PP + piece) * E;
+            if constexpr (kMask) {
 #pragma unroll
-            for (int i = 0; i < kPieces; ++i) {
-                uint4 p = held[i];
-                if constexpr (kMask) p = open_piece<T>(p, mask[i]);
-                if (ragged) {
-                    const int64_t over = element(at, i, c) - last;
-                    if (over > 0) p = P::moved(p, int(over));
-                    p = P::cut(p, valid);
-                } else if (valid <= 0) p = make_uint4(0u, 0u, 0u, 0u);
-                As[spread<PP>(row0 + i * kRowsAtOnce, piece)] = p;
+                for (int i = 0; i < kPieces; ++i) held[i] = open_piece<T>(held[i], mask[i]);
             }
+            if (ragged) {
+#pragma unroll
+                for (int i = 0; i < kPieces; ++i) {
+                    const int64_t over = element(at, i, c) - last;
+                    if (over > 0) held[i] = P::moved(held[i], int(over));
+                    held[i] = P::cut(held[i], valid);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i)
+                As[spread<PP>(row0 + i * kRowsAtOnce, piece)] = valid > 0 ? held[i] : make_uint4(0u, 0u, 0u, 0u);
             if (c == 0 && tid < kTileM) rows[at ^ 1][tid] = pending;
             __syncthreads();
             if (c + 1 < chunks) fetch(at, c + 1);
@@ -449,18 +453,34 @@ __global__ __launch_bounds__(kGgThreads, (kRowBlocksPerCu<TN, PP, kMask>)) void 
                 Chunk<T>::store(reinterpret_cast<T *>(&mine[spread<kRowPieces>(l31, hi * (kRowPieces / 2) + x)]), z);
             }
             __builtin_amdgcn_wave_barrier();
+            constexpr int kStores = kRowPieces / 2;
+            uint4 z[kStores];
+            int32_t v[kStores];
+            bool full = true;
+            const int p = lane % kRowPieces, col = col0 + p * E;
 #pragma unroll
-            for (int x = 0; x < kRowPieces / 2; ++x) {
-                const int r = x * (64 / kRowPieces) + lane / kRowPieces, p = lane % kRowPieces, col = col0 + p * E;
-                const uint4 z = mine[spread<kRowPieces>(r, p)];
-                const int64_t v = rows[at][(wm * TM + i) * 32 + r];
-                if (v < 0 || col >= q.N) continue;
-                T *out = C + v * q.ldc + col;
+            for (int x = 0; x < kStores; ++x) {
+                const int r = x * (64 / kRowPieces) + lane / kRowPieces;
+                z[x] = mine[spread<kRowPieces>(r, p)];
+                v[x] = rows[at][(wm * TM + i) * 32 + r];
+                full = full && v[x] >= 0;
+            }
+            __builtin_amdgcn_wave_barrier();
+            if (kStore16 && __all(full) && col0 + TN * 32 <= q.N) {      // (without a branch between the stores)
+#pragma unroll
+                for (int x = 0; x < kStores; ++x)
+                    __builtin_nontemporal_store(Words4{z[x].x, z[x].y, z[x].z, z[x].w}, reinterpret_cast<Words4 *>(C + int64_t(v[x]) * q.ldc + col));
+                continue;
+            }
+#pragma unroll
+            for (int x = 0; x < kStores; ++x) {
+                if (v[x] < 0 || col >= q.N) continue;
+                T *out = C + int64_t(v[x]) * q.ldc + col;
                 if (kStore16 && col + E <= q.N) {
-                    *reinterpret_cast<Words4 *>(out) = Words4{z.x, z.y, z.z, z.w};
+                    *reinterpret_cast<Words4 *>(out) = Words4{z[x].x, z[x].y, z[x].z, z[x].w};
                 } else {
                     float w[E];
-                    Chunk<T>::widen(z, w);
+                    Chunk<T>::widen(z[x], w);
 #pragma unroll
                     for (int y = 0; y < E; ++y)
                         if (col + y < q.N) {
@@ -469,7 +489,6 @@ __global__ __launch_bounds__(kGgThreads, (kRowBlocksPerCu<TN, PP, kMask>)) void 
                         }
                 }
             }
-            __builtin_amdgcn_wave_barrier();
         }
         if (!more) return;
         share.item = next;
