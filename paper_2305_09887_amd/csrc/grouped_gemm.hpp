@@ -62,13 +62,15 @@ struct TilePlan {        // in the workspace
     int64_t room;        // tiles that fit
 };
 
-// tiles of the groups before each one, in LDS; returns their number.  Blocks of kGgThreads.
-__device__ __forceinline__ int tile_prefix(const GroupList &gl, int height, int (&prefix)[kMaxGroups + 1])
+// Tiles of the groups before each one, in LDS; returns their number.  Blocks of kGgThreads.  Offsets that descend somewhere can ask for any number of
+// tiles: no more than there is room for are counted, so that no one looks for others.
+__device__ __forceinline__ int tile_prefix(const GroupList &gl, int height, int64_t room, int (&prefix)[kMaxGroups + 1])
 {
-    __shared__ int wave_sums[kGgThreads / kWave];
+    __shared__ int64_t wave_sums[kGgThreads / kWave];
     constexpr int kPer = kMaxGroups / kGgThreads;
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    int count[kPer], total = 0;
+    int count[kPer];
+    int64_t total = 0;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
         const int g = int(threadIdx.x) * kPer + j;
@@ -76,14 +78,14 @@ __device__ __forceinline__ int tile_prefix(const GroupList &gl, int height, int 
         count[j] = rows > 0 ? int((rows + height - 1) / height) : 0;
         total += count[j];
     }
-    int incl = total;
+    int64_t incl = total;
     for (int d = 1; d < kWave; d <<= 1) {
-        const int t = __shfl_up(incl, d, kWave);
+        const int64_t t = __shfl_up(incl, d, kWave);
         if (lane >= d) incl += t;
     }
     if (lane == kWave - 1) wave_sums[wave] = incl;
     __syncthreads();
-    int at = incl - total, all = 0;
+    int64_t at = incl - total, all = 0;
     for (int w = 0; w < kGgThreads / kWave; ++w) {
         if (w < wave) at += wave_sums[w];
         all += wave_sums[w];
@@ -91,22 +93,23 @@ __device__ __forceinline__ int tile_prefix(const GroupList &gl, int height, int 
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
         const int g = int(threadIdx.x) * kPer + j;
-        if (g < gl.E) prefix[g] = at;
+        if (g < gl.E) prefix[g] = int(at < room ? at : room);
         at += count[j];
     }
-    if (threadIdx.x == 0) prefix[gl.E] = all;
+    if (all > room) all = room;
+    if (threadIdx.x == 0) prefix[gl.E] = int(all);
     __syncthreads();
-    return all;
+    return int(all);
 }
 
 __device__ __forceinline__ void write_plan(const GroupList &gl, const TilePlan &p, int block)
 {
     __shared__ int prefix[kMaxGroups + 1];
-    const int all = tile_prefix(gl, p.height, prefix);
+    const int all = tile_prefix(gl, p.height, p.room, prefix);
     if (block == 0)
         for (int g = threadIdx.x; g <= gl.E; g += kGgThreads) p.first[g] = prefix[g];
     const int i = block * kGgThreads + threadIdx.x;
-    if (i >= all || i >= p.room) return;
+    if (i >= all) return;
     int lo = 0, hi = gl.E;             // the last group that begins at or before i
     while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;

@@ -260,3 +260,21 @@ def test_gradients_against_differences(B):
         hi[at], lo[at] = t + step * d, t - step * d
         slope = (f(*hi) - f(*lo)) / (2 * step)
         assert abs(slope - (grad.double() * d.double()).sum().item()) <= 8 * 34 * u * mass * 4
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_offsets_that_descend_touch_nothing_else(B, dtype):
+    """Not a list that tma_group_rows writes, so the results are anything: but they stay in the outputs, and the call ends."""
+    n, E, F_in, F_out = 3000, 64, 40, 24
+    g = torch.Generator().manual_seed(5)
+    W = torch.randn(E, F_in, F_out, generator=g).cuda()
+    offsets = torch.tensor([0, n] * (E // 2) + [0], dtype=torch.int32, device="cuda")
+    whole = {F: torch.full((n + 64, 48), 3.0, dtype=dtype, device="cuda") for F in (F_in, F_out)}
+    X = torch.ones(n, F_in, dtype=dtype, device="cuda")
+    dY = torch.ones(n, 48, dtype=dtype, device="cuda")[:, :F_out]
+    Y, dX = whole[F_out][32:32 + n, :F_out], whole[F_in][32:32 + n, :F_in]
+    B.tma_grouped_dense_fwd(X, W, None, offsets, B.TMA_ACT_RELU, Y_out=Y)
+    B.tma_grouped_dense_bwd(X, Y, dY, W, offsets, B.TMA_ACT_RELU, dX_out=dX)
+    torch.cuda.synchronize()
+    for F, t in whole.items():
+        assert (t[:32] == 3).all() and (t[32 + n:] == 3).all() and (t[:, F:] == 3).all()
