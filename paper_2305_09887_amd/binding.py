@@ -55,6 +55,25 @@ class TmaError(RuntimeError):
 _lib = None
 
 
+# Argument types (i int32, l int64, u uint64, z size_t, f float, d double, p address): these calls take plain numbers and addresses.  On a few rows
+# the host's share is what counts, and an object for each of some twenty arguments is a good part of it.
+_CODES = {"i": C.c_int32, "l": C.c_int64, "u": C.c_uint64, "z": C.c_size_t, "f": C.c_float, "d": C.c_double, "p": C.c_void_p}
+_SIGNATURES = {
+    "tma_group_rows_workspace_bytes": "li",
+    "tma_group_rows": "lpipppzp",
+    "tma_grouped_dense_fwd_workspace_bytes": "liiii",
+    "tma_grouped_dense_fwd": "lippplippiiiplpzp",
+    "tma_grouped_dense_bwd_workspace_bytes": "liiiii",
+    "tma_grouped_dense_bwd": "lippplpplpiiiippplpzp",
+    "tma_groupnorm_act_fwd_workspace_bytes": "liili",
+    "tma_groupnorm_act_fwd": "liilplplpppfiiplppzp",
+    "tma_groupnorm_act_bwd_workspace_bytes": "liili",
+    "tma_groupnorm_act_bwd": "liilplplplpppfiipplppppzp",
+    "tma_dropout_fwd": "lipldupliplp",
+    "tma_dropout_bwd": "lipldupliplp",
+}
+
+
 def lib() -> C.CDLL:
     """The loaded C library (raises if libtma.so is missing)."""
     global _lib
@@ -74,6 +93,8 @@ def lib() -> C.CDLL:
                      "tma_grouped_dense_fwd_workspace_bytes", "tma_grouped_dense_bwd_workspace_bytes",
                      "tma_groupnorm_act_fwd_workspace_bytes", "tma_groupnorm_act_bwd_workspace_bytes"):
             getattr(L, name).restype = C.c_size_t
+        for name, codes in _SIGNATURES.items():
+            getattr(L, name).argtypes = [_CODES[c] for c in codes]
         L.tma_mix64.restype = C.c_uint64
         L.tma_mix64.argtypes = [C.c_uint64, C.c_uint64]
         _lib = L
@@ -893,7 +914,7 @@ def _launch(device, stream, call, *args):
     """call(*args, stream) with the tensors' device as the current one (the library launches on that) and, where none is
     given, that device's current stream."""
     index = device.index
-    s = C.c_void_p((torch.cuda.current_stream(index) if stream is None else stream).cuda_stream)
+    s = (torch.cuda.current_stream(index) if stream is None else stream).cuda_stream
     if index == torch.cuda.current_device():
         _check(call(*args, s))
     else:
@@ -901,25 +922,36 @@ def _launch(device, stream, call, *args):
             _check(call(*args, s))
 
 
-def _rows_like(t, name, shape, dtype, device):
+def _rows_like(t, name, shape, dtype):
     """A [rows, cols] tensor of the given shape and type with unit inner stride: its leading dimension."""
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device:
-        raise TmaError(f"{name}: expected {tuple(shape)} of {dtype} on {device}")
+    if t.shape != shape or t.dtype != dtype:
+        raise TmaError(f"{name}: expected {tuple(shape)} of {dtype}")
     ld = _rows_ld(t, name)[2]
     if ld < shape[1]:
         raise TmaError(f"{name}: rows overlap")
     return ld
 
 
-def _vector(t, name, shape, dtype, device):
-    """A dense tensor of the given shape and type."""
-    if tuple(t.shape) != tuple(shape) or t.device != device:
-        raise TmaError(f"{name}: expected shape {tuple(shape)} on {device}")
-    return _ptr(t, dtype, name)
+def _vector(t, name, shape, dtype):
+    """The address of a dense tensor of the given shape and type, or None."""
+    if t is None:
+        return None
+    if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
+        raise TmaError(f"{name}: expected a contiguous tensor of shape {tuple(shape)}, {dtype}")
+    return t.data_ptr()
+
+
+def _room(ws):
+    """A workspace as the library takes it: address and bytes."""
+    if ws is None:
+        return None, 0
+    if not ws.is_contiguous():
+        raise TmaError("ws: expected a contiguous tensor")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
 def tma_group_rows_workspace_bytes(n: int, E: int) -> int:
-    return int(lib().tma_group_rows_workspace_bytes(C.c_int64(n), C.c_int32(E)))
+    return int(lib().tma_group_rows_workspace_bytes(n, E))
 
 
 def tma_group_rows(group, E: int, offsets_out=None, order_out=None, ws=None, stream=None):
@@ -935,15 +967,14 @@ def tma_group_rows(group, E: int, offsets_out=None, order_out=None, ws=None, str
         order_out = _record(torch.empty(n, dtype=torch.int32, device=dev), stream)
     if ws is None:
         ws = _workspace(tma_group_rows_workspace_bytes(n, E), dev, stream)
-    _launch(dev, stream, lib().tma_group_rows, C.c_int64(n), _ptr(group, torch.int32, "group"), C.c_int32(E),
-            _vector(offsets_out, "offsets_out", (E + 1,), torch.int32, dev), _vector(order_out, "order_out", (n,), torch.int32, dev),
-            _ptr(ws), C.c_size_t(ws.numel() * ws.element_size()))
+    _launch(dev, stream, lib().tma_group_rows, n, _vector(group, "group", (n,), torch.int32), E,
+            _vector(offsets_out, "offsets_out", (E + 1,), torch.int32), _vector(order_out, "order_out", (n,), torch.int32),
+            *_room(ws))
     return offsets_out, order_out
 
 
 def tma_grouped_dense_fwd_workspace_bytes(n: int, E: int, F_in: int, F_out: int, dtype: int) -> int:
-    return int(lib().tma_grouped_dense_fwd_workspace_bytes(C.c_int64(n), C.c_int32(E), C.c_int32(F_in), C.c_int32(F_out),
-                                                           C.c_int32(dtype)))
+    return int(lib().tma_grouped_dense_fwd_workspace_bytes(n, E, F_in, F_out, dtype))
 
 
 def tma_grouped_dense_fwd(X, W, bias, offsets, act: int, order=None, Y_out=None, ws=None, stream=None):
@@ -958,21 +989,15 @@ def tma_grouped_dense_fwd(X, W, bias, offsets, act: int, order=None, Y_out=None,
         Y_out = _record(_padded(n, F_out, X.dtype, dev), stream)
     if ws is None:
         ws = _workspace(tma_grouped_dense_fwd_workspace_bytes(n, E, F_in, F_out, _feat_dtype(X)), dev, stream)
-    _launch(dev, stream, lib().tma_grouped_dense_fwd, C.c_int64(n), C.c_int32(E),
-            _vector(offsets, "offsets", (E + 1,), torch.int32, dev),
-            _vector(order, "order", (n,), torch.int32, dev) if order is not None else C.c_void_p(0),
-            C.c_void_p(X.data_ptr()), C.c_int64(_rows_like(X, "X", (n, F_in), X.dtype, dev)), C.c_int32(F_in),
-            _ptr(W, torch.float32, "W"),
-            _vector(bias, "bias", (E, F_out), torch.float32, dev) if bias is not None else C.c_void_p(0), C.c_int32(F_out),
-            C.c_int32(act), C.c_int32(_feat_dtype(X)), C.c_void_p(Y_out.data_ptr()),
-            C.c_int64(_rows_like(Y_out, "Y_out", (n, F_out), X.dtype, dev)), _ptr(ws),
-            C.c_size_t(ws.numel() * ws.element_size()))
+    _launch(dev, stream, lib().tma_grouped_dense_fwd, n, E, _vector(offsets, "offsets", (E + 1,), torch.int32),
+            _vector(order, "order", (n,), torch.int32), X.data_ptr(), _rows_like(X, "X", (n, F_in), X.dtype), F_in,
+            _vector(W, "W", (E, F_in, F_out), torch.float32), _vector(bias, "bias", (E, F_out), torch.float32), F_out, act,
+            _feat_dtype(X), Y_out.data_ptr(), _rows_like(Y_out, "Y_out", (n, F_out), X.dtype), *_room(ws))
     return Y_out
 
 
 def tma_grouped_dense_bwd_workspace_bytes(n: int, E: int, F_in: int, F_out: int, dtype: int, need_dX: bool = True) -> int:
-    return int(lib().tma_grouped_dense_bwd_workspace_bytes(C.c_int64(n), C.c_int32(E), C.c_int32(F_in), C.c_int32(F_out),
-                                                           C.c_int32(dtype), C.c_int32(1 if need_dX else 0)))
+    return int(lib().tma_grouped_dense_bwd_workspace_bytes(n, E, F_in, F_out, dtype, 1 if need_dX else 0))
 
 
 def tma_grouped_dense_bwd(X, Y, dY, W, offsets, act: int, order=None, dW=None, dbias=None, dX_out=None, need_dbias=True,
@@ -983,11 +1008,11 @@ def tma_grouped_dense_bwd(X, Y, dY, W, offsets, act: int, order=None, dW=None, d
     if W.dim() != 3 or W.shape[1] != F_in:
         raise TmaError("tma_grouped_dense_bwd: W must be [E, F_in, F_out]")
     E, _, F_out = W.shape
-    ldy = _rows_like(dY, "dY", (n, F_out), X.dtype, dev)
+    ldy = _rows_like(dY, "dY", (n, F_out), X.dtype)
     if act == TMA_ACT_RELU:
         if Y is None:
             raise TmaError("tma_grouped_dense_bwd: Y is required with ReLU")
-        _rows_like(Y, "Y", (n, F_out), X.dtype, dev)
+        _rows_like(Y, "Y", (n, F_out), X.dtype)
         _same_ld(Y, dY, "tma_grouped_dense_bwd: Y / dY")
     if dW is None:
         dW = _record(torch.empty((E, F_in, F_out), dtype=torch.float32, device=dev), stream)
@@ -999,19 +1024,15 @@ def tma_grouped_dense_bwd(X, Y, dY, W, offsets, act: int, order=None, dW=None, d
         dX_out = _record(_padded(n, F_in, X.dtype, dev), stream)
     if not need_dX:
         dX_out = None
-    ld_dx = _rows_like(dX_out, "dX_out", (n, F_in), X.dtype, dev) if dX_out is not None else F_in
+    ld_dx = _rows_like(dX_out, "dX_out", (n, F_in), X.dtype) if dX_out is not None else F_in
     if ws is None:
         ws = _workspace(tma_grouped_dense_bwd_workspace_bytes(n, E, F_in, F_out, _feat_dtype(X), need_dX), dev, stream)
-    _launch(dev, stream, lib().tma_grouped_dense_bwd, C.c_int64(n), C.c_int32(E),
-            _vector(offsets, "offsets", (E + 1,), torch.int32, dev),
-            _vector(order, "order", (n,), torch.int32, dev) if order is not None else C.c_void_p(0),
-            C.c_void_p(X.data_ptr()), C.c_int64(_rows_like(X, "X", (n, F_in), X.dtype, dev)),
-            C.c_void_p(Y.data_ptr() if Y is not None else 0), C.c_void_p(dY.data_ptr()), C.c_int64(ldy),
-            _ptr(W, torch.float32, "W"), C.c_int32(F_in), C.c_int32(F_out), C.c_int32(act), C.c_int32(_feat_dtype(X)),
-            _vector(dW, "dW", (E, F_in, F_out), torch.float32, dev),
-            _vector(dbias, "dbias", (E, F_out), torch.float32, dev) if dbias is not None else C.c_void_p(0),
-            C.c_void_p(dX_out.data_ptr() if dX_out is not None else 0), C.c_int64(ld_dx), _ptr(ws),
-            C.c_size_t(ws.numel() * ws.element_size()))
+    _launch(dev, stream, lib().tma_grouped_dense_bwd, n, E, _vector(offsets, "offsets", (E + 1,), torch.int32),
+            _vector(order, "order", (n,), torch.int32), X.data_ptr(), _rows_like(X, "X", (n, F_in), X.dtype),
+            Y.data_ptr() if Y is not None else None, dY.data_ptr(), ldy, _vector(W, "W", (E, F_in, F_out), torch.float32),
+            F_in, F_out, act, _feat_dtype(X), _vector(dW, "dW", (E, F_in, F_out), torch.float32),
+            _vector(dbias, "dbias", (E, F_out), torch.float32), dX_out.data_ptr() if dX_out is not None else None, ld_dx,
+            *_room(ws))
     return dW, dbias, dX_out
 
 
@@ -1020,16 +1041,15 @@ def _norm_segments(where, n, segments, rows_per_segment, dev):
     if segments is not None:
         if segments.dim() != 1 or segments.numel() < 2:
             raise TmaError(f"{where}: segments must be offsets of at least one segment")
-        return segments.numel() - 1, _ptr(segments, torch.int32, "segments"), 0, False
+        return segments.numel() - 1, _vector(segments, "segments", segments.shape, torch.int32), 0, False
     R = int(rows_per_segment)
     if R < 1 or n % R:
         raise TmaError(f"{where}: {n} rows are no runs of {R}")
-    return n // R, C.c_void_p(0), R, R == 1
+    return n // R, None, R, R == 1
 
 
 def tma_groupnorm_act_fwd_workspace_bytes(n: int, F: int, G: int, n_segments: int, dtype: int) -> int:
-    return int(lib().tma_groupnorm_act_fwd_workspace_bytes(C.c_int64(n), C.c_int32(F), C.c_int32(G), C.c_int64(n_segments),
-                                                           C.c_int32(dtype)))
+    return int(lib().tma_groupnorm_act_fwd_workspace_bytes(n, F, G, n_segments, dtype))
 
 
 def tma_groupnorm_act_fwd(X, G: int, gamma, beta, act: int = TMA_ACT_NONE, slope=None, segments=None, rows_per_segment: int = 1,
@@ -1050,20 +1070,15 @@ def tma_groupnorm_act_fwd(X, G: int, gamma, beta, act: int = TMA_ACT_NONE, slope
         stats_out = _record(torch.empty((S, G, 2), dtype=torch.float32, device=dev), stream)
     if ws is None and not single:
         ws = _workspace(tma_groupnorm_act_fwd_workspace_bytes(n, F, G, S, _feat_dtype(X)), dev, stream)
-    _launch(dev, stream, lib().tma_groupnorm_act_fwd, C.c_int64(n), C.c_int32(F), C.c_int32(G), C.c_int64(S), seg, C.c_int64(R),
-            C.c_void_p(X.data_ptr()), C.c_int64(_rows_like(X, "X", (n, F), X.dtype, dev)),
-            _vector(gamma, "gamma", (F,), torch.float32, dev), _vector(beta, "beta", (F,), torch.float32, dev),
-            _vector(slope, "slope", (1,), torch.float32, dev) if slope is not None else C.c_void_p(0), C.c_float(eps),
-            C.c_int32(act), C.c_int32(_feat_dtype(X)), C.c_void_p(out.data_ptr()),
-            C.c_int64(_rows_like(out, "out", (n, F), X.dtype, dev)),
-            _vector(stats_out, "stats_out", (S, G, 2), torch.float32, dev) if stats_out is not None else C.c_void_p(0),
-            _ptr(ws), C.c_size_t(ws.numel() * ws.element_size() if ws is not None else 0))
+    _launch(dev, stream, lib().tma_groupnorm_act_fwd, n, F, G, S, seg, R, X.data_ptr(), _rows_like(X, "X", (n, F), X.dtype),
+            _vector(gamma, "gamma", (F,), torch.float32), _vector(beta, "beta", (F,), torch.float32),
+            _vector(slope, "slope", (1,), torch.float32), eps, act, _feat_dtype(X), out.data_ptr(),
+            _rows_like(out, "out", (n, F), X.dtype), _vector(stats_out, "stats_out", (S, G, 2), torch.float32), *_room(ws))
     return out, stats_out
 
 
 def tma_groupnorm_act_bwd_workspace_bytes(n: int, F: int, G: int, n_segments: int, dtype: int) -> int:
-    return int(lib().tma_groupnorm_act_bwd_workspace_bytes(C.c_int64(n), C.c_int32(F), C.c_int32(G), C.c_int64(n_segments),
-                                                           C.c_int32(dtype)))
+    return int(lib().tma_groupnorm_act_bwd_workspace_bytes(n, F, G, n_segments, dtype))
 
 
 def tma_groupnorm_act_bwd(X, dY, G: int, gamma, beta, act: int = TMA_ACT_NONE, slope=None, segments=None,
@@ -1089,17 +1104,12 @@ def tma_groupnorm_act_bwd(X, dY, G: int, gamma, beta, act: int = TMA_ACT_NONE, s
         dslope = _record(torch.empty(1, dtype=torch.float32, device=dev), stream)
     if ws is None:
         ws = _workspace(tma_groupnorm_act_bwd_workspace_bytes(n, F, G, 1 if single else max(S, 1), _feat_dtype(X)), dev, stream)
-    _launch(dev, stream, lib().tma_groupnorm_act_bwd, C.c_int64(n), C.c_int32(F), C.c_int32(G), C.c_int64(S), seg, C.c_int64(R),
-            C.c_void_p(X.data_ptr()), C.c_int64(_rows_like(X, "X", (n, F), X.dtype, dev)),
-            C.c_void_p(dY.data_ptr()), C.c_int64(_rows_like(dY, "dY", (n, F), X.dtype, dev)),
-            _vector(gamma, "gamma", (F,), torch.float32, dev), _vector(beta, "beta", (F,), torch.float32, dev),
-            _vector(slope, "slope", (1,), torch.float32, dev) if slope is not None else C.c_void_p(0), C.c_float(eps),
-            C.c_int32(act), C.c_int32(_feat_dtype(X)),
-            _vector(stats, "stats", (S, G, 2), torch.float32, dev) if not single else C.c_void_p(0),
-            C.c_void_p(dX_out.data_ptr()), C.c_int64(_rows_like(dX_out, "dX_out", (n, F), X.dtype, dev)),
-            _vector(dgamma, "dgamma", (F,), torch.float32, dev), _vector(dbeta, "dbeta", (F,), torch.float32, dev),
-            _vector(dslope, "dslope", (1,), torch.float32, dev) if dslope is not None else C.c_void_p(0), _ptr(ws),
-            C.c_size_t(ws.numel() * ws.element_size()))
+    _launch(dev, stream, lib().tma_groupnorm_act_bwd, n, F, G, S, seg, R, X.data_ptr(), _rows_like(X, "X", (n, F), X.dtype),
+            dY.data_ptr(), _rows_like(dY, "dY", (n, F), X.dtype), _vector(gamma, "gamma", (F,), torch.float32),
+            _vector(beta, "beta", (F,), torch.float32), _vector(slope, "slope", (1,), torch.float32), eps, act,
+            _feat_dtype(X), _vector(stats, "stats", (S, G, 2), torch.float32) if not single else None, dX_out.data_ptr(),
+            _rows_like(dX_out, "dX_out", (n, F), X.dtype), _vector(dgamma, "dgamma", (F,), torch.float32),
+            _vector(dbeta, "dbeta", (F,), torch.float32), _vector(dslope, "dslope", (1,), torch.float32), *_room(ws))
     return dX_out, dgamma, dbeta, dslope
 
 
@@ -1108,11 +1118,9 @@ def _dropout(where, call, X, p, seed, step, first_row, out, stream):
     n, F, _ = _rows_ld(X, "X")
     if out is None:
         out = _record(_padded(n, F, X.dtype, dev), stream)
-    _launch(dev, stream, call, C.c_int64(n), C.c_int32(F), C.c_void_p(X.data_ptr()),
-            C.c_int64(_rows_like(X, "X", (n, F), X.dtype, dev)), C.c_double(p), C.c_uint64(int(seed) & ((1 << 64) - 1)),
-            _vector(step, "step", (1,), torch.int64, dev) if step is not None else C.c_void_p(0), C.c_int64(int(first_row)),
-            C.c_int32(_feat_dtype(X)), C.c_void_p(out.data_ptr()),
-            C.c_int64(_rows_like(out, "out", (n, F), X.dtype, dev)))
+    _launch(dev, stream, call, n, F, X.data_ptr(), _rows_like(X, "X", (n, F), X.dtype), p, int(seed) & ((1 << 64) - 1),
+            _vector(step, "step", (1,), torch.int64), int(first_row), _feat_dtype(X), out.data_ptr(),
+            _rows_like(out, "out", (n, F), X.dtype))
     return out
 
 
