@@ -175,6 +175,8 @@ __device__ __forceinline__ void write_fragments(const GroupList &gl, const float
 // ---- pieces of rows ----------------------------------------------------------------
 typedef uint32_t Words4 __attribute__((ext_vector_type(4), aligned(4)));
 
+__device__ __forceinline__ float widened(float x) { return x; }
+__device__ __forceinline__ float widened(uint16_t x) { return bf16_to_f32(x); }
 __device__ __forceinline__ uint32_t bits1(const float *p) { return __float_as_uint(*p); }
 __device__ __forceinline__ uint32_t bits1(const uint16_t *p) { return *p; }
 
@@ -861,8 +863,21 @@ struct SlabPieces {
     static constexpr int E = 16 / sizeof(T), PP = COLS / E, kAtOnce = THREADS / PP, kPieces = ROWS / kAtOnce;
     static_assert(kPieces >= 1 && kPieces * kAtOnce == ROWS, "pieces of a slab");
     typedef RowPiece<T, kWords> P;
-    // bf16: blocks of 32 columns exchanged by the row's number, for the transposing read takes 4 rows x 16 columns at once
-    static __device__ __forceinline__ int place(int row, int c) { return row * COLS + (sizeof(T) == 2 ? ((c >> 5) ^ (row & 3)) * 32 + (c & 31) : c); }
+    // in LDS, in bf16: blocks of 32 columns exchanged by the row's number, for the transposing read takes 4 rows x 16 columns at once
+    static __device__ __forceinline__ int place(int row, int c) { return row * COLS + ((c >> 5) ^ (row & 3)) * 32 + (c & 31); }
+    // fp32: three parts, a slab each
+    static __device__ __forceinline__ void put(uint16_t *slab, int row, int c, const uint4 &p)
+    {
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<uint4 *>(&slab[place(row, c)]) = p;
+        else {
+            const SplitPair split;
+            uint32_t part[3][2];
+            split(__uint_as_float(p.x), __uint_as_float(p.y), part[0][0], part[1][0], part[2][0]);
+            split(__uint_as_float(p.z), __uint_as_float(p.w), part[0][1], part[1][1], part[2][1]);
+#pragma unroll
+            for (int o = 0; o < 3; ++o) *reinterpret_cast<uint2 *>(&slab[o * ROWS * COLS + place(row, c)]) = make_uint2(part[o][0], part[o][1]);
+        }
+    }
     static __device__ __forceinline__ int row(int i) { return int(threadIdx.x) / PP + i * kAtOnce; }
     static __device__ __forceinline__ int column() { return int(threadIdx.x) % PP * E; }
 };
@@ -872,13 +887,14 @@ template <typename T, int WM, int WN, int TM, int TN, bool kMask, bool kWords>
 __global__ __launch_bounds__(WM *WN * 64, 2) void grouped_weight_kernel(WeightCall q)
 {
     constexpr int kThreads = WM * WN * 64, BM = WM * TM * 32, BN = WN * TN * 32, kDepth = 2;
-    constexpr int E = Step<T>::E, kSlab = sizeof(T) == 2 ? 32 : 16;
+    constexpr bool kSplit = sizeof(T) == 4;
+    constexpr int E = Step<T>::E, kParts = kSplit ? 3 : 1, kSlab = kSplit ? 16 : 32;
     constexpr int kListed = 64 * kSlab;                    // rows whose numbers lie in LDS, twice: these and the ones to come
     typedef SlabPieces<T, kSlab, BM, kThreads, kWords> XS;
     typedef SlabPieces<T, kSlab, BN, kThreads, kWords> ZS;
     typedef RowPiece<T, kWords> P;
-    __shared__ __attribute__((aligned(16))) T Xs[2][kSlab * BM];
-    __shared__ __attribute__((aligned(16))) T Zs[2][kSlab * BN];
+    __shared__ __attribute__((aligned(16))) uint16_t Xs[2][kParts * kSlab * BM];
+    __shared__ __attribute__((aligned(16))) uint16_t Zs[2][kParts * kSlab * BN];
     __shared__ int32_t listed[2][kListed];
     const T *X = static_cast<const T *>(q.X), *G = static_cast<const T *>(q.G), *H = static_cast<const T *>(q.H);
     const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, hi = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -940,7 +956,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void grouped_weight_kernel(WeightCa
             for (int d = 0; d < kDepth; ++d) {
                 const int s = s0 + d;
                 if (s >= slabs) break;
-                T *x = Xs[s & 1], *z = Zs[s & 1];
+                uint16_t *x = Xs[s & 1], *z = Zs[s & 1];
 #pragma unroll
                 for (int i = 0; i < XS::kPieces; ++i) {
                     const int v = row(s, XS::row(i));
@@ -950,7 +966,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void grouped_weight_kernel(WeightCa
                         if (over > 0) p = P::moved(p, int(over));
                     }
                     if (v < 0) p = make_uint4(0u, 0u, 0u, 0u);
-                    *reinterpret_cast<uint4 *>(&x[XS::place(XS::row(i), XS::column())]) = p;
+                    XS::put(x, XS::row(i), XS::column(), p);
                 }
 #pragma unroll
                 for (int i = 0; i < ZS::kPieces; ++i) {
@@ -962,7 +978,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void grouped_weight_kernel(WeightCa
                         if (over > 0) p = P::moved(p, int(over));
                     }
                     if (v < 0) p = make_uint4(0u, 0u, 0u, 0u);
-                    *reinterpret_cast<uint4 *>(&z[ZS::place(ZS::row(i), ZS::column())]) = p;
+                    ZS::put(z, ZS::row(i), ZS::column(), p);
                     if (sum) {
                         float w[E];
                         Chunk<T>::widen(p, w);
@@ -973,32 +989,31 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void grouped_weight_kernel(WeightCa
                 if (s % 64 == 0 && (s + 64) < slabs) list(s / 64 + 1);       // (in use from slab s + 64 - kDepth on, some barriers away)
                 __syncthreads();
                 if (s + kDepth < slabs) fetch(s + kDepth, d);
-                if constexpr (sizeof(T) == 2) {
 #pragma unroll
-                    for (int k = 0; k < kSlab; k += 16) {
-                        uint4 a[TM], b[TN];
+                for (int k = 0; k < kSlab; k += 16) {
+                    uint4 b[TN][kParts];
 #pragma unroll
-                        for (int i = 0; i < TM; ++i) a[i] = along_rows(&x[XS::place(k + tr_row, (wm * TM + i) * 32 + tr_col)], BM);
+                    for (int j = 0; j < TN; ++j)
 #pragma unroll
-                        for (int j = 0; j < TN; ++j) b[j] = along_rows(&z[ZS::place(k + tr_row, (wn * TN + j) * 32 + tr_col)], BN);
+                        for (int o = 0; o < kParts; ++o) b[j][o] = along_rows(&z[o * kSlab * BN + ZS::place(k + tr_row, (wn * TN + j) * 32 + tr_col)], BN);
 #pragma unroll
-                        for (int i = 0; i < TM; ++i)
+                    for (int i = 0; i < TM; ++i) {
+                        uint4 a[kParts];
+#pragma unroll
+                        for (int o = 0; o < kParts; ++o) a[o] = along_rows(&x[o * kSlab * BM + XS::place(k + tr_row, (wm * TM + i) * 32 + tr_col)], BM);
+                        auto times = [&](int pa, int pb) {
 #pragma unroll
                             for (int j = 0; j < TN; ++j)
-                                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a[i]), __builtin_bit_cast(bf16x8, b[j]), acc[i][j], 0, 0, 0);
-                    }
-                } else {
-#pragma unroll
-                    for (int k = 0; k < kSlab; k += 2) {
-                        float a[TM], b[TN];
-#pragma unroll
-                        for (int i = 0; i < TM; ++i) a[i] = x[(k + hi) * BM + (wm * TM + i) * 32 + l31];
-#pragma unroll
-                        for (int j = 0; j < TN; ++j) b[j] = z[(k + hi) * BN + (wn * TN + j) * 32 + l31];
-#pragma unroll
-                        for (int i = 0; i < TM; ++i)
-#pragma unroll
-                            for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[j], acc[i][j], 0, 0, 0);
+                                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a[pa]), __builtin_bit_cast(bf16x8, b[j][pb]), acc[i][j], 0, 0, 0);
+                        };
+                        if constexpr (kSplit) {
+                            times(2, 0);
+                            times(0, 2);
+                            times(1, 1);
+                            times(1, 0);
+                            times(0, 1);
+                        }
+                        times(0, 0);
                     }
                 }
             }
@@ -1006,6 +1021,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void grouped_weight_kernel(WeightCa
         const bool only = q.first[t.x + 1] - q.first[t.x] == 1;
         float *out = only ? q.dW + int64_t(t.x) * q.M * q.N : q.partial + run * int64_t(q.M) * q.N;
         // register r of a lane: row 8 (r / 4) + 4 (lane / 32) + r % 4, column lane % 32
+        bool odd = false;
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -1015,9 +1031,25 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void grouped_weight_kernel(WeightCa
 #pragma unroll
                     for (int j = 0; j < TN; ++j) {
                         const int n = n0 + (wn * TN + j) * 32 + l31;
-                        if (n < q.N) out[int64_t(m) * q.N + n] = acc[i][j][r];
+                        const float v = kSplit ? acc[i][j][r] * kSplitUnscale : acc[i][j][r];
+                        if (n < q.N) {
+                            out[int64_t(m) * q.N + n] = v;
+                            odd = odd || !(fabsf(v) <= FLT_MAX);
+                        }
                     }
                 }
+            }
+        if (kSplit && odd)          // in fp32, from what the operands are
+            for (int c = 0; c < TM * TN * 16; ++c) {
+                const int r = c % 16, m = m0 + (wm * TM + c / 16 / TN) * 32 + 8 * (r / 4) + 4 * hi + r % 4, n = n0 + (wn * TN + c / 16 % TN) * 32 + l31;
+                if (m >= q.M || n >= q.N || fabsf(out[int64_t(m) * q.N + n]) <= FLT_MAX) continue;
+                float total = 0.0f;
+                for (int at = 0; at < t.z; ++at) {
+                    const int64_t v = q.gl.row(t.y + at);
+                    if (v < 0 || (kMask && !(widened(H[v * q.ldg + n]) > 0.0f))) continue;
+                    total = fmaf(widened(X[v * q.ldx + m]), widened(G[v * q.ldg + n]), total);
+                }
+                out[int64_t(m) * q.N + n] = total;
             }
         if (sum) {      // (uniform over the block); the threads that share a column, in order
             __syncthreads();

@@ -278,3 +278,24 @@ def test_offsets_that_descend_touch_nothing_else(B, dtype):
     torch.cuda.synchronize()
     for F, t in whole.items():
         assert (t[:32] == 3).all() and (t[32 + n:] == 3).all() and (t[:, F:] == 3).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("F_in,F_out", [(40, 24), (260, 130)])
+def test_weight_gradients_of_infinities_and_of_values_near_the_range_end(B, dtype, F_in, F_out):
+    c = Case(B, [900, 0, 300], F_in, F_out, dtype, seed=9)
+    bad, large = int(c.rows[0][5]), int(c.rows[2][7])
+    c.dX[bad, 7], c.dX[large, 3] = float("inf"), 2.0 ** 120
+    c.X[large, 3] = 2.0 ** 120
+    c.X[bad, 7] = 0.0                            # (not looked at)
+    dW, db, _ = B.tma_grouped_dense_bwd(c.dX, None, c.dG, c.W.cuda(), c.offsets, B.TMA_ACT_NONE, order=c.order)
+    g = c.G[bad]
+    want = torch.where(g > 0, float("inf"), torch.where(g < 0, float("-inf"), float("nan")))
+    assert torch.equal(dW[0, 7].cpu().double().nan_to_num(nan=0.5, posinf=1.0, neginf=-1.0), want.nan_to_num(nan=0.5, posinf=1.0, neginf=-1.0))
+    for e, r in enumerate(c.rows):
+        keep = torch.ones(F_in, dtype=torch.bool)
+        if e == 0:
+            keep[7] = False
+        tol = (len(r) + 2) * u * (c.X[r].abs().T @ c.G[r].abs())
+        close(dW[e].cpu()[keep], (c.X[r].T @ c.G[r])[keep], tol[keep], f"dW of group {e}")
+        close(db[e].cpu(), c.G[r].sum(0), (len(r) + 2) * u * c.G[r].abs().sum(0), "db")
