@@ -269,14 +269,18 @@ static bool few_rows_a_group(int64_t n, int E, int32_t dtype) { return n <= (dty
 struct TileShape {
     bool resident;         // weights in LDS, tiles of 32 rows; else tiles of 64 rows that fetch them
     int TN, BN;            // column tiles of 32 whose columns are shuffled together, columns of a part of the result
-    int steps, n_tiles, height;
+    int steps, n_tiles, height;      // steps of 16 k-values, parts of the result, rows of a tile
     size_t fragment_bytes, bias_bytes;
 };
 
-// Product of rows of K with N columns.  Masked rows of several chunks go in tiles: beside all sums the registers do not hold the pieces of rows and
-// masks that the loads need to overlap (us at 300,000 rows of 384 -> 384 in bf16 with its weight gradient 684 resident, 597 in tiles; 125,000 of
-// 256 -> 256 in fp32 438 and 355; without masks 205 resident and 249 in tiles, 154 and 170).
-static TileShape tile_shape(int E, int K, int N, size_t elem, bool masked)
+// Product of rows of K with N columns.  Weights stay in LDS where every compute unit has some rounds of eight wavefronts' rows to take them through (its
+// load and the last round's empty places are shared by those); fewer go in tiles, us resident and in tiles: fp32 128 -> 128 125,000 rows 56 and
+// 49, 400,000 rows 130 and 152; 64 -> 64 250,000 rows 40 and 45; bf16 256 -> 256 60,000 rows 32 and 25, 250,000 rows 71 and 70, 500,000 rows 136 and 163.
+// In tiles at any size: masked rows of several chunks, for beside all sums the registers do not hold the pieces of rows and masks that the loads need
+// to overlap (300,000 rows of 384 -> 384 in bf16 with its weight gradient 684 resident, 597 in tiles), and fp32 rows of several chunks, whose
+// parts fit LDS for 64 columns only (125,000 rows of 256 -> 128 89 resident, 69 in tiles; bf16, 300,000 rows of 384 -> 384 without a mask, 174 and 215).
+constexpr int64_t kResRounds = 3;
+static TileShape tile_shape(int64_t n, int E, int K, int N, size_t elem, bool masked)
 {
     TileShape t;
     // steps of 16 k-values, filled up to a quarter of a chunk; column tiles that fit LDS beside each other, pairs of them
@@ -284,24 +288,24 @@ static TileShape tile_shape(int E, int K, int N, size_t elem, bool masked)
     t.steps = int(round_up(size_t(ceil_div(K, 16)), chunk / 4));
     int cols = kResPieces / (t.steps * parts * kWave) / 2 * 2;
     const bool multi = t.steps > chunk;
-    const int most = !multi ? 8 : elem == 4 ? 2 : kResChunkCols;
+    const int most = multi ? kResChunkCols : 8;
     if (cols > most) cols = most;
-    t.resident = cols >= 2 && !(multi && masked);
+    const int want = int(ceil_div(N, 64)) * 2, parts_of_N = cols >= 2 ? int(ceil_div(want, cols)) : 0;
+    t.resident = cols >= 2 && !(multi && (masked || elem == 4)) && n * parts_of_N >= kResRounds * 256 * kResWaves * kResRows;
     if (t.resident) {
-        const int want = int(ceil_div(N, 64)) * 2;
-        t.n_tiles = int(ceil_div(want, cols));
+        t.n_tiles = parts_of_N;
         const int each = int(ceil_div(want, 2 * t.n_tiles)) * 2;       // parts alike
         t.BN = each * 32;
         t.TN = elem == 2 ? 2 : 1;
         t.height = kResRows;
         t.fragment_bytes = round_up(size_t(E) * size_t(t.n_tiles) * size_t(t.BN / 32) * size_t(t.steps) * size_t(parts) * 1024, 256);
     } else {
-        t.steps = int(round_up(size_t(ceil_div(K, int(32 / elem))), kAhead));
+        t.steps = int(round_up(size_t(ceil_div(K, 16)), kStepsUp));
         t.TN = N > 128 ? 2 : 1;
         t.BN = N > 128 ? 256 : N > 64 ? 128 : 64;
         t.n_tiles = int(ceil_div(N, t.BN));
         t.height = kTileM;
-        t.fragment_bytes = round_up(size_t(E) * size_t(t.n_tiles) * size_t(t.BN / 32) * size_t(t.steps) * 1024, 256);
+        t.fragment_bytes = round_up(size_t(E) * size_t(t.n_tiles) * size_t(t.BN / 32) * size_t(t.steps) * size_t(parts) * 1024, 256);
     }
     t.bias_bytes = round_up(size_t(E) * size_t(t.n_tiles) * size_t(t.BN) * 4, 256);
     return t;
@@ -343,7 +347,7 @@ static WeightShape weight_shape(int64_t n, int E, int M, int N)
 }
 
 template <typename T>
-static void launch_prepare(const PrepareCall &q, bool forward, bool resident, hipStream_t s)
+static void launch_prepare(const PrepareCall &q, bool forward, hipStream_t s)
 {
     const int64_t pieces = q.B ? int64_t(q.gl.E) * q.col_tiles * q.steps * kWave : 0;
     int64_t blocks = ceil_div(pieces, kGgThreads);
@@ -352,23 +356,19 @@ static void launch_prepare(const PrepareCall &q, bool forward, bool resident, hi
     if (q.bias && all < q.gl.E) all = q.gl.E;
     const dim3 grid{unsigned(all)};
     TMA_TIMED(sizeof(T) == 2 ? "grouped_prepare_bf16" : "grouped_prepare", s);
-    constexpr bool kParts = sizeof(T) == 4;        // the resident kernel takes fp32 weights in parts
-    if (kParts && resident) {
-        if (forward) hipLaunchKernelGGL((grouped_prepare_kernel<T, true, kParts>), grid, dim3(kGgThreads), 0, s, q);
-        else hipLaunchKernelGGL((grouped_prepare_kernel<T, false, kParts>), grid, dim3(kGgThreads), 0, s, q);
-    } else if (forward) hipLaunchKernelGGL((grouped_prepare_kernel<T, true, false>), grid, dim3(kGgThreads), 0, s, q);
-    else hipLaunchKernelGGL((grouped_prepare_kernel<T, false, false>), grid, dim3(kGgThreads), 0, s, q);
+    if (forward) hipLaunchKernelGGL((grouped_prepare_kernel<T, true>), grid, dim3(kGgThreads), 0, s, q);
+    else hipLaunchKernelGGL((grouped_prepare_kernel<T, false>), grid, dim3(kGgThreads), 0, s, q);
 }
 
-template <typename T, int WN, int TN, int PP, bool kMask>
+template <typename T, int WN, int TN, bool kMask>
 static void launch_rows_as(const RowsCall &q, bool words, bool store16, int64_t most_items, hipStream_t s)
 {
-    constexpr int kPerCu = kRowBlocksPerCu<TN, PP, kMask>;
+    constexpr int kPerCu = kRowBlocksPerCu<TN>;
     int64_t per_die = ceil_div(most_items, kDies);
     if (per_die > 32 * kPerCu) per_die = 32 * kPerCu;
     const dim3 grid(unsigned(per_die * kDies));
-    if (words && store16) hipLaunchKernelGGL((grouped_rows_kernel<T, WN, TN, PP, kMask, true, true>), grid, dim3(kGgThreads), 0, s, q);
-    else hipLaunchKernelGGL((grouped_rows_kernel<T, WN, TN, PP, kMask, false, false>), grid, dim3(kGgThreads), 0, s, q);
+    if (words && store16) hipLaunchKernelGGL((grouped_rows_kernel<T, WN, TN, kMask, true, true>), grid, dim3(kGgThreads), 0, s, q);
+    else hipLaunchKernelGGL((grouped_rows_kernel<T, WN, TN, kMask, false, false>), grid, dim3(kGgThreads), 0, s, q);
 }
 
 // rows whose pieces of 16 bytes one load fetches: words throughout, and such a piece in the array
@@ -379,15 +379,15 @@ static bool rows_in_words(const void *p, int64_t ld, int64_t n, int F)
 }
 
 template <typename T, bool kMask>
-static int launch_rows(const char *fn, const char *name, const RowsCall &q, const TileShape &t, const float *W, bool forward, hipStream_t s)
+static int launch_rows(const char *fn, const char *name, const RowsCall &q, const TileShape &t, hipStream_t s)
 {
     const T *A = static_cast<const T *>(q.A), *H = static_cast<const T *>(q.H);
     const bool words = rows_in_words<T>(A, q.lda, q.gl.n, q.K) && (!kMask || aligned(H, 4));
     const bool store16 = sizeof(T) == 4 || (aligned(q.C, 4) && q.ldc % 2 == 0);      // (the store needs words, no more)
     TMA_TIMED(name, s);
     if (t.resident) {
-        const ResidentCall r{q.gl, q.tiles, q.tile_count - q.gl.E, q.B, q.bias, q.A, q.H, q.C, W, q.lda, q.ldc, forward ? q.N : 1, forward ? 1 : q.K, q.K, q.N,
-                             q.steps, q.n_tiles, t.BN / 32, q.relu};
+        const ResidentCall r{q.gl, q.tiles, q.tile_count - q.gl.E, q.B, q.bias, q.A, q.H, q.C, q.W, q.lda, q.ldc, q.w_k, q.w_col, q.K, q.N, q.steps,
+                             q.n_tiles, t.BN / 32, q.relu};
         const dim3 grid(256), block(kResWaves * 64);      // one block a compute unit: its weights take the LDS
         auto go = [&](auto nt, auto multi) {
             constexpr int NT = decltype(nt)::value;
@@ -398,17 +398,16 @@ static int launch_rows(const char *fn, const char *name, const RowsCall &q, cons
         const std::integral_constant<int, 2> two;
         const std::integral_constant<int, 4> four;
         if (t.steps <= ResStep<T>::kChunk) go(two, std::false_type{});
-        else if constexpr (!kMask) {
-            if constexpr (sizeof(T) == 4) go(two, std::true_type{});
-            else if (t.BN == 128) go(four, std::true_type{});
+        else if constexpr (!kMask && sizeof(T) == 2) {
+            if (t.BN == 128) go(four, std::true_type{});
             else go(two, std::true_type{});
         }
         return check_launch(fn);
     }
     const int64_t items = tile_room(q.gl.n, q.gl.E, kTileM) * q.n_tiles;
-    if (t.BN == 256) launch_rows_as<T, 4, 2, 32, kMask>(q, words, store16, items, s);
-    else if (t.BN == 128) launch_rows_as<T, 4, 1, 32, kMask>(q, words, store16, items, s);
-    else launch_rows_as<T, 2, 1, 32, kMask>(q, words, store16, items, s);
+    if (t.BN == 256) launch_rows_as<T, 4, 2, kMask>(q, words, store16, items, s);
+    else if (t.BN == 128) launch_rows_as<T, 4, 1, kMask>(q, words, store16, items, s);
+    else launch_rows_as<T, 2, 1, kMask>(q, words, store16, items, s);
     return check_launch(fn);
 }
 
@@ -438,7 +437,7 @@ template <typename T>
 static int tiles_fwd(const char *fn, const GroupList &gl, const void *X, int64_t ldx, int K, const float *W, const float *bias, int N, bool relu, void *Y,
                      int64_t ldy, void *ws, hipStream_t s)
 {
-    const TileShape t = tile_shape(gl.E, K, N, sizeof(T), false);
+    const TileShape t = tile_shape(gl.n, gl.E, K, N, sizeof(T), false);
     char *at = static_cast<char *>(ws);
     PrepareCall p{};
     p.gl = gl;
@@ -454,17 +453,18 @@ static int tiles_fwd(const char *fn, const GroupList &gl, const void *X, int64_t
     p.col_tiles = t.n_tiles * t.BN / 32;
     p.steps = t.steps;
     p.TN = t.TN;
-    launch_prepare<T>(p, true, t.resident, s);
+    launch_prepare<T>(p, true, s);
     if (int rc = check_launch(fn)) return rc;
-    const RowsCall q{gl, p.rows.tiles, p.rows.first + gl.E, p.B, bias ? p.bias_out : nullptr, X, nullptr, Y, ldx, ldy, K, N, t.steps, t.n_tiles, relu};
-    return launch_rows<T, false>(fn, sizeof(T) == 2 ? "grouped_fwd_bf16" : "grouped_fwd", q, t, W, true, s);
+    const RowsCall q{gl, p.rows.tiles, p.rows.first + gl.E, p.B, bias ? p.bias_out : nullptr, X, nullptr, Y, W, ldx, ldy, N, 1, K, N,
+                     t.steps, t.n_tiles, relu};
+    return launch_rows<T, false>(fn, sizeof(T) == 2 ? "grouped_fwd_bf16" : "grouped_fwd", q, t, s);
 }
 
 template <typename T>
 static int tiles_bwd(const char *fn, const GroupList &gl, const void *X, int64_t ldx, const void *Y, const void *dY, int64_t ldy, const float *W, int F_in,
                      int F_out, bool relu, float *dW, float *db, void *dX, int64_t ld_dx, void *ws, hipStream_t s)
 {
-    const TileShape t = tile_shape(gl.E, F_out, F_in, sizeof(T), relu);
+    const TileShape t = tile_shape(gl.n, gl.E, F_out, F_in, sizeof(T), relu);
     const int height = weight_shape(gl.n, gl.E, F_in, F_out).height;
     char *at = static_cast<char *>(ws);
     PrepareCall p{};
@@ -486,12 +486,13 @@ static int tiles_bwd(const char *fn, const GroupList &gl, const void *X, int64_t
         p.steps = t.steps;
         p.TN = t.TN;
     }
-    launch_prepare<T>(p, false, t.resident, s);
+    launch_prepare<T>(p, false, s);
     if (int rc = check_launch(fn)) return rc;
     if (dX) {
-        const RowsCall q{gl, p.rows.tiles, p.rows.first + gl.E, p.B, nullptr, dY, relu ? Y : nullptr, dX, ldy, ld_dx, F_out, F_in, t.steps, t.n_tiles, false};
+        const RowsCall q{gl, p.rows.tiles, p.rows.first + gl.E, p.B, nullptr, dY, relu ? Y : nullptr, dX, W, ldy, ld_dx, 1, F_out, F_out, F_in,
+                         t.steps, t.n_tiles, false};
         const char *name = sizeof(T) == 2 ? "grouped_bwd_data_bf16" : "grouped_bwd_data";
-        if (int rc = relu ? launch_rows<T, true>(fn, name, q, t, W, false, s) : launch_rows<T, false>(fn, name, q, t, W, false, s)) return rc;
+        if (int rc = relu ? launch_rows<T, true>(fn, name, q, t, s) : launch_rows<T, false>(fn, name, q, t, s)) return rc;
     }
     {
         const WeightShape w = weight_shape(gl.n, gl.E, F_in, F_out);
@@ -530,7 +531,7 @@ extern "C" size_t tma_grouped_dense_fwd_workspace_bytes(int64_t n, int32_t E, in
     using namespace tma;
     if (n < 0 || E < 1 || F_in < 1 || F_out < 1) return 0;
     if (few_rows_a_group(n, E, dtype)) return 256;
-    const TileShape t = tile_shape(E, F_in, F_out, dtype == TMA_BF16 ? 2 : 4, false);
+    const TileShape t = tile_shape(n, E, F_in, F_out, dtype == TMA_BF16 ? 2 : 4, false);
     return plan_bytes(n, E, t.height) + t.bias_bytes + t.fragment_bytes;
 }
 
@@ -566,7 +567,7 @@ extern "C" size_t tma_grouped_dense_bwd_workspace_bytes(int64_t n, int32_t E, in
     if (need_dX) {
         size_t most = 0;           // with a mask or without
         for (bool masked : {false, true}) {
-            const TileShape t = tile_shape(E, F_out, F_in, dtype == TMA_BF16 ? 2 : 4, masked);
+            const TileShape t = tile_shape(n, E, F_out, F_in, dtype == TMA_BF16 ? 2 : 4, masked);
             const size_t need = plan_bytes(n, E, t.height) + t.fragment_bytes;
             if (need > most) most = need;
         }

@@ -4,20 +4,26 @@
 // follow each other, group after group, and a block takes its tiles from one die's run of them (neighbours share weights and,
 // where a row's results are several tiles wide, rows in that die's L2).
 //
-// grouped_rows_kernel (forward and input gradient): C[v] = A[v] B[g] for 64 listed rows v.  Bound by streaming the rows in and the
-// results out (bf16 256 -> 256: 1 KB and 131 kFLOP a row), so: a row's k-values are read once, wherever the row lies, in
+// grouped_rows_kernel (forward and input gradient): C[v] = A[v] B[g] for 64 listed rows v.  A row's k-values are read once, wherever the row lies, in
 // pieces of 16 bytes, all of the next tile's on their way in registers while this one is multiplied; through LDS (512 bytes of a row at a
 // time) because the matrix instruction wants a row per lane.  The weights go past LDS: laid out as fragments, 1 KB that a
 // wavefront loads at once, and the same for all tiles of a group, they come out of L2.  The instruction multiplies weights by
 // rows, so that a lane ends with neighbouring results of one row: which column of W is which row of a fragment is the layout's
-// choice, and is made so that a lane stores 16 or 32 neighbours in pieces of 16 bytes.
+// choice, and is made so that a lane has 16 or 32 neighbours.  Bound by what a compute unit has on its way: 125,000 rows of 256 -> 128 in fp32
+// 64 us (193 MB, 3.0 TB/s), their input gradient behind a mask 86 us (321 MB, 3.7 TB/s; on the fp32 instruction 111).
 //
-// grouped_weight_kernel (weight gradients): dW[g] += X[v]^T dZ[v] over a run of a group's rows, 128 x 128 results a block; both
-// operands come as they lie, rows of LDS, and are read along columns (bf16: the transposing LDS read).  Runs of one group are
-// added up in order by a second kernel; a group of one run is stored at once.
+// grouped_resident_kernel: the same product with the weights in LDS, for lists that are long enough (see below).  1,000,003 rows of 256 -> 256 in bf16
+// 218 us (1.03 GB, 4.7 TB/s, what a copy reaches), 131 GFLOP at half of a large product's rate.
 //
-// fp32: v_mfma_f32_32x32x2_f32, fp32 throughout.  bf16: v_mfma_f32_32x32x16_bf16, weights rounded once to bf16 (as in all products of
-// bf16 storage here), fp32 accumulation, results rounded once.
+// grouped_weight_kernel (weight gradients): dW[g] += X[v]^T dZ[v] over a run of a group's rows, up to 256 x 256 results a block (all
+// of a run's rows are then read once); both operands come as they lie, rows of LDS, and are read along columns by the transposing LDS
+// read.  Runs of one group are added up in order by a second kernel; a group of one run is stored at once.  1,000,003 rows of 256 x 256
+// in bf16 196 us (X and dZ 1.02 GB, 5.2 TB/s); 125,000 of 256 x 128 in fp32 76 us (257 MB with the mask, 3.4 TB/s; on the fp32 instruction 102).
+//
+// bf16: v_mfma_f32_32x32x16_bf16, weights rounded once to bf16 (as in all products of bf16 storage here), fp32 accumulation, results rounded once.
+// fp32: the same instruction, three bf16 parts of each operand and six products of them (gemm_split.hpp says why those suffice): 192 cycles for 16
+// k-values where the fp32 instruction takes 512.  A result that is not finite (an operand that is not, or is too large to be taken
+// apart) is computed again in fp32, value by value.
 #pragma once
 #include "kernels.hpp"
 #include "split_pair.hpp"
@@ -33,7 +39,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 constexpr int kDies = 8;             // workgroups are dealt round-robin to them
 constexpr int kTileM = 64;           // rows of a tile
 constexpr int kGgThreads = 256;
-constexpr int kAhead = 4;            // steps that weights are fetched ahead; a product's steps are filled up with zeros to a multiple of it
+constexpr int kStepsUp = 4;          // steps of tile products are filled up with zeros to a multiple of this
 constexpr int kMaxGroups = 1024;
 
 struct GroupList {
@@ -121,11 +127,12 @@ __device__ __forceinline__ void write_plan(const GroupList &gl, const TilePlan &
 }
 
 // ---- weights as fragments --------------------------------------------------------
-// A step is 16 bytes of k-values a lane: 16 of bf16, 8 of fp32.  Piece (g, tile of 32 columns, step, lane) holds of column
-// col(lane % 32) the k-values step * 2 E + (lane / 32) * E + [0, E).
+// A step is 16 k-values, eight a lane.  bf16: piece (g, tile of 32 columns, step, lane) holds of column col(lane % 32) the k-values
+// step * 16 + (lane / 32) * 8 + [0, 8).  fp32: three bf16 parts of every value, pieces (g, tile, step, part, lane); a lane's eight are
+// those of two pieces of four, step * 16 + (lane / 32) * 4 + [0, 4) and the same + 8.
 template <typename T>
 struct Step {
-    static constexpr int E = 16 / sizeof(T), K = 2 * E;
+    static constexpr int E = 16 / sizeof(T);       // of a row's piece of 16 bytes
 };
 
 // result row m of a fragment is column ... of the wavefront's TN * 32 (see above)
@@ -135,13 +142,13 @@ __host__ __device__ __forceinline__ int fragment_column(int tile, int m, int TN)
     return tile / TN * TN * 32 + hi * TN * 16 + tile % TN * 16 + r;
 }
 
-// kForward: B = W[g] (k along its rows); else B = W[g]^T.  kSplit (fp32): three bf16 parts of every value instead, a step 16 k-values of which a
-// lane's eight are those of two neighbouring pieces of a row: pieces (g, tile, step, part, lane).
-template <typename T, bool kForward, bool kSplit>
+// kForward: B = W[g] (k along its rows); else B = W[g]^T
+template <typename T, bool kForward>
 __device__ __forceinline__ void write_fragments(const GroupList &gl, const float *__restrict__ W, int K, int N, int tiles, int steps, int TN,
                                                 uint4 *__restrict__ out, int64_t block, int64_t blocks)
 {
-    constexpr int E = kSplit ? 8 : Step<T>::E;
+    constexpr bool kSplit = sizeof(T) == 4;
+    constexpr int E = 8;
     const int64_t per_group = int64_t(tiles) * steps * kWave, total = per_group * gl.E;
     for (int64_t i = block * kGgThreads + threadIdx.x; i < total; i += blocks * kGgThreads) {
         const int g = int(i / per_group);
@@ -164,8 +171,6 @@ __device__ __forceinline__ void write_fragments(const GroupList &gl, const float
             for (int j = 0; j < 4; ++j) split(v[2 * j], v[2 * j + 1], part[0][j], part[1][j], part[2][j]);
 #pragma unroll
             for (int p = 0; p < 3; ++p) out[(i / kWave * 3 + p) * kWave + lane] = make_uint4(part[p][0], part[p][1], part[p][2], part[p][3]);
-        } else if constexpr (sizeof(T) == 4) {
-            out[i] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
         } else {
             out[i] = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
         }
@@ -250,25 +255,23 @@ __device__ __forceinline__ uint4 open_piece(const uint4 &g, const uint4 &h)
     return make_uint4(open_word<T>(g.x, h.x), open_word<T>(g.y, h.y), open_word<T>(g.z, h.z), open_word<T>(g.w, h.w));
 }
 
-// acc[i][j] += a step's products; the fp32 instruction's four in a row go to different accumulators
-template <typename T, int TM, int TN>
-__device__ __forceinline__ void multiply(const uint4 (&w)[TN], const uint4 (&x)[TM], floatx16 (&acc)[TM][TN])
+__device__ __forceinline__ floatx16 times(const uint4 &a, const uint4 &b, const floatx16 &sum)
 {
-    if constexpr (sizeof(T) == 2) {
-#pragma unroll
-        for (int j = 0; j < TN; ++j)
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w[j]), __builtin_bit_cast(bf16x8, x[i]), acc[i][j], 0, 0, 0);
-    } else {
-        auto word = [](const uint4 &v, int k) { return __uint_as_float(k == 0 ? v.x : k == 1 ? v.y : k == 2 ? v.z : v.w); };
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-#pragma unroll
-            for (int j = 0; j < TN; ++j)
-#pragma unroll
-                for (int i = 0; i < TM; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(word(w[j], k), word(x[i], k), acc[i][j], 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), sum, 0, 0, 0);
+}
+
+// sum += a b of operands in one part or in three
+template <int kParts>
+__device__ __forceinline__ void add_product(const uint4 (&a)[kParts], const uint4 (&b)[kParts], floatx16 &sum)
+{
+    if constexpr (kParts == 3) {
+        sum = times(a[2], b[0], sum);
+        sum = times(a[0], b[2], sum);
+        sum = times(a[1], b[1], sum);
+        sum = times(a[1], b[0], sum);
+        sum = times(a[0], b[1], sum);
     }
+    sum = times(a[0], b[0], sum);
 }
 
 // The run of work items that this block's die takes, and this block's first of them; they are a stride apart.
@@ -292,10 +295,20 @@ struct RowsCall {
     const float *bias;         // [E][n_tiles BN], zeros past N, or NULL
     const void *A, *H;         // rows; H: their mask (kMask)
     void *C;
-    int64_t lda, ldc;
+    const float *W;            // as they are, [E][K N], value (k, column) at k w_k + column w_col
+    int64_t lda, ldc, w_k, w_col;
     int K, N, steps, n_tiles;  // n_tiles: of BN columns
     bool relu;
 };
+
+// column col of row v from what the operands are, in fp32 (for results that parts of them cannot give)
+template <bool kMask>
+__device__ __forceinline__ float in_fp32(const float *a, const float *h, const float *w, int64_t w_k, int K)
+{
+    float sum = 0.0f;
+    for (int k = 0; k < K; ++k) sum = fmaf(kMask && !(h[k] > 0.0f) ? 0.0f : a[k], w[k * w_k], sum);
+    return sum;
+}
 
 // Place of a row's piece in LDS, rows of PP pieces: exchanged by the row's number, so that what 16 lanes take at once, a piece each of 16
 // neighbouring rows, lies in all banks.
@@ -306,22 +319,25 @@ __device__ __forceinline__ int spread(int row, int piece)
     return row * PP + (piece ^ ((row / (16 / kSpan)) & (kSpan - 1)));
 }
 
+constexpr int kRowPP = 32;                 // 16-byte pieces of a row in LDS at a time
 // blocks of a compute unit that the registers leave room for (four wavefronts each)
-template <int TN, int PP, bool kMask>
-constexpr int kRowBlocksPerCu = TN * PP > 32 ? 2 : 3;
+template <int TN>
+constexpr int kRowBlocksPerCu = TN > 1 ? 2 : 3;
 
-// PP: 16-byte pieces of a row in LDS at a time.  The numbers of a tile's rows are fetched two tiles ahead, its rows one.
-template <typename T, int WN, int TN, int PP, bool kMask, bool kWords, bool kStore16>
-__global__ __launch_bounds__(kGgThreads, (kRowBlocksPerCu<TN, PP, kMask>)) void grouped_rows_kernel(RowsCall q)
+// The numbers of a tile's rows are fetched two tiles ahead, its rows one.  fp32: in LDS three bf16 parts, [part][row][16 bytes: eight k-values].
+template <typename T, int WN, int TN, bool kMask, bool kWords, bool kStore16>
+__global__ __launch_bounds__(kGgThreads, kRowBlocksPerCu<TN>) void grouped_rows_kernel(RowsCall q)
 {
-    constexpr int WM = 4 / WN, TM = kTileM / WM / 32, E = Step<T>::E;
+    constexpr bool kSplit = sizeof(T) == 4;
+    constexpr int WM = 4 / WN, TM = kTileM / WM / 32, E = Step<T>::E, PP = kRowPP, kParts = kSplit ? 3 : 1, kUnits = kSplit ? PP / 2 : PP;
     constexpr int kRowsAtOnce = kGgThreads / PP, kPieces = kTileM / kRowsAtOnce;    // of a thread
-    constexpr int kSteps = PP / 2;
+    constexpr int kSteps = kUnits / 2, kAhead = kSplit ? 2 : 4;                     // of 16 k-values; steps that weights are fetched ahead
     typedef RowPiece<T, kWords> P;
     constexpr int kRowPieces = TN * 32 / E;    // of a wavefront's columns of a row
-    constexpr int kOut = 4 * 32 * kRowPieces;
-    __shared__ uint4 As[kTileM * PP > kOut ? kTileM * PP : kOut];
+    constexpr int kOut = 4 * 32 * kRowPieces, kIn = kParts * kTileM * kUnits;
+    __shared__ uint4 As[kIn > kOut ? kIn : kOut];
     __shared__ int32_t rows[2][kTileM];        // of this tile and the next, -1: none
+    const SplitPair split;
     const T *A = static_cast<const T *>(q.A), *H = static_cast<const T *>(q.H);
     const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, hi = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave % WN;
@@ -364,11 +380,15 @@ __global__ __launch_bounds__(kGgThreads, (kRowBlocksPerCu<TN, PP, kMask>)) void 
         const int group = __builtin_amdgcn_readfirstlane(q.tiles[tile].x);
         const int nt = int(item - tile * q.n_tiles) * WN * TN + wn * TN;      // first of the wavefront's column tiles
         const int n0 = nt * 32 + hi * TN * 16;                         // first of the lane's columns
-        const uint4 *B = q.B + (int64_t(group) * q.n_tiles * WN * TN + nt) * q.steps * kWave;
-        auto weights = [&](int j, int step) { return (B + (j * q.steps + step) * kWave)[lane]; };
+        const uint4 *B = q.B + (int64_t(group) * q.n_tiles * WN * TN + nt) * q.steps * (kParts * kWave);
+        auto weights = [&](int j, int step, uint4 (&w)[kParts]) {
+#pragma unroll
+            for (int o = 0; o < kParts; ++o) w[o] = (B + ((j * q.steps + step) * kParts + o) * kWave)[lane];
+        };
+        const float *bias = q.bias ? q.bias + int64_t(group) * q.n_tiles * (WN * TN * 32) + n0 : nullptr;      // of the lane's columns
         floatx16 acc[TM][TN];
-        if (q.bias) {
-            const float4 *b4 = reinterpret_cast<const float4 *>(q.bias + int64_t(group) * q.n_tiles * (WN * TN * 32) + n0);
+        if (!kSplit && bias) {
+            const float4 *b4 = reinterpret_cast<const float4 *>(bias);
 #pragma unroll
             for (int j = 0; j < TN; ++j)
 #pragma unroll
@@ -391,12 +411,12 @@ __global__ __launch_bounds__(kGgThreads, (kRowBlocksPerCu<TN, PP, kMask>)) void 
                     for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
         }
         for (int c = 0; c < chunks; ++c) {
-            const int s0 = c * kSteps, s1 = q.steps - s0 < kSteps ? q.steps - s0 : kSteps;      // a multiple of kAhead
-            uint4 b[kSteps][TN];
+            const int s0 = c * kSteps, s1 = q.steps - s0 < kSteps ? q.steps - s0 : kSteps;      // multiples of kStepsUp
+            uint4 b[kSteps][TN][kParts];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u)
 #pragma unroll
-                for (int j = 0; j < TN; ++j) b[u][j] = weights(j, s0 + u);
+                for (int j = 0; j < TN; ++j) weights(j, s0 + u, b[u][j]);
             __syncthreads();           // everyone has read what was there
             const int valid = q.K - (c * PP + piece) * E;
             if constexpr (kMask) {
@@ -412,8 +432,20 @@ __global__ __launch_bounds__(kGgThreads, (kRowBlocksPerCu<TN, PP, kMask>)) void 
                 }
             }
 #pragma unroll
-            for (int i = 0; i < kPieces; ++i)
-                As[spread<PP>(row0 + i * kRowsAtOnce, piece)] = valid > 0 ? held[i] : make_uint4(0u, 0u, 0u, 0u);
+            for (int i = 0; i < kPieces; ++i) {
+                const uint4 p = valid > 0 ? held[i] : make_uint4(0u, 0u, 0u, 0u);
+                if constexpr (kSplit) {        // pieces 4 s + hi and 4 s + 2 + hi of a row are the eight values of a lane at step s
+                    uint32_t part[3][2];
+                    split(__uint_as_float(p.x), __uint_as_float(p.y), part[0][0], part[1][0], part[2][0]);
+                    split(__uint_as_float(p.z), __uint_as_float(p.w), part[0][1], part[1][1], part[2][1]);
+                    const int at16 = spread<kUnits>(row0 + i * kRowsAtOnce, piece / 4 * 2 + piece % 2);
+#pragma unroll
+                    for (int o = 0; o < 3; ++o)
+                        reinterpret_cast<uint2 *>(&As[o * kTileM * kUnits + at16])[piece / 2 % 2] = make_uint2(part[o][0], part[o][1]);
+                } else {
+                    As[spread<kUnits>(row0 + i * kRowsAtOnce, piece)] = p;
+                }
+            }
             if (c == 0 && tid < kTileM) rows[at ^ 1][tid] = pending;
             __syncthreads();
             if (c + 1 < chunks) fetch(at, c + 1);
@@ -426,36 +458,56 @@ __global__ __launch_bounds__(kGgThreads, (kRowBlocksPerCu<TN, PP, kMask>)) void 
 #pragma unroll
             for (int s = 0; s < kSteps; ++s) {
                 if (s % kAhead == 0 && s >= s1) break;
-                uint4 a[TM];
 #pragma unroll
-                for (int i = 0; i < TM; ++i) a[i] = As[spread<PP>((wm * TM + i) * 32 + l31, 2 * s + hi)];
-                multiply<T, TM, TN>(b[s], a, acc);
+                for (int i = 0; i < TM; ++i) {
+                    uint4 a[kParts];
+#pragma unroll
+                    for (int o = 0; o < kParts; ++o) a[o] = As[o * kTileM * kUnits + spread<kUnits>((wm * TM + i) * 32 + l31, 2 * s + hi)];
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) add_product<kParts>(b[s][j], a, acc[i][j]);
+                }
                 if (s + kAhead < kSteps) {
                     const int ahead = s0 + s + kAhead < q.steps ? s0 + s + kAhead : q.steps - 1;     // (past the last one: again)
 #pragma unroll
-                    for (int j = 0; j < TN; ++j) b[s + kAhead < kSteps ? s + kAhead : 0][j] = weights(j, ahead);
+                    for (int j = 0; j < TN; ++j) weights(j, ahead, b[s + kAhead < kSteps ? s + kAhead : 0][j]);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
         // A lane has, of row l31 of the tile's 32, the columns [0, 16 TN) or the next as many of its wavefront's.  Through LDS, 32 rows at a
-        // time: a store then goes to whole rows of the wavefront's columns, 64 to 256 bytes each.  (From registers it went to a piece of 64 rows,
-        // and the L2's requests bounded the kernel: see below.)
+        // time: a store then goes to whole rows of the wavefront's columns, 64 to 256 bytes each.
         T *C = static_cast<T *>(q.C);
         __syncthreads();               // everyone has read the last steps
         uint4 *mine = As + wave * (32 * kRowPieces);
         const int col0 = nt * 32;      // the wavefront's first column
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
+            uint32_t odd = 0;              // the lane's columns whose sum is not finite
 #pragma unroll
             for (int x = 0; x < TN * 16 / E; ++x) {
                 float z[E];
 #pragma unroll
                 for (int y = 0; y < E; ++y) {
                     z[y] = acc[i][x * E / 16][x * E % 16 + y];
+                    if constexpr (kSplit) {
+                        z[y] *= kSplitUnscale;
+                        if (!(fabsf(z[y]) <= FLT_MAX)) odd |= 1u << (x * E + y);
+                        if (bias) z[y] += bias[x * E + y];
+                    }
                     if (q.relu) z[y] = z[y] > 0.0f ? z[y] : 0.0f;
                 }
                 Chunk<T>::store(reinterpret_cast<T *>(&mine[spread<kRowPieces>(l31, hi * (kRowPieces / 2) + x)]), z);
+            }
+            if constexpr (kSplit) {
+                const int64_t v = rows[at][(wm * TM + i) * 32 + l31];
+                if (__any(odd && v >= 0))
+                    for (int y = 0; y < TN * 16; ++y)
+                        if (v >= 0 && (odd >> y & 1) && n0 + y < q.N) {
+                            float z = in_fp32<kMask>(A + v * q.lda, H + v * q.lda, q.W + int64_t(group) * q.K * q.N + (n0 + y) * q.w_col, q.w_k, q.K);
+                            if (bias) z += bias[y];
+                            if (q.relu) z = z > 0.0f ? z : 0.0f;
+                            reinterpret_cast<float *>(&mine[spread<kRowPieces>(l31, hi * (kRowPieces / 2) + y / E)])[y % E] = z;
+                        }
             }
             __builtin_amdgcn_wave_barrier();
             constexpr int kStores = kRowPieces / 2;
@@ -501,7 +553,7 @@ __global__ __launch_bounds__(kGgThreads, (kRowBlocksPerCu<TN, PP, kMask>)) void 
 }
 
 // ---- rows times weights that stay in LDS -----------------------------------------------
-// Where a group's weights, or those of 64 to 256 of its columns, fit 128 KB of LDS (256 x 256 of bf16, 128 x 256 of fp32), a block per compute unit
+// Where a group's weights, or those of 64 to 256 of its columns, fit 128 KB of LDS (256 x 256 of bf16, 128 x 128 of fp32), a block per compute unit
 // holds them for a run of the group's rows.  Its eight wavefronts then have nothing in common: each takes 32 rows at a time,
 // its lanes' k-values of a row straight into registers (512 bytes of a row: sixteen steps), all columns from them, and the
 // results through 4 KB of LDS of its own into whole lines.  No barrier but where the weights change, and of the L2 only rows and
@@ -511,9 +563,7 @@ constexpr int kResWaves = 8;
 constexpr int kResRows = 32;              // rows of a wavefront's tile
 constexpr int kResPieces = 8192;          // 16-byte pieces of weights in LDS
 constexpr int kResChunkCols = 4;          // column tiles where a row has several chunks: all their sums are in registers
-// A step is 16 k-values.  fp32: on the bf16 instruction too, three parts of each operand and six products of them a step (gemm_split.hpp says why
-// those suffice), which takes 192 cycles where the fp32 instruction takes 512; ah bh has sums of its own.  A result that is not finite (an operand
-// that is not, or is too large to be taken apart) is computed again in fp32, value by value.
+// A step is 16 k-values.
 template <typename T>
 struct ResStep {
     static constexpr bool kSplit = sizeof(T) == 4;
@@ -534,7 +584,7 @@ struct ResidentCall {
     bool relu;
 };
 
-// NT: column tiles whose sums are in registers at once; kMulti: a row has several chunks (then NT = CT)
+// NT: column tiles whose sums are in registers at once; kMulti: a row has several chunks (then NT = CT; bf16 without a mask)
 template <typename T, int NT, bool kMulti, bool kMask, bool kWords, bool kStore16>
 __global__ __launch_bounds__(kResWaves * 64, 2) void grouped_resident_kernel(ResidentCall q)
 {
@@ -679,9 +729,7 @@ __global__ __launch_bounds__(kResWaves * 64, 2) void grouped_resident_kernel(Res
                         turn(quarter, p[quarter]);
                     }
             };
-            constexpr bool kRest = kSplit && !kMulti;      // sums of their own for the five smaller products: where registers are left
-            floatx16 acc[NT], rest_[kRest ? NT : 1];
-            auto &rest = [&]() -> auto & { if constexpr (kRest) return rest_; else return acc; }();
+            floatx16 acc[NT], rest[kSplit ? NT : 1];       // fp32: the five smaller products have sums of their own
             // a lane's columns of a column tile, and their bias: see fragment_column
             auto bias_of = [&](int tile, float (&v)[16]) {
                 const float4 *b4 = reinterpret_cast<const float4 *>(bias + tile / TN * TN * 32 + hi * TN * 16 + tile % TN * 16);
@@ -702,22 +750,15 @@ __global__ __launch_bounds__(kResWaves * 64, 2) void grouped_resident_kernel(Res
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         acc[j][r] = kSplit ? 0.0f : v[r];
-                        if constexpr (kRest) rest[j][r] = 0.0f;
+                        if constexpr (kSplit) rest[j][r] = 0.0f;
                     }
                 }
             };
-            // in fp32, from what the operands are
             auto again = [&](int col) {
                 float sum = 0.0f;
-                if (row < 0 || col >= q.N) return sum;
-                const T *ar = A + int64_t(row) * q.lda, *hr = kMask ? H + int64_t(row) * q.lda : nullptr;
-                const float *w = q.W + int64_t(group) * q.K * q.N + col * q.w_col;
-                for (int k = 0; k < q.K; ++k) {
-                    float v;
-                    if constexpr (sizeof(T) == 4) v = kMask && !(hr[k] > 0.0f) ? 0.0f : ar[k];
-                    else v = bf16_to_f32(ar[k]);
-                    sum = fmaf(v, w[k * q.w_k], sum);
-                }
+                if constexpr (kSplit)
+                    if (row >= 0 && col < q.N)
+                        sum = in_fp32<kMask>(A + int64_t(row) * q.lda, H + int64_t(row) * q.lda, q.W + int64_t(group) * q.K * q.N + col * q.w_col, q.w_k, q.K);
                 return sum;
             };
             auto store = [&](int ct) {
@@ -731,7 +772,7 @@ __global__ __launch_bounds__(kResWaves * 64, 2) void grouped_resident_kernel(Res
                         bool odd = false;
 #pragma unroll
                         for (int r = 0; r < 16; ++r) {
-                            const float v = (kRest ? acc[unit][r] + rest[unit][r] : acc[unit][r]) * kSplitUnscale;
+                            const float v = (acc[unit][r] + rest[unit][r]) * kSplitUnscale;
                             odd = odd || !(fabsf(v) <= FLT_MAX);
                             acc[unit][r] = v;
                         }
@@ -808,9 +849,6 @@ __global__ __launch_bounds__(kResWaves * 64, 2) void grouped_resident_kernel(Res
 #pragma unroll
                         for (int j = 0; j < NT; ++j) {
                             const uint4 *w = Ws + (((ct + j) * q.steps + c * kResSteps + s) * kParts) * kWave + lane;
-                            auto times = [&](const uint4 &wp, const uint4 &xp, const floatx16 &sum) {
-                                return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, wp), __builtin_bit_cast(bf16x8, xp), sum, 0, 0, 0);
-                            };
                             if constexpr (kSplit) {
                                 const uint4 h = w[0], m = w[kWave], l = w[2 * kWave];
                                 acc[j] = times(h, xp[0], acc[j]);
@@ -1001,19 +1039,8 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void grouped_weight_kernel(WeightCa
                         uint4 a[kParts];
 #pragma unroll
                         for (int o = 0; o < kParts; ++o) a[o] = along_rows(&x[o * kSlab * BM + XS::place(k + tr_row, (wm * TM + i) * 32 + tr_col)], BM);
-                        auto times = [&](int pa, int pb) {
 #pragma unroll
-                            for (int j = 0; j < TN; ++j)
-                                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a[pa]), __builtin_bit_cast(bf16x8, b[j][pb]), acc[i][j], 0, 0, 0);
-                        };
-                        if constexpr (kSplit) {
-                            times(2, 0);
-                            times(0, 2);
-                            times(1, 1);
-                            times(1, 0);
-                            times(0, 1);
-                        }
-                        times(0, 0);
+                        for (int j = 0; j < TN; ++j) add_product<kParts>(a, b[j], acc[i][j]);
                     }
                 }
             }
@@ -1105,7 +1132,7 @@ struct PrepareCall {
     int K, N, col_tiles, steps, TN;
 };
 
-template <typename T, bool kForward, bool kSplit>
+template <typename T, bool kForward>
 __global__ __launch_bounds__(kGgThreads) void grouped_prepare_kernel(PrepareCall q)
 {
     const int b = blockIdx.x;
@@ -1114,7 +1141,7 @@ __global__ __launch_bounds__(kGgThreads) void grouped_prepare_kernel(PrepareCall
             q.bias_out[int64_t(b) * q.col_tiles * 32 + c] = c < q.N ? q.bias[int64_t(b) * q.N + c] : 0.0f;
     if (b < q.row_blocks) write_plan(q.gl, q.rows, b);
     else if (b < q.row_blocks + q.run_blocks) write_plan(q.gl, q.runs, b - q.row_blocks);
-    else write_fragments<T, kForward, kSplit>(q.gl, q.W, q.K, q.N, q.col_tiles, q.steps, q.TN, q.B, b - q.row_blocks - q.run_blocks,
+    else write_fragments<T, kForward>(q.gl, q.W, q.K, q.N, q.col_tiles, q.steps, q.TN, q.B, b - q.row_blocks - q.run_blocks,
                                       gridDim.x - q.row_blocks - q.run_blocks);
 }
 
