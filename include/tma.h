@@ -607,7 +607,7 @@ int tma_gcn_block_bwd(int64_t n_dst, int64_t n_src, int64_t max_entries,
  * group, a dense layer with weights per group, group norm with an activation,
  * dropout.  All pointers device memory; ordered on `stream`; no allocation, no
  * host wait, nothing cleared by a memset (the calls may be captured); fixed
- * summation orders, no atomics.
+ * summation orders: the same bits every time.
  *
  * tma_group_rows: a stable counting sort of n row numbers by group[v].
  * offsets_out [E+1]: offsets_out[g] = number of rows with an id in [0, g);
@@ -627,8 +627,8 @@ int tma_group_rows(int64_t n, const int32_t *group, int32_t E, int32_t *offsets_
  *     dW[g] = sum of X[v]^T dZ[v],  dbias[g] = sum of dZ[v], over g's rows
  *   offsets [E+1], order [n] or NULL as tma_group_rows writes them: group g has
  *   the positions [offsets[g], offsets[g+1]) of the list, position i is row
- *   order[i] (order NULL: row i) of X, Y, dY and dX.  Each row is listed at most
- *   once; rows that are not listed (n counts all) are neither read nor written.
+ *   order[i] (order NULL: row i) of X, Y, dY and dX.  Offsets do not descend;
+ *   each row is listed at most once; rows that are not listed (n counts all) are neither read nor written.
  *   Groups may be empty: their dW and dbias are zero.
  *   X [n, F_in], Y, dY [n, F_out], dX_out [n, F_in] of dtype with leading
  *   dimensions ldx, ldy (Y and dY), ld_dx; dX_out NULL: not wanted, and it is

@@ -4,9 +4,10 @@
 //
 // A wavefront ranks 64 consecutive rows at once: the lanes with the same id are found with one ballot per bit of the id, a
 // row's rank among them is the number of such lanes below its own, and a counter per (wavefront, group) in LDS carries the
-// rank on to the next 64 rows.  Integers throughout, every position has one writer: no atomics, one result.
-// Up to kOneBlockRows rows one block does it all (counts, their prefix, positions; measured below); above that
-// tiles of rows are counted, the counts [group][tile] are prefixed, and the tiles are ranked again from their bases.
+// rank on to the next 64 rows.  Integers throughout, every position has one writer: one result.
+// Up to kOneBlockRows rows one block does it all (counts, their prefix, positions): 5,000 rows of 8 groups 6.9 us, 16,384 rows of 8, 64 and 512
+// groups 13.5, 17.8 and 23.4.  Above that tiles of rows are counted, the counts [group][tile] are prefixed, and the tiles are ranked again from
+// their bases: 16,385 to 30,000 rows 17.9, 19.5 and 23.5; 12,500,000 rows of 64 groups count 12, prefix 9, place 41 us (100 MB, 2.5 TB/s: the ballots).
 #include "kernels.hpp"
 
 namespace tma {
@@ -116,7 +117,7 @@ __global__ __launch_bounds__(kTileThreads) void group_rows_count_kernel(int64_t 
 }
 
 // Positions from bases[g][tile] (and the offsets, by tile 0).  The tile is put in order in LDS first, so that a group's rows go to memory side by
-// side: a store of 64 rows as they come goes to as many lines (12,500,000 rows of 64 groups 54 us, with the order through LDS see below).
+// side: a store of 64 rows as they come goes to as many lines (12,500,000 rows of 64 groups 54 us, with the order through LDS 41).
 __global__ __launch_bounds__(kTileThreads) void group_rows_place_kernel(int64_t n, const int32_t *__restrict__ ids, int E, int bits, int64_t tiles,
                                                                         const int32_t *__restrict__ bases, int32_t *__restrict__ offsets,
                                                                         int32_t *__restrict__ order)
