@@ -7,7 +7,7 @@
 // rank on to the next 64 rows.  Integers throughout, every position has one writer: one result.
 // Up to kOneBlockRows rows one block does it all (counts, their prefix, positions): 5,000 rows of 8 groups 6.9 us, 16,384 rows of 8, 64 and 512
 // groups 13.5, 17.8 and 23.4.  Above that tiles of rows are counted, the counts [group][tile] are prefixed, and the tiles are ranked again from
-// their bases: 16,385 to 30,000 rows 17.9, 19.5 and 23.5; 12,500,000 rows of 64 groups count 12, prefix 9, place 41 us (100 MB, 2.5 TB/s: the ballots).
+// their bases: 16,385 to 30,000 rows 17.9, 19.5 and 23.5; 12,500,000 rows of 64 groups count 12, prefix 9, place 36 us (100 MB, 2.8 TB/s: the ballots).
 #include "kernels.hpp"
 
 namespace tma {
@@ -20,25 +20,29 @@ constexpr int kTileThreads = 256;
 constexpr int kTileChunks = 16;                                   // 64-row chunks of a wavefront of a tile
 constexpr int kTileRows = kTileThreads * kTileChunks;
 
-// the lanes that hold the same id as this one; `bits`: of the largest id
+// the lanes that hold the same id as this one; `bits`: of the largest id.  (Masks of a bit and its two halves: four vector instructions a bit.)
 __device__ __forceinline__ uint64_t same_id(int id, bool in, int bits)
 {
-    uint64_t m = __ballot(in);
+    const uint64_t all = __ballot(in);
+    uint32_t lo = uint32_t(all), hi = uint32_t(all >> 32);
     for (int b = 0; b < bits; ++b) {
-        const uint64_t set = __ballot((id >> b) & 1);
-        m &= (id >> b) & 1 ? set : ~set;
+        const int mine = __builtin_amdgcn_sbfe(id, b, 1);      // all ones or zero
+        const uint64_t set = __ballot(mine);
+        lo &= ~(uint32_t(set) ^ uint32_t(mine));
+        hi &= ~(uint32_t(set >> 32) ^ uint32_t(mine));
     }
-    return m;
+    return uint64_t(hi) << 32 | lo;
 }
 
-__device__ __forceinline__ int below(uint64_t m, int lane) { return __popcll(m & ((uint64_t(1) << lane) - 1)); }
+// lanes of m below this one
+__device__ __forceinline__ int below(uint64_t m) { return int(__builtin_amdgcn_mbcnt_hi(uint32_t(m >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(m), 0u))); }
 
 // one chunk of 64 rows: rank in the wavefront's own counters, which are left advanced (a wavefront's LDS operations complete
 // in order; the fences keep the compiler from moving them)
-__device__ __forceinline__ int take(volatile int32_t *counters, int id, bool in, int bits, int lane)
+__device__ __forceinline__ int take(volatile int32_t *counters, int id, bool in, int bits)
 {
     const uint64_t m = same_id(id, in, bits);
-    const int rank = below(m, lane);
+    const int rank = below(m);
     int pos = 0;
     if (in) pos = counters[id] + rank;
     __builtin_amdgcn_wave_barrier();
@@ -65,7 +69,7 @@ __global__ __launch_bounds__(kOneThreads) void group_rows_one_kernel(int n, cons
     __syncthreads();
 #pragma unroll
     for (int c = 0; c < kChunks; ++c)
-        if (c < chunks) pos[c] = take(counters + wave * E, id[c], id[c] >= 0 && id[c] < E, bits, lane);
+        if (c < chunks) pos[c] = take(counters + wave * E, id[c], id[c] >= 0 && id[c] < E, bits);
     __syncthreads();
     // counts -> bases: over the wavefronts of a group, then over the groups (a thread each)
     int total = 0;
@@ -117,7 +121,7 @@ __global__ __launch_bounds__(kTileThreads) void group_rows_count_kernel(int64_t 
 }
 
 // Positions from bases[g][tile] (and the offsets, by tile 0).  The tile is put in order in LDS first, so that a group's rows go to memory side by
-// side: a store of 64 rows as they come goes to as many lines (12,500,000 rows of 64 groups 54 us, with the order through LDS 41).
+// side: a store of 64 rows as they come goes to as many lines (12,500,000 rows of 64 groups 54 us, with the order through LDS 36).
 __global__ __launch_bounds__(kTileThreads) void group_rows_place_kernel(int64_t n, const int32_t *__restrict__ ids, int E, int bits, int64_t tiles,
                                                                         const int32_t *__restrict__ bases, int32_t *__restrict__ offsets,
                                                                         int32_t *__restrict__ order)
@@ -140,7 +144,7 @@ __global__ __launch_bounds__(kTileThreads) void group_rows_place_kernel(int64_t 
     __syncthreads();
     int pos[kTileChunks];
 #pragma unroll
-    for (int c = 0; c < kTileChunks; ++c) pos[c] = take(counters + wave * E, id[c], id[c] >= 0 && id[c] < E, bits, lane);
+    for (int c = 0; c < kTileChunks; ++c) pos[c] = take(counters + wave * E, id[c], id[c] >= 0 && id[c] < E, bits);
     __syncthreads();
     // a thread's four groups: their counts, where they begin in the tile
     int mine[kPer], total = 0;
