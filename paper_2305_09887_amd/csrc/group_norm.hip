@@ -145,6 +145,8 @@ struct GnLane {
         for (int c = 0; c < CPL; ++c) in[c] = live && (sub + c * sh.W) * E < sh.cg;
     }
     __device__ __forceinline__ int col(const GnShape &sh, int c) const { return c0 + c * sh.W * E; }
+    // where a piece is loaded from: a lane without one takes its group's first, so that no branch stands between loads (each would be waited for)
+    __device__ __forceinline__ int from(const GnShape &sh, int c) const { return in[c] ? col(sh, c) : g * sh.cg; }
     __device__ __forceinline__ int columns() const
     {
         int k = 0;
@@ -243,7 +245,7 @@ __global__ __launch_bounds__(kGnThreads) void gn_rows_fwd_kernel(GnShape sh, con
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int c = 0; c < CPL; ++c)
-                if (ln.in[c] && v0 + u * stride < sh.n) raw[u][c] = P::load(X + (v0 + u * stride) * ldx + ln.col(sh, c));
+                raw[u][c] = P::load(X + (v0 + u * stride < sh.n ? v0 + u * stride : v0) * ldx + ln.from(sh, c));
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t v = v0 + u * stride;
@@ -329,11 +331,11 @@ __global__ __launch_bounds__(kGnThreads) void gn_rows_bwd_kernel(GnShape sh, con
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int c = 0; c < CPL; ++c)
-                if (ln.in[c] && v0 + u * stride < end) {
-                    rx[u][c] = P::load(X + (v0 + u * stride) * ldx + ln.col(sh, c));
-                    rg[u][c] = P::load(dY + (v0 + u * stride) * ldd + ln.col(sh, c));
-                }
+            for (int c = 0; c < CPL; ++c) {
+                const int64_t v = v0 + u * stride < end ? v0 + u * stride : v0;
+                rx[u][c] = P::load(X + v * ldx + ln.from(sh, c));
+                rg[u][c] = P::load(dY + v * ldd + ln.from(sh, c));
+            }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t v = v0 + u * stride;
@@ -455,7 +457,7 @@ __global__ __launch_bounds__(kGnThreads) void gn_moments_kernel(GnShape sh, GnSe
             for (int u = 0; u < U; ++u)
 #pragma unroll
                 for (int c = 0; c < CPL; ++c)
-                    if (ln.in[c] && row + u < end) raw[u][c] = P::load(X + (row + u) * ldx + ln.col(sh, c));
+                    raw[u][c] = P::load(X + (row + u < end ? row + u : row) * ldx + ln.from(sh, c));
         },
         [&](int64_t, int from, int to) {
             float x[U][CPL][E], sum = 0.0f, sq = 0.0f;
@@ -527,7 +529,7 @@ __global__ __launch_bounds__(kGnThreads) void gn_apply_kernel(GnShape sh, GnSegm
             for (int u = 0; u < U; ++u)
 #pragma unroll
                 for (int c = 0; c < CPL; ++c)
-                    if (ln.in[c] && row + u < end) raw[u][c] = P::load(X + (row + u) * ldx + ln.col(sh, c));
+                    raw[u][c] = P::load(X + (row + u < end ? row + u : row) * ldx + ln.from(sh, c));
         },
         [&](int64_t s, int from, int to) {
             if (s != of) st = stats[s * sh.G + ln.g];
@@ -574,11 +576,11 @@ __global__ __launch_bounds__(kGnThreads) void gn_sums_kernel(GnShape sh, GnSegme
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int c = 0; c < CPL; ++c)
-                    if (ln.in[c] && row + u < end) {
-                        rx[u][c] = P::load(X + (row + u) * ldx + ln.col(sh, c));
-                        rg[u][c] = P::load(dY + (row + u) * ldd + ln.col(sh, c));
-                    }
+                for (int c = 0; c < CPL; ++c) {
+                    const int64_t v = row + u < end ? row + u : row;
+                    rx[u][c] = P::load(X + v * ldx + ln.from(sh, c));
+                    rg[u][c] = P::load(dY + v * ldd + ln.from(sh, c));
+                }
         },
         [&](int64_t s, int from, int to) {
             if (s != of) st = stats[s * sh.G + ln.g];
@@ -656,11 +658,11 @@ __global__ __launch_bounds__(kGnThreads) void gn_apply_bwd_kernel(GnShape sh, Gn
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int c = 0; c < CPL; ++c)
-                    if (ln.in[c] && row + u < end) {
-                        rx[u][c] = P::load(X + (row + u) * ldx + ln.col(sh, c));
-                        rg[u][c] = P::load(dY + (row + u) * ldd + ln.col(sh, c));
-                    }
+                for (int c = 0; c < CPL; ++c) {
+                    const int64_t v = row + u < end ? row + u : row;
+                    rx[u][c] = P::load(X + v * ldx + ln.from(sh, c));
+                    rg[u][c] = P::load(dY + v * ldd + ln.from(sh, c));
+                }
         },
         [&](int64_t s, int from, int to) {
             if (s != of) {
