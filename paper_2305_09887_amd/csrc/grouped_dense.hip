@@ -6,7 +6,8 @@
 //
 // Here: the entry points, and the kernels for groups of few rows, which the weights bound: they are read once as they are, in
 // fp32, every multiplication and sum is fp32.  Grids go over (group, slice of 32 columns), so that small layers still have
-// some hundred blocks; rows of a group go through LDS eight at a time.
+// some hundred blocks; rows of a group go through LDS eight at a time, beside a thread's weights of a chunk in registers.  24 rows of 16 groups, 256 ->
+// 256, 7.9 us: one memory latency for positions, one for rows, one for weights (4.2 MB) and the launch.
 #include "grouped_gemm.hpp"
 
 namespace tma {
@@ -261,10 +262,11 @@ static int few_bwd(const char *fn, const GroupList &gl, const void *X, int64_t l
 }
 
 // ---- tiles ---------------------------------------------------------------------
-// Few rows: the vector kernels, which read the weights once as they are; else tiles, which first lay them out.  Forward and backward of 16 groups of
-// 256 -> 256, in a graph, us: fp32 8 rows a group 16.0 + 34 and 18.6 + 46 in tiles, 16 rows 25 + 57 and 18.6 + 51; bf16 4 rows 12.3 + 26 and 14.7 + 29,
-// 8 rows 17 + 37 and 14.8 + 29 (256 groups of 128 -> 64: fp32 at 8 rows 19.5 and 19.7, bf16 at 4 rows 12.7 and 12.0).
-static bool few_rows_a_group(int64_t n, int E, int32_t dtype) { return n <= (dtype == TMA_BF16 ? 4 : 8) * int64_t(E); }
+// Few rows: the vector kernels, which read the weights once as they are; else tiles, which first lay them out.  Forward + backward in a graph, us,
+// few rows and tiles.  fp32, 6 rows a group: 16 groups of 256 -> 256 12 + 27 and 23 + 42, 256 of 128 -> 64 15.5 + 31 and 15.4 + 31.5, 16 of 64 -> 64
+// 10 + 18.5 and 10 + 19, 16 of 128 -> 512 11 + 41 and 18 + 37.5; 8 rows: 16 + 34 and 23 + 42, 19 + 40 and 15 + 31.5, 13 + 23.5 and 10 + 20, 14 + 52 and
+// 18 + 39.  bf16, 2 rows: 8 + 18 and 11 + 24, 11 + 23 and 9 + 24, 7 + 12 and 8 + 17; 3 rows: 12 + 25 and 11 + 24, 12 + 24 and 9 + 23.5, 10 + 17 and 8 + 17.
+static bool few_rows_a_group(int64_t n, int E, int32_t dtype) { return n <= (dtype == TMA_BF16 ? 2 : 6) * int64_t(E); }
 
 struct TileShape {
     bool resident;         // weights in LDS, tiles of 32 rows; else tiles of 64 rows that fetch them
