@@ -10,15 +10,15 @@
 // lanes: G W lanes cover a row, a wavefront reads whole lines, and a lane keeps its columns, gamma, beta and the sums of dgamma
 // and dbeta in registers.  No group takes lanes from another, so that any number of channels goes (up to 1024 a group).
 //
-// Rows by themselves: one pass, several rows of a lane in flight.  1,000,000 rows of 256 channels in 32 groups, bf16, with PReLU 223 us (1.02 GB, 4.6 TB/s);
-// backward of 604,000 with SiLU 195 us (928 MB, 4.8 TB/s): what a copy reaches.
+// Rows by themselves: one pass, several rows of a lane in flight.  1,000,000 rows of 256 channels in 32 groups, bf16, with PReLU 209 us (1.02 GB, 4.9 TB/s);
+// backward of 604,000 with SiLU 187 us (928 MB, 5.0 TB/s): what a copy reaches.
 // Longer segments: a tile is a run of rows that the lanes walk down, segment after segment.  First pass: count, mean and sum of
 // squares about it of every (tile, segment) pair, whose number tile + segment is its own; a second, small kernel joins them per
 // segment in order (Chan, Golub, LeVeque: updating formulas for pairs of samples; sums of squares of raw values would lose the
 // variance of data far from zero); third pass: the result.  No length of a segment makes a block's work: one segment of all
 // rows and 100,000 of a few rows run alike.  Nothing is an atomic: the same bits every time.  Four passes over X in a forward and backward (statistics
-// need the whole segment first): 125,237 rows of 128 in 8 groups, fp32, 1,200 segments, us: moments 27, apply 34, sums 40, backward 42 (64, 128, 128 and
-// 192 MB moved: 2.4 to 4.6 TB/s; a tile's search of its segment and two chunks of loads follow each other), joins 5 to 6 each.
+// need the whole segment first): 125,237 rows of 128 in 8 groups, fp32, 1,200 segments, us: moments 24, apply 32, sums 38, backward 39 (64, 128, 128 and
+// 192 MB moved: 2.7 to 5 TB/s; a tile's search of its segment and two chunks of loads follow each other), joins 5 to 6 each.
 #include "kernels.hpp"
 
 #include <type_traits>
@@ -29,7 +29,7 @@ constexpr int kGnThreads = 256;
 constexpr int kGnMaxChannels = 1024;          // of a group
 constexpr int kGnBlocks = 256 * 8;            // forward: eight blocks fill a compute unit
 constexpr int kGnBwdBlocks = 1024;            // backward: as many partial rows of dgamma and dbeta
-constexpr int64_t kGnLanes = 256 * 1024;      // lanes that a pass over tiles should have (twice as many, in us as above: 32, 34, 43, 40)
+constexpr int64_t kGnLanes = 256 * 1024;      // lanes that a pass over tiles should have (twice as many, in us as above: 26, 31, 40, 39)
 constexpr int kGnChunk = 8;                   // rows of a lane in flight in the first pass
 
 template <int kBytes>
