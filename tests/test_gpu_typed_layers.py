@@ -155,3 +155,42 @@ def test_kinds_that_are_none_are_refused(B):
                      (dict(norm_act=True, norm_groups=3), "multiples"), (dict(dropout=1.0), "dropout"), (dict(dropout=-0.1), "dropout")]:
         with pytest.raises(B.TmaError, match=text):
             build(**kw)
+
+
+def test_two_streams_at_once(B):
+    """The same chain of calls on two streams, workspaces the calls' own: what each would have given alone, bit for bit."""
+    n, E, F = 40_000, 6, 96
+
+    def inputs(seed):
+        g = torch.Generator().manual_seed(seed)
+        kinds = torch.randint(0, E, (n,), generator=g).int().cuda()
+        X, dY = torch.randn(n, F, generator=g).cuda(), torch.randn(n, F, generator=g).cuda()
+        W, b = (torch.randn(E, F, F, generator=g) * 0.1).cuda(), torch.randn(E, F, generator=g).cuda()
+        cuts = torch.sort(torch.randint(0, n, (30,), generator=g)).values.int()
+        segments = torch.cat([torch.zeros(1, dtype=torch.int32), cuts, torch.tensor([n], dtype=torch.int32)]).cuda()
+        return kinds, X, dY, W, b, segments, torch.ones(F, device="cuda"), torch.zeros(F, device="cuda")
+
+    def chain(x, stream):
+        kinds, X, dY, W, b, segments, gamma, beta = x
+        offsets, order = B.tma_group_rows(kinds, E, stream=stream)
+        Y = B.tma_grouped_dense_fwd(X, W, b, offsets, B.TMA_ACT_RELU, order=order, stream=stream)
+        H, stats = B.tma_groupnorm_act_fwd(Y, 8, gamma, beta, B.TMA_ACT_SILU, segments=segments, stream=stream)
+        D = B.tma_dropout_fwd(H, 0.3, 5, stream=stream)
+        dH = B.tma_dropout_bwd(dY, 0.3, 5, stream=stream)
+        dN, dga, dbe, _ = B.tma_groupnorm_act_bwd(Y, dH, 8, gamma, beta, B.TMA_ACT_SILU, segments=segments, stats=stats, stream=stream)
+        dW, db, dX = B.tma_grouped_dense_bwd(X, Y, dN, W, offsets, B.TMA_ACT_RELU, order=order, stream=stream)
+        return offsets, order, Y, D, dga, dbe, dW, db, dX
+
+    both = [inputs(1), inputs(2)]
+    torch.cuda.synchronize()
+    alone = []
+    for x in both:
+        alone.append(chain(x, None))
+        torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        results = [chain(x, s) for x, s in zip(both, streams)]
+        torch.cuda.synchronize()
+        for got, want in zip(results, alone):
+            for a, c in zip(got, want):
+                assert torch.equal(a, c)
