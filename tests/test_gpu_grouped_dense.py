@@ -299,3 +299,39 @@ def test_weight_gradients_of_infinities_and_of_values_near_the_range_end(B, dtyp
         tol = (len(r) + 2) * u * (c.X[r].abs().T @ c.G[r].abs())
         close(dW[e].cpu()[keep], (c.X[r].T @ c.G[r])[keep], tol[keep], f"dW of group {e}")
         close(db[e].cpu(), c.G[r].sum(0), (len(r) + 2) * u * c.G[r].abs().sum(0), "db")
+
+
+LONG = [([90_000, 0, 1, 120_000, 333], 33, 50), ([200_003], 128, 64), ([17_000, 40, 0, 9_000], 20, 2_100), ([30_000, 5, 25_000], 300, 510),
+        ([30_000, 5, 25_000], 510, 250), ([900, 3, 700], 1_300, 70), ([900, 3, 700], 70, 1_300)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("sizes,F_in,F_out", LONG)
+def test_long_lists_and_wide_products(B, sizes, F_in, F_out, dtype):
+    """Lists that are long, or products that are wide, enough for weights in LDS, and some too wide for that: results, masked and plain gradients, infinities."""
+    h = half_step(dtype)
+    for k, (layout, relu) in enumerate([("padded", True), ("odd", False)]):
+        c = Case(B, sizes, F_in, F_out, dtype, layout, loose=3, seed=30 + k)
+        look = [r[torch.cat([torch.arange(min(len(r), 300)), torch.arange(max(len(r) - 300, 0), len(r))])] for r in c.rows]      # of each group
+        out = B._padded(c.n, F_out, dtype, "cuda").fill_(7.0)
+        B.tma_grouped_dense_fwd(c.dX, c.W.cuda(), c.b.cuda(), c.offsets, int(relu), order=c.order, Y_out=out)
+        dX = B._padded(c.n, F_in, dtype, "cuda").fill_(7.0)
+        B.tma_grouped_dense_bwd(c.dX, c.dH if relu else None, c.dG, c.W.cuda(), c.offsets, int(relu), order=c.order, dX_out=dX)
+        for e, r in enumerate(look):
+            x, w, z = c.X[r], c.W[e].double(), c.G[r] * (c.H[r] > 0) if relu else c.G[r]
+            want, mass = x @ w + c.b[e].double(), x.abs() @ w.abs() + c.b[e].double().abs()
+            tol = ((F_in + 3) * u + c.narrowed) * mass
+            want = want.clamp(min=0) if relu else want
+            close(out[r.cuda()].cpu(), want, tol + h * (want.abs() + tol), f"Y {layout}")
+            want = z @ w.T
+            tol = ((F_out + 3) * u + c.narrowed) * (z.abs() @ w.abs().T)
+            close(dX[r.cuda()].cpu(), want, tol + h * (want.abs() + tol), f"dX {layout}")
+        assert (out[c.free.cuda()] == 7).all() and (dX[c.free.cuda()] == 7).all()
+        bad = int(c.rows[0][77])
+        c.dX[bad, F_in - 1] = float("inf")
+        again = B._padded(c.n, F_out, dtype, "cuda").fill_(7.0)
+        B.tma_grouped_dense_fwd(c.dX, c.W.cuda(), None, c.offsets, 0, order=c.order, Y_out=again)
+        w = c.W[0, -1]
+        assert torch.equal(again[bad].cpu().double(), torch.where(w > 0, float("inf"), float("-inf")).double())
+        finite = torch.isfinite(again.float()).all(1)
+        assert int((~finite).sum()) == 1 and not finite[bad]
