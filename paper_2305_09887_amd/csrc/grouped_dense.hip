@@ -512,6 +512,12 @@ static int tiles_bwd(const char *fn, const GroupList &gl, const void *X, int64_t
     return check_launch(fn);
 }
 
+// sizes that the calls take; their workspaces are computed for no others (a width near the end of 32 bits would leave a count of zero to divide by)
+static bool sizes_ok(int64_t n, int32_t E, int32_t F_in, int32_t F_out)
+{
+    return n >= 0 && n <= INT32_MAX && E >= 1 && E <= kMaxGroups && F_in >= 1 && F_out >= 1 && F_in <= (1 << 16) && F_out <= (1 << 16);
+}
+
 static int check_grouped(const char *fn, int64_t n, int32_t E, const int32_t *offsets, int32_t F_in, int32_t F_out, int32_t act, int32_t dtype,
                          const void *ws, size_t ws_bytes, size_t need)
 {
@@ -531,7 +537,7 @@ static int check_grouped(const char *fn, int64_t n, int32_t E, const int32_t *of
 extern "C" size_t tma_grouped_dense_fwd_workspace_bytes(int64_t n, int32_t E, int32_t F_in, int32_t F_out, int32_t dtype)
 {
     using namespace tma;
-    if (n < 0 || E < 1 || F_in < 1 || F_out < 1) return 0;
+    if (!sizes_ok(n, E, F_in, F_out)) return 0;
     if (few_rows_a_group(n, E, dtype)) return 256;
     const TileShape t = tile_shape(n, E, F_in, F_out, dtype == TMA_BF16 ? 2 : 4, false);
     return plan_bytes(n, E, t.height) + t.bias_bytes + t.fragment_bytes;
@@ -561,7 +567,7 @@ extern "C" int tma_grouped_dense_fwd(int64_t n, int32_t E, const int32_t *offset
 extern "C" size_t tma_grouped_dense_bwd_workspace_bytes(int64_t n, int32_t E, int32_t F_in, int32_t F_out, int32_t dtype, int32_t need_dX)
 {
     using namespace tma;
-    if (n < 0 || E < 1 || F_in < 1 || F_out < 1) return 0;
+    if (!sizes_ok(n, E, F_in, F_out)) return 0;
     if (few_rows_a_group(n, E, dtype)) return 256;
     const int height = weight_shape(n, E, F_in, F_out).height;
     const size_t runs = size_t(tile_room(n, E, height));
