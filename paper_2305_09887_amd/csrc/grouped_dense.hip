@@ -377,7 +377,7 @@ static void launch_rows_as(const RowsCall &q, bool words, bool store16, int64_t 
 template <typename T>
 static bool rows_in_words(const void *p, int64_t ld, int64_t n, int F)
 {
-    return (sizeof(T) == 4 || (aligned(p, 4) && ld % 2 == 0)) && (n - 1) * ld + F >= int64_t(16 / sizeof(T));
+    return (sizeof(T) == 4 || (aligned(p, 4) && ld % 2 == 0)) && RowPiece<T, true>::last_place(n, ld, F) >= 0;
 }
 
 template <typename T, bool kMask>

@@ -26,6 +26,7 @@
 // apart) is computed again in fp32, value by value.
 #pragma once
 #include "kernels.hpp"
+#include "row_piece.hpp"
 #include "split_pair.hpp"
 
 #include <cfloat>
@@ -178,59 +179,8 @@ __device__ __forceinline__ void write_fragments(const GroupList &gl, const float
 }
 
 // ---- pieces of rows ----------------------------------------------------------------
-typedef uint32_t Words4 __attribute__((ext_vector_type(4), aligned(4)));
-
 __device__ __forceinline__ float widened(float x) { return x; }
 __device__ __forceinline__ float widened(uint16_t x) { return bf16_to_f32(x); }
-__device__ __forceinline__ uint32_t bits1(const float *p) { return __float_as_uint(*p); }
-__device__ __forceinline__ uint32_t bits1(const uint16_t *p) { return *p; }
-
-// A piece of 16 bytes from element `at` on of an array, of which the first `valid` elements are wanted and the others read as zero.
-// kWords (4-byte aligned, the load needs no more): one load without a branch; a piece that would run past `last`, the last place where
-// 16 bytes are left, comes from there and is moved back in registers.  Else element by element.
-template <typename T, bool kWords>
-struct RowPiece {
-    static constexpr int E = 16 / sizeof(T);
-    static __device__ __forceinline__ uint4 load(const T *__restrict__ x, int64_t at, int valid, int64_t last)
-    {
-        if constexpr (kWords) {
-            const Words4 w = *reinterpret_cast<const Words4 *>(x + (at < last ? at : last));
-            return make_uint4(w.x, w.y, w.z, w.w);
-        } else {
-            uint32_t w[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-            for (int j = 0; j < E; ++j)
-                if (j < valid) w[j * int(sizeof(T)) / 4] |= bits1(x + at + j) << (sizeof(T) == 2 ? 16 * (j & 1) : 0);
-            return make_uint4(w[0], w[1], w[2], w[3]);
-        }
-    }
-    // back: elements by which the piece was fetched too early
-    static __device__ __forceinline__ uint4 moved(const uint4 &p, int back)
-    {
-        uint64_t lo = uint64_t(p.y) << 32 | p.x, hi = uint64_t(p.w) << 32 | p.z;
-        int bits = back * int(sizeof(T)) * 8;
-        if (bits >= 64) {
-            lo = hi;
-            hi = 0;
-            bits -= 64;
-        }
-        if (bits > 0) {
-            lo = lo >> bits | hi << (64 - bits);
-            hi >>= bits;
-        }
-        return make_uint4(uint32_t(lo), uint32_t(lo >> 32), uint32_t(hi), uint32_t(hi >> 32));
-    }
-    static __device__ __forceinline__ uint4 cut(const uint4 &p, int valid)
-    {
-        uint32_t w[4] = {p.x, p.y, p.z, p.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (sizeof(T) == 4) w[i] = valid > i ? w[i] : 0u;
-            else w[i] &= valid > 2 * i + 1 ? ~0u : valid > 2 * i ? 0xFFFFu : 0u;
-        }
-        return make_uint4(w[0], w[1], w[2], w[3]);
-    }
-};
 
 // open_word, open_piece: g where h > 0 (a NaN in h: not), zeros elsewhere
 template <typename T>
@@ -342,7 +292,7 @@ __global__ __launch_bounds__(kGgThreads, kRowBlocksPerCu<TN>) void grouped_rows_
     const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, hi = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave % WN;
     const int piece = tid % PP, row0 = tid / PP;
-    const int64_t last = (q.gl.n - 1) * q.lda + q.K - E;
+    const int64_t last = P::last_place(q.gl.n, q.lda, q.K);
     Share share(int64_t(*q.tile_count) * q.n_tiles);
     if (share.item >= share.end) return;
     const int chunks = (q.steps + kSteps - 1) / kSteps;
@@ -427,7 +377,7 @@ __global__ __launch_bounds__(kGgThreads, kRowBlocksPerCu<TN>) void grouped_rows_
 #pragma unroll
                 for (int i = 0; i < kPieces; ++i) {
                     const int64_t over = element(at, i, c) - last;
-                    if (over > 0) held[i] = P::moved(held[i], int(over));
+                    if (over > 0) held[i] = P::moved(held[i], int(over), P::left_out(A, kMask ? H : nullptr, q.gl.n, q.lda, q.K));
                     held[i] = P::cut(held[i], valid);
                 }
             }
@@ -599,7 +549,7 @@ __global__ __launch_bounds__(kResWaves * 64, 2) void grouped_resident_kernel(Res
     const T *A = static_cast<const T *>(q.A), *H = static_cast<const T *>(q.H);
     T *C = static_cast<T *>(q.C);
     const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, hi = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int64_t last = (q.gl.n - 1) * q.lda + q.K - E;
+    const int64_t last = P::last_place(q.gl.n, q.lda, q.K);
     const int chunks = kMulti ? (q.steps + kResSteps - 1) / kResSteps : 1;
     uint4 *mine = staging[wave];
 
@@ -662,7 +612,7 @@ __global__ __launch_bounds__(kResWaves * 64, 2) void grouped_resident_kernel(Res
             const int32_t after = row_of(t + 2 * kResWaves);
             // rows x * 8 + lane / 8 of the tile, whose pieces lane % 8, + 8, ... this lane loads and stores
             int32_t v[4];
-            int limit[4];                  // the last place in the row where 16 bytes are left
+            int limit[4];                  // the last place in the row where 16 bytes of whole words are left
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
                 v[x] = __shfl(row, x * 8 + lane / 8, kWave);
@@ -723,7 +673,8 @@ __global__ __launch_bounds__(kResWaves * 64, 2) void grouped_resident_kernel(Res
                         for (int r = 0; r < 4; ++r) {
                             uint4 &o = p[quarter][r];
                             if constexpr (kMask) o = open_piece<T>(o, m[quarter][r]);
-                            if (kWords && in_row(quarter) > limit[r]) o = P::moved(o, in_row(quarter) - limit[r]);
+                            if (kWords && in_row(quarter) > limit[r])
+                                o = P::moved(o, in_row(quarter) - limit[r], P::left_out(A, kMask ? H : nullptr, q.gl.n, q.lda, q.K));
                             if (kWords) o = P::cut(o, q.K - k0 - quarter * kQuarter);
                         }
                         turn(quarter, p[quarter]);
@@ -937,7 +888,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void grouped_weight_kernel(WeightCa
     const T *X = static_cast<const T *>(q.X), *G = static_cast<const T *>(q.G), *H = static_cast<const T *>(q.H);
     const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, hi = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave % WN;
-    const int64_t x_last = (q.gl.n - 1) * q.ldx + q.M - E, g_last = (q.gl.n - 1) * q.ldg + q.N - E;
+    const int64_t x_last = P::last_place(q.gl.n, q.ldx, q.M), g_last = P::last_place(q.gl.n, q.ldg, q.N);
     const int tiles = q.m_tiles * q.n_tiles;
     const int quarter = lane >> 4, i16 = lane & 15;
     const int tr_row = 8 * (quarter >> 1) + (i16 >> 2), tr_col = 16 * (quarter & 1) + 4 * (i16 & 3);
@@ -1001,7 +952,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void grouped_weight_kernel(WeightCa
                     uint4 p = xh[d][i];
                     if (x_ragged && v >= 0) {
                         const int64_t over = int64_t(v) * q.ldx + (xv > 0 ? xc : 0) - x_last;
-                        if (over > 0) p = P::moved(p, int(over));
+                        if (over > 0) p = P::moved(p, int(over), P::left_out(X, nullptr, q.gl.n, q.ldx, q.M));
                     }
                     if (v < 0) p = make_uint4(0u, 0u, 0u, 0u);
                     XS::put(x, XS::row(i), XS::column(), p);
@@ -1013,7 +964,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void grouped_weight_kernel(WeightCa
                     if constexpr (kMask) p = open_piece<T>(p, hh[d][i]);
                     if (z_ragged && v >= 0) {
                         const int64_t over = int64_t(v) * q.ldg + (zv > 0 ? zc : 0) - g_last;
-                        if (over > 0) p = P::moved(p, int(over));
+                        if (over > 0) p = P::moved(p, int(over), P::left_out(G, kMask ? H : nullptr, q.gl.n, q.ldg, q.N));
                     }
                     if (v < 0) p = make_uint4(0u, 0u, 0u, 0u);
                     ZS::put(z, ZS::row(i), ZS::column(), p);
