@@ -64,7 +64,7 @@ __global__ __launch_bounds__(kFewThreads) void grouped_few_fwd_kernel(GroupList 
                                                                       int64_t ldy, int slices)
 {
     __shared__ float rows[kSideRows][kFewK + 4];
-    __shared__ float sums[kFewThreads / kWave][kSideRows][kFewCols];
+    __shared__ __attribute__((aligned(16))) float sums[kFewThreads / kWave][kSideRows][kFewCols];
     const int g = int(blockIdx.x) / slices, n0 = int(blockIdx.x) % slices * kFewCols;
     const int64_t begin = gl.begin(g), end = gl.begin(g + 1);
     const int q = int(threadIdx.x) % 8, ks = int(threadIdx.x) / 8, wave = int(threadIdx.x) / kWave, lane = int(threadIdx.x) % kWave;
@@ -179,7 +179,7 @@ __global__ __launch_bounds__(kFewThreads) void grouped_few_bwd_weight_kernel(Gro
                                                                              float *__restrict__ db, int slices)
 {
     __shared__ float xs[kSideRows][kFewCols];
-    __shared__ float zs[kSideRows][kFewO];
+    __shared__ __attribute__((aligned(16))) float zs[kSideRows][kFewO];
     const int g = int(blockIdx.x) / slices, m0 = int(blockIdx.x) % slices * kFewCols, il = int(threadIdx.x) / 8, q = int(threadIdx.x) % 8;
     const int64_t begin = gl.begin(g), end = gl.begin(g + 1);
     for (int o0 = 0; o0 < N; o0 += kFewO) {
