@@ -8,7 +8,7 @@ import pytest
 
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2305_09887_amd", "csrc")
 SOURCES = [f for k in ("group_*.hip", "grouped_*", "dropout.hip") for f in sorted(glob.glob(os.path.join(CSRC, k)))]
-BYTES = {"float": 4, "int32_t": 4, "uint16_t": 2, "int64_t": 8, "float2": 8, "uint2": 8, "float4": 16, "uint4": 16}
+BYTES = {"float": 4, "int": 4, "int32_t": 4, "uint16_t": 2, "int64_t": 8, "float2": 8, "uint2": 8, "float4": 16, "uint4": 16}
 
 
 def misdeclared(text):
@@ -17,7 +17,7 @@ def misdeclared(text):
     for m in re.finditer(r"__shared__ (?:__attribute__\(\(aligned\((\d+)\)\)\) )?(\w+) (\w+)\[|reinterpret_cast<(?:const )?(\w+) \*>\(&(\w+)\[", text):
         if m.group(3):
             declared[m.group(3)] = max(int(m.group(1) or 0), BYTES[m.group(2)])
-        elif m.group(5) in declared and declared[m.group(5)] < BYTES[m.group(4)]:
+        elif m.group(5) in declared and declared[m.group(5)] < BYTES.get(m.group(4), 0):      # (a template's type: no piece)
             wrong.append((m.group(5), declared[m.group(5)], BYTES[m.group(4)]))
     return wrong
 
