@@ -125,6 +125,8 @@ class LocalTrainer:
             ws_bytes = max(max(B.tma_grouped_dense_fwd_workspace_bytes(self.n, self.n_kinds, fi, fo, dt),
                                B.tma_grouped_dense_bwd_workspace_bytes(self.n, self.n_kinds, fi, fo, dt, l > 0))
                            for l, (fi, fo) in enumerate(pairs))
+            self.kind_offsets = torch.empty(self.n_kinds + 1, dtype=torch.int32, device=dev)
+            self.kind_order = torch.empty(self.n, dtype=torch.int32, device=dev)
             self.set_kinds(node_kinds)
         else:
             ws_bytes = max(B.tma_dense_bwd_workspace_bytes(self.n, fi, fo) for fi, fo in pairs)
@@ -153,14 +155,22 @@ class LocalTrainer:
             self.stream.wait_stream(torch.cuda.current_stream(dev))
 
     def set_kinds(self, node_kinds):
-        """The kind of each of the trainer's nodes (int32 in [0, n_kinds)); waits for the stream, to see that each has one."""
+        """The kind of each of the trainer's nodes (int32 in [0, n_kinds)); waits for the stream, to see that each has one.  The list goes
+        into the buffers that the trainer has had from the start, so that steps captured before run on the new kinds; a call that is refused
+        leaves the kinds as they were."""
+        if not self.n_kinds:
+            raise B.TmaError("LocalTrainer.set_kinds: the trainer was made without kinds")
+        if node_kinds.device != self.X.device:
+            raise B.TmaError("LocalTrainer.set_kinds: kinds must be on the trainer's device")
         if node_kinds.numel() != self.n:
             raise B.TmaError("LocalTrainer.set_kinds: one kind per node")
         self.stream.wait_stream(torch.cuda.current_stream(node_kinds.device))
         with torch.cuda.stream(self.stream):
-            self.kind_offsets, self.kind_order = B.tma_group_rows(node_kinds, self.n_kinds)
-            if int(self.kind_offsets[-1]) != self.n:
+            offsets, order = B.tma_group_rows(node_kinds, self.n_kinds)
+            if int(offsets[-1]) != self.n:
                 raise B.TmaError("LocalTrainer.set_kinds: a node's kind is outside [0, n_kinds)")
+            self.kind_offsets.copy_(offsets)
+            self.kind_order.copy_(order)
 
     def set_graph(self, rowptr, colidx, inv_deg, rowptr_T=None, colidx_T=None, nnz=None):
         """Point the trainer at a freshly extracted subgraph with the same node count."""
