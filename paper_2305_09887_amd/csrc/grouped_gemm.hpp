@@ -950,9 +950,10 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void grouped_weight_kernel(WeightCa
                 for (int i = 0; i < XS::kPieces; ++i) {
                     const int v = row(s, XS::row(i));
                     uint4 p = xh[d][i];
-                    if (x_ragged && v >= 0) {
+                    if (x_ragged && v >= 0) {        // (fp32: a column is taken apart together with its neighbour, which may be none)
                         const int64_t over = int64_t(v) * q.ldx + (xv > 0 ? xc : 0) - x_last;
                         if (over > 0) p = P::moved(p, int(over), P::left_out(X, nullptr, q.gl.n, q.ldx, q.M));
+                        if constexpr (kSplit) p = P::cut(p, xv);
                     }
                     if (v < 0) p = make_uint4(0u, 0u, 0u, 0u);
                     XS::put(x, XS::row(i), XS::column(), p);
@@ -965,6 +966,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void grouped_weight_kernel(WeightCa
                     if (z_ragged && v >= 0) {
                         const int64_t over = int64_t(v) * q.ldg + (zv > 0 ? zc : 0) - g_last;
                         if (over > 0) p = P::moved(p, int(over), P::left_out(G, kMask ? H : nullptr, q.gl.n, q.ldg, q.N));
+                        if constexpr (kSplit) p = P::cut(p, zv);
                     }
                     if (v < 0) p = make_uint4(0u, 0u, 0u, 0u);
                     ZS::put(z, ZS::row(i), ZS::column(), p);
