@@ -628,7 +628,8 @@ int tma_group_rows(int64_t n, const int32_t *group, int32_t E, int32_t *offsets_
  *   offsets [E+1], order [n] or NULL as tma_group_rows writes them: group g has
  *   the positions [offsets[g], offsets[g+1]) of the list, position i is row
  *   order[i] (order NULL: row i) of X, Y, dY and dX.  Offsets do not descend;
- *   each row is listed at most once; rows that are not listed (n counts all) are neither read nor written.
+ *   each row is listed at most once; rows that are not listed (n counts all) are not written and their values have no influence, but all n
+ *   rows are memory that may be read: a tile's empty places and a row's ragged end fetch from a neighbouring or the first row.
  *   Groups may be empty: their dW and dbias are zero.
  *   X [n, F_in], Y, dY [n, F_out], dX_out [n, F_in] of dtype with leading
  *   dimensions ldx, ldy (Y and dY), ld_dx; dX_out NULL: not wanted, and it is
@@ -660,7 +661,8 @@ int tma_grouped_dense_bwd(int64_t n, int32_t E, const int32_t *offsets, const in
  *     Xh = (X - mean) / sqrt(var + eps),  Y = act(gamma (.) Xh + beta)
  *   segments != NULL: segment s is the rows [segments[s], segments[s+1]), int32
  *     [n_segments + 1], non-decreasing, within [0, n]; segments may be empty,
- *     and rows outside all of them are neither read nor written.
+ *     and rows outside all of them are not written and their values have no influence (they may be read: rows are fetched in chunks before
+ *     their segments are known).
  *   segments == NULL: runs of rows_per_segment rows, which divides n
  *     (n_segments is not read); with rows_per_segment = 1 each row is normalised
  *     by itself (G = 1: layer normalisation).
