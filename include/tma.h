@@ -635,7 +635,10 @@ int tma_group_rows(int64_t n, const int32_t *group, int32_t E, int32_t *offsets_
  *   dimensions ldx, ldy (Y and dY), ld_dx; dX_out NULL: not wanted, and it is
  *   none of the inputs.  W [E, F_in, F_out] fp32, bias [E, F_out] fp32 or NULL;
  *   dW [E, F_in, F_out], dbias [E, F_out] (or NULL) fp32 OVERWRITTEN.
- *   act: TMA_ACT_NONE or TMA_ACT_RELU (Y is read by the backward only then).
+ *   act: TMA_ACT_NONE or TMA_ACT_RELU (Y is read by the backward only then).  The ReLU of a NaN is 0 and closed.
+ *   dtype TMA_BF16: from n > 2 E rows on the weights are rounded once to bf16 (as in the library's other bf16 products), of fewer rows they are
+ *   multiplied as they are, in fp32: a row's result can change by that rounding where the list grows past 2 E.  Sums are fp32, Y and dX
+ *   are rounded once.  Times are those of groups alike up to 6 E rows (bf16 2 E): there a group's rows are a few blocks' work.
  *   Widths up to 65536, 1 <= E <= 1024.
  * Workspaces, 256-byte aligned: tma_grouped_dense_fwd_workspace_bytes(n, E,
  * F_in, F_out, dtype), tma_grouped_dense_bwd_workspace_bytes(..., dX_out != NULL).
@@ -667,7 +670,7 @@ int tma_grouped_dense_bwd(int64_t n, int32_t E, const int32_t *offsets, const in
  *     (n_segments is not read); with rows_per_segment = 1 each row is normalised
  *     by itself (G = 1: layer normalisation).
  *   act: TMA_ACT_NONE, _RELU, _PRELU (slope: one fp32 value in device memory,
- *     as for tma_layernorm_prelu_*; else slope may be NULL), _SILU.
+ *     as for tma_layernorm_prelu_*; else slope may be NULL), _SILU.  The ReLU of a NaN is 0.
  *   gamma, beta [F] fp32; X, Y, dY, dX [n, F] of dtype with their own leading
  *     dimensions.  Y_out and dX_out are not X; dX_out may be dY.
  *   stats_out [n_segments, G, 2] fp32, 8-byte aligned, or NULL: mean and

@@ -171,7 +171,9 @@ struct GnAct {
         : slope(act == TMA_ACT_PRELU ? *slope_p : act == TMA_ACT_RELU ? 0.0f : 1.0f), zero(act == TMA_ACT_RELU)
     {
     }
-    // kExact (fp32 storage): the library's exponential and division; else the instructions, whose last bits bf16 does not hold
+    // kExact (fp32 storage): the library's exponential and division; else the instructions, off by some (2 |y| + 8) 2^-23 of themselves, which bf16 does not
+    // hold.  In the sums of dgamma and dbeta, fp32 also for bf16 storage, that is what an element's share may be off by: 2 10^-6 for y of three, where the
+    // rounding of the bf16 inputs is 4 10^-3
     static __device__ __forceinline__ float sigmoid(float y)
     {
         if constexpr (kExact) return 1.0f / (1.0f + expf(-y));

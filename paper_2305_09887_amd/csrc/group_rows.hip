@@ -5,7 +5,7 @@
 // A wavefront ranks 64 consecutive rows at once: the lanes with the same id are found with one ballot per bit of the id, a
 // row's rank among them is the number of such lanes below its own, and a counter per (wavefront, group) in LDS carries the
 // rank on to the next 64 rows.  Integers throughout, every position has one writer: one result.
-// Up to kOneBlockRows rows one block does it all (counts, their prefix, positions): 5,000 rows of 8 groups 6.9 us, 16,384 rows of 8, 64 and 512
+// Up to kOneBlockRows rows one block does it all (counts, their prefix, positions): 5,000 rows of 8 groups 6.3 us, 16,384 rows of 8, 64 and 512
 // groups 13.5, 17.8 and 23.4.  Above that tiles of rows are counted, the counts [group][tile] are prefixed, and the tiles are ranked again from
 // their bases: 16,385 to 30,000 rows 17.9, 19.5 and 23.5; 12,500,000 rows of 64 groups count 12, prefix 9, place 36 us (100 MB, 2.8 TB/s: the ballots).
 #include "kernels.hpp"

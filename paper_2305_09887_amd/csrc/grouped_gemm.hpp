@@ -18,7 +18,7 @@
 // grouped_weight_kernel (weight gradients): dW[g] += X[v]^T dZ[v] over a run of a group's rows, up to 256 x 256 results a block (all
 // of a run's rows are then read once); both operands come as they lie, rows of LDS, and are read along columns by the transposing LDS
 // read.  Runs of one group are added up in order by a second kernel; a group of one run is stored at once.  604,000 rows of 256 x 256
-// in bf16 196 to 211 us (X, dY and the mask 928 MB, 4.4 to 4.7 TB/s); 125,237 of 128 x 256 in fp32 76 us (321 MB, 4.2 TB/s; on the fp32 instruction 102).
+// in bf16 196 to 216 us (X, dY and the mask 928 MB, 4.3 to 4.7 TB/s); 125,237 of 128 x 256 in fp32 74 us (321 MB, 4.3 TB/s; on the fp32 instruction 102).
 //
 // bf16: v_mfma_f32_32x32x16_bf16, weights rounded once to bf16 (as in all products of bf16 storage here), fp32 accumulation, results rounded once.
 // fp32: the same instruction, three bf16 parts of each operand and six products of them (gemm_split.hpp says why those suffice): 192 cycles for 16

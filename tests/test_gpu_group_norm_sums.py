@@ -227,7 +227,7 @@ def test_gradients_over_many_tiles(B, edges, dtype, act):
 
 def test_gradients_against_differences(B):
     """L = sum(G (.) Y) along the gradient's own signs, a central difference of the fp32 forward pass.  Its truncation is what the same difference has in 64 bits; the rounding of a
-    pass is at most sum|G| times an element's bound, 4 (160 + 44 / 8) u (|gamma| (|xh| + mean|x| rstd) + |beta|) and u |y| more, here below 800 u (|gamma| + |beta|) 5."""
+    pass is at most sum|G| times an element's bound, 4 (160 + 44 / 8) u (|gamma| (|xh| + mean|x| rstd) + |beta|) and u |y| more, here below 800 u times 8 (the factor is 5.5)."""
     edges, G, cg, step = [0, 20, 64], 4, 8, 2.0 ** -5
     c = Gradients(64, G, cg, edges, torch.float32, "silu", 7)
     of, _ = of_and_rows(edges, 64)
