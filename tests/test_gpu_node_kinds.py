@@ -60,3 +60,19 @@ def test_a_refused_call_leaves_the_kinds_as_they_were(B):
 def test_a_trainer_without_kinds_takes_none(B):
     with pytest.raises(B.TmaError, match="without kinds"):
         make(B, "mlp", 20, [4, 8, 3], 0, 0.0, 0, torch.float32)[0].set_kinds(torch.zeros(20, dtype=torch.int32, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_trainer_without_nodes(B, dtype):
+    """No rows at all: every layer's gradients are zero, and the parameters stay."""
+    from paper_2305_09887_amd.trainer import LocalTrainer
+    i32 = lambda k: torch.zeros(k, dtype=torch.int32, device="cuda")
+    tr = LocalTrainer(i32(1), i32(1), torch.zeros(0, device="cuda"), torch.zeros((0, 8), dtype=dtype, device="cuda"), i32(0), [8, 16, 12, 4], encoder="mlp", norm_act=True,
+                      norm_groups=4, dropout=0.5, node_kinds=i32(0), n_kinds=3)
+    tr.W.copy_(torch.randn(tr.W.shape, generator=torch.Generator().manual_seed(1)))
+    tr.set_kinds(i32(0))
+    held = tr.W.clone()
+    tr.dW.fill_(7.0)
+    assert tr.forward().shape == (0, 4)
+    tr.step(0.1)
+    assert not tr.dW.any() and torch.equal(tr.W, held)
