@@ -48,8 +48,8 @@ typedef enum {
 } tma_status;
 
 typedef enum { TMA_F32 = 0, TMA_BF16 = 1 } tma_dtype;
-/* PRELU and SILU: tma_groupnorm_act_* alone takes them. */
-typedef enum { TMA_ACT_NONE = 0, TMA_ACT_RELU = 1, TMA_ACT_PRELU = 2, TMA_ACT_SILU = 3 } tma_act;
+/* PRELU: tma_groupnorm_act_* alone takes it; SILU: that and the wide layers (tma_gated_dense_*, tma_dense_residual_*), which alone take GELU. */
+typedef enum { TMA_ACT_NONE = 0, TMA_ACT_RELU = 1, TMA_ACT_PRELU = 2, TMA_ACT_SILU = 3, TMA_ACT_GELU = 4 } tma_act;
 
 /* Library version as major*10000 + minor*100 + patch. */
 int tma_version(void);
@@ -716,6 +716,90 @@ int tma_dropout_fwd(int64_t n, int32_t F, const void *X, int64_t ldx, double p, 
 
 int tma_dropout_bwd(int64_t n, int32_t F, const void *dY, int64_t ldy, double p, uint64_t seed, const int64_t *d_step,
                     int64_t first_row, int32_t dtype, void *dX_out, int64_t ldx, tma_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Wide layers: a gated dense layer, and a dense layer that adds to what goes
+ * past it.  A residual block is one call of each: with the first's G, U,
+ * H' = H + (act(G) (.) U) W + b.  All pointers device memory; ordered on `stream`; no allocation, no host wait,
+ * nothing cleared by a memset (the calls may be captured); fixed summation
+ * orders: the same bits every time.
+ *
+ * tma_gated_dense_fwd / _bwd:
+ *     G = X W_gate + b_gate,  U = X W_up + b_up,  H = act(G) (.) U
+ *     dG = dH (.) U (.) act'(G),  dU = dH (.) act(G)
+ *     dW_gate = X^T dG,  dW_up = X^T dU,  db_gate = 1^T dG,  db_up = 1^T dU
+ *     dX = dG W_gate^T + dU W_up^T + R
+ *   X [n, F_in], G, U, H, dH [n, F_out], dX, R [n, F_in] of dtype with leading
+ *   dimensions ldx, ldg (G and U), ldh, ld_dx, ldr.  W_gate, W_up [F_in, F_out],
+ *   b_gate, b_up [F_out] fp32; each b may be NULL.  act: NONE, RELU, SILU, GELU
+ *   (z Phi(z), exact).  G_out, U_out: NULL together where no backward pass
+ *   follows (H does not change by that).  R NULL: nothing is added; R may be dX_out.
+ *   dX_out NULL: not wanted.  dW_* [F_in, F_out], db_* [F_out] (NULL together)
+ *   fp32 OVERWRITTEN; zeros where n = 0.
+ *
+ * tma_dense_residual_fwd / _bwd:
+ *     Z = X W + 1 b^T,  Y = act(Z) + R
+ *     dZ = dY (.) act'(Z),  dW = X^T dZ,  dbias = 1^T dZ,  dX = dZ W^T + R
+ *   as above; R [n, F_out] forward (NULL: nothing; may be Y_out), [n, F_in]
+ *   backward (NULL: nothing; may be dX_out, and dY where F_in = F_out).  Z_out
+ *   NULL where no backward pass follows or act is NONE; the backward reads Z
+ *   with an activation only.
+ *
+ * dtype TMA_BF16: weights are rounded to bf16 for the products, sums are fp32,
+ * results are rounded once; the gradients of weights are fp32, of pre-activations of 16 bits
+ * or more.  TMA_F32: products of three bf16 parts of each value, which hold its 24
+ * bits; absolute error of a part 2^-126.  A NaN or an infinity in an input makes
+ * results that it reaches non-finite (NaN where fp32 arithmetic may give an
+ * infinity).  The ReLU of a NaN is 0 and closed.  Widths up to 65536.  What lies in a row's padding has no
+ * influence and is left as it is.
+ * Workspaces, 256-byte aligned: the *_workspace_bytes queries.
+ * ---------------------------------------------------------------------- */
+size_t tma_gated_dense_fwd_workspace_bytes(int64_t n, int32_t F_in, int32_t F_out, int32_t dtype);
+
+int tma_gated_dense_fwd(int64_t n, const void *X, int64_t ldx, int32_t F_in, const float *W_gate, const float *W_up,
+                        const float *b_gate, const float *b_up, int32_t F_out, int32_t act, int32_t dtype, void *G_out, void *U_out,
+                        int64_t ldg, void *H_out, int64_t ldh, void *ws, size_t ws_bytes, tma_stream_t stream);
+
+size_t tma_gated_dense_bwd_workspace_bytes(int64_t n, int32_t F_in, int32_t F_out, int32_t dtype, int32_t need_dX);
+
+int tma_gated_dense_bwd(int64_t n, const void *X, int64_t ldx, const void *G, const void *U, int64_t ldg, const void *dH, int64_t ldh,
+                        const float *W_gate, const float *W_up, int32_t F_in, int32_t F_out, int32_t act, int32_t dtype,
+                        float *dW_gate, float *dW_up, float *db_gate, float *db_up, void *dX_out, int64_t ld_dx,
+                        const void *R, int64_t ldr, void *ws, size_t ws_bytes, tma_stream_t stream);
+
+size_t tma_dense_residual_fwd_workspace_bytes(int64_t n, int32_t F_in, int32_t F_out, int32_t dtype);
+
+int tma_dense_residual_fwd(int64_t n, const void *X, int64_t ldx, int32_t F_in, const float *W, const float *bias, int32_t F_out,
+                           int32_t act, int32_t dtype, const void *R, int64_t ldr, void *Z_out, int64_t ldz, void *Y_out, int64_t ldy,
+                           void *ws, size_t ws_bytes, tma_stream_t stream);
+
+size_t tma_dense_residual_bwd_workspace_bytes(int64_t n, int32_t F_in, int32_t F_out, int32_t act, int32_t dtype, int32_t need_dX);
+
+int tma_dense_residual_bwd(int64_t n, const void *X, int64_t ldx, const void *Z, int64_t ldz, const void *dY, int64_t ldy,
+                           const float *W, int32_t F_in, int32_t F_out, int32_t act, int32_t dtype, float *dW, float *dbias,
+                           void *dX_out, int64_t ld_dx, const void *R, int64_t ldr, void *ws, size_t ws_bytes, tma_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * The norm of a model's gradients, n_tensors of them, and clipping by it:
+ *     norm = sqrt(sum of g^2 over all tensors)
+ *     out = g * c,   c = 1 where norm <= max_norm, else max_norm / norm
+ * h_grads, h_outs: HOST arrays of n_tensors device pointers, h_sizes: HOST array
+ * of their lengths (0 is allowed); read before the call returns.  Tensors are dense, of
+ * dtype, aligned to it, and do not overlap; h_outs NULL: in place (nothing is
+ * written where c = 1); h_outs[i] may be h_grads[i].  norm_out [1] fp32
+ * (device).  Squares and their sum are fp64, each result is rounded once.  A
+ * norm of NaN makes all results NaN, an infinite one finite gradients 0 and
+ * infinite ones NaN.  max_norm >= 0.  At most 131072 tensors.
+ * The calls may be captured: a graph keeps the pointers and lengths.
+ * Workspace: tma_grad_norm_workspace_bytes(n_tensors), 256-byte aligned.
+ * ---------------------------------------------------------------------- */
+size_t tma_grad_norm_workspace_bytes(int32_t n_tensors);
+
+int tma_grad_norm(int32_t n_tensors, const void *const *h_grads, const int64_t *h_sizes, int32_t dtype, float *norm_out,
+                  void *ws, size_t ws_bytes, tma_stream_t stream);
+
+int tma_grad_clip(int32_t n_tensors, const void *const *h_grads, void *const *h_outs, const int64_t *h_sizes, int32_t dtype,
+                  double max_norm, float *norm_out, void *ws, size_t ws_bytes, tma_stream_t stream);
 
 /* ------------------------------------------------------------------------
  * Losses on the last layer's output.

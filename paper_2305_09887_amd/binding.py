@@ -16,7 +16,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.environ.get("TMA_LIBRARY_PATH") or os.path.join(_PKG, "libtma.so")   # (a build elsewhere: set TMA_LIBRARY_PATH)
 
 TMA_F32, TMA_BF16 = 0, 1
-TMA_ACT_NONE, TMA_ACT_RELU, TMA_ACT_PRELU, TMA_ACT_SILU = 0, 1, 2, 3      # the last two: tma_groupnorm_act_* alone
+TMA_ACT_NONE, TMA_ACT_RELU, TMA_ACT_PRELU, TMA_ACT_SILU, TMA_ACT_GELU = 0, 1, 2, 3, 4    # tma.h says which calls take the last three
 
 EXPORTS = (
     "tma_version", "tma_last_error", "tma_partition", "tma_mix64",
@@ -42,6 +42,9 @@ EXPORTS = (
     "tma_grouped_dense_bwd",
     "tma_groupnorm_act_fwd_workspace_bytes", "tma_groupnorm_act_fwd", "tma_groupnorm_act_bwd_workspace_bytes",
     "tma_groupnorm_act_bwd", "tma_dropout_fwd", "tma_dropout_bwd",
+    "tma_gated_dense_fwd_workspace_bytes", "tma_gated_dense_fwd", "tma_gated_dense_bwd_workspace_bytes", "tma_gated_dense_bwd",
+    "tma_dense_residual_fwd_workspace_bytes", "tma_dense_residual_fwd", "tma_dense_residual_bwd_workspace_bytes",
+    "tma_dense_residual_bwd", "tma_grad_norm_workspace_bytes", "tma_grad_norm", "tma_grad_clip",
     "tma_loss_workspace_bytes", "tma_softmax_ce", "tma_sigmoid_l2", "tma_sgd_step", "tma_adam_step", "tma_average",
     "tma_gather_rows", "tma_profile_begin", "tma_profile_end", "tma_profile_count", "tma_profile_entry",
     "tma_profile_sequence_count", "tma_profile_sequence_entry",
@@ -71,6 +74,17 @@ _SIGNATURES = {
     "tma_groupnorm_act_bwd": "liilplplplpppfiipplppppzp",
     "tma_dropout_fwd": "lipldupliplp",
     "tma_dropout_bwd": "lipldupliplp",
+    "tma_gated_dense_fwd_workspace_bytes": "liii",
+    "tma_gated_dense_fwd": "lplippppiiipplplpzp",
+    "tma_gated_dense_bwd_workspace_bytes": "liiii",
+    "tma_gated_dense_bwd": "lplpplplppiiiippppplplpzp",
+    "tma_dense_residual_fwd_workspace_bytes": "liii",
+    "tma_dense_residual_fwd": "lplippiiiplplplpzp",
+    "tma_dense_residual_bwd_workspace_bytes": "liiiii",
+    "tma_dense_residual_bwd": "lplplplpiiiippplplpzp",
+    "tma_grad_norm_workspace_bytes": "i",
+    "tma_grad_norm": "ippippzp",
+    "tma_grad_clip": "ipppidppzp",
 }
 
 
@@ -91,7 +105,10 @@ def lib() -> C.CDLL:
                      "tma_mfg_relabel_workspace_bytes", "tma_sage_block_bwd_workspace_bytes",
                      "tma_gcn_block_bwd_workspace_bytes", "tma_sage_weights_bf16_bytes", "tma_group_rows_workspace_bytes",
                      "tma_grouped_dense_fwd_workspace_bytes", "tma_grouped_dense_bwd_workspace_bytes",
-                     "tma_groupnorm_act_fwd_workspace_bytes", "tma_groupnorm_act_bwd_workspace_bytes"):
+                     "tma_groupnorm_act_fwd_workspace_bytes", "tma_groupnorm_act_bwd_workspace_bytes",
+                     "tma_gated_dense_fwd_workspace_bytes", "tma_gated_dense_bwd_workspace_bytes",
+                     "tma_dense_residual_fwd_workspace_bytes", "tma_dense_residual_bwd_workspace_bytes",
+                     "tma_grad_norm_workspace_bytes"):
             getattr(L, name).restype = C.c_size_t
         for name, codes in _SIGNATURES.items():
             getattr(L, name).argtypes = [_CODES[c] for c in codes]
@@ -1133,6 +1150,184 @@ def tma_dropout_fwd(X, p: float, seed: int, step=None, first_row: int = 0, out=N
 def tma_dropout_bwd(dY, p: float, seed: int, step=None, first_row: int = 0, out=None, stream=None):
     """dX of tma_dropout_fwd with the same arguments.  out may be dY."""
     return _dropout("tma_dropout_bwd", lib().tma_dropout_bwd, dY, p, seed, step, first_row, out, stream)
+
+
+def _rows_or_none(t, name, shape, dtype):
+    """Address and leading dimension of a [rows, cols] tensor, or of none."""
+    if t is None:
+        return None, shape[1]
+    return t.data_ptr(), _rows_like(t, name, shape, dtype)
+
+
+def _weight_shape(where, name, W, F_in):
+    if W.dim() != 2 or W.shape[0] != F_in:
+        raise TmaError(f"{where}: {name} must be [F_in, F_out]")
+    return W.shape[1]
+
+
+def tma_gated_dense_fwd_workspace_bytes(n: int, F_in: int, F_out: int, dtype: int) -> int:
+    return int(lib().tma_gated_dense_fwd_workspace_bytes(n, F_in, F_out, dtype))
+
+
+def tma_gated_dense_fwd(X, W_gate, W_up, b_gate=None, b_up=None, act: int = TMA_ACT_SILU, save=True, G_out=None, U_out=None,
+                        H_out=None, ws=None, stream=None):
+    """Returns (H, G, U): G = X W_gate + b_gate, U = X W_up + b_up, H = act(G) (.) U; G and U, which the backward call takes,
+    are None with ``save`` false."""
+    where = "tma_gated_dense_fwd"
+    dev = _device(where, X, W_gate, W_up, b_gate, b_up, G_out, U_out, H_out, ws)
+    n, F_in, ldx = _rows_ld(X, "X")
+    F_out = _weight_shape(where, "W_gate", W_gate, F_in)
+    dtype = _feat_dtype(X)
+    if not save:
+        G_out = U_out = None
+    elif G_out is None or U_out is None:
+        if G_out is not None or U_out is not None:
+            raise TmaError(f"{where}: G_out and U_out go together")
+        G_out, U_out = (_record(_padded(n, F_out, X.dtype, dev), stream) for _ in range(2))
+    if H_out is None:
+        H_out = _record(_padded(n, F_out, X.dtype, dev), stream)
+    _same_ld(G_out, U_out, f"{where}: G_out / U_out")
+    if ws is None:
+        ws = _workspace(tma_gated_dense_fwd_workspace_bytes(n, F_in, F_out, dtype), dev, stream)
+    G, ldg = _rows_or_none(G_out, "G_out", (n, F_out), X.dtype)
+    _launch(dev, stream, lib().tma_gated_dense_fwd, n, X.data_ptr(), _rows_like(X, "X", (n, F_in), X.dtype), F_in,
+            _vector(W_gate, "W_gate", (F_in, F_out), torch.float32), _vector(W_up, "W_up", (F_in, F_out), torch.float32),
+            _vector(b_gate, "b_gate", (F_out,), torch.float32), _vector(b_up, "b_up", (F_out,), torch.float32), F_out, act, dtype,
+            G, _rows_or_none(U_out, "U_out", (n, F_out), X.dtype)[0], ldg, H_out.data_ptr(),
+            _rows_like(H_out, "H_out", (n, F_out), X.dtype), *_room(ws))
+    return H_out, G_out, U_out
+
+
+def tma_gated_dense_bwd_workspace_bytes(n: int, F_in: int, F_out: int, dtype: int, need_dX: bool = True) -> int:
+    return int(lib().tma_gated_dense_bwd_workspace_bytes(n, F_in, F_out, dtype, 1 if need_dX else 0))
+
+
+def tma_gated_dense_bwd(X, G, U, dH, W_gate, W_up, act: int = TMA_ACT_SILU, R=None, dW_gate=None, dW_up=None, db_gate=None,
+                        db_up=None, dX_out=None, need_dbias=True, need_dX=True, ws=None, stream=None):
+    """Returns (dW_gate, dW_up, db_gate or None, db_up or None, dX or None); R, where given, is added to dX."""
+    where = "tma_gated_dense_bwd"
+    dev = _device(where, X, G, U, dH, W_gate, W_up, R, dW_gate, dW_up, db_gate, db_up, dX_out, ws)
+    n, F_in, _ = _rows_ld(X, "X")
+    F_out = _weight_shape(where, "W_gate", W_gate, F_in)
+    dtype = _feat_dtype(X)
+    _same_ld(G, U, f"{where}: G / U")
+    new = lambda shape: _record(torch.empty(shape, dtype=torch.float32, device=dev), stream)
+    dW_gate = new((F_in, F_out)) if dW_gate is None else dW_gate
+    dW_up = new((F_in, F_out)) if dW_up is None else dW_up
+    db_gate = None if not need_dbias else new((F_out,)) if db_gate is None else db_gate
+    db_up = None if not need_dbias else new((F_out,)) if db_up is None else db_up
+    dX_out = None if not need_dX else _record(_padded(n, F_in, X.dtype, dev), stream) if dX_out is None else dX_out
+    if ws is None:
+        ws = _workspace(tma_gated_dense_bwd_workspace_bytes(n, F_in, F_out, dtype, need_dX), dev, stream)
+    _rows_like(U, "U", (n, F_out), X.dtype)
+    _launch(dev, stream, lib().tma_gated_dense_bwd, n, X.data_ptr(), _rows_like(X, "X", (n, F_in), X.dtype), G.data_ptr(), U.data_ptr(),
+            _rows_like(G, "G", (n, F_out), X.dtype), dH.data_ptr(), _rows_like(dH, "dH", (n, F_out), X.dtype),
+            _vector(W_gate, "W_gate", (F_in, F_out), torch.float32), _vector(W_up, "W_up", (F_in, F_out), torch.float32), F_in, F_out,
+            act, dtype, _vector(dW_gate, "dW_gate", (F_in, F_out), torch.float32), _vector(dW_up, "dW_up", (F_in, F_out), torch.float32),
+            _vector(db_gate, "db_gate", (F_out,), torch.float32), _vector(db_up, "db_up", (F_out,), torch.float32),
+            *_rows_or_none(dX_out, "dX_out", (n, F_in), X.dtype), *_rows_or_none(R, "R", (n, F_in), X.dtype), *_room(ws))
+    return dW_gate, dW_up, db_gate, db_up, dX_out
+
+
+def tma_dense_residual_fwd_workspace_bytes(n: int, F_in: int, F_out: int, dtype: int) -> int:
+    return int(lib().tma_dense_residual_fwd_workspace_bytes(n, F_in, F_out, dtype))
+
+
+def tma_dense_residual_fwd(X, W, bias=None, act: int = TMA_ACT_NONE, R=None, save=False, Z_out=None, Y_out=None, ws=None,
+                           stream=None):
+    """Returns (Y, Z): Z = X W + bias, Y = act(Z) + R; Z, which the backward call takes with an activation, is None unless
+    ``save`` is true or Z_out given.  R may be Y_out."""
+    where = "tma_dense_residual_fwd"
+    dev = _device(where, X, W, bias, R, Z_out, Y_out, ws)
+    n, F_in, _ = _rows_ld(X, "X")
+    F_out = _weight_shape(where, "W", W, F_in)
+    dtype = _feat_dtype(X)
+    if save and Z_out is None:
+        Z_out = _record(_padded(n, F_out, X.dtype, dev), stream)
+    if Y_out is None:
+        Y_out = _record(_padded(n, F_out, X.dtype, dev), stream)
+    if ws is None:
+        ws = _workspace(tma_dense_residual_fwd_workspace_bytes(n, F_in, F_out, dtype), dev, stream)
+    _launch(dev, stream, lib().tma_dense_residual_fwd, n, X.data_ptr(), _rows_like(X, "X", (n, F_in), X.dtype), F_in,
+            _vector(W, "W", (F_in, F_out), torch.float32), _vector(bias, "bias", (F_out,), torch.float32), F_out, act, dtype,
+            *_rows_or_none(R, "R", (n, F_out), X.dtype), *_rows_or_none(Z_out, "Z_out", (n, F_out), X.dtype), Y_out.data_ptr(),
+            _rows_like(Y_out, "Y_out", (n, F_out), X.dtype), *_room(ws))
+    return Y_out, Z_out
+
+
+def tma_dense_residual_bwd_workspace_bytes(n: int, F_in: int, F_out: int, act: int, dtype: int, need_dX: bool = True) -> int:
+    return int(lib().tma_dense_residual_bwd_workspace_bytes(n, F_in, F_out, act, dtype, 1 if need_dX else 0))
+
+
+def tma_dense_residual_bwd(X, Z, dY, W, act: int = TMA_ACT_NONE, R=None, dW=None, dbias=None, dX_out=None, need_dbias=True,
+                           need_dX=True, ws=None, stream=None):
+    """Returns (dW, dbias or None, dX or None); Z may be None without an activation; R, where given, is added to dX."""
+    where = "tma_dense_residual_bwd"
+    dev = _device(where, X, Z, dY, W, R, dW, dbias, dX_out, ws)
+    n, F_in, _ = _rows_ld(X, "X")
+    F_out = _weight_shape(where, "W", W, F_in)
+    dtype = _feat_dtype(X)
+    if act == TMA_ACT_NONE:
+        Z = None
+    elif Z is None:
+        raise TmaError(f"{where}: Z is required with an activation")
+    new = lambda shape: _record(torch.empty(shape, dtype=torch.float32, device=dev), stream)
+    dW = new((F_in, F_out)) if dW is None else dW
+    dbias = None if not need_dbias else new((F_out,)) if dbias is None else dbias
+    dX_out = None if not need_dX else _record(_padded(n, F_in, X.dtype, dev), stream) if dX_out is None else dX_out
+    if ws is None:
+        ws = _workspace(tma_dense_residual_bwd_workspace_bytes(n, F_in, F_out, act, dtype, need_dX), dev, stream)
+    _launch(dev, stream, lib().tma_dense_residual_bwd, n, X.data_ptr(), _rows_like(X, "X", (n, F_in), X.dtype),
+            *_rows_or_none(Z, "Z", (n, F_out), X.dtype), dY.data_ptr(), _rows_like(dY, "dY", (n, F_out), X.dtype),
+            _vector(W, "W", (F_in, F_out), torch.float32), F_in, F_out, act, dtype, _vector(dW, "dW", (F_in, F_out), torch.float32),
+            _vector(dbias, "dbias", (F_out,), torch.float32), *_rows_or_none(dX_out, "dX_out", (n, F_in), X.dtype),
+            *_rows_or_none(R, "R", (n, F_in), X.dtype), *_room(ws))
+    return dW, dbias, dX_out
+
+
+def tma_grad_norm_workspace_bytes(n_tensors: int) -> int:
+    return int(lib().tma_grad_norm_workspace_bytes(n_tensors))
+
+
+def _grad_list(where, grads, out, norm_out, ws, stream):
+    """(device, number of tensors, their addresses and lengths as host arrays, type, norm_out, workspace)"""
+    if not grads:
+        raise TmaError(f"{where}: no gradients")
+    dev, kind = grads[0].device, grads[0].dtype
+    dtype = _feat_dtype(grads[0])
+    for t in grads:
+        if t.dtype != kind or t.device != dev or not t.is_contiguous():
+            raise TmaError(f"{where}: gradients must be contiguous tensors of one type on one device")
+    if out is not None:
+        if len(out) != len(grads):
+            raise TmaError(f"{where}: one result for each gradient")
+        for t, o in zip(grads, out):
+            if o.dtype != kind or o.device != dev or not o.is_contiguous() or o.numel() != t.numel():
+                raise TmaError(f"{where}: a result differs from its gradient in type, device or size")
+    if norm_out is None:
+        norm_out = _record(torch.empty(1, dtype=torch.float32, device=dev), stream)
+    _device(where, grads[0], norm_out, ws)
+    _vector(norm_out, "norm_out", (1,), torch.float32)
+    n = len(grads)
+    if ws is None:
+        ws = _workspace(tma_grad_norm_workspace_bytes(n), dev, stream)
+    return (dev, n, (C.c_void_p * n)(*[t.data_ptr() for t in grads]), (C.c_int64 * n)(*[t.numel() for t in grads]), dtype, norm_out, ws)
+
+
+def tma_grad_norm(grads, norm_out=None, ws=None, stream=None):
+    """The norm of all gradients together (a list of dense tensors of one type), [1] fp32 on their device."""
+    dev, n, ptrs, sizes, dtype, norm_out, ws = _grad_list("tma_grad_norm", grads, None, norm_out, ws, stream)
+    _launch(dev, stream, lib().tma_grad_norm, n, ptrs, sizes, dtype, norm_out.data_ptr(), *_room(ws))
+    return norm_out
+
+
+def tma_grad_clip(grads, max_norm: float, out=None, norm_out=None, ws=None, stream=None):
+    """Gradients whose norm together is above max_norm are scaled to it, in place or into the tensors of ``out``; returns the
+    norm before that, [1] fp32 on their device."""
+    dev, n, ptrs, sizes, dtype, norm_out, ws = _grad_list("tma_grad_clip", grads, out, norm_out, ws, stream)
+    outs = None if out is None else (C.c_void_p * n)(*[t.data_ptr() for t in out])
+    _launch(dev, stream, lib().tma_grad_clip, n, ptrs, outs, sizes, dtype, float(max_norm), norm_out.data_ptr(), *_room(ws))
+    return norm_out
 
 
 def tma_loss_workspace_bytes(n: int, Cc: int) -> int:

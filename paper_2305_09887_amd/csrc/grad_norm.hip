@@ -1,0 +1,261 @@
+// The global norm of a model's gradients, many tensors at once, and clipping by it:
+//     norm = sqrt(sum over all tensors of g^2),  out = g * c,  c = norm > max_norm ? max_norm / norm : 1.
+// A list of tensors goes to the kernels as their arguments, kListed at a time: no table in device memory, no copy of one, nothing that a captured graph
+// could find changed.  A tensor is cut into chunks, blocks take every grid-th chunk of the list and keep its squares' sum in 64 bits: the squares of
+// fp32 values are exact there and neither overflow nor vanish, and the vector units have the time (two instructions for four bytes).  Sums are joined in a
+// fixed order; clipping's second kernel does so in every block, and takes the chunks from the last to the first, since the last were just read and are in
+// the cache.  Bound by memory: a gradient is read once, and once more and written where it is clipped.
+#include "kernels.hpp"
+
+namespace tma {
+
+constexpr int kListed = 128, kChunk = 1 << 14, kNormBlocks = 2048, kNormThreads = 256;
+
+struct GradTensors {
+    const void *in[kListed];
+    int64_t size[kListed];
+    int first[kListed];        // chunks before it
+    int count, chunks;
+};
+struct GradOutputs {
+    void *out[kListed];
+};
+
+// the tensor that chunk c is of: the last that begins at or before it
+__device__ __forceinline__ int tensor_of(const GradTensors &q, int c)
+{
+    const int lane = threadIdx.x & 63;
+    const uint64_t low = __ballot(lane < q.count && q.first[lane] <= c), high = __ballot(lane + 64 < q.count && q.first[lane + 64] <= c);
+    return __popcll(low) + __popcll(high) - 1;
+}
+
+template <typename T>
+__device__ __forceinline__ void add_squares(const T *p, int64_t n, double (&sum)[4])
+{
+    constexpr int E = 16 / sizeof(T);
+    const int t = threadIdx.x;
+    int64_t head = (-reinterpret_cast<intptr_t>(p) & 15) / int64_t(sizeof(T));
+    head = head < n ? head : n;
+    auto one = [&](int64_t i) {
+        const double x = std::is_same<T, float>::value ? double(p[i]) : double(__uint_as_float(uint32_t(p[i]) << 16));
+        sum[0] = fma(x, x, sum[0]);
+    };
+    if (t < head) one(t);
+    const int64_t pieces = (n - head) / E, tail = head + pieces * E;
+    const uint4 *v = reinterpret_cast<const uint4 *>(p + head);
+    auto add = [&](const uint4 &w) {
+        float x[E];
+        Chunk<T>::widen(w, x);
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            const double d = x[j];
+            sum[j % 4] = fma(d, d, sum[j % 4]);
+        }
+    };
+    int64_t i = t;
+    for (; i + 3 * kNormThreads < pieces; i += 4 * kNormThreads) {
+        const uint4 a = v[i], b = v[i + kNormThreads], c = v[i + 2 * kNormThreads], d = v[i + 3 * kNormThreads];
+        add(a);
+        add(b);
+        add(c);
+        add(d);
+    }
+    for (; i < pieces; i += kNormThreads) add(v[i]);
+    if (tail + t < n) one(tail + t);
+}
+
+// the sum over the block's threads, in a fixed order; thread 0 has it
+__device__ __forceinline__ double block_sum(double s)
+{
+    __shared__ double waves[kNormThreads / kWave];
+    for (int d = kWave / 2; d; d >>= 1) s += __shfl_down(s, d, kWave);
+    if (threadIdx.x % kWave == 0) waves[threadIdx.x / kWave] = s;
+    __syncthreads();
+    return (waves[0] + waves[1]) + (waves[2] + waves[3]);
+}
+
+// partial[block] = its chunks' squares
+template <typename T>
+__global__ __launch_bounds__(kNormThreads) void grad_squares_kernel(GradTensors q, double *partial)
+{
+    double sum[4] = {0, 0, 0, 0};
+    for (int c = blockIdx.x; c < q.chunks; c += gridDim.x) {
+        const int i = __builtin_amdgcn_readfirstlane(tensor_of(q, c));
+        const int64_t at = int64_t(c - q.first[i]) * kChunk, left = q.size[i] - at;
+        add_squares(static_cast<const T *>(q.in[i]) + at, left < kChunk ? left : kChunk, sum);
+    }
+    const double all = block_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
+    if (threadIdx.x == 0) partial[blockIdx.x] = all;
+}
+
+__device__ __forceinline__ double norm_of(const double *partial, int count)
+{
+    double s = 0.0;
+    for (int i = threadIdx.x; i < count; i += kNormThreads) s += partial[i];
+    return sqrt(block_sum(s));
+}
+
+__global__ __launch_bounds__(kNormThreads) void grad_norm_kernel(const double *partial, int count, float *norm_out)
+{
+    const double norm = norm_of(partial, count);
+    if (threadIdx.x == 0) *norm_out = float(norm);
+}
+
+__device__ __forceinline__ void scale_piece(const float *in, float *out, float c)
+{
+    float v[4];
+    Chunk<float>::load(in, v);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] *= c;
+    Chunk<float>::store(out, v);
+}
+__device__ __forceinline__ void scale_piece(const uint16_t *in, uint16_t *out, float c)
+{
+    float v[8];
+    Chunk<uint16_t>::load(in, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] *= c;
+    Chunk<uint16_t>::store(out, v);
+}
+__device__ __forceinline__ void scale_one(const float *in, float *out, float c) { *out = *in * c; }
+__device__ __forceinline__ void scale_one(const uint16_t *in, uint16_t *out, float c) { *out = f32_to_bf16(bf16_to_f32(*in) * c); }
+
+// first: this launch writes norm_out.  Where the factor is 1 nothing is written in place.
+template <typename T>
+__global__ __launch_bounds__(kNormThreads) void grad_scale_kernel(GradTensors q, GradOutputs o, const double *partial, int count, double max_norm, bool first,
+                                                                  float *norm_out)
+{
+    constexpr int E = 16 / sizeof(T);
+    const double norm = norm_of(partial, count);
+    if (first && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = float(norm);
+    // (a norm that is NaN makes every gradient NaN)
+    const float factor = norm <= max_norm ? 1.0f : float(max_norm / norm);
+    const int t = threadIdx.x;
+    for (int b = blockIdx.x; b < q.chunks; b += gridDim.x) {
+        const int c = q.chunks - 1 - b;
+        const int i = __builtin_amdgcn_readfirstlane(tensor_of(q, c));
+        const int64_t at = int64_t(c - q.first[i]) * kChunk, left = q.size[i] - at, n = left < kChunk ? left : kChunk;
+        const T *in = static_cast<const T *>(q.in[i]) + at;
+        T *out = static_cast<T *>(o.out[i]) + at;
+        if (in == out && factor == 1.0f) continue;
+        int64_t head = 0, pieces = 0;
+        if (((reinterpret_cast<intptr_t>(in) ^ reinterpret_cast<intptr_t>(out)) & 15) == 0) {
+            head = (-reinterpret_cast<intptr_t>(in) & 15) / int64_t(sizeof(T));
+            head = head < n ? head : n;
+            pieces = (n - head) / E;
+        }
+        for (int64_t j = t; j < pieces; j += kNormThreads) scale_piece(in + head + j * E, out + head + j * E, factor);
+        for (int64_t j = t; j < n - pieces * E; j += kNormThreads) {
+            const int64_t k = j < head ? j : j + pieces * E;
+            scale_one(in + k, out + k, factor);
+        }
+    }
+}
+
+// the next of the list's tensors, from `begin` on, as arguments; empty ones are left out.  Returns where the rest begins.
+static int list_tensors(int begin, int n_tensors, const void *const *h_grads, void *const *h_outs, const int64_t *h_sizes, GradTensors &q, GradOutputs &o)
+{
+    q.count = q.chunks = 0;
+    int i = begin;
+    for (; i < n_tensors && q.count < kListed; ++i) {
+        if (h_sizes[i] == 0) continue;
+        const int64_t more = ceil_div(h_sizes[i], kChunk);
+        if (q.chunks + more > INT32_MAX / 2) break;     // (one tensor alone is below this: see the checks)
+        q.in[q.count] = h_grads[i];
+        o.out[q.count] = h_outs ? h_outs[i] : const_cast<void *>(h_grads[i]);
+        q.size[q.count] = h_sizes[i];
+        q.first[q.count] = q.chunks;
+        q.chunks += int(more);
+        ++q.count;
+    }
+    return i;
+}
+
+constexpr int kMaxLists = 1 << 10;     // of kListed tensors each, at least
+static size_t norm_workspace(int32_t n_tensors) { return round_up(size_t(ceil_div(n_tensors > 0 ? n_tensors : 1, kListed) + 1) * kNormBlocks * sizeof(double), 256); }
+
+template <typename T>
+static int grad_norm(const char *fn, int32_t n_tensors, const void *const *h_grads, void *const *h_outs, const int64_t *h_sizes, bool clip, double max_norm, float *norm_out,
+                     double *partial, size_t room, hipStream_t s)
+{
+    GradTensors q;
+    GradOutputs o;
+    int count = 0;
+    for (int at = 0; at < n_tensors;) {
+        at = list_tensors(at, n_tensors, h_grads, h_outs, h_sizes, q, o);
+        if (!q.count) break;
+        const int blocks = q.chunks < kNormBlocks ? q.chunks : kNormBlocks;
+        TMA_REQUIRE(size_t(count + blocks) * sizeof(double) <= room, TMA_ERR_WORKSPACE_TOO_SMALL, "%s: workspace for %d sums", fn, count + blocks);
+        TMA_TIMED(sizeof(T) == 2 ? "grad_squares_bf16" : "grad_squares", s);
+        hipLaunchKernelGGL(grad_squares_kernel<T>, dim3(unsigned(blocks)), dim3(kNormThreads), 0, s, q, partial + count);
+        if (int rc = check_launch(fn)) return rc;
+        count += blocks;
+    }
+    if (!clip || count == 0) {
+        TMA_TIMED("grad_norm", s);
+        hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(kNormThreads), 0, s, partial, count, norm_out);
+        return check_launch(fn);
+    }
+    bool first = true;
+    for (int at = 0; at < n_tensors;) {
+        at = list_tensors(at, n_tensors, h_grads, h_outs, h_sizes, q, o);
+        if (!q.count) break;
+        const int blocks = q.chunks < kNormBlocks ? q.chunks : kNormBlocks;
+        TMA_TIMED(sizeof(T) == 2 ? "grad_scale_bf16" : "grad_scale", s);
+        hipLaunchKernelGGL(grad_scale_kernel<T>, dim3(unsigned(blocks)), dim3(kNormThreads), 0, s, q, o, partial, count, max_norm, first, norm_out);
+        if (int rc = check_launch(fn)) return rc;
+        first = false;
+    }
+    return TMA_OK;
+}
+
+static int check_grads(const char *fn, int32_t n_tensors, const void *const *h_grads, const void *const *h_outs, const int64_t *h_sizes, int32_t dtype, const float *norm_out,
+                       const void *ws, size_t ws_bytes)
+{
+    TMA_REQUIRE(n_tensors >= 0 && n_tensors <= kMaxLists * kListed, TMA_ERR_INVALID_ARG, "%s: n_tensors=%d outside [0, %d]", fn, n_tensors, kMaxLists * kListed);
+    TMA_REQUIRE(dtype == TMA_F32 || dtype == TMA_BF16, TMA_ERR_UNSUPPORTED_DTYPE, "%s: dtype %d", fn, dtype);
+    TMA_REQUIRE(norm_out && (n_tensors == 0 || (h_grads && h_sizes)), TMA_ERR_INVALID_ARG, "%s: NULL argument", fn);
+    TMA_REQUIRE(ws && aligned(ws, 256), TMA_ERR_INVALID_ARG, "%s: workspace NULL or not 256-byte aligned", fn);
+    TMA_REQUIRE(ws_bytes >= norm_workspace(n_tensors), TMA_ERR_WORKSPACE_TOO_SMALL, "%s: workspace %zu < %zu", fn, ws_bytes, norm_workspace(n_tensors));
+    const size_t size = dtype == TMA_BF16 ? 2 : 4;
+    for (int i = 0; i < n_tensors; ++i) {
+        TMA_REQUIRE(h_sizes[i] >= 0 && h_sizes[i] < (int64_t(1) << 43), TMA_ERR_BAD_SHAPE, "%s: size of tensor %d", fn, i);
+        if (h_sizes[i] == 0) continue;
+        TMA_REQUIRE(h_grads[i] && aligned(h_grads[i], size) && (!h_outs || (h_outs[i] && aligned(h_outs[i], size))), TMA_ERR_INVALID_ARG,
+                    "%s: tensor %d is NULL or not aligned to its type", fn, i);
+    }
+    return TMA_OK;
+}
+
+}  // namespace tma
+
+extern "C" size_t tma_grad_norm_workspace_bytes(int32_t n_tensors)
+{
+    using namespace tma;
+    return n_tensors < 0 || n_tensors > kMaxLists * kListed ? 0 : norm_workspace(n_tensors);
+}
+
+extern "C" int tma_grad_norm(int32_t n_tensors, const void *const *h_grads, const int64_t *h_sizes, int32_t dtype, float *norm_out, void *ws, size_t ws_bytes,
+                             tma_stream_t stream)
+{
+    using namespace tma;
+    const char *fn = "tma_grad_norm";
+    if (int rc = check_grads(fn, n_tensors, h_grads, nullptr, h_sizes, dtype, norm_out, ws, ws_bytes)) return rc;
+    hipStream_t s = as_stream(stream);
+    double *partial = static_cast<double *>(ws);
+    return dtype == TMA_BF16 ? grad_norm<uint16_t>(fn, n_tensors, h_grads, nullptr, h_sizes, false, 0.0, norm_out, partial, ws_bytes, s)
+                             : grad_norm<float>(fn, n_tensors, h_grads, nullptr, h_sizes, false, 0.0, norm_out, partial, ws_bytes, s);
+}
+
+extern "C" int tma_grad_clip(int32_t n_tensors, const void *const *h_grads, void *const *h_outs, const int64_t *h_sizes, int32_t dtype, double max_norm, float *norm_out,
+                             void *ws, size_t ws_bytes, tma_stream_t stream)
+{
+    using namespace tma;
+    const char *fn = "tma_grad_clip";
+    if (int rc = check_grads(fn, n_tensors, h_grads, h_outs, h_sizes, dtype, norm_out, ws, ws_bytes)) return rc;
+    TMA_REQUIRE(max_norm >= 0.0, TMA_ERR_INVALID_ARG, "%s: max_norm below 0, or NaN", fn);
+    hipStream_t s = as_stream(stream);
+    double *partial = static_cast<double *>(ws);
+    return dtype == TMA_BF16 ? grad_norm<uint16_t>(fn, n_tensors, h_grads, h_outs, h_sizes, true, max_norm, norm_out, partial, ws_bytes, s)
+                             : grad_norm<float>(fn, n_tensors, h_grads, h_outs, h_sizes, true, max_norm, norm_out, partial, ws_bytes, s);
+}

@@ -1,0 +1,362 @@
+// Products of wide layers (gated_dense.hip, dense_residual.hip) on v_mfma_f32_32x32x16_bf16: both operands are laid out as fragments first, so that a product
+// has one form for every type, width, pitch, alignment and direction.
+//
+// Packed operands.  A unit is 1 KB: 32 rows of an operand by 16 k-values, 16 bytes a lane, in the order in which the matrix instruction wants them; what lies
+// outside the operand is zero.  Eight units of 256 rows follow each other, then those of the next k-values, of the next rows (a slab of a tile is one run of
+// memory; units of rows past the last are never written, and reach only results that are not stored), then planes: fp32 values are taken apart into bf16 parts whose sum
+// they are (three of them hold all 24 bits, two hold 17), one plane a part, and a product of such operands is the sum of products of planes, the small ones
+// first.  So an fp32 product is a bf16 product of six times the length (192 cycles of the matrix unit for 16 k-values, where the fp32 instruction takes
+// 512), and a weight gradient in fp32 from bf16 rows one of twice the length.
+//
+// A unit is what one wavefront fetches straight into LDS with one instruction and what it reads from there without conflicts: no swizzle, no edges, no
+// masks between memory and the matrix units.  The layout costs a pass over the operands, bytes against the product's rows times columns.
+//
+// The instruction multiplies weights (its rows) by rows (its columns): a lane ends with results of one row.  Which column a fragment's row is, is the layout's choice: fragment row
+// m holds column 16 (m / 4 mod 2) + 4 (m / 8) + m mod 4 of its 32, which makes a lane's sixteen results neighbours.
+#pragma once
+#include "kernels.hpp"
+#include "lds_fetch.hpp"
+
+namespace tma {
+
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kUnitRows = 32, kUnitK = 16, kUnitBytes = 1024;
+constexpr int kWideDies = 8;
+
+struct Packed {
+    char *at;
+    int rbs, kgs;              // units along the rows and along k (an even number: a slab is two)
+    __host__ __device__ __forceinline__ int64_t plane() const { return int64_t((rbs + 7) / 8) * kgs * (8 * kUnitBytes); }
+    __host__ __device__ __forceinline__ int64_t unit(int64_t rb, int64_t kg) const { return ((rb / 8 * kgs + kg) * 8 + rb % 8) * kUnitBytes; }
+    __host__ size_t bytes(int parts) const { return size_t(plane()) * size_t(parts); }
+};
+inline Packed packed_shape(int64_t rows, int64_t k)
+{
+    return Packed{nullptr, int(ceil_div(rows > 0 ? rows : 1, kUnitRows)), int(round_up(size_t(ceil_div(k > 0 ? k : 1, kUnitK)), 2))};
+}
+
+// the row of a unit in which column c (of 32) of the weights' side lies
+__host__ __device__ __forceinline__ int fragment_row(int c) { return ((c >> 4) & 1) * 4 + ((c >> 2) & 3) * 8 + (c & 3); }
+
+// ---- parts ---------------------------------------------------------------------
+// x as a sum of bf16 parts, each the rounding of what the ones before left over.  A finite value beyond the largest bf16 is cut instead of rounded; of an
+// infinity or a NaN the first part is that and the others are zero.  Parts below 2^-126 are lost: an error of 2^-126, whatever the value.
+template <int kParts>
+__device__ __forceinline__ void take_apart(float x, float (&part)[kParts])
+{
+#pragma unroll
+    for (int p = 0; p < kParts; ++p) {
+        float h = bf16_to_f32(f32_to_bf16(x));
+        if constexpr (kParts > 1) {
+            const bool beyond = (__float_as_uint(h) & 0x7F800000u) == 0x7F800000u;
+            if (beyond && (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u) h = __uint_as_float(__float_as_uint(x) & 0xFFFF0000u);
+            part[p] = h;
+            x = (__float_as_uint(x) & 0x7F800000u) == 0x7F800000u ? 0.0f : x - h;
+        } else {
+            part[p] = h;
+        }
+    }
+}
+
+// eight values of a row along k -> the lane's 16 bytes of each part
+template <int kParts>
+__device__ __forceinline__ void pack_eight(const float (&v)[8], uint4 (&out)[kParts])
+{
+    if constexpr (kParts == 1) {
+        out[0] = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+    } else {
+        uint32_t w[kParts][4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float a[kParts], b[kParts];
+            take_apart<kParts>(v[2 * j], a);
+            take_apart<kParts>(v[2 * j + 1], b);
+#pragma unroll
+            for (int p = 0; p < kParts; ++p) w[p][j] = (__float_as_uint(a[p]) >> 16) | (__float_as_uint(b[p]) & 0xFFFF0000u);
+        }
+#pragma unroll
+        for (int p = 0; p < kParts; ++p) out[p] = make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]);
+    }
+}
+
+__device__ __forceinline__ float widen1(float x) { return x; }
+__device__ __forceinline__ float widen1(uint16_t x) { return bf16_to_f32(x); }
+
+// eight neighbours of a row from column c on, zeros past `cols`; kWhole: rows begin at 16 bytes
+template <typename T>
+__device__ __forceinline__ void load_eight(const T *row, int64_t c, int64_t cols, bool whole, float (&v)[8])
+{
+    if (whole && c + 8 <= cols) {
+        if constexpr (sizeof(T) == 2) {
+            Chunk<uint16_t>::load(row + c, v);
+        } else {
+            const float4 a = *reinterpret_cast<const float4 *>(row + c), b = *reinterpret_cast<const float4 *>(row + c + 4);
+            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+            v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = c + j < cols ? widen1(row[c + j]) : 0.0f;
+    }
+}
+template <typename T>
+inline bool whole_rows(const T *p, int64_t ld) { return aligned(p, 16) && ld * int64_t(sizeof(T)) % 16 == 0; }
+
+// ---- layouts -------------------------------------------------------------------
+constexpr int kPackThreads = 256;
+
+// Operand rows are the rows of src [rows, cols], k along them.  A block takes 32 rows by 64 columns at a time, through LDS: 128 bytes of a row (bf16) are read
+// at once and four whole units written.
+// The operand may come from `sides` matrices side by side along k, side_kgs units each.  weights: its rows are a fragment's columns.
+struct RowsPack {
+    const void *src[2];
+    int64_t ld, rows, cols;
+    bool whole, weights;
+    int side_kgs;
+    Packed out;
+};
+template <typename T, int kParts>
+__global__ __launch_bounds__(kPackThreads) void pack_rows_kernel(RowsPack q)
+{
+    __shared__ __attribute__((aligned(16))) uint4 tile[kParts][kPackThreads];
+    const int t = threadIdx.x, r = t / 8, piece = t % 8;
+    const int quads = (q.out.kgs + 3) / 4;
+    const int64_t all = int64_t(q.out.rbs) * quads;
+    const int slot = (piece / 2) * 64 + (piece % 2) * 32 + (q.weights ? fragment_row(r) : r);
+    for (int64_t i = blockIdx.x; i < all; i += gridDim.x) {
+        const int64_t rb = i / quads, row = rb * kUnitRows + r;
+        const int kg0 = int(i % quads) * 4, kg = kg0 + piece / 2;
+        const int side = kg < q.side_kgs ? 0 : 1;
+        const int64_t c = int64_t(kg - side * q.side_kgs) * kUnitK + piece % 2 * 8;
+        float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (row < q.rows && kg < q.out.kgs) load_eight(static_cast<const T *>(q.src[side]) + row * q.ld, c, q.cols, q.whole, v);
+        uint4 parts[kParts];
+        pack_eight<kParts>(v, parts);
+        __syncthreads();
+#pragma unroll
+        for (int p = 0; p < kParts; ++p) tile[p][slot] = parts[p];
+        __syncthreads();
+        if (kg0 + t / 64 < q.out.kgs) {
+#pragma unroll
+            for (int p = 0; p < kParts; ++p)
+                *reinterpret_cast<uint4 *>(q.out.at + p * q.out.plane() + q.out.unit(rb, kg0 + t / 64) + t % 64 * 16) = tile[p][t];
+        }
+    }
+}
+
+// Operand rows are the columns of src [rows, cols], k along its rows: a thread takes eight rows of a column, 32 threads of a half wavefront write 512 bytes.
+// `sides` matrices give every other unit of 32 operand rows each (a gated layer's two weights).
+struct ColsPack {
+    const void *src[2];
+    int64_t ld, rows, cols;
+    int sides;
+    bool weights;
+    Packed out;
+};
+template <typename T, int kParts>
+__global__ __launch_bounds__(kPackThreads) void pack_cols_kernel(ColsPack q)
+{
+    const int t = threadIdx.x, c_in = t % 128, half = t / 128;
+    const int side_rbs = q.out.rbs / q.sides, strips = (side_rbs + 3) / 4;
+    const int64_t all = int64_t(strips) * q.out.kgs * q.sides;
+    const int slot = half * 32 + (q.weights ? fragment_row(c_in % 32) : c_in % 32);
+    for (int64_t i = blockIdx.x; i < all; i += gridDim.x) {
+        const int strip = int(i % strips), side = int(i / strips % q.sides);
+        const int64_t kg = i / strips / q.sides;
+        const int64_t col = int64_t(strip) * 128 + c_in, k0 = kg * kUnitK + half * 8;
+        const int rb = strip * 4 + c_in / 32;
+        if (rb >= side_rbs) continue;
+        const T *src = static_cast<const T *>(q.src[side]) + col;
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = col < q.cols && k0 + j < q.rows ? widen1(src[(k0 + j) * q.ld]) : 0.0f;
+        uint4 parts[kParts];
+        pack_eight<kParts>(v, parts);
+#pragma unroll
+        for (int p = 0; p < kParts; ++p)
+            *reinterpret_cast<uint4 *>(q.out.at + p * q.out.plane() + q.out.unit(rb * q.sides + side, kg) + slot * 16) = parts[p];
+    }
+}
+
+inline unsigned pack_blocks(int64_t items) { return unsigned(items < 1 ? 1 : items > 8192 ? 8192 : items); }
+
+template <typename T, int kParts>
+static void launch_pack_rows(const char *name, const void *first, const void *second, int64_t ld, int64_t rows, int64_t cols, bool weights, const Packed &out, hipStream_t s)
+{
+    const bool whole = whole_rows(static_cast<const T *>(first), ld) && (!second || whole_rows(static_cast<const T *>(second), ld));
+    const RowsPack q{{first, second}, ld, rows, cols, whole, weights, second ? out.kgs / 2 : out.kgs, out};
+    TMA_TIMED(name, s);
+    hipLaunchKernelGGL((pack_rows_kernel<T, kParts>), dim3(pack_blocks(int64_t(out.rbs) * ((out.kgs + 3) / 4))), dim3(kPackThreads), 0, s, q);
+}
+template <typename T, int kParts>
+static void launch_pack_cols(const char *name, const void *first, const void *second, int64_t ld, int64_t rows, int64_t cols, bool weights, const Packed &out, hipStream_t s)
+{
+    const int sides = second ? 2 : 1;
+    const ColsPack q{{first, second}, ld, rows, cols, sides, weights, out};
+    TMA_TIMED(name, s);
+    hipLaunchKernelGGL((pack_cols_kernel<T, kParts>), dim3(pack_blocks(int64_t((out.rbs / sides + 3) / 4) * out.kgs * sides)), dim3(kPackThreads), 0, s, q);
+}
+
+// ---- the product ---------------------------------------------------------------
+struct Planes {            // pairs of planes, four bits each, the first multiplied in the lowest
+    int count;
+    uint32_t a, b;
+};
+inline Planes planes_of(int a_parts, int b_parts)
+{
+    if (a_parts == 3) return {6, 0x001120u, 0x010102u};     // (2,0) (0,2) (1,1) (1,0) (0,1) (0,0)
+    if (b_parts == 2) return {2, 0x00u, 0x01u};             // (0,1) (0,0)
+    return {1, 0u, 0u};
+}
+
+// C[m][n] = sum over k of A[m][k] B[n][k]: A's rows are rows of the result, B's are the weights' side.
+struct WideCall {
+    Packed a, b;
+    Planes planes;
+    int m_tiles, n_tiles, panel;      // panel: column tiles that a die's blocks share rows of
+    int splits, split_slabs;          // ranges of k, of that many slabs
+    __host__ __device__ __forceinline__ int slabs_of(int split) const
+    {
+        const int left = a.kgs / 2 - split * split_slabs;
+        return left < split_slabs ? left : split_slabs;
+    }
+};
+struct WideTile {
+    int m, n, split;
+};
+__device__ __forceinline__ WideTile wide_tile(const WideCall &q, int64_t work)
+{
+    const int tiles = q.m_tiles * q.n_tiles, t = int(work % tiles);
+    const int per_panel = q.panel * q.m_tiles, p = t / per_panel, in = t % per_panel;
+    const int width = (p + 1) * q.panel <= q.n_tiles ? q.panel : q.n_tiles - p * q.panel;
+    return {in / width, p * q.panel + in % width, int(work / tiles)};
+}
+
+constexpr int kWideStages = 4;
+
+// MF x NF units a tile, WM x WN wavefronts.  A ring of slabs of 32 k-values, fetched three ahead through tile boundaries; the fragments of 16 k-values are read
+// while those before are multiplied, so that one wavefront a SIMD keeps its matrix unit busy.
+template <int MF, int NF, int WM, int WN, class Epi>
+__global__ __launch_bounds__(WM *WN * 64, 1) void wide_gemm_kernel(WideCall q, Epi epi)
+{
+    constexpr int kWaves = WM * WN, TM = MF / WM, TN = NF / WN, kUnits = (MF + NF) * 2, kLoads = kUnits / kWaves, kAhead = kWideStages - 1;
+    constexpr int kYoung = (kAhead - 1) * kLoads;
+    constexpr int kYoungStores = kYoung + TM * TN * Epi::kStores < 63 ? kYoung + TM * TN * Epi::kStores : 63;
+    static_assert(MF % WM == 0 && NF % WN == 0 && kUnits % kWaves == 0 && MF % kLoads == 0 && NF % kLoads == 0 && 8 % MF == 0 && 8 % NF == 0 && kYoung <= 63 && TN % Epi::kSides == 0, "tile shape");
+    __shared__ __attribute__((aligned(1024))) uint4 ring[kWideStages][kUnits][64];
+
+    const int lane = threadIdx.x & 63, l31 = lane & 31, hi = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / WN, wn = wave % WN;
+
+    const int64_t total = int64_t(q.m_tiles) * q.n_tiles * q.splits;
+    const int64_t per_die = (total + kWideDies - 1) / kWideDies, die = blockIdx.x % kWideDies, stride = gridDim.x / kWideDies;
+    const int64_t end = (die + 1) * per_die < total ? (die + 1) * per_die : total;
+    int64_t work = die * per_die + blockIdx.x / kWideDies;
+    if (work >= end) return;
+
+    // ---- the cursor: the slab that is fetched next
+    const uint32_t ring0 = lds_address(&ring[0][0][0]), lane_at = uint32_t(lane) * 16u;
+    int64_t c_work = work;
+    int c_left = 0, c_pair = 0, c_stage = 0;
+    bool c_open = true;
+    // this wavefront's units of a slab: kLoads neighbours of one operand and one of its two k-units
+    const int u0 = wave * kLoads;
+    const bool rows_side = u0 < 2 * MF;
+    const int in_side = rows_side ? u0 : u0 - 2 * MF, k_unit = in_side / (rows_side ? MF : NF), rb_in = in_side % (rows_side ? MF : NF);
+    const char *from = nullptr;
+    auto fetch_next = [&]() {
+        if (!c_open) return;
+        if (c_left == 0) {
+            const WideTile tile = wide_tile(q, c_work);
+            const int rb = (rows_side ? tile.m * MF : tile.n * NF) + rb_in, pair = 4 * c_pair;
+            const Packed &o = rows_side ? q.a : q.b;
+            from = o.at + (((rows_side ? q.planes.a : q.planes.b) >> pair) & 15u) * o.plane() + o.unit(rb, int64_t(tile.split) * q.split_slabs * 2 + k_unit);
+            c_left = q.slabs_of(tile.split);
+        }
+        const uint32_t to = ring0 + uint32_t(c_stage) * uint32_t(kUnits * kUnitBytes) + uint32_t(u0) * uint32_t(kUnitBytes);
+#pragma unroll
+        for (int v = 0; v < kLoads; ++v) lds_fetch<4>(to + uint32_t(v) * uint32_t(kUnitBytes), reinterpret_cast<const float *>(from), lane_at + uint32_t(v) * uint32_t(kUnitBytes));
+        from += 16 * kUnitBytes;
+        c_stage = c_stage == kWideStages - 1 ? 0 : c_stage + 1;
+        if (--c_left == 0 && ++c_pair == q.planes.count) {
+            c_pair = 0;
+            c_work += stride;
+            c_open = c_work < end;
+        }
+    };
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s) fetch_next();
+
+    uint4 xa[2][TM], xb[2][TN];
+    auto read = [&](int stage, int g, uint4 (&a)[TM], uint4 (&b)[TN]) {
+        const uint4 *base = &ring[stage][0][lane];
+#pragma unroll
+        for (int i = 0; i < TM; ++i) a[i] = base[(g * MF + wm * TM + i) * 64];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) b[j] = base[(2 * MF + g * NF + wn * TN + j) * 64];
+    };
+    int stage = 0, storing = 0;
+    if (c_open) wait_and_meet<kYoung>();
+    else wait_and_meet<0>();
+    fetch_next();
+    read(0, 0, xa[0], xb[0]);
+    for (;;) {
+        const WideTile tile = wide_tile(q, work);
+        const int slabs = q.slabs_of(tile.split) * q.planes.count;
+        const bool last = work + stride >= end;
+        floatx16 acc[TN][TM];
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[j][i][r] = 0.0f;
+        auto multiply = [&](const uint4 (&a)[TM], const uint4 (&b)[TN]) {
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+                    acc[j][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, b[j]), __builtin_bit_cast(bf16x8, a[i]), acc[j][i], 0, 0, 0);
+        };
+        for (int s = 0; s < slabs; ++s) {
+            read(stage, 1, xa[1], xb[1]);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(xa[0], xb[0]);
+            __builtin_amdgcn_sched_barrier(0);
+            stage = stage == kWideStages - 1 ? 0 : stage + 1;
+            if (!(last && s + 1 == slabs)) {
+                // the next slab is there, and all have read this one, whose place the fetch takes
+                if (!c_open) wait_and_meet<0>();
+                else if (storing > 0) wait_and_meet<kYoungStores>();
+                else wait_and_meet<kYoung>();
+                --storing;
+                fetch_next();
+                read(stage, 0, xa[0], xb[0]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(xa[1], xb[1]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        constexpr int S = Epi::kSides;
+#pragma unroll
+        for (int j = 0; j < TN; j += S) {
+            const int col = ((tile.n * NF + wn * TN + j) / S) * 32 + hi * 16;
+            typename Epi::Cols cols;
+            epi.columns(col, cols);
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                epi.store(int64_t(tile.m) * (MF * 32) + (wm * TM + i) * 32 + l31, col, tile.split, cols, acc[j][i], acc[j + S - 1][i]);
+                __builtin_amdgcn_sched_barrier(0);      // (several at once would not fit the registers)
+            }
+        }
+        const bool whole = epi.whole(int64_t(tile.m) * (MF * 32) + MF * 32, (tile.n + 1) * NF / S * 32);
+        storing = whole ? kAhead : 0;     // (fewer stores may not be counted on)
+        work += stride;
+        if (last) break;
+    }
+}
+
+}  // namespace tma

@@ -1,0 +1,494 @@
+// What the gated layers and the dense layers with a residual share beside their products (wide_gemm.hpp): activations, what becomes of a product, the
+// gradients of the pre-activations, and the host's plans.
+#pragma once
+#include "wide_gemm.hpp"
+
+namespace tma {
+
+// ---- activations ---------------------------------------------------------------
+// silu z = z s(z), s = 1 / (1 + e^-z); gelu z = z Phi(z), Phi(z) = erfc(-z / sqrt 2) / 2 (not 1 + erf, whose sum loses what is left of a small Phi).
+__device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
+__device__ __forceinline__ float normal_below(float z) { return 0.5f * erfcf(z * -0.70710678f); }
+
+template <int N>
+__device__ __forceinline__ void activate(int act, float (&v)[N])
+{
+    if (act == TMA_ACT_SILU) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] *= logistic(v[j]);
+    } else if (act == TMA_ACT_GELU) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] *= normal_below(v[j]);
+    } else if (act == TMA_ACT_RELU) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = v[j] > 0.0f ? v[j] : 0.0f;
+    }
+}
+// act(z) and act'(z)
+template <int N>
+__device__ __forceinline__ void activate_both(int act, const float (&z)[N], float (&value)[N], float (&slope)[N])
+{
+    if (act == TMA_ACT_SILU) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const float t = logistic(z[j]);
+            value[j] = z[j] * t;
+            slope[j] = t * (1.0f + z[j] * (1.0f - t));
+        }
+    } else if (act == TMA_ACT_GELU) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const float p = normal_below(z[j]);
+            value[j] = z[j] * p;
+            slope[j] = p + z[j] * (0.39894228f * __expf(-0.5f * z[j] * z[j]));
+        }
+    } else if (act == TMA_ACT_RELU) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            value[j] = z[j] > 0.0f ? z[j] : 0.0f;
+            slope[j] = z[j] > 0.0f ? 1.0f : 0.0f;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            value[j] = z[j];
+            slope[j] = 1.0f;
+        }
+    }
+}
+
+// ---- rows of results -----------------------------------------------------------
+// sixteen neighbours of a row, of which those before `cols` exist; whole: rows begin at 16 bytes
+__device__ __forceinline__ void store_sixteen(float *row, int c, int cols, bool whole, const float (&v)[16])
+{
+    if (whole && c + 16 <= cols) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) reinterpret_cast<float4 *>(row + c)[j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            if (c + j < cols) row[c + j] = v[j];
+    }
+}
+__device__ __forceinline__ void store_sixteen(uint16_t *row, int c, int cols, bool whole, const float (&v)[16])
+{
+    if (whole && c + 16 <= cols) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            reinterpret_cast<uint4 *>(row + c)[j] = make_uint4(pack_bf16(v[8 * j], v[8 * j + 1]), pack_bf16(v[8 * j + 2], v[8 * j + 3]),
+                                                               pack_bf16(v[8 * j + 4], v[8 * j + 5]), pack_bf16(v[8 * j + 6], v[8 * j + 7]));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            if (c + j < cols) row[c + j] = f32_to_bf16(v[j]);
+    }
+}
+template <typename T>
+__device__ __forceinline__ void load_sixteen(const T *row, int c, int cols, bool whole, float (&v)[16])
+{
+    float a[8], b[8];
+    load_eight(row, c, cols, whole, a);
+    load_eight(row, c + 8, cols, whole, b);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        v[j] = a[j];
+        v[8 + j] = b[j];
+    }
+}
+struct Bias16 {
+    float v[16];
+    __device__ __forceinline__ void load(const float *bias, int c, int cols)
+    {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) v[j] = bias && c + j < cols ? bias[c + j] : 0.0f;
+    }
+};
+
+// ---- what becomes of a product -------------------------------------------------
+// H = act(G) (.) U of two results in one lane, G and U kept where asked for
+template <typename T>
+struct GatedEpilogue {
+    static constexpr int kSides = 2, kStores = sizeof(T) == 2 ? 1 : 2;
+    T *G, *U, *H;                 // G, U: NULL together
+    int64_t ldg, ldh, M;
+    const float *b_gate, *b_up;   // may be NULL
+    int N, act;
+    bool wg, wh;                  // rows of G and U, of H, begin at 16 bytes
+    struct Cols {
+        Bias16 g, u;
+    };
+    __device__ __forceinline__ void columns(int c, Cols &k) const
+    {
+        k.g.load(b_gate, c, N);
+        k.u.load(b_up, c, N);
+    }
+    __device__ __forceinline__ void store(int64_t row, int c, int, const Cols &k, const floatx16 &g, const floatx16 &u) const
+    {
+        if (row >= M || c >= N) return;
+        float a[16], b[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            a[j] = g[j] + k.g.v[j];
+            b[j] = u[j] + k.u.v[j];
+        }
+        if (G) {
+            store_sixteen(G + row * ldg, c, N, wg, a);
+            store_sixteen(U + row * ldg, c, N, wg, b);
+        }
+        activate(act, a);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) a[j] *= b[j];
+        store_sixteen(H + row * ldh, c, N, wh, a);
+    }
+    __device__ __forceinline__ bool whole(int64_t m_end, int n_end) const { return wh && m_end <= M && n_end <= N; }
+};
+
+// Y = act(Z) + R, Z = product + bias kept where asked for
+template <typename T>
+struct ResidualEpilogue {
+    static constexpr int kSides = 1, kStores = sizeof(T) == 2 ? 2 : 4;
+    T *Z, *Y;                     // Z may be NULL
+    const T *R;                   // may be NULL, may be Y
+    int64_t ldz, ldy, ldr, M;
+    const float *bias;            // may be NULL
+    int N, act;
+    bool wz, wy, wr;
+    typedef Bias16 Cols;
+    __device__ __forceinline__ void columns(int c, Cols &k) const { k.load(bias, c, N); }
+    __device__ __forceinline__ void store(int64_t row, int c, int, const Cols &k, const floatx16 &z, const floatx16 &) const
+    {
+        if (row >= M || c >= N) return;
+        float a[16], past[16];
+        if (R) load_sixteen(R + row * ldr, c, N, wr, past);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) a[j] = z[j] + k.v[j];
+        if (Z) store_sixteen(Z + row * ldz, c, N, wz, a);
+        activate(act, a);
+        if (R) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) a[j] += past[j];
+        }
+        store_sixteen(Y + row * ldy, c, N, wy, a);
+    }
+    __device__ __forceinline__ bool whole(int64_t m_end, int n_end) const { return wy && m_end <= M && n_end <= N; }
+};
+
+// a weight gradient, or a range's share of it: the columns of `sides` matrices behind each other, each padded to whole units
+struct WeightEpilogue {
+    static constexpr int kSides = 1, kStores = 4;
+    float *out[2];
+    int64_t split_stride, M;
+    int N, padded, sides;
+    bool w;
+    struct Cols {};
+    __device__ __forceinline__ void columns(int, Cols &) const {}
+    __device__ __forceinline__ void store(int64_t row, int c, int split, const Cols &, const floatx16 &v, const floatx16 &) const
+    {
+        const int side = sides == 2 && c >= padded ? 1 : 0, cc = c - side * padded;     // (tiles may reach past the last side)
+        if (row >= M || cc >= N) return;
+        float a[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) a[j] = v[j];
+        store_sixteen(out[side] + split * split_stride + row * N, cc, N, w, a);
+    }
+    __device__ __forceinline__ bool whole(int64_t m_end, int n_end) const { return w && m_end <= M && N == padded && n_end <= sides * padded; }
+};
+
+// ---- gradients of pre-activations ----------------------------------------------
+// Gated: dG = dH U act'(G), dU = dH act(G).  One-sided: dZ = dY act'(Z).  Computed once, in fp32, and laid out for both products that take them: with the
+// rows along the result's rows (dX = [dG | dU] [W_gate | W_up]^T, one part of bf16 rows' gradients: the result is rounded to as much) and with the rows
+// along k (dW = X^T [dG | dU], two parts of them: dW is fp32).  The columns' sums go along: a block keeps them over its rows.
+template <typename T>
+struct GradCall {
+    const T *Z, *U, *dY;          // Z: the gate's pre-activations; Z may be NULL without an activation
+    int64_t ldz, ldy, n;
+    int N, act;
+    bool wz, wy;
+    Packed by_rows, by_cols;      // by_rows.at may be NULL
+    float *sums;                  // [blocks along the rows][sides * padded], or NULL
+    int row_blocks;
+};
+template <typename T, int kSides, int kPartsR, int kPartsC>
+__global__ __launch_bounds__(256) void grad_pack_kernel(GradCall<T> q)
+{
+    __shared__ float tile[kSides][32][65];
+    __shared__ float joined[kSides][4][64];
+    const int t = threadIdx.x, r = t / 8, piece = t % 8, col_in = t % 64, quarter = t / 64;
+    const int strips = (q.N + 63) / 64, strip = int(blockIdx.x) % strips, rows_at = int(blockIdx.x) / strips;
+    const int c0 = strip * 64, padded = (q.N + 31) / 32 * 32, c = c0 + piece * 8;
+    const int64_t tiles = (q.n + 31) / 32;
+    float sum[kSides] = {};
+    for (int64_t i = rows_at; i < tiles; i += q.row_blocks) {
+        const int64_t row = i * 32 + r;
+        float d[kSides][8] = {};
+        if (row < q.n && c < q.N) {
+            float dy[8];
+            load_eight(q.dY + row * q.ldy, c, q.N, q.wy, dy);
+            if constexpr (kSides == 1) {
+                float z[8], value[8], slope[8];
+                if (q.act != TMA_ACT_NONE) load_eight(q.Z + row * q.ldz, c, q.N, q.wz, z);
+                else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) z[j] = 0.0f;
+                }
+                activate_both(q.act, z, value, slope);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) d[0][j] = q.act == TMA_ACT_NONE ? dy[j] : dy[j] * slope[j];
+            } else {
+                float g[8], u[8], value[8], slope[8];
+                load_eight(q.Z + row * q.ldz, c, q.N, q.wz, g);
+                load_eight(q.U + row * q.ldz, c, q.N, q.wz, u);
+                activate_both(q.act, g, value, slope);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    d[0][j] = dy[j] * u[j] * slope[j];
+                    d[kSides - 1][j] = dy[j] * value[j];
+                }
+            }
+        }
+        if (q.by_rows.at && c < padded) {
+#pragma unroll
+            for (int side = 0; side < kSides; ++side) {
+                uint4 parts[kPartsR];
+                pack_eight<kPartsR>(d[side], parts);
+                const int kg = side * (padded / kUnitK) + c / kUnitK;
+#pragma unroll
+                for (int p = 0; p < kPartsR; ++p)
+                    *reinterpret_cast<uint4 *>(q.by_rows.at + p * q.by_rows.plane() + q.by_rows.unit(i, kg) + (piece % 2 * 32 + r) * 16) = parts[p];
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int side = 0; side < kSides; ++side)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) tile[side][r][piece * 8 + j] = d[side][j];
+        __syncthreads();
+        if (c0 + col_in < padded) {
+#pragma unroll
+            for (int side = 0; side < kSides; ++side) {
+                float v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = tile[side][quarter * 8 + j][col_in];
+                uint4 parts[kPartsC];
+                pack_eight<kPartsC>(v, parts);
+                const int64_t rb = side * (padded / kUnitRows) + (c0 + col_in) / kUnitRows, kg = i * 2 + quarter / 2;
+                const int slot = quarter % 2 * 32 + fragment_row(col_in % 32);
+#pragma unroll
+                for (int p = 0; p < kPartsC; ++p)
+                    *reinterpret_cast<uint4 *>(q.by_cols.at + p * q.by_cols.plane() + q.by_cols.unit(rb, kg) + slot * 16) = parts[p];
+                sum[side] += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+            }
+        }
+    }
+    if (!q.sums) return;
+#pragma unroll
+    for (int side = 0; side < kSides; ++side) joined[side][quarter][col_in] = sum[side];
+    __syncthreads();
+    if (t < 64 && c0 + t < padded) {
+#pragma unroll
+        for (int side = 0; side < kSides; ++side)
+            q.sums[(int64_t(rows_at) * kSides + side) * padded + c0 + t] = (joined[side][0][t] + joined[side][1][t]) + (joined[side][2][t] + joined[side][3][t]);
+    }
+}
+
+// out[side][i] = the ranges' shares added up in their order
+static __global__ __launch_bounds__(256) void join_ranges_kernel(const float *__restrict__ partial, int ranges, int64_t range_stride, int64_t side_stride, int64_t count,
+                                                          float *first, float *second)
+{
+    float *out = blockIdx.y ? second : first;
+    const float *in = partial + blockIdx.y * side_stride;
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < count; i += int64_t(gridDim.x) * 256) {
+        float sum = 0.0f;
+#pragma unroll 4
+        for (int p = 0; p < ranges; ++p) sum += in[p * range_stride + i];
+        out[i] = sum;
+    }
+}
+static void launch_join(const char *name, const float *partial, int ranges, int64_t range_stride, int64_t side_stride, int64_t count, float *first, float *second, hipStream_t s)
+{
+    TMA_TIMED(name, s);
+    int64_t blocks = ceil_div(count, 256);
+    if (blocks > 4096) blocks = 4096;
+    hipLaunchKernelGGL(join_ranges_kernel, dim3(unsigned(blocks < 1 ? 1 : blocks), second ? 2 : 1), dim3(256), 0, s, partial, ranges, range_stride, side_stride, count, first, second);
+}
+
+// ---- plans ---------------------------------------------------------------------
+constexpr int kCus = 256;
+struct WidePlan {
+    bool big;                     // tiles of 256 x 256 results, else of 128 x 128
+    int splits, split_slabs;
+};
+inline int64_t wide_tiles(int m_units, int n_units, bool big) { return ceil_div(m_units, big ? 8 : 4) * ceil_div(n_units, big ? 8 : 4); }
+// one range of k: results go through an epilogue
+inline WidePlan plan_rows(const Packed &a, const Packed &b)
+{
+    return {wide_tiles(a.rbs, b.rbs, true) >= kCus * 3 / 4, 1, a.kgs / 2};
+}
+// ranges of k until the tiles fill the chip, 512 rows each at least
+inline WidePlan plan_weight(const Packed &a, const Packed &b)
+{
+    const int slabs = a.kgs / 2, most = slabs / 16 > 1 ? slabs / 16 : 1;
+    for (bool big : {true, false}) {
+        const int64_t tiles = wide_tiles(a.rbs, b.rbs, big), slots = big ? kCus : 2 * kCus;
+        int64_t want = slots / tiles;
+        want = want < 1 ? 1 : want > most ? most : want;
+        if (big && tiles * want < kCus / 2) continue;
+        const int per = int(ceil_div(slabs, want));
+        return {big, int(ceil_div(slabs, per)), per};
+    }
+    return {false, 1, slabs};
+}
+
+template <class Epi>
+static int launch_wide(const char *name, const Packed &a, const Packed &b, const Planes &planes, const WidePlan &p, const Epi &e, hipStream_t s)
+{
+    WideCall q{a, b, planes, 0, 0, 8, p.splits, p.split_slabs};
+    const int units = p.big ? 8 : 4, per_cu = p.big ? 1 : 2;
+    q.m_tiles = int(ceil_div(a.rbs, units));
+    q.n_tiles = int(ceil_div(b.rbs, units));
+    if (q.panel > q.n_tiles) q.panel = q.n_tiles;
+    const int64_t total = int64_t(q.m_tiles) * q.n_tiles * q.splits;
+    int64_t per_die = ceil_div(total, kWideDies);
+    if (per_die > 32 * per_cu) per_die = 32 * per_cu;
+    TMA_TIMED(name, s);
+    const dim3 grid(unsigned(per_die * kWideDies)), block(256);
+    if (p.big) hipLaunchKernelGGL((wide_gemm_kernel<8, 8, 2, 2, Epi>), grid, block, 0, s, q, e);
+    else hipLaunchKernelGGL((wide_gemm_kernel<4, 4, 2, 2, Epi>), grid, block, 0, s, q, e);
+    return check_launch(name);
+}
+
+template <typename T>
+constexpr int kPartsOf = sizeof(T) == 2 ? 1 : 3;
+
+// the workspace, cut piece by piece
+struct Cutter {
+    char *at;
+    size_t used = 0;
+    void *take(size_t bytes)
+    {
+        void *p = at ? at + used : nullptr;
+        used += round_up(bytes, 256);
+        return p;
+    }
+    void take(Packed &p, int parts) { p.at = static_cast<char *>(take(p.bytes(parts))); }
+};
+
+// forward: rows and weights laid out
+struct ForwardPlan {
+    Packed a, b;
+    size_t bytes;
+};
+template <typename T>
+inline ForwardPlan plan_forward(int64_t n, int32_t F_in, int32_t F_out, int sides, void *ws)
+{
+    ForwardPlan p;
+    p.a = packed_shape(n, F_in);
+    p.b = packed_shape(F_out, F_in);
+    p.b.rbs *= sides;
+    Cutter cut{static_cast<char *>(ws)};
+    cut.take(p.a, kPartsOf<T>);
+    cut.take(p.b, kPartsOf<T>);
+    p.bytes = cut.used;
+    return p;
+}
+
+struct BackwardPlan {
+    Packed d_rows, d_cols, x_cols, w_rows;
+    int padded, row_blocks, parts_c;
+    WidePlan weight;
+    float *sums, *partial;
+    size_t bytes;
+};
+// exact: the gradients of the pre-activations are bf16 as they come (no activation on bf16 rows)
+template <typename T>
+inline BackwardPlan plan_backward(int64_t n, int32_t F_in, int32_t F_out, int sides, bool exact, bool need_dX, void *ws)
+{
+    BackwardPlan p;
+    p.padded = int(round_up(size_t(F_out), 32));
+    p.parts_c = sizeof(T) == 4 ? 3 : exact ? 1 : 2;
+    p.d_rows = packed_shape(n, int64_t(sides) * p.padded);
+    p.d_cols = packed_shape(int64_t(sides) * p.padded, n);
+    p.x_cols = packed_shape(F_in, n);
+    p.w_rows = packed_shape(F_in, int64_t(sides) * p.padded);
+    p.weight = plan_weight(p.x_cols, p.d_cols);
+    const int strips = int(ceil_div(F_out, 64));
+    int64_t blocks = ceil_div(4096, strips);
+    if (blocks > ceil_div(n > 0 ? n : 1, 32)) blocks = ceil_div(n > 0 ? n : 1, 32);
+    p.row_blocks = int(blocks);
+    Cutter cut{static_cast<char *>(ws)};
+    cut.take(p.d_cols, p.parts_c);
+    cut.take(p.x_cols, kPartsOf<T>);
+    p.sums = static_cast<float *>(cut.take(size_t(p.row_blocks) * size_t(sides) * size_t(p.padded) * 4));
+    p.partial = p.weight.splits > 1 ? static_cast<float *>(cut.take(size_t(p.weight.splits) * size_t(sides) * size_t(F_in) * size_t(F_out) * 4)) : nullptr;
+    if (need_dX) {
+        cut.take(p.d_rows, kPartsOf<T>);
+        cut.take(p.w_rows, kPartsOf<T>);
+    } else {
+        p.d_rows.at = nullptr;
+    }
+    p.bytes = cut.used;
+    return p;
+}
+
+// dW, db of one matrix or two, and dX + R
+template <typename T, int kSides>
+static int wide_backward(const char *fn, const char *what, int64_t n, const T *X, int64_t ldx, GradCall<T> g, const float *const (&W)[2], int32_t F_in, float *const (&dW)[2],
+                         float *const (&db)[2], T *dX, int64_t ld_dx, const T *R, int64_t ldr, void *ws, hipStream_t s)
+{
+    const int32_t N = g.N;
+    if (n == 0) {      // (no ranges: zeros)
+        launch_join("wide_join", nullptr, 0, 0, 0, int64_t(F_in) * N, dW[0], kSides == 2 ? dW[1] : nullptr, s);
+        if (db[0]) launch_join("wide_join_sums", nullptr, 0, 0, 0, N, db[0], kSides == 2 ? db[1] : nullptr, s);
+        return check_launch(fn);
+    }
+    const bool exact = kSides == 1 && g.act == TMA_ACT_NONE;
+    const BackwardPlan p = plan_backward<T>(n, F_in, N, kSides, exact, dX != nullptr, ws);
+    constexpr int kP = kPartsOf<T>;
+    g.by_rows = p.d_rows;
+    g.by_cols = p.d_cols;
+    g.sums = db[0] ? p.sums : nullptr;
+    g.row_blocks = p.row_blocks;
+    {
+        TMA_TIMED("wide_grad_pack", s);
+        const dim3 grid(unsigned(ceil_div(N, 64) * p.row_blocks)), block(256);
+        if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((grad_pack_kernel<T, kSides, 3, 3>), grid, block, 0, s, g);
+        else if constexpr (kSides == 2) hipLaunchKernelGGL((grad_pack_kernel<T, kSides, 1, 2>), grid, block, 0, s, g);
+        else if (exact) hipLaunchKernelGGL((grad_pack_kernel<T, kSides, 1, 1>), grid, block, 0, s, g);
+        else hipLaunchKernelGGL((grad_pack_kernel<T, kSides, 1, 2>), grid, block, 0, s, g);
+        if (int rc = check_launch(fn)) return rc;
+    }
+    launch_pack_cols<T, kP>("wide_pack_cols", X, nullptr, ldx, n, F_in, false, p.x_cols, s);
+    if (int rc = check_launch(fn)) return rc;
+    const int64_t cells = int64_t(F_in) * N;
+    const bool split = p.weight.splits > 1;
+    WeightEpilogue we{{split ? p.partial : dW[0], split ? p.partial + cells : dW[1]}, cells * kSides, F_in, N, p.padded, kSides, false};
+    we.w = N % 4 == 0 && aligned(we.out[0], 16) && (kSides == 1 || aligned(we.out[1], 16));
+    char name[64];
+    snprintf(name, sizeof(name), "%s_bwd_weight%s", what, sizeof(T) == 2 ? "_bf16" : "");
+    if (int rc = launch_wide(name, p.x_cols, p.d_cols, planes_of(kP, p.parts_c), p.weight, we, s)) return rc;
+    if (split) launch_join("wide_join", p.partial, p.weight.splits, cells * kSides, cells, cells, dW[0], kSides == 2 ? dW[1] : nullptr, s);
+    if (db[0]) launch_join("wide_join_sums", p.sums, p.row_blocks, int64_t(kSides) * p.padded, p.padded, N, db[0], kSides == 2 ? db[1] : nullptr, s);
+    if (int rc = check_launch(fn)) return rc;
+    if (!dX) return TMA_OK;
+    launch_pack_rows<float, kP>("wide_pack_rows", W[0], kSides == 2 ? W[1] : nullptr, N, F_in, N, true, p.w_rows, s);
+    if (int rc = check_launch(fn)) return rc;
+    const ResidualEpilogue<T> re{nullptr, dX, R, 0, ld_dx, ldr, n, nullptr, F_in, TMA_ACT_NONE, false, whole_rows(dX, ld_dx), R && whole_rows(R, ldr)};
+    snprintf(name, sizeof(name), "%s_bwd_data%s", what, sizeof(T) == 2 ? "_bf16" : "");
+    return launch_wide(name, p.d_rows, p.w_rows, planes_of(kP, kP), plan_rows(p.d_rows, p.w_rows), re, s);
+}
+
+// every number of a call that asks for a workspace, too
+inline bool wide_sizes_ok(int64_t n, int32_t F_in, int32_t F_out) { return n >= 0 && n <= INT32_MAX && F_in >= 1 && F_out >= 1 && F_in <= (1 << 16) && F_out <= (1 << 16); }
+inline bool wide_act_ok(int32_t act) { return act == TMA_ACT_NONE || act == TMA_ACT_RELU || act == TMA_ACT_SILU || act == TMA_ACT_GELU; }
+inline int check_wide(const char *fn, int64_t n, int32_t F_in, int32_t F_out, int32_t act, int32_t dtype, const void *ws, size_t ws_bytes, size_t need)
+{
+    TMA_REQUIRE(n >= 0 && n <= INT32_MAX, TMA_ERR_INVALID_ARG, "%s: n outside [0, 2^31)", fn);
+    TMA_REQUIRE(F_in >= 1 && F_out >= 1 && F_in <= (1 << 16) && F_out <= (1 << 16), TMA_ERR_BAD_SHAPE, "%s: F_in=%d F_out=%d", fn, F_in, F_out);
+    TMA_REQUIRE(wide_act_ok(act), TMA_ERR_INVALID_ARG, "%s: act %d", fn, act);
+    TMA_REQUIRE(dtype == TMA_F32 || dtype == TMA_BF16, TMA_ERR_UNSUPPORTED_DTYPE, "%s: dtype %d", fn, dtype);
+    TMA_REQUIRE(ws && aligned(ws, 256), TMA_ERR_INVALID_ARG, "%s: workspace NULL or not 256-byte aligned", fn);
+    TMA_REQUIRE(ws_bytes >= need, TMA_ERR_WORKSPACE_TOO_SMALL, "%s: workspace %zu < %zu", fn, ws_bytes, need);
+    return TMA_OK;
+}
+
+}  // namespace tma

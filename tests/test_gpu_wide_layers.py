@@ -1,0 +1,318 @@
+"""Gated dense layers and dense layers with a residual against plain fp64 forms of their formulas.
+
+Small whole numbers are exact in every step (their products' sums stay below 2^24), so with them results have to be the reference's, rounded once: any
+misplaced, lost or doubled term shows.  Normal values are compared element by element with a bound from the roundings that the calls are allowed:
+u_s = 2^-8 of bf16 storage (2^-24 of fp32) for each result and, with bf16, each weight; fp32 sums of K terms K 2^-24 of the sum of magnitudes."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+DTYPES = [torch.float32, torch.bfloat16]
+
+
+@pytest.fixture(scope="module")
+def B():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2305_09887_amd import binding
+    binding.lib()
+    return binding
+
+
+def _buffer(values, dtype, pitch, offset=0, fill=math.nan):
+    """`values` as rows `pitch` elements apart, `offset` elements into a buffer filled with something else."""
+    n, w = values.shape
+    flat = torch.full((max(n, 1) * pitch + offset + 16,), fill, dtype=dtype, device="cuda")
+    t = flat[offset:offset + max(n, 1) * pitch].view(max(n, 1), pitch)[:n, :w]
+    t.copy_(values.to(dtype))
+    return t, flat
+
+
+def _untouched(flat, t, fill):
+    """Whether all of `flat` outside the rows of `t` is still `fill`."""
+    mask = torch.ones_like(flat, dtype=torch.bool)
+    n, w = t.shape
+    off = t.storage_offset()
+    for_rows = mask[off:off + max(n, 1) * t.stride(0)] if n else mask[:0]
+    if n:
+        for_rows.view(n, t.stride(0))[:, :w] = False
+    return bool((flat[mask] == fill).all())
+
+
+def _whole(g, *shape, top=3):
+    return torch.randint(-top, top + 1, shape, generator=g).double()
+
+
+def _act(name, z):
+    if name == "silu":
+        return z * torch.sigmoid(z)
+    if name == "gelu":
+        return 0.5 * z * torch.erfc(-z / math.sqrt(2))
+    return z.clamp(min=0) if name == "relu" else z
+
+
+def _slope(name, z):
+    if name == "silu":
+        t = torch.sigmoid(z)
+        return t * (1 + z * (1 - t))
+    if name == "gelu":
+        return 0.5 * torch.erfc(-z / math.sqrt(2)) + z * torch.exp(-z * z / 2) / math.sqrt(2 * math.pi)
+    return (z > 0).double() if name == "relu" else torch.ones_like(z)
+
+
+def _code(B, name):
+    return {"none": B.TMA_ACT_NONE, "relu": B.TMA_ACT_RELU, "silu": B.TMA_ACT_SILU, "gelu": B.TMA_ACT_GELU}[name]
+
+
+# (n, F_in, F_out, pitch beyond the width, offset into the buffer): one row, units and tiles that end inside, rows that begin anywhere
+SHAPES = [(1, 1, 1, 0, 0), (1, 17, 33, 0, 0), (2, 64, 32, 0, 0), (5, 16, 100, 4, 0), (31, 33, 31, 3, 1), (33, 100, 47, 0, 0), (70, 8, 130, 8, 8),
+          (127, 129, 65, 1, 3), (128, 128, 128, 0, 0), (300, 96, 300, 4, 4), (257, 513, 255, 0, 0), (1030, 40, 72, 0, 0)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("act", ["none", "relu"])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_gated_whole_numbers(B, shape, act, dtype):
+    n, fi, fo, more, off = shape
+    g = torch.Generator().manual_seed(fi * 1000 + fo)
+    X, Wg, Wu, bg, bu = _whole(g, n, fi), _whole(g, fi, fo), _whole(g, fi, fo), _whole(g, fo), _whole(g, fo)
+    G, U = X @ Wg + bg, X @ Wu + bu
+    x, _ = _buffer(X, dtype, fi + more, off)
+    outs = [_buffer(torch.zeros(n, fo), dtype, fo + more, off, fill=7.0) for _ in range(3)]
+    d = lambda t: t.float().cuda()
+    h, gg, uu = B.tma_gated_dense_fwd(x, d(Wg), d(Wu), d(bg), d(bu), _code(B, act), G_out=outs[1][0], U_out=outs[2][0], H_out=outs[0][0])
+    want = _act(act, G) * U
+    for got, w, (t, flat) in zip((h, gg, uu), (want, G, U), outs):
+        assert torch.equal(got.cpu(), w.float().to(dtype))       # (below 2^24: exact in fp32)
+        assert _untouched(flat, t, 7.0)
+    alone, none_g, none_u = B.tma_gated_dense_fwd(x, d(Wg), d(Wu), None, d(bu), _code(B, act), save=False)
+    assert none_g is None and none_u is None and torch.equal(alone.cpu(), (_act(act, X @ Wg) * U).float().to(dtype))
+
+    G, U, dH, R = _whole(g, n, fo, top=2), _whole(g, n, fo, top=2), _whole(g, n, fo, top=2), _whole(g, n, fi)
+    gg, uu, dh, r = (_buffer(t, dtype, t.shape[1] + more, off)[0] for t in (G, U, dH, R))
+    dG, dU = dH * U * _slope(act, G), dH * _act(act, G)
+    dx, flat = _buffer(torch.zeros(n, fi), dtype, fi + more, off, fill=7.0)
+    got = B.tma_gated_dense_bwd(x, gg, uu, dh, d(Wg), d(Wu), _code(B, act), R=r, dX_out=dx)
+    for t, w in zip(got[:4], (X.t() @ dG, X.t() @ dU, dG.sum(0), dU.sum(0))):
+        assert torch.equal(t.cpu().double(), w)
+    assert torch.equal(got[4].cpu(), (dG @ Wg.t() + dU @ Wu.t() + R).float().to(dtype)) and _untouched(flat, dx, 7.0)
+    got = B.tma_gated_dense_bwd(x, gg, uu, dh, d(Wg), d(Wu), _code(B, act), need_dX=False, need_dbias=False)
+    assert torch.equal(got[0].cpu().double(), X.t() @ dG) and got[2] is None and got[3] is None and got[4] is None
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("act", ["none", "relu"])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_residual_whole_numbers(B, shape, act, dtype):
+    n, fi, fo, more, off = shape
+    g = torch.Generator().manual_seed(fi * 1000 + fo + 1)
+    X, W, b, R = _whole(g, n, fi), _whole(g, fi, fo), _whole(g, fo), _whole(g, n, fo)
+    Z = X @ W + b
+    x, r = _buffer(X, dtype, fi + more, off)[0], _buffer(R, dtype, fo + more, off)[0]
+    (z, z_flat), (y, y_flat) = (_buffer(torch.zeros(n, fo), dtype, fo + more, off, fill=7.0) for _ in range(2))
+    d = lambda t: t.float().cuda()
+    B.tma_dense_residual_fwd(x, d(W), d(b), _code(B, act), R=r, Z_out=z, Y_out=y)
+    want = (_act(act, Z) + R).float().to(dtype)
+    assert torch.equal(z.cpu(), Z.float().to(dtype)) and torch.equal(y.cpu(), want)
+    assert _untouched(z_flat, z, 7.0) and _untouched(y_flat, y, 7.0)
+    B.tma_dense_residual_fwd(x, d(W), d(b), _code(B, act), R=r, Y_out=r)          # in place
+    assert torch.equal(r.cpu(), want)
+    plain, none_z = B.tma_dense_residual_fwd(x, d(W), act=_code(B, act))
+    assert none_z is None and torch.equal(plain.cpu(), _act(act, X @ W).float().to(dtype))
+
+    Z, dY, R = _whole(g, n, fo), _whole(g, n, fo), _whole(g, n, fi)
+    z, dy, r = (_buffer(t, dtype, t.shape[1] + more, off)[0] for t in (Z, dY, R))
+    dZ = dY * _slope(act, Z)
+    dx, flat = _buffer(torch.zeros(n, fi), dtype, fi + more, off, fill=7.0)
+    dW, db, _ = B.tma_dense_residual_bwd(x, z if act != "none" else None, dy, d(W), _code(B, act), R=r, dX_out=dx)
+    assert torch.equal(dW.cpu().double(), X.t() @ dZ) and torch.equal(db.cpu().double(), dZ.sum(0))
+    want = (dZ @ W.t() + R).float().to(dtype)
+    assert torch.equal(dx.cpu(), want) and _untouched(flat, dx, 7.0)
+    B.tma_dense_residual_bwd(x, z, dy, d(W), _code(B, act), R=r, dX_out=r)          # in place
+    assert torch.equal(r.cpu(), want)
+    dW, db, dx = B.tma_dense_residual_bwd(x, z, dy, d(W), _code(B, act), need_dX=False, need_dbias=False)
+    assert torch.equal(dW.cpu().double(), X.t() @ dZ) and db is None and dx is None
+
+
+LIPSCHITZ = 1.13          # the steepest slope of silu is 1.0999, of gelu 1.1290
+CURVE = 0.80              # the largest |act''|: of silu 1/2, of gelu 2 / sqrt(2 pi)
+
+
+def _sum_bound(A, W, dtype, K):
+    """Of a product's sums: its weights' roundings with bf16, fp32 sums of K terms and of the parts that they come in."""
+    m = A.abs() @ W.abs()
+    return m * ((2.0 ** -8 if dtype == torch.bfloat16 else 0.0) + (K + 16) * 2.0 ** -24)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("act", ["none", "relu", "silu", "gelu"])
+@pytest.mark.parametrize("n,fi,fo", [(1, 40, 70), (77, 130, 96), (400, 64, 258)])
+def test_normal_values(B, n, fi, fo, act, dtype):
+    g = torch.Generator().manual_seed(n)
+    N = lambda *s: torch.randn(s, generator=g, dtype=torch.float64)
+    store = lambda t: t.to(dtype).double()
+    u = 2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -24
+    X, R = store(N(n, fi)), store(N(n, fo))
+    Wg, Wu, bg, bu = ((t / s).float().double() for t, s in ((N(fi, fo), fi ** 0.5), (N(fi, fo), fi ** 0.5), (N(fo), 4), (N(fo), 4)))
+    d, s = lambda t: t.float().cuda(), lambda t: t.to(dtype).cuda()
+    G, U = X @ Wg + bg, X @ Wu + bu
+    eg, eu = _sum_bound(X, Wg, dtype, fi) + 2.0 ** -23 * G.abs(), _sum_bound(X, Wu, dtype, fi) + 2.0 ** -23 * U.abs()
+    h, gg, uu = B.tma_gated_dense_fwd(s(X), d(Wg), d(Wu), d(bg), d(bu), _code(B, act))
+    a = _act(act, G)
+    # (the functions themselves: 2^-20 of z, which is more than their value's error)
+    ea = LIPSCHITZ * eg + 2.0 ** -20 * G.abs()
+    H, eh = a * U, ea * (U.abs() + eu) + a.abs() * eu + 2.0 ** -23 * (a * U).abs()
+    for got, want, e in ((gg, G, eg), (uu, U, eu), (h, H, eh)):
+        assert bool(((got.cpu().double() - want).abs() <= e + u * (want.abs() + e)).all())
+    y, z = B.tma_dense_residual_fwd(s(X), d(Wg), d(bg), _code(B, act), R=s(R), save=True)
+    want = a + R
+    assert torch.equal(z, gg)
+    assert bool(((y.cpu().double() - want).abs() <= ea + u * (want.abs() + ea) + 2.0 ** -23 * want.abs()).all())
+
+    G, U, dH, R = store(N(n, fo)), store(N(n, fo)), store(N(n, fo) / n), store(N(n, fi) / n)
+    a, slope = _act(act, G), _slope(act, G)
+    dG, dU, dZ = dH * U * slope, dH * a, dH * slope
+    small = 2.0 ** -19          # of the functions, and of the parts that a gradient is held in
+    es = small * (1 + G.abs())
+    got = B.tma_gated_dense_bwd(s(X), s(G), s(U), s(dH), d(Wg), d(Wu), _code(B, act), R=s(R))
+    eG, eU, eZ = (dH * U).abs() * es + dG.abs() * 2.0 ** -16, dH.abs() * es + dU.abs() * 2.0 ** -16, dH.abs() * es + dZ.abs() * 2.0 ** -16
+    for t, D, e in zip(got[:2], (dG, dU), (eG, eU)):
+        assert bool(((t.cpu().double() - X.t() @ D).abs() <= X.abs().t() @ (e + (n + 16) * 2.0 ** -24 * D.abs())).all())
+    for t, D, e in zip(got[2:4], (dG, dU), (eG, eU)):
+        assert bool(((t.cpu().double() - D.sum(0)).abs() <= (e + (n + 16) * 2.0 ** -24 * D.abs()).sum(0)).all())
+    ub = 2.0 ** -8 if dtype == torch.bfloat16 else 0.0          # of an operand that is rounded
+
+    def close(t, pairs):
+        want, e = R.clone(), torch.zeros_like(R)
+        for D, eD, W in pairs:
+            want += D @ W.t()
+            e += (eD + ub * D.abs()) @ W.abs().t() * (1 + ub) + _sum_bound(D, W.t(), dtype, 2 * fo)
+        e += 2.0 ** -23 * want.abs()
+        return bool(((t.cpu().double() - want).abs() <= e + u * (want.abs() + e)).all())
+
+    assert close(got[4], ((dG, eG, Wg), (dU, eU, Wu)))
+    dW, db, dX = B.tma_dense_residual_bwd(s(X), s(G), s(dH), d(Wg), _code(B, act), R=s(R))
+    assert bool(((dW.cpu().double() - X.t() @ dZ).abs() <= X.abs().t() @ (eZ + (n + 16) * 2.0 ** -24 * dZ.abs())).all())
+    assert bool(((db.cpu().double() - dZ.sum(0)).abs() <= (eZ + (n + 16) * 2.0 ** -24 * dZ.abs()).sum(0)).all())
+    assert close(dX, ((dZ, eZ, Wg),))
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_gradients_are_the_differences(B, act):
+    """Central differences of sum(c H) along random directions, fp32: the step h = 2^-6 leaves an error of h^2 / 6 times a third derivative (of a product of
+    a smooth function and a linear one along one direction, some units) and 2^-22 of the loss over 2 h."""
+    g = torch.Generator().manual_seed(3)
+    n, fi, fo = 40, 24, 56
+    N = lambda *s: torch.randn(s, generator=g).cuda()
+    X, Wg, Wu, Wd, bg, bu, bd = N(n, fi), N(fi, fo) / 5, N(fi, fo) / 5, N(fo, fi) / 8, N(fo) / 4, N(fo) / 4, N(fi) / 4
+    c, code = N(n, fi), _code(B, act)
+
+    def block(t):
+        H, G, U = B.tma_gated_dense_fwd(t[0], t[1], t[2], t[3], t[4], code)
+        return B.tma_dense_residual_fwd(H, t[5], t[6], R=t[0])[0], H, G, U
+
+    leaves = [X, Wg, Wu, bg, bu, Wd, bd]
+    Y, H, G, U = block(leaves)
+    dWd, dbd, dH = B.tma_dense_residual_bwd(H, None, c, Wd)
+    dWg, dWu, dbg, dbu, dX = B.tma_gated_dense_bwd(X, G, U, dH, Wg, Wu, code, R=c)
+    for i, grad in enumerate((dX, dWg, dWu, dbg, dbu, dWd, dbd)):
+        v = torch.randn(leaves[i].shape, generator=g).cuda()
+        v /= v.norm()
+        h = 2.0 ** -6
+        loss = [float((block([t + s * h * v if j == i else t for j, t in enumerate(leaves)])[0].double() * c.double()).sum()) for s in (1, -1)]
+        want, got = (loss[0] - loss[1]) / (2 * h), float((grad.double() * v.double()).sum())
+        scale = float(grad.norm())
+        assert abs(got - want) <= 2e-3 * scale, (i, got, want, scale)
+
+
+# many tiles of both sizes, ranges of the rows that are joined, a block's several tiles one after the other
+MANY = [(6_000, 520, 1_500), (20_011, 96, 100), (2_300, 2_050, 600), (300, 4_100, 2_304), (40_000, 31, 257), (16_400, 260, 1_100)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("n,fi,fo", MANY)
+def test_many_tiles_of_whole_numbers(B, n, fi, fo, dtype):
+    g = torch.Generator(device="cuda").manual_seed(n)
+    W = lambda *s: torch.randint(-1, 2, s, generator=g, device="cuda").double()
+    s, d = lambda t: t.to(dtype), lambda t: t.float()
+    X, Wg, Wu, bg, bu, R = W(n, fi), W(fi, fo), W(fi, fo), W(fo), W(fo), W(n, fo)
+    G, U = X @ Wg + bg, X @ Wu + bu
+    h, gg, uu = B.tma_gated_dense_fwd(s(X), d(Wg), d(Wu), d(bg), d(bu), B.TMA_ACT_RELU)
+    for got, want in ((gg, G), (uu, U), (h, G.clamp(min=0) * U)):
+        assert torch.equal(got, want.float().to(dtype))
+    y, z = B.tma_dense_residual_fwd(s(X), d(Wg), d(bg), B.TMA_ACT_RELU, R=s(R), save=True)
+    assert torch.equal(z, gg) and torch.equal(y, (G.clamp(min=0) + R).float().to(dtype))
+    del G, U, h, gg, uu, y, z
+    G, U, dH, R = W(n, fo), W(n, fo), W(n, fo), W(n, fi)
+    dG, dU = dH * U * (G > 0), dH * G.clamp(min=0)
+    want = X.t() @ dG, X.t() @ dU, dG.sum(0), dU.sum(0), (dG @ Wg.t() + dU @ Wu.t() + R).float().to(dtype).double()
+    for repeat in range(2):
+        got = B.tma_gated_dense_bwd(s(X), s(G), s(U), s(dH), d(Wg), d(Wu), B.TMA_ACT_RELU, R=s(R))
+        for t, w in zip(got, want):
+            assert torch.equal(t.double(), w)
+    for act, D in ((B.TMA_ACT_NONE, dH), (B.TMA_ACT_RELU, dH * (G > 0))):
+        dW, db, dX = B.tma_dense_residual_bwd(s(X), s(G), s(dH), d(Wg), act, R=s(R))
+        assert torch.equal(dW.double(), X.t() @ D) and torch.equal(db.double(), D.sum(0))
+        assert torch.equal(dX, (D @ Wg.t() + R).float().to(dtype))
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=["f32", "bf16"])
+def test_no_rows(B, dtype):
+    e = lambda w: torch.empty((0, w), dtype=dtype, device="cuda")
+    W = torch.ones((5, 9), device="cuda")
+    full = lambda *s: torch.full(s, 7.0, device="cuda")
+    assert B.tma_gated_dense_fwd(e(5), W, W)[0].shape == (0, 9)
+    assert B.tma_dense_residual_fwd(e(5), W)[0].shape == (0, 9)
+    out = [full(5, 9), full(5, 9), full(9), full(9)]
+    B.tma_gated_dense_bwd(e(5), e(9), e(9), e(9), W, W, dW_gate=out[0], dW_up=out[1], db_gate=out[2], db_up=out[3])
+    assert not any(t.any() for t in out)
+    out = [full(5, 9), full(9)]
+    B.tma_dense_residual_bwd(e(5), e(9), e(9), W, B.TMA_ACT_SILU, dW=out[0], dbias=out[1])
+    assert not any(t.any() for t in out)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=["f32", "bf16"])
+def test_values_that_are_no_numbers_stay_in_their_row(B, dtype):
+    """A NaN and an infinity in one row, and in the padding of all rows, reach that row's results and, backward, the weights' gradients of their columns; nothing else."""
+    g = torch.Generator().manual_seed(8)
+    n, fi, fo = 150, 50, 70
+    N = lambda *s: torch.randn(s, generator=g)
+    X, Wg, Wu = N(n, fi), N(fi, fo).cuda(), N(fi, fo).cuda()
+    x, _ = _buffer(X, dtype, fi + 14)
+    h, gg, uu = B.tma_gated_dense_fwd(x, Wg, Wu)
+    y, _ = B.tma_dense_residual_fwd(x, Wg, R=h)
+    dh, _ = _buffer(N(n, fo), dtype, fo + 10)
+    clean = B.tma_gated_dense_bwd(x, gg, uu, dh, Wg, Wu)
+    assert all(bool(t.isfinite().all()) for t in (h, gg, uu, y) + clean)
+    for bad in (math.nan, math.inf):
+        xb = x.clone()
+        xb[33, 7] = bad
+        hb, gb, ub = B.tma_gated_dense_fwd(xb, Wg, Wu)
+        yb, _ = B.tma_dense_residual_fwd(xb, Wg, R=h)
+        keep = torch.arange(n, device="cuda") != 33
+        for t, was in ((hb, h), (gb, gg), (ub, uu), (yb, y)):
+            assert torch.equal(t[keep], was[keep])
+        assert not bool(gb[33].isfinite().any()) and not bool(yb[33].isfinite().any())
+        got = B.tma_gated_dense_bwd(xb, gg, uu, dh, Wg, Wu)
+        cols = torch.arange(fi, device="cuda") != 7
+        for i in (0, 1):
+            assert torch.equal(got[i][cols], clean[i][cols]) and not bool(got[i][7].isfinite().any())
+        assert torch.equal(got[4], clean[4]) and torch.equal(got[2], clean[2])
+        gbad = B._padded(n, fo, dtype, 'cuda').copy_(gg)       # (G and U share a pitch)
+        gbad[33, 9] = bad
+        got = B.tma_gated_dense_bwd(x, gbad, uu, dh, Wg, Wu)
+        other = torch.arange(fo, device="cuda") != 9
+        assert torch.equal(got[0][:, other], clean[0][:, other]) and torch.equal(got[4][keep], clean[4][keep])
+        assert not bool(got[1][:, 9].isfinite().any()) and not bool(got[4][33].isfinite().any())
+
+
+def test_large_and_small_fp32_values(B):
+    """Values near the end of fp32's range and far below one: 24 bits of each count.  A product of two powers of two is exact."""
+    big, small = 2.0 ** 127 * (2 - 2.0 ** -23), 2.0 ** -100 * (1 + 2.0 ** -23)
+    X = torch.tensor([[big, 0.0], [0.0, small], [-big, 0.0]], device="cuda")
+    W = torch.tensor([[1.0, 0.5, 0.0], [2.0, 0.0, 2.0 ** 60]], device="cuda")
+    Y, _ = B.tma_dense_residual_fwd(X, W)
+    assert torch.equal(Y, torch.tensor([[big, big / 2, 0.0], [2 * small, 0.0, small * 2.0 ** 60], [-big, -big / 2, 0.0]], device="cuda"))
