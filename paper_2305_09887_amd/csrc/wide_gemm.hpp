@@ -236,8 +236,19 @@ __device__ __forceinline__ WideTile wide_tile(const WideCall &q, int64_t work)
 
 constexpr int kWideStages = 4;
 
-// MF x NF units a tile, WM x WN wavefronts.  A ring of slabs of 32 k-values, fetched three ahead through tile boundaries; the fragments of 16 k-values are read
-// while those before are multiplied, so that one wavefront a SIMD keeps its matrix unit busy.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+// A unit into LDS.  The base may come from a vector register by way of a scalar one just before: five wait states, which only the compiler's own
+// instructions get from it, are kept here.
+__device__ __forceinline__ void fetch_unit(uint32_t lds, const char *base, uint32_t offset)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+// MF x NF units a tile, WM x WN wavefronts.  A ring of slabs of 32 k-values, fetched three ahead through tile boundaries.  One wavefront a SIMD has to keep its
+// matrix unit busy by itself: the fragments of the next 16 k-values are read, and the units of a later slab fetched, one between every two matrix
+// instructions (each takes the unit 32 cycles).
 template <int MF, int NF, int WM, int WN, class Epi>
 __global__ __launch_bounds__(WM *WN * 64, 1) void wide_gemm_kernel(WideCall q, Epi epi)
 {
@@ -257,56 +268,72 @@ __global__ __launch_bounds__(WM *WN * 64, 1) void wide_gemm_kernel(WideCall q, E
     int64_t work = die * per_die + blockIdx.x / kWideDies;
     if (work >= end) return;
 
-    // ---- the cursor: the slab that is fetched next
+    // ---- the cursor: the slab that is fetched next.  Past the last it stays there: fetched again, into places that nobody reads.
     const uint32_t ring0 = lds_address(&ring[0][0][0]), lane_at = uint32_t(lane) * 16u;
-    int64_t c_work = work;
-    int c_left = 0, c_pair = 0, c_stage = 0;
-    bool c_open = true;
     // this wavefront's units of a slab: kLoads neighbours of one operand and one of its two k-units
     const int u0 = wave * kLoads;
     const bool rows_side = u0 < 2 * MF;
     const int in_side = rows_side ? u0 : u0 - 2 * MF, k_unit = in_side / (rows_side ? MF : NF), rb_in = in_side % (rows_side ? MF : NF);
+    int64_t c_work = work;
+    int c_left = 1, c_pair = -1, c_stage = kWideStages - 1, c_step = 16 * kUnitBytes;
     const char *from = nullptr;
-    auto fetch_next = [&]() {
-        if (!c_open) return;
-        if (c_left == 0) {
-            const WideTile tile = wide_tile(q, c_work);
-            const int rb = (rows_side ? tile.m * MF : tile.n * NF) + rb_in, pair = 4 * c_pair;
-            const Packed &o = rows_side ? q.a : q.b;
-            from = o.at + (((rows_side ? q.planes.a : q.planes.b) >> pair) & 15u) * o.plane() + o.unit(rb, int64_t(tile.split) * q.split_slabs * 2 + k_unit);
-            c_left = q.slabs_of(tile.split);
-        }
-        const uint32_t to = ring0 + uint32_t(c_stage) * uint32_t(kUnits * kUnitBytes) + uint32_t(u0) * uint32_t(kUnitBytes);
-#pragma unroll
-        for (int v = 0; v < kLoads; ++v) lds_fetch<4>(to + uint32_t(v) * uint32_t(kUnitBytes), reinterpret_cast<const float *>(from), lane_at + uint32_t(v) * uint32_t(kUnitBytes));
-        from += 16 * kUnitBytes;
+    uint32_t to = 0;
+    auto step = [&]() {
         c_stage = c_stage == kWideStages - 1 ? 0 : c_stage + 1;
-        if (--c_left == 0 && ++c_pair == q.planes.count) {
+        to = ring0 + uint32_t(c_stage) * uint32_t(kUnits * kUnitBytes) + uint32_t(u0) * uint32_t(kUnitBytes);
+        from += c_step;
+        c_left -= c_step != 0;
+        if (c_left > 0) return;
+        if (++c_pair == q.planes.count) {
             c_pair = 0;
             c_work += stride;
-            c_open = c_work < end;
+            if (c_work >= end) {       // (never zero again, and no further)
+                c_step = 0;
+                c_left = INT32_MAX;
+                from -= 16 * kUnitBytes;
+                return;
+            }
         }
+        const WideTile tile = wide_tile(q, c_work);
+        const int rb = (rows_side ? tile.m * MF : tile.n * NF) + rb_in, pair = 4 * c_pair;
+        const Packed &o = rows_side ? q.a : q.b;
+        from = o.at + (((rows_side ? q.planes.a : q.planes.b) >> pair) & 15u) * o.plane() + o.unit(rb, int64_t(tile.split) * q.split_slabs * 2 + k_unit);
+        c_left = q.slabs_of(tile.split);
+    };
+    const char *base = nullptr;      // `from` in scalar registers
+    auto fetch = [&](int v) { fetch_unit(to + uint32_t(v) * uint32_t(kUnitBytes), base, lane_at + uint32_t(v) * uint32_t(kUnitBytes)); };
+    auto next_slab = [&]() {
+        step();
+        const uint64_t at = reinterpret_cast<uint64_t>(from);
+        base = reinterpret_cast<const char *>(uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(int(at >> 32)))) << 32 | uint32_t(__builtin_amdgcn_readfirstlane(int(at))));
     };
 #pragma unroll
-    for (int s = 0; s < kAhead; ++s) fetch_next();
+    for (int s = 0; s < kAhead; ++s) {
+        next_slab();
+#pragma unroll
+        for (int v = 0; v < kLoads; ++v) fetch(v);
+    }
 
+    // fragments, in the order in which they are wanted: the first of the weights, all rows, the other weights
     uint4 xa[2][TM], xb[2][TN];
-    auto read = [&](int stage, int g, uint4 (&a)[TM], uint4 (&b)[TN]) {
-        const uint4 *base = &ring[stage][0][lane];
-#pragma unroll
-        for (int i = 0; i < TM; ++i) a[i] = base[(g * MF + wm * TM + i) * 64];
-#pragma unroll
-        for (int j = 0; j < TN; ++j) b[j] = base[(2 * MF + g * NF + wn * TN + j) * 64];
+    constexpr int kReads = TM + TN, kProducts = TM * TN;
+    static_assert(kReads <= kProducts && kLoads <= kProducts, "a read and a fetch for every product");
+    auto read = [&](int at, int g, int v, uint4 (&a)[TM], uint4 (&b)[TN]) {
+        const uint4 *units = &ring[at][0][lane];
+        if (v == 0) b[0] = units[(2 * MF + g * NF + wn * TN) * 64];
+        else if (v <= TM) a[v - 1] = units[(g * MF + wm * TM + v - 1) * 64];
+        else b[v - TM] = units[(2 * MF + g * NF + wn * TN + v - TM) * 64];
     };
     int stage = 0, storing = 0;
-    if (c_open) wait_and_meet<kYoung>();
-    else wait_and_meet<0>();
-    fetch_next();
-    read(0, 0, xa[0], xb[0]);
+    wait_and_meet<kYoung>();
+    next_slab();
+#pragma unroll
+    for (int v = 0; v < kLoads; ++v) fetch(v);
+#pragma unroll
+    for (int v = 0; v < kReads; ++v) read(0, 0, v, xa[0], xb[0]);
     for (;;) {
         const WideTile tile = wide_tile(q, work);
         const int slabs = q.slabs_of(tile.split) * q.planes.count;
-        const bool last = work + stride >= end;
         floatx16 acc[TN][TM];
 #pragma unroll
         for (int j = 0; j < TN; ++j)
@@ -314,31 +341,31 @@ __global__ __launch_bounds__(WM *WN * 64, 1) void wide_gemm_kernel(WideCall q, E
             for (int i = 0; i < TM; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[j][i][r] = 0.0f;
-        auto multiply = [&](const uint4 (&a)[TM], const uint4 (&b)[TN]) {
-#pragma unroll
-            for (int j = 0; j < TN; ++j)
-#pragma unroll
-                for (int i = 0; i < TM; ++i)
-                    acc[j][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, b[j]), __builtin_bit_cast(bf16x8, a[i]), acc[j][i], 0, 0, 0);
+        auto multiply = [&](int p, const uint4 (&a)[TM], const uint4 (&b)[TN]) {
+            const int j = p / TM, i = p % TM;
+            acc[j][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, b[j]), __builtin_bit_cast(bf16x8, a[i]), acc[j][i], 0, 0, 0);
         };
         for (int s = 0; s < slabs; ++s) {
-            read(stage, 1, xa[1], xb[1]);
             __builtin_amdgcn_sched_barrier(0);
-            multiply(xa[0], xb[0]);
-            __builtin_amdgcn_sched_barrier(0);
-            stage = stage == kWideStages - 1 ? 0 : stage + 1;
-            if (!(last && s + 1 == slabs)) {
-                // the next slab is there, and all have read this one, whose place the fetch takes
-                if (!c_open) wait_and_meet<0>();
-                else if (storing > 0) wait_and_meet<kYoungStores>();
-                else wait_and_meet<kYoung>();
-                --storing;
-                fetch_next();
-                read(stage, 0, xa[0], xb[0]);
+#pragma unroll
+            for (int p = 0; p < kProducts; ++p) {
+                if (p < kReads) read(stage, 1, p, xa[1], xb[1]);
+                multiply(p, xa[0], xb[0]);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            __builtin_amdgcn_sched_barrier(0);
-            multiply(xa[1], xb[1]);
-            __builtin_amdgcn_sched_barrier(0);
+            stage = stage == kWideStages - 1 ? 0 : stage + 1;
+            next_slab();
+            // the next slab is there, and all have read this one, whose place the fetches take
+            if (storing > 0) wait_and_meet<kYoungStores>();
+            else wait_and_meet<kYoung>();
+            --storing;
+#pragma unroll
+            for (int p = 0; p < kProducts; ++p) {
+                if (p < kReads) read(stage, 0, p, xa[0], xb[0]);
+                if (p < kLoads) fetch(p);
+                multiply(p, xa[1], xb[1]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
         constexpr int S = Epi::kSides;
 #pragma unroll
@@ -355,8 +382,9 @@ __global__ __launch_bounds__(WM *WN * 64, 1) void wide_gemm_kernel(WideCall q, E
         const bool whole = epi.whole(int64_t(tile.m) * (MF * 32) + MF * 32, (tile.n + 1) * NF / S * 32);
         storing = whole ? kAhead : 0;     // (fewer stores may not be counted on)
         work += stride;
-        if (last) break;
+        if (work >= end) break;
     }
+    wait_and_meet<0>();      // (what is still on its way writes into this block's LDS)
 }
 
 }  // namespace tma
