@@ -16,7 +16,8 @@ static int residual_fwd(const char *fn, int64_t n, const void *X, int64_t ldx, i
     if (int rc = check_launch(fn)) return rc;
     T *z = static_cast<T *>(Z), *y = static_cast<T *>(Y);
     const T *r = static_cast<const T *>(R);
-    const ResidualEpilogue<T> e{z, y, r, ldz, ldy, ldr, n, bias, F_out, act, z && whole_rows(z, ldz), whole_rows(y, ldy), r && whole_rows(r, ldr)};
+    const ResidualEpilogue<T> e{z, y, r, ldz, ldy, ldr, n, bias, F_out, act, whole_rows(y, ldy) && (!z || whole_rows(z, ldz)), r && whole_rows(r, ldr),
+                                bias_pieces(bias, F_out)};
     return launch_wide(sizeof(T) == 2 ? "residual_fwd_bf16" : "residual_fwd", p.a, p.b, planes_of(kP, kP), plan_rows(p.a, p.b), e, s);
 }
 

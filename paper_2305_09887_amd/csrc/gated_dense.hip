@@ -17,7 +17,8 @@ static int gated_fwd(const char *fn, int64_t n, const void *X, int64_t ldx, int3
     launch_pack_cols<float, kP>("wide_pack_cols", W_gate, W_up, F_out, F_in, F_out, true, p.b, s);
     if (int rc = check_launch(fn)) return rc;
     T *g = static_cast<T *>(G), *u = static_cast<T *>(U), *h = static_cast<T *>(H);
-    const GatedEpilogue<T> e{g, u, h, ldg, ldh, n, b_gate, b_up, F_out, act, g && whole_rows(g, ldg) && whole_rows(u, ldg), whole_rows(h, ldh)};
+    const GatedEpilogue<T> e{g, u, h, ldg, ldh, n, b_gate, b_up, F_out, act, whole_rows(h, ldh) && (!g || (whole_rows(g, ldg) && whole_rows(u, ldg))),
+                             bias_pieces(b_gate, F_out) && bias_pieces(b_up, F_out)};
     return launch_wide(sizeof(T) == 2 ? "gated_fwd_bf16" : "gated_fwd", p.a, p.b, planes_of(kP, kP), plan_rows(p.a, p.b), e, s);
 }
 

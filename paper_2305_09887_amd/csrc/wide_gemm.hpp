@@ -17,6 +17,9 @@
 #include "kernels.hpp"
 #include "lds_fetch.hpp"
 
+#include <type_traits>
+#include <utility>
+
 namespace tma {
 
 typedef float floatx16 __attribute__((ext_vector_type(16)));
@@ -234,8 +237,6 @@ __device__ __forceinline__ WideTile wide_tile(const WideCall &q, int64_t work)
     return {in / width, p * q.panel + in % width, int(work / tiles)};
 }
 
-constexpr int kWideStages = 4;
-
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
 // A unit into LDS.  The base may come from a vector register by way of a scalar one just before: five wait states, which only the compiler's own
@@ -246,19 +247,62 @@ __device__ __forceinline__ void fetch_unit(uint32_t lds, const char *base, uint3
 }
 #pragma clang diagnostic pop
 
-// MF x NF units a tile, WM x WN wavefronts.  A ring of slabs of 32 k-values, fetched three ahead through tile boundaries.  One wavefront a SIMD has to keep its
+// Write-out.  A lane has sixteen columns of a row, and a store of those would go to 32 rows.  So a wavefront's results go through its part of LDS, kRows rows by
+// kCols columns of sums at a time, and come back as the E neighbours that 16 bytes of storage hold, of a few rows: bias, activation and addition happen there,
+// in loops that are short enough to be unrolled, on whole lines of memory.  (What the compiler does not unroll indexes the results and so keeps them in scratch
+// memory: 8,192 rows 2048 -> 4096 in bf16 took 177 us so.)  32 rows by 64 columns, but where two results make one (gated) and two bytes are stored: 16 rows by
+// 128, for half lines stored one after the other are dear (2048 -> 8192 with three results 640 us).  The 16-byte pieces of a row are exchanged by its number, so that 16
+// lanes never meet in a bank, whether they write 16 rows or read one, two or four.
+template <int kRows_, int kCols_>
+struct Stage {
+    static constexpr int kRows = kRows_, kCols = kCols_;
+    float *at;
+    int lane;
+    static __device__ __forceinline__ int place(int row, int piece)
+    {
+        return row * kCols + (piece ^ ((piece >> 4 & 1) * 8) ^ (((row & 1) * 9) ^ ((row >> 1) & 7))) * 4;
+    }
+    // of columns `block` * 32 + [0, 32) this lane's sixteen, where its row is one of `part`'s
+    __device__ __forceinline__ void put(int part, int block, const floatx16 &v) const
+    {
+        const int row = lane & 31, first = block * 8 + (lane >> 5) * 4;
+        if (kRows == 32 || row / kRows == part) {
+#pragma unroll
+            for (int p = 0; p < 4; ++p) *reinterpret_cast<float4 *>(at + place(row % kRows, first + p)) = make_float4(v[4 * p], v[4 * p + 1], v[4 * p + 2], v[4 * p + 3]);
+        }
+    }
+    template <int E>
+    __device__ __forceinline__ void get(int row, int col, float (&v)[E]) const
+    {
+#pragma unroll
+        for (int p = 0; p < E / 4; ++p) {
+            const float4 x = *reinterpret_cast<const float4 *>(at + place(row, col / 4 + p));
+            v[4 * p] = x.x;
+            v[4 * p + 1] = x.y;
+            v[4 * p + 2] = x.z;
+            v[4 * p + 3] = x.w;
+        }
+    }
+};
+
+// The value is there: a load that a path leaves without a use would be waited for, with all fetches, in the main loop, each time its register is written.
+__device__ __forceinline__ void arrived(float &v) { asm volatile("" : "+v"(v)); }
+__device__ __forceinline__ void arrived(uint4 &v) { asm volatile("" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w)); }
+
+// MF x NF units a tile, WM x WN wavefronts.  A ring of slabs of 32 k-values, fetched kStages - 1 ahead through tile boundaries.  One wavefront a SIMD has to keep its
 // matrix unit busy by itself: the fragments of the next 16 k-values are read, and the units of a later slab fetched, one between every two matrix
 // instructions (each takes the unit 32 cycles).
-template <int MF, int NF, int WM, int WN, class Epi>
-__global__ __launch_bounds__(WM *WN * 64, 1) void wide_gemm_kernel(WideCall q, Epi epi)
+template <int MF, int NF, int WM, int WN, int kStages, class Epi>
+__global__ __launch_bounds__(WM *WN * 64, kStages * (MF + NF) >= 64 ? 1 : 2) void wide_gemm_kernel(WideCall q, Epi epi)
 {
-    constexpr int kWaves = WM * WN, TM = MF / WM, TN = NF / WN, kUnits = (MF + NF) * 2, kLoads = kUnits / kWaves, kAhead = kWideStages - 1;
+    constexpr int kWaves = WM * WN, TM = MF / WM, TN = NF / WN, kUnits = (MF + NF) * 2, kLoads = kUnits / kWaves, kAhead = kStages - 1;
     constexpr int kYoung = (kAhead - 1) * kLoads;
     constexpr int kYoungStores = kYoung + TM * TN * Epi::kStores < 63 ? kYoung + TM * TN * Epi::kStores : 63;
-    static_assert(MF % WM == 0 && NF % WN == 0 && kUnits % kWaves == 0 && MF % kLoads == 0 && NF % kLoads == 0 && 8 % MF == 0 && 8 % NF == 0 && kYoung <= 63 && TN % Epi::kSides == 0, "tile shape");
-    __shared__ __attribute__((aligned(1024))) uint4 ring[kWideStages][kUnits][64];
+    static_assert(MF % WM == 0 && NF % WN == 0 && kUnits % kWaves == 0 && MF % kLoads == 0 && NF % kLoads == 0 && 8 % MF == 0 && 8 % NF == 0 && kYoung <= 63 && TN % 2 == 0, "tile shape");
+    __shared__ __attribute__((aligned(1024))) uint4 ring[kStages][kUnits][64];
+    __shared__ __attribute__((aligned(1024))) uint4 stages[kWaves][512];
 
-    const int lane = threadIdx.x & 63, l31 = lane & 31, hi = lane >> 5;
+    const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
 
@@ -275,11 +319,11 @@ __global__ __launch_bounds__(WM *WN * 64, 1) void wide_gemm_kernel(WideCall q, E
     const bool rows_side = u0 < 2 * MF;
     const int in_side = rows_side ? u0 : u0 - 2 * MF, k_unit = in_side / (rows_side ? MF : NF), rb_in = in_side % (rows_side ? MF : NF);
     int64_t c_work = work;
-    int c_left = 1, c_pair = -1, c_stage = kWideStages - 1, c_step = 16 * kUnitBytes;
+    int c_left = 1, c_pair = -1, c_stage = kStages - 1, c_step = 16 * kUnitBytes;
     const char *from = nullptr;
     uint32_t to = 0;
     auto step = [&]() {
-        c_stage = c_stage == kWideStages - 1 ? 0 : c_stage + 1;
+        c_stage = c_stage == kStages - 1 ? 0 : c_stage + 1;
         to = ring0 + uint32_t(c_stage) * uint32_t(kUnits * kUnitBytes) + uint32_t(u0) * uint32_t(kUnitBytes);
         from += c_step;
         c_left -= c_step != 0;
@@ -353,7 +397,7 @@ __global__ __launch_bounds__(WM *WN * 64, 1) void wide_gemm_kernel(WideCall q, E
                 multiply(p, xa[0], xb[0]);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            stage = stage == kWideStages - 1 ? 0 : stage + 1;
+            stage = stage == kStages - 1 ? 0 : stage + 1;
             next_slab();
             // the next slab is there, and all have read this one, whose place the fetches take
             if (storing > 0) wait_and_meet<kYoungStores>();
@@ -368,17 +412,31 @@ __global__ __launch_bounds__(WM *WN * 64, 1) void wide_gemm_kernel(WideCall q, E
             }
         }
         constexpr int S = Epi::kSides;
+        typedef typename Epi::template StageOf<TN> Staged;
+        constexpr int kJ = Staged::kCols / 32, kGroups = TN / kJ, kParts = 32 / Staged::kRows, kSteps = TM * kGroups * kParts;
+        const int64_t row0 = int64_t(tile.m) * (MF * 32) + wm * TM * 32;
+        const int col0 = (tile.n * NF + wn * TN) / S * 32;
+        const Staged staged{reinterpret_cast<float *>(&stages[wave][0]), lane};
+        typename Epi::template Cols<Staged> cols[kGroups];
 #pragma unroll
-        for (int j = 0; j < TN; j += S) {
-            const int col = ((tile.n * NF + wn * TN + j) / S) * 32 + hi * 16;
-            typename Epi::Cols cols;
-            epi.columns(col, cols);
+        for (int j = 0; j < kGroups; ++j) epi.columns(col0 + j * (Staged::kCols / S), lane, cols[j]);
+        typename Epi::Past past[2];
+        epi.past(row0, col0, lane, past[0]);
 #pragma unroll
-            for (int i = 0; i < TM; ++i) {
-                epi.store(int64_t(tile.m) * (MF * 32) + (wm * TM + i) * 32 + l31, col, tile.split, cols, acc[j][i], acc[j + S - 1][i]);
-                __builtin_amdgcn_sched_barrier(0);      // (several at once would not fit the registers)
-            }
-        }
+        for (int j = 0; j < kGroups; ++j) cols[j].wait();
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < kGroups; ++j)
+#pragma unroll
+                for (int h = 0; h < kParts; ++h) {
+                    const int step = (i * kGroups + j) * kParts + h;
+                    if (step + 1 < kSteps && Epi::kPast)
+                        epi.past(row0 + (step + 1) / kGroups * 32, col0 + (step + 1) % kGroups * (Staged::kCols / S), lane, past[(step + 1) % 2]);
+#pragma unroll
+                    for (int b = 0; b < kJ; ++b) staged.put(h, b, acc[j * kJ + b][i]);
+                    epi.emit(staged, row0 + i * 32 + h * Staged::kRows, col0 + j * (Staged::kCols / S), tile.split, cols[j], past[step % 2]);
+                }
         const bool whole = epi.whole(int64_t(tile.m) * (MF * 32) + MF * 32, (tile.n + 1) * NF / S * 32);
         storing = whole ? kAhead : 0;     // (fewer stores may not be counted on)
         work += stride;
