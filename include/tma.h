@@ -745,8 +745,10 @@ int tma_dropout_bwd(int64_t n, int32_t F, const void *dY, int64_t ldy, double p,
  *   NULL where no backward pass follows or act is NONE; the backward reads Z
  *   with an activation only.
  *
- * dtype TMA_BF16: weights are rounded to bf16 for the products, sums are fp32,
- * results are rounded once; the gradients of weights are fp32, of pre-activations of 16 bits
+ * dtype TMA_BF16: weights are rounded to bf16 for the products (the forward ones
+ * of up to 64 rows take them as they are: a row's result can change by that
+ * rounding where the list grows past 64), sums are fp32, results are rounded
+ * once; the gradients of weights are fp32, of pre-activations of 16 bits
  * or more.  TMA_F32: products of three bf16 parts of each value, which hold its 24
  * bits; absolute error of a part 2^-126.  A NaN or an infinity in an input makes
  * results that it reaches non-finite (NaN where fp32 arithmetic may give an

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from array import array
 
 import torch
 
@@ -1289,35 +1290,43 @@ def tma_grad_norm_workspace_bytes(n_tensors: int) -> int:
     return int(lib().tma_grad_norm_workspace_bytes(n_tensors))
 
 
+def _addresses(tensors):
+    """Their addresses as a host array."""
+    return array("Q", map(torch.Tensor.data_ptr, tensors))
+
+
 def _grad_list(where, grads, out, norm_out, ws, stream):
-    """(device, number of tensors, their addresses and lengths as host arrays, type, norm_out, workspace)"""
+    """(device, number of tensors, their addresses and lengths as host arrays, type, norm_out, workspace).  (Lists are long and the host's share is what
+    counts on a small model: whole lists go through built-in functions.)"""
     if not grads:
         raise TmaError(f"{where}: no gradients")
     dev, kind = grads[0].device, grads[0].dtype
     dtype = _feat_dtype(grads[0])
-    for t in grads:
-        if t.dtype != kind or t.device != dev or not t.is_contiguous():
-            raise TmaError(f"{where}: gradients must be contiguous tensors of one type on one device")
+    lengths = list(map(torch.Tensor.numel, grads))
+    every = list(grads)
     if out is not None:
         if len(out) != len(grads):
             raise TmaError(f"{where}: one result for each gradient")
-        for t, o in zip(grads, out):
-            if o.dtype != kind or o.device != dev or not o.is_contiguous() or o.numel() != t.numel():
-                raise TmaError(f"{where}: a result differs from its gradient in type, device or size")
+        if list(map(torch.Tensor.numel, out)) != lengths:
+            raise TmaError(f"{where}: a result differs from its gradient in size")
+        every += out
+    if ({t.dtype for t in every} != {kind} or set(map(torch.Tensor.get_device, every)) != {dev.index} or dev.type != "cuda"
+            or not all(map(torch.Tensor.is_contiguous, every))):
+        raise TmaError(f"{where}: gradients and results must be contiguous tensors of one type on one device")
     if norm_out is None:
         norm_out = _record(torch.empty(1, dtype=torch.float32, device=dev), stream)
     _device(where, grads[0], norm_out, ws)
     _vector(norm_out, "norm_out", (1,), torch.float32)
-    n = len(grads)
+    n = len(lengths)
     if ws is None:
         ws = _workspace(tma_grad_norm_workspace_bytes(n), dev, stream)
-    return (dev, n, (C.c_void_p * n)(*[t.data_ptr() for t in grads]), (C.c_int64 * n)(*[t.numel() for t in grads]), dtype, norm_out, ws)
+    return dev, n, _addresses(grads), array("q", lengths), dtype, norm_out, ws
 
 
 def tma_grad_norm(grads, norm_out=None, ws=None, stream=None):
     """The norm of all gradients together (a list of dense tensors of one type), [1] fp32 on their device."""
     dev, n, ptrs, sizes, dtype, norm_out, ws = _grad_list("tma_grad_norm", grads, None, norm_out, ws, stream)
-    _launch(dev, stream, lib().tma_grad_norm, n, ptrs, sizes, dtype, norm_out.data_ptr(), *_room(ws))
+    _launch(dev, stream, lib().tma_grad_norm, n, ptrs.buffer_info()[0], sizes.buffer_info()[0], dtype, norm_out.data_ptr(), *_room(ws))
     return norm_out
 
 
@@ -1325,8 +1334,9 @@ def tma_grad_clip(grads, max_norm: float, out=None, norm_out=None, ws=None, stre
     """Gradients whose norm together is above max_norm are scaled to it, in place or into the tensors of ``out``; returns the
     norm before that, [1] fp32 on their device."""
     dev, n, ptrs, sizes, dtype, norm_out, ws = _grad_list("tma_grad_clip", grads, out, norm_out, ws, stream)
-    outs = None if out is None else (C.c_void_p * n)(*[t.data_ptr() for t in out])
-    _launch(dev, stream, lib().tma_grad_clip, n, ptrs, outs, sizes, dtype, float(max_norm), norm_out.data_ptr(), *_room(ws))
+    outs = None if out is None else _addresses(out)
+    _launch(dev, stream, lib().tma_grad_clip, n, ptrs.buffer_info()[0], outs.buffer_info()[0] if outs is not None else None,
+            sizes.buffer_info()[0], dtype, float(max_norm), norm_out.data_ptr(), *_room(ws))
     return norm_out
 
 

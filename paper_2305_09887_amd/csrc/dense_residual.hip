@@ -10,14 +10,15 @@ static int residual_fwd(const char *fn, int64_t n, const void *X, int64_t ldx, i
                         int64_t ldr, void *Z, int64_t ldz, void *Y, int64_t ldy, void *ws, hipStream_t s)
 {
     constexpr int kP = kPartsOf<T>;
-    const ForwardPlan p = plan_forward<T>(n, F_in, F_out, 1, ws);
-    launch_pack_rows<T, kP>("wide_pack_rows", X, nullptr, ldx, n, F_in, false, p.a, s);
-    launch_pack_cols<float, kP>("wide_pack_cols", W, nullptr, F_out, F_in, F_out, true, p.b, s);
-    if (int rc = check_launch(fn)) return rc;
     T *z = static_cast<T *>(Z), *y = static_cast<T *>(Y);
     const T *r = static_cast<const T *>(R);
     const ResidualEpilogue<T> e{z, y, r, ldz, ldy, ldr, n, bias, F_out, act, whole_rows(y, ldy) && (!z || whole_rows(z, ldz)), r && whole_rows(r, ldr),
                                 bias_pieces(bias, F_out)};
+    if (n <= kFewMost) return launch_few<T, 1>(fn, sizeof(T) == 2 ? "residual_few_bf16" : "residual_few", n, X, ldx, W, nullptr, F_in, F_out, e, s);
+    const ForwardPlan p = plan_forward<T>(n, F_in, F_out, 1, ws);
+    launch_pack_rows<T, kP>("wide_pack_rows", X, nullptr, ldx, n, F_in, false, p.a, s);
+    launch_pack_cols<float, kP>("wide_pack_cols", W, nullptr, F_out, F_in, F_out, true, p.b, s);
+    if (int rc = check_launch(fn)) return rc;
     return launch_wide(sizeof(T) == 2 ? "residual_fwd_bf16" : "residual_fwd", p.a, p.b, planes_of(kP, kP), plan_rows(p.a, p.b), e, s);
 }
 

@@ -12,13 +12,14 @@ static int gated_fwd(const char *fn, int64_t n, const void *X, int64_t ldx, int3
                      int32_t F_out, int32_t act, void *G, void *U, int64_t ldg, void *H, int64_t ldh, void *ws, hipStream_t s)
 {
     constexpr int kP = kPartsOf<T>;
+    T *g = static_cast<T *>(G), *u = static_cast<T *>(U), *h = static_cast<T *>(H);
+    const GatedEpilogue<T> e{g, u, h, ldg, ldh, n, b_gate, b_up, F_out, act, whole_rows(h, ldh) && (!g || (whole_rows(g, ldg) && whole_rows(u, ldg))),
+                             bias_pieces(b_gate, F_out) && bias_pieces(b_up, F_out)};
+    if (n <= kFewMost) return launch_few<T, 2>(fn, sizeof(T) == 2 ? "gated_few_bf16" : "gated_few", n, X, ldx, W_gate, W_up, F_in, F_out, e, s);
     const ForwardPlan p = plan_forward<T>(n, F_in, F_out, 2, ws);
     launch_pack_rows<T, kP>("wide_pack_rows", X, nullptr, ldx, n, F_in, false, p.a, s);
     launch_pack_cols<float, kP>("wide_pack_cols", W_gate, W_up, F_out, F_in, F_out, true, p.b, s);
     if (int rc = check_launch(fn)) return rc;
-    T *g = static_cast<T *>(G), *u = static_cast<T *>(U), *h = static_cast<T *>(H);
-    const GatedEpilogue<T> e{g, u, h, ldg, ldh, n, b_gate, b_up, F_out, act, whole_rows(h, ldh) && (!g || (whole_rows(g, ldg) && whole_rows(u, ldg))),
-                             bias_pieces(b_gate, F_out) && bias_pieces(b_up, F_out)};
     return launch_wide(sizeof(T) == 2 ? "gated_fwd_bf16" : "gated_fwd", p.a, p.b, planes_of(kP, kP), plan_rows(p.a, p.b), e, s);
 }
 

@@ -63,14 +63,48 @@ __device__ __forceinline__ void take_apart(float x, float (&part)[kParts])
     }
 }
 
-// eight values of a row along k -> the lane's 16 bytes of each part
+// Eight values of a row along k -> the lane's 16 bytes of each part.  What a rounding left over comes from one instruction, as in split_pair.hpp: v - h as the dot
+// product of the pair (h0, h1) with (-1, 0) or (0, -1), plus v.  (Value by value, with its selects, the parts took the few-row products 600 cycles a wavefront
+// and 32 k-values: one row 4096 -> 1024 23 us.)  Values beyond the largest bf16, and what is no number, take the careful way.
+struct Remainder {
+    typedef __bf16 Pair __attribute__((ext_vector_type(2)));
+    uint32_t first, second;
+    __device__ __forceinline__ Remainder() : first(0x0000BF80u), second(0xBF800000u)
+    {
+        // held in registers: as an inline constant of this instruction -1.0 would stand in the other half
+        asm("" : "+s"(first));
+        asm("" : "+s"(second));
+    }
+    __device__ __forceinline__ void operator()(float &x, float &y, uint32_t parts) const
+    {
+        x = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(Pair, parts), __builtin_bit_cast(Pair, first), x, false);
+        y = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(Pair, parts), __builtin_bit_cast(Pair, second), y, false);
+    }
+};
 template <int kParts>
 __device__ __forceinline__ void pack_eight(const float (&v)[8], uint4 (&out)[kParts])
 {
     if constexpr (kParts == 1) {
         out[0] = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+        return;
+    }
+    uint32_t w[kParts][4];
+    // (a NaN makes the comparison false: fmaxf would drop it)
+    bool plain = true;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) plain = plain && fabsf(v[j]) < 0x1p127f;
+    if (__all(plain)) {
+        const Remainder rest;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float x = v[2 * j], y = v[2 * j + 1];
+#pragma unroll
+            for (int p = 0; p < kParts; ++p) {
+                w[p][j] = pack_bf16(x, y);
+                if (p + 1 < kParts) rest(x, y, w[p][j]);
+            }
+        }
     } else {
-        uint32_t w[kParts][4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             float a[kParts], b[kParts];
@@ -79,9 +113,9 @@ __device__ __forceinline__ void pack_eight(const float (&v)[8], uint4 (&out)[kPa
 #pragma unroll
             for (int p = 0; p < kParts; ++p) w[p][j] = (__float_as_uint(a[p]) >> 16) | (__float_as_uint(b[p]) & 0xFFFF0000u);
         }
-#pragma unroll
-        for (int p = 0; p < kParts; ++p) out[p] = make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]);
     }
+#pragma unroll
+    for (int p = 0; p < kParts; ++p) out[p] = make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]);
 }
 
 __device__ __forceinline__ float widen1(float x) { return x; }

@@ -1,6 +1,7 @@
 // What the gated layers and the dense layers with a residual share beside their products (wide_gemm.hpp): activations, what becomes of a product, the
 // gradients of the pre-activations, and the host's plans.
 #pragma once
+#include "wide_few.hpp"
 #include "wide_gemm.hpp"
 
 namespace tma {
@@ -98,6 +99,9 @@ __device__ __forceinline__ void store_some(uint16_t *p, int c, int cols, bool wh
             if (c + j < cols) p[c + j] = f32_to_bf16(v[j]);
     }
 }
+__device__ __forceinline__ void narrow(float *p, float v) { *p = v; }
+__device__ __forceinline__ void narrow(uint16_t *p, float v) { *p = f32_to_bf16(v); }
+
 // (every load without a condition of its own: each of those was waited for before the next, 100 us of 8,192 rows 2048 -> 8192)
 template <int E>
 __device__ __forceinline__ void bias_of(const float *bias, int c, int cols, bool pieces, float (&v)[E])
@@ -191,6 +195,19 @@ struct GatedEpilogue {
         }
     }
     __device__ __forceinline__ bool whole(int64_t m_end, int n_end) const { return whole16 && m_end <= M && n_end <= N; }
+    // of one place
+    __device__ __forceinline__ void one(int64_t row, int c, float g, float u) const
+    {
+        if (b_gate) g += b_gate[c];
+        if (b_up) u += b_up[c];
+        if (G) {
+            narrow(G + row * ldg + c, g);
+            narrow(U + row * ldg + c, u);
+        }
+        float v[1] = {g};
+        activate(act, v);
+        narrow(H + row * ldh + c, v[0] * u);
+    }
 };
 
 // Y = act(Z) + R, Z = product + bias kept where asked for.  R is on its way before the sums that it is added to are in LDS.
@@ -269,6 +286,15 @@ struct ResidualEpilogue {
         }
     }
     __device__ __forceinline__ bool whole(int64_t m_end, int n_end) const { return whole16 && m_end <= M && n_end <= N; }
+    __device__ __forceinline__ void one(int64_t row, int c, float z, float) const
+    {
+        if (bias) z += bias[c];
+        if (Z) narrow(Z + row * ldz + c, z);
+        float v[1] = {z};
+        activate(act, v);
+        if (R) v[0] += widen1(R[row * ldr + c]);
+        narrow(Y + row * ldy + c, v[0]);
+    }
 };
 
 // a weight gradient, or a range's share of it: the columns of `sides` matrices behind each other, each padded to whole units
@@ -496,7 +522,11 @@ struct ForwardPlan {
 template <typename T>
 inline ForwardPlan plan_forward(int64_t n, int32_t F_in, int32_t F_out, int sides, void *ws)
 {
-    ForwardPlan p;
+    ForwardPlan p{};
+    if (n <= kFewMost) {      // nothing is laid out
+        p.bytes = 256;
+        return p;
+    }
     p.a = packed_shape(n, F_in);
     p.b = packed_shape(F_out, F_in);
     p.b.rbs *= sides;

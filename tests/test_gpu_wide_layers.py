@@ -68,7 +68,7 @@ def _code(B, name):
 
 
 # (n, F_in, F_out, pitch beyond the width, offset into the buffer): one row, units and tiles that end inside, rows that begin anywhere
-SHAPES = [(1, 1, 1, 0, 0), (1, 17, 33, 0, 0), (2, 64, 32, 0, 0), (5, 16, 100, 4, 0), (31, 33, 31, 3, 1), (33, 100, 47, 0, 0), (70, 8, 130, 8, 8),
+SHAPES = [(1, 1, 1, 0, 0), (1, 17, 33, 0, 0), (2, 64, 32, 0, 0), (5, 16, 100, 4, 0), (16, 31, 48, 0, 0), (17, 64, 20, 0, 0), (31, 33, 31, 3, 1), (32, 1030, 16, 2, 2), (64, 600, 50, 0, 0), (65, 600, 50, 0, 0), (33, 100, 47, 0, 0), (70, 8, 130, 8, 8),
           (127, 129, 65, 1, 3), (128, 128, 128, 0, 0), (300, 96, 300, 4, 4), (257, 513, 255, 0, 0), (1030, 40, 72, 0, 0)]
 
 
