@@ -754,7 +754,7 @@ int tma_dropout_bwd(int64_t n, int32_t F, const void *dY, int64_t ldy, double p,
  * results that it reaches non-finite (NaN where fp32 arithmetic may give an
  * infinity).  The ReLU of a NaN is 0 and closed.  Widths up to 65536.  What lies in a row's padding has no
  * influence and is left as it is.
- * Workspaces, 256-byte aligned: the *_workspace_bytes queries.
+ * Workspaces, 256-byte aligned: the *_workspace_bytes queries (none forward of up to 64 rows, ws may then be NULL).
  * ---------------------------------------------------------------------- */
 size_t tma_gated_dense_fwd_workspace_bytes(int64_t n, int32_t F_in, int32_t F_out, int32_t dtype);
 

@@ -1153,6 +1153,18 @@ def tma_dropout_bwd(dY, p: float, seed: int, step=None, first_row: int = 0, out=
     return _dropout("tma_dropout_bwd", lib().tma_dropout_bwd, dY, p, seed, step, first_row, out, stream)
 
 
+def _new_rows(n, cols, dtype, dev, stream):
+    """_padded, but for widths that need no padding in one call."""
+    if n and cols * (2 if dtype == torch.bfloat16 else 4) % 16 == 0:
+        return _record(torch.empty((n, cols), dtype=dtype, device=dev), stream)
+    return _record(_padded(n, cols, dtype, dev), stream)
+
+
+def _forward_room(ws, nbytes, dev, stream):
+    """The workspace of a forward call, or none where it needs none."""
+    return _workspace(nbytes, dev, stream) if ws is None and nbytes else ws
+
+
 def _rows_or_none(t, name, shape, dtype):
     """Address and leading dimension of a [rows, cols] tensor, or of none."""
     if t is None:
@@ -1184,12 +1196,11 @@ def tma_gated_dense_fwd(X, W_gate, W_up, b_gate=None, b_up=None, act: int = TMA_
     elif G_out is None or U_out is None:
         if G_out is not None or U_out is not None:
             raise TmaError(f"{where}: G_out and U_out go together")
-        G_out, U_out = (_record(_padded(n, F_out, X.dtype, dev), stream) for _ in range(2))
+        G_out, U_out = (_new_rows(n, F_out, X.dtype, dev, stream) for _ in range(2))
     if H_out is None:
-        H_out = _record(_padded(n, F_out, X.dtype, dev), stream)
+        H_out = _new_rows(n, F_out, X.dtype, dev, stream)
     _same_ld(G_out, U_out, f"{where}: G_out / U_out")
-    if ws is None:
-        ws = _workspace(tma_gated_dense_fwd_workspace_bytes(n, F_in, F_out, dtype), dev, stream)
+    ws = _forward_room(ws, tma_gated_dense_fwd_workspace_bytes(n, F_in, F_out, dtype), dev, stream)
     G, ldg = _rows_or_none(G_out, "G_out", (n, F_out), X.dtype)
     _launch(dev, stream, lib().tma_gated_dense_fwd, n, X.data_ptr(), _rows_like(X, "X", (n, F_in), X.dtype), F_in,
             _vector(W_gate, "W_gate", (F_in, F_out), torch.float32), _vector(W_up, "W_up", (F_in, F_out), torch.float32),
@@ -1217,7 +1228,7 @@ def tma_gated_dense_bwd(X, G, U, dH, W_gate, W_up, act: int = TMA_ACT_SILU, R=No
     dW_up = new((F_in, F_out)) if dW_up is None else dW_up
     db_gate = None if not need_dbias else new((F_out,)) if db_gate is None else db_gate
     db_up = None if not need_dbias else new((F_out,)) if db_up is None else db_up
-    dX_out = None if not need_dX else _record(_padded(n, F_in, X.dtype, dev), stream) if dX_out is None else dX_out
+    dX_out = None if not need_dX else _new_rows(n, F_in, X.dtype, dev, stream) if dX_out is None else dX_out
     if ws is None:
         ws = _workspace(tma_gated_dense_bwd_workspace_bytes(n, F_in, F_out, dtype, need_dX), dev, stream)
     _rows_like(U, "U", (n, F_out), X.dtype)
@@ -1244,11 +1255,10 @@ def tma_dense_residual_fwd(X, W, bias=None, act: int = TMA_ACT_NONE, R=None, sav
     F_out = _weight_shape(where, "W", W, F_in)
     dtype = _feat_dtype(X)
     if save and Z_out is None:
-        Z_out = _record(_padded(n, F_out, X.dtype, dev), stream)
+        Z_out = _new_rows(n, F_out, X.dtype, dev, stream)
     if Y_out is None:
-        Y_out = _record(_padded(n, F_out, X.dtype, dev), stream)
-    if ws is None:
-        ws = _workspace(tma_dense_residual_fwd_workspace_bytes(n, F_in, F_out, dtype), dev, stream)
+        Y_out = _new_rows(n, F_out, X.dtype, dev, stream)
+    ws = _forward_room(ws, tma_dense_residual_fwd_workspace_bytes(n, F_in, F_out, dtype), dev, stream)
     _launch(dev, stream, lib().tma_dense_residual_fwd, n, X.data_ptr(), _rows_like(X, "X", (n, F_in), X.dtype), F_in,
             _vector(W, "W", (F_in, F_out), torch.float32), _vector(bias, "bias", (F_out,), torch.float32), F_out, act, dtype,
             *_rows_or_none(R, "R", (n, F_out), X.dtype), *_rows_or_none(Z_out, "Z_out", (n, F_out), X.dtype), Y_out.data_ptr(),
@@ -1275,7 +1285,7 @@ def tma_dense_residual_bwd(X, Z, dY, W, act: int = TMA_ACT_NONE, R=None, dW=None
     new = lambda shape: _record(torch.empty(shape, dtype=torch.float32, device=dev), stream)
     dW = new((F_in, F_out)) if dW is None else dW
     dbias = None if not need_dbias else new((F_out,)) if dbias is None else dbias
-    dX_out = None if not need_dX else _record(_padded(n, F_in, X.dtype, dev), stream) if dX_out is None else dX_out
+    dX_out = None if not need_dX else _new_rows(n, F_in, X.dtype, dev, stream) if dX_out is None else dX_out
     if ws is None:
         ws = _workspace(tma_dense_residual_bwd_workspace_bytes(n, F_in, F_out, act, dtype, need_dX), dev, stream)
     _launch(dev, stream, lib().tma_dense_residual_bwd, n, X.data_ptr(), _rows_like(X, "X", (n, F_in), X.dtype),

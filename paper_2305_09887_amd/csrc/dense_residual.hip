@@ -19,7 +19,8 @@ static int residual_fwd(const char *fn, int64_t n, const void *X, int64_t ldx, i
     launch_pack_rows<T, kP>("wide_pack_rows", X, nullptr, ldx, n, F_in, false, p.a, s);
     launch_pack_cols<float, kP>("wide_pack_cols", W, nullptr, F_out, F_in, F_out, true, p.b, s);
     if (int rc = check_launch(fn)) return rc;
-    return launch_wide(sizeof(T) == 2 ? "residual_fwd_bf16" : "residual_fwd", p.a, p.b, planes_of(kP, kP), plan_rows(p.a, p.b), e, s);
+    const Planes planes = planes_of(kP, kP);
+    return launch_wide(sizeof(T) == 2 ? "residual_fwd_bf16" : "residual_fwd", p.a, p.b, planes, plan_rows(p.a, p.b, planes, r != nullptr), e, s);
 }
 
 template <typename T>

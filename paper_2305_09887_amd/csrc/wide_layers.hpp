@@ -453,6 +453,29 @@ static void launch_join(const char *name, const float *partial, int ranges, int6
     hipLaunchKernelGGL(join_ranges_kernel, dim3(unsigned(blocks < 1 ? 1 : blocks), second ? 2 : 1), dim3(256), 0, s, partial, ranges, range_stride, side_stride, count, first, second);
 }
 
+// out[side][i] = the blocks' sums of column i: 64 threads a column, each every 64th of them, joined in a fixed order
+static __global__ __launch_bounds__(1024) void join_sums_kernel(const float *__restrict__ sums, int blocks, int sides, int padded, int N, float *first, float *second)
+{
+    __shared__ float part[64][17];
+    const int c = threadIdx.x % 16, g = threadIdx.x / 16, side = blockIdx.y, col = blockIdx.x * 16 + c;
+    float sum = 0.0f;
+    if (col < N) {
+#pragma unroll 8
+        for (int p = g; p < blocks; p += 64) sum += sums[(int64_t(p) * sides + side) * padded + col];
+    }
+    part[g][c] = sum;
+    for (int half = 32; half; half >>= 1) {
+        __syncthreads();
+        if (g < half) part[g][c] += part[g + half][c];
+    }
+    if (g == 0 && col < N) (side ? second : first)[col] = part[0][c];
+}
+static void launch_join_sums(const float *sums, int blocks, int sides, int padded, int N, float *first, float *second, hipStream_t s)
+{
+    TMA_TIMED("wide_join_sums", s);
+    hipLaunchKernelGGL(join_sums_kernel, dim3(unsigned(ceil_div(N, 16)), unsigned(sides)), dim3(1024), 0, s, sums, blocks, sides, padded, N, first, second);
+}
+
 // ---- plans ---------------------------------------------------------------------
 constexpr int kCus = 256;
 struct WidePlan {
@@ -460,10 +483,18 @@ struct WidePlan {
     int splits, split_slabs;
 };
 inline int64_t wide_tiles(int m_units, int n_units, bool big) { return ceil_div(m_units, big ? 8 : 4) * ceil_div(n_units, big ? 8 : 4); }
-// one range of k: results go through an epilogue
-inline WidePlan plan_rows(const Packed &a, const Packed &b)
+// whether tiles of 256 x 256 multiply hardly more than there is (128 of 256 columns fill half of one: weight gradients of 128 x 512, 125,237 rows in fp32
+// 230 us so)
+inline bool fills_big(int m_units, int n_units) { return wide_tiles(m_units, n_units, true) * 4 * 10 <= wide_tiles(m_units, n_units, false) * 11; }
+// One range of k: results go through an epilogue.  A large tile is multiplied 7 % faster (8192 -> 2048, 8,192 rows 267 and 287 us) but is alone on its unit, which does
+// nothing else while results are written: where a product is short beside them, and first of all where they are added to something that has to be
+// read, two small ones a unit are faster (256 -> 256 with a residual, 1,000,003 rows in bf16, eight slabs: 719 and 490 us; gated 128 -> 256 in fp32, 24 slabs,
+// nothing added: 162 and 188).
+inline WidePlan plan_rows(const Packed &a, const Packed &b, const Planes &planes, bool reads)
 {
-    return {wide_tiles(a.rbs, b.rbs, true) >= kCus * 3 / 4, 1, a.kgs / 2};
+    const int slabs = a.kgs / 2;
+    const bool big = wide_tiles(a.rbs, b.rbs, true) >= kCus * 3 / 4 && fills_big(a.rbs, b.rbs) && int64_t(slabs) * planes.count >= (reads ? 64 : 16);
+    return {big, 1, slabs};
 }
 // ranges of k until the tiles fill the chip, 512 rows each at least
 inline WidePlan plan_weight(const Packed &a, const Packed &b)
@@ -473,7 +504,7 @@ inline WidePlan plan_weight(const Packed &a, const Packed &b)
         const int64_t tiles = wide_tiles(a.rbs, b.rbs, big), slots = big ? kCus : 2 * kCus;
         int64_t want = slots / tiles;
         want = want < 1 ? 1 : want > most ? most : want;
-        if (big && tiles * want < kCus / 2) continue;
+        if (big && (tiles * want < kCus / 2 || !fills_big(a.rbs, b.rbs))) continue;
         const int per = int(ceil_div(slabs, want));
         return {big, int(ceil_div(slabs, per)), per};
     }
@@ -523,10 +554,7 @@ template <typename T>
 inline ForwardPlan plan_forward(int64_t n, int32_t F_in, int32_t F_out, int sides, void *ws)
 {
     ForwardPlan p{};
-    if (n <= kFewMost) {      // nothing is laid out
-        p.bytes = 256;
-        return p;
-    }
+    if (n <= kFewMost) return p;      // nothing is laid out
     p.a = packed_shape(n, F_in);
     p.b = packed_shape(F_out, F_in);
     p.b.rbs *= sides;
@@ -583,7 +611,7 @@ static int wide_backward(const char *fn, const char *what, int64_t n, const T *X
     const int32_t N = g.N;
     if (n == 0) {      // (no ranges: zeros)
         launch_join("wide_join", nullptr, 0, 0, 0, int64_t(F_in) * N, dW[0], kSides == 2 ? dW[1] : nullptr, s);
-        if (db[0]) launch_join("wide_join_sums", nullptr, 0, 0, 0, N, db[0], kSides == 2 ? db[1] : nullptr, s);
+        if (db[0]) launch_join_sums(nullptr, 0, kSides, 0, N, db[0], db[1], s);
         return check_launch(fn);
     }
     const bool exact = kSides == 1 && g.act == TMA_ACT_NONE;
@@ -612,14 +640,15 @@ static int wide_backward(const char *fn, const char *what, int64_t n, const T *X
     snprintf(name, sizeof(name), "%s_bwd_weight%s", what, sizeof(T) == 2 ? "_bf16" : "");
     if (int rc = launch_wide(name, p.x_cols, p.d_cols, planes_of(kP, p.parts_c), p.weight, we, s)) return rc;
     if (split) launch_join("wide_join", p.partial, p.weight.splits, cells * kSides, cells, cells, dW[0], kSides == 2 ? dW[1] : nullptr, s);
-    if (db[0]) launch_join("wide_join_sums", p.sums, p.row_blocks, int64_t(kSides) * p.padded, p.padded, N, db[0], kSides == 2 ? db[1] : nullptr, s);
+    if (db[0]) launch_join_sums(p.sums, p.row_blocks, kSides, p.padded, N, db[0], db[1], s);
     if (int rc = check_launch(fn)) return rc;
     if (!dX) return TMA_OK;
     launch_pack_rows<float, kP>("wide_pack_rows", W[0], kSides == 2 ? W[1] : nullptr, N, F_in, N, true, p.w_rows, s);
     if (int rc = check_launch(fn)) return rc;
     const ResidualEpilogue<T> re{nullptr, dX, R, 0, ld_dx, ldr, n, nullptr, F_in, TMA_ACT_NONE, whole_rows(dX, ld_dx), R && whole_rows(R, ldr), false};
     snprintf(name, sizeof(name), "%s_bwd_data%s", what, sizeof(T) == 2 ? "_bf16" : "");
-    return launch_wide(name, p.d_rows, p.w_rows, planes_of(kP, kP), plan_rows(p.d_rows, p.w_rows), re, s);
+    const Planes planes = planes_of(kP, kP);
+    return launch_wide(name, p.d_rows, p.w_rows, planes, plan_rows(p.d_rows, p.w_rows, planes, R != nullptr), re, s);
 }
 
 // every number of a call that asks for a workspace, too
@@ -631,7 +660,7 @@ inline int check_wide(const char *fn, int64_t n, int32_t F_in, int32_t F_out, in
     TMA_REQUIRE(F_in >= 1 && F_out >= 1 && F_in <= (1 << 16) && F_out <= (1 << 16), TMA_ERR_BAD_SHAPE, "%s: F_in=%d F_out=%d", fn, F_in, F_out);
     TMA_REQUIRE(wide_act_ok(act), TMA_ERR_INVALID_ARG, "%s: act %d", fn, act);
     TMA_REQUIRE(dtype == TMA_F32 || dtype == TMA_BF16, TMA_ERR_UNSUPPORTED_DTYPE, "%s: dtype %d", fn, dtype);
-    TMA_REQUIRE(ws && aligned(ws, 256), TMA_ERR_INVALID_ARG, "%s: workspace NULL or not 256-byte aligned", fn);
+    TMA_REQUIRE(!need || (ws && aligned(ws, 256)), TMA_ERR_INVALID_ARG, "%s: workspace NULL or not 256-byte aligned", fn);
     TMA_REQUIRE(ws_bytes >= need, TMA_ERR_WORKSPACE_TOO_SMALL, "%s: workspace %zu < %zu", fn, ws_bytes, need);
     return TMA_OK;
 }
