@@ -16,11 +16,9 @@ static int residual_fwd(const char *fn, int64_t n, const void *X, int64_t ldx, i
                                 bias_pieces(bias, F_out)};
     if (n <= kFewMost) return launch_few<T, 1>(fn, sizeof(T) == 2 ? "residual_few_bf16" : "residual_few", n, X, ldx, W, nullptr, F_in, F_out, e, s);
     const ForwardPlan p = plan_forward<T>(n, F_in, F_out, 1, ws);
-    launch_pack_rows<T, kP>("wide_pack_rows", X, nullptr, ldx, n, F_in, false, p.a, s);
     launch_pack_cols<float, kP>("wide_pack_cols", W, nullptr, F_out, F_in, F_out, true, p.b, s);
     if (int rc = check_launch(fn)) return rc;
-    const Planes planes = planes_of(kP, kP);
-    return launch_wide(sizeof(T) == 2 ? "residual_fwd_bf16" : "residual_fwd", p.a, p.b, planes, plan_rows(p.a, p.b, planes, r != nullptr), e, s);
+    return forward_product<T>(fn, sizeof(T) == 2 ? "residual_fwd_bf16" : "residual_fwd", n, static_cast<const T *>(X), ldx, F_in, p, r != nullptr, e, s);
 }
 
 template <typename T>

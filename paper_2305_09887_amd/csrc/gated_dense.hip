@@ -17,11 +17,9 @@ static int gated_fwd(const char *fn, int64_t n, const void *X, int64_t ldx, int3
                              bias_pieces(b_gate, F_out) && bias_pieces(b_up, F_out)};
     if (n <= kFewMost) return launch_few<T, 2>(fn, sizeof(T) == 2 ? "gated_few_bf16" : "gated_few", n, X, ldx, W_gate, W_up, F_in, F_out, e, s);
     const ForwardPlan p = plan_forward<T>(n, F_in, F_out, 2, ws);
-    launch_pack_rows<T, kP>("wide_pack_rows", X, nullptr, ldx, n, F_in, false, p.a, s);
     launch_pack_cols<float, kP>("wide_pack_cols", W_gate, W_up, F_out, F_in, F_out, true, p.b, s);
     if (int rc = check_launch(fn)) return rc;
-    const Planes planes = planes_of(kP, kP);
-    return launch_wide(sizeof(T) == 2 ? "gated_fwd_bf16" : "gated_fwd", p.a, p.b, planes, plan_rows(p.a, p.b, planes, false), e, s);
+    return forward_product<T>(fn, sizeof(T) == 2 ? "gated_fwd_bf16" : "gated_fwd", n, static_cast<const T *>(X), ldx, F_in, p, false, e, s);
 }
 
 template <typename T>

@@ -5,8 +5,7 @@
 // outside the operand is zero.  Eight units of 256 rows follow each other, then those of the next k-values, of the next rows (a slab of a tile is one run of
 // memory; units of rows past the last are never written, and reach only results that are not stored), then planes: fp32 values are taken apart into bf16 parts whose sum
 // they are (three of them hold all 24 bits, two hold 17), one plane a part, and a product of such operands is the sum of products of planes, the small ones
-// first.  So an fp32 product is a bf16 product of six times the length (192 cycles of the matrix unit for 16 k-values, where the fp32 instruction takes
-// 512), and a weight gradient in fp32 from bf16 rows one of twice the length.
+// first: a weight gradient in fp32 from bf16 rows is a product of twice the length; fp32 operands have a kernel of their own (wide_split.hpp).
 //
 // A unit is what one wavefront fetches straight into LDS with one instruction and what it reads from there without conflicts: no swizzle, no edges, no
 // masks between memory and the matrix units.  The layout costs a pass over the operands, bytes against the product's rows times columns.
@@ -241,19 +240,21 @@ struct Planes {            // pairs of planes, four bits each, the first multipl
     int count;
     uint32_t a, b;
 };
-inline Planes planes_of(int a_parts, int b_parts)
+inline Planes planes_of(int b_parts)
 {
-    if (a_parts == 3) return {6, 0x001120u, 0x010102u};     // (2,0) (0,2) (1,1) (1,0) (0,1) (0,0)
     if (b_parts == 2) return {2, 0x00u, 0x01u};             // (0,1) (0,0)
     return {1, 0u, 0u};
 }
 
 // C[m][n] = sum over k of A[m][k] B[n][k]: A's rows are rows of the result, B's are the weights' side.
+// direct: A are rows of bf16 where they lie, at multiples of 16 bytes, of a multiple of 32 elements: nothing of them is laid out.  A wavefront's load then takes
+// 64 bytes of 16 rows, and LDS has those rows, their 16-byte pieces exchanged by a quarter of the row's number (16 lanes read as many rows: all banks).
 struct WideCall {
     Packed a, b;
     Planes planes;
     int m_tiles, n_tiles, panel;      // panel: column tiles that a die's blocks share rows of
     int splits, split_slabs;          // ranges of k, of that many slabs
+    int64_t lda, rows;                // direct: A's pitch in elements, its rows
     __host__ __device__ __forceinline__ int slabs_of(int split) const
     {
         const int left = a.kgs / 2 - split * split_slabs;
@@ -323,17 +324,47 @@ struct Stage {
 __device__ __forceinline__ void arrived(float &v) { asm volatile("" : "+v"(v)); }
 __device__ __forceinline__ void arrived(uint4 &v) { asm volatile("" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w)); }
 
+// A wavefront's TN by TM fragments, of rows from row0 and columns from col0 on, by way of its part of LDS
+template <int TM, int TN, class Epi>
+__device__ __forceinline__ void write_out(const Epi &epi, const floatx16 (&acc)[TN][TM], int64_t row0, int col0, int split, float *at, int lane)
+{
+    constexpr int S = Epi::kSides;
+    typedef typename Epi::template StageOf<TN> Staged;
+    constexpr int kJ = Staged::kCols / 32, kGroups = TN / kJ, kParts = 32 / Staged::kRows, kSteps = TM * kGroups * kParts;
+    const Staged staged{at, lane};
+    typename Epi::template Cols<Staged> cols[kGroups];
+#pragma unroll
+    for (int j = 0; j < kGroups; ++j) epi.columns(col0 + j * (Staged::kCols / S), lane, cols[j]);
+    typename Epi::Past past[2];
+    epi.past(row0, col0, lane, past[0]);
+#pragma unroll
+    for (int j = 0; j < kGroups; ++j) cols[j].wait();
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < kGroups; ++j)
+#pragma unroll
+            for (int h = 0; h < kParts; ++h) {
+                const int step = (i * kGroups + j) * kParts + h;
+                if (step + 1 < kSteps && Epi::kPast)
+                    epi.past(row0 + (step + 1) / kGroups * 32, col0 + (step + 1) % kGroups * (Staged::kCols / S), lane, past[(step + 1) % 2]);
+#pragma unroll
+                for (int b = 0; b < kJ; ++b) staged.put(h, b, acc[j * kJ + b][i]);
+                epi.emit(staged, row0 + i * 32 + h * Staged::kRows, col0 + j * (Staged::kCols / S), split, cols[j], past[step % 2]);
+            }
+}
+
 // MF x NF units a tile, WM x WN wavefronts.  A ring of slabs of 32 k-values, fetched kStages - 1 ahead through tile boundaries.  One wavefront a SIMD has to keep its
 // matrix unit busy by itself: the fragments of the next 16 k-values are read, and the units of a later slab fetched, one between every two matrix
 // instructions (each takes the unit 32 cycles).
-template <int MF, int NF, int WM, int WN, int kStages, class Epi>
+template <int MF, int NF, int WM, int WN, int kStages, bool kDirect, class Epi>
 __global__ __launch_bounds__(WM *WN * 64, kStages * (MF + NF) >= 64 ? 1 : 2) void wide_gemm_kernel(WideCall q, Epi epi)
 {
     constexpr int kWaves = WM * WN, TM = MF / WM, TN = NF / WN, kUnits = (MF + NF) * 2, kLoads = kUnits / kWaves, kAhead = kStages - 1;
     constexpr int kYoung = (kAhead - 1) * kLoads;
     constexpr int kYoungStores = kYoung + TM * TN * Epi::kStores < 63 ? kYoung + TM * TN * Epi::kStores : 63;
     static_assert(MF % WM == 0 && NF % WN == 0 && kUnits % kWaves == 0 && MF % kLoads == 0 && NF % kLoads == 0 && 8 % MF == 0 && 8 % NF == 0 && kYoung <= 63 && TN % 2 == 0, "tile shape");
-    __shared__ __attribute__((aligned(1024))) uint4 ring[kStages][kUnits][64];
+    __shared__ __attribute__((aligned(1024))) uint4 ring[kStages * kUnits * 64];
     __shared__ __attribute__((aligned(1024))) uint4 stages[kWaves][512];
 
     const int lane = threadIdx.x & 63;
@@ -347,42 +378,56 @@ __global__ __launch_bounds__(WM *WN * 64, kStages * (MF + NF) >= 64 ? 1 : 2) voi
     if (work >= end) return;
 
     // ---- the cursor: the slab that is fetched next.  Past the last it stays there: fetched again, into places that nobody reads.
-    const uint32_t ring0 = lds_address(&ring[0][0][0]), lane_at = uint32_t(lane) * 16u;
+    const uint32_t ring0 = lds_address(&ring[0]);
     // this wavefront's units of a slab: kLoads neighbours of one operand and one of its two k-units
     const int u0 = wave * kLoads;
     const bool rows_side = u0 < 2 * MF;
     const int in_side = rows_side ? u0 : u0 - 2 * MF, k_unit = in_side / (rows_side ? MF : NF), rb_in = in_side % (rows_side ? MF : NF);
     int64_t c_work = work;
-    int c_left = 1, c_pair = -1, c_stage = kStages - 1, c_step = 16 * kUnitBytes;
+    const int slab_bytes = kDirect && rows_side ? 64 : 16 * kUnitBytes;
+    int c_at = 0, c_slabs = 1, c_last = INT32_MAX, c_pair = -1, c_stage = kStages - 1;
+    // a lane's place in load v: row min(row + 16 v, most) of `pitch` bytes, and its piece of it (units are rows of 64 bytes, one behind the other)
+    const bool lying = kDirect && rows_side;
+    const uint32_t pitch = lying ? uint32_t(q.lda * 2) : 64u, piece_at = uint32_t(lying ? (lane & 3) ^ (lane >> 4) : lane & 3) * 16u;
+    const int row_in = lane / 4 + (lying ? u0 * 16 : 0);
+    int most = INT32_MAX;
     const char *from = nullptr;
     uint32_t to = 0;
     auto step = [&]() {
         c_stage = c_stage == kStages - 1 ? 0 : c_stage + 1;
         to = ring0 + uint32_t(c_stage) * uint32_t(kUnits * kUnitBytes) + uint32_t(u0) * uint32_t(kUnitBytes);
-        from += c_step;
-        c_left -= c_step != 0;
-        if (c_left > 0) return;
+        if (++c_at < c_slabs) return;
         if (++c_pair == q.planes.count) {
             c_pair = 0;
             c_work += stride;
-            if (c_work >= end) {       // (never zero again, and no further)
-                c_step = 0;
-                c_left = INT32_MAX;
-                from -= 16 * kUnitBytes;
+            if (c_work >= end) {
+                c_last = c_slabs - 1;
+                c_slabs = INT32_MAX;
                 return;
             }
         }
+        c_at = 0;
         const WideTile tile = wide_tile(q, c_work);
         const int rb = (rows_side ? tile.m * MF : tile.n * NF) + rb_in, pair = 4 * c_pair;
-        const Packed &o = rows_side ? q.a : q.b;
-        from = o.at + (((rows_side ? q.planes.a : q.planes.b) >> pair) & 15u) * o.plane() + o.unit(rb, int64_t(tile.split) * q.split_slabs * 2 + k_unit);
-        c_left = q.slabs_of(tile.split);
+        if (!kDirect || !rows_side) {
+            const Packed &o = rows_side ? q.a : q.b;
+            from = o.at + (((rows_side ? q.planes.a : q.planes.b) >> pair) & 15u) * o.plane() + o.unit(rb, int64_t(tile.split) * q.split_slabs * 2 + k_unit);
+            c_slabs = q.slabs_of(tile.split);
+        } else {
+            const int64_t row0 = int64_t(tile.m) * (MF * 32), left = q.rows - 1 - row0;
+            most = left < MF * 32 ? int(left) : MF * 32;
+            from = q.a.at + row0 * q.lda * 2;
+            c_slabs = q.a.kgs / 2;
+        }
     };
     const char *base = nullptr;      // `from` in scalar registers
-    auto fetch = [&](int v) { fetch_unit(to + uint32_t(v) * uint32_t(kUnitBytes), base, lane_at + uint32_t(v) * uint32_t(kUnitBytes)); };
+    auto fetch = [&](int v) {
+        const int row = row_in + v * 16;
+        fetch_unit(to + uint32_t(v) * uint32_t(kUnitBytes), base, kDirect ? uint32_t(row < most ? row : most) * pitch + piece_at : uint32_t(v * kUnitBytes + lane * 16));
+    };
     auto next_slab = [&]() {
         step();
-        const uint64_t at = reinterpret_cast<uint64_t>(from);
+        const uint64_t at = reinterpret_cast<uint64_t>(from) + uint64_t(c_at < c_last ? c_at : c_last) * uint32_t(slab_bytes);
         base = reinterpret_cast<const char *>(uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(int(at >> 32)))) << 32 | uint32_t(__builtin_amdgcn_readfirstlane(int(at))));
     };
 #pragma unroll
@@ -396,9 +441,12 @@ __global__ __launch_bounds__(WM *WN * 64, kStages * (MF + NF) >= 64 ? 1 : 2) voi
     uint4 xa[2][TM], xb[2][TN];
     constexpr int kReads = TM + TN, kProducts = TM * TN;
     static_assert(kReads <= kProducts && kLoads <= kProducts, "a read and a fetch for every product");
+    // direct: of 32 rows of 64 bytes this lane's piece of the first and of the second 16 k-values
+    const int row_at0 = (lane & 31) * 4 + ((lane >> 5) ^ ((lane >> 2) & 3)), row_at1 = row_at0 ^ 2;
     auto read = [&](int at, int g, int v, uint4 (&a)[TM], uint4 (&b)[TN]) {
-        const uint4 *units = &ring[at][0][lane];
+        const uint4 *slab = &ring[at * (kUnits * 64)], *units = slab + lane;
         if (v == 0) b[0] = units[(2 * MF + g * NF + wn * TN) * 64];
+        else if (v <= TM && kDirect) a[v - 1] = slab[(wm * TM + v - 1) * 128 + (g ? row_at1 : row_at0)];
         else if (v <= TM) a[v - 1] = units[(g * MF + wm * TM + v - 1) * 64];
         else b[v - TM] = units[(2 * MF + g * NF + wn * TN + v - TM) * 64];
     };
@@ -446,31 +494,7 @@ __global__ __launch_bounds__(WM *WN * 64, kStages * (MF + NF) >= 64 ? 1 : 2) voi
             }
         }
         constexpr int S = Epi::kSides;
-        typedef typename Epi::template StageOf<TN> Staged;
-        constexpr int kJ = Staged::kCols / 32, kGroups = TN / kJ, kParts = 32 / Staged::kRows, kSteps = TM * kGroups * kParts;
-        const int64_t row0 = int64_t(tile.m) * (MF * 32) + wm * TM * 32;
-        const int col0 = (tile.n * NF + wn * TN) / S * 32;
-        const Staged staged{reinterpret_cast<float *>(&stages[wave][0]), lane};
-        typename Epi::template Cols<Staged> cols[kGroups];
-#pragma unroll
-        for (int j = 0; j < kGroups; ++j) epi.columns(col0 + j * (Staged::kCols / S), lane, cols[j]);
-        typename Epi::Past past[2];
-        epi.past(row0, col0, lane, past[0]);
-#pragma unroll
-        for (int j = 0; j < kGroups; ++j) cols[j].wait();
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-            for (int j = 0; j < kGroups; ++j)
-#pragma unroll
-                for (int h = 0; h < kParts; ++h) {
-                    const int step = (i * kGroups + j) * kParts + h;
-                    if (step + 1 < kSteps && Epi::kPast)
-                        epi.past(row0 + (step + 1) / kGroups * 32, col0 + (step + 1) % kGroups * (Staged::kCols / S), lane, past[(step + 1) % 2]);
-#pragma unroll
-                    for (int b = 0; b < kJ; ++b) staged.put(h, b, acc[j * kJ + b][i]);
-                    epi.emit(staged, row0 + i * 32 + h * Staged::kRows, col0 + j * (Staged::kCols / S), tile.split, cols[j], past[step % 2]);
-                }
+        write_out<TM, TN>(epi, acc, int64_t(tile.m) * (MF * 32) + wm * TM * 32, (tile.n * NF + wn * TN) / S * 32, tile.split, reinterpret_cast<float *>(&stages[wave][0]), lane);
         const bool whole = epi.whole(int64_t(tile.m) * (MF * 32) + MF * 32, (tile.n + 1) * NF / S * 32);
         storing = whole ? kAhead : 0;     // (fewer stores may not be counted on)
         work += stride;

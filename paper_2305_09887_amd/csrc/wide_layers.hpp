@@ -3,6 +3,7 @@
 #pragma once
 #include "wide_few.hpp"
 #include "wide_gemm.hpp"
+#include "wide_split.hpp"
 
 namespace tma {
 
@@ -488,45 +489,60 @@ inline int64_t wide_tiles(int m_units, int n_units, bool big) { return ceil_div(
 inline bool fills_big(int m_units, int n_units) { return wide_tiles(m_units, n_units, true) * 4 * 10 <= wide_tiles(m_units, n_units, false) * 11; }
 // One range of k: results go through an epilogue.  A large tile is multiplied 7 % faster (8192 -> 2048, 8,192 rows 267 and 287 us) but is alone on its unit, which does
 // nothing else while results are written: where a product is short beside them, and first of all where they are added to something that has to be
-// read, two small ones a unit are faster (256 -> 256 with a residual, 1,000,003 rows in bf16, eight slabs: 719 and 490 us; gated 128 -> 256 in fp32, 24 slabs,
-// nothing added: 162 and 188).
-inline WidePlan plan_rows(const Packed &a, const Packed &b, const Planes &planes, bool reads)
+// read, two small ones a unit are faster (256 -> 256 with a residual, 1,000,003 rows in bf16, eight slabs: 719 and 490 us).
+inline WidePlan plan_rows(const Packed &a, const Packed &b, bool reads)
 {
     const int slabs = a.kgs / 2;
-    const bool big = wide_tiles(a.rbs, b.rbs, true) >= kCus * 3 / 4 && fills_big(a.rbs, b.rbs) && int64_t(slabs) * planes.count >= (reads ? 64 : 16);
-    return {big, 1, slabs};
+    return {wide_tiles(a.rbs, b.rbs, true) >= kCus * 3 / 4 && fills_big(a.rbs, b.rbs) && slabs >= (reads ? 64 : 16), 1, slabs};
 }
-// ranges of k until the tiles fill the chip, 512 rows each at least
-inline WidePlan plan_weight(const Packed &a, const Packed &b)
+// ranges of k until the tiles fill the chip, 512 rows each at least; fp32 has small tiles only
+inline WidePlan plan_weight(const Packed &a, const Packed &b, bool fp32)
 {
     const int slabs = a.kgs / 2, most = slabs / 16 > 1 ? slabs / 16 : 1;
     for (bool big : {true, false}) {
         const int64_t tiles = wide_tiles(a.rbs, b.rbs, big), slots = big ? kCus : 2 * kCus;
         int64_t want = slots / tiles;
         want = want < 1 ? 1 : want > most ? most : want;
-        if (big && (tiles * want < kCus / 2 || !fills_big(a.rbs, b.rbs))) continue;
+        if (big && (fp32 || tiles * want < kCus / 2 || !fills_big(a.rbs, b.rbs))) continue;
         const int per = int(ceil_div(slabs, want));
         return {big, int(ceil_div(slabs, per)), per};
     }
     return {false, 1, slabs};
 }
 
-template <class Epi>
-static int launch_wide(const char *name, const Packed &a, const Packed &b, const Planes &planes, const WidePlan &p, const Epi &e, hipStream_t s)
+template <bool kDirect, class Epi>
+static int launch_wide_as(const char *name, WideCall q, const WidePlan &p, const Epi &e, hipStream_t s)
 {
-    WideCall q{a, b, planes, 0, 0, 8, p.splits, p.split_slabs};
     const int units = p.big ? 8 : 4, per_cu = p.big ? 1 : 2;
-    q.m_tiles = int(ceil_div(a.rbs, units));
-    q.n_tiles = int(ceil_div(b.rbs, units));
+    q.m_tiles = int(ceil_div(q.a.rbs, units));
+    q.n_tiles = int(ceil_div(q.b.rbs, units));
     if (q.panel > q.n_tiles) q.panel = q.n_tiles;
     const int64_t total = int64_t(q.m_tiles) * q.n_tiles * q.splits;
     int64_t per_die = ceil_div(total, kWideDies);
     if (per_die > 32 * per_cu) per_die = 32 * per_cu;
     TMA_TIMED(name, s);
     const dim3 grid(unsigned(per_die * kWideDies)), block(256);
-    if (p.big) hipLaunchKernelGGL((wide_gemm_kernel<8, 8, 2, 2, 4, Epi>), grid, block, 0, s, q, e);
-    else hipLaunchKernelGGL((wide_gemm_kernel<4, 4, 2, 2, 3, Epi>), grid, block, 0, s, q, e);
+    if (p.big) hipLaunchKernelGGL((wide_gemm_kernel<8, 8, 2, 2, 4, kDirect, Epi>), grid, block, 0, s, q, e);
+    else hipLaunchKernelGGL((wide_gemm_kernel<4, 4, 2, 2, 3, kDirect, Epi>), grid, block, 0, s, q, e);
     return check_launch(name);
+}
+// operands of type T laid out: of bf16 in b_parts parts on the weights' side, of fp32 in three on both
+template <typename T, class Epi>
+static int launch_wide(const char *name, const Packed &a, const Packed &b, int b_parts, const WidePlan &p, const Epi &e, hipStream_t s)
+{
+    WideCall q{a, b, planes_of(b_parts), 0, 0, 8, p.splits, p.split_slabs, 0, 0};
+    if constexpr (sizeof(T) == 2) {
+        return launch_wide_as<false>(name, q, p, e, s);
+    } else {
+        q.m_tiles = int(ceil_div(a.rbs, 4));
+        q.n_tiles = int(ceil_div(b.rbs, 4));
+        if (q.panel > q.n_tiles) q.panel = q.n_tiles;
+        const int64_t blocks = ceil_div(int64_t(q.m_tiles) * q.n_tiles * q.splits, kWideDies) * kWideDies;
+        if (blocks > INT32_MAX) return fail(TMA_ERR_BAD_SHAPE, "%s: too many tiles", name);
+        TMA_TIMED(name, s);
+        hipLaunchKernelGGL(wide_split_kernel<Epi>, dim3(unsigned(blocks)), dim3(256), 0, s, q, e);
+        return check_launch(name);
+    }
 }
 
 template <typename T>
@@ -550,6 +566,29 @@ struct ForwardPlan {
     Packed a, b;
     size_t bytes;
 };
+// Rows that a product takes where they lie (see WideCall).  (A tile's rows are within 32 bits of each other.)  That takes their pass off and a tenth more time, for
+// half lines of memory: 1,000,003 rows 256 -> 256 690 -> 500 us, 8,192 rows 8192 -> 2048 290 -> 280, 2048 -> 2 x 8192 530 -> 565.
+template <typename T>
+inline bool direct_rows(const T *X, int64_t ldx, int32_t F_in, int n_units)
+{
+    return sizeof(T) == 2 && whole_rows(X, ldx) && F_in % 32 == 0 && ldx <= (1 << 22) && n_units <= 128;
+}
+
+// the product of laid-out weights and of rows, which are laid out here where they have to be
+template <typename T, class Epi>
+static int forward_product(const char *fn, const char *name, int64_t n, const T *X, int64_t ldx, int32_t F_in, ForwardPlan p, bool reads, const Epi &e, hipStream_t s)
+{
+    const WidePlan w = plan_rows(p.a, p.b, reads);
+    if constexpr (sizeof(T) == 2)
+        if (direct_rows(X, ldx, F_in, p.b.rbs)) {
+            p.a.at = const_cast<char *>(reinterpret_cast<const char *>(X));
+            return launch_wide_as<true>(name, WideCall{p.a, p.b, planes_of(1), 0, 0, 8, w.splits, w.split_slabs, ldx, n}, w, e, s);
+        }
+    launch_pack_rows<T, kPartsOf<T>>("wide_pack_rows", X, nullptr, ldx, n, F_in, false, p.a, s);
+    if (int rc = check_launch(fn)) return rc;
+    return launch_wide<T>(name, p.a, p.b, 1, w, e, s);
+}
+
 template <typename T>
 inline ForwardPlan plan_forward(int64_t n, int32_t F_in, int32_t F_out, int sides, void *ws)
 {
@@ -583,7 +622,7 @@ inline BackwardPlan plan_backward(int64_t n, int32_t F_in, int32_t F_out, int si
     p.d_cols = packed_shape(int64_t(sides) * p.padded, n);
     p.x_cols = packed_shape(F_in, n);
     p.w_rows = packed_shape(F_in, int64_t(sides) * p.padded);
-    p.weight = plan_weight(p.x_cols, p.d_cols);
+    p.weight = plan_weight(p.x_cols, p.d_cols, sizeof(T) == 4);
     const int strips = int(ceil_div(F_out, 64));
     int64_t blocks = ceil_div(4096, strips);
     if (blocks > ceil_div(n > 0 ? n : 1, 32)) blocks = ceil_div(n > 0 ? n : 1, 32);
@@ -638,7 +677,7 @@ static int wide_backward(const char *fn, const char *what, int64_t n, const T *X
     we.whole16 = N % 4 == 0 && aligned(we.out[0], 16) && (kSides == 1 || aligned(we.out[1], 16));
     char name[64];
     snprintf(name, sizeof(name), "%s_bwd_weight%s", what, sizeof(T) == 2 ? "_bf16" : "");
-    if (int rc = launch_wide(name, p.x_cols, p.d_cols, planes_of(kP, p.parts_c), p.weight, we, s)) return rc;
+    if (int rc = launch_wide<T>(name, p.x_cols, p.d_cols, p.parts_c, p.weight, we, s)) return rc;
     if (split) launch_join("wide_join", p.partial, p.weight.splits, cells * kSides, cells, cells, dW[0], kSides == 2 ? dW[1] : nullptr, s);
     if (db[0]) launch_join_sums(p.sums, p.row_blocks, kSides, p.padded, N, db[0], db[1], s);
     if (int rc = check_launch(fn)) return rc;
@@ -647,8 +686,7 @@ static int wide_backward(const char *fn, const char *what, int64_t n, const T *X
     if (int rc = check_launch(fn)) return rc;
     const ResidualEpilogue<T> re{nullptr, dX, R, 0, ld_dx, ldr, n, nullptr, F_in, TMA_ACT_NONE, whole_rows(dX, ld_dx), R && whole_rows(R, ldr), false};
     snprintf(name, sizeof(name), "%s_bwd_data%s", what, sizeof(T) == 2 ? "_bf16" : "");
-    const Planes planes = planes_of(kP, kP);
-    return launch_wide(name, p.d_rows, p.w_rows, planes, plan_rows(p.d_rows, p.w_rows, planes, R != nullptr), re, s);
+    return launch_wide<T>(name, p.d_rows, p.w_rows, 1, plan_rows(p.d_rows, p.w_rows, R != nullptr), re, s);
 }
 
 // every number of a call that asks for a workspace, too

@@ -1,0 +1,92 @@
+// Products of fp32 operands, laid out in three bf16 parts each (wide_gemm.hpp; why three parts and six products suffice: gemm_split.hpp).
+//
+// A slab is 16 k-values of all parts of 128 rows and 128 columns, 24 KB, fetched once and multiplied six times: 192 cycles of a matrix unit for 16 k-values of a
+// fragment, where the fp32 instruction takes 512.  The product of the first parts has accumulators of its own, the other five, 2^-8 and less of
+// it, share the rest.  Two blocks a compute unit, one tile each: one multiplies while the other waits, fills its ring or writes.
+// (Plane after plane through the bf16 kernel, six sweeps over operands that no cache holds: weight gradients of 128 x 512 from 125,237 rows 199 us, so 127; 30,011 rows
+// 301 -> 777 146 and 111, their input gradient 147 and 117.)
+#pragma once
+#include "wide_gemm.hpp"
+
+namespace tma {
+
+template <class Epi>
+__global__ __launch_bounds__(256, 2) void wide_split_kernel(WideCall q, Epi epi)
+{
+    constexpr int F = 4, T = 2, kStages = 3, kUnits = 6 * F, kLoads = 6, kStageBytes = kUnits * kUnitBytes;
+    __shared__ __attribute__((aligned(1024))) uint4 ring[kStages * kUnits * 64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / 2, wn = wave % 2;
+    const int64_t total = int64_t(q.m_tiles) * q.n_tiles * q.splits, per_die = (total + kWideDies - 1) / kWideDies;
+    const int64_t work = blockIdx.x % kWideDies * per_die + blockIdx.x / kWideDies;
+    if (blockIdx.x / kWideDies >= per_die || work >= total) return;
+    const WideTile tile = wide_tile(q, work);
+    const int steps = q.slabs_of(tile.split) * 2;
+
+    // A slab in LDS: [operand][part][unit].  This wavefront fetches half of one operand's: parts 0 0 0 0 1 1 or 1 1 2 2 2 2, units 0 1 2 3 0 1 or 2 3 0 1 2 3, in
+    // three pairs of neighbours.
+    const bool rows_side = wave < 2;
+    const int half = wave & 1;
+    const Packed &o = rows_side ? q.a : q.b;
+    const char *first = o.at + o.unit((rows_side ? tile.m : tile.n) * F, int64_t(tile.split) * q.split_slabs * 2);
+    const char *from[3] = {first + half * (o.plane() + 2 * kUnitBytes), first + half * 2 * o.plane() + (half ? 0 : 2 * kUnitBytes),
+                           first + (1 + half) * o.plane() + (half ? 2 * kUnitBytes : 0)};
+    const uint32_t ring0 = lds_address(&ring[0]) + uint32_t(wave * kLoads * kUnitBytes), lane_at = uint32_t(lane * 16);
+    auto fetch = [&](int step) {
+        const uint32_t to = ring0 + uint32_t(step % kStages * kStageBytes);
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+            const uint64_t at = reinterpret_cast<uint64_t>(from[p]) + uint64_t(uint32_t(step)) * (8 * kUnitBytes);
+            const char *base = reinterpret_cast<const char *>(uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(int(at >> 32)))) << 32 |
+                                                              uint32_t(__builtin_amdgcn_readfirstlane(int(at))));
+            fetch_unit(to + uint32_t(2 * p * kUnitBytes), base, lane_at);
+            fetch_unit(to + uint32_t((2 * p + 1) * kUnitBytes), base, lane_at + uint32_t(kUnitBytes));
+        }
+    };
+    floatx16 sum[T][T], rest[T][T];
+#pragma unroll
+    for (int j = 0; j < T; ++j)
+#pragma unroll
+        for (int i = 0; i < T; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sum[j][i][r] = rest[j][i][r] = 0.0f;
+    fetch(0);
+    if (steps > 1) fetch(1);
+    for (int s = 0; s < steps; ++s) {
+        if (s + 1 < steps) wait_and_meet<kLoads>();
+        else wait_and_meet<0>();
+        if (s + 2 < steps) fetch(s + 2);      // into the place that every wavefront has read before this meeting
+        const uint4 *slab = &ring[s % kStages * (kUnits * 64) + lane];
+        uint4 a[3][T], b[3][T];
+#pragma unroll
+        for (int p = 0; p < 3; ++p)
+#pragma unroll
+            for (int i = 0; i < T; ++i) {
+                a[p][i] = slab[(p * F + wm * T + i) * 64];
+                b[p][i] = slab[(3 * F + p * F + wn * T + i) * 64];
+            }
+        auto add = [&](int pa, int pb, floatx16 (&to)[T][T]) {
+#pragma unroll
+            for (int j = 0; j < T; ++j)
+#pragma unroll
+                for (int i = 0; i < T; ++i)
+                    to[j][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, b[pb][j]), __builtin_bit_cast(bf16x8, a[pa][i]), to[j][i], 0, 0, 0);
+        };
+        add(0, 0, sum);
+        add(1, 0, rest);
+        add(0, 1, rest);
+        add(1, 1, rest);
+        add(2, 0, rest);
+        add(0, 2, rest);
+    }
+#pragma unroll
+    for (int j = 0; j < T; ++j)
+#pragma unroll
+        for (int i = 0; i < T; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sum[j][i][r] += rest[j][i][r];
+    wait_and_meet<0>();      // the ring is read: its place takes the results
+    constexpr int S = Epi::kSides;
+    write_out<T, T>(epi, sum, int64_t(tile.m) * (F * 32) + wm * T * 32, (tile.n * F + wn * T) / S * 32, tile.split, reinterpret_cast<float *>(&ring[wave * 512]), lane);
+}
+
+}  // namespace tma
