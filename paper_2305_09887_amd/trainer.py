@@ -37,15 +37,20 @@ class LocalTrainer:
     SplitMix64(dropout_seed, l) and the step's number, which is counted on the device, so that a captured step draws anew at every
     replay.  ``node_kinds`` [n] int32 in [0, ``n_kinds``) (MLP encoder): every node is of one of several kinds, and a layer
     has weights per kind, W [n_kinds, F_in, F_out] and bias [n_kinds, F_out].
+
+    ``block_width`` = F > 0 (MLP encoder): a hidden layer whose output is as wide as its input becomes a residual block with a
+    gated layer of width F, H' = H + (silu(H W_gate + b_gate) (.) (H W_up + b_up)) W_down + b_down; its parameters are these six
+    in the order W_gate, W_up, b_gate, b_up, W_down, b_down.  ``clip_norm`` = c > 0: before the optimizer the gradients, all of
+    them together, are held to the norm c; ``grad_norm`` [1] is what their norm was.
     """
 
     # (what a subclass with buffers of its own leaves as it is)
-    norm_groups, dropout, n_kinds, training = 0, 0.0, 0, True
+    norm_groups, dropout, n_kinds, training, block_width = 0, 0.0, 0, True, 0
 
     def __init__(self, rowptr, colidx, inv_deg, X, labels, dims, params=None, stream=None,
                  rowptr_T=None, colidx_T=None, norm_act=False, optimizer="sgd", encoder="sage",
                  decoder_dims=None, batch_size=0, batch_seed=0, nnz=None, norm_groups=0, dropout=0.0, dropout_seed=0,
-                 node_kinds=None, n_kinds=0):
+                 node_kinds=None, n_kinds=0, block_width=0, clip_norm=0.0):
         self.norm_act = bool(norm_act)
         self.norm_groups, self.dropout, self.n_kinds = int(norm_groups), float(dropout), int(n_kinds)
         if self.norm_groups < 0 or (self.norm_groups and (not self.norm_act or any(f % self.norm_groups for f in dims[1:-1]))):
@@ -54,6 +59,11 @@ class LocalTrainer:
             raise B.TmaError("LocalTrainer: dropout must be in [0, 1)")
         if (node_kinds is None) != (self.n_kinds == 0) or self.n_kinds < 0 or (self.n_kinds and encoder != "mlp"):
             raise B.TmaError("LocalTrainer: node_kinds and n_kinds come together, with the MLP encoder")
+        self.block_width = int(block_width)
+        if self.block_width < 0 or (self.block_width and (encoder != "mlp" or self.norm_act or self.n_kinds
+                                                          or not any(a == b for a, b in zip(dims[:-2], dims[1:-1])))):
+            raise B.TmaError("LocalTrainer: block_width needs the MLP encoder without norm_act or kinds, and a hidden layer as wide as its input")
+        self._set_clipping(clip_norm, X.device)
         self.dec_dims = list(decoder_dims) if decoder_dims is not None else None
         if self.dec_dims is not None:
             if self.dec_dims[0] != dims[-1] or self.dec_dims[-1] != 1 or len(self.dec_dims) < 2 or batch_size < 1:
@@ -83,7 +93,9 @@ class LocalTrainer:
             raise B.TmaError("LocalTrainer: X width differs from dims[0]")
 
         n_w = 2 if encoder == "sage" else 1
-        self.n_params = max(self.n_kinds, 1) * sum(n_w * fi * fo + fo for fi, fo in zip(dims[:-1], dims[1:]))
+        F = self.block_width
+        self.n_params = max(self.n_kinds, 1) * sum(3 * fi * F + 2 * F + fi if self._is_block(l) else n_w * fi * fo + fo
+                                                   for l, (fi, fo) in enumerate(zip(dims[:-1], dims[1:])))
         if self.norm_act:
             self.n_params += sum(2 * fo + 1 for fo in dims[1:-1])
         if self.dec_dims is not None:
@@ -130,6 +142,15 @@ class LocalTrainer:
             self.set_kinds(node_kinds)
         else:
             ws_bytes = max(B.tma_dense_bwd_workspace_bytes(self.n, fi, fo) for fi, fo in pairs)
+            # a block's pre-activations and the gated layer's result, kept for backward; that result's gradient
+            self.gates = {l: tuple(B._padded(self.n, F, self.dtype, dev) for _ in range(3)) for l in range(self.L) if self._is_block(l)}
+            self.dgated = B._padded(self.n, F, self.dtype, dev) if F else None
+            for l in self.gates:
+                f = dims[l]
+                ws_bytes = max(ws_bytes, B.tma_gated_dense_fwd_workspace_bytes(self.n, f, F, dt),
+                               B.tma_gated_dense_bwd_workspace_bytes(self.n, f, F, dt, l > 0),
+                               B.tma_dense_residual_fwd_workspace_bytes(self.n, F, f, dt),
+                               B.tma_dense_residual_bwd_workspace_bytes(self.n, F, f, B.TMA_ACT_NONE, dt))
         ws_bytes = max(ws_bytes, B.tma_loss_workspace_bytes(self.n, dims[-1]))
         if self.norm_groups and self.L > 1:
             ws_bytes = max(ws_bytes, max(B.tma_groupnorm_act_bwd_workspace_bytes(self.n, f, self.norm_groups, 1, dt) for f in dims[1:-1]))
@@ -153,6 +174,17 @@ class LocalTrainer:
             self.drop_seeds = [B.tma_mix64(int(dropout_seed), l) for l in range(self.L)]
             self.drop_step = torch.zeros(1, dtype=torch.int64, device=dev)
             self.stream.wait_stream(torch.cuda.current_stream(dev))
+
+    def _set_clipping(self, clip_norm, dev):
+        self.clip_norm = float(clip_norm)
+        if not 0.0 <= self.clip_norm < float("inf"):
+            raise B.TmaError("trainer: clip_norm must be a number from 0 on")
+        if self.clip_norm:
+            self.grad_norm = torch.zeros(1, dtype=torch.float32, device=dev)
+            self.clip_ws = torch.empty(B.tma_grad_norm_workspace_bytes(1), dtype=torch.uint8, device=dev)
+
+    def _is_block(self, l):
+        return bool(self.block_width) and l < self.L - 1 and self.dims[l] == self.dims[l + 1]
 
     def set_kinds(self, node_kinds):
         """The kind of each of the trainer's nodes (int32 in [0, n_kinds)); waits for the stream, to see that each has one.  The list goes
@@ -199,8 +231,12 @@ class LocalTrainer:
     def _views(self, flat):
         out, o = [], 0
         for l, (fi, fo) in enumerate(zip(self.dims[:-1], self.dims[1:])):
-            layer, E = [], self.n_kinds
-            if E:
+            layer, E, F = [], self.n_kinds, self.block_width
+            if self._is_block(l):
+                for shape in ((fi, F), (fi, F), (F,), (F,), (F, fi), (fi,)):
+                    n = shape[0] * (shape[1] if len(shape) == 2 else 1)
+                    layer.append(flat[o:o + n].view(shape)); o += n
+            elif E:
                 layer.append(flat[o:o + E * fi * fo].view(E, fi, fo)); o += E * fi * fo
                 layer.append(flat[o:o + E * fo].view(E, fo)); o += E * fo
             else:
@@ -234,7 +270,23 @@ class LocalTrainer:
                 for dst, src in zip(mine, given):
                     dst.copy_(torch.as_tensor(src, dtype=torch.float32).reshape(dst.shape))
 
+    def _block_fwd(self, l, out):
+        W_gate, W_up, b_gate, b_up, W_down, b_down = self.layers[l]
+        G, U, A = self.gates[l]
+        B.tma_gated_dense_fwd(self.H[l], W_gate, W_up, b_gate, b_up, B.TMA_ACT_SILU, G_out=G, U_out=U, H_out=A, ws=self.ws,
+                              stream=self.stream)
+        B.tma_dense_residual_fwd(A, W_down, b_down, B.TMA_ACT_NONE, R=self.H[l], Y_out=out, ws=self.ws, stream=self.stream)
+
+    def _block_bwd(self, l):
+        W_gate, W_up, _, _, W_down, _ = self.layers[l]
+        g, (G, U, A), d = self.grads[l], self.gates[l], self.dH[l + 1]
+        B.tma_dense_residual_bwd(A, None, d, W_down, B.TMA_ACT_NONE, dW=g[4], dbias=g[5], dX_out=self.dgated, ws=self.ws, stream=self.stream)
+        B.tma_gated_dense_bwd(self.H[l], G, U, self.dgated, W_gate, W_up, B.TMA_ACT_SILU, R=d, dW_gate=g[0], dW_up=g[1], db_gate=g[2],
+                              db_up=g[3], dX_out=self.dH[l], need_dX=l > 0, ws=self.ws, stream=self.stream)
+
     def _layer_fwd(self, l, act, out):
+        if self._is_block(l):
+            return self._block_fwd(l, out)
         lin = self.layers[l][:self.n_lin]
         if self.encoder == "sage":
             Wt = None
@@ -262,6 +314,8 @@ class LocalTrainer:
             B.tma_dense_fwd(self.H[l], lin[0], lin[1], act, Y_out=out, stream=self.stream)
 
     def _layer_bwd(self, l, act, out_act):
+        if self._is_block(l):
+            return self._block_bwd(l)
         lin, g = self.layers[l][:self.n_lin], self.grads[l][:self.n_lin]
         if self.encoder == "sage":
             B.tma_sage_layer_bwd(self.rowptr_T, self.colidx_T, self.inv_deg, self.H[l], self.M[l], out_act,
@@ -380,6 +434,8 @@ class LocalTrainer:
             self._mark("bwd", l)
 
     def _optimizer_step(self, lr: float):
+        if self.clip_norm:
+            B.tma_grad_clip([self.dW], self.clip_norm, norm_out=self.grad_norm, ws=self.clip_ws, stream=self.stream)
         if self.optimizer == "adam":
             B.tma_adam_step(self.W, self.dW, self.adam_m, self.adam_v, lr, self.steps_done + 1, stream=self.stream)
         else:
@@ -461,8 +517,9 @@ class SampledLinkTrainer(LocalTrainer):
 
     def __init__(self, rowptr, colidx, nnz, X, dims, decoder_dims, fanouts, batch_size, batch_seed=0, params=None,
                  decoder_params=None, stream=None, optimizer="sgd", norm_act=False, nnz_cap=None, encoder="sage",
-                 device_counts=True):
+                 device_counts=True, clip_norm=0.0):
         self.device_counts = bool(device_counts)
+        self._set_clipping(clip_norm, X.device)
         if len(fanouts) != len(dims) - 1:
             raise B.TmaError("SampledLinkTrainer: one fan-out per layer")
         if colidx.numel() < nnz or (nnz_cap is not None and nnz_cap < nnz):
