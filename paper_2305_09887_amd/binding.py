@@ -8,6 +8,7 @@ there is no fallback path.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from array import array
 
@@ -932,9 +933,11 @@ def _launch(device, stream, call, *args):
     """call(*args, stream) with the tensors' device as the current one (the library launches on that) and, where none is
     given, that device's current stream."""
     index = device.index
-    s = (torch.cuda.current_stream(index) if stream is None else stream).cuda_stream
+    s = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
     if index == torch.cuda.current_device():
-        _check(call(*args, s))
+        rc = call(*args, s)
+        if rc != 0:
+            _check(rc)
     else:
         with torch.cuda.device(index):
             _check(call(*args, s))
@@ -1165,6 +1168,14 @@ def _forward_room(ws, nbytes, dev, stream):
     return _workspace(nbytes, dev, stream) if ws is None and nbytes else ws
 
 
+def _rows_of(t, name):
+    """(rows, columns, leading dimension) of a matrix whose rows do not overlap."""
+    n, cols, ld = _rows_ld(t, name)
+    if ld < cols:
+        raise TmaError(f"{name}: rows overlap")
+    return n, cols, ld
+
+
 def _rows_or_none(t, name, shape, dtype):
     """Address and leading dimension of a [rows, cols] tensor, or of none."""
     if t is None:
@@ -1178,6 +1189,7 @@ def _weight_shape(where, name, W, F_in):
     return W.shape[1]
 
 
+@functools.lru_cache(256)
 def tma_gated_dense_fwd_workspace_bytes(n: int, F_in: int, F_out: int, dtype: int) -> int:
     return int(lib().tma_gated_dense_fwd_workspace_bytes(n, F_in, F_out, dtype))
 
@@ -1188,7 +1200,7 @@ def tma_gated_dense_fwd(X, W_gate, W_up, b_gate=None, b_up=None, act: int = TMA_
     are None with ``save`` false."""
     where = "tma_gated_dense_fwd"
     dev = _device(where, X, W_gate, W_up, b_gate, b_up, G_out, U_out, H_out, ws)
-    n, F_in, ldx = _rows_ld(X, "X")
+    n, F_in, ldx = _rows_of(X, "X")
     F_out = _weight_shape(where, "W_gate", W_gate, F_in)
     dtype = _feat_dtype(X)
     if not save:
@@ -1202,7 +1214,7 @@ def tma_gated_dense_fwd(X, W_gate, W_up, b_gate=None, b_up=None, act: int = TMA_
     _same_ld(G_out, U_out, f"{where}: G_out / U_out")
     ws = _forward_room(ws, tma_gated_dense_fwd_workspace_bytes(n, F_in, F_out, dtype), dev, stream)
     G, ldg = _rows_or_none(G_out, "G_out", (n, F_out), X.dtype)
-    _launch(dev, stream, lib().tma_gated_dense_fwd, n, X.data_ptr(), _rows_like(X, "X", (n, F_in), X.dtype), F_in,
+    _launch(dev, stream, lib().tma_gated_dense_fwd, n, X.data_ptr(), ldx, F_in,
             _vector(W_gate, "W_gate", (F_in, F_out), torch.float32), _vector(W_up, "W_up", (F_in, F_out), torch.float32),
             _vector(b_gate, "b_gate", (F_out,), torch.float32), _vector(b_up, "b_up", (F_out,), torch.float32), F_out, act, dtype,
             G, _rows_or_none(U_out, "U_out", (n, F_out), X.dtype)[0], ldg, H_out.data_ptr(),
@@ -1210,6 +1222,7 @@ def tma_gated_dense_fwd(X, W_gate, W_up, b_gate=None, b_up=None, act: int = TMA_
     return H_out, G_out, U_out
 
 
+@functools.lru_cache(256)
 def tma_gated_dense_bwd_workspace_bytes(n: int, F_in: int, F_out: int, dtype: int, need_dX: bool = True) -> int:
     return int(lib().tma_gated_dense_bwd_workspace_bytes(n, F_in, F_out, dtype, 1 if need_dX else 0))
 
@@ -1219,7 +1232,7 @@ def tma_gated_dense_bwd(X, G, U, dH, W_gate, W_up, act: int = TMA_ACT_SILU, R=No
     """Returns (dW_gate, dW_up, db_gate or None, db_up or None, dX or None); R, where given, is added to dX."""
     where = "tma_gated_dense_bwd"
     dev = _device(where, X, G, U, dH, W_gate, W_up, R, dW_gate, dW_up, db_gate, db_up, dX_out, ws)
-    n, F_in, _ = _rows_ld(X, "X")
+    n, F_in, ldx = _rows_of(X, "X")
     F_out = _weight_shape(where, "W_gate", W_gate, F_in)
     dtype = _feat_dtype(X)
     _same_ld(G, U, f"{where}: G / U")
@@ -1232,7 +1245,7 @@ def tma_gated_dense_bwd(X, G, U, dH, W_gate, W_up, act: int = TMA_ACT_SILU, R=No
     if ws is None:
         ws = _workspace(tma_gated_dense_bwd_workspace_bytes(n, F_in, F_out, dtype, need_dX), dev, stream)
     _rows_like(U, "U", (n, F_out), X.dtype)
-    _launch(dev, stream, lib().tma_gated_dense_bwd, n, X.data_ptr(), _rows_like(X, "X", (n, F_in), X.dtype), G.data_ptr(), U.data_ptr(),
+    _launch(dev, stream, lib().tma_gated_dense_bwd, n, X.data_ptr(), ldx, G.data_ptr(), U.data_ptr(),
             _rows_like(G, "G", (n, F_out), X.dtype), dH.data_ptr(), _rows_like(dH, "dH", (n, F_out), X.dtype),
             _vector(W_gate, "W_gate", (F_in, F_out), torch.float32), _vector(W_up, "W_up", (F_in, F_out), torch.float32), F_in, F_out,
             act, dtype, _vector(dW_gate, "dW_gate", (F_in, F_out), torch.float32), _vector(dW_up, "dW_up", (F_in, F_out), torch.float32),
@@ -1241,6 +1254,7 @@ def tma_gated_dense_bwd(X, G, U, dH, W_gate, W_up, act: int = TMA_ACT_SILU, R=No
     return dW_gate, dW_up, db_gate, db_up, dX_out
 
 
+@functools.lru_cache(256)
 def tma_dense_residual_fwd_workspace_bytes(n: int, F_in: int, F_out: int, dtype: int) -> int:
     return int(lib().tma_dense_residual_fwd_workspace_bytes(n, F_in, F_out, dtype))
 
@@ -1251,7 +1265,7 @@ def tma_dense_residual_fwd(X, W, bias=None, act: int = TMA_ACT_NONE, R=None, sav
     ``save`` is true or Z_out given.  R may be Y_out."""
     where = "tma_dense_residual_fwd"
     dev = _device(where, X, W, bias, R, Z_out, Y_out, ws)
-    n, F_in, _ = _rows_ld(X, "X")
+    n, F_in, ldx = _rows_of(X, "X")
     F_out = _weight_shape(where, "W", W, F_in)
     dtype = _feat_dtype(X)
     if save and Z_out is None:
@@ -1259,13 +1273,14 @@ def tma_dense_residual_fwd(X, W, bias=None, act: int = TMA_ACT_NONE, R=None, sav
     if Y_out is None:
         Y_out = _new_rows(n, F_out, X.dtype, dev, stream)
     ws = _forward_room(ws, tma_dense_residual_fwd_workspace_bytes(n, F_in, F_out, dtype), dev, stream)
-    _launch(dev, stream, lib().tma_dense_residual_fwd, n, X.data_ptr(), _rows_like(X, "X", (n, F_in), X.dtype), F_in,
+    _launch(dev, stream, lib().tma_dense_residual_fwd, n, X.data_ptr(), ldx, F_in,
             _vector(W, "W", (F_in, F_out), torch.float32), _vector(bias, "bias", (F_out,), torch.float32), F_out, act, dtype,
             *_rows_or_none(R, "R", (n, F_out), X.dtype), *_rows_or_none(Z_out, "Z_out", (n, F_out), X.dtype), Y_out.data_ptr(),
             _rows_like(Y_out, "Y_out", (n, F_out), X.dtype), *_room(ws))
     return Y_out, Z_out
 
 
+@functools.lru_cache(256)
 def tma_dense_residual_bwd_workspace_bytes(n: int, F_in: int, F_out: int, act: int, dtype: int, need_dX: bool = True) -> int:
     return int(lib().tma_dense_residual_bwd_workspace_bytes(n, F_in, F_out, act, dtype, 1 if need_dX else 0))
 
@@ -1275,7 +1290,7 @@ def tma_dense_residual_bwd(X, Z, dY, W, act: int = TMA_ACT_NONE, R=None, dW=None
     """Returns (dW, dbias or None, dX or None); Z may be None without an activation; R, where given, is added to dX."""
     where = "tma_dense_residual_bwd"
     dev = _device(where, X, Z, dY, W, R, dW, dbias, dX_out, ws)
-    n, F_in, _ = _rows_ld(X, "X")
+    n, F_in, ldx = _rows_of(X, "X")
     F_out = _weight_shape(where, "W", W, F_in)
     dtype = _feat_dtype(X)
     if act == TMA_ACT_NONE:
@@ -1288,7 +1303,7 @@ def tma_dense_residual_bwd(X, Z, dY, W, act: int = TMA_ACT_NONE, R=None, dW=None
     dX_out = None if not need_dX else _new_rows(n, F_in, X.dtype, dev, stream) if dX_out is None else dX_out
     if ws is None:
         ws = _workspace(tma_dense_residual_bwd_workspace_bytes(n, F_in, F_out, act, dtype, need_dX), dev, stream)
-    _launch(dev, stream, lib().tma_dense_residual_bwd, n, X.data_ptr(), _rows_like(X, "X", (n, F_in), X.dtype),
+    _launch(dev, stream, lib().tma_dense_residual_bwd, n, X.data_ptr(), ldx,
             *_rows_or_none(Z, "Z", (n, F_out), X.dtype), dY.data_ptr(), _rows_like(dY, "dY", (n, F_out), X.dtype),
             _vector(W, "W", (F_in, F_out), torch.float32), F_in, F_out, act, dtype, _vector(dW, "dW", (F_in, F_out), torch.float32),
             _vector(dbias, "dbias", (F_out,), torch.float32), *_rows_or_none(dX_out, "dX_out", (n, F_in), X.dtype),
@@ -1296,6 +1311,7 @@ def tma_dense_residual_bwd(X, Z, dY, W, act: int = TMA_ACT_NONE, R=None, dW=None
     return dW, dbias, dX_out
 
 
+@functools.lru_cache(256)
 def tma_grad_norm_workspace_bytes(n_tensors: int) -> int:
     return int(lib().tma_grad_norm_workspace_bytes(n_tensors))
 

@@ -9,7 +9,9 @@
 
 namespace tma {
 
-constexpr int kListed = 128, kChunk = 1 << 14, kNormBlocks = 2048, kNormThreads = 256;
+constexpr int kListed = 128, kNormBlocks = 2048, kNormThreads = 256;
+template <typename T>
+constexpr int kChunk = (1 << 16) / sizeof(T);      // 64 KB: the search for its tensor takes a microsecond
 
 struct GradTensors {
     const void *in[kListed];
@@ -81,8 +83,8 @@ __global__ __launch_bounds__(kNormThreads) void grad_squares_kernel(GradTensors 
     double sum[4] = {0, 0, 0, 0};
     for (int c = blockIdx.x; c < q.chunks; c += gridDim.x) {
         const int i = __builtin_amdgcn_readfirstlane(tensor_of(q, c));
-        const int64_t at = int64_t(c - q.first[i]) * kChunk, left = q.size[i] - at;
-        add_squares(static_cast<const T *>(q.in[i]) + at, left < kChunk ? left : kChunk, sum);
+        const int64_t at = int64_t(c - q.first[i]) * kChunk<T>, left = q.size[i] - at;
+        add_squares(static_cast<const T *>(q.in[i]) + at, left < kChunk<T> ? left : kChunk<T>, sum);
     }
     const double all = block_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
     if (threadIdx.x == 0) partial[blockIdx.x] = all;
@@ -134,7 +136,7 @@ __global__ __launch_bounds__(kNormThreads) void grad_scale_kernel(GradTensors q,
     for (int b = blockIdx.x; b < q.chunks; b += gridDim.x) {
         const int c = q.chunks - 1 - b;
         const int i = __builtin_amdgcn_readfirstlane(tensor_of(q, c));
-        const int64_t at = int64_t(c - q.first[i]) * kChunk, left = q.size[i] - at, n = left < kChunk ? left : kChunk;
+        const int64_t at = int64_t(c - q.first[i]) * kChunk<T>, left = q.size[i] - at, n = left < kChunk<T> ? left : kChunk<T>;
         const T *in = static_cast<const T *>(q.in[i]) + at;
         T *out = static_cast<T *>(o.out[i]) + at;
         if (in == out && factor == 1.0f) continue;
@@ -153,13 +155,14 @@ __global__ __launch_bounds__(kNormThreads) void grad_scale_kernel(GradTensors q,
 }
 
 // the next of the list's tensors, from `begin` on, as arguments; empty ones are left out.  Returns where the rest begins.
+template <typename T>
 static int list_tensors(int begin, int n_tensors, const void *const *h_grads, void *const *h_outs, const int64_t *h_sizes, GradTensors &q, GradOutputs &o)
 {
     q.count = q.chunks = 0;
     int i = begin;
     for (; i < n_tensors && q.count < kListed; ++i) {
         if (h_sizes[i] == 0) continue;
-        const int64_t more = ceil_div(h_sizes[i], kChunk);
+        const int64_t more = ceil_div(h_sizes[i], kChunk<T>);
         if (q.chunks + more > INT32_MAX / 2) break;     // (one tensor alone is below this: see the checks)
         q.in[q.count] = h_grads[i];
         o.out[q.count] = h_outs ? h_outs[i] : const_cast<void *>(h_grads[i]);
@@ -182,7 +185,7 @@ static int grad_norm(const char *fn, int32_t n_tensors, const void *const *h_gra
     GradOutputs o;
     int count = 0;
     for (int at = 0; at < n_tensors;) {
-        at = list_tensors(at, n_tensors, h_grads, h_outs, h_sizes, q, o);
+        at = list_tensors<T>(at, n_tensors, h_grads, h_outs, h_sizes, q, o);
         if (!q.count) break;
         const int blocks = q.chunks < kNormBlocks ? q.chunks : kNormBlocks;
         TMA_REQUIRE(size_t(count + blocks) * sizeof(double) <= room, TMA_ERR_WORKSPACE_TOO_SMALL, "%s: workspace for %d sums", fn, count + blocks);
@@ -198,7 +201,7 @@ static int grad_norm(const char *fn, int32_t n_tensors, const void *const *h_gra
     }
     bool first = true;
     for (int at = 0; at < n_tensors;) {
-        at = list_tensors(at, n_tensors, h_grads, h_outs, h_sizes, q, o);
+        at = list_tensors<T>(at, n_tensors, h_grads, h_outs, h_sizes, q, o);
         if (!q.count) break;
         const int blocks = q.chunks < kNormBlocks ? q.chunks : kNormBlocks;
         TMA_TIMED(sizeof(T) == 2 ? "grad_scale_bf16" : "grad_scale", s);

@@ -182,7 +182,8 @@ __global__ __launch_bounds__(kPackThreads) void pack_rows_kernel(RowsPack q)
     }
 }
 
-// Operand rows are the columns of src [rows, cols], k along its rows: a thread takes eight rows of a column, 32 threads of a half wavefront write 512 bytes.
+// Operand rows are the columns of src [rows, cols], k along its rows: a thread takes eight rows of kTogether columns (two of bf16, where words allow it), 32 threads
+// of a half wavefront write 512 bytes.
 // `sides` matrices give every other unit of 32 operand rows each (a gated layer's two weights).
 struct ColsPack {
     const void *src[2];
@@ -191,28 +192,40 @@ struct ColsPack {
     bool weights;
     Packed out;
 };
-template <typename T, int kParts>
+template <typename T, int kParts, int kTogether>
 __global__ __launch_bounds__(kPackThreads) void pack_cols_kernel(ColsPack q)
 {
-    const int t = threadIdx.x, c_in = t % 128, half = t / 128;
-    const int side_rbs = q.out.rbs / q.sides, strips = (side_rbs + 3) / 4;
+    constexpr int kWidth = 128 * kTogether;
+    const int t = threadIdx.x, c_in = t % 128 * kTogether, half = t / 128;
+    const int side_rbs = q.out.rbs / q.sides, strips = (side_rbs * kUnitRows + kWidth - 1) / kWidth;
     const int64_t all = int64_t(strips) * q.out.kgs * q.sides;
-    const int slot = half * 32 + (q.weights ? fragment_row(c_in % 32) : c_in % 32);
     for (int64_t i = blockIdx.x; i < all; i += gridDim.x) {
         const int strip = int(i % strips), side = int(i / strips % q.sides);
         const int64_t kg = i / strips / q.sides;
-        const int64_t col = int64_t(strip) * 128 + c_in, k0 = kg * kUnitK + half * 8;
-        const int rb = strip * 4 + c_in / 32;
+        const int64_t col = int64_t(strip) * kWidth + c_in, k0 = kg * kUnitK + half * 8;
+        const int64_t rb = col / kUnitRows;
         if (rb >= side_rbs) continue;
         const T *src = static_cast<const T *>(q.src[side]) + col;
-        float v[8];
+        float v[kTogether][8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = col < q.cols && k0 + j < q.rows ? widen1(src[(k0 + j) * q.ld]) : 0.0f;
-        uint4 parts[kParts];
-        pack_eight<kParts>(v, parts);
+        for (int j = 0; j < 8; ++j) {
+            const bool in = k0 + j < q.rows;
+            if constexpr (kTogether == 2) {
+                const uint32_t w = in && col < q.cols ? *reinterpret_cast<const uint32_t *>(src + (k0 + j) * q.ld) : 0u;      // (cols is even)
+                v[0][j] = __uint_as_float(w << 16);
+                v[1][j] = __uint_as_float(w & 0xFFFF0000u);
+            } else {
+                v[0][j] = in && col < q.cols ? widen1(src[(k0 + j) * q.ld]) : 0.0f;
+            }
+        }
 #pragma unroll
-        for (int p = 0; p < kParts; ++p)
-            *reinterpret_cast<uint4 *>(q.out.at + p * q.out.plane() + q.out.unit(rb * q.sides + side, kg) + slot * 16) = parts[p];
+        for (int w = 0; w < kTogether; ++w) {
+            uint4 parts[kParts];
+            pack_eight<kParts>(v[w], parts);
+            const int c = (c_in + w) % kUnitRows, slot = half * 32 + (q.weights ? fragment_row(c) : c);
+#pragma unroll
+            for (int p = 0; p < kParts; ++p) *reinterpret_cast<uint4 *>(q.out.at + p * q.out.plane() + q.out.unit(rb * q.sides + side, kg) + slot * 16) = parts[p];
+        }
     }
 }
 
@@ -232,7 +245,12 @@ static void launch_pack_cols(const char *name, const void *first, const void *se
     const int sides = second ? 2 : 1;
     const ColsPack q{{first, second}, ld, rows, cols, sides, weights, out};
     TMA_TIMED(name, s);
-    hipLaunchKernelGGL((pack_cols_kernel<T, kParts>), dim3(pack_blocks(int64_t((out.rbs / sides + 3) / 4) * out.kgs * sides)), dim3(kPackThreads), 0, s, q);
+    if constexpr (sizeof(T) == 2)
+        if (cols % 2 == 0 && ld % 2 == 0 && aligned(first, 4) && aligned(second, 4)) {
+            hipLaunchKernelGGL((pack_cols_kernel<T, kParts, 2>), dim3(pack_blocks(ceil_div(out.rbs / sides, 8) * out.kgs * sides)), dim3(kPackThreads), 0, s, q);
+            return;
+        }
+    hipLaunchKernelGGL((pack_cols_kernel<T, kParts, 1>), dim3(pack_blocks(ceil_div(out.rbs / sides, 4) * out.kgs * sides)), dim3(kPackThreads), 0, s, q);
 }
 
 // ---- the product ---------------------------------------------------------------

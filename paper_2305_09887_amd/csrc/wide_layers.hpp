@@ -495,12 +495,12 @@ inline WidePlan plan_rows(const Packed &a, const Packed &b, bool reads)
     const int slabs = a.kgs / 2;
     return {wide_tiles(a.rbs, b.rbs, true) >= kCus * 3 / 4 && fills_big(a.rbs, b.rbs) && slabs >= (reads ? 64 : 16), 1, slabs};
 }
-// ranges of k until the tiles fill the chip, 512 rows each at least; fp32 has small tiles only
+// ranges of k until the tiles fill the chip, 512 rows each at least; fp32 has small tiles only, three a unit
 inline WidePlan plan_weight(const Packed &a, const Packed &b, bool fp32)
 {
     const int slabs = a.kgs / 2, most = slabs / 16 > 1 ? slabs / 16 : 1;
     for (bool big : {true, false}) {
-        const int64_t tiles = wide_tiles(a.rbs, b.rbs, big), slots = big ? kCus : 2 * kCus;
+        const int64_t tiles = wide_tiles(a.rbs, b.rbs, big), slots = big ? kCus : fp32 ? 3 * kCus : 2 * kCus;
         int64_t want = slots / tiles;
         want = want < 1 ? 1 : want > most ? most : want;
         if (big && (fp32 || tiles * want < kCus / 2 || !fills_big(a.rbs, b.rbs))) continue;

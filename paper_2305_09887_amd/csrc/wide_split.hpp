@@ -2,7 +2,8 @@
 //
 // A slab is 16 k-values of all parts of 128 rows and 128 columns, 24 KB, fetched once and multiplied six times: 192 cycles of a matrix unit for 16 k-values of a
 // fragment, where the fp32 instruction takes 512.  The product of the first parts has accumulators of its own, the other five, 2^-8 and less of
-// it, share the rest.  Two blocks a compute unit, one tile each: one multiplies while the other waits, fills its ring or writes.
+// it, share the rest.  Three blocks a compute unit, one tile each (two where something is added to the results, which takes registers): one multiplies while the others
+// wait, fill their ring or write (gated 128 -> 256, 125,237 rows: two 163 us, three 148).
 // (Plane after plane through the bf16 kernel, six sweeps over operands that no cache holds: weight gradients of 128 x 512 from 125,237 rows 199 us, so 127; 30,011 rows
 // 301 -> 777 146 and 111, their input gradient 147 and 117.)
 #pragma once
@@ -11,9 +12,9 @@
 namespace tma {
 
 template <class Epi>
-__global__ __launch_bounds__(256, 2) void wide_split_kernel(WideCall q, Epi epi)
+__global__ __launch_bounds__(256, Epi::kPast ? 2 : 3) void wide_split_kernel(WideCall q, Epi epi)
 {
-    constexpr int F = 4, T = 2, kStages = 3, kUnits = 6 * F, kLoads = 6, kStageBytes = kUnits * kUnitBytes;
+    constexpr int F = 4, T = 2, kStages = Epi::kPast ? 3 : 2, kUnits = 6 * F, kLoads = 6, kStageBytes = kUnits * kUnitBytes;
     __shared__ __attribute__((aligned(1024))) uint4 ring[kStages * kUnits * 64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / 2, wn = wave % 2;
     const int64_t total = int64_t(q.m_tiles) * q.n_tiles * q.splits, per_die = (total + kWideDies - 1) / kWideDies;
@@ -49,12 +50,13 @@ __global__ __launch_bounds__(256, 2) void wide_split_kernel(WideCall q, Epi epi)
         for (int i = 0; i < T; ++i)
 #pragma unroll
             for (int r = 0; r < 16; ++r) sum[j][i][r] = rest[j][i][r] = 0.0f;
-    fetch(0);
-    if (steps > 1) fetch(1);
+#pragma unroll
+    for (int s = 0; s < kStages - 1; ++s)
+        if (s < steps) fetch(s);
     for (int s = 0; s < steps; ++s) {
-        if (s + 1 < steps) wait_and_meet<kLoads>();
+        if (s + kStages - 2 < steps) wait_and_meet<(kStages - 2) * kLoads>();
         else wait_and_meet<0>();
-        if (s + 2 < steps) fetch(s + 2);      // into the place that every wavefront has read before this meeting
+        if (s + kStages - 1 < steps) fetch(s + kStages - 1);      // into the place that every wavefront has read before this meeting
         const uint4 *slab = &ring[s % kStages * (kUnits * 64) + lane];
         uint4 a[3][T], b[3][T];
 #pragma unroll
