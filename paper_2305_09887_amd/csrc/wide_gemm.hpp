@@ -41,6 +41,12 @@ inline Packed packed_shape(int64_t rows, int64_t k)
 
 // the row of a unit in which column c (of 32) of the weights' side lies
 __host__ __device__ __forceinline__ int fragment_row(int c) { return ((c >> 4) & 1) * 4 + ((c >> 2) & 3) * 8 + (c & 3); }
+// Where in a unit row r's eight k-values `half` lie, in pieces of 16 bytes.  A unit of rows is in the order of the lanes.  On the weights' side a row's two pieces are
+// neighbours, exchanged in every second eight rows: so 16 lanes that read as many rows meet in no bank, and a unit can be read along its rows as
+// well (the transposing read takes 16 k-values of four rows): the gradients of pre-activations, laid out for dW with their columns as rows, are dX's rows of k.  In every
+// second unit along k rows are four apart exchanged: such a read takes two of them at once (8,192 rows of 2 x 8192, dX 484 us without).
+__host__ __device__ __forceinline__ int rows_place(int r, int half) { return half * 32 + r; }
+__host__ __device__ __forceinline__ int weights_place(int r, int half, int kg) { return (r ^ (kg & 1) * 4) * 2 + (half ^ ((r >> 3) & 1)); }
 
 // ---- parts ---------------------------------------------------------------------
 // x as a sum of bf16 parts, each the rounding of what the ones before left over.  A finite value beyond the largest bf16 is cut instead of rounded; of an
@@ -145,7 +151,8 @@ constexpr int kPackThreads = 256;
 
 // Operand rows are the rows of src [rows, cols], k along them.  A block takes 32 rows by 64 columns at a time, through LDS: 128 bytes of a row (bf16) are read
 // at once and four whole units written.
-// The operand may come from `sides` matrices side by side along k, side_kgs units each.  weights: its rows are a fragment's columns.
+// The operand may come from `sides` matrices side by side along k, side_kgs units each.  weights: its rows are a fragment's columns, and its k-values, 32 of them,
+// stand in the order of such a unit's rows (the other operand is read along those).
 struct RowsPack {
     const void *src[2];
     int64_t ld, rows, cols;
@@ -160,14 +167,37 @@ __global__ __launch_bounds__(kPackThreads) void pack_rows_kernel(RowsPack q)
     const int t = threadIdx.x, r = t / 8, piece = t % 8;
     const int quads = (q.out.kgs + 3) / 4;
     const int64_t all = int64_t(q.out.rbs) * quads;
-    const int slot = (piece / 2) * 64 + (piece % 2) * 32 + (q.weights ? fragment_row(r) : r);
+    const int slot = (piece / 2) * 64 + (q.weights ? weights_place(fragment_row(r), piece % 2, piece / 2) : rows_place(r, piece % 2));
     for (int64_t i = blockIdx.x; i < all; i += gridDim.x) {
         const int64_t rb = i / quads, row = rb * kUnitRows + r;
         const int kg0 = int(i % quads) * 4, kg = kg0 + piece / 2;
         const int side = kg < q.side_kgs ? 0 : 1;
         const int64_t c = int64_t(kg - side * q.side_kgs) * kUnitK + piece % 2 * 8;
         float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (row < q.rows && kg < q.out.kgs) load_eight(static_cast<const T *>(q.src[side]) + row * q.ld, c, q.cols, q.whole, v);
+        if (row < q.rows && kg < q.out.kgs) {
+            const T *from = static_cast<const T *>(q.src[side]) + row * q.ld;
+            if (q.weights) {      // rows 8 e + [0, 8) of a unit: its columns 4 e + [0, 4) and 16 + 4 e + [0, 4)
+                const int64_t c4 = c / 32 * 32 + c % 32 / 8 * 4;
+                bool fours = false;
+                if constexpr (sizeof(T) == 4) {
+                    fours = q.whole && c4 + 20 <= q.cols;
+                    if (fours) {
+                        const float4 x = *reinterpret_cast<const float4 *>(from + c4), y = *reinterpret_cast<const float4 *>(from + c4 + 16);
+                        v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+                        v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+                    }
+                }
+                if (!fours) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int64_t at = c4 + j / 4 * 16 + j % 4;
+                        v[j] = at < q.cols ? widen1(from[at]) : 0.0f;
+                    }
+                }
+            } else {
+                load_eight(from, c, q.cols, q.whole, v);
+            }
+        }
         uint4 parts[kParts];
         pack_eight<kParts>(v, parts);
         __syncthreads();
@@ -222,7 +252,7 @@ __global__ __launch_bounds__(kPackThreads) void pack_cols_kernel(ColsPack q)
         for (int w = 0; w < kTogether; ++w) {
             uint4 parts[kParts];
             pack_eight<kParts>(v[w], parts);
-            const int c = (c_in + w) % kUnitRows, slot = half * 32 + (q.weights ? fragment_row(c) : c);
+            const int c = (c_in + w) % kUnitRows, slot = q.weights ? weights_place(fragment_row(c), half, int(kg & 1)) : rows_place(c, half);
 #pragma unroll
             for (int p = 0; p < kParts; ++p) *reinterpret_cast<uint4 *>(q.out.at + p * q.out.plane() + q.out.unit(rb * q.sides + side, kg) + slot * 16) = parts[p];
         }
@@ -265,17 +295,20 @@ inline Planes planes_of(int b_parts)
 }
 
 // C[m][n] = sum over k of A[m][k] B[n][k]: A's rows are rows of the result, B's are the weights' side.
-// direct: A are rows of bf16 where they lie, at multiples of 16 bytes, of a multiple of 32 elements: nothing of them is laid out.  A wavefront's load then takes
+// kLying: A are rows of bf16 where they lie, at multiples of 16 bytes, of a multiple of 32 elements: nothing of them is laid out.  A wavefront's load then takes
 // 64 bytes of 16 rows, and LDS has those rows, their 16-byte pieces exchanged by a quarter of the row's number (16 lanes read as many rows: all banks).
+// kTurned: A is laid out as the weights' side of another product, its k-values as rows; a slab is 32 of those, of 16 of A's rows a unit, and is read along them.
+enum RowsAs { kUnits_, kLying, kTurned };
 struct WideCall {
     Packed a, b;
     Planes planes;
     int m_tiles, n_tiles, panel;      // panel: column tiles that a die's blocks share rows of
     int splits, split_slabs;          // ranges of k, of that many slabs
-    int64_t lda, rows;                // direct: A's pitch in elements, its rows
+    int64_t lda, rows;                // kLying: A's pitch in elements, its rows
+    int row_units;                    // of 32 rows of the result
     __host__ __device__ __forceinline__ int slabs_of(int split) const
     {
-        const int left = a.kgs / 2 - split * split_slabs;
+        const int left = b.kgs / 2 - split * split_slabs;
         return left < split_slabs ? left : split_slabs;
     }
 };
@@ -342,6 +375,27 @@ struct Stage {
 __device__ __forceinline__ void arrived(float &v) { asm volatile("" : "+v"(v)); }
 __device__ __forceinline__ void arrived(uint4 &v) { asm volatile("" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w)); }
 
+// A fragment of 32 rows that are the k-values of two units, 16 of each, `stride` bytes apart, and of 16 k-values that are rows of theirs: this lane's eight.  Of four
+// rows' 16 k-values, which the lanes of a quarter wavefront address in pieces of four, the transposing read gives each lane one k-value's four.
+typedef short shortx4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
+struct AlongRows {
+    uint32_t low, high;      // of the lower four of its eight rows, of the other four
+    __device__ __forceinline__ AlongRows(int lane, int stride)
+    {
+        const int quarter = lane >> 4, i = lane & 15, row = 8 * (quarter >> 1) + (i >> 2), unit = quarter & 1;
+        low = uint32_t(unit * stride + weights_place(row, (i & 3) >> 1, unit) * 16 + (i & 1) * 8);
+        high = uint32_t(unit * stride + weights_place(row + 4, (i & 3) >> 1, unit) * 16 + (i & 1) * 8);
+    }
+};
+__device__ __forceinline__ uint4 along_rows(const uint4 *units, const AlongRows &at)
+{
+    const char *p = reinterpret_cast<const char *>(units);
+    const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4 *)(p + at.low)));
+    const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4 *)(p + at.high)));
+    return make_uint4(lo.x, lo.y, hi.x, hi.y);
+}
+
 // A wavefront's TN by TM fragments, of rows from row0 and columns from col0 on, by way of its part of LDS
 template <int TM, int TN, class Epi>
 __device__ __forceinline__ void write_out(const Epi &epi, const floatx16 (&acc)[TN][TM], int64_t row0, int col0, int split, float *at, int lane)
@@ -375,7 +429,7 @@ __device__ __forceinline__ void write_out(const Epi &epi, const floatx16 (&acc)[
 // MF x NF units a tile, WM x WN wavefronts.  A ring of slabs of 32 k-values, fetched kStages - 1 ahead through tile boundaries.  One wavefront a SIMD has to keep its
 // matrix unit busy by itself: the fragments of the next 16 k-values are read, and the units of a later slab fetched, one between every two matrix
 // instructions (each takes the unit 32 cycles).
-template <int MF, int NF, int WM, int WN, int kStages, bool kDirect, class Epi>
+template <int MF, int NF, int WM, int WN, int kStages, RowsAs kRows, class Epi>
 __global__ __launch_bounds__(WM *WN * 64, kStages * (MF + NF) >= 64 ? 1 : 2) void wide_gemm_kernel(WideCall q, Epi epi)
 {
     constexpr int kWaves = WM * WN, TM = MF / WM, TN = NF / WN, kUnits = (MF + NF) * 2, kLoads = kUnits / kWaves, kAhead = kStages - 1;
@@ -402,11 +456,12 @@ __global__ __launch_bounds__(WM *WN * 64, kStages * (MF + NF) >= 64 ? 1 : 2) voi
     const bool rows_side = u0 < 2 * MF;
     const int in_side = rows_side ? u0 : u0 - 2 * MF, k_unit = in_side / (rows_side ? MF : NF), rb_in = in_side % (rows_side ? MF : NF);
     int64_t c_work = work;
-    const int slab_bytes = kDirect && rows_side ? 64 : 16 * kUnitBytes;
     int c_at = 0, c_slabs = 1, c_last = INT32_MAX, c_pair = -1, c_stage = kStages - 1;
-    // a lane's place in load v: row min(row + 16 v, most) of `pitch` bytes, and its piece of it (units are rows of 64 bytes, one behind the other)
-    const bool lying = kDirect && rows_side;
-    const uint32_t pitch = lying ? uint32_t(q.lda * 2) : 64u, piece_at = uint32_t(lying ? (lane & 3) ^ (lane >> 4) : lane & 3) * 16u;
+    // Load v of a lane, from the slab's base on.  kLying: row min(row_in + 16 v, most), this lane's piece of it; kTurned: unit min(v, most), 8 KB apart.  (Of the
+    // other operand: its units of 1 KB.)
+    const bool lying = kRows == kLying && rows_side, turned = kRows == kTurned && rows_side;
+    const uint32_t pitch = lying ? uint32_t(q.lda * 2) : kRows == kLying ? 64u : turned ? uint32_t(8 * kUnitBytes) : uint32_t(kUnitBytes);
+    const uint32_t piece_at = kRows != kLying ? uint32_t(lane) * 16u : uint32_t(lying ? (lane & 3) ^ (lane >> 4) : lane & 3) * 16u;
     const int row_in = lane / 4 + (lying ? u0 * 16 : 0);
     int most = INT32_MAX;
     const char *from = nullptr;
@@ -427,25 +482,34 @@ __global__ __launch_bounds__(WM *WN * 64, kStages * (MF + NF) >= 64 ? 1 : 2) voi
         c_at = 0;
         const WideTile tile = wide_tile(q, c_work);
         const int rb = (rows_side ? tile.m * MF : tile.n * NF) + rb_in, pair = 4 * c_pair;
-        if (!kDirect || !rows_side) {
-            const Packed &o = rows_side ? q.a : q.b;
-            from = o.at + (((rows_side ? q.planes.a : q.planes.b) >> pair) & 15u) * o.plane() + o.unit(rb, int64_t(tile.split) * q.split_slabs * 2 + k_unit);
-            c_slabs = q.slabs_of(tile.split);
-        } else {
+        c_slabs = q.slabs_of(tile.split);
+        if (lying) {
             const int64_t row0 = int64_t(tile.m) * (MF * 32), left = q.rows - 1 - row0;
             most = left < MF * 32 ? int(left) : MF * 32;
             from = q.a.at + row0 * q.lda * 2;
-            c_slabs = q.a.kgs / 2;
+        } else if (turned) {
+            const int kg = tile.m * (MF * 2) + u0, left = q.a.kgs - 1 - kg;
+            most = left > 0 ? left : 0;
+            from = q.a.at + int64_t(left < 0 ? q.a.kgs - 1 : kg) * (8 * kUnitBytes);
+        } else {
+            const Packed &o = rows_side ? q.a : q.b;
+            from = o.at + (((rows_side ? q.planes.a : q.planes.b) >> pair) & 15u) * o.plane() + o.unit(rb, int64_t(tile.split) * q.split_slabs * 2 + k_unit);
         }
     };
     const char *base = nullptr;      // `from` in scalar registers
     auto fetch = [&](int v) {
         const int row = row_in + v * 16;
-        fetch_unit(to + uint32_t(v) * uint32_t(kUnitBytes), base, kDirect ? uint32_t(row < most ? row : most) * pitch + piece_at : uint32_t(v * kUnitBytes + lane * 16));
+        const uint32_t at = kRows == kLying    ? uint32_t(row < most ? row : most) * pitch + piece_at
+                            : kRows == kTurned ? uint32_t(v < most ? v : most) * pitch + piece_at
+                                               : uint32_t(v * kUnitBytes + lane * 16);
+        fetch_unit(to + uint32_t(v) * uint32_t(kUnitBytes), base, at);
     };
     auto next_slab = [&]() {
         step();
-        const uint64_t at = reinterpret_cast<uint64_t>(from) + uint64_t(c_at < c_last ? c_at : c_last) * uint32_t(slab_bytes);
+        const uint32_t slab = uint32_t(c_at < c_last ? c_at : c_last);
+        const uint64_t step_bytes = turned ? uint64_t(slab >> 3) * (uint64_t(uint32_t(q.a.kgs)) * (8 * kUnitBytes)) + (slab & 7) * uint32_t(kUnitBytes)
+                                           : uint64_t(slab) * (lying ? 64u : uint32_t(16 * kUnitBytes));
+        const uint64_t at = reinterpret_cast<uint64_t>(from) + step_bytes;
         base = reinterpret_cast<const char *>(uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(int(at >> 32)))) << 32 | uint32_t(__builtin_amdgcn_readfirstlane(int(at))));
     };
 #pragma unroll
@@ -459,14 +523,17 @@ __global__ __launch_bounds__(WM *WN * 64, kStages * (MF + NF) >= 64 ? 1 : 2) voi
     uint4 xa[2][TM], xb[2][TN];
     constexpr int kReads = TM + TN, kProducts = TM * TN;
     static_assert(kReads <= kProducts && kLoads <= kProducts, "a read and a fetch for every product");
-    // direct: of 32 rows of 64 bytes this lane's piece of the first and of the second 16 k-values
+    const int weights_at0 = weights_place(lane & 31, lane >> 5, 0), weights_at1 = weights_place(lane & 31, lane >> 5, 1);
+    const AlongRows turned_at(lane, kUnitBytes);
+    // kLying: of 32 rows of 64 bytes this lane's piece of the first and of the second 16 k-values
     const int row_at0 = (lane & 31) * 4 + ((lane >> 5) ^ ((lane >> 2) & 3)), row_at1 = row_at0 ^ 2;
     auto read = [&](int at, int g, int v, uint4 (&a)[TM], uint4 (&b)[TN]) {
-        const uint4 *slab = &ring[at * (kUnits * 64)], *units = slab + lane;
-        if (v == 0) b[0] = units[(2 * MF + g * NF + wn * TN) * 64];
-        else if (v <= TM && kDirect) a[v - 1] = slab[(wm * TM + v - 1) * 128 + (g ? row_at1 : row_at0)];
+        const uint4 *slab = &ring[at * (kUnits * 64)], *units = slab + lane, *weights = slab + (g ? weights_at1 : weights_at0);
+        if (v == 0) b[0] = weights[(2 * MF + g * NF + wn * TN) * 64];
+        else if (v <= TM && kRows == kLying) a[v - 1] = slab[(wm * TM + v - 1) * 128 + (g ? row_at1 : row_at0)];
+        else if (v <= TM && kRows == kTurned) a[v - 1] = along_rows(slab + (wm * TM + v - 1) * 128 + g * 32, turned_at);
         else if (v <= TM) a[v - 1] = units[(g * MF + wm * TM + v - 1) * 64];
-        else b[v - TM] = units[(2 * MF + g * NF + wn * TN + v - TM) * 64];
+        else b[v - TM] = weights[(2 * MF + g * NF + wn * TN + v - TM) * 64];
     };
     int stage = 0, storing = 0;
     wait_and_meet<kYoung>();

@@ -337,20 +337,22 @@ struct WeightEpilogue {
 };
 
 // ---- gradients of pre-activations ----------------------------------------------
-// Gated: dG = dH U act'(G), dU = dH act(G).  One-sided: dZ = dY act'(Z).  Computed once, in fp32, and laid out for both products that take them: with the
-// rows along the result's rows (dX = [dG | dU] [W_gate | W_up]^T, one part of bf16 rows' gradients: the result is rounded to as much) and with the rows
-// along k (dW = X^T [dG | dU], two parts of them: dW is fp32).  The columns' sums go along: a block keeps them over its rows.
+// Gated: dG = dH U act'(G), dU = dH act(G).  One-sided: dZ = dY act'(Z).  Computed once, in fp32, and laid out once, the columns as a unit's rows: along k for
+// dW = X^T [dG | dU], along its rows for dX = [dG | dU] [W_gate | W_up]^T.  In two bf16 parts of bf16 rows' gradients: dW is fp32, and its error from the parts
+// is 2.8e-6 (2^-17 a value; sums of 8,192 products in fp32 have 1.6e-6; a third part would make dW half as dear again), dX, which is rounded to bf16, takes the first alone.
+// The columns' sums go along: a block keeps them over its rows.  (Laid out for each of the two products they took a third more: 8,192 rows of 2 x 8192 in bf16
+// 230 us, 125,237 of 2 x 256 in fp32 225, five TB/s.)
 template <typename T>
 struct GradCall {
     const T *Z, *U, *dY;          // Z: the gate's pre-activations; Z may be NULL without an activation
     int64_t ldz, ldy, n;
     int N, act;
     bool wz, wy;
-    Packed by_rows, by_cols;      // by_rows.at may be NULL
+    Packed by_cols;
     float *sums;                  // [blocks along the rows][sides * padded], or NULL
     int row_blocks;
 };
-template <typename T, int kSides, int kPartsR, int kPartsC>
+template <typename T, int kSides, int kParts>
 __global__ __launch_bounds__(256) void grad_pack_kernel(GradCall<T> q)
 {
     __shared__ float tile[kSides][32][65];
@@ -388,17 +390,6 @@ __global__ __launch_bounds__(256) void grad_pack_kernel(GradCall<T> q)
                 }
             }
         }
-        if (q.by_rows.at && c < padded) {
-#pragma unroll
-            for (int side = 0; side < kSides; ++side) {
-                uint4 parts[kPartsR];
-                pack_eight<kPartsR>(d[side], parts);
-                const int kg = side * (padded / kUnitK) + c / kUnitK;
-#pragma unroll
-                for (int p = 0; p < kPartsR; ++p)
-                    *reinterpret_cast<uint4 *>(q.by_rows.at + p * q.by_rows.plane() + q.by_rows.unit(i, kg) + (piece % 2 * 32 + r) * 16) = parts[p];
-            }
-        }
         __syncthreads();
 #pragma unroll
         for (int side = 0; side < kSides; ++side)
@@ -411,12 +402,12 @@ __global__ __launch_bounds__(256) void grad_pack_kernel(GradCall<T> q)
                 float v[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] = tile[side][quarter * 8 + j][col_in];
-                uint4 parts[kPartsC];
-                pack_eight<kPartsC>(v, parts);
+                uint4 parts[kParts];
+                pack_eight<kParts>(v, parts);
                 const int64_t rb = side * (padded / kUnitRows) + (c0 + col_in) / kUnitRows, kg = i * 2 + quarter / 2;
-                const int slot = quarter % 2 * 32 + fragment_row(col_in % 32);
+                const int slot = weights_place(fragment_row(col_in % 32), quarter % 2, quarter / 2);
 #pragma unroll
-                for (int p = 0; p < kPartsC; ++p)
+                for (int p = 0; p < kParts; ++p)
                     *reinterpret_cast<uint4 *>(q.by_cols.at + p * q.by_cols.plane() + q.by_cols.unit(rb, kg) + slot * 16) = parts[p];
                 sum[side] += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
             }
@@ -490,17 +481,18 @@ inline bool fills_big(int m_units, int n_units) { return wide_tiles(m_units, n_u
 // One range of k: results go through an epilogue.  A large tile is multiplied 7 % faster (8192 -> 2048, 8,192 rows 267 and 287 us) but is alone on its unit, which does
 // nothing else while results are written: where a product is short beside them, and first of all where they are added to something that has to be
 // read, two small ones a unit are faster (256 -> 256 with a residual, 1,000,003 rows in bf16, eight slabs: 719 and 490 us).
-inline WidePlan plan_rows(const Packed &a, const Packed &b, bool reads)
+inline WidePlan plan_rows(int row_units, const Packed &b, bool reads)
 {
-    const int slabs = a.kgs / 2;
-    return {wide_tiles(a.rbs, b.rbs, true) >= kCus * 3 / 4 && fills_big(a.rbs, b.rbs) && slabs >= (reads ? 64 : 16), 1, slabs};
+    const int slabs = b.kgs / 2;
+    return {wide_tiles(row_units, b.rbs, true) >= kCus * 3 / 4 && fills_big(row_units, b.rbs) && slabs >= (reads ? 64 : 16), 1, slabs};
 }
-// ranges of k until the tiles fill the chip, 512 rows each at least; fp32 has small tiles only, three a unit
+// ranges of k until the tiles fill the chip, 512 rows each at least; fp32 has small tiles only (two ranges a
+// unit: three were no faster and wrote more, 125,237 rows of 128 x 512 141 and 144 us with their sums)
 inline WidePlan plan_weight(const Packed &a, const Packed &b, bool fp32)
 {
     const int slabs = a.kgs / 2, most = slabs / 16 > 1 ? slabs / 16 : 1;
     for (bool big : {true, false}) {
-        const int64_t tiles = wide_tiles(a.rbs, b.rbs, big), slots = big ? kCus : fp32 ? 3 * kCus : 2 * kCus;
+        const int64_t tiles = wide_tiles(a.rbs, b.rbs, big), slots = big ? kCus : 2 * kCus;
         int64_t want = slots / tiles;
         want = want < 1 ? 1 : want > most ? most : want;
         if (big && (fp32 || tiles * want < kCus / 2 || !fills_big(a.rbs, b.rbs))) continue;
@@ -510,11 +502,11 @@ inline WidePlan plan_weight(const Packed &a, const Packed &b, bool fp32)
     return {false, 1, slabs};
 }
 
-template <bool kDirect, class Epi>
+template <RowsAs kRows, class Epi>
 static int launch_wide_as(const char *name, WideCall q, const WidePlan &p, const Epi &e, hipStream_t s)
 {
     const int units = p.big ? 8 : 4, per_cu = p.big ? 1 : 2;
-    q.m_tiles = int(ceil_div(q.a.rbs, units));
+    q.m_tiles = int(ceil_div(q.row_units, units));
     q.n_tiles = int(ceil_div(q.b.rbs, units));
     if (q.panel > q.n_tiles) q.panel = q.n_tiles;
     const int64_t total = int64_t(q.m_tiles) * q.n_tiles * q.splits;
@@ -522,25 +514,25 @@ static int launch_wide_as(const char *name, WideCall q, const WidePlan &p, const
     if (per_die > 32 * per_cu) per_die = 32 * per_cu;
     TMA_TIMED(name, s);
     const dim3 grid(unsigned(per_die * kWideDies)), block(256);
-    if (p.big) hipLaunchKernelGGL((wide_gemm_kernel<8, 8, 2, 2, 4, kDirect, Epi>), grid, block, 0, s, q, e);
-    else hipLaunchKernelGGL((wide_gemm_kernel<4, 4, 2, 2, 3, kDirect, Epi>), grid, block, 0, s, q, e);
+    if (p.big) hipLaunchKernelGGL((wide_gemm_kernel<8, 8, 2, 2, 4, kRows, Epi>), grid, block, 0, s, q, e);
+    else hipLaunchKernelGGL((wide_gemm_kernel<4, 4, 2, 2, 3, kRows, Epi>), grid, block, 0, s, q, e);
     return check_launch(name);
 }
-// operands of type T laid out: of bf16 in b_parts parts on the weights' side, of fp32 in three on both
-template <typename T, class Epi>
-static int launch_wide(const char *name, const Packed &a, const Packed &b, int b_parts, const WidePlan &p, const Epi &e, hipStream_t s)
+// operands of type T laid out: of bf16 in b_parts parts on the weights' side, of fp32 in three on both; kTurned or not
+template <typename T, RowsAs kRows, class Epi>
+static int launch_wide(const char *name, const Packed &a, const Packed &b, int row_units, int b_parts, const WidePlan &p, const Epi &e, hipStream_t s)
 {
-    WideCall q{a, b, planes_of(b_parts), 0, 0, 8, p.splits, p.split_slabs, 0, 0};
+    WideCall q{a, b, planes_of(b_parts), 0, 0, 8, p.splits, p.split_slabs, 0, 0, row_units};
     if constexpr (sizeof(T) == 2) {
-        return launch_wide_as<false>(name, q, p, e, s);
+        return launch_wide_as<kRows>(name, q, p, e, s);
     } else {
-        q.m_tiles = int(ceil_div(a.rbs, 4));
+        q.m_tiles = int(ceil_div(row_units, 4));
         q.n_tiles = int(ceil_div(b.rbs, 4));
         if (q.panel > q.n_tiles) q.panel = q.n_tiles;
         const int64_t blocks = ceil_div(int64_t(q.m_tiles) * q.n_tiles * q.splits, kWideDies) * kWideDies;
         if (blocks > INT32_MAX) return fail(TMA_ERR_BAD_SHAPE, "%s: too many tiles", name);
         TMA_TIMED(name, s);
-        hipLaunchKernelGGL(wide_split_kernel<Epi>, dim3(unsigned(blocks)), dim3(256), 0, s, q, e);
+        hipLaunchKernelGGL((wide_split_kernel<kRows == kTurned, Epi>), dim3(unsigned(blocks)), dim3(256), 0, s, q, e);
         return check_launch(name);
     }
 }
@@ -578,15 +570,15 @@ inline bool direct_rows(const T *X, int64_t ldx, int32_t F_in, int n_units)
 template <typename T, class Epi>
 static int forward_product(const char *fn, const char *name, int64_t n, const T *X, int64_t ldx, int32_t F_in, ForwardPlan p, bool reads, const Epi &e, hipStream_t s)
 {
-    const WidePlan w = plan_rows(p.a, p.b, reads);
+    const WidePlan w = plan_rows(p.a.rbs, p.b, reads);
     if constexpr (sizeof(T) == 2)
         if (direct_rows(X, ldx, F_in, p.b.rbs)) {
             p.a.at = const_cast<char *>(reinterpret_cast<const char *>(X));
-            return launch_wide_as<true>(name, WideCall{p.a, p.b, planes_of(1), 0, 0, 8, w.splits, w.split_slabs, ldx, n}, w, e, s);
+            return launch_wide_as<kLying>(name, WideCall{p.a, p.b, planes_of(1), 0, 0, 8, w.splits, w.split_slabs, ldx, n, p.a.rbs}, w, e, s);
         }
     launch_pack_rows<T, kPartsOf<T>>("wide_pack_rows", X, nullptr, ldx, n, F_in, false, p.a, s);
     if (int rc = check_launch(fn)) return rc;
-    return launch_wide<T>(name, p.a, p.b, 1, w, e, s);
+    return launch_wide<T, kUnits_>(name, p.a, p.b, p.a.rbs, 1, w, e, s);
 }
 
 template <typename T>
@@ -605,7 +597,7 @@ inline ForwardPlan plan_forward(int64_t n, int32_t F_in, int32_t F_out, int side
 }
 
 struct BackwardPlan {
-    Packed d_rows, d_cols, x_cols, w_rows;
+    Packed d_cols, x_cols, w_rows;
     int padded, row_blocks, parts_c;
     WidePlan weight;
     float *sums, *partial;
@@ -618,7 +610,6 @@ inline BackwardPlan plan_backward(int64_t n, int32_t F_in, int32_t F_out, int si
     BackwardPlan p;
     p.padded = int(round_up(size_t(F_out), 32));
     p.parts_c = sizeof(T) == 4 ? 3 : exact ? 1 : 2;
-    p.d_rows = packed_shape(n, int64_t(sides) * p.padded);
     p.d_cols = packed_shape(int64_t(sides) * p.padded, n);
     p.x_cols = packed_shape(F_in, n);
     p.w_rows = packed_shape(F_in, int64_t(sides) * p.padded);
@@ -632,12 +623,7 @@ inline BackwardPlan plan_backward(int64_t n, int32_t F_in, int32_t F_out, int si
     cut.take(p.x_cols, kPartsOf<T>);
     p.sums = static_cast<float *>(cut.take(size_t(p.row_blocks) * size_t(sides) * size_t(p.padded) * 4));
     p.partial = p.weight.splits > 1 ? static_cast<float *>(cut.take(size_t(p.weight.splits) * size_t(sides) * size_t(F_in) * size_t(F_out) * 4)) : nullptr;
-    if (need_dX) {
-        cut.take(p.d_rows, kPartsOf<T>);
-        cut.take(p.w_rows, kPartsOf<T>);
-    } else {
-        p.d_rows.at = nullptr;
-    }
+    if (need_dX) cut.take(p.w_rows, kPartsOf<T>);
     p.bytes = cut.used;
     return p;
 }
@@ -656,17 +642,16 @@ static int wide_backward(const char *fn, const char *what, int64_t n, const T *X
     const bool exact = kSides == 1 && g.act == TMA_ACT_NONE;
     const BackwardPlan p = plan_backward<T>(n, F_in, N, kSides, exact, dX != nullptr, ws);
     constexpr int kP = kPartsOf<T>;
-    g.by_rows = p.d_rows;
     g.by_cols = p.d_cols;
     g.sums = db[0] ? p.sums : nullptr;
     g.row_blocks = p.row_blocks;
     {
         TMA_TIMED("wide_grad_pack", s);
         const dim3 grid(unsigned(ceil_div(N, 64) * p.row_blocks)), block(256);
-        if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((grad_pack_kernel<T, kSides, 3, 3>), grid, block, 0, s, g);
-        else if constexpr (kSides == 2) hipLaunchKernelGGL((grad_pack_kernel<T, kSides, 1, 2>), grid, block, 0, s, g);
-        else if (exact) hipLaunchKernelGGL((grad_pack_kernel<T, kSides, 1, 1>), grid, block, 0, s, g);
-        else hipLaunchKernelGGL((grad_pack_kernel<T, kSides, 1, 2>), grid, block, 0, s, g);
+        if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((grad_pack_kernel<T, kSides, 3>), grid, block, 0, s, g);
+        else if constexpr (kSides == 2) hipLaunchKernelGGL((grad_pack_kernel<T, kSides, 2>), grid, block, 0, s, g);
+        else if (exact) hipLaunchKernelGGL((grad_pack_kernel<T, kSides, 1>), grid, block, 0, s, g);
+        else hipLaunchKernelGGL((grad_pack_kernel<T, kSides, 2>), grid, block, 0, s, g);
         if (int rc = check_launch(fn)) return rc;
     }
     launch_pack_cols<T, kP>("wide_pack_cols", X, nullptr, ldx, n, F_in, false, p.x_cols, s);
@@ -677,7 +662,7 @@ static int wide_backward(const char *fn, const char *what, int64_t n, const T *X
     we.whole16 = N % 4 == 0 && aligned(we.out[0], 16) && (kSides == 1 || aligned(we.out[1], 16));
     char name[64];
     snprintf(name, sizeof(name), "%s_bwd_weight%s", what, sizeof(T) == 2 ? "_bf16" : "");
-    if (int rc = launch_wide<T>(name, p.x_cols, p.d_cols, p.parts_c, p.weight, we, s)) return rc;
+    if (int rc = launch_wide<T, kUnits_>(name, p.x_cols, p.d_cols, p.x_cols.rbs, p.parts_c, p.weight, we, s)) return rc;
     if (split) launch_join("wide_join", p.partial, p.weight.splits, cells * kSides, cells, cells, dW[0], kSides == 2 ? dW[1] : nullptr, s);
     if (db[0]) launch_join_sums(p.sums, p.row_blocks, kSides, p.padded, N, db[0], db[1], s);
     if (int rc = check_launch(fn)) return rc;
@@ -686,7 +671,8 @@ static int wide_backward(const char *fn, const char *what, int64_t n, const T *X
     if (int rc = check_launch(fn)) return rc;
     const ResidualEpilogue<T> re{nullptr, dX, R, 0, ld_dx, ldr, n, nullptr, F_in, TMA_ACT_NONE, whole_rows(dX, ld_dx), R && whole_rows(R, ldr), false};
     snprintf(name, sizeof(name), "%s_bwd_data%s", what, sizeof(T) == 2 ? "_bf16" : "");
-    return launch_wide<T>(name, p.d_rows, p.w_rows, 1, plan_rows(p.d_rows, p.w_rows, R != nullptr), re, s);
+    const int row_units = int(ceil_div(n, kUnitRows));
+    return launch_wide<T, kTurned>(name, p.d_cols, p.w_rows, row_units, 1, plan_rows(row_units, p.w_rows, R != nullptr), re, s);
 }
 
 // every number of a call that asks for a workspace, too

@@ -11,7 +11,7 @@
 
 namespace tma {
 
-template <class Epi>
+template <bool kTurnedRows, class Epi>
 __global__ __launch_bounds__(256, Epi::kPast ? 2 : 3) void wide_split_kernel(WideCall q, Epi epi)
 {
     constexpr int F = 4, T = 2, kStages = Epi::kPast ? 3 : 2, kUnits = 6 * F, kLoads = 6, kStageBytes = kUnits * kUnitBytes;
@@ -22,25 +22,36 @@ __global__ __launch_bounds__(256, Epi::kPast ? 2 : 3) void wide_split_kernel(Wid
     if (blockIdx.x / kWideDies >= per_die || work >= total) return;
     const WideTile tile = wide_tile(q, work);
     const int steps = q.slabs_of(tile.split) * 2;
+    const AlongRows turned_at(lane, 512);
+    const int weights_at[2] = {weights_place(lane & 31, lane >> 5, 0), weights_place(lane & 31, lane >> 5, 1)};
 
     // A slab in LDS: [operand][part][unit].  This wavefront fetches half of one operand's: parts 0 0 0 0 1 1 or 1 1 2 2 2 2, units 0 1 2 3 0 1 or 2 3 0 1 2 3, in
     // three pairs of neighbours.
-    const bool rows_side = wave < 2;
+    const bool rows_side = wave < 2, turned = kTurnedRows && rows_side;
     const int half = wave & 1;
     const Packed &o = rows_side ? q.a : q.b;
-    const char *first = o.at + o.unit((rows_side ? tile.m : tile.n) * F, int64_t(tile.split) * q.split_slabs * 2);
-    const char *from[3] = {first + half * (o.plane() + 2 * kUnitBytes), first + half * 2 * o.plane() + (half ? 0 : 2 * kUnitBytes),
-                           first + (1 + half) * o.plane() + (half ? 2 * kUnitBytes : 0)};
-    const uint32_t ring0 = lds_address(&ring[0]) + uint32_t(wave * kLoads * kUnitBytes), lane_at = uint32_t(lane * 16);
+    // turned: 16 of a unit's rows are a slab's k-values, 512 bytes, and a load takes those of two units, 32 rows of the result; units past the last are the last again
+    const int kg = tile.m * (2 * F), pairs = (o.kgs - kg) / 2;
+    const char *first = turned ? o.at + int64_t(kg) * (8 * kUnitBytes) : o.at + o.unit((rows_side ? tile.m : tile.n) * F, int64_t(tile.split) * q.split_slabs * 2);
+    const char *from[3] = {first + half * o.plane(), first + half * 2 * o.plane(), first + (1 + half) * o.plane()};
+    const int unit[3] = {half * 2, half ? 0 : 2, half * 2};
+    const uint32_t ring0 = lds_address(&ring[0]) + uint32_t(wave * kLoads * kUnitBytes);
+    const uint32_t lane_at = turned ? uint32_t((lane >> 5) * (8 * kUnitBytes) + (lane & 31) * 16) : uint32_t(lane * 16);
     auto fetch = [&](int step) {
         const uint32_t to = ring0 + uint32_t(step % kStages * kStageBytes);
+        const uint64_t along = turned ? uint64_t(uint32_t(step >> 4)) * (uint64_t(uint32_t(o.kgs)) * (8 * kUnitBytes)) + uint32_t(step >> 1 & 7) * uint32_t(kUnitBytes) +
+                                            uint32_t(step & 1) * 512u
+                                      : uint64_t(uint32_t(step)) * (8 * kUnitBytes);
 #pragma unroll
         for (int p = 0; p < 3; ++p) {
-            const uint64_t at = reinterpret_cast<uint64_t>(from[p]) + uint64_t(uint32_t(step)) * (8 * kUnitBytes);
+            const uint64_t at = reinterpret_cast<uint64_t>(from[p]) + along;
             const char *base = reinterpret_cast<const char *>(uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(int(at >> 32)))) << 32 |
                                                               uint32_t(__builtin_amdgcn_readfirstlane(int(at))));
-            fetch_unit(to + uint32_t(2 * p * kUnitBytes), base, lane_at);
-            fetch_unit(to + uint32_t((2 * p + 1) * kUnitBytes), base, lane_at + uint32_t(kUnitBytes));
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+                const int u = unit[p] + v;
+                fetch_unit(to + uint32_t((2 * p + v) * kUnitBytes), base, lane_at + uint32_t(turned ? (u < pairs ? u : pairs - 1) * (16 * kUnitBytes) : u * kUnitBytes));
+            }
         }
     };
     floatx16 sum[T][T], rest[T][T];
@@ -57,14 +68,15 @@ __global__ __launch_bounds__(256, Epi::kPast ? 2 : 3) void wide_split_kernel(Wid
         if (s + kStages - 2 < steps) wait_and_meet<(kStages - 2) * kLoads>();
         else wait_and_meet<0>();
         if (s + kStages - 1 < steps) fetch(s + kStages - 1);      // into the place that every wavefront has read before this meeting
-        const uint4 *slab = &ring[s % kStages * (kUnits * 64) + lane];
+        const uint4 *slab = &ring[s % kStages * (kUnits * 64)], *units = slab + lane, *weights = slab + (s & 1 ? weights_at[1] : weights_at[0]);
         uint4 a[3][T], b[3][T];
 #pragma unroll
         for (int p = 0; p < 3; ++p)
 #pragma unroll
             for (int i = 0; i < T; ++i) {
-                a[p][i] = slab[(p * F + wm * T + i) * 64];
-                b[p][i] = slab[(3 * F + p * F + wn * T + i) * 64];
+                if constexpr (kTurnedRows) a[p][i] = along_rows(slab + (p * F + wm * T + i) * 64, turned_at);
+                else a[p][i] = units[(p * F + wm * T + i) * 64];
+                b[p][i] = weights[(3 * F + p * F + wn * T + i) * 64];
             }
         auto add = [&](int pa, int pb, floatx16 (&to)[T][T]) {
 #pragma unroll
