@@ -44,7 +44,7 @@ __host__ __device__ __forceinline__ int fragment_row(int c) { return ((c >> 4) &
 // Where in a unit row r's eight k-values `half` lie, in pieces of 16 bytes.  A unit of rows is in the order of the lanes.  On the weights' side a row's two pieces are
 // neighbours, exchanged in every second eight rows: so 16 lanes that read as many rows meet in no bank, and a unit can be read along its rows as
 // well (the transposing read takes 16 k-values of four rows): the gradients of pre-activations, laid out for dW with their columns as rows, are dX's rows of k.  In every
-// second unit along k rows are four apart exchanged: such a read takes two of them at once (8,192 rows of 2 x 8192, dX 484 us without).
+// second unit along k rows are four apart exchanged: such a read takes two of them at once.
 __host__ __device__ __forceinline__ int rows_place(int r, int half) { return half * 32 + r; }
 __host__ __device__ __forceinline__ int weights_place(int r, int half, int kg) { return (r ^ (kg & 1) * 4) * 2 + (half ^ ((r >> 3) & 1)); }
 
