@@ -754,7 +754,7 @@ int tma_dropout_bwd(int64_t n, int32_t F, const void *dY, int64_t ldy, double p,
  * results that it reaches non-finite (NaN where fp32 arithmetic may give an
  * infinity).  The ReLU of a NaN is 0 and closed.  Widths up to 65536.  What lies in a row's padding has no
  * influence and is left as it is.
- * Workspaces, 256-byte aligned: the *_workspace_bytes queries (none forward of up to 64 rows, ws may then be NULL).
+ * Workspaces, 256-byte aligned: the *_workspace_bytes queries (0 forward of small weights and up to 64 rows: ws may then be NULL).
  * ---------------------------------------------------------------------- */
 size_t tma_gated_dense_fwd_workspace_bytes(int64_t n, int32_t F_in, int32_t F_out, int32_t dtype);
 
@@ -791,7 +791,8 @@ int tma_dense_residual_bwd(int64_t n, const void *X, int64_t ldx, const void *Z,
  * written where c = 1); h_outs[i] may be h_grads[i].  norm_out [1] fp32
  * (device).  Squares and their sum are fp64, each result is rounded once.  A
  * norm of NaN makes all results NaN, an infinite one finite gradients 0 and
- * infinite ones NaN.  max_norm >= 0.  At most 131072 tensors.
+ * infinite ones NaN.  max_norm >= 0.  At most 131072 tensors.  Results that
+ * overlap are refused.
  * The calls may be captured: a graph keeps the pointers and lengths.
  * Workspace: tma_grad_norm_workspace_bytes(n_tensors), 256-byte aligned.
  * ---------------------------------------------------------------------- */

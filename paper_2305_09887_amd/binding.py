@@ -158,9 +158,12 @@ def _feat_dtype(t) -> int:
 
 def _rows_ld(t, name):
     """2-D row-major tensor, possibly with padded rows: returns (rows, cols, ld)."""
-    if t.dim() != 2 or t.stride(1) != 1:
+    stride = t.stride()
+    if len(stride) != 2 or stride[1] != 1:
         raise TmaError(f"{name}: expected a 2-D tensor with unit inner stride")
-    return t.shape[0], t.shape[1], (t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1]))
+    rows, cols = t.shape
+    ld = stride[0]
+    return rows, cols, ld if rows > 1 or ld >= cols else cols
 
 
 def _padded(n: int, cols: int, dtype, device) -> torch.Tensor:
@@ -923,10 +926,13 @@ def tma_gcn_block_bwd(n_dst: int, n_src: int, max_entries: int, blk_rowptr, blk_
 # ---------------------------------------------------------------------------
 def _device(where, first, *others):
     """The device that the tensors share (the first is one; others may be None)."""
-    dev = first.device
-    if dev.type != "cuda" or any(t is not None and t.device != dev for t in others):
+    index = first.get_device()
+    for t in others:
+        if t is not None and t.get_device() != index:
+            index = -1
+    if index < 0:
         raise TmaError(f"{where}: expected tensors on one CUDA/HIP device")
-    return dev
+    return first.device
 
 
 def _launch(device, stream, call, *args):
@@ -947,8 +953,8 @@ def _rows_like(t, name, shape, dtype):
     """A [rows, cols] tensor of the given shape and type with unit inner stride: its leading dimension."""
     if t.shape != shape or t.dtype != dtype:
         raise TmaError(f"{name}: expected {tuple(shape)} of {dtype}")
-    ld = _rows_ld(t, name)[2]
-    if ld < shape[1]:
+    _, cols, ld = _rows_ld(t, name)
+    if ld < cols:
         raise TmaError(f"{name}: rows overlap")
     return ld
 
@@ -968,7 +974,7 @@ def _room(ws):
         return None, 0
     if not ws.is_contiguous():
         raise TmaError("ws: expected a contiguous tensor")
-    return ws.data_ptr(), ws.numel() * ws.element_size()
+    return ws.data_ptr(), ws.nbytes
 
 
 def tma_group_rows_workspace_bytes(n: int, E: int) -> int:
@@ -1156,16 +1162,17 @@ def tma_dropout_bwd(dY, p: float, seed: int, step=None, first_row: int = 0, out=
     return _dropout("tma_dropout_bwd", lib().tma_dropout_bwd, dY, p, seed, step, first_row, out, stream)
 
 
-def _new_rows(n, cols, dtype, dev, stream):
-    """_padded, but for widths that need no padding in one call."""
-    if n and cols * (2 if dtype == torch.bfloat16 else 4) % 16 == 0:
-        return _record(torch.empty((n, cols), dtype=dtype, device=dev), stream)
-    return _record(_padded(n, cols, dtype, dev), stream)
+def _new_rows(X, cols, stream):
+    """_padded, of X's rows, type and device, but for widths that need no padding in one call."""
+    n = X.shape[0]
+    if n and cols % 8 == 0:
+        return _record(X.new_empty((n, cols)), stream)
+    return _record(_padded(n, cols, X.dtype, X.device), stream)
 
 
-def _forward_room(ws, nbytes, dev, stream):
-    """The workspace of a forward call, or none where it needs none."""
-    return _workspace(nbytes, dev, stream) if ws is None and nbytes else ws
+def _forward_room(ws, nbytes, X, stream):
+    """The workspace of a forward call on X's device (of X's type: the shortest way to memory), or none where it needs none."""
+    return _record(X.new_empty(nbytes // X.itemsize), stream) if ws is None and nbytes else ws
 
 
 def _rows_of(t, name):
@@ -1208,11 +1215,11 @@ def tma_gated_dense_fwd(X, W_gate, W_up, b_gate=None, b_up=None, act: int = TMA_
     elif G_out is None or U_out is None:
         if G_out is not None or U_out is not None:
             raise TmaError(f"{where}: G_out and U_out go together")
-        G_out, U_out = (_new_rows(n, F_out, X.dtype, dev, stream) for _ in range(2))
+        G_out, U_out = (_new_rows(X, F_out, stream) for _ in range(2))
     if H_out is None:
-        H_out = _new_rows(n, F_out, X.dtype, dev, stream)
+        H_out = _new_rows(X, F_out, stream)
     _same_ld(G_out, U_out, f"{where}: G_out / U_out")
-    ws = _forward_room(ws, tma_gated_dense_fwd_workspace_bytes(n, F_in, F_out, dtype), dev, stream)
+    ws = _forward_room(ws, tma_gated_dense_fwd_workspace_bytes(n, F_in, F_out, dtype), X, stream)
     G, ldg = _rows_or_none(G_out, "G_out", (n, F_out), X.dtype)
     _launch(dev, stream, lib().tma_gated_dense_fwd, n, X.data_ptr(), ldx, F_in,
             _vector(W_gate, "W_gate", (F_in, F_out), torch.float32), _vector(W_up, "W_up", (F_in, F_out), torch.float32),
@@ -1241,7 +1248,7 @@ def tma_gated_dense_bwd(X, G, U, dH, W_gate, W_up, act: int = TMA_ACT_SILU, R=No
     dW_up = new((F_in, F_out)) if dW_up is None else dW_up
     db_gate = None if not need_dbias else new((F_out,)) if db_gate is None else db_gate
     db_up = None if not need_dbias else new((F_out,)) if db_up is None else db_up
-    dX_out = None if not need_dX else _new_rows(n, F_in, X.dtype, dev, stream) if dX_out is None else dX_out
+    dX_out = None if not need_dX else _new_rows(X, F_in, stream) if dX_out is None else dX_out
     if ws is None:
         ws = _workspace(tma_gated_dense_bwd_workspace_bytes(n, F_in, F_out, dtype, need_dX), dev, stream)
     _rows_like(U, "U", (n, F_out), X.dtype)
@@ -1269,10 +1276,10 @@ def tma_dense_residual_fwd(X, W, bias=None, act: int = TMA_ACT_NONE, R=None, sav
     F_out = _weight_shape(where, "W", W, F_in)
     dtype = _feat_dtype(X)
     if save and Z_out is None:
-        Z_out = _new_rows(n, F_out, X.dtype, dev, stream)
+        Z_out = _new_rows(X, F_out, stream)
     if Y_out is None:
-        Y_out = _new_rows(n, F_out, X.dtype, dev, stream)
-    ws = _forward_room(ws, tma_dense_residual_fwd_workspace_bytes(n, F_in, F_out, dtype), dev, stream)
+        Y_out = _new_rows(X, F_out, stream)
+    ws = _forward_room(ws, tma_dense_residual_fwd_workspace_bytes(n, F_in, F_out, dtype), X, stream)
     _launch(dev, stream, lib().tma_dense_residual_fwd, n, X.data_ptr(), ldx, F_in,
             _vector(W, "W", (F_in, F_out), torch.float32), _vector(bias, "bias", (F_out,), torch.float32), F_out, act, dtype,
             *_rows_or_none(R, "R", (n, F_out), X.dtype), *_rows_or_none(Z_out, "Z_out", (n, F_out), X.dtype), Y_out.data_ptr(),
@@ -1300,7 +1307,7 @@ def tma_dense_residual_bwd(X, Z, dY, W, act: int = TMA_ACT_NONE, R=None, dW=None
     new = lambda shape: _record(torch.empty(shape, dtype=torch.float32, device=dev), stream)
     dW = new((F_in, F_out)) if dW is None else dW
     dbias = None if not need_dbias else new((F_out,)) if dbias is None else dbias
-    dX_out = None if not need_dX else _new_rows(n, F_in, X.dtype, dev, stream) if dX_out is None else dX_out
+    dX_out = None if not need_dX else _new_rows(X, F_in, stream) if dX_out is None else dX_out
     if ws is None:
         ws = _workspace(tma_dense_residual_bwd_workspace_bytes(n, F_in, F_out, act, dtype, need_dX), dev, stream)
     _launch(dev, stream, lib().tma_dense_residual_bwd, n, X.data_ptr(), ldx,

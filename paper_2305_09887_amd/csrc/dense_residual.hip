@@ -14,7 +14,7 @@ static int residual_fwd(const char *fn, int64_t n, const void *X, int64_t ldx, i
     const T *r = static_cast<const T *>(R);
     const ResidualEpilogue<T> e{z, y, r, ldz, ldy, ldr, n, bias, F_out, act, whole_rows(y, ldy) && (!z || whole_rows(z, ldz)), r && whole_rows(r, ldr),
                                 bias_pieces(bias, F_out)};
-    if (n <= kFewMost) return launch_few<T, 1>(fn, sizeof(T) == 2 ? "residual_few_bf16" : "residual_few", n, X, ldx, W, nullptr, F_in, F_out, e, s);
+    if (n <= kFewMost) return launch_few<T, 1>(fn, sizeof(T) == 2 ? "residual_few_bf16" : "residual_few", n, X, ldx, W, nullptr, F_in, F_out, e, ws, s);
     const ForwardPlan p = plan_forward<T>(n, F_in, F_out, 1, ws);
     launch_pack_cols<float, kP>("wide_pack_cols", W, nullptr, F_out, F_in, F_out, true, p.b, s);
     if (int rc = check_launch(fn)) return rc;
@@ -74,7 +74,7 @@ extern "C" int tma_dense_residual_bwd(int64_t n, const void *X, int64_t ldx, con
     using namespace tma;
     const char *fn = "tma_dense_residual_bwd";
     if (int rc = check_wide(fn, n, F_in, F_out, act, dtype, ws, ws_bytes, tma_dense_residual_bwd_workspace_bytes(n, F_in, F_out, act, dtype, dX_out != nullptr))) return rc;
-    TMA_REQUIRE(dW, TMA_ERR_INVALID_ARG, "%s: dW is NULL", fn);
+    TMA_REQUIRE(dW && dW != W, TMA_ERR_INVALID_ARG, "%s: dW is NULL, or W", fn);
     if (n > 0) {
         TMA_REQUIRE(X && dY && (!dX_out || W), TMA_ERR_INVALID_ARG, "%s: NULL argument", fn);
         TMA_REQUIRE(act == TMA_ACT_NONE || Z, TMA_ERR_INVALID_ARG, "%s: Z is required with an activation", fn);

@@ -15,7 +15,7 @@ static int gated_fwd(const char *fn, int64_t n, const void *X, int64_t ldx, int3
     T *g = static_cast<T *>(G), *u = static_cast<T *>(U), *h = static_cast<T *>(H);
     const GatedEpilogue<T> e{g, u, h, ldg, ldh, n, b_gate, b_up, F_out, act, whole_rows(h, ldh) && (!g || (whole_rows(g, ldg) && whole_rows(u, ldg))),
                              bias_pieces(b_gate, F_out) && bias_pieces(b_up, F_out)};
-    if (n <= kFewMost) return launch_few<T, 2>(fn, sizeof(T) == 2 ? "gated_few_bf16" : "gated_few", n, X, ldx, W_gate, W_up, F_in, F_out, e, s);
+    if (n <= kFewMost) return launch_few<T, 2>(fn, sizeof(T) == 2 ? "gated_few_bf16" : "gated_few", n, X, ldx, W_gate, W_up, F_in, F_out, e, ws, s);
     const ForwardPlan p = plan_forward<T>(n, F_in, F_out, 2, ws);
     launch_pack_cols<float, kP>("wide_pack_cols", W_gate, W_up, F_out, F_in, F_out, true, p.b, s);
     if (int rc = check_launch(fn)) return rc;
@@ -79,6 +79,7 @@ extern "C" int tma_gated_dense_bwd(int64_t n, const void *X, int64_t ldx, const 
     if (int rc = check_wide(fn, n, F_in, F_out, act, dtype, ws, ws_bytes, tma_gated_dense_bwd_workspace_bytes(n, F_in, F_out, dtype, dX_out != nullptr))) return rc;
     TMA_REQUIRE(dW_gate && dW_up && dW_gate != dW_up, TMA_ERR_INVALID_ARG, "%s: dW_gate or dW_up is NULL, or they are one", fn);
     TMA_REQUIRE(!db_gate == !db_up && (!db_gate || db_gate != db_up), TMA_ERR_INVALID_ARG, "%s: db_gate and db_up go together", fn);
+    for (const float *w : {W_gate, W_up}) TMA_REQUIRE(w != dW_gate && w != dW_up, TMA_ERR_INVALID_ARG, "%s: a weight is its gradient", fn);
     if (n > 0) {
         TMA_REQUIRE(X && G && U && dH && (!dX_out || (W_gate && W_up)), TMA_ERR_INVALID_ARG, "%s: NULL argument", fn);
         TMA_REQUIRE(ldx >= F_in && ldg >= F_out && ldh >= F_out && (!dX_out || (ld_dx >= F_in && (!R || ldr >= F_in))), TMA_ERR_BAD_SHAPE,

@@ -7,6 +7,9 @@
 // the cache.  Bound by memory: a gradient is read once, and once more and written where it is clipped.
 #include "kernels.hpp"
 
+#include <algorithm>
+#include <cstdlib>
+
 namespace tma {
 
 constexpr int kListed = 128, kNormBlocks = 2048, kNormThreads = 256;
@@ -230,6 +233,36 @@ static int check_grads(const char *fn, int32_t n_tensors, const void *const *h_g
     return TMA_OK;
 }
 
+// Tensors that are written may not share memory (one given twice would be scaled twice, or in part).  Lists in the order of their addresses, as a flat buffer's parts are,
+// need no sorting.
+static int check_apart(const char *fn, int32_t n_tensors, const void *const *outs, const int64_t *h_sizes, size_t size)
+{
+    struct Range {
+        uintptr_t from, to;
+    };
+    auto range = [&](int i) { return Range{reinterpret_cast<uintptr_t>(outs[i]), reinterpret_cast<uintptr_t>(outs[i]) + uintptr_t(h_sizes[i]) * size}; };
+    uintptr_t end = 0;
+    bool ordered = true;
+    for (int i = 0; i < n_tensors && ordered; ++i) {
+        if (h_sizes[i] == 0) continue;
+        const Range r = range(i);
+        ordered = r.from >= end;
+        end = r.to;
+    }
+    if (ordered) return TMA_OK;
+    Range few[256], *all = n_tensors <= 256 ? few : static_cast<Range *>(malloc(size_t(n_tensors) * sizeof(Range)));
+    TMA_REQUIRE(all, TMA_ERR_INVALID_ARG, "%s: no host memory for %d tensors", fn, n_tensors);
+    int count = 0;
+    for (int i = 0; i < n_tensors; ++i)
+        if (h_sizes[i]) all[count++] = range(i);
+    std::sort(all, all + count, [](const Range &a, const Range &b) { return a.from < b.from; });
+    bool apart = true;
+    for (int i = 1; i < count; ++i) apart = apart && all[i].from >= all[i - 1].to;
+    if (all != few) free(all);
+    TMA_REQUIRE(apart, TMA_ERR_INVALID_ARG, "%s: two of the results overlap", fn);
+    return TMA_OK;
+}
+
 }  // namespace tma
 
 extern "C" size_t tma_grad_norm_workspace_bytes(int32_t n_tensors)
@@ -257,6 +290,7 @@ extern "C" int tma_grad_clip(int32_t n_tensors, const void *const *h_grads, void
     const char *fn = "tma_grad_clip";
     if (int rc = check_grads(fn, n_tensors, h_grads, h_outs, h_sizes, dtype, norm_out, ws, ws_bytes)) return rc;
     TMA_REQUIRE(max_norm >= 0.0, TMA_ERR_INVALID_ARG, "%s: max_norm below 0, or NaN", fn);
+    if (int rc = check_apart(fn, n_tensors, h_outs ? const_cast<const void *const *>(h_outs) : h_grads, h_sizes, dtype == TMA_BF16 ? 2 : 4)) return rc;
     hipStream_t s = as_stream(stream);
     double *partial = static_cast<double *>(ws);
     return dtype == TMA_BF16 ? grad_norm<uint16_t>(fn, n_tensors, h_grads, h_outs, h_sizes, true, max_norm, norm_out, partial, ws_bytes, s)

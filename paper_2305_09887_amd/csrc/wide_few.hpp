@@ -1,9 +1,11 @@
 // Forward products of few rows (serving: one token, a few requests together): bound by reading the fp32 weights once, so nothing is laid out before.
 //
-// A block takes 16 columns (of both weights where there are two) and all of k; its sixteen wavefronts share k out, and each loads the weights as they lie, eight
-// neighbours along k of a column a lane, straight into the registers that v_mfma_f32_16x16x32_bf16 wants them in: 64 bytes of a weight's row by 16 lanes, the rest of
-// the line by the block beside it, which runs on the same die.  One row 2048 -> 5632 gated in bf16 (92 MB) 24 us, 3.8 TB/s.  The matrix unit has time to spare, so the weights are taken as they are, in three bf16 parts (24 bits).
-// The shares of k are joined in LDS, in their order.
+// A block takes 16 columns of both weights, or 32 of one, and all of k or a range of it; its wavefronts share that out, and each loads the weights as they lie, eight
+// neighbours along k of a column a lane, straight into the registers that v_mfma_f32_16x16x32_bf16 wants them in.  The matrix unit has time to spare, so the
+// weights are taken as they are, in three bf16 parts (24 bits).  Their shares of k are joined in LDS, in their order.
+//
+// A compute unit reads some 20 bytes a nanosecond, whatever the others do: 128 blocks, alone on theirs, take as long as 256, and 352 twice as long.  So k is split over
+// blocks where that spreads the bytes, and a second kernel joins the ranges, in their order.
 #pragma once
 #include "wide_gemm.hpp"
 
@@ -17,93 +19,113 @@ struct FewCall {
     const void *X;
     int64_t ldx;
     const float *W[2];
-    int n, K, N, blocks;
+    int n, K, N, blocks, splits;   // blocks: of 32 / kSides columns
     bool whole;                    // rows of X begin at 16 bytes
+    float *partial;                // [splits][kSides][n][N], where k is split over blocks
 };
 
-// kFrags: of 16 rows.  kWaves: 16 where a compute unit has one block at most and 128 registers suffice, else 8 (64 rows 4096 -> 1024 in fp32 99 -> 48 us: with 16
-// their registers went to scratch memory).
+// kFrags: of 16 rows.  A wavefront has two fragments of weights: one of either matrix, or one matrix's even and odd columns.
 template <typename T, int kSides, int kFrags, int kWaves, class Out>
-__global__ __launch_bounds__(kWaves * 64) void few_rows_kernel(FewCall q, Out out)
+__global__ __launch_bounds__(kWaves * 64, kWaves == 8 ? 4 : 2) void few_rows_kernel(FewCall q, Out out)
 {
-    constexpr int kX = sizeof(T) == 2 ? 1 : 3, kDeep = kSides * kFrags > 1 ? 1 : 2;      // (what 128 registers hold, twice)
-    __shared__ __attribute__((aligned(16))) float shares[kWaves][kFrags * kSides][256];
+    constexpr int kX = sizeof(T) == 2 ? 1 : 3, kWide = 2 / kSides, kCols = 16 * kWide;
+    __shared__ __attribute__((aligned(16))) float shares[kWaves][kFrags * kSides * kWide][256];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l15 = lane & 15, group = lane >> 4;
     // neighbours on one die
-    const int per_die = (q.blocks + kWideDies - 1) / kWideDies, unit = int(blockIdx.x) % kWideDies * per_die + int(blockIdx.x) / kWideDies;
-    if (unit >= q.blocks) return;
-    const int c0 = unit * 16, col = c0 + l15 < q.N ? c0 + l15 : q.N - 1;
-    const int steps = (q.K + 31) / 32, first = int(int64_t(steps) * wave / kWaves), last = int(int64_t(steps) * (wave + 1) / kWaves);
+    const int units = q.blocks * q.splits, per_die = (units + kWideDies - 1) / kWideDies, in_die = int(blockIdx.x) / kWideDies, unit = int(blockIdx.x) % kWideDies * per_die + in_die;
+    if (in_die >= per_die || unit >= units) return;
+    const int split = unit / q.blocks, c0 = unit % q.blocks * kCols;
+    const bool inside = c0 + kCols <= q.N;
+    const int steps = (q.K + 31) / 32, from_step = int(int64_t(steps) * split / q.splits), mine = int(int64_t(steps) * (split + 1) / q.splits) - from_step;
+    const int first = from_step + mine * wave / kWaves, last = from_step + mine * (wave + 1) / kWaves;
 
-    floatx4 acc[kFrags][kSides];
+    floatx4 acc[kFrags][kSides][kWide];
 #pragma unroll
     for (int f = 0; f < kFrags; ++f)
 #pragma unroll
-        for (int s = 0; s < kSides; ++s) acc[f][s] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int s = 0; s < kSides; ++s)
+#pragma unroll
+            for (int c = 0; c < kWide; ++c) acc[f][s][c] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
     struct Loaded {
-        float w[kDeep][kSides][8];
-        uint4 x[kDeep][kFrags][kX];
+        float w[kSides][kWide][8];
+        float x32[kX == 3 ? kFrags : 1][8];
+        uint4 x16[kX == 1 ? kFrags : 1];
     };
-    // steps [step, step + kDeep) before `last`.  A whole step's addresses are a scalar base and a lane's offsets that stay.
+    // of a whole step the addresses are a scalar base and a lane's offsets that stay
     uint32_t at[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) at[j] = uint32_t((group * 8 + j) * int64_t(q.N) + col) * 4u;
-    const int whole_steps = q.K / 32;
-    auto load = [&](int step, Loaded &v) {
+    for (int j = 0; j < 8; ++j) at[j] = uint32_t((group * 8 + j) * int64_t(q.N) + c0 + l15 * kWide) * 4u;
+    const int whole_steps = inside ? q.K / 32 : 0;
+    auto load = [&](int t, Loaded &v) {
+        if (t >= last) return;
+        if (t < whole_steps) {
 #pragma unroll
-        for (int d = 0; d < kDeep; ++d) {
-            const int t = step + d;
-            if (t >= last) break;
-            if (t < whole_steps) {
+            for (int s = 0; s < kSides; ++s) {
+                const char *base = reinterpret_cast<const char *>(q.W[s] + int64_t(t) * 32 * q.N);
 #pragma unroll
-                for (int s = 0; s < kSides; ++s) {
-                    const char *base = reinterpret_cast<const char *>(q.W[s] + int64_t(t) * 32 * q.N);
+                for (int j = 0; j < 8; ++j) {
+                    float w[kWide];
+                    __builtin_memcpy(w, base + at[j], sizeof(w));
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) v.w[d][s][j] = *reinterpret_cast<const float *>(base + at[j]);
+                    for (int c = 0; c < kWide; ++c) v.w[s][c][j] = w[c];
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int k = t * 32 + group * 8 + j;
+#pragma unroll
+                for (int s = 0; s < kSides; ++s)
+#pragma unroll
+                    for (int c = 0; c < kWide; ++c) {
+                        const int col = c0 + l15 * kWide + c;
+                        const float w = q.W[s][int64_t(k < q.K ? k : q.K - 1) * q.N + (col < q.N ? col : q.N - 1)];
+                        v.w[s][c][j] = k < q.K ? w : 0.0f;
+                    }
+            }
+        }
+#pragma unroll
+        for (int f = 0; f < kFrags; ++f) {
+            const int row = f * 16 + l15, k0 = t * 32 + group * 8;
+            const T *from = static_cast<const T *>(q.X) + row * q.ldx;
+            if constexpr (kX == 1) {
+                v.x16[f] = make_uint4(0, 0, 0, 0);
+                if (row < q.n) {
+                    if (q.whole && k0 + 8 <= q.K) {
+                        v.x16[f] = *reinterpret_cast<const uint4 *>(from + k0);
+                    } else {
+                        float one[8];
+                        uint4 packed[1];
+                        load_eight(from, k0, q.K, false, one);
+                        pack_eight<1>(one, packed);
+                        v.x16[f] = packed[0];
+                    }
                 }
             } else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int k = t * 32 + group * 8 + j;
-#pragma unroll
-                    for (int s = 0; s < kSides; ++s) v.w[d][s][j] = q.W[s][int64_t(k < q.K ? k : q.K - 1) * q.N + col];      // (past the end: times a zero)
-                }
-            }
-#pragma unroll
-            for (int f = 0; f < kFrags; ++f) {
-                const int row = f * 16 + l15, k0 = t * 32 + group * 8;
-                const T *from = static_cast<const T *>(q.X) + row * q.ldx;
-                if constexpr (kX == 1) {
-                    v.x[d][f][0] = make_uint4(0, 0, 0, 0);
-                    if (row < q.n) {
-                        if (q.whole && k0 + 8 <= q.K) {
-                            v.x[d][f][0] = *reinterpret_cast<const uint4 *>(from + k0);
-                        } else {
-                            float one[8];
-                            load_eight(from, k0, q.K, false, one);
-                            pack_eight<1>(one, v.x[d][f]);
-                        }
-                    }
-                } else {
-                    float one[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-                    if (row < q.n) load_eight(from, k0, q.K, q.whole, one);
-                    pack_eight<kX>(one, v.x[d][f]);
-                }
+                for (int j = 0; j < 8; ++j) v.x32[f][j] = 0.0f;
+                if (row < q.n) load_eight(from, k0, q.K, q.whole, v.x32[f]);
             }
         }
     };
-    auto multiply = [&](int step, const Loaded &v) {
+    auto multiply = [&](int t, const Loaded &v) {
+        if (t >= last) return;
+        uint4 x[kFrags][kX];
 #pragma unroll
-        for (int d = 0; d < kDeep; ++d) {
-            if (step + d >= last) break;
+        for (int f = 0; f < kFrags; ++f) {
+            if constexpr (kX == 1) x[f][0] = v.x16[f];
+            else pack_eight<3>(v.x32[f], x[f]);
+        }
 #pragma unroll
-            for (int s = 0; s < kSides; ++s) {
+        for (int s = 0; s < kSides; ++s)
+#pragma unroll
+            for (int c = 0; c < kWide; ++c) {
                 uint4 parts[3];
-                pack_eight<3>(v.w[d][s], parts);
+                pack_eight<3>(v.w[s][c], parts);
 #pragma unroll
                 for (int f = 0; f < kFrags; ++f) {
                     auto add = [&](int p, int r) {
-                        acc[f][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, parts[p]), __builtin_bit_cast(bf16x8, v.x[d][f][r]), acc[f][s], 0, 0, 0);
+                        acc[f][s][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, parts[p]), __builtin_bit_cast(bf16x8, x[f][r]), acc[f][s][c], 0, 0, 0);
                     };
                     if constexpr (kX == 3) {
                         add(2, 0);
@@ -119,50 +141,99 @@ __global__ __launch_bounds__(kWaves * 64) void few_rows_kernel(FewCall q, Out ou
                     }
                 }
             }
-        }
     };
     Loaded v[2];
     load(first, v[0]);
-    for (int step = first; step < last; step += 2 * kDeep) {
-        load(step + kDeep, v[1]);
-        multiply(step, v[0]);
-        load(step + 2 * kDeep, v[0]);
-        multiply(step + kDeep, v[1]);
+    for (int t = first; t < last; t += 2) {
+        load(t + 1, v[1]);
+        multiply(t, v[0]);
+        load(t + 2, v[0]);
+        multiply(t + 1, v[1]);
     }
-    // register r of lane l: column 4 (l / 16) + r of row l % 16
+    // register r of lane l: column kWide (4 (l / 16) + r) + c of row l % 16
 #pragma unroll
     for (int f = 0; f < kFrags; ++f)
 #pragma unroll
-        for (int s = 0; s < kSides; ++s) *reinterpret_cast<float4 *>(&shares[wave][f * kSides + s][lane * 4]) = make_float4(acc[f][s][0], acc[f][s][1], acc[f][s][2], acc[f][s][3]);
+        for (int s = 0; s < kSides; ++s)
+#pragma unroll
+            for (int c = 0; c < kWide; ++c) {
+                const floatx4 &a = acc[f][s][c];
+                *reinterpret_cast<float4 *>(&shares[wave][(f * kSides + s) * kWide + c][lane * 4]) = make_float4(a[0], a[1], a[2], a[3]);
+            }
     __syncthreads();
-    for (int t = threadIdx.x; t < kFrags * 256; t += kWaves * 64) {
-        const int c = t % 16, in = t / 16 % 16, f = t / 256, row = f * 16 + in;
+    for (int t = threadIdx.x; t < kFrags * 16 * kCols; t += kWaves * 64) {
+        const int c = t % kCols, in = t / kCols % 16, f = t / (16 * kCols), row = f * 16 + in, i = c / kWide;
         if (row >= q.n || c0 + c >= q.N) continue;
         float sum[kSides] = {};
         for (int w = 0; w < kWaves; ++w)
 #pragma unroll
-            for (int s = 0; s < kSides; ++s) sum[s] += shares[w][f * kSides + s][(c / 4 * 16 + in) * 4 + c % 4];
-        out.one(row, c0 + c, sum[0], sum[kSides - 1]);
+            for (int s = 0; s < kSides; ++s) sum[s] += shares[w][(f * kSides + s) * kWide + c % kWide][(i / 4 * 16 + in) * 4 + i % 4];
+        if (q.splits == 1) {
+            out.one(row, c0 + c, sum[0], sum[kSides - 1]);
+        } else {
+#pragma unroll
+            for (int s = 0; s < kSides; ++s) q.partial[(int64_t(split * kSides + s) * q.n + row) * q.N + c0 + c] = sum[s];
+        }
     }
+}
+
+// the shares of k added up in their order, and what becomes of them
+template <int kSides, class Out>
+__global__ __launch_bounds__(256) void few_join_kernel(const float *__restrict__ partial, int splits, int n, int N, Out out)
+{
+    const int i = int(blockIdx.x) * 256 + int(threadIdx.x), cells = n * N;
+    if (i >= cells) return;
+    float sum[kSides] = {};
+#pragma unroll 4
+    for (int p = 0; p < splits; ++p)
+#pragma unroll
+        for (int s = 0; s < kSides; ++s) sum[s] += partial[int64_t(p * kSides + s) * cells + i];
+    out.one(i / N, i % N, sum[0], sum[kSides - 1]);
+}
+
+// Ranges of k: as many as make the bytes least that the busiest compute unit moves, eight wavefronts at a time, for all have the same rate, some 20 bytes a
+// nanosecond; such a turn costs as much as 8 KB more, the second kernel as much as 50.  (One range, then the one chosen: 24 rows 2048 -> 2 x 5632 in bf16, 352 blocks,
+// 39.6 and 30 us; one row 4096 -> 1024 in fp32, 32 blocks, 37 and 11.5; one row 1024 -> 2 x 4096 in bf16, 256 blocks, 11.5, of two 14.5.)
+struct FewPlan {
+    int blocks, splits;
+    size_t bytes;
+};
+inline int few_waves(int64_t n) { return n <= 16 ? 8 : 4; }
+inline FewPlan plan_few(int64_t n, int32_t F_in, int32_t F_out, int sides, int size)
+{
+    const int64_t blocks = ceil_div(F_out, 32 / sides), steps = ceil_div(F_in, 32), waves = few_waves(n);
+    FewPlan best{int(blocks), 1, 0};
+    int64_t least = INT64_MAX;
+    for (int splits = 1; splits <= 16; splits *= 2) {
+        const int64_t turns = ceil_div(blocks * splits * waves, 8 * 256);
+        const size_t partial = splits > 1 ? size_t(splits) * size_t(sides) * size_t(n) * size_t(F_out) * 4 : 0;
+        const int64_t moved = turns * (8 * ceil_div(steps, splits * waves) * (4096 + n * 32 * size) + 8000) + (splits > 1 ? 50000 + int64_t(partial) * 2 / 256 : 0);
+        if (moved < least) {
+            least = moved;
+            best.splits = splits;
+            best.bytes = partial;
+        }
+    }
+    return best;
 }
 
 template <typename T, int kSides, class Out>
 static int launch_few(const char *fn, const char *name, int64_t n, const void *X, int64_t ldx, const float *W, const float *second, int32_t F_in, int32_t F_out, const Out &out,
-                      hipStream_t s)
+                      void *ws, hipStream_t s)
 {
-    const FewCall q{X, ldx, {W, second}, int(n), F_in, F_out, int(ceil_div(F_out, 16)), whole_rows(static_cast<const T *>(X), ldx)};
-    const dim3 grid(unsigned(round_up(size_t(q.blocks), kWideDies)));
-    TMA_TIMED(name, s);
-    auto go = [&](auto frags, auto waves) {
-        constexpr int F = decltype(frags)::value, V = decltype(waves)::value;
-        hipLaunchKernelGGL((few_rows_kernel<T, kSides, F, V, Out>), grid, dim3(V * 64), 0, s, q, out);
-    };
-    const std::integral_constant<int, 16> sixteen;
-    const std::integral_constant<int, 8> eight;
-    const bool alone = q.blocks <= 256;
-    if (n <= 16) alone ? go(std::integral_constant<int, 1>{}, sixteen) : go(std::integral_constant<int, 1>{}, eight);
-    else if (n <= 32) go(std::integral_constant<int, 2>{}, eight);
-    else go(std::integral_constant<int, 4>{}, eight);
+    const FewPlan p = plan_few(n, F_in, F_out, kSides, sizeof(T));
+    const FewCall q{X, ldx, {W, second}, int(n), F_in, F_out, p.blocks, p.splits, whole_rows(static_cast<const T *>(X), ldx), static_cast<float *>(ws)};
+    const dim3 grid(unsigned(round_up(size_t(q.blocks) * size_t(q.splits), kWideDies)));
+    {
+        TMA_TIMED(name, s);
+        if (n <= 16) hipLaunchKernelGGL((few_rows_kernel<T, kSides, 1, 8, Out>), grid, dim3(512), 0, s, q, out);
+        else if (n <= 32) hipLaunchKernelGGL((few_rows_kernel<T, kSides, 2, 4, Out>), grid, dim3(256), 0, s, q, out);
+        else hipLaunchKernelGGL((few_rows_kernel<T, kSides, 4, 4, Out>), grid, dim3(256), 0, s, q, out);
+        if (int rc = check_launch(fn)) return rc;
+    }
+    if (q.splits == 1) return TMA_OK;
+    TMA_TIMED("few_join", s);
+    hipLaunchKernelGGL((few_join_kernel<kSides, Out>), dim3(unsigned(ceil_div(n * F_out, 256))), dim3(256), 0, s, q.partial, q.splits, q.n, q.N, out);
     return check_launch(fn);
 }
 

@@ -585,7 +585,10 @@ template <typename T>
 inline ForwardPlan plan_forward(int64_t n, int32_t F_in, int32_t F_out, int sides, void *ws)
 {
     ForwardPlan p{};
-    if (n <= kFewMost) return p;      // nothing is laid out
+    if (n <= kFewMost) {      // nothing is laid out
+        p.bytes = round_up(plan_few(n, F_in, F_out, sides, sizeof(T)).bytes, 256);
+        return p;
+    }
     p.a = packed_shape(n, F_in);
     p.b = packed_shape(F_out, F_in);
     p.b.rbs *= sides;

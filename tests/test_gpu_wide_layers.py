@@ -316,3 +316,116 @@ def test_large_and_small_fp32_values(B):
     W = torch.tensor([[1.0, 0.5, 0.0], [2.0, 0.0, 2.0 ** 60]], device="cuda")
     Y, _ = B.tma_dense_residual_fwd(X, W)
     assert torch.equal(Y, torch.tensor([[big, big / 2, 0.0], [2 * small, 0.0, small * 2.0 ** 60], [-big, -big / 2, 0.0]], device="cuda"))
+
+
+# few rows of wide weights, whose k blocks share out: ranges of even and of uneven length, last ones that are shorter, columns that end inside a block, rows anywhere
+FEW = [(1, 4_096, 1_024, 0, 0), (1, 8_000, 40, 0, 0), (16, 5_003, 77, 3, 1), (17, 4_096, 300, 0, 0), (24, 2_048, 5_632, 0, 0), (31, 8_191, 33, 1, 2), (64, 2_000, 1_001, 0, 0), (48, 1_111, 512, 8, 8),
+       (3, 512, 70, 0, 0), (64, 96, 300, 0, 0)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("n,fi,fo,more,off", FEW)
+def test_few_rows_of_whole_numbers(B, n, fi, fo, more, off, dtype):
+    g = torch.Generator().manual_seed(fi)
+    W = lambda *s: torch.randint(-1, 2, s, generator=g).double()
+    X, Wg, Wu, bg, bu, R = W(n, fi), W(fi, fo), W(fi, fo), W(fo), W(fo), W(n, fo)
+    G, U = X @ Wg + bg, X @ Wu + bu
+    x, r = _buffer(X, dtype, fi + more, off)[0], _buffer(R, dtype, fo + more, off)[0]
+    outs = [_buffer(torch.zeros(n, fo), dtype, fo + more, off, fill=7.0) for _ in range(4)]
+    d = lambda t: t.float().cuda()
+    want = G.clamp(min=0) * U, G, U, G.clamp(min=0) + R
+    for repeat in range(2):
+        B.tma_gated_dense_fwd(x, d(Wg), d(Wu), d(bg), d(bu), B.TMA_ACT_RELU, G_out=outs[1][0], U_out=outs[2][0], H_out=outs[0][0])
+        B.tma_dense_residual_fwd(x, d(Wg), d(bg), B.TMA_ACT_RELU, R=r, Y_out=outs[3][0])
+        for (t, flat), w in zip(outs, want):
+            assert torch.equal(t.cpu(), w.float().to(dtype)) and _untouched(flat, t, 7.0)
+    alone, _ = B.tma_dense_residual_fwd(x, d(Wu))
+    assert torch.equal(alone.cpu(), (X @ Wu).float().to(dtype))
+
+
+def test_an_infinite_last_weight_of_few_rows(B):
+    """k ends inside a step: what stands for the weights behind it is a zero, whatever the last one is."""
+    X, W = torch.ones((2, 37)), torch.ones((37, 20))
+    W[36, 3] = math.inf
+    for dtype in DTYPES:
+        got = B.tma_dense_residual_fwd(X.to(dtype).cuda(), W.cuda())[0].float().cpu()
+        rest = [c for c in range(20) if c != 3]
+        assert torch.equal(got[:, rest], torch.full((2, 19), 37.0))
+        # (fp32 rows come in three parts, and an infinity times a part that is zero is no number: the documented exception)
+        assert bool((got[:, 3] == math.inf).all()) if dtype == torch.bfloat16 else not torch.isfinite(got[:, 3]).any()
+
+
+def _block_step(B, t, ws, stream=None):
+    """A residual block's step: forward, backward, clipping of the gradients."""
+    H, G, U = B.tma_gated_dense_fwd(t["X"], t["Wg"], t["Wu"], t["bg"], t["bu"], B.TMA_ACT_SILU, G_out=t["G"], U_out=t["U"], H_out=t["H"], ws=ws, stream=stream)
+    B.tma_dense_residual_fwd(H, t["Wd"], t["bd"], R=t["X"], Y_out=t["Y"], ws=ws, stream=stream)
+    B.tma_dense_residual_bwd(H, None, t["dY"], t["Wd"], dW=t["dWd"], dbias=t["dbd"], dX_out=t["dH"], ws=ws, stream=stream)
+    B.tma_gated_dense_bwd(t["X"], G, U, t["dH"], t["Wg"], t["Wu"], B.TMA_ACT_SILU, R=t["dY"], dW_gate=t["dWg"], dW_up=t["dWu"], db_gate=t["dbg"], db_up=t["dbu"],
+                          dX_out=t["dX"], ws=ws, stream=stream)
+    B.tma_grad_clip([t[k] for k in ("dWd", "dbd", "dWg", "dWu", "dbg", "dbu")], 0.5, norm_out=t["norm"], ws=ws, stream=stream)
+
+
+RESULTS = ("H", "G", "U", "Y", "dH", "dX", "dWd", "dbd", "dWg", "dWu", "dbg", "dbu", "norm")
+
+
+def _block_tensors(n, F, K, dtype, seed):
+    g = torch.Generator().manual_seed(seed)
+    r = lambda *s: (torch.randn(s, generator=g) / s[0] ** 0.5).cuda()
+    e, rows = (lambda *s: torch.empty(s, device="cuda")), lambda w: torch.empty((n, w), dtype=dtype, device="cuda")
+    return dict(X=torch.randn((n, F), generator=g).to(dtype).cuda(), dY=torch.randn((n, F), generator=g).to(dtype).cuda(), Wg=r(F, K), Wu=r(F, K), bg=r(K), bu=r(K), Wd=r(K, F),
+                bd=r(F), H=rows(K), G=rows(K), U=rows(K), Y=rows(F), dH=rows(K), dX=rows(F), dWd=e(K, F), dbd=e(F), dWg=e(F, K), dWu=e(F, K), dbg=e(K), dbu=e(K), norm=e(1))
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=["f32", "bf16"])
+def test_two_captured_blocks_share_a_workspace(B, dtype):
+    """Steps of two sizes captured into a graph each, with one workspace; replayed in turn with eager steps between them, on the capture's and on another stream."""
+    sizes = (900, 96, 264), (40, 1_024, 2_048)
+    code = B.TMA_BF16 if dtype == torch.bfloat16 else B.TMA_F32
+    room = max(max(B.tma_gated_dense_fwd_workspace_bytes(n, F, K, code), B.tma_gated_dense_bwd_workspace_bytes(n, F, K, code), B.tma_dense_residual_fwd_workspace_bytes(n, K, F, code),
+                   B.tma_dense_residual_bwd_workspace_bytes(n, K, F, B.TMA_ACT_NONE, code), B.tma_grad_norm_workspace_bytes(6)) for n, F, K in sizes)
+    ws = torch.empty(room, dtype=torch.uint8, device="cuda")
+    steps, graphs, want = [_block_tensors(*s, dtype, i) for i, s in enumerate(sizes)], [], []
+    for t in steps:
+        _block_step(B, t, ws)
+        want.append({k: t[k].clone() for k in RESULTS})
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for t in steps:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            _block_step(B, t, ws, side)
+        graphs.append(graph)
+    other = torch.cuda.Stream()
+    for turn in range(4):
+        for i in (0, 1):
+            for k in RESULTS:
+                steps[i][k].fill_(math.nan)
+            ws.fill_(255)
+            torch.cuda.synchronize()
+            with torch.cuda.stream(other if turn % 2 else side):
+                graphs[i].replay()
+            torch.cuda.synchronize()
+            for k in RESULTS:
+                assert torch.equal(steps[i][k], want[i][k]), (turn, i, k)
+            if turn == 2:
+                _block_step(B, steps[1 - i], None)
+                for k in RESULTS:
+                    assert torch.equal(steps[1 - i][k], want[1 - i][k]), (turn, i, k)
+
+
+def test_two_streams_at_once(B):
+    """Steps on two streams at the same time, workspaces and results from the allocator."""
+    steps = [_block_tensors(700, 128, 320, torch.bfloat16, 3), _block_tensors(33, 2_048, 1_024, torch.bfloat16, 4)]
+    want = []
+    for t in steps:
+        _block_step(B, t, None)
+        want.append({k: t[k].clone() for k in RESULTS})
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in steps]
+    for _ in range(5):
+        for t, s in zip(steps, streams):
+            _block_step(B, t, None, s)
+    torch.cuda.synchronize()
+    for t, w in zip(steps, want):
+        for k in RESULTS:
+            assert torch.equal(t[k], w[k]), k

@@ -66,6 +66,9 @@ def test_gated(lib):
     refused(lib, gated_bwd(lib, R=A[11], ldr=7), -2, b"leading dimension")
     for k in (A[0], A[3], A[4], A[5]):
         refused(lib, gated_bwd(lib, dX=k), -1, b"dX_out is one of")
+    for k in ("Wg", "Wu"):
+        refused(lib, gated_bwd(lib, **{k: A[7]}), -1, b"a weight is its gradient")
+        refused(lib, gated_bwd(lib, **{k: A[8]}), -1, b"a weight is its gradient")
     refused(lib, gated_bwd(lib, R=A[9], ldr=9), -2, b"in place")
 
 
@@ -78,6 +81,7 @@ def test_residual(lib):
         refused(lib, res_fwd(lib, **k), -1, b"Z_out is one")
     refused(lib, res_fwd(lib, R=A[4], ldr=9), -2, b"in place")
     refused(lib, res_bwd(lib, dW=None), -1, b"dW is NULL")
+    refused(lib, res_bwd(lib, dW=A[1]), -1, b"dW is NULL, or W")
     for k in ("dY", "W"):
         refused(lib, res_bwd(lib, **{k: None}), -1, b"NULL")
     refused(lib, res_bwd(lib, Z=None), -1, b"Z is required")
@@ -90,7 +94,7 @@ def test_residual(lib):
 
 def test_workspace_sizes(lib):
     for query in (lib.tma_gated_dense_fwd_workspace_bytes, lib.tma_dense_residual_fwd_workspace_bytes):
-        assert query(64, 300, 300, 1) == 0 and query(65, 300, 300, 1) > 0
+        assert query(1, 64, 64, 1) == 0 and query(64, 32, 32, 0) == 0 and query(1, 8192, 1024, 1) >= 2 * 1024 * 4 and query(65, 64, 64, 1) > 0
         for n, fi, fo in ((-1, 8, 8), (1 << 31, 8, 8), (100, 0, 8), (100, 8, 0), (100, 65537, 8), (100, 8, 65537), (100, -5, 8)):
             assert query(n, fi, fo, 0) == 0
         assert query(1000, 300, 77, 0) % 256 == 0
@@ -129,6 +133,11 @@ def test_lists_of_gradients(lib):
     refused(lib, clip(outs=(ctypes.c_void_p * 2)(4096, None)), -1, b"tensor 1")
     for bound in (-1.0, float("nan")):
         refused(lib, clip(bound=bound), -1, b"max_norm")
+    for p, s in (((4096, 4096), (10, 20)), ((8192, 4096), (10, 1025)), ((4096, 4100), (10, 20)), ((4096,) * 2 + tuple(range(8192, 8192 + 64 * 400, 64)), (1, 1) + (16,) * 400)):
+        P_, S_ = (ctypes.c_void_p * len(p))(*p), (ctypes.c_int64 * len(s))(*s)
+        refused(lib, clip(n=len(p), p=P_, s=S_), -1, b"overlap")
+        apart = (ctypes.c_void_p * len(p))(*[(1 << 30) - (1 << 14) * i for i in range(len(p))])
+        refused(lib, clip(n=len(p), p=apart, s=S_, outs=P_), -1, b"overlap")
 
 
 def test_trainers_refuse_blocks_that_are_none():
