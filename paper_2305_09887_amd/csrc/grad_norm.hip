@@ -106,21 +106,14 @@ __global__ __launch_bounds__(kNormThreads) void grad_norm_kernel(const double *p
     if (threadIdx.x == 0) *norm_out = float(norm);
 }
 
-__device__ __forceinline__ void scale_piece(const float *in, float *out, float c)
+template <typename T>
+__device__ __forceinline__ void scale_piece(const uint4 &piece, T *out, float c)
 {
-    float v[4];
-    Chunk<float>::load(in, v);
+    float v[16 / sizeof(T)];
+    Chunk<T>::widen(piece, v);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] *= c;
-    Chunk<float>::store(out, v);
-}
-__device__ __forceinline__ void scale_piece(const uint16_t *in, uint16_t *out, float c)
-{
-    float v[8];
-    Chunk<uint16_t>::load(in, v);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] *= c;
-    Chunk<uint16_t>::store(out, v);
+    for (size_t j = 0; j < 16 / sizeof(T); ++j) v[j] *= c;
+    Chunk<T>::store(out, v);
 }
 __device__ __forceinline__ void scale_one(const float *in, float *out, float c) { *out = *in * c; }
 __device__ __forceinline__ void scale_one(const uint16_t *in, uint16_t *out, float c) { *out = f32_to_bf16(bf16_to_f32(*in) * c); }
@@ -149,9 +142,19 @@ __global__ __launch_bounds__(kNormThreads) void grad_scale_kernel(GradTensors q,
             head = head < n ? head : n;
             pieces = (n - head) / E;
         }
-        for (int64_t j = t; j < pieces; j += kNormThreads) scale_piece(in + head + j * E, out + head + j * E, factor);
-        for (int64_t j = t; j < n - pieces * E; j += kNormThreads) {
-            const int64_t k = j < head ? j : j + pieces * E;
+        const uint4 *from = reinterpret_cast<const uint4 *>(in + head);
+        T *to = out + head;
+        int64_t j = t;
+        for (; j + 3 * kNormThreads < pieces; j += 4 * kNormThreads) {
+            uint4 w[4];
+#pragma unroll
+            for (int p = 0; p < 4; ++p) w[p] = from[j + p * kNormThreads];
+#pragma unroll
+            for (int p = 0; p < 4; ++p) scale_piece(w[p], to + (j + p * kNormThreads) * E, factor);
+        }
+        for (; j < pieces; j += kNormThreads) scale_piece(from[j], to + j * E, factor);
+        for (int64_t i = t; i < n - pieces * E; i += kNormThreads) {
+            const int64_t k = i < head ? i : i + pieces * E;
             scale_one(in + k, out + k, factor);
         }
     }
