@@ -1323,53 +1323,61 @@ def tma_grad_norm_workspace_bytes(n_tensors: int) -> int:
     return int(lib().tma_grad_norm_workspace_bytes(n_tensors))
 
 
-def _addresses(tensors):
-    """Their addresses as a host array."""
-    return array("Q", map(torch.Tensor.data_ptr, tensors))
+@functools.lru_cache(1)
+def _lists():
+    """The reader of lists of tensors (tensor_list.cpp; raises if it is not built)."""
+    path = os.path.join(_PKG, "libtma_lists.so")
+    if not os.path.exists(path):
+        raise TmaError(f"{path} not found: build it with `python -m paper_2305_09887_amd.build`")
+    call = C.PyDLL(path).tma_read_tensors
+    call.argtypes = [C.py_object, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]
+    return call
+
+
+def _read(where, tensors, dtype, index, addresses, lengths, same, what):
+    """Their addresses and lengths into host arrays; ``same``: the lengths are given."""
+    at = C.c_int32()
+    rc = _lists()(tensors if type(tensors) is list else list(tensors), len(tensors), dtype, index, same, addresses, lengths, C.byref(at))
+    if rc:
+        raise TmaError(f"{where}: {what} {at.value}: expected contiguous tensors of one type on one CUDA/HIP device" if rc != 5 else
+                       f"{where}: a result differs from its gradient in size, or there is not one for each")
 
 
 def _grad_list(where, grads, out, norm_out, ws, stream):
-    """(device, number of tensors, their addresses and lengths as host arrays, type, norm_out, workspace).  (Lists are long and the host's share is what
-    counts on a small model: whole lists go through built-in functions.)"""
+    """(device, number of tensors, a host array of their addresses, their lengths and the results' addresses, that array's address, type, norm_out, workspace)."""
     if not grads:
         raise TmaError(f"{where}: no gradients")
-    dev, kind = grads[0].device, grads[0].dtype
-    dtype = _feat_dtype(grads[0])
-    lengths = list(map(torch.Tensor.numel, grads))
-    every = list(grads)
-    if out is not None:
-        if len(out) != len(grads):
-            raise TmaError(f"{where}: one result for each gradient")
-        if list(map(torch.Tensor.numel, out)) != lengths:
-            raise TmaError(f"{where}: a result differs from its gradient in size")
-        every += out
-    if ({t.dtype for t in every} != {kind} or set(map(torch.Tensor.get_device, every)) != {dev.index} or dev.type != "cuda"
-            or not all(map(torch.Tensor.is_contiguous, every))):
-        raise TmaError(f"{where}: gradients and results must be contiguous tensors of one type on one device")
+    first, n = grads[0], len(grads)
+    dtype = _feat_dtype(first)
     if norm_out is None:
-        norm_out = _record(torch.empty(1, dtype=torch.float32, device=dev), stream)
-    _device(where, grads[0], norm_out, ws)
+        norm_out = _record(torch.empty(1, dtype=torch.float32, device=first.device), stream)
+    dev = _device(where, first, norm_out, ws)
+    room = array("Q", bytes(24 * n))
+    at = room.buffer_info()[0]
+    _read(where, grads, dtype, dev.index, at, at + 8 * n, 0, "gradient")
+    if out is not None:
+        if len(out) != n:
+            raise TmaError(f"{where}: one result for each gradient")
+        _read(where, out, dtype, dev.index, at + 16 * n, at + 8 * n, 1, "result")
     _vector(norm_out, "norm_out", (1,), torch.float32)
-    n = len(lengths)
     if ws is None:
         ws = _workspace(tma_grad_norm_workspace_bytes(n), dev, stream)
-    return dev, n, _addresses(grads), array("q", lengths), dtype, norm_out, ws
+    return dev, n, room, at, dtype, norm_out, ws
 
 
 def tma_grad_norm(grads, norm_out=None, ws=None, stream=None):
     """The norm of all gradients together (a list of dense tensors of one type), [1] fp32 on their device."""
-    dev, n, ptrs, sizes, dtype, norm_out, ws = _grad_list("tma_grad_norm", grads, None, norm_out, ws, stream)
-    _launch(dev, stream, lib().tma_grad_norm, n, ptrs.buffer_info()[0], sizes.buffer_info()[0], dtype, norm_out.data_ptr(), *_room(ws))
+    dev, n, room, at, dtype, norm_out, ws = _grad_list("tma_grad_norm", grads, None, norm_out, ws, stream)
+    _launch(dev, stream, lib().tma_grad_norm, n, at, at + 8 * n, dtype, norm_out.data_ptr(), *_room(ws))
     return norm_out
 
 
 def tma_grad_clip(grads, max_norm: float, out=None, norm_out=None, ws=None, stream=None):
     """Gradients whose norm together is above max_norm are scaled to it, in place or into the tensors of ``out``; returns the
     norm before that, [1] fp32 on their device."""
-    dev, n, ptrs, sizes, dtype, norm_out, ws = _grad_list("tma_grad_clip", grads, out, norm_out, ws, stream)
-    outs = None if out is None else _addresses(out)
-    _launch(dev, stream, lib().tma_grad_clip, n, ptrs.buffer_info()[0], outs.buffer_info()[0] if outs is not None else None,
-            sizes.buffer_info()[0], dtype, float(max_norm), norm_out.data_ptr(), *_room(ws))
+    dev, n, room, at, dtype, norm_out, ws = _grad_list("tma_grad_clip", grads, out, norm_out, ws, stream)
+    _launch(dev, stream, lib().tma_grad_clip, n, at, None if out is None else at + 16 * n, at + 8 * n, dtype, float(max_norm),
+            norm_out.data_ptr(), *_room(ws))
     return norm_out
 
 

@@ -1,4 +1,4 @@
-"""Builds libtma.so (HIP, gfx950) in-tree with hipcc.  Cross-compiles without a GPU."""
+"""Builds libtma.so (HIP, gfx950) in-tree with hipcc, and libtma_lists.so, host code of the binding, with the host's compiler.  Cross-compiles without a GPU."""
 from __future__ import annotations
 
 import concurrent.futures as cf
@@ -6,12 +6,14 @@ import glob
 import os
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libtma.so")
+LISTS = os.path.join(PKG, "libtma_lists.so")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
@@ -28,11 +30,23 @@ def _compile(src: str) -> str:
     return obj
 
 
+def build_lists() -> str:
+    import torch
+    include = os.path.join(os.path.dirname(torch.__file__), "include")
+    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                           "-isystem", include, "-isystem", os.path.join(include, "torch", "csrc", "api", "include"),
+                           "-isystem", sysconfig.get_paths()["include"], "-Wall", os.path.join(CSRC, "tensor_list.cpp"), "-o", LISTS,
+                           "-L", os.path.join(os.path.dirname(torch.__file__), "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"])
+    return LISTS
+
+
 def build(verbose: bool = True) -> str:
     os.makedirs(OBJ, exist_ok=True)
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")))
     with cf.ThreadPoolExecutor(max_workers=min(8, len(srcs))) as ex:
+        lists = ex.submit(build_lists)
         objs = list(ex.map(_compile, srcs))
+        lists.result()
     subprocess.check_call([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs])
     if verbose:
         print(f"built {LIB} from {len(srcs)} sources", file=sys.stderr)

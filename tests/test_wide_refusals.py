@@ -151,3 +151,33 @@ def test_trainers_refuse_blocks_that_are_none():
     for c in (-1.0, float("nan"), float("inf")):
         with pytest.raises(B.TmaError, match="clip_norm"):
             LocalTrainer(None, None, None, X, None, [8, 4], clip_norm=c)
+
+
+def test_the_reader_of_lists_of_tensors():
+    """On host tensors (device -1): what it takes, what it refuses and where."""
+    from paper_2305_09887_amd import binding as B
+    from paper_2305_09887_amd import build
+    if not os.path.exists(build.LISTS):
+        build.build_lists()
+
+    def read(tensors, dtype=0, index=-1, lengths=None):
+        n = len(tensors)
+        a, s = (ctypes.c_uint64 * max(n, 1))(), (ctypes.c_int64 * max(n, 1))(*(lengths or [0] * n))
+        B._read("here", tensors, dtype, index, ctypes.addressof(a), ctypes.addressof(s), 1 if lengths else 0, "tensor")
+        return list(a)[:n], list(s)[:n]
+
+    flat = torch.arange(40.0)
+    ts = [flat[:7], flat[7:8], torch.empty(0), flat[8:].view(4, 8), torch.nn.Parameter(torch.ones(3, 5)), torch.tensor(2.0)]
+    for tensors in (ts, tuple(ts)):
+        a, s = read(tensors)
+        assert s == [7, 1, 0, 32, 15, 1] and a == [t.data_ptr() for t in ts]
+        assert read(tensors, lengths=s) == (a, s)
+    assert read([t.detach().bfloat16() for t in ts], dtype=1)[1] == [7, 1, 0, 32, 15, 1]
+    assert read([]) == ([], [])
+    for bad in (flat.double(), flat.half(), flat.bfloat16(), flat.view(5, 8).t(), flat[::2], flat.expand(2, 40), torch.ones(3).to_sparse(), 3.0, None, torch.empty(3, device="meta")):
+        with pytest.raises(B.TmaError, match="here: tensor 1:"):
+            read([flat, bad, flat])
+    with pytest.raises(B.TmaError, match="here: tensor 0:"):
+        read([flat], index=0)
+    with pytest.raises(B.TmaError, match="differs from its gradient in size"):
+        read([flat, flat[:3]], lengths=[40, 4])
