@@ -15,10 +15,10 @@ static int residual_fwd(const char *fn, int64_t n, const void *X, int64_t ldx, i
     const ResidualEpilogue<T> e{z, y, r, ldz, ldy, ldr, n, bias, F_out, act, whole_rows(y, ldy) && (!z || whole_rows(z, ldz)), r && whole_rows(r, ldr),
                                 bias_pieces(bias, F_out)};
     if (n <= kFewMost) return launch_few<T, 1>(fn, sizeof(T) == 2 ? "residual_few_bf16" : "residual_few", n, X, ldx, W, nullptr, F_in, F_out, e, ws, s);
-    const ForwardPlan p = plan_forward<T>(n, F_in, F_out, 1, ws);
+    const ForwardPlan p = plan_forward<T>(n, F_in, F_out, 1, r != nullptr, ws);
     launch_pack_cols<float, kP>("wide_pack_cols", W, nullptr, F_out, F_in, F_out, true, p.b, s);
     if (int rc = check_launch(fn)) return rc;
-    return forward_product<T>(fn, sizeof(T) == 2 ? "residual_fwd_bf16" : "residual_fwd", n, static_cast<const T *>(X), ldx, F_in, p, r != nullptr, e, s);
+    return forward_product<T>(fn, sizeof(T) == 2 ? "residual_fwd_bf16" : "residual_fwd", n, static_cast<const T *>(X), ldx, F_in, F_out, p, e, s);
 }
 
 template <typename T>
@@ -39,7 +39,7 @@ extern "C" size_t tma_dense_residual_fwd_workspace_bytes(int64_t n, int32_t F_in
 {
     using namespace tma;
     if (!wide_sizes_ok(n, F_in, F_out)) return 0;
-    return (dtype == TMA_BF16 ? plan_forward<uint16_t>(n, F_in, F_out, 1, nullptr) : plan_forward<float>(n, F_in, F_out, 1, nullptr)).bytes;
+    return (dtype == TMA_BF16 ? plan_forward<uint16_t>(n, F_in, F_out, 1, true, nullptr) : plan_forward<float>(n, F_in, F_out, 1, true, nullptr)).bytes;
 }
 
 extern "C" int tma_dense_residual_fwd(int64_t n, const void *X, int64_t ldx, int32_t F_in, const float *W, const float *bias, int32_t F_out, int32_t act, int32_t dtype,
@@ -63,8 +63,8 @@ extern "C" size_t tma_dense_residual_bwd_workspace_bytes(int64_t n, int32_t F_in
     using namespace tma;
     if (!wide_sizes_ok(n, F_in, F_out)) return 0;
     const bool exact = act == TMA_ACT_NONE;
-    return (dtype == TMA_BF16 ? plan_backward<uint16_t>(n, F_in, F_out, 1, exact, need_dX != 0, nullptr)
-                              : plan_backward<float>(n, F_in, F_out, 1, exact, need_dX != 0, nullptr)).bytes;
+    return (dtype == TMA_BF16 ? plan_backward<uint16_t>(n, F_in, F_out, 1, exact, need_dX != 0, false, nullptr)
+                              : plan_backward<float>(n, F_in, F_out, 1, exact, need_dX != 0, false, nullptr)).bytes;
 }
 
 extern "C" int tma_dense_residual_bwd(int64_t n, const void *X, int64_t ldx, const void *Z, int64_t ldz, const void *dY, int64_t ldy, const float *W, int32_t F_in,

@@ -16,10 +16,10 @@ static int gated_fwd(const char *fn, int64_t n, const void *X, int64_t ldx, int3
     const GatedEpilogue<T> e{g, u, h, ldg, ldh, n, b_gate, b_up, F_out, act, whole_rows(h, ldh) && (!g || (whole_rows(g, ldg) && whole_rows(u, ldg))),
                              bias_pieces(b_gate, F_out) && bias_pieces(b_up, F_out)};
     if (n <= kFewMost) return launch_few<T, 2>(fn, sizeof(T) == 2 ? "gated_few_bf16" : "gated_few", n, X, ldx, W_gate, W_up, F_in, F_out, e, ws, s);
-    const ForwardPlan p = plan_forward<T>(n, F_in, F_out, 2, ws);
+    const ForwardPlan p = plan_forward<T>(n, F_in, F_out, 2, false, ws);
     launch_pack_cols<float, kP>("wide_pack_cols", W_gate, W_up, F_out, F_in, F_out, true, p.b, s);
     if (int rc = check_launch(fn)) return rc;
-    return forward_product<T>(fn, sizeof(T) == 2 ? "gated_fwd_bf16" : "gated_fwd", n, static_cast<const T *>(X), ldx, F_in, p, false, e, s);
+    return forward_product<T>(fn, sizeof(T) == 2 ? "gated_fwd_bf16" : "gated_fwd", n, static_cast<const T *>(X), ldx, F_in, F_out, p, e, s);
 }
 
 template <typename T>
@@ -41,7 +41,7 @@ extern "C" size_t tma_gated_dense_fwd_workspace_bytes(int64_t n, int32_t F_in, i
 {
     using namespace tma;
     if (!wide_sizes_ok(n, F_in, F_out)) return 0;
-    return (dtype == TMA_BF16 ? plan_forward<uint16_t>(n, F_in, F_out, 2, nullptr) : plan_forward<float>(n, F_in, F_out, 2, nullptr)).bytes;
+    return (dtype == TMA_BF16 ? plan_forward<uint16_t>(n, F_in, F_out, 2, false, nullptr) : plan_forward<float>(n, F_in, F_out, 2, false, nullptr)).bytes;
 }
 
 extern "C" int tma_gated_dense_fwd(int64_t n, const void *X, int64_t ldx, int32_t F_in, const float *W_gate, const float *W_up, const float *b_gate, const float *b_up,
@@ -66,8 +66,8 @@ extern "C" size_t tma_gated_dense_bwd_workspace_bytes(int64_t n, int32_t F_in, i
 {
     using namespace tma;
     if (!wide_sizes_ok(n, F_in, F_out)) return 0;
-    return (dtype == TMA_BF16 ? plan_backward<uint16_t>(n, F_in, F_out, 2, false, need_dX != 0, nullptr)
-                              : plan_backward<float>(n, F_in, F_out, 2, false, need_dX != 0, nullptr)).bytes;
+    return (dtype == TMA_BF16 ? plan_backward<uint16_t>(n, F_in, F_out, 2, false, need_dX != 0, false, nullptr)
+                              : plan_backward<float>(n, F_in, F_out, 2, false, need_dX != 0, false, nullptr)).bytes;
 }
 
 extern "C" int tma_gated_dense_bwd(int64_t n, const void *X, int64_t ldx, const void *G, const void *U, int64_t ldg, const void *dH, int64_t ldh, const float *W_gate,

@@ -457,6 +457,7 @@ __global__ __launch_bounds__(WM *WN * 64, kStages * (MF + NF) >= 64 ? 1 : 2) voi
     const int in_side = rows_side ? u0 : u0 - 2 * MF, k_unit = in_side / (rows_side ? MF : NF), rb_in = in_side % (rows_side ? MF : NF);
     int64_t c_work = work;
     int c_at = 0, c_slabs = 1, c_last = INT32_MAX, c_pair = -1, c_stage = kStages - 1;
+    int c_first = 0;      // kTurned: the range's first slab
     // Load v of a lane, from the slab's base on.  kLying: row min(row_in + 16 v, most), this lane's piece of it; kTurned: unit min(v, most), 8 KB apart.  (Of the
     // other operand: its units of 1 KB.)
     const bool lying = kRows == kLying && rows_side, turned = kRows == kTurned && rows_side;
@@ -486,11 +487,12 @@ __global__ __launch_bounds__(WM *WN * 64, kStages * (MF + NF) >= 64 ? 1 : 2) voi
         if (lying) {
             const int64_t row0 = int64_t(tile.m) * (MF * 32), left = q.rows - 1 - row0;
             most = left < MF * 32 ? int(left) : MF * 32;
-            from = q.a.at + row0 * q.lda * 2;
+            from = q.a.at + row0 * q.lda * 2 + int64_t(tile.split) * q.split_slabs * 64;
         } else if (turned) {
             const int kg = tile.m * (MF * 2) + u0, left = q.a.kgs - 1 - kg;
             most = left > 0 ? left : 0;
             from = q.a.at + int64_t(left < 0 ? q.a.kgs - 1 : kg) * (8 * kUnitBytes);
+            c_first = tile.split * q.split_slabs;
         } else {
             const Packed &o = rows_side ? q.a : q.b;
             from = o.at + (((rows_side ? q.planes.a : q.planes.b) >> pair) & 15u) * o.plane() + o.unit(rb, int64_t(tile.split) * q.split_slabs * 2 + k_unit);
@@ -506,7 +508,7 @@ __global__ __launch_bounds__(WM *WN * 64, kStages * (MF + NF) >= 64 ? 1 : 2) voi
     };
     auto next_slab = [&]() {
         step();
-        const uint32_t slab = uint32_t(c_at < c_last ? c_at : c_last);
+        const uint32_t slab = uint32_t((c_at < c_last ? c_at : c_last) + (kRows == kTurned ? c_first : 0));
         const uint64_t step_bytes = turned ? uint64_t(slab >> 3) * (uint64_t(uint32_t(q.a.kgs)) * (8 * kUnitBytes)) + (slab & 7) * uint32_t(kUnitBytes)
                                            : uint64_t(slab) * (lying ? 64u : uint32_t(16 * kUnitBytes));
         const uint64_t at = reinterpret_cast<uint64_t>(from) + step_bytes;

@@ -478,14 +478,31 @@ inline int64_t wide_tiles(int m_units, int n_units, bool big) { return ceil_div(
 // whether tiles of 256 x 256 multiply hardly more than there is (128 of 256 columns fill half of one: weight gradients of 128 x 512, 125,237 rows in fp32
 // 230 us so)
 inline bool fills_big(int m_units, int n_units) { return wide_tiles(m_units, n_units, true) * 4 * 10 <= wide_tiles(m_units, n_units, false) * 11; }
-// One range of k: results go through an epilogue.  A large tile is multiplied 7 % faster (8192 -> 2048, 8,192 rows 267 and 287 us) but is alone on its unit, which does
+// Products of rows.  A large tile is multiplied 7 % faster (8192 -> 2048, 8,192 rows 267 and 287 us) but is alone on its unit, which does
 // nothing else while results are written: where a product is short beside them, and first of all where they are added to something that has to be
 // read, two small ones a unit are faster (256 -> 256 with a residual, 1,000,003 rows in bf16, eight slabs: 719 and 490 us).
-inline WidePlan plan_rows(int row_units, const Packed &b, bool reads)
+// Where the tiles are few and long, ranges of k go to more blocks, and a second kernel joins their shares: as many as make least what a range's slabs take one after the
+// other, 0.3 us each (fp32 1.1), with 3 us for the second kernel and the shares' way to memory and back.  (One range, then those chosen: 128 rows 4096 -> 4096 in bf16 with a
+// residual 59 and 36 us; 100 rows 4096 -> 2 x 1024 in fp32 159 and 42; input gradient and all else backward of 128 rows 2048 -> 2 x 5632 in bf16 186 and 90.)
+inline WidePlan plan_rows(int64_t n, const Packed &b, bool reads, bool fp32)
 {
-    const int slabs = b.kgs / 2;
-    return {wide_tiles(row_units, b.rbs, true) >= kCus * 3 / 4 && fills_big(row_units, b.rbs) && slabs >= (reads ? 64 : 16), 1, slabs};
+    const int slabs = b.kgs / 2, row_units = int(ceil_div(n, kUnitRows));
+    const int64_t tiles = wide_tiles(row_units, b.rbs, false);
+    int ranges = 1;       // of the sizes alone: the workspace is asked for without `reads`
+    float least = 1e30f;
+    for (int r = 1; r == 1 || (r <= 16 && r * tiles <= 2 * kCus && r * 4 <= slabs); ++r) {
+        const float t = float(ceil_div(slabs, r)) * (fp32 ? 1.1f : 0.3f) + (r > 1 ? 3.0f + float(r) * float(n) * float(b.rbs) * (32 * 8 / 3e6f) : 0.0f);
+        if (t < least) {
+            least = t;
+            ranges = r;
+        }
+    }
+    if (ranges == 1)
+        return {!fp32 && wide_tiles(row_units, b.rbs, true) >= kCus * 3 / 4 && fills_big(row_units, b.rbs) && slabs >= (reads ? 64 : 16), 1, slabs};
+    const int per = int(ceil_div(slabs, ranges));
+    return {false, int(ceil_div(slabs, per)), per};
 }
+inline size_t row_shares(const WidePlan &p, int64_t n, const Packed &b) { return p.splits > 1 ? size_t(p.splits) * size_t(n) * size_t(b.rbs) * (kUnitRows * 4) : 0; }
 // ranges of k until the tiles fill the chip, 512 rows each at least; fp32 has small tiles only (two ranges a
 // unit: three were no faster and wrote more, 125,237 rows of 128 x 512 141 and 144 us with their sums)
 inline WidePlan plan_weight(const Packed &a, const Packed &b, bool fp32)
@@ -502,7 +519,7 @@ inline WidePlan plan_weight(const Packed &a, const Packed &b, bool fp32)
     return {false, 1, slabs};
 }
 
-template <RowsAs kRows, class Epi>
+template <RowsAs kRows, bool kSmall, class Epi>
 static int launch_wide_as(const char *name, WideCall q, const WidePlan &p, const Epi &e, hipStream_t s)
 {
     const int units = p.big ? 8 : 4, per_cu = p.big ? 1 : 2;
@@ -514,20 +531,23 @@ static int launch_wide_as(const char *name, WideCall q, const WidePlan &p, const
     if (per_die > 32 * per_cu) per_die = 32 * per_cu;
     TMA_TIMED(name, s);
     const dim3 grid(unsigned(per_die * kWideDies)), block(256);
-    if (p.big) hipLaunchKernelGGL((wide_gemm_kernel<8, 8, 2, 2, 4, kRows, Epi>), grid, block, 0, s, q, e);
-    else hipLaunchKernelGGL((wide_gemm_kernel<4, 4, 2, 2, 3, kRows, Epi>), grid, block, 0, s, q, e);
+    if constexpr (!kSmall)
+        if (p.big) {
+            hipLaunchKernelGGL((wide_gemm_kernel<8, 8, 2, 2, 4, kRows, Epi>), grid, block, 0, s, q, e);
+            return check_launch(name);
+        }
+    hipLaunchKernelGGL((wide_gemm_kernel<4, 4, 2, 2, 3, kRows, Epi>), grid, block, 0, s, q, e);
     return check_launch(name);
 }
-// operands of type T laid out: of bf16 in b_parts parts on the weights' side, of fp32 in three on both; kTurned or not
-template <typename T, RowsAs kRows, class Epi>
-static int launch_wide(const char *name, const Packed &a, const Packed &b, int row_units, int b_parts, const WidePlan &p, const Epi &e, hipStream_t s)
+// operands of type T laid out: of bf16 in one part, on the weights' side in two where q says so, of fp32 in three; kSmall: the plan has small tiles
+template <typename T, RowsAs kRows, bool kSmall = false, class Epi>
+static int launch_wide(const char *name, WideCall q, const WidePlan &p, const Epi &e, hipStream_t s)
 {
-    WideCall q{a, b, planes_of(b_parts), 0, 0, 8, p.splits, p.split_slabs, 0, 0, row_units};
     if constexpr (sizeof(T) == 2) {
-        return launch_wide_as<kRows>(name, q, p, e, s);
+        return launch_wide_as<kRows, kSmall>(name, q, p, e, s);
     } else {
-        q.m_tiles = int(ceil_div(row_units, 4));
-        q.n_tiles = int(ceil_div(b.rbs, 4));
+        q.m_tiles = int(ceil_div(q.row_units, 4));
+        q.n_tiles = int(ceil_div(q.b.rbs, 4));
         if (q.panel > q.n_tiles) q.panel = q.n_tiles;
         const int64_t blocks = ceil_div(int64_t(q.m_tiles) * q.n_tiles * q.splits, kWideDies) * kWideDies;
         if (blocks > INT32_MAX) return fail(TMA_ERR_BAD_SHAPE, "%s: too many tiles", name);
@@ -535,6 +555,42 @@ static int launch_wide(const char *name, const Packed &a, const Packed &b, int r
         hipLaunchKernelGGL((wide_split_kernel<kRows == kTurned, Epi>), dim3(unsigned(blocks)), dim3(256), 0, s, q, e);
         return check_launch(name);
     }
+}
+
+// A product of rows, in ranges of k where the plan says so: their shares [range][row][packed column], and what becomes of the sums
+template <int kSides, class Out>
+static __global__ __launch_bounds__(256) void join_rows_kernel(const float *__restrict__ shares, int ranges, int64_t n, int N, int pitch, Out out)
+{
+    const int64_t cells = n * N, stride = n * pitch;
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < cells; i += int64_t(gridDim.x) * 256) {
+        const int64_t row = i / N;
+        const int c = int(i - row * N);
+        const float *from = shares + row * pitch + (kSides == 2 ? c / 32 * 64 + c % 32 : c);
+        float sum[kSides] = {};
+#pragma unroll 4
+        for (int p = 0; p < ranges; ++p)
+#pragma unroll
+            for (int s = 0; s < kSides; ++s) sum[s] += from[p * stride + s * 32];
+        out.one(row, c, sum[0], sum[kSides - 1]);
+    }
+}
+template <typename T, RowsAs kRows, class Epi>
+static int launch_rows(const char *name, WideCall q, const WidePlan &p, float *shares, int64_t n, int N, const Epi &e, hipStream_t s)
+{
+    q.planes = planes_of(1);
+    q.panel = 8;
+    q.splits = p.splits;
+    q.split_slabs = p.split_slabs;
+    q.row_units = int(ceil_div(n, kUnitRows));
+    if (p.splits == 1) return launch_wide<T, kRows>(name, q, p, e, s);
+    const int pitch = q.b.rbs * kUnitRows;
+    const WeightEpilogue share{{shares, nullptr}, n * pitch, n, pitch, pitch, 1, true};
+    if (int rc = launch_wide<T, kRows, true>(name, q, p, share, s)) return rc;
+    TMA_TIMED("wide_join_rows", s);
+    int64_t blocks = ceil_div(n * N, 256);
+    if (blocks > 8192) blocks = 8192;
+    hipLaunchKernelGGL((join_rows_kernel<Epi::kSides, Epi>), dim3(unsigned(blocks)), dim3(256), 0, s, shares, p.splits, n, N, pitch, e);
+    return check_launch(name);
 }
 
 template <typename T>
@@ -556,6 +612,8 @@ struct Cutter {
 // forward: rows and weights laid out
 struct ForwardPlan {
     Packed a, b;
+    WidePlan rows;
+    float *shares;
     size_t bytes;
 };
 // Rows that a product takes where they lie (see WideCall).  (A tile's rows are within 32 bits of each other.)  That takes their pass off and a tenth more time, for
@@ -568,21 +626,25 @@ inline bool direct_rows(const T *X, int64_t ldx, int32_t F_in, int n_units)
 
 // the product of laid-out weights and of rows, which are laid out here where they have to be
 template <typename T, class Epi>
-static int forward_product(const char *fn, const char *name, int64_t n, const T *X, int64_t ldx, int32_t F_in, ForwardPlan p, bool reads, const Epi &e, hipStream_t s)
+static int forward_product(const char *fn, const char *name, int64_t n, const T *X, int64_t ldx, int32_t F_in, int32_t F_out, const ForwardPlan &p, const Epi &e, hipStream_t s)
 {
-    const WidePlan w = plan_rows(p.a.rbs, p.b, reads);
+    WideCall q{};
+    q.a = p.a;
+    q.b = p.b;
     if constexpr (sizeof(T) == 2)
         if (direct_rows(X, ldx, F_in, p.b.rbs)) {
-            p.a.at = const_cast<char *>(reinterpret_cast<const char *>(X));
-            return launch_wide_as<kLying>(name, WideCall{p.a, p.b, planes_of(1), 0, 0, 8, w.splits, w.split_slabs, ldx, n, p.a.rbs}, w, e, s);
+            q.a.at = const_cast<char *>(reinterpret_cast<const char *>(X));
+            q.lda = ldx;
+            q.rows = n;
+            return launch_rows<T, kLying>(name, q, p.rows, p.shares, n, F_out, e, s);
         }
     launch_pack_rows<T, kPartsOf<T>>("wide_pack_rows", X, nullptr, ldx, n, F_in, false, p.a, s);
     if (int rc = check_launch(fn)) return rc;
-    return launch_wide<T, kUnits_>(name, p.a, p.b, p.a.rbs, 1, w, e, s);
+    return launch_rows<T, kUnits_>(name, q, p.rows, p.shares, n, F_out, e, s);
 }
 
 template <typename T>
-inline ForwardPlan plan_forward(int64_t n, int32_t F_in, int32_t F_out, int sides, void *ws)
+inline ForwardPlan plan_forward(int64_t n, int32_t F_in, int32_t F_out, int sides, bool reads, void *ws)
 {
     ForwardPlan p{};
     if (n <= kFewMost) {      // nothing is laid out
@@ -595,6 +657,8 @@ inline ForwardPlan plan_forward(int64_t n, int32_t F_in, int32_t F_out, int side
     Cutter cut{static_cast<char *>(ws)};
     cut.take(p.a, kPartsOf<T>);
     cut.take(p.b, kPartsOf<T>);
+    p.rows = plan_rows(n, p.b, reads, sizeof(T) == 4);
+    p.shares = static_cast<float *>(cut.take(row_shares(p.rows, n, p.b)));
     p.bytes = cut.used;
     return p;
 }
@@ -602,13 +666,14 @@ inline ForwardPlan plan_forward(int64_t n, int32_t F_in, int32_t F_out, int side
 struct BackwardPlan {
     Packed d_cols, x_cols, w_rows;
     int padded, row_blocks, parts_c;
-    WidePlan weight;
-    float *sums, *partial;
+    WidePlan weight, data;
+    float *sums, *partial, *shares;
     size_t bytes;
 };
-// exact: the gradients of the pre-activations are bf16 as they come (no activation on bf16 rows)
+// exact: the gradients of the pre-activations are bf16 as they come (no activation on bf16 rows); reads: something is added to dX (no matter for the sizes:
+// only tiles enough for large ones, which have no ranges, depend on it)
 template <typename T>
-inline BackwardPlan plan_backward(int64_t n, int32_t F_in, int32_t F_out, int sides, bool exact, bool need_dX, void *ws)
+inline BackwardPlan plan_backward(int64_t n, int32_t F_in, int32_t F_out, int sides, bool exact, bool need_dX, bool reads, void *ws)
 {
     BackwardPlan p;
     p.padded = int(round_up(size_t(F_out), 32));
@@ -626,7 +691,12 @@ inline BackwardPlan plan_backward(int64_t n, int32_t F_in, int32_t F_out, int si
     cut.take(p.x_cols, kPartsOf<T>);
     p.sums = static_cast<float *>(cut.take(size_t(p.row_blocks) * size_t(sides) * size_t(p.padded) * 4));
     p.partial = p.weight.splits > 1 ? static_cast<float *>(cut.take(size_t(p.weight.splits) * size_t(sides) * size_t(F_in) * size_t(F_out) * 4)) : nullptr;
-    if (need_dX) cut.take(p.w_rows, kPartsOf<T>);
+    p.shares = nullptr;
+    if (need_dX) {
+        cut.take(p.w_rows, kPartsOf<T>);
+        p.data = plan_rows(n, p.w_rows, reads, sizeof(T) == 4);
+        p.shares = static_cast<float *>(cut.take(row_shares(p.data, n, p.w_rows)));
+    }
     p.bytes = cut.used;
     return p;
 }
@@ -643,7 +713,7 @@ static int wide_backward(const char *fn, const char *what, int64_t n, const T *X
         return check_launch(fn);
     }
     const bool exact = kSides == 1 && g.act == TMA_ACT_NONE;
-    const BackwardPlan p = plan_backward<T>(n, F_in, N, kSides, exact, dX != nullptr, ws);
+    const BackwardPlan p = plan_backward<T>(n, F_in, N, kSides, exact, dX != nullptr, R != nullptr, ws);
     constexpr int kP = kPartsOf<T>;
     g.by_cols = p.d_cols;
     g.sums = db[0] ? p.sums : nullptr;
@@ -665,7 +735,8 @@ static int wide_backward(const char *fn, const char *what, int64_t n, const T *X
     we.whole16 = N % 4 == 0 && aligned(we.out[0], 16) && (kSides == 1 || aligned(we.out[1], 16));
     char name[64];
     snprintf(name, sizeof(name), "%s_bwd_weight%s", what, sizeof(T) == 2 ? "_bf16" : "");
-    if (int rc = launch_wide<T, kUnits_>(name, p.x_cols, p.d_cols, p.x_cols.rbs, p.parts_c, p.weight, we, s)) return rc;
+    const WideCall weight{p.x_cols, p.d_cols, planes_of(p.parts_c), 0, 0, 8, p.weight.splits, p.weight.split_slabs, 0, 0, p.x_cols.rbs};
+    if (int rc = launch_wide<T, kUnits_>(name, weight, p.weight, we, s)) return rc;
     if (split) launch_join("wide_join", p.partial, p.weight.splits, cells * kSides, cells, cells, dW[0], kSides == 2 ? dW[1] : nullptr, s);
     if (db[0]) launch_join_sums(p.sums, p.row_blocks, kSides, p.padded, N, db[0], db[1], s);
     if (int rc = check_launch(fn)) return rc;
@@ -674,8 +745,10 @@ static int wide_backward(const char *fn, const char *what, int64_t n, const T *X
     if (int rc = check_launch(fn)) return rc;
     const ResidualEpilogue<T> re{nullptr, dX, R, 0, ld_dx, ldr, n, nullptr, F_in, TMA_ACT_NONE, whole_rows(dX, ld_dx), R && whole_rows(R, ldr), false};
     snprintf(name, sizeof(name), "%s_bwd_data%s", what, sizeof(T) == 2 ? "_bf16" : "");
-    const int row_units = int(ceil_div(n, kUnitRows));
-    return launch_wide<T, kTurned>(name, p.d_cols, p.w_rows, row_units, 1, plan_rows(row_units, p.w_rows, R != nullptr), re, s);
+    WideCall data{};
+    data.a = p.d_cols;
+    data.b = p.w_rows;
+    return launch_rows<T, kTurned>(name, data, p.data, p.shares, n, F_in, re, s);
 }
 
 // every number of a call that asks for a workspace, too

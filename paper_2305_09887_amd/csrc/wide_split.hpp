@@ -37,8 +37,10 @@ __global__ __launch_bounds__(256, Epi::kPast ? 2 : 3) void wide_split_kernel(Wid
     const int unit[3] = {half * 2, half ? 0 : 2, half * 2};
     const uint32_t ring0 = lds_address(&ring[0]) + uint32_t(wave * kLoads * kUnitBytes);
     const uint32_t lane_at = turned ? uint32_t((lane >> 5) * (8 * kUnitBytes) + (lane & 31) * 16) : uint32_t(lane * 16);
-    auto fetch = [&](int step) {
-        const uint32_t to = ring0 + uint32_t(step % kStages * kStageBytes);
+    const int turned_from = turned ? tile.split * q.split_slabs * 2 : 0;
+    auto fetch = [&](int at_step) {
+        const uint32_t to = ring0 + uint32_t(at_step % kStages * kStageBytes);
+        const int step = turned_from + at_step;
         const uint64_t along = turned ? uint64_t(uint32_t(step >> 4)) * (uint64_t(uint32_t(o.kgs)) * (8 * kUnitBytes)) + uint32_t(step >> 1 & 7) * uint32_t(kUnitBytes) +
                                             uint32_t(step & 1) * 512u
                                       : uint64_t(uint32_t(step)) * (8 * kUnitBytes);
