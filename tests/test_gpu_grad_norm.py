@@ -96,6 +96,18 @@ def test_norms_of_nothing_of_zero_and_of_no_number(B):
     assert torch.isnan(t).all() and torch.isnan(other).all()
 
 
+def test_more_than_32_bits_of_values(B):
+    n = (1 << 31) + 77
+    t = torch.full((n,), 0.5, dtype=torch.bfloat16, device="cuda")
+    small = torch.full((5,), 0.5, dtype=torch.bfloat16, device="cuda")
+    norm = float(B.tma_grad_norm([small, t]))
+    assert abs(norm - 0.5 * math.sqrt(n + 5)) <= 2.0 ** -23 * norm
+    B.tma_grad_clip([small, t], norm / 4)
+    # 0.5 times a factor within 2^-22 of 1/4: one of bf16's values beside 1/8 at most
+    for part in (small, t[:1000], t[n // 2:n // 2 + 1000], t[-1000:]):
+        assert bool(((part.float() - 0.125).abs() <= 0.125 * 2.0 ** -7).all())
+
+
 def test_an_infinite_bound_leaves_gradients_as_they_are(B):
     t = torch.randn(1000, device="cuda")
     was = t.clone()

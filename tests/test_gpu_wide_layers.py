@@ -341,6 +341,8 @@ def test_few_rows_of_whole_numbers(B, n, fi, fo, more, off, dtype):
             assert torch.equal(t.cpu(), w.float().to(dtype)) and _untouched(flat, t, 7.0)
     alone, _ = B.tma_dense_residual_fwd(x, d(Wu))
     assert torch.equal(alone.cpu(), (X @ Wu).float().to(dtype))
+    B.tma_dense_residual_fwd(x, d(Wg), d(bg), B.TMA_ACT_RELU, R=r, Y_out=r)          # in place
+    assert torch.equal(r.cpu(), want[3].float().to(dtype))
 
 
 def test_an_infinite_last_weight_of_few_rows(B):
@@ -429,3 +431,36 @@ def test_two_streams_at_once(B):
     for t, w in zip(steps, want):
         for k in RESULTS:
             assert torch.equal(t[k], w[k]), k
+
+
+def test_places_past_32_bits(B):
+    """Rows whose places, in elements and more so in bytes, do not fit into 32 bits: of whole numbers, checked at the first and the last ones."""
+    n, fi, fo = 270_001, 64, 8_192
+    g = torch.Generator(device="cuda").manual_seed(0)
+    W = lambda *s, dtype=torch.bfloat16: torch.randint(-1, 2, s, generator=g, device="cuda", dtype=torch.int8).to(dtype)
+    X, Wt, dY, R = W(n, fi), W(fi, fo, dtype=torch.float32), W(n, fo), W(n, fi)
+    assert dY.numel() > 1 << 31
+    Y, _ = B.tma_dense_residual_fwd(X, Wt, R=dY)
+    ends = [slice(0, 200), slice(n // 2, n // 2 + 200), slice(n - 200, n)]
+    for rows in ends:
+        assert torch.equal(Y[rows], (X[rows].float() @ Wt + dY[rows].float()).bfloat16())
+    del Y
+    H, G, U = B.tma_gated_dense_fwd(X, Wt, Wt, act=B.TMA_ACT_NONE)
+    for rows in ends:
+        z = X[rows].float() @ Wt
+        assert torch.equal(G[rows], z.bfloat16()) and torch.equal(U[rows], G[rows]) and torch.equal(H[rows], (z * z).bfloat16())
+    del H, G, U
+    dW, db, dX = B.tma_dense_residual_bwd(X, None, dY, Wt, R=R)
+    for rows in ends:
+        assert torch.equal(dX[rows], (dY[rows].float() @ Wt.t() + R[rows].float()).bfloat16())
+    want, sums = torch.zeros((fi, fo), device="cuda"), torch.zeros(fo, device="cuda")
+    for a in range(0, n, 30_000):          # (sums of whole numbers below 2^24: exact)
+        part = dY[a:a + 30_000].float()
+        want += X[a:a + 30_000].float().t() @ part
+        sums += part.sum(0)
+    assert torch.equal(dW, want) and torch.equal(db, sums)
+    # rows where they lie, far apart
+    far = W(n, 8_192)[:, 96:160]
+    got, _ = B.tma_dense_residual_fwd(far, Wt[:, :40].contiguous())
+    for rows in ends:
+        assert torch.equal(got[rows], (far[rows].float() @ Wt[:, :40]).bfloat16())
