@@ -9,16 +9,14 @@ template <typename T>
 static int residual_fwd(const char *fn, int64_t n, const void *X, int64_t ldx, int32_t F_in, const float *W, const float *bias, int32_t F_out, int32_t act, const void *R,
                         int64_t ldr, void *Z, int64_t ldz, void *Y, int64_t ldy, void *ws, hipStream_t s)
 {
-    constexpr int kP = kPartsOf<T>;
     T *z = static_cast<T *>(Z), *y = static_cast<T *>(Y);
     const T *r = static_cast<const T *>(R);
     const ResidualEpilogue<T> e{z, y, r, ldz, ldy, ldr, n, bias, F_out, act, whole_rows(y, ldy) && (!z || whole_rows(z, ldz)), r && whole_rows(r, ldr),
                                 bias_pieces(bias, F_out)};
     if (n <= kFewMost) return launch_few<T, 1>(fn, sizeof(T) == 2 ? "residual_few_bf16" : "residual_few", n, X, ldx, W, nullptr, F_in, F_out, e, ws, s);
     const ForwardPlan p = plan_forward<T>(n, F_in, F_out, 1, r != nullptr, ws);
-    launch_pack_cols<float, kP>("wide_pack_cols", W, nullptr, F_out, F_in, F_out, true, p.b, s);
-    if (int rc = check_launch(fn)) return rc;
-    return forward_product<T>(fn, sizeof(T) == 2 ? "residual_fwd_bf16" : "residual_fwd", n, static_cast<const T *>(X), ldx, F_in, F_out, p, e, s);
+    const float *const one[2] = {W, nullptr};
+    return forward_product<T>(fn, sizeof(T) == 2 ? "residual_fwd_bf16" : "residual_fwd", n, static_cast<const T *>(X), ldx, F_in, one, F_out, p, e, s);
 }
 
 template <typename T>

@@ -11,15 +11,13 @@ template <typename T>
 static int gated_fwd(const char *fn, int64_t n, const void *X, int64_t ldx, int32_t F_in, const float *W_gate, const float *W_up, const float *b_gate, const float *b_up,
                      int32_t F_out, int32_t act, void *G, void *U, int64_t ldg, void *H, int64_t ldh, void *ws, hipStream_t s)
 {
-    constexpr int kP = kPartsOf<T>;
     T *g = static_cast<T *>(G), *u = static_cast<T *>(U), *h = static_cast<T *>(H);
     const GatedEpilogue<T> e{g, u, h, ldg, ldh, n, b_gate, b_up, F_out, act, whole_rows(h, ldh) && (!g || (whole_rows(g, ldg) && whole_rows(u, ldg))),
                              bias_pieces(b_gate, F_out) && bias_pieces(b_up, F_out)};
     if (n <= kFewMost) return launch_few<T, 2>(fn, sizeof(T) == 2 ? "gated_few_bf16" : "gated_few", n, X, ldx, W_gate, W_up, F_in, F_out, e, ws, s);
     const ForwardPlan p = plan_forward<T>(n, F_in, F_out, 2, false, ws);
-    launch_pack_cols<float, kP>("wide_pack_cols", W_gate, W_up, F_out, F_in, F_out, true, p.b, s);
-    if (int rc = check_launch(fn)) return rc;
-    return forward_product<T>(fn, sizeof(T) == 2 ? "gated_fwd_bf16" : "gated_fwd", n, static_cast<const T *>(X), ldx, F_in, F_out, p, e, s);
+    const float *const W[2] = {W_gate, W_up};
+    return forward_product<T>(fn, sizeof(T) == 2 ? "gated_fwd_bf16" : "gated_fwd", n, static_cast<const T *>(X), ldx, F_in, W, F_out, p, e, s);
 }
 
 template <typename T>

@@ -160,15 +160,16 @@ struct RowsPack {
     int side_kgs;
     Packed out;
 };
+template <int kParts>
+using RowsTile = uint4[kParts][kPackThreads];
 template <typename T, int kParts>
-__global__ __launch_bounds__(kPackThreads) void pack_rows_kernel(RowsPack q)
+__device__ __forceinline__ void pack_rows(const RowsPack &q, int block, int blocks, RowsTile<kParts> &tile)
 {
-    __shared__ __attribute__((aligned(16))) uint4 tile[kParts][kPackThreads];
     const int t = threadIdx.x, r = t / 8, piece = t % 8;
     const int quads = (q.out.kgs + 3) / 4;
     const int64_t all = int64_t(q.out.rbs) * quads;
     const int slot = (piece / 2) * 64 + (q.weights ? weights_place(fragment_row(r), piece % 2, piece / 2) : rows_place(r, piece % 2));
-    for (int64_t i = blockIdx.x; i < all; i += gridDim.x) {
+    for (int64_t i = block; i < all; i += blocks) {
         const int64_t rb = i / quads, row = rb * kUnitRows + r;
         const int kg0 = int(i % quads) * 4, kg = kg0 + piece / 2;
         const int side = kg < q.side_kgs ? 0 : 1;
@@ -219,17 +220,17 @@ struct ColsPack {
     const void *src[2];
     int64_t ld, rows, cols;
     int sides;
-    bool weights;
+    bool weights, pairs;
     Packed out;
 };
 template <typename T, int kParts, int kTogether>
-__global__ __launch_bounds__(kPackThreads) void pack_cols_kernel(ColsPack q)
+__device__ __forceinline__ void pack_cols_as(const ColsPack &q, int block, int blocks)
 {
     constexpr int kWidth = 128 * kTogether;
     const int t = threadIdx.x, c_in = t % 128 * kTogether, half = t / 128;
     const int side_rbs = q.out.rbs / q.sides, strips = (side_rbs * kUnitRows + kWidth - 1) / kWidth;
     const int64_t all = int64_t(strips) * q.out.kgs * q.sides;
-    for (int64_t i = blockIdx.x; i < all; i += gridDim.x) {
+    for (int64_t i = block; i < all; i += blocks) {
         const int strip = int(i % strips), side = int(i / strips % q.sides);
         const int64_t kg = i / strips / q.sides;
         const int64_t col = int64_t(strip) * kWidth + c_in, k0 = kg * kUnitK + half * 8;
@@ -259,28 +260,37 @@ __global__ __launch_bounds__(kPackThreads) void pack_cols_kernel(ColsPack q)
     }
 }
 
-inline unsigned pack_blocks(int64_t items) { return unsigned(items < 1 ? 1 : items > 8192 ? 8192 : items); }
-
 template <typename T, int kParts>
-static void launch_pack_rows(const char *name, const void *first, const void *second, int64_t ld, int64_t rows, int64_t cols, bool weights, const Packed &out, hipStream_t s)
+__device__ __forceinline__ void pack_cols(const ColsPack &q, int block, int blocks)
+{
+    if constexpr (sizeof(T) == 2)
+        if (q.pairs) return pack_cols_as<T, kParts, 2>(q, block, blocks);
+    pack_cols_as<T, kParts, 1>(q, block, blocks);
+}
+
+inline int pack_blocks(int64_t items) { return int(items < 1 ? 1 : items > 8192 ? 8192 : items); }
+template <typename T>
+inline RowsPack rows_pack(const void *first, const void *second, int64_t ld, int64_t rows, int64_t cols, bool weights, const Packed &out)
 {
     const bool whole = whole_rows(static_cast<const T *>(first), ld) && (!second || whole_rows(static_cast<const T *>(second), ld));
-    const RowsPack q{{first, second}, ld, rows, cols, whole, weights, second ? out.kgs / 2 : out.kgs, out};
-    TMA_TIMED(name, s);
-    hipLaunchKernelGGL((pack_rows_kernel<T, kParts>), dim3(pack_blocks(int64_t(out.rbs) * ((out.kgs + 3) / 4))), dim3(kPackThreads), 0, s, q);
+    return {{first, second}, ld, rows, cols, whole, weights, second ? out.kgs / 2 : out.kgs, out};
 }
-template <typename T, int kParts>
-static void launch_pack_cols(const char *name, const void *first, const void *second, int64_t ld, int64_t rows, int64_t cols, bool weights, const Packed &out, hipStream_t s)
+inline int blocks_of(const RowsPack &q) { return pack_blocks(int64_t(q.out.rbs) * ((q.out.kgs + 3) / 4)); }
+template <typename T>
+inline ColsPack cols_pack(const void *first, const void *second, int64_t ld, int64_t rows, int64_t cols, bool weights, const Packed &out)
 {
-    const int sides = second ? 2 : 1;
-    const ColsPack q{{first, second}, ld, rows, cols, sides, weights, out};
-    TMA_TIMED(name, s);
-    if constexpr (sizeof(T) == 2)
-        if (cols % 2 == 0 && ld % 2 == 0 && aligned(first, 4) && aligned(second, 4)) {
-            hipLaunchKernelGGL((pack_cols_kernel<T, kParts, 2>), dim3(pack_blocks(ceil_div(out.rbs / sides, 8) * out.kgs * sides)), dim3(kPackThreads), 0, s, q);
-            return;
-        }
-    hipLaunchKernelGGL((pack_cols_kernel<T, kParts, 1>), dim3(pack_blocks(ceil_div(out.rbs / sides, 4) * out.kgs * sides)), dim3(kPackThreads), 0, s, q);
+    const bool pairs = sizeof(T) == 2 && cols % 2 == 0 && ld % 2 == 0 && aligned(first, 4) && aligned(second, 4);
+    return {{first, second}, ld, rows, cols, second ? 2 : 1, weights, pairs, out};
+}
+inline int blocks_of(const ColsPack &q) { return pack_blocks(ceil_div(q.out.rbs / q.sides, q.pairs ? 8 : 4) * q.out.kgs * q.sides); }
+
+// Forward: weights by columns, in the first `cols` blocks, and rows, in what blocks there are beyond
+template <typename T, int kParts>
+__global__ __launch_bounds__(kPackThreads) void forward_layouts_kernel(ColsPack w, RowsPack x, int cols)
+{
+    __shared__ __attribute__((aligned(16))) RowsTile<kParts> tile;
+    if (int(blockIdx.x) < cols) pack_cols<float, kParts>(w, int(blockIdx.x), cols);
+    else pack_rows<T, kParts>(x, int(blockIdx.x) - cols, int(gridDim.x) - cols, tile);
 }
 
 // ---- the product ---------------------------------------------------------------

@@ -352,13 +352,17 @@ struct GradCall {
     float *sums;                  // [blocks along the rows][sides * padded], or NULL
     int row_blocks;
 };
+template <int kSides>
+struct GradTile {
+    float tile[kSides][32][65], joined[kSides][4][64];
+};
 template <typename T, int kSides, int kParts>
-__global__ __launch_bounds__(256) void grad_pack_kernel(GradCall<T> q)
+__device__ __forceinline__ void grad_pack(const GradCall<T> &q, int block, GradTile<kSides> &lds)
 {
-    __shared__ float tile[kSides][32][65];
-    __shared__ float joined[kSides][4][64];
+    auto &tile = lds.tile;
+    auto &joined = lds.joined;
     const int t = threadIdx.x, r = t / 8, piece = t % 8, col_in = t % 64, quarter = t / 64;
-    const int strips = (q.N + 63) / 64, strip = int(blockIdx.x) % strips, rows_at = int(blockIdx.x) / strips;
+    const int strips = (q.N + 63) / 64, strip = block % strips, rows_at = block / strips;
     const int c0 = strip * 64, padded = (q.N + 31) / 32 * 32, c = c0 + piece * 8;
     const int64_t tiles = (q.n + 31) / 32;
     float sum[kSides] = {};
@@ -424,48 +428,73 @@ __global__ __launch_bounds__(256) void grad_pack_kernel(GradCall<T> q)
     }
 }
 
-// out[side][i] = the ranges' shares added up in their order
-static __global__ __launch_bounds__(256) void join_ranges_kernel(const float *__restrict__ partial, int ranges, int64_t range_stride, int64_t side_stride, int64_t count,
-                                                          float *first, float *second)
+// Backward: the gradients of the pre-activations in the first `grads` blocks, the rows by columns in the next `cols`, the weights by rows in what blocks there are
+// beyond.  One launch: a call of a few hundred rows is launches above all.
+template <typename T, int kSides, int kParts>
+__global__ __launch_bounds__(256) void backward_layouts_kernel(GradCall<T> g, ColsPack x, RowsPack w, int grads, int cols)
 {
-    float *out = blockIdx.y ? second : first;
-    const float *in = partial + blockIdx.y * side_stride;
-    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < count; i += int64_t(gridDim.x) * 256) {
-        float sum = 0.0f;
-#pragma unroll 4
-        for (int p = 0; p < ranges; ++p) sum += in[p * range_stride + i];
-        out[i] = sum;
-    }
-}
-static void launch_join(const char *name, const float *partial, int ranges, int64_t range_stride, int64_t side_stride, int64_t count, float *first, float *second, hipStream_t s)
-{
-    TMA_TIMED(name, s);
-    int64_t blocks = ceil_div(count, 256);
-    if (blocks > 4096) blocks = 4096;
-    hipLaunchKernelGGL(join_ranges_kernel, dim3(unsigned(blocks < 1 ? 1 : blocks), second ? 2 : 1), dim3(256), 0, s, partial, ranges, range_stride, side_stride, count, first, second);
+    constexpr int kP = sizeof(T) == 2 ? 1 : 3;
+    __shared__ __attribute__((aligned(16))) union {
+        GradTile<kSides> gradients;
+        RowsTile<kP> rows;
+    } lds;
+    const int block = int(blockIdx.x);
+    if (block < grads) grad_pack<T, kSides, kParts>(g, block, lds.gradients);
+    else if (block < grads + cols) pack_cols<T, kP>(x, block - grads, cols);
+    else pack_rows<float, kP>(w, block - grads - cols, int(gridDim.x) - grads - cols, lds.rows);
 }
 
-// out[side][i] = the blocks' sums of column i: 64 threads a column, each every 64th of them, joined in a fixed order
-static __global__ __launch_bounds__(1024) void join_sums_kernel(const float *__restrict__ sums, int blocks, int sides, int padded, int N, float *first, float *second)
+// What the ranges and the blocks of the layouts left: out[side][i] = the ranges' shares added up in their order, in the first sides * range_blocks blocks; then
+// sums_out[side][i] = the blocks' sums of column i, 16 columns a block, 64 threads a column, each every 64th of them, joined in a fixed order.
+struct JoinCall {
+    const float *partial;
+    int ranges, range_blocks, sides;
+    int64_t range_stride, side_stride, count;
+    float *out[2];
+    const float *sums;
+    int sum_blocks, padded, N;
+    float *sums_out[2];
+};
+static __global__ __launch_bounds__(1024) void join_kernel(JoinCall q)
 {
     __shared__ float part[64][17];
-    const int c = threadIdx.x % 16, g = threadIdx.x / 16, side = blockIdx.y, col = blockIdx.x * 16 + c;
+    const int block = int(blockIdx.x), of_ranges = q.sides * q.range_blocks;
+    if (block < of_ranges) {
+        const int side = block / q.range_blocks;
+        const float *in = q.partial + side * q.side_stride;
+        float *out = side ? q.out[1] : q.out[0];
+        for (int64_t i = int64_t(block % q.range_blocks) * 1024 + threadIdx.x; i < q.count; i += int64_t(q.range_blocks) * 1024) {
+            float sum = 0.0f;
+#pragma unroll 4
+            for (int p = 0; p < q.ranges; ++p) sum += in[p * q.range_stride + i];
+            out[i] = sum;
+        }
+        return;
+    }
+    const int strips = (q.N + 15) / 16, at = block - of_ranges, side = at / strips;
+    const int c = threadIdx.x % 16, g = threadIdx.x / 16, col = at % strips * 16 + c;
     float sum = 0.0f;
-    if (col < N) {
+    if (col < q.N) {
 #pragma unroll 8
-        for (int p = g; p < blocks; p += 64) sum += sums[(int64_t(p) * sides + side) * padded + col];
+        for (int p = g; p < q.sum_blocks; p += 64) sum += q.sums[(int64_t(p) * q.sides + side) * q.padded + col];
     }
     part[g][c] = sum;
     for (int half = 32; half; half >>= 1) {
         __syncthreads();
         if (g < half) part[g][c] += part[g + half][c];
     }
-    if (g == 0 && col < N) (side ? second : first)[col] = part[0][c];
+    if (g == 0 && col < q.N) (side ? q.sums_out[1] : q.sums_out[0])[col] = part[0][c];
 }
-static void launch_join_sums(const float *sums, int blocks, int sides, int padded, int N, float *first, float *second, hipStream_t s)
+// partial NULL and ranges 1: the product has stored its results itself; sums_out NULL: not wanted
+static int launch_join(const char *fn, JoinCall q, hipStream_t s)
 {
-    TMA_TIMED("wide_join_sums", s);
-    hipLaunchKernelGGL(join_sums_kernel, dim3(unsigned(ceil_div(N, 16)), unsigned(sides)), dim3(1024), 0, s, sums, blocks, sides, padded, N, first, second);
+    const int64_t wide = ceil_div(q.count, 1024);
+    q.range_blocks = q.ranges == 1 ? 0 : int(wide < 1 ? 1 : wide > 1024 ? 1024 : wide);
+    const int64_t blocks = int64_t(q.sides) * (q.range_blocks + (q.sums_out[0] ? ceil_div(q.N, 16) : 0));
+    if (blocks == 0) return TMA_OK;
+    TMA_TIMED("wide_join", s);
+    hipLaunchKernelGGL(join_kernel, dim3(unsigned(blocks)), dim3(1024), 0, s, q);
+    return check_launch(fn);
 }
 
 // ---- plans ---------------------------------------------------------------------
@@ -624,22 +653,31 @@ inline bool direct_rows(const T *X, int64_t ldx, int32_t F_in, int n_units)
     return sizeof(T) == 2 && whole_rows(X, ldx) && F_in % 32 == 0 && ldx <= (1 << 22) && n_units <= 128;
 }
 
-// the product of laid-out weights and of rows, which are laid out here where they have to be
+// the product of weights, laid out here, and of rows, laid out where they have to be
 template <typename T, class Epi>
-static int forward_product(const char *fn, const char *name, int64_t n, const T *X, int64_t ldx, int32_t F_in, int32_t F_out, const ForwardPlan &p, const Epi &e, hipStream_t s)
+static int forward_product(const char *fn, const char *name, int64_t n, const T *X, int64_t ldx, int32_t F_in, const float *const (&W)[2], int32_t F_out, const ForwardPlan &p,
+                           const Epi &e, hipStream_t s)
 {
+    constexpr int kP = kPartsOf<T>;
+    const ColsPack w = cols_pack<float>(W[0], W[1], F_out, F_in, F_out, true, p.b);
+    const RowsPack x = rows_pack<T>(X, nullptr, ldx, n, F_in, false, p.a);
+    const bool direct = direct_rows(X, ldx, F_in, p.b.rbs);
+    {
+        const int cols = blocks_of(w);
+        TMA_TIMED("wide_layouts", s);
+        hipLaunchKernelGGL((forward_layouts_kernel<T, kP>), dim3(unsigned(cols + (direct ? 0 : blocks_of(x)))), dim3(kPackThreads), 0, s, w, x, cols);
+        if (int rc = check_launch(fn)) return rc;
+    }
     WideCall q{};
     q.a = p.a;
     q.b = p.b;
     if constexpr (sizeof(T) == 2)
-        if (direct_rows(X, ldx, F_in, p.b.rbs)) {
+        if (direct) {
             q.a.at = const_cast<char *>(reinterpret_cast<const char *>(X));
             q.lda = ldx;
             q.rows = n;
             return launch_rows<T, kLying>(name, q, p.rows, p.shares, n, F_out, e, s);
         }
-    launch_pack_rows<T, kPartsOf<T>>("wide_pack_rows", X, nullptr, ldx, n, F_in, false, p.a, s);
-    if (int rc = check_launch(fn)) return rc;
     return launch_rows<T, kUnits_>(name, q, p.rows, p.shares, n, F_out, e, s);
 }
 
@@ -707,29 +745,26 @@ static int wide_backward(const char *fn, const char *what, int64_t n, const T *X
                          float *const (&db)[2], T *dX, int64_t ld_dx, const T *R, int64_t ldr, void *ws, hipStream_t s)
 {
     const int32_t N = g.N;
-    if (n == 0) {      // (no ranges: zeros)
-        launch_join("wide_join", nullptr, 0, 0, 0, int64_t(F_in) * N, dW[0], kSides == 2 ? dW[1] : nullptr, s);
-        if (db[0]) launch_join_sums(nullptr, 0, kSides, 0, N, db[0], db[1], s);
-        return check_launch(fn);
-    }
+    const int64_t cells = int64_t(F_in) * N;
+    JoinCall join{nullptr, 0, 0, kSides, 0, 0, cells, {dW[0], dW[1]}, nullptr, 0, 0, N, {db[0], db[1]}};
+    if (n == 0) return launch_join(fn, join, s);      // (no ranges: zeros)
     const bool exact = kSides == 1 && g.act == TMA_ACT_NONE;
     const BackwardPlan p = plan_backward<T>(n, F_in, N, kSides, exact, dX != nullptr, R != nullptr, ws);
-    constexpr int kP = kPartsOf<T>;
     g.by_cols = p.d_cols;
     g.sums = db[0] ? p.sums : nullptr;
     g.row_blocks = p.row_blocks;
     {
-        TMA_TIMED("wide_grad_pack", s);
-        const dim3 grid(unsigned(ceil_div(N, 64) * p.row_blocks)), block(256);
-        if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((grad_pack_kernel<T, kSides, 3>), grid, block, 0, s, g);
-        else if constexpr (kSides == 2) hipLaunchKernelGGL((grad_pack_kernel<T, kSides, 2>), grid, block, 0, s, g);
-        else if (exact) hipLaunchKernelGGL((grad_pack_kernel<T, kSides, 1>), grid, block, 0, s, g);
-        else hipLaunchKernelGGL((grad_pack_kernel<T, kSides, 2>), grid, block, 0, s, g);
+        const ColsPack x = cols_pack<T>(X, nullptr, ldx, n, F_in, false, p.x_cols);
+        const RowsPack w = rows_pack<float>(W[0], kSides == 2 ? W[1] : nullptr, N, F_in, N, true, p.w_rows);
+        const int grads = int(ceil_div(N, 64)) * p.row_blocks, cols = blocks_of(x);
+        TMA_TIMED("wide_layouts", s);
+        const dim3 grid(unsigned(grads + cols + (dX ? blocks_of(w) : 0))), block(256);
+        if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((backward_layouts_kernel<T, kSides, 3>), grid, block, 0, s, g, x, w, grads, cols);
+        else if constexpr (kSides == 2) hipLaunchKernelGGL((backward_layouts_kernel<T, kSides, 2>), grid, block, 0, s, g, x, w, grads, cols);
+        else if (exact) hipLaunchKernelGGL((backward_layouts_kernel<T, kSides, 1>), grid, block, 0, s, g, x, w, grads, cols);
+        else hipLaunchKernelGGL((backward_layouts_kernel<T, kSides, 2>), grid, block, 0, s, g, x, w, grads, cols);
         if (int rc = check_launch(fn)) return rc;
     }
-    launch_pack_cols<T, kP>("wide_pack_cols", X, nullptr, ldx, n, F_in, false, p.x_cols, s);
-    if (int rc = check_launch(fn)) return rc;
-    const int64_t cells = int64_t(F_in) * N;
     const bool split = p.weight.splits > 1;
     WeightEpilogue we{{split ? p.partial : dW[0], split ? p.partial + cells : dW[1]}, cells * kSides, F_in, N, p.padded, kSides, false};
     we.whole16 = N % 4 == 0 && aligned(we.out[0], 16) && (kSides == 1 || aligned(we.out[1], 16));
@@ -737,12 +772,15 @@ static int wide_backward(const char *fn, const char *what, int64_t n, const T *X
     snprintf(name, sizeof(name), "%s_bwd_weight%s", what, sizeof(T) == 2 ? "_bf16" : "");
     const WideCall weight{p.x_cols, p.d_cols, planes_of(p.parts_c), 0, 0, 8, p.weight.splits, p.weight.split_slabs, 0, 0, p.x_cols.rbs};
     if (int rc = launch_wide<T, kUnits_>(name, weight, p.weight, we, s)) return rc;
-    if (split) launch_join("wide_join", p.partial, p.weight.splits, cells * kSides, cells, cells, dW[0], kSides == 2 ? dW[1] : nullptr, s);
-    if (db[0]) launch_join_sums(p.sums, p.row_blocks, kSides, p.padded, N, db[0], db[1], s);
-    if (int rc = check_launch(fn)) return rc;
+    join.partial = p.partial;
+    join.ranges = p.weight.splits;
+    join.range_stride = cells * kSides;
+    join.side_stride = cells;
+    join.sums = p.sums;
+    join.sum_blocks = p.row_blocks;
+    join.padded = p.padded;
+    if (int rc = launch_join(fn, join, s)) return rc;
     if (!dX) return TMA_OK;
-    launch_pack_rows<float, kP>("wide_pack_rows", W[0], kSides == 2 ? W[1] : nullptr, N, F_in, N, true, p.w_rows, s);
-    if (int rc = check_launch(fn)) return rc;
     const ResidualEpilogue<T> re{nullptr, dX, R, 0, ld_dx, ldr, n, nullptr, F_in, TMA_ACT_NONE, whole_rows(dX, ld_dx), R && whole_rows(R, ldr), false};
     snprintf(name, sizeof(name), "%s_bwd_data%s", what, sizeof(T) == 2 ? "_bf16" : "");
     WideCall data{};
