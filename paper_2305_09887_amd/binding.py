@@ -1170,8 +1170,8 @@ def _new_rows(X, cols, stream):
     return _record(_padded(n, cols, X.dtype, X.device), stream)
 
 
-def _forward_room(ws, nbytes, X, stream):
-    """The workspace of a forward call on X's device (of X's type: the shortest way to memory), or none where it needs none."""
+def _wide_room(ws, nbytes, X, stream):
+    """The workspace of a call on X's device (of X's type: the shortest way to memory), or none where it needs none."""
     return _record(X.new_empty(nbytes // X.itemsize), stream) if ws is None and nbytes else ws
 
 
@@ -1219,7 +1219,7 @@ def tma_gated_dense_fwd(X, W_gate, W_up, b_gate=None, b_up=None, act: int = TMA_
     if H_out is None:
         H_out = _new_rows(X, F_out, stream)
     _same_ld(G_out, U_out, f"{where}: G_out / U_out")
-    ws = _forward_room(ws, tma_gated_dense_fwd_workspace_bytes(n, F_in, F_out, dtype), X, stream)
+    ws = _wide_room(ws, tma_gated_dense_fwd_workspace_bytes(n, F_in, F_out, dtype), X, stream)
     G, ldg = _rows_or_none(G_out, "G_out", (n, F_out), X.dtype)
     _launch(dev, stream, lib().tma_gated_dense_fwd, n, X.data_ptr(), ldx, F_in,
             _vector(W_gate, "W_gate", (F_in, F_out), torch.float32), _vector(W_up, "W_up", (F_in, F_out), torch.float32),
@@ -1243,14 +1243,13 @@ def tma_gated_dense_bwd(X, G, U, dH, W_gate, W_up, act: int = TMA_ACT_SILU, R=No
     F_out = _weight_shape(where, "W_gate", W_gate, F_in)
     dtype = _feat_dtype(X)
     _same_ld(G, U, f"{where}: G / U")
-    new = lambda shape: _record(torch.empty(shape, dtype=torch.float32, device=dev), stream)
+    new = lambda shape: _record(W_gate.new_empty(shape), stream)
     dW_gate = new((F_in, F_out)) if dW_gate is None else dW_gate
     dW_up = new((F_in, F_out)) if dW_up is None else dW_up
     db_gate = None if not need_dbias else new((F_out,)) if db_gate is None else db_gate
     db_up = None if not need_dbias else new((F_out,)) if db_up is None else db_up
     dX_out = None if not need_dX else _new_rows(X, F_in, stream) if dX_out is None else dX_out
-    if ws is None:
-        ws = _workspace(tma_gated_dense_bwd_workspace_bytes(n, F_in, F_out, dtype, need_dX), dev, stream)
+    ws = _wide_room(ws, tma_gated_dense_bwd_workspace_bytes(n, F_in, F_out, dtype, need_dX), X, stream)
     _rows_like(U, "U", (n, F_out), X.dtype)
     _launch(dev, stream, lib().tma_gated_dense_bwd, n, X.data_ptr(), ldx, G.data_ptr(), U.data_ptr(),
             _rows_like(G, "G", (n, F_out), X.dtype), dH.data_ptr(), _rows_like(dH, "dH", (n, F_out), X.dtype),
@@ -1279,7 +1278,7 @@ def tma_dense_residual_fwd(X, W, bias=None, act: int = TMA_ACT_NONE, R=None, sav
         Z_out = _new_rows(X, F_out, stream)
     if Y_out is None:
         Y_out = _new_rows(X, F_out, stream)
-    ws = _forward_room(ws, tma_dense_residual_fwd_workspace_bytes(n, F_in, F_out, dtype), X, stream)
+    ws = _wide_room(ws, tma_dense_residual_fwd_workspace_bytes(n, F_in, F_out, dtype), X, stream)
     _launch(dev, stream, lib().tma_dense_residual_fwd, n, X.data_ptr(), ldx, F_in,
             _vector(W, "W", (F_in, F_out), torch.float32), _vector(bias, "bias", (F_out,), torch.float32), F_out, act, dtype,
             *_rows_or_none(R, "R", (n, F_out), X.dtype), *_rows_or_none(Z_out, "Z_out", (n, F_out), X.dtype), Y_out.data_ptr(),
@@ -1304,12 +1303,11 @@ def tma_dense_residual_bwd(X, Z, dY, W, act: int = TMA_ACT_NONE, R=None, dW=None
         Z = None
     elif Z is None:
         raise TmaError(f"{where}: Z is required with an activation")
-    new = lambda shape: _record(torch.empty(shape, dtype=torch.float32, device=dev), stream)
+    new = lambda shape: _record(W.new_empty(shape), stream)
     dW = new((F_in, F_out)) if dW is None else dW
     dbias = None if not need_dbias else new((F_out,)) if dbias is None else dbias
     dX_out = None if not need_dX else _new_rows(X, F_in, stream) if dX_out is None else dX_out
-    if ws is None:
-        ws = _workspace(tma_dense_residual_bwd_workspace_bytes(n, F_in, F_out, act, dtype, need_dX), dev, stream)
+    ws = _wide_room(ws, tma_dense_residual_bwd_workspace_bytes(n, F_in, F_out, act, dtype, need_dX), X, stream)
     _launch(dev, stream, lib().tma_dense_residual_bwd, n, X.data_ptr(), ldx,
             *_rows_or_none(Z, "Z", (n, F_out), X.dtype), dY.data_ptr(), _rows_like(dY, "dY", (n, F_out), X.dtype),
             _vector(W, "W", (F_in, F_out), torch.float32), F_in, F_out, act, dtype, _vector(dW, "dW", (F_in, F_out), torch.float32),
