@@ -11,12 +11,17 @@ static int residual_fwd(const char *fn, int64_t n, const void *X, int64_t ldx, i
 {
     T *z = static_cast<T *>(Z), *y = static_cast<T *>(Y);
     const T *r = static_cast<const T *>(R);
-    const ResidualEpilogue<T> e{z, y, r, ldz, ldy, ldr, n, bias, F_out, act, whole_rows(y, ldy) && (!z || whole_rows(z, ldz)), r && whole_rows(r, ldr),
-                                bias_pieces(bias, F_out)};
-    if (n <= kFewMost) return launch_few<T, 1>(fn, sizeof(T) == 2 ? "residual_few_bf16" : "residual_few", n, X, ldx, W, nullptr, F_in, F_out, e, ws, s);
+    auto make = [&](auto streamed) {
+        return ResidualEpilogue<T, decltype(streamed)::value>{z, y, r, ldz, ldy, ldr, n, bias, F_out, act, whole_rows(y, ldy) && (!z || whole_rows(z, ldz)),
+                                                              r && whole_rows(r, ldr), bias_pieces(bias, F_out)};
+    };
+    if (n <= kFewMost) return launch_few<T, 1>(fn, sizeof(T) == 2 ? "residual_few_bf16" : "residual_few", n, X, ldx, W, nullptr, F_in, F_out, make(std::false_type{}), ws, s);
     const ForwardPlan p = plan_forward<T>(n, F_in, F_out, 1, r != nullptr, ws);
     const float *const one[2] = {W, nullptr};
-    return forward_product<T>(fn, sizeof(T) == 2 ? "residual_fwd_bf16" : "residual_fwd", n, static_cast<const T *>(X), ldx, F_in, one, F_out, p, e, s);
+    auto go = [&](auto streamed) {
+        return forward_product<T>(fn, sizeof(T) == 2 ? "residual_fwd_bf16" : "residual_fwd", n, static_cast<const T *>(X), ldx, F_in, one, F_out, p, make(streamed), s);
+    };
+    return past_caches(n, F_out, sizeof(T) * (z ? 2 : 1)) ? go(std::true_type{}) : go(std::false_type{});
 }
 
 template <typename T>

@@ -12,12 +12,18 @@ static int gated_fwd(const char *fn, int64_t n, const void *X, int64_t ldx, int3
                      int32_t F_out, int32_t act, void *G, void *U, int64_t ldg, void *H, int64_t ldh, void *ws, hipStream_t s)
 {
     T *g = static_cast<T *>(G), *u = static_cast<T *>(U), *h = static_cast<T *>(H);
-    const GatedEpilogue<T> e{g, u, h, ldg, ldh, n, b_gate, b_up, F_out, act, whole_rows(h, ldh) && (!g || (whole_rows(g, ldg) && whole_rows(u, ldg))),
-                             bias_pieces(b_gate, F_out) && bias_pieces(b_up, F_out)};
-    if (n <= kFewMost) return launch_few<T, 2>(fn, sizeof(T) == 2 ? "gated_few_bf16" : "gated_few", n, X, ldx, W_gate, W_up, F_in, F_out, e, ws, s);
+    auto make = [&](auto streamed) {
+        return GatedEpilogue<T, decltype(streamed)::value>{g, u, h, ldg, ldh, n, b_gate, b_up, F_out, act, whole_rows(h, ldh) && (!g || (whole_rows(g, ldg) && whole_rows(u, ldg))),
+                                                           bias_pieces(b_gate, F_out) && bias_pieces(b_up, F_out)};
+    };
+    if (n <= kFewMost)
+        return launch_few<T, 2>(fn, sizeof(T) == 2 ? "gated_few_bf16" : "gated_few", n, X, ldx, W_gate, W_up, F_in, F_out, make(std::false_type{}), ws, s);
     const ForwardPlan p = plan_forward<T>(n, F_in, F_out, 2, false, ws);
     const float *const W[2] = {W_gate, W_up};
-    return forward_product<T>(fn, sizeof(T) == 2 ? "gated_fwd_bf16" : "gated_fwd", n, static_cast<const T *>(X), ldx, F_in, W, F_out, p, e, s);
+    auto go = [&](auto streamed) {
+        return forward_product<T>(fn, sizeof(T) == 2 ? "gated_fwd_bf16" : "gated_fwd", n, static_cast<const T *>(X), ldx, F_in, W, F_out, p, make(streamed), s);
+    };
+    return past_caches(n, F_out, sizeof(T) * (g ? 3 : 1)) ? go(std::true_type{}) : go(std::false_type{});
 }
 
 template <typename T>
