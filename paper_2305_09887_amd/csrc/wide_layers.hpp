@@ -261,7 +261,11 @@ struct ResidualEpilogue {
             if (row >= M || c >= N) continue;
             const T *from = R + row * ldr + c;
             if (past16 && c + L::E <= N) {
-                p.v[k] = *reinterpret_cast<const uint4 *>(from);
+                const Words *words = reinterpret_cast<const Words *>(from);
+                Words w;
+                if constexpr (kStreamed) w = __builtin_nontemporal_load(words);
+                else w = *words;
+                p.v[k] = make_uint4(w[0], w[1], w[2], w[3]);
             } else {
                 T one[L::E];
 #pragma unroll
