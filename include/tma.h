@@ -791,8 +791,8 @@ int tma_dense_residual_bwd(int64_t n, const void *X, int64_t ldx, const void *Z,
  * written where c = 1); h_outs[i] may be h_grads[i].  norm_out [1] fp32
  * (device).  Squares and their sum are fp64, each result is rounded once.  A
  * norm of NaN makes all results NaN, an infinite one finite gradients 0 and
- * infinite ones NaN.  max_norm >= 0.  At most 131072 tensors.  Results that
- * overlap are refused.
+ * infinite ones NaN.  max_norm >= 0.  At most 131072 tensors.  Refused: results that
+ * overlap each other, or a gradient that is not h_outs[i]'s own h_grads[i]; norm_out of a clipping within a gradient or result.
  * The calls may be captured: a graph keeps the pointers and lengths.
  * Workspace: tma_grad_norm_workspace_bytes(n_tensors), 256-byte aligned.
  * ---------------------------------------------------------------------- */

@@ -236,33 +236,54 @@ static int check_grads(const char *fn, int32_t n_tensors, const void *const *h_g
     return TMA_OK;
 }
 
-// Tensors that are written may not share memory (one given twice would be scaled twice, or in part).  Lists in the order of their addresses, as a flat buffer's parts are,
-// need no sorting.
-static int check_apart(const char *fn, int32_t n_tensors, const void *const *outs, const int64_t *h_sizes, size_t size)
+// What is written may share memory with nothing else that the call reads or writes, but a result with its own gradient, in place: results are written while other
+// blocks still read gradients (one given twice would be scaled twice, or in part).  Lists in the order of their addresses, as a flat buffer's parts are, and
+// apart from the others' need no sorting.
+struct Range {
+    uintptr_t from, to;
+    bool operator<(const Range &b) const { return from < b.from; }
+    bool meets(const Range &b) const { return from < b.to && b.from < to; }
+};
+static int check_apart(const char *fn, int32_t n_tensors, const void *const *h_grads, const void *const *h_outs, const int64_t *h_sizes, size_t size, const float *norm_out)
 {
-    struct Range {
-        uintptr_t from, to;
+    auto range = [&](const void *const *list, int i) {
+        return Range{reinterpret_cast<uintptr_t>(list[i]), reinterpret_cast<uintptr_t>(list[i]) + uintptr_t(h_sizes[i]) * size};
     };
-    auto range = [&](int i) { return Range{reinterpret_cast<uintptr_t>(outs[i]), reinterpret_cast<uintptr_t>(outs[i]) + uintptr_t(h_sizes[i]) * size}; };
-    uintptr_t end = 0;
-    bool ordered = true;
-    for (int i = 0; i < n_tensors && ordered; ++i) {
+    const void *const *outs = h_outs ? h_outs : h_grads;
+    const Range norm{reinterpret_cast<uintptr_t>(norm_out), reinterpret_cast<uintptr_t>(norm_out) + sizeof(float)};
+    Range written{UINTPTR_MAX, 0}, read{UINTPTR_MAX, 0};      // by results that are not in place, as gradients
+    uintptr_t end = 0, g_end = 0;
+    bool ordered = true, on_norm = false;
+    for (int i = 0; i < n_tensors; ++i) {
         if (h_sizes[i] == 0) continue;
-        const Range r = range(i);
-        ordered = r.from >= end;
+        const Range r = range(outs, i), g = range(h_grads, i);
+        ordered = ordered && r.from >= end && g.from >= g_end;
         end = r.to;
+        g_end = g.to;
+        on_norm = on_norm || r.meets(norm) || g.meets(norm);
+        read = {std::min(read.from, g.from), std::max(read.to, g.to)};
+        if (r.from != g.from) written = {std::min(written.from, r.from), std::max(written.to, r.to)};
     }
-    if (ordered) return TMA_OK;
+    TMA_REQUIRE(!on_norm, TMA_ERR_INVALID_ARG, "%s: norm_out overlaps a gradient or a result", fn);
+    if (ordered && !(written.from < written.to && written.meets(read))) return TMA_OK;
     Range few[256], *all = n_tensors <= 256 ? few : static_cast<Range *>(malloc(size_t(n_tensors) * sizeof(Range)));
     TMA_REQUIRE(all, TMA_ERR_INVALID_ARG, "%s: no host memory for %d tensors", fn, n_tensors);
     int count = 0;
     for (int i = 0; i < n_tensors; ++i)
-        if (h_sizes[i]) all[count++] = range(i);
-    std::sort(all, all + count, [](const Range &a, const Range &b) { return a.from < b.from; });
-    bool apart = true;
+        if (h_sizes[i]) all[count++] = range(outs, i);
+    std::sort(all, all + count);
+    bool apart = true, clear = true;
     for (int i = 1; i < count; ++i) apart = apart && all[i].from >= all[i - 1].to;
+    // results that are apart: of those that meet a gradient the first is its own, which then is the only one, or an overlap
+    for (int i = 0; apart && clear && i < n_tensors; ++i) {
+        if (h_sizes[i] == 0) continue;
+        const Range g = range(h_grads, i);
+        const Range *first = std::lower_bound(all, all + count, g.from, [](const Range &r, uintptr_t at) { return r.to <= at; });
+        clear = first == all + count || !first->meets(g) || (outs[i] == h_grads[i] && first->from == g.from);
+    }
     if (all != few) free(all);
     TMA_REQUIRE(apart, TMA_ERR_INVALID_ARG, "%s: two of the results overlap", fn);
+    TMA_REQUIRE(clear, TMA_ERR_INVALID_ARG, "%s: a result overlaps a gradient that is not its own, or its own at another place", fn);
     return TMA_OK;
 }
 
@@ -293,7 +314,7 @@ extern "C" int tma_grad_clip(int32_t n_tensors, const void *const *h_grads, void
     const char *fn = "tma_grad_clip";
     if (int rc = check_grads(fn, n_tensors, h_grads, h_outs, h_sizes, dtype, norm_out, ws, ws_bytes)) return rc;
     TMA_REQUIRE(max_norm >= 0.0, TMA_ERR_INVALID_ARG, "%s: max_norm below 0, or NaN", fn);
-    if (int rc = check_apart(fn, n_tensors, h_outs ? const_cast<const void *const *>(h_outs) : h_grads, h_sizes, dtype == TMA_BF16 ? 2 : 4)) return rc;
+    if (int rc = check_apart(fn, n_tensors, h_grads, h_outs, h_sizes, dtype == TMA_BF16 ? 2 : 4, norm_out)) return rc;
     hipStream_t s = as_stream(stream);
     double *partial = static_cast<double *>(ws);
     return dtype == TMA_BF16 ? grad_norm<uint16_t>(fn, n_tensors, h_grads, h_outs, h_sizes, true, max_norm, norm_out, partial, ws_bytes, s)
