@@ -3,7 +3,8 @@
 //
 // Packed operands.  A unit is 1 KB: 32 rows of an operand by 16 k-values, 16 bytes a lane, in the order in which the matrix instruction wants them; what lies
 // outside the operand is zero.  Eight units of 256 rows follow each other, then those of the next k-values, of the next rows (a slab of a tile is one run of
-// memory; units of rows past the last are never written, and reach only results that are not stored), then planes: fp32 values are taken apart into bf16 parts whose sum
+// memory; the last rows' groups have the units that there are, so that a narrow layer's gradients, whose rows are its columns, take no more than they are; a
+// tile past them has the last one again, for results that are not stored), then planes: fp32 values are taken apart into bf16 parts whose sum
 // they are (three of them hold all 24 bits, two hold 17), one plane a part, and a product of such operands is the sum of products of planes, the small ones
 // first: a weight gradient in fp32 from bf16 rows is a product of twice the length; fp32 operands have a kernel of their own (wide_split.hpp).
 //
@@ -30,8 +31,10 @@ constexpr int kWideDies = 8;
 struct Packed {
     char *at;
     int rbs, kgs;              // units along the rows and along k (an even number: a slab is two)
-    __host__ __device__ __forceinline__ int64_t plane() const { return int64_t((rbs + 7) / 8) * kgs * (8 * kUnitBytes); }
-    __host__ __device__ __forceinline__ int64_t unit(int64_t rb, int64_t kg) const { return ((rb / 8 * kgs + kg) * 8 + rb % 8) * kUnitBytes; }
+    __host__ __device__ __forceinline__ int64_t plane() const { return int64_t(rbs) * kgs * kUnitBytes; }
+    // units of the group of eight, or of the last ones, that rb is in
+    __host__ __device__ __forceinline__ int group(int rb) const { return rbs - (rb & ~7) < 8 ? rbs - (rb & ~7) : 8; }
+    __host__ __device__ __forceinline__ int64_t unit(int rb, int64_t kg) const { return (int64_t(rb & ~7) * kgs + kg * group(rb) + (rb & 7)) * kUnitBytes; }
     __host__ size_t bytes(int parts) const { return size_t(plane()) * size_t(parts); }
 };
 inline Packed packed_shape(int64_t rows, int64_t k)
@@ -170,7 +173,8 @@ __device__ __forceinline__ void pack_rows(const RowsPack &q, int block, int bloc
     const int64_t all = int64_t(q.out.rbs) * quads;
     const int slot = (piece / 2) * 64 + (q.weights ? weights_place(fragment_row(r), piece % 2, piece / 2) : rows_place(r, piece % 2));
     for (int64_t i = block; i < all; i += blocks) {
-        const int64_t rb = i / quads, row = rb * kUnitRows + r;
+        const int rb = int(i / quads);
+        const int64_t row = int64_t(rb) * kUnitRows + r;
         const int kg0 = int(i % quads) * 4, kg = kg0 + piece / 2;
         const int side = kg < q.side_kgs ? 0 : 1;
         const int64_t c = int64_t(kg - side * q.side_kgs) * kUnitK + piece % 2 * 8;
@@ -234,7 +238,7 @@ __device__ __forceinline__ void pack_cols_as(const ColsPack &q, int block, int b
         const int strip = int(i % strips), side = int(i / strips % q.sides);
         const int64_t kg = i / strips / q.sides;
         const int64_t col = int64_t(strip) * kWidth + c_in, k0 = kg * kUnitK + half * 8;
-        const int64_t rb = col / kUnitRows;
+        const int rb = int(col / kUnitRows);
         if (rb >= side_rbs) continue;
         const T *src = static_cast<const T *>(q.src[side]) + col;
         float v[kTogether][8];
@@ -467,11 +471,12 @@ __global__ __launch_bounds__(WM *WN * 64, kStages * (MF + NF) >= 64 ? 1 : 2) voi
     const int in_side = rows_side ? u0 : u0 - 2 * MF, k_unit = in_side / (rows_side ? MF : NF), rb_in = in_side % (rows_side ? MF : NF);
     int64_t c_work = work;
     int c_at = 0, c_slabs = 1, c_last = INT32_MAX, c_pair = -1, c_stage = kStages - 1;
-    int c_first = 0;      // kTurned: the range's first slab
-    // Load v of a lane, from the slab's base on.  kLying: row min(row_in + 16 v, most), this lane's piece of it; kTurned: unit min(v, most), 8 KB apart.  (Of the
-    // other operand: its units of 1 KB.)
+    int c_first = 0, c_kg = 0;      // kTurned: the range's first slab, this wavefront's first unit along k
+    uint32_t c_apart = 0;           // else: bytes from slab to slab
+    // Load v of a lane, from the slab's base on.  kLying: row min(row_in + 16 v, most), this lane's piece of it (of the other operand: 64 bytes of a unit's 1 KB);
+    // else unit min(v, most), of 1 KB, or, kTurned, as far apart as its group has units.
     const bool lying = kRows == kLying && rows_side, turned = kRows == kTurned && rows_side;
-    const uint32_t pitch = lying ? uint32_t(q.lda * 2) : kRows == kLying ? 64u : turned ? uint32_t(8 * kUnitBytes) : uint32_t(kUnitBytes);
+    uint32_t pitch = lying ? uint32_t(q.lda * 2) : kRows == kLying ? 64u : uint32_t(kUnitBytes);
     const uint32_t piece_at = kRows != kLying ? uint32_t(lane) * 16u : uint32_t(lying ? (lane & 3) ^ (lane >> 4) : lane & 3) * 16u;
     const int row_in = lane / 4 + (lying ? u0 * 16 : 0);
     int most = INT32_MAX;
@@ -498,29 +503,37 @@ __global__ __launch_bounds__(WM *WN * 64, kStages * (MF + NF) >= 64 ? 1 : 2) voi
             const int64_t row0 = int64_t(tile.m) * (MF * 32), left = q.rows - 1 - row0;
             most = left < MF * 32 ? int(left) : MF * 32;
             from = q.a.at + row0 * q.lda * 2 + int64_t(tile.split) * q.split_slabs * 64;
+            c_apart = 64;
         } else if (turned) {
             const int kg = tile.m * (MF * 2) + u0, left = q.a.kgs - 1 - kg;
             most = left > 0 ? left : 0;
-            from = q.a.at + int64_t(left < 0 ? q.a.kgs - 1 : kg) * (8 * kUnitBytes);
+            from = q.a.at;
+            c_kg = left < 0 ? q.a.kgs - 1 : kg;
             c_first = tile.split * q.split_slabs;
         } else {
             const Packed &o = rows_side ? q.a : q.b;
-            from = o.at + (((rows_side ? q.planes.a : q.planes.b) >> pair) & 15u) * o.plane() + o.unit(rb, int64_t(tile.split) * q.split_slabs * 2 + k_unit);
+            const int left = o.rbs - 1 - rb, there = left < 0 ? o.rbs - 1 : rb;
+            most = left > 0 ? left : 0;
+            if (kRows == kLying) most = most * 16 + 15;
+            from = o.at + (((rows_side ? q.planes.a : q.planes.b) >> pair) & 15u) * o.plane() + o.unit(there, int64_t(tile.split) * q.split_slabs * 2 + k_unit);
+            c_apart = uint32_t(o.group(there)) * uint32_t(2 * kUnitBytes);
         }
     };
     const char *base = nullptr;      // `from` in scalar registers
     auto fetch = [&](int v) {
         const int row = row_in + v * 16;
-        const uint32_t at = kRows == kLying    ? uint32_t(row < most ? row : most) * pitch + piece_at
-                            : kRows == kTurned ? uint32_t(v < most ? v : most) * pitch + piece_at
-                                               : uint32_t(v * kUnitBytes + lane * 16);
-        fetch_unit(to + uint32_t(v) * uint32_t(kUnitBytes), base, at);
+        const uint32_t place = to + uint32_t(v) * uint32_t(kUnitBytes), unit_at = uint32_t(v < most ? v : most) * pitch;
+        if constexpr (kRows == kLying) fetch_unit(place, base, uint32_t(row < most ? row : most) * pitch + piece_at);
+        else fetch_unit(place, base + unit_at, piece_at);
     };
     auto next_slab = [&]() {
         step();
         const uint32_t slab = uint32_t((c_at < c_last ? c_at : c_last) + (kRows == kTurned ? c_first : 0));
-        const uint64_t step_bytes = turned ? uint64_t(slab >> 3) * (uint64_t(uint32_t(q.a.kgs)) * (8 * kUnitBytes)) + (slab & 7) * uint32_t(kUnitBytes)
-                                           : uint64_t(slab) * (lying ? 64u : uint32_t(16 * kUnitBytes));
+        uint64_t step_bytes = uint64_t(slab) * c_apart;
+        if (turned) {      // the slab is a unit along the gradients' columns
+            pitch = uint32_t(q.a.group(int(slab))) * uint32_t(kUnitBytes);
+            step_bytes = uint64_t(q.a.unit(int(slab), c_kg));
+        }
         const uint64_t at = reinterpret_cast<uint64_t>(from) + step_bytes;
         base = reinterpret_cast<const char *>(uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(int(at >> 32)))) << 32 | uint32_t(__builtin_amdgcn_readfirstlane(int(at))));
     };

@@ -424,7 +424,8 @@ __device__ __forceinline__ void grad_pack(const GradCall<T> &q, int block, GradT
                 for (int j = 0; j < 8; ++j) v[j] = tile[side][quarter * 8 + j][col_in];
                 uint4 parts[kParts];
                 pack_eight<kParts>(v, parts);
-                const int64_t rb = side * (padded / kUnitRows) + (c0 + col_in) / kUnitRows, kg = i * 2 + quarter / 2;
+                const int rb = side * (padded / kUnitRows) + (c0 + col_in) / kUnitRows;
+                const int64_t kg = i * 2 + quarter / 2;
                 const int slot = weights_place(fragment_row(col_in % 32), quarter % 2, quarter / 2);
 #pragma unroll
                 for (int p = 0; p < kParts; ++p)

@@ -31,28 +31,34 @@ __global__ __launch_bounds__(256, Epi::kPast ? 2 : 3) void wide_split_kernel(Wid
     const int half = wave & 1;
     const Packed &o = rows_side ? q.a : q.b;
     // turned: 16 of a unit's rows are a slab's k-values, 512 bytes, and a load takes those of two units, 32 rows of the result; units past the last are the last again
-    const int kg = tile.m * (2 * F), pairs = (o.kgs - kg) / 2;
-    const char *first = turned ? o.at + int64_t(kg) * (8 * kUnitBytes) : o.at + o.unit((rows_side ? tile.m : tile.n) * F, int64_t(tile.split) * q.split_slabs * 2);
+    const int kg = tile.m * (2 * F), rb = (rows_side ? tile.m : tile.n) * F, units_left = turned ? (o.kgs - kg) / 2 : o.rbs - rb;
+    const char *first = turned ? o.at : o.at + o.unit(rb, int64_t(tile.split) * q.split_slabs * 2);
+    const uint32_t apart = turned ? 0u : uint32_t(o.group(rb)) * uint32_t(kUnitBytes);
     const char *from[3] = {first + half * o.plane(), first + half * 2 * o.plane(), first + (1 + half) * o.plane()};
     const int unit[3] = {half * 2, half ? 0 : 2, half * 2};
     const uint32_t ring0 = lds_address(&ring[0]) + uint32_t(wave * kLoads * kUnitBytes);
-    const uint32_t lane_at = turned ? uint32_t((lane >> 5) * (8 * kUnitBytes) + (lane & 31) * 16) : uint32_t(lane * 16);
+    const uint32_t lane_at = uint32_t((turned ? lane & 31 : lane) * 16), second = turned ? uint32_t(lane >> 5) : 0u;      // of a pair of units
     const int turned_from = turned ? tile.split * q.split_slabs * 2 : 0;
     auto fetch = [&](int at_step) {
         const uint32_t to = ring0 + uint32_t(at_step % kStages * kStageBytes);
         const int step = turned_from + at_step;
-        const uint64_t along = turned ? uint64_t(uint32_t(step >> 4)) * (uint64_t(uint32_t(o.kgs)) * (8 * kUnitBytes)) + uint32_t(step >> 1 & 7) * uint32_t(kUnitBytes) +
-                                            uint32_t(step & 1) * 512u
-                                      : uint64_t(uint32_t(step)) * (8 * kUnitBytes);
+        const uint64_t along = turned ? uint64_t(o.unit(step >> 1, kg)) + uint32_t(step & 1) * 512u : uint64_t(uint32_t(step)) * apart;
+        const uint32_t group = turned ? uint32_t(o.group(step >> 1)) * uint32_t(kUnitBytes) : 0u;      // from unit to unit along the result's rows
+        const uint32_t lane_from = lane_at + second * group;
+        auto scalar = [](uint64_t at) {
+            return reinterpret_cast<const char *>(uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(int(at >> 32)))) << 32 | uint32_t(__builtin_amdgcn_readfirstlane(int(at))));
+        };
 #pragma unroll
         for (int p = 0; p < 3; ++p) {
             const uint64_t at = reinterpret_cast<uint64_t>(from[p]) + along;
-            const char *base = reinterpret_cast<const char *>(uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(int(at >> 32)))) << 32 |
-                                                              uint32_t(__builtin_amdgcn_readfirstlane(int(at))));
+            const char *base = scalar(at);
 #pragma unroll
             for (int v = 0; v < 2; ++v) {
-                const int u = unit[p] + v;
-                fetch_unit(to + uint32_t((2 * p + v) * kUnitBytes), base, lane_at + uint32_t(turned ? (u < pairs ? u : pairs - 1) * (16 * kUnitBytes) : u * kUnitBytes));
+                const int u = unit[p] + v < units_left ? unit[p] + v : units_left - 1;
+                const uint32_t place = to + uint32_t((2 * p + v) * kUnitBytes);
+                // (turned: units' distances change on the way, and registers are short)
+                if constexpr (kTurnedRows) fetch_unit(place, scalar(at + uint32_t(u) * (turned ? 2 * group : uint32_t(kUnitBytes))), lane_from);
+                else fetch_unit(place, base, lane_at + uint32_t(u) * uint32_t(kUnitBytes));
             }
         }
     };
