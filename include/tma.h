@@ -754,9 +754,12 @@ int tma_dropout_bwd(int64_t n, int32_t F, const void *dY, int64_t ldy, double p,
  * results that it reaches non-finite (NaN where fp32 arithmetic may give an
  * infinity).  The ReLU of a NaN is 0 and closed.  Widths up to 65536.  What lies in a row's padding has no
  * influence and is left as it is.
- * Workspaces, 256-byte aligned: the *_workspace_bytes queries (0 forward of small weights and up to 64 rows: ws may then be NULL).
+ * Workspaces, 256-byte aligned: the *_workspace_bytes queries (0 forward of small weights and up to 64 rows: ws may then be NULL).  Forward,
+ * *_workspace_bytes_at16 is what calls need whose rows of X begin at 16 bytes, 2^22 elements apart at most: bf16 rows of a multiple
+ * of 32 elements are then read where they lie, up to 4096 columns (of gated layers 2048), and take no room.
  * ---------------------------------------------------------------------- */
 size_t tma_gated_dense_fwd_workspace_bytes(int64_t n, int32_t F_in, int32_t F_out, int32_t dtype);
+size_t tma_gated_dense_fwd_workspace_bytes_at16(int64_t n, int32_t F_in, int32_t F_out, int32_t dtype);
 
 int tma_gated_dense_fwd(int64_t n, const void *X, int64_t ldx, int32_t F_in, const float *W_gate, const float *W_up,
                         const float *b_gate, const float *b_up, int32_t F_out, int32_t act, int32_t dtype, void *G_out, void *U_out,
@@ -770,6 +773,7 @@ int tma_gated_dense_bwd(int64_t n, const void *X, int64_t ldx, const void *G, co
                         const void *R, int64_t ldr, void *ws, size_t ws_bytes, tma_stream_t stream);
 
 size_t tma_dense_residual_fwd_workspace_bytes(int64_t n, int32_t F_in, int32_t F_out, int32_t dtype);
+size_t tma_dense_residual_fwd_workspace_bytes_at16(int64_t n, int32_t F_in, int32_t F_out, int32_t dtype);
 
 int tma_dense_residual_fwd(int64_t n, const void *X, int64_t ldx, int32_t F_in, const float *W, const float *bias, int32_t F_out,
                            int32_t act, int32_t dtype, const void *R, int64_t ldr, void *Z_out, int64_t ldz, void *Y_out, int64_t ldy,

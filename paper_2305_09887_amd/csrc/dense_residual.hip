@@ -40,9 +40,12 @@ static int residual_bwd(const char *fn, int64_t n, const void *X, int64_t ldx, c
 
 extern "C" size_t tma_dense_residual_fwd_workspace_bytes(int64_t n, int32_t F_in, int32_t F_out, int32_t dtype)
 {
-    using namespace tma;
-    if (!wide_sizes_ok(n, F_in, F_out)) return 0;
-    return (dtype == TMA_BF16 ? plan_forward<uint16_t>(n, F_in, F_out, 1, true, nullptr) : plan_forward<float>(n, F_in, F_out, 1, true, nullptr)).bytes;
+    return tma::forward_workspace(n, F_in, F_out, 1, dtype, false);
+}
+
+extern "C" size_t tma_dense_residual_fwd_workspace_bytes_at16(int64_t n, int32_t F_in, int32_t F_out, int32_t dtype)
+{
+    return tma::forward_workspace(n, F_in, F_out, 1, dtype, true);
 }
 
 extern "C" int tma_dense_residual_fwd(int64_t n, const void *X, int64_t ldx, int32_t F_in, const float *W, const float *bias, int32_t F_out, int32_t act, int32_t dtype,
@@ -50,7 +53,7 @@ extern "C" int tma_dense_residual_fwd(int64_t n, const void *X, int64_t ldx, int
 {
     using namespace tma;
     const char *fn = "tma_dense_residual_fwd";
-    if (int rc = check_wide(fn, n, F_in, F_out, act, dtype, ws, ws_bytes, tma_dense_residual_fwd_workspace_bytes(n, F_in, F_out, dtype))) return rc;
+    if (int rc = check_wide(fn, n, F_in, F_out, act, dtype, ws, ws_bytes, forward_workspace(n, F_in, F_out, 1, dtype, rows_at16(X, ldx)))) return rc;
     if (n == 0) return TMA_OK;
     TMA_REQUIRE(X && W && Y_out, TMA_ERR_INVALID_ARG, "%s: NULL argument", fn);
     TMA_REQUIRE(Y_out != X && Z_out != X && Z_out != Y_out && (!Z_out || Z_out != R), TMA_ERR_INVALID_ARG, "%s: Z_out is one of X, R, Y_out, or Y_out is X", fn);

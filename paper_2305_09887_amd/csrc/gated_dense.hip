@@ -43,9 +43,12 @@ static int gated_bwd(const char *fn, int64_t n, const void *X, int64_t ldx, cons
 
 extern "C" size_t tma_gated_dense_fwd_workspace_bytes(int64_t n, int32_t F_in, int32_t F_out, int32_t dtype)
 {
-    using namespace tma;
-    if (!wide_sizes_ok(n, F_in, F_out)) return 0;
-    return (dtype == TMA_BF16 ? plan_forward<uint16_t>(n, F_in, F_out, 2, false, nullptr) : plan_forward<float>(n, F_in, F_out, 2, false, nullptr)).bytes;
+    return tma::forward_workspace(n, F_in, F_out, 2, dtype, false);
+}
+
+extern "C" size_t tma_gated_dense_fwd_workspace_bytes_at16(int64_t n, int32_t F_in, int32_t F_out, int32_t dtype)
+{
+    return tma::forward_workspace(n, F_in, F_out, 2, dtype, true);
 }
 
 extern "C" int tma_gated_dense_fwd(int64_t n, const void *X, int64_t ldx, int32_t F_in, const float *W_gate, const float *W_up, const float *b_gate, const float *b_up,
@@ -54,7 +57,7 @@ extern "C" int tma_gated_dense_fwd(int64_t n, const void *X, int64_t ldx, int32_
 {
     using namespace tma;
     const char *fn = "tma_gated_dense_fwd";
-    if (int rc = check_wide(fn, n, F_in, F_out, act, dtype, ws, ws_bytes, tma_gated_dense_fwd_workspace_bytes(n, F_in, F_out, dtype))) return rc;
+    if (int rc = check_wide(fn, n, F_in, F_out, act, dtype, ws, ws_bytes, forward_workspace(n, F_in, F_out, 2, dtype, rows_at16(X, ldx)))) return rc;
     TMA_REQUIRE(!G_out == !U_out, TMA_ERR_INVALID_ARG, "%s: G_out and U_out go together", fn);
     if (n == 0) return TMA_OK;
     TMA_REQUIRE(X && W_gate && W_up && H_out, TMA_ERR_INVALID_ARG, "%s: NULL argument", fn);

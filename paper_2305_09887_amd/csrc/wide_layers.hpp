@@ -655,19 +655,21 @@ struct Cutter {
     void take(Packed &p, int parts) { p.at = static_cast<char *>(take(p.bytes(parts))); }
 };
 
-// forward: rows and weights laid out
+// forward: weights laid out, and rows; lying: bytes of all but the rows, the last, where a call reads those where they lie
 struct ForwardPlan {
     Packed a, b;
     WidePlan rows;
     float *shares;
-    size_t bytes;
+    size_t lying, bytes;
 };
 // Rows that a product takes where they lie (see WideCall).  (A tile's rows are within 32 bits of each other.)  That takes their pass off and a tenth more time, for
 // half lines of memory: 1,000,003 rows 256 -> 256 690 -> 500 us, 8,192 rows 8192 -> 2048 290 -> 280, 2048 -> 2 x 8192 530 -> 565.
 template <typename T>
+inline bool direct_sizes(int32_t F_in, int n_units) { return sizeof(T) == 2 && F_in % 32 == 0 && n_units <= 128; }
+template <typename T>
 inline bool direct_rows(const T *X, int64_t ldx, int32_t F_in, int n_units)
 {
-    return sizeof(T) == 2 && whole_rows(X, ldx) && F_in % 32 == 0 && ldx <= (1 << 22) && n_units <= 128;
+    return direct_sizes<T>(F_in, n_units) && whole_rows(X, ldx) && ldx <= (1 << 22);
 }
 
 // the product of weights, laid out here, and of rows, laid out where they have to be
@@ -703,17 +705,18 @@ inline ForwardPlan plan_forward(int64_t n, int32_t F_in, int32_t F_out, int side
 {
     ForwardPlan p{};
     if (n <= kFewMost) {      // nothing is laid out
-        p.bytes = round_up(plan_few(n, F_in, F_out, sides, sizeof(T)).bytes, 256);
+        p.bytes = p.lying = round_up(plan_few(n, F_in, F_out, sides, sizeof(T)).bytes, 256);
         return p;
     }
     p.a = packed_shape(n, F_in);
     p.b = packed_shape(F_out, F_in);
     p.b.rbs *= sides;
     Cutter cut{static_cast<char *>(ws)};
-    cut.take(p.a, kPartsOf<T>);
     cut.take(p.b, kPartsOf<T>);
     p.rows = plan_rows(n, p.b, reads, sizeof(T) == 4);
     p.shares = static_cast<float *>(cut.take(row_shares(p.rows, n, p.b)));
+    p.lying = cut.used;
+    cut.take(p.a, kPartsOf<T>);
     p.bytes = cut.used;
     return p;
 }
@@ -811,6 +814,19 @@ static int wide_backward(const char *fn, const char *what, int64_t n, const T *X
 
 // every number of a call that asks for a workspace, too
 inline bool wide_sizes_ok(int64_t n, int32_t F_in, int32_t F_out) { return n >= 0 && n <= INT32_MAX && F_in >= 1 && F_out >= 1 && F_in <= (1 << 16) && F_out <= (1 << 16); }
+// of a forward call; at16: of one whose rows begin at 16 bytes, 2^22 elements apart at most
+template <typename T>
+inline size_t forward_bytes(int64_t n, int32_t F_in, int32_t F_out, int sides, bool at16)
+{
+    const ForwardPlan p = plan_forward<T>(n, F_in, F_out, sides, true, nullptr);
+    return at16 && direct_sizes<T>(F_in, p.b.rbs) ? p.lying : p.bytes;
+}
+inline size_t forward_workspace(int64_t n, int32_t F_in, int32_t F_out, int sides, int32_t dtype, bool at16)
+{
+    if (!wide_sizes_ok(n, F_in, F_out)) return 0;
+    return dtype == TMA_BF16 ? forward_bytes<uint16_t>(n, F_in, F_out, sides, at16) : forward_bytes<float>(n, F_in, F_out, sides, at16);
+}
+inline bool rows_at16(const void *X, int64_t ldx) { return whole_rows(static_cast<const uint16_t *>(X), ldx) && ldx <= (1 << 22); }      // (of bf16: fp32 rows are laid out)
 inline bool wide_act_ok(int32_t act) { return act == TMA_ACT_NONE || act == TMA_ACT_RELU || act == TMA_ACT_SILU || act == TMA_ACT_GELU; }
 inline int check_wide(const char *fn, int64_t n, int32_t F_in, int32_t F_out, int32_t act, int32_t dtype, const void *ws, size_t ws_bytes, size_t need)
 {
