@@ -11,7 +11,9 @@ namespace tma {
 // silu z = z s(z), s = 1 / (1 + e^-z); gelu z = z Phi(z), Phi(-|z|) = erfc(|z| / sqrt 2) / 2.
 __device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
 // Phi(z), from e = e^(-z^2 / 2).  erfc(x) = e^(-x^2) t Q(t), t = 1 / (1 + x / 2): Q of degree 8 is a fit of erfcx(x) / t over 0 <= x <= 12 by weighted least
-// squares, relative error 4.4e-8; in fp32 3.4e-7 at most and 8e-8 in the mean over 0 <= x <= 9, in the tail too.  (The library's erfc takes some five times
+// squares, relative error 4.4e-8; in fp32 3.4e-7 at most and 8e-8 in the mean over 0 <= x <= 9.  What callers pass for e is e^(-z^2 / 2) (1 + d), |d| up to
+// 2^-24 z^2: the exponent is rounded when it is squared and when it is multiplied by log2 e.  So the tail is off by 1.9e-6 of itself at z = -6 and 7e-6 at -12.5
+// (SiLU's by 4e-6 at -87), Phi by 1.6e-7 at most, absolute; an exponent in two parts would take six instructions more.  (The library's erfc takes some five times
 // the instructions: 8,192 rows 2048 -> 8192 gated 577 us, with silu 483.)
 __device__ __forceinline__ float normal_below(float z, float e)
 {
