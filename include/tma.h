@@ -794,7 +794,7 @@ int tma_dense_residual_bwd(int64_t n, const void *X, int64_t ldx, const void *Z,
  * of their lengths (0 is allowed); read before the call returns.  Tensors are dense, of
  * dtype, aligned to it, and do not overlap; h_outs NULL: in place (nothing is
  * written where c = 1); h_outs[i] may be h_grads[i].  norm_out [1] fp32
- * (device).  Squares and their sum are fp64, each result is rounded once.  A
+ * (device).  Squares, their sum, c and products are fp64, each result is rounded once (to bf16 by way of fp32).  A
  * norm of NaN makes all results NaN, an infinite one finite gradients 0 and
  * infinite ones NaN.  max_norm >= 0.  At most 131072 tensors.  Refused: results that
  * overlap each other, or a gradient that is not h_outs[i]'s own h_grads[i]; norm_out of a clipping within a gradient or result.

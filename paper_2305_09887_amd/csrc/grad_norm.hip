@@ -106,17 +106,24 @@ __global__ __launch_bounds__(kNormThreads) void grad_norm_kernel(const double *p
     if (threadIdx.x == 0) *norm_out = float(norm);
 }
 
+// In 64 bits: the factor of gradients that exploded, or of a tiny bound, is no normal fp32 number, while its products are.
+__device__ __forceinline__ float scaled(float g, double c)
+{
+    float v = float(double(g) * c);
+    asm("" : "+v"(v));      // (of a single value the compiler would round 64 bits to bf16 at once, of a pair it does not: one value, two results)
+    return v;
+}
 template <typename T>
-__device__ __forceinline__ void scale_piece(const uint4 &piece, T *out, float c)
+__device__ __forceinline__ void scale_piece(const uint4 &piece, T *out, double c)
 {
     float v[16 / sizeof(T)];
     Chunk<T>::widen(piece, v);
 #pragma unroll
-    for (size_t j = 0; j < 16 / sizeof(T); ++j) v[j] *= c;
+    for (size_t j = 0; j < 16 / sizeof(T); ++j) v[j] = scaled(v[j], c);
     Chunk<T>::store(out, v);
 }
-__device__ __forceinline__ void scale_one(const float *in, float *out, float c) { *out = *in * c; }
-__device__ __forceinline__ void scale_one(const uint16_t *in, uint16_t *out, float c) { *out = f32_to_bf16(bf16_to_f32(*in) * c); }
+__device__ __forceinline__ void scale_one(const float *in, float *out, double c) { *out = scaled(*in, c); }
+__device__ __forceinline__ void scale_one(const uint16_t *in, uint16_t *out, double c) { *out = f32_to_bf16(scaled(bf16_to_f32(*in), c)); }
 
 // first: this launch writes norm_out.  Where the factor is 1 nothing is written in place.
 template <typename T>
@@ -127,7 +134,7 @@ __global__ __launch_bounds__(kNormThreads) void grad_scale_kernel(GradTensors q,
     const double norm = norm_of(partial, count);
     if (first && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = float(norm);
     // (a norm that is NaN makes every gradient NaN)
-    const float factor = norm <= max_norm ? 1.0f : float(max_norm / norm);
+    const double factor = norm <= max_norm ? 1.0 : max_norm / norm;
     const int t = threadIdx.x;
     for (int b = blockIdx.x; b < q.chunks; b += gridDim.x) {
         const int c = q.chunks - 1 - b;
@@ -135,7 +142,7 @@ __global__ __launch_bounds__(kNormThreads) void grad_scale_kernel(GradTensors q,
         const int64_t at = int64_t(c - q.first[i]) * kChunk<T>, left = q.size[i] - at, n = left < kChunk<T> ? left : kChunk<T>;
         const T *in = static_cast<const T *>(q.in[i]) + at;
         T *out = static_cast<T *>(o.out[i]) + at;
-        if (in == out && factor == 1.0f) continue;
+        if (in == out && factor == 1.0) continue;
         int64_t head = 0, pieces = 0;
         if (((reinterpret_cast<intptr_t>(in) ^ reinterpret_cast<intptr_t>(out)) & 15) == 0) {
             head = (-reinterpret_cast<intptr_t>(in) & 15) / int64_t(sizeof(T));
