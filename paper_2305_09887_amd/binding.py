@@ -1350,7 +1350,15 @@ def _lists():
     path = os.path.join(_PKG, "libtma_lists.so")
     if not os.path.exists(path):
         raise TmaError(f"{path} not found: build it with `python -m paper_2305_09887_amd.build`")
-    call = C.PyDLL(path).tma_read_tensors
+    try:
+        so = C.PyDLL(path)
+        so.tma_lists_torch.restype = C.c_char_p
+        built = so.tma_lists_torch().decode()
+        call = so.tma_read_tensors
+    except (OSError, AttributeError) as e:
+        raise TmaError(f"{path}: {e}: build it with `python -m paper_2305_09887_amd.build`") from None
+    if built != torch.__version__:
+        raise TmaError(f"{path} was built with torch {built}, this is {torch.__version__}: build it with `python -m paper_2305_09887_amd.build`")
     call.argtypes = [C.py_object, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]
     return call
 

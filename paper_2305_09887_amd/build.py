@@ -34,6 +34,7 @@ def build_lists() -> str:
     import torch
     include = os.path.join(os.path.dirname(torch.__file__), "include")
     subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                           f'-DTMA_TORCH="{torch.__version__}"',
                            "-isystem", include, "-isystem", os.path.join(include, "torch", "csrc", "api", "include"),
                            "-isystem", sysconfig.get_paths()["include"], "-Wall", os.path.join(CSRC, "tensor_list.cpp"), "-o", LISTS,
                            "-L", os.path.join(os.path.dirname(torch.__file__), "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"])
@@ -46,8 +47,8 @@ def build(verbose: bool = True) -> str:
     with cf.ThreadPoolExecutor(max_workers=min(8, len(srcs))) as ex:
         lists = ex.submit(build_lists)
         objs = list(ex.map(_compile, srcs))
-        lists.result()
     subprocess.check_call([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs])
+    lists.result()       # (the kernels' library does not need it)
     if verbose:
         print(f"built {LIB} from {len(srcs)} sources", file=sys.stderr)
     return LIB

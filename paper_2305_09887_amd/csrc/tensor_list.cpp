@@ -6,6 +6,9 @@
 
 #include <cstdint>
 
+// the torch whose classes this was compiled for
+extern "C" const char *tma_lists_torch() { return TMA_TORCH; }
+
 enum { kRead = 0, kNoTensor = 1, kOtherType = 2, kOtherDevice = 3, kNotDense = 4, kOtherLength = 5 };
 
 // Addresses and lengths of `n` tensors, a list or a tuple: dense, of fp32 or bf16 (dtype 0, 1), on device `device` (-1: the host's memory).  same: lengths are given, and
