@@ -40,7 +40,8 @@ class LocalTrainer:
 
     ``block_width`` = F > 0 (MLP encoder): a hidden layer whose output is as wide as its input becomes a residual block with a
     gated layer of width F, H' = H + (silu(H W_gate + b_gate) (.) (H W_up + b_up)) W_down + b_down; its parameters are these six
-    in the order W_gate, W_up, b_gate, b_up, W_down, b_down.  ``clip_norm`` = c > 0: before the optimizer the gradients, all of
+    in the order W_gate, W_up, b_gate, b_up, W_down, b_down; ``dropout`` drops a block's whole output, H' with what went past
+    the layer.  ``clip_norm`` = c > 0: before the optimizer the gradients, all of
     them together, are held to the norm c; ``grad_norm`` [1] is what their norm was.
     """
 
