@@ -436,7 +436,9 @@ __device__ __forceinline__ void write_out(const Epi &epi, const floatx16 (&acc)[
                     epi.past(row0 + (step + 1) / kGroups * 32, col0 + (step + 1) % kGroups * (Staged::kCols / S), lane, past[(step + 1) % 2]);
 #pragma unroll
                 for (int b = 0; b < kJ; ++b) staged.put(h, b, acc[j * kJ + b][i]);
+                __builtin_amdgcn_wave_barrier();      // lanes read what others wrote, and these write again: in the order of the program, which LDS keeps
                 epi.emit(staged, row0 + i * 32 + h * Staged::kRows, col0 + j * (Staged::kCols / S), split, cols[j], past[step % 2]);
+                __builtin_amdgcn_wave_barrier();
             }
 }
 

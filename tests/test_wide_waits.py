@@ -39,3 +39,14 @@ def test_products(assembly):  # noqa: F811
         assert by_hand >= 1, name
         seen += 1
     assert seen >= 6
+
+
+def test_every_exchange_is_marked(assembly):  # noqa: F811
+    """Lanes of a wavefront exchange results through LDS: the compiler is told so at each exchange, before the reads and before the next writes, and keeps the order that LDS
+    then keeps as well (a lane's own addresses alone would let it move the one past the other)."""
+    seen = 0
+    for name, lines in kernels(assembly):
+        marks = sum("wave barrier" in x for x in lines)
+        assert marks >= 4 and marks % 2 == 0, (name, marks)
+        seen += 1
+    assert seen >= 6
