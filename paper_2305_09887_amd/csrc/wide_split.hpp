@@ -33,18 +33,23 @@ __global__ __launch_bounds__(256, Epi::kPast ? 2 : 3) void wide_split_kernel(Wid
     // turned: 16 of a unit's rows are a slab's k-values, 512 bytes, and a load takes those of two units, 32 rows of the result; units past the last are the last again
     const int kg = tile.m * (2 * F), rb = (rows_side ? tile.m : tile.n) * F, units_left = turned ? (o.kgs - kg) / 2 : o.rbs - rb;
     const char *first = turned ? o.at : o.at + o.unit(rb, int64_t(tile.split) * q.split_slabs * 2);
-    const uint32_t apart = turned ? 0u : uint32_t(o.group(rb)) * uint32_t(kUnitBytes);
     const char *from[3] = {first + half * o.plane(), first + half * 2 * o.plane(), first + (1 + half) * o.plane()};
     const int unit[3] = {half * 2, half ? 0 : 2, half * 2};
     const uint32_t ring0 = lds_address(&ring[0]) + uint32_t(wave * kLoads * kUnitBytes);
-    const uint32_t lane_at = uint32_t((turned ? lane & 31 : lane) * 16), second = turned ? uint32_t(lane >> 5) : 0u;      // of a pair of units
-    const int turned_from = turned ? tile.split * q.split_slabs * 2 : 0;
+    const uint32_t lane_at = uint32_t((turned ? lane & 31 : lane) * 16);
+    // the slab that is fetched next: bytes from `from`, from slab to slab (turned: in a group), and from unit to unit along the result's rows (turned: as many as the group has)
+    int step = turned ? tile.split * q.split_slabs * 2 : 0;
+    uint64_t along = 0;
+    uint32_t apart = 512, group = kUnitBytes, lane_from = lane_at;
+    auto enter_group = [&]() {
+        along = uint64_t(o.unit(step >> 1, kg));
+        group = uint32_t(o.group(step >> 1)) * uint32_t(2 * kUnitBytes);
+        lane_from = lane_at + (lane >> 5) * (group / 2);      // (a pair of units)
+    };
+    if (turned) enter_group();
+    else apart = uint32_t(o.group(rb)) * uint32_t(kUnitBytes);
     auto fetch = [&](int at_step) {
         const uint32_t to = ring0 + uint32_t(at_step % kStages * kStageBytes);
-        const int step = turned_from + at_step;
-        const uint64_t along = turned ? uint64_t(o.unit(step >> 1, kg)) + uint32_t(step & 1) * 512u : uint64_t(uint32_t(step)) * apart;
-        const uint32_t group = turned ? uint32_t(o.group(step >> 1)) * uint32_t(kUnitBytes) : 0u;      // from unit to unit along the result's rows
-        const uint32_t lane_from = lane_at + second * group;
         auto scalar = [](uint64_t at) {
             return reinterpret_cast<const char *>(uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(int(at >> 32)))) << 32 | uint32_t(__builtin_amdgcn_readfirstlane(int(at))));
         };
@@ -56,12 +61,17 @@ __global__ __launch_bounds__(256, Epi::kPast ? 2 : 3) void wide_split_kernel(Wid
             for (int v = 0; v < 2; ++v) {
                 const int u = unit[p] + v < units_left ? unit[p] + v : units_left - 1;
                 const uint32_t place = to + uint32_t((2 * p + v) * kUnitBytes);
-                // (turned: units' distances change on the way, and registers are short)
-                if constexpr (kTurnedRows) fetch_unit(place, scalar(at + uint32_t(u) * (turned ? 2 * group : uint32_t(kUnitBytes))), lane_from);
+                // (turned: registers are short)
+                if constexpr (kTurnedRows) fetch_unit(place, scalar(at + uint32_t(u) * group), lane_from);
                 else fetch_unit(place, base, lane_at + uint32_t(u) * uint32_t(kUnitBytes));
             }
         }
+        along += apart;
+        if constexpr (kTurnedRows)
+            if (turned && (++step & 15) == 0 && (step >> 1) < o.rbs) enter_group();
     };
+    // a wavefront whose units are all past the last fetches for the others only
+    const bool idle = tile.n * F + wn * T >= q.b.rbs || (!kTurnedRows && tile.m * F + wm * T >= q.a.rbs);
     floatx16 sum[T][T], rest[T][T];
 #pragma unroll
     for (int j = 0; j < T; ++j)
@@ -76,6 +86,7 @@ __global__ __launch_bounds__(256, Epi::kPast ? 2 : 3) void wide_split_kernel(Wid
         if (s + kStages - 2 < steps) wait_and_meet<(kStages - 2) * kLoads>();
         else wait_and_meet<0>();
         if (s + kStages - 1 < steps) fetch(s + kStages - 1);      // into the place that every wavefront has read before this meeting
+        if (idle) continue;
         const uint4 *slab = &ring[s % kStages * (kUnits * 64)], *units = slab + lane, *weights = slab + (s & 1 ? weights_at[1] : weights_at[0]);
         uint4 a[3][T], b[3][T];
 #pragma unroll

@@ -16,7 +16,8 @@ def small(n, F_in, F_out, sides):
     weights = 3 * 2 * up(F_in, 32) * (sides * up(F_out, 32) + 32)
     sums = (4096 + 64) * sides * up(F_out, 32) * 4
     shares = 512 * sides * F_in * F_out * 4
-    return weights + sums + shares + 8 * 256
+    planes = 9 * 65536          # of three operands, each rounded up to 64 KB
+    return weights + sums + shares + planes + 8 * 256
 
 
 @pytest.mark.parametrize("n,F_in,F_out", SIZES)
