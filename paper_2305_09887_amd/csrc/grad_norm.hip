@@ -3,8 +3,10 @@
 // A list of tensors goes to the kernels as their arguments, kListed at a time: no table in device memory, no copy of one, nothing that a captured graph
 // could find changed.  A tensor is cut into chunks, blocks take every grid-th chunk of the list and keep its squares' sum in 64 bits: the squares of
 // fp32 values are exact there and neither overflow nor vanish, and the vector units have the time (two instructions for four bytes).  Sums are joined in a
-// fixed order; clipping's second kernel does so in every block, and takes the chunks from the last to the first, since the last were just read and are in
-// the cache.  Bound by memory: a gradient is read once, and once more and written where it is clipped.
+// fixed order; clipping's second kernel does so in every block, and takes a list's chunks from the last to the first, since the last were just read and a
+// cache may still have them.  Lists go first to last both times: of 400 M bf16 values in three the second pass reads from memory what the first did (counted: 828 MB
+// and 817).  Bound by memory: a gradient is read once, and once more and written where it is clipped.  400 M bf16 values in one tensor 443 us, 5.4 TB/s; 200 tensors
+// that begin at whole lines, two lists, 483; 290 of odd lengths, three lists, whose pieces of 1 KB lie across lines, 530.
 #include "kernels.hpp"
 
 #include <algorithm>
