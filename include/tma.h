@@ -749,8 +749,8 @@ int tma_dropout_bwd(int64_t n, int32_t F, const void *dY, int64_t ldy, double p,
  * of up to 64 rows take them as they are: a row's result can change by that
  * rounding where the list grows past 64), sums are fp32, results are rounded
  * once; gradients of weights are fp32, from gradients of pre-activations in two bf16 parts (17 bits); dX takes the first of
- * these parts alone.  SiLU and GELU: fp32 functions within 2^-20 of z; where they are small, within 2^-20 + 2^-24 |z| and
- * 2^-20 + 2^-24 z^2 of themselves.  TMA_F32: products of three bf16 parts of each value, which hold its 24
+ * these parts alone.  SiLU and GELU: fp32 functions within 2^-20 of z; where they are small, within 2^-20 + 1.25 2^-24 |z| and
+ * 2^-20 + 1.125 2^-24 z^2 of themselves.  TMA_F32: products of three bf16 parts of each value, which hold its 24
  * bits; absolute error of a part 2^-126, results within 2^-7 of fp32's largest may be infinite.  A NaN or an infinity in an input makes
  * results that it reaches non-finite (NaN where fp32 arithmetic may give an
  * infinity).  The ReLU of a NaN is 0 and closed.  Widths up to 65536.  What lies in a row's padding has no
